@@ -452,6 +452,81 @@ typedef struct {
 tc_status tc_stats(tc_ctx *ctx, const tc_model *model, const tc_codebook *cb, const tc_tensor *x,
                    tc_stats_out *out, void *cuda_stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Layers between coded maps: products of 8-bit matrices, and residual norms.
+ *
+ * A feature map that tc_decode returns goes through the next layer before tc_encode codes it again (Fig. 2); the paper's
+ * networks run those layers on 8-bit weights and activations (Table C.1).  The calls below are such layers on the pixels' C-vectors: a
+ * 1 x 1 convolution is a product of the pixels' rows and the weights', and a list of T tokens is a
+ * tensor of shape (T, C, 1, 1).
+ *
+ * tc_blocks: a matrix of e4m3 codes (8-bit floating point: 4 bits of exponent, 3 of mantissa, largest value 448) with a scale for
+ * each block of 128 consecutive codes of a row, or (`square`) for each tile of 128 x 128; a value is code * scale.
+ *   codes   DEVICE [rows][ld] bytes, 16-byte aligned; ld >= cols, a multiple of 16.  Bytes behind a row's `cols` are never used.
+ *   scales  DEVICE float, 16-byte aligned: [ceil(cols / 128)][rows rounded up to a multiple of 128], the floats behind `rows`
+ *           never used; square: [ceil(cols / 128)][ceil(rows / 128)].
+ * ------------------------------------------------------------------------------------- */
+typedef struct {
+    void *codes;
+    float *scales;
+    int64_t ld;
+    int32_t rows, cols;
+    int32_t square;
+} tc_blocks;
+
+/* Codes of `x`, by its pixels ([P][C], what a product over the channels reads), by its channels ([C][P], what the gradient of a
+ * weight reads), or both in one pass; either may be NULL.  `x` is a map of activations, or a weight: (C_out, C_in, 1, 1).
+ *     scale = max|x| / 448 over the block (max|x| at least 2^-100), code = the e4m3 value nearest to x / scale (ties to even).
+ * The scale is the fp32 product of max|x| and fl(1/448), the code that of the fp32 product of x and fl(1/scale).  A block that holds an
+ * infinity or a NaN gets a NaN for its scale: so is everything computed from it.  Both `square` fields must be equal.
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 - 256 pixels, more than 2^22 channels), CUDA. */
+tc_status tc_quantize_blocks(tc_ctx *ctx, const tc_tensor *x, const tc_blocks *pixels, const tc_blocks *channels, void *cuda_stream);
+
+/* out[p][o] = act(bias[o] + sum_k a[p][k] b[o][k]), a [P][K] and b [O][K] block matrices (square or not, each), `out` a tensor of P pixels and
+ * O channels, fp32 or bf16; `bias` DEVICE [O] or NULL; act = max(., 0) if `relu`, else none.  Codes are multiplied exactly, each block of 128 is
+ * summed by the tensor cores in fp32, scaled, and added in fp32 in ascending order; sums of few, long rows are cut into parts that are added in
+ * their order, so a call's result depends on its sizes, types and alignment, not on timing.
+ *   layer            a = codes of x by pixels,  b = codes of W (C_out, C_in) by pixels
+ *   gradient to x    a = codes of dy by pixels, b = codes of W by channels
+ *   gradient to W    a = codes of dy by channels, b = codes of x by channels, out (C_out, C_in, 1, 1)
+ * With K = 0 the sums are empty.  `out` must not overlap the operands.  Partial sums live in the context's arena (where that memory cannot be had, each
+ * sum is taken in one part).  May be captured into a graph.
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 - 256 rows, more than 2^30 tiles), CUDA; TIMEOUT by tc_get_status. */
+tc_status tc_matmul_blocks(tc_ctx *ctx, const tc_blocks *a, const tc_blocks *b, const float *bias, int32_t relu, const tc_tensor *out,
+                           void *cuda_stream);
+
+/* The norm after a layer, its gate and scale, the residual sum, and the norm before the next layer, over each pixel's channels:
+ *     n = y / sqrt(mean_c y^2 + eps), u = n * after (no `after`: u = y);   s = h + scale * gate * u;
+ *     x = s / sqrt(mean_c s^2 + eps) * before
+ * Statistics, sums and products in fp32; s and x are rounded once, x is computed from the s that is not rounded yet. */
+typedef struct {
+    const tc_tensor *y;        /* layer's output; NULL: s = h, which is not written                     */
+    const float *after;        /* DEVICE [C]; NULL: no norm after the layer                             */
+    const float *gate;         /* DEVICE [C]; NULL: none                                                */
+    const tc_tensor *gate_map; /* a gate for each value, of y's shape and type, instead of `gate`; or NULL */
+    const float *scale;        /* DEVICE [1]; NULL: 1                                                   */
+    const float *before;       /* DEVICE [C]; NULL: no x                                                */
+    float eps;                 /* >= 0                                                                  */
+} tc_norm_params;
+
+/* `sum` receives s (required with y), `x` and `codes` (block codes by pixels, not square) receive x; either or both, with `before`.
+ * All tensors have the shape and type of `h`; outputs overlap neither inputs nor each other.  May be captured into a graph.
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 16384 channels, more than 2^31 - 256 pixels), CUDA. */
+tc_status tc_residual_norms(tc_ctx *ctx, const tc_tensor *h, const tc_norm_params *params, const tc_tensor *sum, const tc_tensor *x,
+                            const tc_blocks *codes, void *cuda_stream);
+
+/* Gradients of tc_residual_norms at the sum `s` it wrote (y = NULL: at h), from those of x (`dx`, NULL exactly without `before`; the same
+ * whether x left as a tensor or as codes) and of s (`ds`, NULL = zero).  dh always; dy where y is given; the others where wanted, each only where
+ * its input is given (scale's may be asked for with y).  Gradients of vectors are sums over all pixels, in fp32, in an order that does not depend on
+ * timing.  Conventions and errors as above. */
+typedef struct {
+    const tc_tensor *dh, *dy;
+    const tc_tensor *dgate_map;                  /* required with gate_map               */
+    float *dafter, *dgate, *dscale, *dbefore;    /* DEVICE [C], [C], [1], [C], or NULL   */
+} tc_norm_grads;
+tc_status tc_residual_norms_backward(tc_ctx *ctx, const tc_tensor *s, const tc_norm_params *params, const tc_tensor *dx, const tc_tensor *ds,
+                                     const tc_norm_grads *out, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

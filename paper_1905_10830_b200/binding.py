@@ -4,6 +4,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -59,6 +60,21 @@ class _DebugOut(C.Structure):
     _fields_ = [("coefficients", C.c_void_p), ("symbols", C.c_void_p)]
 
 
+class _Blocks(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("ld", C.c_int64), ("rows", C.c_int32), ("cols", C.c_int32),
+                ("square", C.c_int32)]
+
+
+class _NormParams(C.Structure):
+    _fields_ = [("y", C.POINTER(_Tensor)), ("after", C.c_void_p), ("gate", C.c_void_p), ("gate_map", C.POINTER(_Tensor)),
+                ("scale", C.c_void_p), ("before", C.c_void_p), ("eps", C.c_float)]
+
+
+class _NormGrads(C.Structure):
+    _fields_ = [("dh", C.POINTER(_Tensor)), ("dy", C.POINTER(_Tensor)), ("dgate_map", C.POINTER(_Tensor)), ("dafter", C.c_void_p),
+                ("dgate", C.c_void_p), ("dscale", C.c_void_p), ("dbefore", C.c_void_p)]
+
+
 class _StatsOut(C.Structure):
     _fields_ = [("groups", C.c_int32), ("hist", C.c_void_p), ("entropy", C.c_double),
                 ("mean_length", C.c_double), ("mse", C.c_double), ("clamped_fraction", C.c_double),
@@ -70,7 +86,8 @@ EXPORTS = ["tc_create", "tc_destroy", "tc_status_string", "tc_get_status", "tc_f
            "tc_codebook_import", "tc_codebook_export", "tc_codebook_free",
            "tc_host_huffman_lengths", "tc_host_eigh", "tc_device_eigh", "tc_encode_bound", "tc_encode", "tc_encode_noalloc", "tc_decode", "tc_encode_many", "tc_decode_many", "tc_roundtrip_host",
            "tc_stats", "tc_fit_state_create", "tc_fit_state_free", "tc_fit_state_update", "tc_fit_state_export",
-           "tc_fit_state_import", "tc_fit_state_finish", "tc_fold_forward", "tc_fold_inverse"]
+           "tc_fit_state_import", "tc_fit_state_finish", "tc_fold_forward", "tc_fold_inverse",
+           "tc_quantize_blocks", "tc_matmul_blocks", "tc_residual_norms", "tc_residual_norms_backward"]
 
 _lib = None
 
@@ -131,6 +148,10 @@ def load_library() -> C.CDLL:
         lib.tc_fit_state_finish.argtypes = [vp, vp, P(_Tensor), P(_FitParams), P(vp), vp]
         lib.tc_fold_forward.argtypes = [vp, vp, vp, vp, vp, C.c_int64, vp, vp]
         lib.tc_fold_inverse.argtypes = [vp, vp, vp, i32, i32, vp, vp]
+        lib.tc_quantize_blocks.argtypes = [vp, P(_Tensor), P(_Blocks), P(_Blocks), vp]
+        lib.tc_matmul_blocks.argtypes = [vp, P(_Blocks), P(_Blocks), vp, i32, P(_Tensor), vp]
+        lib.tc_residual_norms.argtypes = [vp, P(_Tensor), P(_NormParams), P(_Tensor), P(_Tensor), P(_Blocks), vp]
+        lib.tc_residual_norms_backward.argtypes = [vp, P(_Tensor), P(_NormParams), P(_Tensor), P(_Tensor), P(_NormGrads), vp]
         _lib = lib
     return _lib
 
@@ -590,3 +611,166 @@ def tc_stats(ctx: Context, model: Model, cb: Codebook | None, x: torch.Tensor, *
     _check(load_library().tc_stats(ctx.ptr, model.ptr, cb.ptr if cb is not None else None, C.byref(t), C.byref(s),
                                    _stream_ptr(ctx.device)), "tc_stats")
     return Stats(s.entropy, s.mean_length, s.mse, s.clamped_fraction, s.zero_fraction, s.energy_ratio_90, hist)
+
+
+# ---- layers between coded maps ---------------------------------------------------------------
+
+@dataclass
+class Blocks:
+    """A matrix of e4m3 codes with a scale for each block of 128 codes of a row, or (`square`) for each tile of 128 x 128:
+    a value is code * scale (tc_blocks in include/tc.h has the layout)."""
+    codes: torch.Tensor        # float8_e4m3fn [rows, cols rounded up to a multiple of 16]
+    scales: torch.Tensor       # float32 [blocks of a row, rows rounded up to a multiple of 128], square: [blocks, blocks]
+    cols: int
+    square: bool = False
+
+    @property
+    def rows(self) -> int:
+        return self.codes.shape[0]
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, square: bool = False, device="cuda") -> "Blocks":
+        tall = -(-rows // 128)
+        return cls(torch.empty((rows, -(-cols // 16) * 16), dtype=torch.float8_e4m3fn, device=device),
+                   torch.empty((-(-cols // 128), tall if square else tall * 128), dtype=torch.float32, device=device), cols, square)
+
+    def dequantize(self) -> torch.Tensor:
+        """The values the codes stand for, float32 [rows, cols] (for inspection; no product reads them)."""
+        scales = self.scales.repeat_interleave(128, 1) if self.square else self.scales
+        return self.codes[:, :self.cols].float() * scales[:, :self.rows].t().repeat_interleave(128, 1)[:, :self.cols]
+
+
+def _on_device(ctx: Context, *tensors) -> None:
+    for x in tensors:
+        if x is not None and x.get_device() != ctx.device:
+            raise ValueError(f"expected tensors on the context's device, cuda:{ctx.device}")
+
+
+def _blocks(ctx: Context, b: Blocks) -> _Blocks:
+    codes, scales = b.codes, b.scales
+    _on_device(ctx, codes, scales)
+    if codes.dim() != 2 or scales.dim() != 2 or codes.dtype != torch.float8_e4m3fn or scales.dtype != torch.float32 or \
+            not codes.is_contiguous() or not scales.is_contiguous():
+        raise ValueError("block matrices have contiguous float8_e4m3fn codes [rows, ld] and float32 scales")
+    rows, ld = codes.shape
+    tall = (rows + 127) // 128
+    if not 0 <= b.cols <= ld or scales.shape != ((b.cols + 127) // 128, tall if b.square else tall * 128):
+        raise ValueError("block matrix: codes, scales and cols do not belong together")
+    return _Blocks(codes.data_ptr(), scales.data_ptr(), ld, rows, b.cols, b.square)
+
+
+def _vector(ctx: Context, v, n: int, name: str) -> int | None:
+    if v is None:
+        return None
+    if v.dtype != torch.float32 or v.numel() != n or not v.is_contiguous() or v.get_device() != ctx.device:
+        raise ValueError(f"{name}: expected {n} contiguous float32 values on the context's device")
+    return v.data_ptr()
+
+
+def tc_quantize_blocks(ctx: Context, x: torch.Tensor, *, rows: str = "pixels", square: bool = False, out=None):
+    """Codes of `x` (N, C, H, W): a row for each pixel ("pixels", blocks along the channels), for each channel ("channels",
+    blocks along the pixels), or "both" as a pair.  `out` reuses the Blocks of an earlier call."""
+    if rows not in ("pixels", "channels", "both"):
+        raise ValueError('rows: "pixels", "channels" or "both"')
+    t = _tensor(x)
+    _on_device(ctx, x)
+    p = t.n * t.h * t.w
+    shapes = {"pixels": [(p, t.c)], "channels": [(t.c, p)], "both": [(p, t.c), (t.c, p)]}[rows]
+    if out is None:
+        got = [Blocks.empty(r, c, square, x.device) for r, c in shapes]
+    else:
+        got = list(out) if rows == "both" else [out]
+        if len(got) != len(shapes) or any(bool(b.square) != bool(square) for b in got):
+            raise ValueError("out: Blocks as this call returns them")
+    made = [_blocks(ctx, b) for b in got]
+    refs = [C.byref(b) for b in made]
+    pixels, channels = (refs[0], refs[1]) if rows == "both" else (refs[0], None) if rows == "pixels" else (None, refs[0])
+    _check(load_library().tc_quantize_blocks(ctx.ptr, C.byref(t), pixels, channels, _tensor_stream(ctx.device)), "tc_quantize_blocks")
+    return tuple(got) if rows == "both" else got[0]
+
+
+def tc_matmul_blocks(ctx: Context, a: Blocks, b: Blocks, *, shape=None, dtype=torch.bfloat16, bias: torch.Tensor | None = None,
+                     relu: bool = False, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Product of a's rows (the output's pixels) and b's rows (its channels), (N, O, H, W) with `shape` = (N, H, W), by default
+    (rows of a, 1, 1); `bias` [O], `relu` on the result."""
+    ma, mb = _blocks(ctx, a), _blocks(ctx, b)
+    if out is None:
+        n, h, w = (ma.rows, 1, 1) if shape is None else shape
+        out = torch.empty((n, mb.rows, h, w), dtype=dtype, device=a.codes.device)
+    t = _tensor(out)
+    _on_device(ctx, out)
+    _check(load_library().tc_matmul_blocks(ctx.ptr, C.byref(ma), C.byref(mb), _vector(ctx, bias, mb.rows, "bias"), relu, C.byref(t),
+                                           _tensor_stream(ctx.device)), "tc_matmul_blocks")
+    return out
+
+
+def _norm_params(ctx: Context, h: torch.Tensor, y, after, gate, scale, before, eps):
+    """The C structure, and what it points to."""
+    _on_device(ctx, h, y)
+    c = h.shape[1]
+    ty = None if y is None else _tensor(y)
+    tg = None
+    if gate is not None and gate.dim() == 4:
+        _on_device(ctx, gate)
+        tg = _tensor(gate)
+    p = _NormParams(None if ty is None else C.pointer(ty), _vector(ctx, after, c, "after"), None if tg is not None else _vector(ctx, gate, c, "gate"),
+                    None if tg is None else C.pointer(tg), _vector(ctx, scale, 1, "scale"), _vector(ctx, before, c, "before"), eps)
+    return p, (ty, tg)
+
+
+def tc_residual_norms(ctx: Context, h: torch.Tensor, y: torch.Tensor | None = None, *, after: torch.Tensor | None = None,
+                      gate: torch.Tensor | None = None, scale: torch.Tensor | None = None, before: torch.Tensor | None = None,
+                      eps: float = 1e-6, blocks: bool = False, sum_out: torch.Tensor | None = None, out=None):
+    """(s, x): s = h + scale * gate * norm(y) * after, x = norm(s) * before, norms over the channels of each pixel.  x is a
+    tensor like h, or with `blocks` its codes by pixels; without `before` it is None.  Without `y` s is h itself.  `gate` is
+    [C], or a tensor like y."""
+    th = _tensor(h)
+    p, keep = _norm_params(ctx, h, y, after, gate, scale, before, eps)
+    s = h if y is None else torch.empty_like(h) if sum_out is None else sum_out
+    ts = None if y is None else _tensor(s)
+    x, tx, bx = None, None, None
+    if before is not None:
+        if blocks:
+            x = Blocks.empty(th.n * th.h * th.w, th.c, False, h.device) if out is None else out
+            bx = _blocks(ctx, x)
+        else:
+            x = torch.empty_like(h) if out is None else out
+            tx = _tensor(x)
+            _on_device(ctx, x)
+    _on_device(ctx, s)
+    ref = lambda v: None if v is None else C.byref(v)                            # noqa: E731
+    _check(load_library().tc_residual_norms(ctx.ptr, C.byref(th), C.byref(p), ref(ts), ref(tx), ref(bx), _tensor_stream(ctx.device)),
+           "tc_residual_norms")
+    del keep
+    return s, x
+
+
+class NormGrads(NamedTuple):
+    """Gradients of tc_residual_norms by its arguments' names; None where an argument was not given."""
+    h: torch.Tensor
+    y: torch.Tensor | None
+    after: torch.Tensor | None
+    gate: torch.Tensor | None
+    scale: torch.Tensor | None
+    before: torch.Tensor | None
+
+
+def tc_residual_norms_backward(ctx: Context, s: torch.Tensor, y: torch.Tensor | None, dx: torch.Tensor | None, ds: torch.Tensor | None, *,
+                               after: torch.Tensor | None = None, gate: torch.Tensor | None = None, scale: torch.Tensor | None = None,
+                               before: torch.Tensor | None = None, eps: float = 1e-6) -> NormGrads:
+    """Gradients at the sum `s` that tc_residual_norms returned, from the gradients `dx` of x (None without `before`) and `ds` of s
+    (None: zero)."""
+    t = _tensor(s)
+    p, keep = _norm_params(ctx, s, y, after, gate, scale, before, eps)
+    _on_device(ctx, dx, ds)
+    gate_map = gate is not None and gate.dim() == 4
+    like = lambda v: None if v is None else torch.empty_like(v)                  # noqa: E731
+    g = NormGrads(torch.empty_like(s), like(y), like(after), like(gate), like(scale), like(before))
+    tensors = [None if v is None else _tensor(v) for v in (g.h, g.y, g.gate if gate_map else None, dx, ds)]
+    ptr = [None if v is None else C.pointer(v) for v in tensors]
+    data = lambda v: None if v is None else v.data_ptr()                         # noqa: E731
+    out = _NormGrads(ptr[0], ptr[1], ptr[2], data(g.after), None if gate_map else data(g.gate), data(g.scale), data(g.before))
+    _check(load_library().tc_residual_norms_backward(ctx.ptr, C.byref(t), C.byref(p), ptr[3], ptr[4], C.byref(out),
+                                                     _tensor_stream(ctx.device)), "tc_residual_norms_backward")
+    del keep
+    return g

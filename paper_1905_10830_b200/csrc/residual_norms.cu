@@ -1,0 +1,646 @@
+// tc_residual_norms and its gradient: the norm after a block, its gate and scale, the residual sum and the norm before the
+// next block, in one pass over the maps.
+//
+//   q = 1 / sqrt(mean_c y^2 + eps), n = y q, u = n after;  s = h + scale gate u;  r = 1 / sqrt(mean_c s^2 + eps), x = s r before
+//
+// and, with t = dx before, m = mean_c t s, D = ds + r t - s r^3 m, g = gate, v = scale D g after:
+//
+//   dh = D;  dy = q (v - n mean_c v n);  dbefore = sum_p dx s r;  dafter = scale sum_p D g n;  dgate = scale D u;  dscale = sum D g u
+//
+// Bound by the bytes of the maps: each is read once and written once.  The gradient's mean_c v n is a sum of D's three parts, so
+// that all sums over a pixel's channels -- s s, t s, y y, and ds, t and s times g after y -- are taken together and
+// a pixel waits for one reduction.  All sums are fp32, in an order that does not depend on the launch's timing; sums over the pixels are first
+// taken by block, and a second kernel adds the blocks' sums in their order.
+#include "block_codes.cuh"
+#include "tc_internal.h"
+
+namespace {
+
+using namespace tcdev;
+using namespace blk;
+
+__device__ __forceinline__ float inv_sqrt(float v) { return __frcp_rn(__fsqrt_rn(v)); }
+
+// ---- single pixels (H W = 1): a pixel's channels are a row in memory ------------------------------
+// kWarps warps a row, kV chunks of eight channels a thread; rows of one warp share a block of eight.
+template <typename T, int kV>
+struct RowChunks {
+    Raw8<T> raw[kV];
+};
+template <int kThreadsRow>
+__device__ __forceinline__ int chunk_at(int t, int i) { return (i * kThreadsRow + t) * 8; }
+
+template <typename T>
+__device__ __forceinline__ void load_chunk(Raw8<T> &r, const T *row, int k, int c, bool vec)
+{
+    if (k >= c) { zero8(r); return; }
+    if (vec) load8(r, row + k);
+    else load8(r, row + k, min(8, c - k));
+}
+__device__ __forceinline__ void load_vector(float (&f)[8], const float *v, int k, int c, bool vec)
+{
+    if (vec && k < c) {
+        const float4 a = reinterpret_cast<const float4 *>(v + k)[0], b = reinterpret_cast<const float4 *>(v + k)[1];
+        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = k + j < c ? v[k + j] : 0.f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_chunk(T *row, const float (&f)[8], int k, int c, bool vec)
+{
+    if (k >= c) return;
+    if (vec) store8(row + k, f);
+    else store8(row + k, f, min(8, c - k));
+}
+
+template <int kWarps>
+__device__ __forceinline__ float row_sum(float v, float *s_part)
+{
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    if constexpr (kWarps > 1) {
+        if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) v += s_part[w];
+    }
+    return v;
+}
+
+template <typename T, int kWarps, int kV>
+__global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32) norm_rows_kernel(NormArgs a)
+{
+    constexpr int kThreadsRow = kWarps * 32;
+    __shared__ float s_part[2][kWarps];
+    chain_next();
+    chain_wait();
+    const int t = threadIdx.x % kThreadsRow;
+    const long long row = kWarps == 1 ? (long long)blockIdx.x * 8 + (threadIdx.x >> 5) : (long long)blockIdx.x;
+    if (row >= a.pixels) return;                              // whole warps; with more than one a row, whole blocks
+    const bool vec = a.vec != 0;
+    const long long base = row * a.c;
+    Raw8<T> rh[kV], ry[kV], rg[kV];
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+        const int k = chunk_at<kThreadsRow>(t, i);
+        load_chunk(rh[i], (const T *)a.h + base, k, a.c, vec);
+        if (a.y) load_chunk(ry[i], (const T *)a.y + base, k, a.c, vec);
+        if (a.gate_map) load_chunk(rg[i], (const T *)a.gate_map + base, k, a.c, vec);
+    }
+    float s[kV][8];
+#pragma unroll
+    for (int i = 0; i < kV; ++i) values8(rh[i], s[i]);
+    const float inv_c = 1.0f / (float)a.c;
+    if (a.y) {
+        float q = 1.f;
+        if (a.after) {
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < kV; ++i) {
+                float y[8];
+                values8(ry[i], y);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum = fmaf(y[j], y[j], sum);
+            }
+            q = inv_sqrt(fmaf(row_sum<kWarps>(sum, s_part[0]), inv_c, a.eps));
+        }
+        const float scale = a.scale ? *a.scale : 1.f;
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const int k = chunk_at<kThreadsRow>(t, i);
+            float u[8];
+            values8(ry[i], u);
+            if (a.after) {
+                float w[8];
+                load_vector(w, a.after, k, a.c, vec);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) u[j] = u[j] * q * w[j];
+            }
+            if (a.gate_map || a.gate) {
+                float g[8];
+                if (a.gate_map) values8(rg[i], g);
+                else load_vector(g, a.gate, k, a.c, vec);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) u[j] *= g[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[i][j] = fmaf(scale, u[j], s[i][j]);
+            store_chunk((T *)a.sum + base, s[i], k, a.c, vec);
+        }
+    }
+    if (!a.before) return;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum = fmaf(s[i][j], s[i][j], sum);
+    const float r = inv_sqrt(fmaf(row_sum<kWarps>(sum, s_part[1]), inv_c, a.eps));
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+        const int k = chunk_at<kThreadsRow>(t, i);
+        float w[8];
+        load_vector(w, a.before, k, a.c, vec);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = s[i][j] * r * w[j];
+        if (a.x) store_chunk((T *)a.x + base, w, k, a.c, vec);
+        if (a.codes.codes) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = max(m, abs_bits(w[j]));
+            const float scale = scale_of(max16(m));           // 16 threads' chunks are a block
+            if (k < a.c) {
+                *reinterpret_cast<uint2 *>(a.codes.codes + row * a.codes.ld + k) = codes8(w, __frcp_rn(scale));
+                if ((t & 15) == 0) a.codes.scales[(long long)(k / kBlock) * a.codes.scale_ld + row] = scale;
+            }
+        }
+    }
+}
+
+// ---- maps: a pixel's channels lie H W apart ------------------------------------------------------
+// 32 pixels a block, a lane for each; of each block of 128 channels a warp takes 16.  The maps are read again for each of the
+// passes (sums of y, of s, the output), from L1 and L2.
+template <typename T>
+__global__ void __launch_bounds__(256) norm_maps_kernel(NormArgs a)
+{
+    __shared__ float s_part[2][8][32];
+    __shared__ uint32_t s_max[2][8][32];
+    chain_next();
+    chain_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long p = (long long)blockIdx.x * 32 + lane;
+    const bool ok = p < a.pixels;
+    const long long img = p / a.hw, base = img * a.c * (long long)a.hw + (p - img * a.hw);
+    const T *h = (const T *)a.h + base, *y = a.y ? (const T *)a.y + base : nullptr, *gm = a.gate_map ? (const T *)a.gate_map + base : nullptr;
+    const float scale = a.y && a.scale ? *a.scale : 1.f, inv_c = 1.0f / (float)a.c;
+    auto over = [&](float (&part)[8][32], float v) {
+        part[warp][lane] = v;
+        __syncthreads();
+        v = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) v += part[w][lane];
+        return v;
+    };
+    float q = 1.f;
+    auto sum_at = [&](int ch) {
+        const long long at = (long long)ch * a.hw;
+        float s = load1(h + at);
+        if (y) {
+            float u = load1(y + at) * q;
+            if (a.after) u *= a.after[ch];
+            if (gm) u *= load1(gm + at);
+            else if (a.gate) u *= a.gate[ch];
+            s = fmaf(scale, u, s);
+        }
+        return s;
+    };
+    if (y && a.after) {
+        float sum = 0.f;
+        for (int c0 = warp * 16; c0 < a.c; c0 += kBlock) {
+            float v[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = ok && c0 + j < a.c ? load1(y + (long long)(c0 + j) * a.hw) : 0.f;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sum = fmaf(v[j], v[j], sum);
+        }
+        q = inv_sqrt(fmaf(over(s_part[0], sum), inv_c, a.eps));
+    }
+    float sum = 0.f;
+    for (int c0 = warp * 16; c0 < a.c; c0 += kBlock) {
+        float v[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = ok && c0 + j < a.c ? sum_at(c0 + j) : 0.f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            sum = fmaf(v[j], v[j], sum);
+            if (y && ok && c0 + j < a.c) store1((T *)a.sum + base + (long long)(c0 + j) * a.hw, v[j]);
+        }
+    }
+    if (!a.before) return;
+    const float r = inv_sqrt(fmaf(over(s_part[1], sum), inv_c, a.eps));
+    int turn = 0;
+    for (int b0 = 0; b0 < a.c; b0 += kBlock, turn ^= 1) {
+        const int c0 = b0 + warp * 16;
+        float v[16];
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            v[j] = 0.f;
+            if (ok && c0 + j < a.c) v[j] = sum_at(c0 + j) * r * a.before[c0 + j];
+            m = max(m, abs_bits(v[j]));
+        }
+        if (a.x) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (ok && c0 + j < a.c) store1((T *)a.x + base + (long long)(c0 + j) * a.hw, v[j]);
+        }
+        if (a.codes.codes) {
+            s_max[turn][warp][lane] = m;
+            __syncthreads();                                  // (the other half's readers are past this barrier before it is written again)
+#pragma unroll
+            for (int w = 0; w < 8; ++w) m = max(m, s_max[turn][w][lane]);
+            const float sc = scale_of(m), inv = __frcp_rn(sc);
+            if (ok && c0 < a.c)
+                *reinterpret_cast<uint4 *>(a.codes.codes + p * a.codes.ld + c0) = make_uint4(
+                    codes4(v[0], v[1], v[2], v[3], inv), codes4(v[4], v[5], v[6], v[7], inv), codes4(v[8], v[9], v[10], v[11], inv), codes4(v[12], v[13], v[14], v[15], inv));
+            if (ok && warp == 0) a.codes.scales[(long long)(b0 / kBlock) * a.codes.scale_ld + p] = sc;
+        }
+    }
+}
+
+// ---- gradient ----------------------------------------------------------------------------------
+constexpr int kSums = 6;        // s s, t s, y y, and ds, t, s times gate after y
+
+// What a pixel's sums give.
+struct PixelFactors {
+    float r, r3m, q, mean;      // D = ds + r t - r3m s;  dy = q (v - y q mean)
+};
+__device__ __forceinline__ PixelFactors pixel_factors(const float (&sums)[kSums], const NormGradArgs &a, float scale)
+{
+    const float inv_c = 1.0f / (float)a.c;
+    PixelFactors f;
+    f.r = a.before ? inv_sqrt(fmaf(sums[0], inv_c, a.eps)) : 0.f;
+    f.r3m = f.r * f.r * f.r * (sums[1] * inv_c);
+    f.q = a.after ? inv_sqrt(fmaf(sums[2], inv_c, a.eps)) : 1.f;
+    const float dot = fmaf(-f.r3m, sums[5], fmaf(f.r, sums[4], sums[3]));           // sum D gate after y
+    f.mean = a.after ? scale * f.q * dot * inv_c : 0.f;
+    return f;
+}
+
+// Sums of eight values over the warp at once: afterwards lane l holds that of value l / 4.
+__device__ __forceinline__ float sum8_over_warp(const float (&v)[8], int lane)
+{
+    float a[4], b[2];
+    const bool h16 = lane & 16, h8 = lane & 8, h4 = lane & 4;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float keep = h16 ? v[4 + j] : v[j], give = h16 ? v[j] : v[4 + j];
+        a[j] = keep + __shfl_xor_sync(0xffffffffu, give, 16);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const float keep = h8 ? a[2 + j] : a[j], give = h8 ? a[j] : a[2 + j];
+        b[j] = keep + __shfl_xor_sync(0xffffffffu, give, 8);
+    }
+    float c = (h4 ? b[1] : b[0]) + __shfl_xor_sync(0xffffffffu, h4 ? b[0] : b[1], 4);
+    c += __shfl_xor_sync(0xffffffffu, c, 2);
+    c += __shfl_xor_sync(0xffffffffu, c, 1);
+    return c;
+}
+
+// The row's six sums in every thread.
+template <int kWarps>
+__device__ __forceinline__ void row_sums(float (&v)[8], float (*s_part)[8])
+{
+    const int lane = threadIdx.x & 31;
+    float mine = sum8_over_warp(v, lane);
+    if constexpr (kWarps > 1) {
+        if ((lane & 3) == 0) s_part[threadIdx.x >> 5][lane >> 2] = mine;
+        __syncthreads();
+        mine = 0.f;                                           // lane l: value l / 4, every fourth warp from l % 4 on
+#pragma unroll
+        for (int w = 0; w < (kWarps + 3) / 4; ++w)
+            if (kWarps % 4 == 0 || 4 * w + (lane & 3) < kWarps) mine += s_part[4 * w + (lane & 3)][lane >> 2];
+        mine += __shfl_xor_sync(0xffffffffu, mine, 1);
+        mine += __shfl_xor_sync(0xffffffffu, mine, 2);
+    }
+#pragma unroll
+    for (int i = 0; i < kSums; ++i) v[i] = __shfl_sync(0xffffffffu, mine, 4 * i);
+}
+
+template <typename T, int kWarps, int kV>
+__global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32, kWarps == 1 ? 2 : (kWarps >= 16 ? 1 : 16 / kWarps)) norm_rows_grad_kernel(NormGradArgs a)
+{
+    constexpr int kThreadsRow = kWarps * 32, kRows = kWarps == 1 ? 8 : 1;
+    extern __shared__ float s_dyn[];                          // rows of one warp: [8][2][256 kV] sums of the warps
+    __shared__ float s_part[2][kWarps][8];
+    __shared__ float s_scale[32];
+    chain_next();
+    chain_wait();
+    const int t = threadIdx.x % kThreadsRow, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const bool vec = a.vec != 0;
+    const float scale = a.y && a.scale ? *a.scale : 1.f;
+    float sum_y[kV][8], sum_x[kV][8], sum_scale = 0.f;        // D n (times a map's gate);  dx s r
+#pragma unroll
+    for (int i = 0; i < kV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum_y[i][j] = sum_x[i][j] = 0.f;
+    int turn = 0;
+    for (long long row = (long long)blockIdx.x * kRows + (kRows > 1 ? warp : 0); row < a.pixels; row += (long long)gridDim.x * kRows, turn ^= 1) {
+        const long long base = row * a.c;
+        Raw8<T> rs[kV], ry[kV], rx[kV], rd[kV], rg[kV];
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const int k = chunk_at<kThreadsRow>(t, i);
+            zero8(rs[i]); zero8(ry[i]); zero8(rx[i]); zero8(rd[i]);
+            if (a.before) { load_chunk(rs[i], (const T *)a.s + base, k, a.c, vec); load_chunk(rx[i], (const T *)a.dx + base, k, a.c, vec); }
+            if (a.y) load_chunk(ry[i], (const T *)a.y + base, k, a.c, vec);
+            if (a.ds) load_chunk(rd[i], (const T *)a.ds + base, k, a.c, vec);
+            if (a.gate_map) load_chunk(rg[i], (const T *)a.gate_map + base, k, a.c, vec);
+        }
+        // gate times after of a chunk
+        auto factors = [&](int i, int k, float (&g)[8], float (&w)[8]) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[j] = w[j] = 1.f;
+            if (a.gate_map) values8(rg[i], g);
+            else if (a.gate) load_vector(g, a.gate, k, a.c, vec);
+            if (a.after) load_vector(w, a.after, k, a.c, vec);
+        };
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const int k = chunk_at<kThreadsRow>(t, i);
+            float s[8], y[8], dx[8], ds[8], g[8], w[8], b[8];
+            values8(rs[i], s); values8(ry[i], y); values8(rx[i], dx); values8(rd[i], ds);
+            factors(i, k, g, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) b[j] = 0.f;
+            if (a.before) load_vector(b, a.before, k, a.c, vec);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float tt = dx[j] * b[j], gy = g[j] * w[j] * y[j];
+                v[0] = fmaf(s[j], s[j], v[0]);
+                v[1] = fmaf(tt, s[j], v[1]);
+                v[2] = fmaf(y[j], y[j], v[2]);
+                v[3] = fmaf(ds[j], gy, v[3]);
+                v[4] = fmaf(tt, gy, v[4]);
+                v[5] = fmaf(s[j], gy, v[5]);
+            }
+        }
+        row_sums<kWarps>(v, s_part[turn]);
+        const float sums[kSums] = {v[0], v[1], v[2], v[3], v[4], v[5]};
+        const PixelFactors f = pixel_factors(sums, a, scale);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const int k = chunk_at<kThreadsRow>(t, i);
+            float s[8], y[8], dx[8], d[8], g[8], w[8], b[8];
+            values8(rs[i], s); values8(ry[i], y); values8(rx[i], dx); values8(rd[i], d);
+            factors(i, k, g, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) b[j] = 0.f;
+            if (a.before) load_vector(b, a.before, k, a.c, vec);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                d[j] = fmaf(-f.r3m, s[j], fmaf(f.r, dx[j] * b[j], d[j]));
+                sum_x[i][j] = fmaf(dx[j] * f.r, s[j], sum_x[i][j]);
+            }
+            store_chunk((T *)a.dh + base, d, k, a.c, vec);
+            if (a.y) {
+                float dy[8], dg[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float n = y[j] * f.q, dn = d[j] * n, e = dn * g[j] * w[j];
+                    sum_scale += e;
+                    sum_y[i][j] += a.gate ? dn : dn * g[j];
+                    dg[j] = scale * (dn * w[j]);
+                    dy[j] = f.q * fmaf(-n, f.mean, scale * (d[j] * (g[j] * w[j])));
+                }
+                store_chunk((T *)a.dy + base, dy, k, a.c, vec);
+                if (a.gate_map) store_chunk((T *)a.dgate_map + base, dg, k, a.c, vec);
+            }
+        }
+    }
+    // the block's sums
+    float *const part = a.partial + (long long)blockIdx.x * 2 * a.c;
+    if constexpr (kRows > 1) {
+        constexpr int kRow = 256 * kV;
+        float *const mine = s_dyn + warp * 2 * kRow;
+#pragma unroll
+        for (int i = 0; i < kV; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                mine[chunk_at<32>(lane, i) + j] = sum_y[i][j];
+                mine[kRow + chunk_at<32>(lane, i) + j] = sum_x[i][j];
+            }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * kRow; i += 256) {
+            const int k = i % kRow;
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) v += s_dyn[w * 2 * kRow + i];
+            if (k < a.c) part[(i / kRow) * (long long)a.c + k] = v;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const int k = chunk_at<kThreadsRow>(t, i);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (k + j < a.c) {
+                    part[k + j] = sum_y[i][j];
+                    part[a.c + k + j] = sum_x[i][j];
+                }
+        }
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum_scale += __shfl_xor_sync(0xffffffffu, sum_scale, d);
+    if (lane == 0) s_scale[warp] = sum_scale;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float v = 0.f;
+        for (int w = 0; w < (int)(blockDim.x >> 5); ++w) v += s_scale[w];
+        a.partial_scale[blockIdx.x] = v;
+    }
+}
+
+// Maps: 32 pixels at a time, a lane for each; warps take slices of eight channels in turn.  The sums over the pixels are
+// kept in shared memory, each channel's by the one warp that has it.
+template <typename T>
+__global__ void __launch_bounds__(256) norm_maps_grad_kernel(NormGradArgs a)
+{
+    extern __shared__ float s_dyn[];                          // [2][c]
+    __shared__ float s_part[8][kSums][32];
+    __shared__ float s_scale[8];
+    chain_next();
+    chain_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const float scale = a.y && a.scale ? *a.scale : 1.f;
+    for (int i = threadIdx.x; i < 2 * a.c; i += 256) s_dyn[i] = 0.f;
+    float sum_scale = 0.f;
+    const long long groups = (a.pixels + 31) / 32;
+    for (long long group = blockIdx.x; group < groups; group += gridDim.x) {
+        const long long p = group * 32 + lane;
+        const bool ok = p < a.pixels;
+        const long long img = p / a.hw, base = img * a.c * (long long)a.hw + (p - img * a.hw);
+        float sums[kSums] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int c0 = warp * 8; c0 < a.c; c0 += 64) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int ch = c0 + j;
+                if (!ok || ch >= a.c) continue;
+                const long long at = base + (long long)ch * a.hw;
+                const float s = a.before ? load1((const T *)a.s + at) : 0.f, t = a.before ? load1((const T *)a.dx + at) * a.before[ch] : 0.f;
+                const float y = a.y ? load1((const T *)a.y + at) : 0.f, ds = a.ds ? load1((const T *)a.ds + at) : 0.f;
+                float gy = y;
+                if (a.after) gy *= a.after[ch];
+                if (a.gate_map) gy *= load1((const T *)a.gate_map + at);
+                else if (a.gate) gy *= a.gate[ch];
+                sums[0] = fmaf(s, s, sums[0]);
+                sums[1] = fmaf(t, s, sums[1]);
+                sums[2] = fmaf(y, y, sums[2]);
+                sums[3] = fmaf(ds, gy, sums[3]);
+                sums[4] = fmaf(t, gy, sums[4]);
+                sums[5] = fmaf(s, gy, sums[5]);
+            }
+        }
+        __syncthreads();                                      // the last group's readers
+#pragma unroll
+        for (int i = 0; i < kSums; ++i) s_part[warp][i][lane] = sums[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kSums; ++i) {
+            sums[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) sums[i] += s_part[w][i][lane];
+        }
+        const PixelFactors f = pixel_factors(sums, a, scale);
+        for (int c0 = warp * 8; c0 < a.c; c0 += 64) {
+            float sum_y[8], sum_x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int ch = c0 + j;
+                sum_y[j] = sum_x[j] = 0.f;
+                if (!ok || ch >= a.c) continue;
+                const long long at = base + (long long)ch * a.hw;
+                float d = a.ds ? load1((const T *)a.ds + at) : 0.f;
+                if (a.before) {
+                    const float s = load1((const T *)a.s + at), dx = load1((const T *)a.dx + at);
+                    d = fmaf(-f.r3m, s, fmaf(f.r, dx * a.before[ch], d));
+                    sum_x[j] = dx * f.r * s;
+                }
+                store1((T *)a.dh + at, d);
+                if (a.y) {
+                    const float n = load1((const T *)a.y + at) * f.q, w = a.after ? a.after[ch] : 1.f;
+                    const float g = a.gate_map ? load1((const T *)a.gate_map + at) : a.gate ? a.gate[ch] : 1.f, dn = d * n;
+                    sum_scale += dn * g * w;
+                    sum_y[j] = a.gate ? dn : dn * g;
+                    store1((T *)a.dy + at, f.q * fmaf(-n, f.mean, scale * (d * (g * w))));
+                    if (a.gate_map) store1((T *)a.dgate_map + at, scale * (dn * w));
+                }
+            }
+            const float vy = sum8_over_warp(sum_y, lane), vx = sum8_over_warp(sum_x, lane);
+            if ((lane & 3) == 0 && c0 + (lane >> 2) < a.c) {
+                s_dyn[c0 + (lane >> 2)] += vy;
+                s_dyn[a.c + c0 + (lane >> 2)] += vx;
+            }
+        }
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum_scale += __shfl_xor_sync(0xffffffffu, sum_scale, d);
+    if (lane == 0) s_scale[warp] = sum_scale;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * a.c; i += 256) a.partial[(long long)blockIdx.x * 2 * a.c + i] = s_dyn[i];
+    if (threadIdx.x == 0) {
+        float v = 0.f;
+        for (int w = 0; w < 8; ++w) v += s_scale[w];
+        a.partial_scale[blockIdx.x] = v;
+    }
+}
+
+// The blocks' sums, in their order: 32 channels a block, every eighth of the blocks' sums a warp.
+__global__ void __launch_bounds__(256) norm_vectors_kernel(NormGradArgs a, int blocks)
+{
+    __shared__ float s_sum[2][8][32];
+    chain_next();
+    chain_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, ch = blockIdx.x * 32 + lane;
+    float vy = 0.f, vx = 0.f;
+    if (ch < a.c)
+        for (int b = warp; b < blocks; b += 8) {
+            vy += a.partial[(long long)b * 2 * a.c + ch];
+            vx += a.partial[(long long)b * 2 * a.c + a.c + ch];
+        }
+    s_sum[0][warp][lane] = vy;
+    s_sum[1][warp][lane] = vx;
+    __syncthreads();
+    if (warp == 0 && ch < a.c) {
+        vy = vx = 0.f;
+        for (int w = 0; w < 8; ++w) { vy += s_sum[0][w][lane]; vx += s_sum[1][w][lane]; }
+        const float scale = a.y && a.scale ? *a.scale : 1.f;
+        if (a.dafter) a.dafter[ch] = scale * vy * (a.gate ? a.gate[ch] : 1.f);
+        if (a.dgate) a.dgate[ch] = scale * vy * (a.after ? a.after[ch] : 1.f);
+        if (a.dbefore) a.dbefore[ch] = vx;
+    }
+    if (warp == 1 && blockIdx.x == 0 && a.dscale) {
+        float v = 0.f;
+        for (int b = lane; b < blocks; b += 32) v += a.partial_scale[b];
+#pragma unroll
+        for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+        if (lane == 0) *a.dscale = v;
+    }
+}
+
+template <typename T, int kWarps, int kV>
+tc_status launch_norm_rows(const NormArgs &a, cudaStream_t s)
+{
+    const long long blocks = kWarps == 1 ? (a.pixels + 7) / 8 : a.pixels;
+    return launch_first(true, norm_rows_kernel<T, kWarps, kV>, dim3((unsigned int)blocks), dim3(kWarps == 1 ? 256 : kWarps * 32), 0, s, a) == cudaSuccess
+               ? TC_OK : TC_ERR_CUDA;
+}
+
+template <typename T>
+tc_status norms(const NormArgs &a, cudaStream_t s)
+{
+    if (a.hw > 1)
+        return launch_first(true, norm_maps_kernel<T>, dim3((unsigned int)((a.pixels + 31) / 32)), dim3(256), 0, s, a) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
+    if (a.c <= 256) return launch_norm_rows<T, 1, 1>(a, s);
+    if (a.c <= 512) return launch_norm_rows<T, 1, 2>(a, s);
+    if (a.c <= 1024) return launch_norm_rows<T, 4, 1>(a, s);
+    if (a.c <= 2048) return launch_norm_rows<T, 8, 1>(a, s);
+    if (a.c <= 4096) return launch_norm_rows<T, 8, 2>(a, s);
+    if (a.c <= 8192) return launch_norm_rows<T, 16, 2>(a, s);
+    return launch_norm_rows<T, 16, 4>(a, s);
+}
+
+template <typename T, int kWarps, int kV>
+cudaError_t launch_grad_rows(const NormGradArgs &a, int blocks, cudaStream_t s)
+{
+    const size_t smem = kWarps == 1 ? 8 * 2 * 256 * kV * sizeof(float) : 0;
+    return launch_first(true, norm_rows_grad_kernel<T, kWarps, kV>, dim3((unsigned int)blocks), dim3(kWarps == 1 ? 256 : kWarps * 32), smem, s, a);
+}
+
+template <typename T>
+tc_status gradient(const NormGradArgs &a, int blocks, cudaStream_t s)
+{
+    cudaError_t err = cudaSuccess;
+    if (blocks == 0) {                                        // no pixels: the vectors' gradients are zero
+    } else if (a.hw > 1) {
+        const size_t smem = (size_t)2 * a.c * sizeof(float);
+        err = cudaFuncSetAttribute(norm_maps_grad_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (err == cudaSuccess) err = launch_first(true, norm_maps_grad_kernel<T>, dim3((unsigned int)blocks), dim3(256), smem, s, a);
+    } else if (a.c <= 256) err = launch_grad_rows<T, 1, 1>(a, blocks, s);
+    else if (a.c <= 512) err = launch_grad_rows<T, 2, 1>(a, blocks, s);
+    else if (a.c <= 1024) err = launch_grad_rows<T, 4, 1>(a, blocks, s);
+    else if (a.c <= 2048) err = launch_grad_rows<T, 8, 1>(a, blocks, s);
+    else if (a.c <= 4096) err = launch_grad_rows<T, 16, 1>(a, blocks, s);
+    else if (a.c <= 8192) err = launch_grad_rows<T, 32, 1>(a, blocks, s);
+    else err = launch_grad_rows<T, 32, 2>(a, blocks, s);
+    if (err != cudaSuccess) { cudaGetLastError(); return TC_ERR_CUDA; }
+    return launch_chained(blocks > 0, norm_vectors_kernel, dim3((unsigned int)((a.c + 31) / 32)), dim3(256), 0, s, a, blocks) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
+}
+
+}  // namespace
+
+tc_status tc_launch_residual_norms(const NormArgs &a, int dtype, cudaStream_t s)
+{
+    return dtype == TC_BF16 ? norms<__nv_bfloat16>(a, s) : norms<float>(a, s);
+}
+
+// Blocks of the gradient's kernel: as many as an SM holds of its row's width, four of the maps' kernel.
+int tc_norm_grad_blocks(long long pixels, int c, int hw, int sm_count)
+{
+    long long rows = pixels, per_sm = 1;
+    if (hw > 1) { rows = (pixels + 31) / 32; per_sm = 4; }
+    else if (c <= 256) { rows = (pixels + 7) / 8; per_sm = 2; }
+    else for (int w = 2; w < 16 && per_sm == 1; w *= 2)
+        if (c <= 256 * w) per_sm = 16 / w;
+    const long long most = per_sm * sm_count;
+    return (int)(rows < most ? rows : most);
+}
+
+tc_status tc_launch_residual_norms_backward(const NormGradArgs &a, int dtype, int blocks, cudaStream_t s)
+{
+    return dtype == TC_BF16 ? gradient<__nv_bfloat16>(a, blocks, s) : gradient<float>(a, blocks, s);
+}

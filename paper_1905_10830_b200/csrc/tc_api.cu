@@ -42,6 +42,18 @@ bool tc_tensor_map_sw128(CUtensorMap *map, const void *base, long long rows, int
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool tc_tensor_map_codes(CUtensorMap *map, const void *base, long long rows, long long cols, long long ld, int box_rows)
+{
+    const EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld};
+    const cuuint32_t box[2] = {128u, (cuuint32_t)box_rows};
+    const cuuint32_t elem[2] = {1u, 1u};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 #define TC_CUDA(call)                                   \
     do {                                                \
         if ((call) != cudaSuccess) { cudaGetLastError(); return TC_ERR_CUDA; } \
@@ -1778,6 +1790,226 @@ tc_status tc_stats(tc_ctx *ctx, const tc_model *m, const tc_codebook *cb, const 
     }
     out->energy_ratio_90 = (double)need / (double)m->c;
     return TC_OK;
+}
+
+}  // extern "C"
+
+// ---- block-scaled 8-bit matrices and residual norms ----------------------------------------------
+
+namespace {
+
+constexpr long long kMostRows = (1ll << 31) - 256;      // rows that 32-bit row numbers, rounded up to a tile, hold
+constexpr int kMostNormChannels = 16384;                // a row's channels in the registers of a block
+
+size_t element_size(int dtype) { return dtype == TC_BF16 ? 2 : 4; }
+bool aligned_tensor(const tc_tensor *t) { return valid_tensor(t) && ((uintptr_t)t->data & (element_size(t->dtype) - 1)) == 0; }
+long long pixels_of(const tc_tensor *t) { return (long long)t->n * t->h * t->w; }
+bool same_shape(const tc_tensor *a, const tc_tensor *b) { return a->n == b->n && a->c == b->c && a->h == b->h && a->w == b->w && a->dtype == b->dtype; }
+
+bool valid_blocks(const tc_blocks *b)
+{
+    return b && b->rows >= 0 && b->cols >= 0 && b->ld >= b->cols && b->ld % 16 == 0 &&
+           (((b->codes && b->scales) && ((uintptr_t)b->codes & 15u) == 0 && ((uintptr_t)b->scales & 15u) == 0) || b->rows == 0 || b->cols == 0);
+}
+BlockMatrix block_matrix(const tc_blocks *b)
+{
+    BlockMatrix m;
+    if (!b) return m;
+    m.codes = (uint8_t *)b->codes;
+    m.scales = b->scales;
+    m.ld = b->ld;
+    m.scale_ld = b->square ? ((long long)b->rows + 127) / 128 : ((long long)b->rows + 127) / 128 * 128;
+    return m;
+}
+
+// Byte ranges of a call's buffers: its outputs overlap neither one another nor its inputs.
+struct Ranges {
+    struct Range { const char *first, *end; bool out; };
+    Range all[24];
+    int count = 0;
+    void add(const void *p, size_t bytes, bool out) { if (p && bytes) all[count++] = {(const char *)p, (const char *)p + bytes, out}; }
+    void add(const tc_tensor *t, bool out) { if (t) add(t->data, (size_t)pixels_of(t) * t->c * element_size(t->dtype), out); }
+    void add(const tc_blocks *b, bool out)
+    {
+        if (!b) return;
+        add(b->codes, (size_t)b->rows * b->ld, out);
+        add(b->scales, (size_t)((b->cols + 127ll) / 128) * block_matrix(b).scale_ld * sizeof(float), out);
+    }
+    bool apart() const
+    {
+        for (int i = 0; i < count; ++i)
+            for (int j = 0; j < i; ++j)
+                if ((all[i].out || all[j].out) && all[i].first < all[j].end && all[j].first < all[i].end) return false;
+        return true;
+    }
+};
+
+// The parameters both directions share, against the tensor they belong to.
+bool valid_norm_params(const tc_tensor *h, const tc_norm_params *p)
+{
+    if (!aligned_tensor(h) || !p || !(p->eps >= 0.f) || (!p->y && !p->before)) return false;
+    if (p->y ? !aligned_tensor(p->y) || !same_shape(h, p->y) : p->after || p->gate || p->gate_map || p->scale) return false;
+    return !p->gate_map || (!p->gate && aligned_tensor(p->gate_map) && same_shape(h, p->gate_map));
+}
+void add_norm_params(Ranges &r, const tc_tensor *h, const tc_norm_params *p)
+{
+    r.add(h, false);
+    r.add(p->y, false);
+    r.add(p->gate_map, false);
+    for (const float *v : {p->after, p->gate, p->before}) r.add(v, (size_t)h->c * sizeof(float), false);
+    r.add(p->scale, sizeof(float), false);
+}
+template <typename... P>
+bool aligned16(P... p) { return ((((uintptr_t)p) | ...) & 15u) == 0; }
+const void *data_of(const tc_tensor *t) { return t ? t->data : nullptr; }
+
+}  // namespace
+
+extern "C" {
+
+tc_status tc_quantize_blocks(tc_ctx *ctx, const tc_tensor *x, const tc_blocks *pixels, const tc_blocks *channels, void *cuda_stream)
+{
+    if (!ctx || !aligned_tensor(x) || (!pixels && !channels)) return TC_ERR_INVALID_ARG;
+    const long long p = pixels_of(x);
+    if (p > kMostRows || x->c > 1 << 22) return TC_ERR_UNSUPPORTED;
+    if (pixels && (!valid_blocks(pixels) || pixels->rows != p || pixels->cols != x->c)) return TC_ERR_INVALID_ARG;
+    if (channels && (!valid_blocks(channels) || channels->rows != x->c || channels->cols != p)) return TC_ERR_INVALID_ARG;
+    if (pixels && channels && !pixels->square != !channels->square) return TC_ERR_INVALID_ARG;
+    Ranges ranges;
+    ranges.add(x, false);
+    ranges.add(pixels, true);
+    ranges.add(channels, true);
+    if (!ranges.apart()) return TC_ERR_INVALID_ARG;
+    if (p == 0) return TC_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return TC_ERR_CUDA;
+    return tc_launch_quantize_blocks(x->data, x->dtype, x->n, x->c, x->h * x->w, (pixels ? pixels : channels)->square != 0, block_matrix(pixels),
+                                     block_matrix(channels), (cudaStream_t)cuda_stream);
+}
+
+tc_status tc_matmul_blocks(tc_ctx *ctx, const tc_blocks *a, const tc_blocks *b, const float *bias, int32_t relu, const tc_tensor *out, void *cuda_stream)
+{
+    if (!ctx || !valid_blocks(a) || !valid_blocks(b) || !aligned_tensor(out)) return TC_ERR_INVALID_ARG;
+    if (a->cols != b->cols || pixels_of(out) != a->rows || out->c != b->rows) return TC_ERR_INVALID_ARG;
+    if (a->rows > kMostRows || b->rows > kMostRows || a->cols > kMostRows) return TC_ERR_UNSUPPORTED;
+    Ranges ranges;
+    ranges.add(a, false);
+    ranges.add(b, false);
+    ranges.add(bias, (size_t)b->rows * sizeof(float), false);
+    ranges.add(out, true);
+    if (!ranges.apart()) return TC_ERR_INVALID_ARG;
+    if (a->rows == 0) return TC_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return TC_ERR_CUDA;
+    MatmulArgs args;
+    args.pixels = {block_matrix(a), a->rows, a->square != 0};
+    args.channels = {block_matrix(b), b->rows, b->square != 0};
+    args.cols = a->cols;
+    args.bias = bias;
+    args.relu = relu != 0;
+    args.out = out->data;
+    args.dtype = out->dtype;
+    args.hw = out->h * out->w;
+    args.status = ctx->d_status;
+    MatmulPlan plan = tc_plan_matmul(args, ctx->sm_count);
+    if (plan.tiles > 1 << 30) return TC_ERR_UNSUPPORTED;
+    CallScratch scratch;
+    const tc_status st = call_scratch(ctx, 0, plan.workspace, (cudaStream_t)cuda_stream, &scratch);
+    if (st != TC_OK) return st;
+    if (plan.workspace && !scratch.at) plan.splits = 1;
+    return tc_launch_matmul_blocks(ctx, args, plan, scratch.at, (cudaStream_t)cuda_stream);
+}
+
+tc_status tc_residual_norms(tc_ctx *ctx, const tc_tensor *h, const tc_norm_params *params, const tc_tensor *sum, const tc_tensor *x, const tc_blocks *codes,
+                            void *cuda_stream)
+{
+    if (!ctx || !valid_norm_params(h, params)) return TC_ERR_INVALID_ARG;
+    if (params->y ? !aligned_tensor(sum) || !same_shape(h, sum) : sum != nullptr) return TC_ERR_INVALID_ARG;
+    if ((params->before != nullptr) != (x || codes)) return TC_ERR_INVALID_ARG;
+    if (x && (!aligned_tensor(x) || !same_shape(h, x))) return TC_ERR_INVALID_ARG;
+    const long long p = pixels_of(h);
+    if (p > kMostRows || h->c > kMostNormChannels) return TC_ERR_UNSUPPORTED;
+    if (codes && (!valid_blocks(codes) || codes->rows != p || codes->cols != h->c || codes->square)) return TC_ERR_INVALID_ARG;
+    Ranges ranges;
+    add_norm_params(ranges, h, params);
+    ranges.add(sum, true);
+    ranges.add(x, true);
+    ranges.add(codes, true);
+    if (!ranges.apart()) return TC_ERR_INVALID_ARG;
+    if (p == 0) return TC_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return TC_ERR_CUDA;
+    NormArgs a{};
+    a.h = h->data;
+    a.y = data_of(params->y);
+    a.gate_map = data_of(params->gate_map);
+    a.after = params->after;
+    a.gate = params->gate;
+    a.scale = params->scale;
+    a.before = params->before;
+    a.eps = params->eps;
+    a.sum = (void *)data_of(sum);
+    a.x = (void *)data_of(x);
+    a.codes = block_matrix(codes);
+    a.pixels = p;
+    a.c = h->c;
+    a.hw = h->h * h->w;
+    a.vec = h->c % 8 == 0 && aligned16(a.h, a.y, a.gate_map, a.after, a.gate, a.before, a.sum, a.x);
+    return tc_launch_residual_norms(a, h->dtype, (cudaStream_t)cuda_stream);
+}
+
+tc_status tc_residual_norms_backward(tc_ctx *ctx, const tc_tensor *s, const tc_norm_params *params, const tc_tensor *dx, const tc_tensor *ds,
+                                     const tc_norm_grads *out, void *cuda_stream)
+{
+    if (!ctx || !valid_norm_params(s, params) || !out) return TC_ERR_INVALID_ARG;
+    if ((params->before != nullptr) != (dx != nullptr) || (dx && (!aligned_tensor(dx) || !same_shape(s, dx)))) return TC_ERR_INVALID_ARG;
+    if (ds && (!aligned_tensor(ds) || !same_shape(s, ds))) return TC_ERR_INVALID_ARG;
+    if (!aligned_tensor(out->dh) || !same_shape(s, out->dh)) return TC_ERR_INVALID_ARG;
+    if (params->y ? !aligned_tensor(out->dy) || !same_shape(s, out->dy) : out->dy || out->dscale) return TC_ERR_INVALID_ARG;
+    if (params->gate_map ? !aligned_tensor(out->dgate_map) || !same_shape(s, out->dgate_map) : out->dgate_map != nullptr) return TC_ERR_INVALID_ARG;
+    if ((out->dafter && !params->after) || (out->dgate && !params->gate) || (out->dbefore && !params->before)) return TC_ERR_INVALID_ARG;
+    const long long p = pixels_of(s);
+    if (p > kMostRows || s->c > kMostNormChannels) return TC_ERR_UNSUPPORTED;
+    Ranges ranges;
+    add_norm_params(ranges, s, params);
+    ranges.add(dx, false);
+    ranges.add(ds, false);
+    for (const tc_tensor *t : {out->dh, out->dy, out->dgate_map}) ranges.add(t, true);
+    for (const float *v : {out->dafter, out->dgate, out->dbefore}) ranges.add(v, (size_t)s->c * sizeof(float), true);
+    ranges.add(out->dscale, sizeof(float), true);
+    if (!ranges.apart()) return TC_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return TC_ERR_CUDA;
+    NormGradArgs a{};
+    a.s = s->data;
+    a.y = data_of(params->y);
+    a.dx = data_of(dx);
+    a.ds = data_of(ds);
+    a.gate_map = data_of(params->gate_map);
+    a.after = params->after;
+    a.gate = params->gate;
+    a.scale = params->scale;
+    a.before = params->before;
+    a.eps = params->eps;
+    a.dh = out->dh->data;
+    a.dy = (void *)data_of(out->dy);
+    a.dgate_map = (void *)data_of(out->dgate_map);
+    a.dafter = out->dafter;
+    a.dgate = out->dgate;
+    a.dscale = out->dscale;
+    a.dbefore = out->dbefore;
+    a.pixels = p;
+    a.c = s->c;
+    a.hw = p ? s->h * s->w : 1;
+    a.vec = s->c % 8 == 0 && aligned16(a.s, a.y, a.dx, a.ds, a.gate_map, a.after, a.gate, a.before, a.dh, a.dy, a.dgate_map);
+    const int blocks = tc_norm_grad_blocks(p, a.c, a.hw, ctx->sm_count);
+    CallScratch scratch;
+    const size_t bytes = ((size_t)blocks * (2 * (size_t)a.c + 1) + 1) * sizeof(float);
+    const tc_status st = call_scratch(ctx, bytes, bytes, (cudaStream_t)cuda_stream, &scratch);
+    if (st != TC_OK) return st;
+    a.partial = (float *)scratch.at;
+    a.partial_scale = a.partial + (size_t)blocks * 2 * a.c;
+    return tc_launch_residual_norms_backward(a, s->dtype, blocks, (cudaStream_t)cuda_stream);
 }
 
 }  // extern "C"

@@ -286,6 +286,65 @@ constexpr int kHistCopies = 8;
 // tensors of fewer tiles than this many per SM take the one-thread-per-value exact kernels
 constexpr int kExactParallelTilesPerSm = 2;
 
+// ---- block-scaled 8-bit matrices and residual norms -------------------------------------------
+// The kernels' side of tc_blocks: codes [rows][ld], scales [blocks][scale_ld].
+struct BlockMatrix {
+    uint8_t *codes = nullptr;
+    float *scales = nullptr;
+    long long ld = 0, scale_ld = 0;
+};
+tc_status tc_launch_quantize_blocks(const void *x, int dtype, int n, int c, int hw, bool square, const BlockMatrix &pixels, const BlockMatrix &channels,
+                                    cudaStream_t s);
+struct MatmulOperand {
+    BlockMatrix m;
+    int rows;
+    bool square;
+};
+struct MatmulArgs {
+    MatmulOperand pixels, channels;   // rows of the output's pixels, of its channels
+    int cols;                         // length of the sums
+    const float *bias;                // [channels.rows], or null
+    int relu;
+    void *out;
+    int dtype, hw;
+    unsigned int *status;
+};
+// How a product is cut into the units of its kernel.
+struct MatmulPlan {
+    bool swapped = false;             // rows of the MMA are channels
+    int n = 0;                        // columns of a tile (its rows: 128)
+    int splits = 1;                   // parts of the sums' length
+    long long tiles = 0;
+    size_t workspace = 0;             // bytes for the parts' sums
+};
+MatmulPlan tc_plan_matmul(const MatmulArgs &a, int sm_count);
+tc_status tc_launch_matmul_blocks(const tc_ctx *ctx, const MatmulArgs &a, const MatmulPlan &plan, void *workspace, cudaStream_t s);
+struct NormArgs {
+    const void *h, *y, *gate_map;     // y null: nothing is added to h;  gate_map: a gate for each value
+    const float *after, *gate, *scale, *before;     // null: no norm, no gate, 1, no output x
+    float eps;
+    void *sum, *x;
+    BlockMatrix codes;
+    long long pixels;
+    int c, hw, vec;                   // vec: rows and vectors can be moved 16 bytes at a time
+};
+tc_status tc_launch_residual_norms(const NormArgs &a, int dtype, cudaStream_t s);
+struct NormGradArgs {
+    const void *s, *y, *dx, *ds, *gate_map;         // dx null where before is; ds null: zero
+    const float *after, *gate, *scale, *before;
+    float eps;
+    void *dh, *dy, *dgate_map;
+    float *dafter, *dgate, *dscale, *dbefore;       // null: not wanted
+    long long pixels;
+    int c, hw, vec;
+    float *partial;                   // [blocks][2][c]
+    float *partial_scale;             // [blocks]
+};
+int tc_norm_grad_blocks(long long pixels, int c, int hw, int sm_count);
+tc_status tc_launch_residual_norms_backward(const NormGradArgs &a, int dtype, int blocks, cudaStream_t s);
+// Tensor map of e4m3 codes [rows][ld] of which `cols` count: boxes of 128 codes x box_rows rows, 128-byte swizzle.
+bool tc_tensor_map_codes(CUtensorMap *map, const void *base, long long rows, long long cols, long long ld, int box_rows);
+
 // ---- launchers (defined in the .cu files) ----------------------------------------------
 tc_status tc_launch_encode_simt(const tc_ctx *ctx, const EncodeArgs &a, int dtype, cudaStream_t s);
 tc_status tc_launch_decode_simt(const tc_ctx *ctx, const DecodeArgs &a, int dtype, cudaStream_t s);

@@ -75,3 +75,42 @@ def run_chain(ctx: tc.Context, stages: Sequence[Callable[[torch.Tensor], torch.T
         recons.append(cur)
         bits.append(nbits)
     return maps, recons, bits
+
+
+class ResidualBlock:
+    """A residual block on the pixels' vectors, to stand between two coded maps (a stage of the functions above) or to be
+    trained: s = h + scale * gate * norm(W norm(h) before) after, the 1 x 1 convolution W [C][C] as a product of 8-bit blocks.
+    Vectors are float32 CUDA tensors [C] (`scale`: one value); `gate` and `scale` may be None."""
+
+    def __init__(self, ctx: tc.Context, weight: torch.Tensor, *, before: torch.Tensor, after: torch.Tensor,
+                 gate: torch.Tensor | None = None, scale: torch.Tensor | None = None, eps: float = 1e-6):
+        if weight.dim() != 2 or weight.shape[0] != weight.shape[1]:
+            raise ValueError("weight: expected [C][C]")
+        self.ctx, self.eps, self.before = ctx, eps, before
+        self.around = dict(after=after, gate=gate, scale=scale)
+        self.set_weight(weight)
+
+    def set_weight(self, weight: torch.Tensor) -> None:
+        """New values of W: its codes, by rows for the product and by columns for the gradient to its input."""
+        self.rows, self.columns = tc.tc_quantize_blocks(self.ctx, weight[:, :, None, None].contiguous(), rows="both", square=True)
+
+    def __call__(self, h: torch.Tensor) -> torch.Tensor:
+        n, _, hh, ww = h.shape
+        _, codes = tc.tc_residual_norms(self.ctx, h, before=self.before, eps=self.eps, blocks=True)
+        y = tc.tc_matmul_blocks(self.ctx, codes, self.rows, shape=(n, hh, ww), dtype=h.dtype)
+        return tc.tc_residual_norms(self.ctx, h, y, eps=self.eps, **self.around)[0]
+
+    def gradients(self, h: torch.Tensor, ds: torch.Tensor) -> dict:
+        """Gradients to `h`, the weight (float32) and the vectors, from the gradient `ds` of the block's output; the forward
+        pass is computed again, the products' operands in both directions are 8-bit blocks."""
+        n, c, hh, ww = h.shape
+        _, x = tc.tc_residual_norms(self.ctx, h, before=self.before, eps=self.eps)
+        x_pixels, x_channels = tc.tc_quantize_blocks(self.ctx, x, rows="both")
+        y = tc.tc_matmul_blocks(self.ctx, x_pixels, self.rows, shape=(n, hh, ww), dtype=h.dtype)
+        s = tc.tc_residual_norms(self.ctx, h, y, eps=self.eps, **self.around)[0]
+        outer = tc.tc_residual_norms_backward(self.ctx, s, y, None, ds, eps=self.eps, **self.around)
+        dy_pixels, dy_channels = tc.tc_quantize_blocks(self.ctx, outer.y, rows="both")
+        dx = tc.tc_matmul_blocks(self.ctx, dy_pixels, self.columns, shape=(n, hh, ww), dtype=h.dtype)
+        dw = tc.tc_matmul_blocks(self.ctx, dy_channels, x_channels, dtype=torch.float32)
+        inner = tc.tc_residual_norms_backward(self.ctx, h, None, dx, outer.h, before=self.before, eps=self.eps)
+        return dict(h=inner.h, weight=dw.reshape(c, c), before=inner.before, after=outer.after, gate=outer.gate, scale=outer.scale)
