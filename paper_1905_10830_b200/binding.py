@@ -66,12 +66,12 @@ class _Blocks(C.Structure):
 
 
 class _NormParams(C.Structure):
-    _fields_ = [("y", C.POINTER(_Tensor)), ("after", C.c_void_p), ("gate", C.c_void_p), ("gate_map", C.POINTER(_Tensor)),
+    _fields_ = [("y", C.c_void_p), ("after", C.c_void_p), ("gate", C.c_void_p), ("gate_map", C.c_void_p),
                 ("scale", C.c_void_p), ("before", C.c_void_p), ("eps", C.c_float)]
 
 
 class _NormGrads(C.Structure):
-    _fields_ = [("dh", C.POINTER(_Tensor)), ("dy", C.POINTER(_Tensor)), ("dgate_map", C.POINTER(_Tensor)), ("dafter", C.c_void_p),
+    _fields_ = [("dh", C.c_void_p), ("dy", C.c_void_p), ("dgate_map", C.c_void_p), ("dafter", C.c_void_p),
                 ("dgate", C.c_void_p), ("dscale", C.c_void_p), ("dbefore", C.c_void_p)]
 
 
@@ -148,10 +148,10 @@ def load_library() -> C.CDLL:
         lib.tc_fit_state_finish.argtypes = [vp, vp, P(_Tensor), P(_FitParams), P(vp), vp]
         lib.tc_fold_forward.argtypes = [vp, vp, vp, vp, vp, C.c_int64, vp, vp]
         lib.tc_fold_inverse.argtypes = [vp, vp, vp, i32, i32, vp, vp]
-        lib.tc_quantize_blocks.argtypes = [vp, P(_Tensor), P(_Blocks), P(_Blocks), vp]
-        lib.tc_matmul_blocks.argtypes = [vp, P(_Blocks), P(_Blocks), vp, i32, P(_Tensor), vp]
-        lib.tc_residual_norms.argtypes = [vp, P(_Tensor), P(_NormParams), P(_Tensor), P(_Tensor), P(_Blocks), vp]
-        lib.tc_residual_norms_backward.argtypes = [vp, P(_Tensor), P(_NormParams), P(_Tensor), P(_Tensor), P(_NormGrads), vp]
+        lib.tc_quantize_blocks.argtypes = [vp] * 5          # (structures by address)
+        lib.tc_matmul_blocks.argtypes = [vp, vp, vp, vp, i32, vp, vp]
+        lib.tc_residual_norms.argtypes = [vp] * 7
+        lib.tc_residual_norms_backward.argtypes = [vp] * 7
         _lib = lib
     return _lib
 
@@ -206,6 +206,7 @@ class Context(_Handle):
     def __init__(self, ptr: int, device: int):
         super().__init__(ptr)
         self.device = device
+        self.empty = None          # tensors without values that new ones are made from
 
 
 class Model(_Handle):
@@ -614,6 +615,8 @@ def tc_stats(ctx: Context, model: Model, cb: Codebook | None, x: torch.Tensor, *
 
 
 # ---- layers between coded maps ---------------------------------------------------------------
+# A single token's calls take the GPU a few microseconds, so the host's part is kept short: pointers are passed as addresses (a
+# ctypes pointer object costs 0.3 us), and buffers are made from an empty tensor of their type (1.0 us instead of torch.empty's 2.4).
 
 @dataclass
 class Blocks:
@@ -630,9 +633,8 @@ class Blocks:
 
     @classmethod
     def empty(cls, rows: int, cols: int, square: bool = False, device="cuda") -> "Blocks":
-        tall = -(-rows // 128)
-        return cls(torch.empty((rows, -(-cols // 16) * 16), dtype=torch.float8_e4m3fn, device=device),
-                   torch.empty((-(-cols // 128), tall if square else tall * 128), dtype=torch.float32, device=device), cols, square)
+        return cls(*_block_buffers(torch.empty(0, dtype=torch.float8_e4m3fn, device=device), torch.empty(0, dtype=torch.float32, device=device),
+                                   rows, cols, square), cols, square)
 
     def dequantize(self) -> torch.Tensor:
         """The values the codes stand for, float32 [rows, cols] (for inspection; no product reads them)."""
@@ -640,15 +642,23 @@ class Blocks:
         return self.codes[:, :self.cols].float() * scales[:, :self.rows].t().repeat_interleave(128, 1)[:, :self.cols]
 
 
-def _on_device(ctx: Context, *tensors) -> None:
-    for x in tensors:
-        if x is not None and x.get_device() != ctx.device:
-            raise ValueError(f"expected tensors on the context's device, cuda:{ctx.device}")
+def _block_buffers(codes, scales, rows, cols, square):
+    tall = (rows + 127) // 128
+    return codes.new_empty(rows, (cols + 15) // 16 * 16), scales.new_empty((cols + 127) // 128, tall if square else tall * 128)
+
+
+def _new_blocks(ctx: Context, rows: int, cols: int, square: bool):
+    """Blocks on the context's device, and their C structure."""
+    if ctx.empty is None:
+        ctx.empty = tuple(torch.empty(0, dtype=t, device=f"cuda:{ctx.device}") for t in (torch.float8_e4m3fn, torch.float32))
+    codes, scales = _block_buffers(*ctx.empty, rows, cols, square)
+    return Blocks(codes, scales, cols, square), _Blocks(codes.data_ptr(), scales.data_ptr(), (cols + 15) // 16 * 16, rows, cols, square)
 
 
 def _blocks(ctx: Context, b: Blocks) -> _Blocks:
     codes, scales = b.codes, b.scales
-    _on_device(ctx, codes, scales)
+    if codes.get_device() != ctx.device or scales.get_device() != ctx.device:
+        raise ValueError(_ELSEWHERE)
     if codes.dim() != 2 or scales.dim() != 2 or codes.dtype != torch.float8_e4m3fn or scales.dtype != torch.float32 or \
             not codes.is_contiguous() or not scales.is_contiguous():
         raise ValueError("block matrices have contiguous float8_e4m3fn codes [rows, ld] and float32 scales")
@@ -657,6 +667,16 @@ def _blocks(ctx: Context, b: Blocks) -> _Blocks:
     if not 0 <= b.cols <= ld or scales.shape != ((b.cols + 127) // 128, tall if b.square else tall * 128):
         raise ValueError("block matrix: codes, scales and cols do not belong together")
     return _Blocks(codes.data_ptr(), scales.data_ptr(), ld, rows, b.cols, b.square)
+
+
+_ELSEWHERE = "expected tensors on the context's device"
+
+
+def _local(ctx: Context, x: torch.Tensor) -> _Tensor:
+    t = _tensor(x)
+    if x.get_device() != ctx.device:
+        raise ValueError(_ELSEWHERE)
+    return t
 
 
 def _vector(ctx: Context, v, n: int, name: str) -> int | None:
@@ -670,23 +690,27 @@ def _vector(ctx: Context, v, n: int, name: str) -> int | None:
 def tc_quantize_blocks(ctx: Context, x: torch.Tensor, *, rows: str = "pixels", square: bool = False, out=None):
     """Codes of `x` (N, C, H, W): a row for each pixel ("pixels", blocks along the channels), for each channel ("channels",
     blocks along the pixels), or "both" as a pair.  `out` reuses the Blocks of an earlier call."""
-    if rows not in ("pixels", "channels", "both"):
-        raise ValueError('rows: "pixels", "channels" or "both"')
-    t = _tensor(x)
-    _on_device(ctx, x)
+    t = _local(ctx, x)
     p = t.n * t.h * t.w
-    shapes = {"pixels": [(p, t.c)], "channels": [(t.c, p)], "both": [(p, t.c), (t.c, p)]}[rows]
-    if out is None:
-        got = [Blocks.empty(r, c, square, x.device) for r, c in shapes]
+    if rows == "pixels":
+        shapes = ((p, t.c),)
+    elif rows == "channels":
+        shapes = ((t.c, p),)
+    elif rows == "both":
+        shapes = ((p, t.c), (t.c, p))
     else:
-        got = list(out) if rows == "both" else [out]
-        if len(got) != len(shapes) or any(bool(b.square) != bool(square) for b in got):
+        raise ValueError('rows: "pixels", "channels" or "both"')
+    if out is None:
+        made = [_new_blocks(ctx, r, c, square) for r, c in shapes]
+    else:
+        given = tuple(out) if rows == "both" else (out,)
+        if len(given) != len(shapes) or any(bool(b.square) != bool(square) for b in given):
             raise ValueError("out: Blocks as this call returns them")
-    made = [_blocks(ctx, b) for b in got]
-    refs = [C.byref(b) for b in made]
-    pixels, channels = (refs[0], refs[1]) if rows == "both" else (refs[0], None) if rows == "pixels" else (None, refs[0])
-    _check(load_library().tc_quantize_blocks(ctx.ptr, C.byref(t), pixels, channels, _tensor_stream(ctx.device)), "tc_quantize_blocks")
-    return tuple(got) if rows == "both" else got[0]
+        made = [(b, _blocks(ctx, b)) for b in given]
+    at = C.addressof(made[0][1])
+    pixels, channels = (at, C.addressof(made[1][1])) if rows == "both" else (at, None) if rows == "pixels" else (None, at)
+    _check(load_library().tc_quantize_blocks(ctx.ptr, C.addressof(t), pixels, channels, _tensor_stream(ctx.device)), "tc_quantize_blocks")
+    return (made[0][0], made[1][0]) if rows == "both" else made[0][0]
 
 
 def tc_matmul_blocks(ctx: Context, a: Blocks, b: Blocks, *, shape=None, dtype=torch.bfloat16, bias: torch.Tensor | None = None,
@@ -697,25 +721,20 @@ def tc_matmul_blocks(ctx: Context, a: Blocks, b: Blocks, *, shape=None, dtype=to
     if out is None:
         n, h, w = (ma.rows, 1, 1) if shape is None else shape
         out = torch.empty((n, mb.rows, h, w), dtype=dtype, device=a.codes.device)
-    t = _tensor(out)
-    _on_device(ctx, out)
-    _check(load_library().tc_matmul_blocks(ctx.ptr, C.byref(ma), C.byref(mb), _vector(ctx, bias, mb.rows, "bias"), relu, C.byref(t),
+    t = _local(ctx, out)
+    _check(load_library().tc_matmul_blocks(ctx.ptr, C.addressof(ma), C.addressof(mb), _vector(ctx, bias, mb.rows, "bias"), relu, C.addressof(t),
                                            _tensor_stream(ctx.device)), "tc_matmul_blocks")
     return out
 
 
-def _norm_params(ctx: Context, h: torch.Tensor, y, after, gate, scale, before, eps):
-    """The C structure, and what it points to."""
-    _on_device(ctx, h, y)
-    c = h.shape[1]
-    ty = None if y is None else _tensor(y)
-    tg = None
-    if gate is not None and gate.dim() == 4:
-        _on_device(ctx, gate)
-        tg = _tensor(gate)
-    p = _NormParams(None if ty is None else C.pointer(ty), _vector(ctx, after, c, "after"), None if tg is not None else _vector(ctx, gate, c, "gate"),
-                    None if tg is None else C.pointer(tg), _vector(ctx, scale, 1, "scale"), _vector(ctx, before, c, "before"), eps)
-    return p, (ty, tg)
+def _norm_params(ctx: Context, h: _Tensor, y, after, gate, scale, before, eps):
+    """The C structure, and the tensors it points to."""
+    c = h.c
+    ty = None if y is None else _local(ctx, y)
+    tg = gate if gate is None or gate.dim() != 4 else _local(ctx, gate)
+    in_channels = tg is gate                      # no gate, or one for each channel
+    return _NormParams(None if ty is None else C.addressof(ty), _vector(ctx, after, c, "after"), _vector(ctx, gate, c, "gate") if in_channels else None,
+                       None if in_channels else C.addressof(tg), _vector(ctx, scale, 1, "scale"), _vector(ctx, before, c, "before"), eps), ty, tg
 
 
 def tc_residual_norms(ctx: Context, h: torch.Tensor, y: torch.Tensor | None = None, *, after: torch.Tensor | None = None,
@@ -724,23 +743,22 @@ def tc_residual_norms(ctx: Context, h: torch.Tensor, y: torch.Tensor | None = No
     """(s, x): s = h + scale * gate * norm(y) * after, x = norm(s) * before, norms over the channels of each pixel.  x is a
     tensor like h, or with `blocks` its codes by pixels; without `before` it is None.  Without `y` s is h itself.  `gate` is
     [C], or a tensor like y."""
-    th = _tensor(h)
-    p, keep = _norm_params(ctx, h, y, after, gate, scale, before, eps)
-    s = h if y is None else torch.empty_like(h) if sum_out is None else sum_out
-    ts = None if y is None else _tensor(s)
-    x, tx, bx = None, None, None
+    th = _local(ctx, h)
+    p, *keep = _norm_params(ctx, th, y, after, gate, scale, before, eps)
+    s, at_s, x, at_x, at_b = h, None, None, None, None
+    if y is not None:
+        s = torch.empty_like(h) if sum_out is None else sum_out
+        ts = _local(ctx, s)
+        at_s = C.addressof(ts)
     if before is not None:
         if blocks:
-            x = Blocks.empty(th.n * th.h * th.w, th.c, False, h.device) if out is None else out
-            bx = _blocks(ctx, x)
+            x, b = _new_blocks(ctx, th.n * th.h * th.w, th.c, False) if out is None else (out, _blocks(ctx, out))
+            at_b = C.addressof(b)
         else:
             x = torch.empty_like(h) if out is None else out
-            tx = _tensor(x)
-            _on_device(ctx, x)
-    _on_device(ctx, s)
-    ref = lambda v: None if v is None else C.byref(v)                            # noqa: E731
-    _check(load_library().tc_residual_norms(ctx.ptr, C.byref(th), C.byref(p), ref(ts), ref(tx), ref(bx), _tensor_stream(ctx.device)),
-           "tc_residual_norms")
+            tx = _local(ctx, x)
+            at_x = C.addressof(tx)
+    _check(load_library().tc_residual_norms(ctx.ptr, C.addressof(th), C.addressof(p), at_s, at_x, at_b, _tensor_stream(ctx.device)), "tc_residual_norms")
     del keep
     return s, x
 
@@ -760,17 +778,22 @@ def tc_residual_norms_backward(ctx: Context, s: torch.Tensor, y: torch.Tensor | 
                                before: torch.Tensor | None = None, eps: float = 1e-6) -> NormGrads:
     """Gradients at the sum `s` that tc_residual_norms returned, from the gradients `dx` of x (None without `before`) and `ds` of s
     (None: zero)."""
-    t = _tensor(s)
-    p, keep = _norm_params(ctx, s, y, after, gate, scale, before, eps)
-    _on_device(ctx, dx, ds)
-    gate_map = gate is not None and gate.dim() == 4
-    like = lambda v: None if v is None else torch.empty_like(v)                  # noqa: E731
-    g = NormGrads(torch.empty_like(s), like(y), like(after), like(gate), like(scale), like(before))
-    tensors = [None if v is None else _tensor(v) for v in (g.h, g.y, g.gate if gate_map else None, dx, ds)]
-    ptr = [None if v is None else C.pointer(v) for v in tensors]
-    data = lambda v: None if v is None else v.data_ptr()                         # noqa: E731
-    out = _NormGrads(ptr[0], ptr[1], ptr[2], data(g.after), None if gate_map else data(g.gate), data(g.scale), data(g.before))
-    _check(load_library().tc_residual_norms_backward(ctx.ptr, C.byref(t), C.byref(p), ptr[3], ptr[4], C.byref(out),
+    t = _local(ctx, s)
+    p, _, tg = keep = _norm_params(ctx, t, y, after, gate, scale, before, eps)
+    tx, td = None if dx is None else _local(ctx, dx), None if ds is None else _local(ctx, ds)
+    vectors = [v if v is None else torch.empty_like(v) for v in (after, gate, scale, before)]
+    dafter, dgate, dscale, dbefore = [None if v is None else v.data_ptr() for v in vectors]
+    dh, th = torch.empty_like(s), _Tensor(0, t.n, t.c, t.h, t.w, t.dtype)
+    th.data = dh.data_ptr()
+    dy = ty = tgate = None
+    if y is not None:
+        dy = torch.empty_like(y)
+        ty = _Tensor(dy.data_ptr(), *y.shape, t.dtype)
+    if p.gate_map:
+        tgate, dgate = _Tensor(dgate, tg.n, tg.c, tg.h, tg.w, tg.dtype), None
+    at = lambda v: None if v is None else C.addressof(v)                         # noqa: E731
+    out = _NormGrads(C.addressof(th), at(ty), at(tgate), dafter, dgate, dscale, dbefore)
+    _check(load_library().tc_residual_norms_backward(ctx.ptr, C.addressof(t), C.addressof(p), at(tx), at(td), C.addressof(out),
                                                      _tensor_stream(ctx.device)), "tc_residual_norms_backward")
     del keep
-    return g
+    return NormGrads(dh, dy, *vectors)

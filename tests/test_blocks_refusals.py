@@ -33,12 +33,13 @@ def blocks(rows, cols, square=False, at=2 * AT, ld=None):
     return B._Blocks(at, at + (1 << 36), -(-cols // 16) * 16 if ld is None else ld, rows, cols, square)
 
 
-def ref(v):
-    return None if v is None else C.byref(v)
+def at(v):
+    return None if v is None else C.addressof(v)
+
 
 
 def test_quantize(lib, ctx):
-    call = lambda x, p, c, cx=ctx: lib.tc_quantize_blocks(cx, ref(x), ref(p), ref(c), None)              # noqa: E731
+    call = lambda x, p, c, cx=ctx: lib.tc_quantize_blocks(cx, at(x), at(p), at(c), None)              # noqa: E731
     x = tensor(8, 64)
     assert call(x, blocks(8, 64), None, None) == INVALID
     assert call(x, None, None) == INVALID
@@ -57,7 +58,7 @@ def test_quantize(lib, ctx):
 
 
 def test_matmul(lib, ctx):
-    call = lambda a, b, out, cx=ctx, bias=None: lib.tc_matmul_blocks(cx, ref(a), ref(b), bias, 0, ref(out), None)   # noqa: E731
+    call = lambda a, b, out, cx=ctx, bias=None: lib.tc_matmul_blocks(cx, at(a), at(b), bias, 0, at(out), None)   # noqa: E731
     a, b, out = blocks(8, 64), blocks(16, 64, True, 3 * AT), tensor(8, 16)
     assert call(a, b, out, None) == INVALID
     for args in ((None, b, out), (a, None, out), (a, b, None), (a, blocks(16, 48, True, 3 * AT), out), (a, b, tensor(8, 15)), (a, b, tensor(7, 16)),
@@ -69,12 +70,13 @@ def test_matmul(lib, ctx):
 
 def params(**k):
     v = {"y": None, "after": None, "gate": None, "gate_map": None, "scale": None, "before": None, "eps": 1e-6, **k}
-    ptr = lambda t: None if t is None else C.pointer(t)                                   # noqa: E731
-    return B._NormParams(ptr(v["y"]), v["after"], v["gate"], ptr(v["gate_map"]), v["scale"], v["before"], v["eps"])
+    p = B._NormParams(at(v["y"]), v["after"], v["gate"], at(v["gate_map"]), v["scale"], v["before"], v["eps"])
+    p.keep = v
+    return p
 
 
 def test_norms(lib, ctx):
-    call = lambda h, p, s, x, b=None, cx=ctx: lib.tc_residual_norms(cx, ref(h), ref(p), ref(s), ref(x), ref(b), None)   # noqa: E731
+    call = lambda h, p, s, x, b=None, cx=ctx: lib.tc_residual_norms(cx, at(h), at(p), at(s), at(x), at(b), None)   # noqa: E731
     t = lambda i, **k: tensor(**{"n": 8, "c": 64, "at": i * AT, **k})                     # noqa: E731
     whole = dict(y=t(2), after=3 * AT, gate=4 * AT, scale=5 * AT, before=6 * AT)
     assert call(t(1), params(**whole), t(7), t(8), None, None) == INVALID
@@ -96,12 +98,13 @@ def test_norms(lib, ctx):
 
 def test_norms_backward(lib, ctx):
     t = lambda i, **k: tensor(**{"n": 8, "c": 64, "at": i * AT, **k})                     # noqa: E731
-    ptr = lambda v: None if v is None else C.pointer(v)                                   # noqa: E731
 
     def grads(dh=None, dy=None, dgate_map=None, dafter=None, dgate=None, dscale=None, dbefore=None):
-        return B._NormGrads(ptr(dh), ptr(dy), ptr(dgate_map), dafter, dgate, dscale, dbefore)
+        g = B._NormGrads(at(dh), at(dy), at(dgate_map), dafter, dgate, dscale, dbefore)
+        g.keep = dh, dy, dgate_map
+        return g
 
-    call = lambda s, p, dx, ds, g, cx=ctx: lib.tc_residual_norms_backward(cx, ref(s), ref(p), ref(dx), ref(ds), ref(g), None)   # noqa: E731
+    call = lambda s, p, dx, ds, g, cx=ctx: lib.tc_residual_norms_backward(cx, at(s), at(p), at(dx), at(ds), at(g), None)   # noqa: E731
     whole = dict(y=t(2), after=3 * AT, gate=4 * AT, scale=5 * AT, before=6 * AT)
     out = dict(dh=t(10), dy=t(11), dafter=12 * AT, dgate=13 * AT, dscale=14 * AT, dbefore=15 * AT)
     p = params(**whole)
