@@ -4,8 +4,12 @@
 //
 // A block of 128 codes is one row of a 128-byte swizzle atom, so a stage of the ring is a block: four MMAs of 32 codes
 // leave its sum in tensor memory, the epilogue's warps read it back, multiply it by the block's scales and add it to sums in
-// registers (fp32), while the MMAs of the next blocks fill the other buffers.  One CTA an SM walks tiles of 128 rows x
-// up to 256 columns.
+// registers (fp32), while the MMAs of the next blocks fill the other buffers.
+//
+// Large products: pairs of CTAs (cta_group::2) walk tiles of 256 x 256, each CTA with half the rows of both operands in its
+// shared memory.  With one CTA on a tile of 128 x 256 the operands' way from L2 bounds the kernel (48 KB a block and SM against 32).
+// Small ones: one CTA walks tiles of 128 rows x 16 to 256 columns; where tiles are fewer than SMs the sums' length is cut into
+// parts, by the CTAs of a cluster that add through their shared memory, or, for very long sums, through a workspace.
 #include "device_utils.cuh"
 #include "sm100_ptx.cuh"
 #include "tc_internal.h"
@@ -32,6 +36,17 @@ template <int kN> struct Shape {
     static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes;
 };
 
+// Tiles of a pair of CTAs: 256 x 256, 128 rows of each operand a CTA.
+namespace pair {
+constexpr int kN = 256, kRows = 256;
+constexpr int kStageBytes = 2 * kStageA, kStages = kRing / kStageBytes, kBuffers = 2, kTmemCols = 512;
+constexpr int kSets = 2, kCols = kN / kSets;
+constexpr int kEpiWarps = 8, kProducer = 8, kMma = 9;         // warps 10 and 11 only give registers away
+constexpr int kThreads = 12 * 32;
+constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes;
+// Registers: 384 threads are launched with 168 each; 256 x 216 + 128 x 72 is the same sum.
+}
+
 struct TileArgs {
     int rows_a, rows_b;               // of the MMA's operands
     int k_blocks, splits;
@@ -39,7 +54,8 @@ struct TileArgs {
     const float *scale_a, *scale_b;
     long long scale_a_ld, scale_b_ld;
     int shift_a, shift_b;             // 0: a scale for each row, 7: for each 128
-    int swapped;
+    int group;                        // tile rows that are worked on together
+    int swapped, cluster;             // cluster: the parts of a tile's length are a cluster's CTAs
     int out_channels, hw, relu, vec;
     const float *bias;
     void *out;
@@ -76,17 +92,16 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
 struct Unit {
     int tile_m, tile_n, k_first, k_end;
 };
-// Units in the order they are worked on: the parts of a tile's length one after the other; tiles in columns of 16 tile rows, so
-// that the SMs' operands at any time are few rows of both matrices.
+// Units in the order they are worked on: the parts of a tile's length one after the other; tiles in columns of `group` tile rows,
+// so that the SMs' operands at any time are few rows of both matrices.
 __device__ __forceinline__ Unit unit_of(const TileArgs &a, int u)
 {
     const int tile = u / a.splits, split = u - tile * a.splits;
-    constexpr int kGroup = 16;
-    const int per_group = kGroup * a.tiles_n, g = tile / per_group, rest = tile - g * per_group;
-    const int high = min(kGroup, a.tiles_m - g * kGroup);
+    const int per_group = a.group * a.tiles_n, g = tile / per_group, rest = tile - g * per_group;
+    const int high = min(a.group, a.tiles_m - g * a.group);
     Unit r;
     r.tile_n = rest / high;
-    r.tile_m = g * kGroup + rest - r.tile_n * high;
+    r.tile_m = g * a.group + rest - r.tile_n * high;
     r.k_first = (int)((long long)a.k_blocks * split / a.splits);
     r.k_end = (int)((long long)a.k_blocks * (split + 1) / a.splits);
     return r;
@@ -103,7 +118,78 @@ __device__ __forceinline__ long long pixel_at(const TileArgs &a, int p)
 __device__ __forceinline__ void put(float *out, long long at, float v) { out[at] = v; }
 __device__ __forceinline__ void put(__nv_bfloat16 *out, long long at, float v) { out[at] = __float2bfloat16_rn(v); }
 
-// kCols: B has a scale for each row (a column of the tile), else one for each 128.
+// One value, with bias and activation.
+template <typename T>
+__device__ __forceinline__ void store_value(const TileArgs &a, int row, int col, float v)
+{
+    if (row >= a.rows_a || col >= a.rows_b) return;
+    const int p = a.swapped ? col : row, o = a.swapped ? row : col;
+    if (a.bias) v += a.bias[o];
+    if (a.relu && v < 0.f) v = 0.f;                           // (a NaN stays one: a comparison with it fails)
+    put((T *)a.out, pixel_at(a, p) + (long long)o * a.hw, v);
+}
+
+// The sums of a thread's row and kCols columns from `col0` on, to the output.
+template <typename T, int kCols>
+__device__ __forceinline__ void store_row(const TileArgs &a, const uint64_t (&sum)[kCols / 2], int row, int col0)
+{
+    if (row >= a.rows_a) return;
+    T *const out = (T *)a.out;
+    const float floor_v = a.relu ? 0.f : __int_as_float((int)0xff800000u);
+    const int cols_here = min(kCols, a.rows_b - col0);
+    if (!a.swapped) {
+        long long dst = pixel_at(a, row) + (long long)col0 * a.hw;
+        if (a.vec && cols_here == kCols) {
+            constexpr int kPer = 16 / (int)sizeof(T);
+#pragma unroll
+            for (int i = 0; i < kCols; i += kPer) {
+                float v[kPer];
+#pragma unroll
+                for (int j = 0; j < kPer; j += 2) {
+                    halves(sum[(i + j) / 2], v[j], v[j + 1]);
+                    if (a.bias) { v[j] += a.bias[col0 + i + j]; v[j + 1] += a.bias[col0 + i + j + 1]; }
+                    // (a NaN stays one: a comparison with it fails)
+                    v[j] = v[j] < floor_v ? floor_v : v[j];
+                    v[j + 1] = v[j + 1] < floor_v ? floor_v : v[j + 1];
+                }
+                __align__(16) T w[kPer];
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) put(w, j, v[j]);
+                *reinterpret_cast<uint4 *>(out + dst + i) = *reinterpret_cast<const uint4 *>(w);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kCols / 2; ++i) {
+                float x, y;
+                halves(sum[i], x, y);
+                if (2 * i < cols_here) {
+                    if (a.bias) x += a.bias[col0 + 2 * i];
+                    put(out, dst + (long long)(2 * i) * a.hw, x < floor_v ? floor_v : x);
+                }
+                if (2 * i + 1 < cols_here) {
+                    if (a.bias) y += a.bias[col0 + 2 * i + 1];
+                    put(out, dst + (long long)(2 * i + 1) * a.hw, y < floor_v ? floor_v : y);
+                }
+            }
+        }
+    } else {
+        const float bias = a.bias ? a.bias[row] : 0.f;
+        const long long ch = (long long)row * a.hw;
+#pragma unroll
+        for (int i = 0; i < kCols / 2; ++i) {
+            float v[2];
+            halves(sum[i], v[0], v[1]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                if (2 * i + j < cols_here) {
+                    const float x = v[j] + bias;
+                    put(out, ch + pixel_at(a, col0 + 2 * i + j), x < floor_v ? floor_v : x);
+                }
+        }
+    }
+}
+
+// kColumnScales: B has a scale for each row (a column of the tile), else one for each 128.
 template <typename T, int kN, bool kColumnScales>
 __global__ void __launch_bounds__(Shape<kN>::kThreads, 1)
 block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b)
@@ -241,6 +327,18 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
                 if (++b == S::kBuffers) { b = 0; tphase ^= 1u; }
             }
             if (!alive) break;
+            if (a.cluster) {
+                // this part's sums, [column][128 rows], in the ring, which the tensor cores are done with
+                float *dst = reinterpret_cast<float *>(smem_raw + (ring - smem_u32(smem_raw))) + set * S::kCols * kRowsM + row_in_tile;
+#pragma unroll
+                for (int i = 0; i < S::kCols / 2; ++i) {
+                    float x, y;
+                    halves(sum[i], x, y);
+                    dst[(2 * i) * kRowsM] = x;
+                    dst[(2 * i + 1) * kRowsM] = y;
+                }
+                break;                                        // a CTA has one part
+            }
             if (a.partial) {
                 float *dst = a.partial + ((long long)u * kN + set * S::kCols) * kRowsM + row_in_tile;
 #pragma unroll
@@ -252,61 +350,7 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
                 }
                 continue;
             }
-            if (row < a.rows_a) {
-                T *const out = (T *)a.out;
-                const float floor_v = a.relu ? 0.f : __int_as_float((int)0xff800000u);
-                const int cols_here = min(S::kCols, a.rows_b - col0);
-                if (!a.swapped) {
-                    long long dst = pixel_at(a, row) + (long long)col0 * a.hw;
-                    if (a.vec && cols_here == S::kCols) {
-                        constexpr int kPer = 16 / (int)sizeof(T);
-    #pragma unroll
-                        for (int i = 0; i < S::kCols; i += kPer) {
-                            float v[kPer];
-    #pragma unroll
-                            for (int j = 0; j < kPer; j += 2) {
-                                halves(sum[(i + j) / 2], v[j], v[j + 1]);
-                                if (a.bias) { v[j] += a.bias[col0 + i + j]; v[j + 1] += a.bias[col0 + i + j + 1]; }
-                                // (a NaN stays one: a comparison with it fails)
-                                v[j] = v[j] < floor_v ? floor_v : v[j];
-                                v[j + 1] = v[j + 1] < floor_v ? floor_v : v[j + 1];
-                            }
-                            __align__(16) T w[kPer];
-    #pragma unroll
-                            for (int j = 0; j < kPer; ++j) put(w, j, v[j]);
-                            *reinterpret_cast<uint4 *>(out + dst + i) = *reinterpret_cast<const uint4 *>(w);
-                        }
-                    } else {
-    #pragma unroll
-                        for (int i = 0; i < S::kCols / 2; ++i) {
-                            float x, y;
-                            halves(sum[i], x, y);
-                            if (2 * i < cols_here) {
-                                if (a.bias) x += a.bias[col0 + 2 * i];
-                                put(out, dst + (long long)(2 * i) * a.hw, x < floor_v ? floor_v : x);
-                            }
-                            if (2 * i + 1 < cols_here) {
-                                if (a.bias) y += a.bias[col0 + 2 * i + 1];
-                                put(out, dst + (long long)(2 * i + 1) * a.hw, y < floor_v ? floor_v : y);
-                            }
-                        }
-                    }
-                } else {
-                    const float bias = a.bias ? a.bias[row] : 0.f;
-                    const long long ch = (long long)row * a.hw;
-    #pragma unroll
-                    for (int i = 0; i < S::kCols / 2; ++i) {
-                        float v[2];
-                        halves(sum[i], v[0], v[1]);
-    #pragma unroll
-                        for (int j = 0; j < 2; ++j)
-                            if (2 * i + j < cols_here) {
-                                const float x = v[j] + bias;
-                                put(out, ch + pixel_at(a, col0 + 2 * i + j), x < floor_v ? floor_v : x);
-                            }
-                    }
-                }
-            }
+            store_row<T, S::kCols>(a, sum, row, col0);
             __syncwarp();
         }
         if (!alive && lane == 0) tc_dev_set_status(a.status, TC_ERR_TIMEOUT);
@@ -316,6 +360,24 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
     if (warp == S::kMma) {
         tc_fence_after_sync();
         tmem_dealloc(tmem_base, S::kTmemCols);
+    }
+    if (a.cluster) {
+        // The cluster's CTAs each add their share of the columns over all parts, in the parts' order.
+        cluster_sync();
+        const int u = blockIdx.x, rank = u % a.splits, share = (kN + a.splits - 1) / a.splits;
+        const Unit t = unit_of(a, u);
+        const int first = rank * share, end = min(kN, first + share);
+        for (int i = first * kRowsM + tid; i < end * kRowsM; i += S::kThreads) {
+            const int row = t.tile_m * kRowsM + (i & (kRowsM - 1)), col = t.tile_n * kN + (i >> 7);
+            float v = 0.f;
+            for (int part = 0; part < a.splits; ++part) {
+                float x;
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(cluster_address(ring + 4u * (uint32_t)i, (uint32_t)part)));
+                v += x;
+            }
+            store_value<T>(a, row, col, v);
+        }
+        cluster_sync();                                       // this block's shared memory is read no more
     }
 }
 
@@ -334,30 +396,204 @@ __global__ void __launch_bounds__(256) block_matmul_join_kernel(TileArgs a, int 
     a.splits = 1;
     const Unit t = unit_of(a, tile);
     const int row = t.tile_m * kRowsM + row_in_tile, col = t.tile_n * n + col_in_tile;
-    if (row >= a.rows_a || col >= a.rows_b) return;
     float v = 0.f;
     const float *src = a.partial + ((long long)tile * splits * n + col_in_tile) * kRowsM + row_in_tile;
     for (int s = 0; s < splits; ++s) v += src[(long long)s * n * kRowsM];
-    const int p = a.swapped ? col : row, o = a.swapped ? row : col;
-    if (a.bias) v += a.bias[o];
-    if (a.relu && v < 0.f) v = 0.f;
-    put((T *)a.out, pixel_at(a, p) + (long long)o * a.hw, v);
+    store_value<T>(a, row, col, v);
+}
+
+// ---- pairs of CTAs -------------------------------------------------------------------------
+template <typename T, bool kColumnScales>
+__global__ void __launch_bounds__(pair::kThreads, 1)
+block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b)
+{
+    using namespace pair;
+    extern __shared__ unsigned char smem_raw[];
+    // s_full and s_tempty are the even CTA's: both CTAs' copies and epilogues report there; s_empty and s_tfull are each CTA's own.
+    __shared__ __align__(8) unsigned long long s_full[kStages], s_empty[kStages], s_tfull[kBuffers], s_tempty[kBuffers];
+    __shared__ uint32_t s_tmem_base;
+    __shared__ __align__(16) float s_scale[kColumnScales ? kEpiWarps : 1][2][kColumnScales ? kCols : 4];
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+    const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const int rank = blockIdx.x & 1;                          // the cluster is two neighbours
+    chain_next();
+    if (tid == 0) {
+        for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
+        for (int b = 0; b < kBuffers; ++b) { mbar_init(smem_u32(&s_tfull[b]), 1); mbar_init(smem_u32(&s_tempty[b]), 2 * kEpiWarps); }
+        mbar_fence_init();
+    }
+    if (warp == kMma) { tmem_alloc_pair(smem_u32(&s_tmem_base), kTmemCols); tmem_relinquish_pair(); }
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_sync();                                           // the other CTA's barriers are there
+    tc_fence_after_sync();
+    const uint32_t tmem_base = __shfl_sync(0xffffffffu, s_tmem_base, 0);
+    chain_wait();
+    const int units = a.tiles_m * a.tiles_n, step = gridDim.x >> 1;
+
+    if (warp >= kEpiWarps) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (warp == kProducer && lane == 0) {
+            int s = 0;
+            long long issued = 0;
+            uint32_t phase = 1;
+            bool alive = true;
+            for (int u = blockIdx.x >> 1; u < units && alive; u += step) {
+                const Unit t = unit_of(a, u);
+                for (int kb = 0; kb < a.k_blocks; ++kb) {
+                    if (!mbar_wait(smem_u32(&s_empty[s]), phase)) { alive = false; break; }
+                    const uint32_t dst = ring + (uint32_t)s * kStageBytes, bar = cluster_address(smem_u32(&s_full[s]), 0);
+                    if (rank == 0) mbar_arrive_expect_tx(smem_u32(&s_full[s]), 2u * kStageBytes);
+                    tma_load_2d_pair(dst, &map_a, kb * kBlockK, t.tile_m * kRows + rank * kRowsM, bar);
+                    tma_load_2d_pair(dst + kStageA, &map_b, kb * kBlockK, t.tile_n * kN + rank * kRowsM, bar);
+                    ++issued;
+                    if (++s == kStages) { s = 0; phase ^= 1u; }
+                }
+            }
+            if (!alive) tc_dev_set_status(a.status, TC_ERR_TIMEOUT);
+            // The copies in flight land before the block ends: with every stage handed back there are none.
+            for (long long i = issued > kStages ? issued - kStages : 0; i < issued; ++i) mbar_wait(smem_u32(&s_empty[i % kStages]), (uint32_t)(i / kStages & 1));
+        } else if (warp == kMma && rank == 0) {
+            const uint32_t issuer = lane == 0 ? 1u : 0u;
+            const uint32_t idesc = make_idesc_e4m3(kRows, kN);
+            const uint64_t desc = make_smem_desc_sw128(ring, 1024);
+            const uint32_t desc_lo = (uint32_t)desc, desc_hi = (uint32_t)(desc >> 32);
+            int s = 0, b = 0;
+            uint32_t phase = 0, tphase = 1;
+            bool alive = true;
+            for (int u = blockIdx.x >> 1; u < units && alive; u += step) {
+                for (int kb = 0; kb < a.k_blocks; ++kb) {
+                    if (!mbar_wait_cluster(smem_u32(&s_tempty[b]), tphase) || !mbar_wait_cluster(smem_u32(&s_full[s]), phase)) { alive = false; break; }
+                    tc_fence_after_sync();
+                    const uint32_t a_lo = desc_lo + (uint32_t)s * (kStageBytes >> 4), b_lo = a_lo + (kStageA >> 4);
+#pragma unroll
+                    for (int q = 0; q < kBlockK / 32; ++q)
+                        mma_e4m3_ss_pair_guarded(tmem_base + b * kN, a_lo + 2 * q, desc_hi, b_lo + 2 * q, desc_hi, idesc, q ? 1u : 0u, issuer);
+                    mma_commit_pair_guarded(smem_u32(&s_empty[s]), issuer);
+                    mma_commit_pair_guarded(smem_u32(&s_tfull[b]), issuer);
+                    if (++s == kStages) { s = 0; phase ^= 1u; }
+                    if (++b == kBuffers) { b = 0; tphase ^= 1u; }
+                }
+            }
+            if (!alive && issuer) tc_dev_set_status(a.status, TC_ERR_TIMEOUT);
+        }
+        __syncwarp();
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        constexpr int kPieces = kCols / 32;
+        const int set = warp >> 2, wq = warp & 3;
+        float(*const scales)[kColumnScales ? kCols : 4] = s_scale[kColumnScales ? warp : 0];
+        uint32_t tempty[kBuffers];
+#pragma unroll
+        for (int b = 0; b < kBuffers; ++b) tempty[b] = cluster_address(smem_u32(&s_tempty[b]), 0);
+        int b = 0;
+        uint32_t tphase = 0;
+        bool alive = true;
+        for (int u = blockIdx.x >> 1; u < units && alive; u += step) {
+            const Unit t = unit_of(a, u);
+            const int row = t.tile_m * kRows + rank * kRowsM + wq * 32 + lane, col0 = t.tile_n * kN + set * kCols;
+            uint64_t sum[kCols / 2];
+#pragma unroll
+            for (int i = 0; i < kCols / 2; ++i) sum[i] = 0ull;
+            // (rows behind the last 128 have no scales: they take another's, and nothing of theirs is stored)
+            const float *at_a = a.scale_a + (a.shift_a ? min(row, a.rows_a - 1) >> 7 : min(row, (int)a.scale_a_ld - 1));
+            const float *at_b = kColumnScales ? a.scale_b + col0 + 4 * lane : a.scale_b + min(col0 >> 7, (a.rows_b - 1) >> 7);
+            const bool has_b = kColumnScales && col0 + 4 * lane < a.scale_b_ld;
+            float next_a = 0.f, next_b = 0.f;
+            float4 next_cols = make_float4(0.f, 0.f, 0.f, 0.f);
+            auto ask = [&](int kb) {
+                next_a = at_a[kb * a.scale_a_ld];
+                if constexpr (kColumnScales) {
+                    if (has_b) next_cols = *reinterpret_cast<const float4 *>(at_b + kb * a.scale_b_ld);
+                } else
+                    next_b = at_b[kb * a.scale_b_ld];
+            };
+            ask(0);
+            for (int kb = 0; kb < a.k_blocks; ++kb) {
+                const float scale = kColumnScales ? next_a : next_a * next_b;
+                float *const cols = scales[kColumnScales ? kb & 1 : 0];
+                if constexpr (kColumnScales) {
+                    *reinterpret_cast<float4 *>(cols + 4 * lane) = next_cols;
+                    __syncwarp();
+                }
+                if (kb + 1 < a.k_blocks) ask(kb + 1);
+                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&s_tfull[b]), tphase, 20u))) { alive = false; break; }
+                tc_fence_after_sync();
+                const uint32_t at = tmem_base + b * kN + set * kCols + ((uint32_t)(wq * 32) << 16);
+                const uint64_t scale2 = pair_of(scale, scale);
+                uint32_t r[2][32];
+                tmem_ld_32x32b_x32(at, r[0]);
+#pragma unroll
+                for (int i = 0; i < kPieces; ++i) {
+                    tmem_ld_wait(r[i & 1]);
+                    if (i + 1 < kPieces) tmem_ld_32x32b_x32(at + 32 * (i + 1), r[(i + 1) & 1]);
+                    else {
+                        tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_cluster(tempty[b]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const uint64_t v = pair_of(r[i & 1][2 * j], r[i & 1][2 * j + 1]);
+                        uint64_t f = scale2;
+                        if constexpr (kColumnScales) f = mul2(f, *reinterpret_cast<const uint64_t *>(cols + 32 * i + 2 * j));
+                        sum[16 * i + j] = fma2(v, f, sum[16 * i + j]);
+                    }
+                }
+                if (++b == kBuffers) { b = 0; tphase ^= 1u; }
+            }
+            if (!alive) break;
+            store_row<T, kCols>(a, sum, row, col0);
+            __syncwarp();
+        }
+        if (!alive && lane == 0) tc_dev_set_status(a.status, TC_ERR_TIMEOUT);
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_sync();                                           // nothing reports to this block any more
+    if (warp == kMma) {
+        tc_fence_after_sync();
+        tmem_dealloc_pair(tmem_base, kTmemCols);
+    }
+}
+
+// Shared memory of a kernel, asked for once on a device.
+template <auto kKernel>
+bool allow_shared(int device, size_t bytes)
+{
+    static std::atomic<unsigned long long> done{0};
+    const unsigned long long bit = device < 64 ? 1ull << device : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return true;
+    if (cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) { cudaGetLastError(); return false; }
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return true;
 }
 
 template <typename T, int kN, bool kColumnScales>
 tc_status launch_tiles(const tc_ctx *ctx, const TileArgs &a, const CUtensorMap &map_a, const CUtensorMap &map_b, cudaStream_t s)
 {
-    auto *kernel = block_matmul_kernel<T, kN, kColumnScales>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<kN>::kSmem) != cudaSuccess) { cudaGetLastError(); return TC_ERR_CUDA; }
+    constexpr auto kernel = block_matmul_kernel<T, kN, kColumnScales>;
+    if (!allow_shared<kernel>(ctx->device, Shape<kN>::kSmem)) return TC_ERR_CUDA;
     const long long units = (long long)a.tiles_m * a.tiles_n * a.splits;
-    const dim3 grid((unsigned int)(units < ctx->sm_count ? units : ctx->sm_count));
-    return launch_first(true, kernel, grid, dim3(Shape<kN>::kThreads), Shape<kN>::kSmem, s, a, map_a, map_b) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
+    const dim3 grid((unsigned int)(units < ctx->sm_count || a.cluster ? units : ctx->sm_count));
+    return launch_first_cluster(a.cluster ? a.splits : 1, kernel, grid, dim3(Shape<kN>::kThreads), Shape<kN>::kSmem, s, a, map_a, map_b) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
+}
+
+template <typename T, bool kColumnScales>
+tc_status launch_pairs(const tc_ctx *ctx, const TileArgs &a, const CUtensorMap &map_a, const CUtensorMap &map_b, cudaStream_t s)
+{
+    constexpr auto kernel = block_matmul_pair_kernel<T, kColumnScales>;
+    if (!allow_shared<kernel>(ctx->device, pair::kSmem)) return TC_ERR_CUDA;
+    const long long units = (long long)a.tiles_m * a.tiles_n, pairs = ctx->sm_count / 2;
+    const dim3 grid((unsigned int)(2 * (units < pairs ? units : pairs)));
+    return launch_first_cluster(2, kernel, grid, dim3(pair::kThreads), pair::kSmem, s, a, map_a, map_b) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
 
 template <typename T>
-tc_status launch(const tc_ctx *ctx, const TileArgs &a, int n, const CUtensorMap &map_a, const CUtensorMap &map_b, cudaStream_t s)
+tc_status launch(const tc_ctx *ctx, const TileArgs &a, bool pairs, int n, const CUtensorMap &map_a, const CUtensorMap &map_b, cudaStream_t s)
 {
     const bool cols = a.shift_b == 0;
+    if (pairs) return cols ? launch_pairs<T, true>(ctx, a, map_a, map_b, s) : launch_pairs<T, false>(ctx, a, map_a, map_b, s);
     switch (n) {
     case 16: return cols ? launch_tiles<T, 16, true>(ctx, a, map_a, map_b, s) : TC_ERR_UNSUPPORTED;
     case 32: return cols ? launch_tiles<T, 32, true>(ctx, a, map_a, map_b, s) : TC_ERR_UNSUPPORTED;
@@ -374,29 +610,36 @@ MatmulPlan tc_plan_matmul(const MatmulArgs &a, int sm_count)
     MatmulPlan best;
     const int k_blocks = (a.cols + kBlockK - 1) / kBlockK;
     double best_cost = 0.0;
-    for (int swapped = 0; swapped < 2; ++swapped) {
+    auto consider = [&](bool swapped, bool pairs, int n) {
         const MatmulOperand &m = swapped ? a.channels : a.pixels, &c = swapped ? a.pixels : a.channels;
-        for (int n = 16; n <= 256; n *= 2) {
-            if (n < 64 && (!swapped || c.square)) continue;
-            const long long tiles = (long long)((m.rows + kRowsM - 1) / kRowsM) * ((c.rows + n - 1) / n);
-            int splits = 1;
-            if (tiles * 2 <= sm_count && k_blocks > 1) splits = (int)(sm_count / tiles < (k_blocks + 1) / 2 ? sm_count / tiles : (k_blocks + 1) / 2);
-            const long long rounds = (tiles * splits + sm_count - 1) / sm_count;
-            // a block's cycles: its operands from L2, or its sums; a tile's: its store
-            const double load = (kRowsM + n) * 2.6, add = n * (c.square ? 2.2 : 4.2);
-            const double cost = (double)rounds * ((double)((k_blocks + splits - 1) / splits) * (load > add ? load : add) + 600 + 8 * n) +
-                                (splits > 1 ? 3000 + (double)tiles * splits * n * 0.5 : 0);
-            if (best.n == 0 || cost < best_cost) {
-                best_cost = cost;
-                best.swapped = swapped;
-                best.n = n;
-                best.splits = splits;
-                best.tiles = tiles;
-                best.workspace = splits > 1 ? (size_t)tiles * splits * n * kRowsM * sizeof(float) : 0;
-            }
+        const int rows = pairs ? pair::kRows : kRowsM, workers = pairs ? sm_count / 2 : sm_count;
+        const long long tiles = (long long)((m.rows + rows - 1) / rows) * ((c.rows + n - 1) / n);
+        int splits = 1;
+        if (!pairs && tiles * 2 <= sm_count && k_blocks > 1) splits = (int)(sm_count / tiles < (k_blocks + 1) / 2 ? sm_count / tiles : (k_blocks + 1) / 2);
+        if (splits > 8 && splits < 17) splits = 8;
+        const bool cluster = splits > 1 && splits <= 8;
+        const long long rounds = (tiles * splits + workers - 1) / workers;
+        // a block's cycles: its operands from L2, or its sums; a tile's: its store
+        const double load = pairs ? 870 : (kRowsM + n) * 3.4, add = n * (c.square ? 3.2 : pairs ? 4.5 : 9.6);
+        const double cost = (double)rounds * ((double)((k_blocks + splits - 1) / splits) * (load > add ? load : add) + 600 + 8 * n) +
+                            (cluster ? 2000 + n * 16 : splits > 1 ? 6000 + (double)tiles * splits * n * 0.5 : 0);
+        if (best.n == 0 || cost < best_cost) {
+            best_cost = cost;
+            best.swapped = swapped;
+            best.pairs = pairs;
+            best.n = n;
+            best.splits = splits;
+            best.cluster = cluster;
+            best.tiles = tiles;
+            best.workspace = splits > 1 && !cluster ? (size_t)tiles * splits * n * kRowsM * sizeof(float) : 0;
         }
+    };
+    for (int swapped = 0; swapped < 2; ++swapped) {
+        for (int n = 16; n <= 256; n *= 2)
+            if (n >= 64 || (swapped && !a.pixels.square)) consider(swapped, false, n);
+        if (sm_count > 1) consider(swapped, true, pair::kN);
     }
-    if (k_blocks == 0) { best.splits = 0; best.workspace = 0; }
+    if (k_blocks == 0) { best.splits = 0; best.pairs = best.cluster = false; best.workspace = 0; }
     return best;
 }
 
@@ -408,7 +651,10 @@ tc_status tc_launch_matmul_blocks(const tc_ctx *ctx, const MatmulArgs &m, const 
     a.rows_b = rb.rows;
     a.k_blocks = (m.cols + kBlockK - 1) / kBlockK;
     a.splits = plan.splits;
-    a.tiles_m = (ra.rows + kRowsM - 1) / kRowsM;
+    const int rows_tile = plan.pairs ? pair::kRows : kRowsM;
+    a.tiles_m = (ra.rows + rows_tile - 1) / rows_tile;
+    a.group = plan.pairs ? 8 : 16;
+    a.cluster = plan.cluster;
     a.tiles_n = (rb.rows + plan.n - 1) / plan.n;
     a.scale_a = ra.m.scales;
     a.scale_b = rb.m.scales;
@@ -423,14 +669,14 @@ tc_status tc_launch_matmul_blocks(const tc_ctx *ctx, const MatmulArgs &m, const 
     a.vec = m.hw == 1 && !plan.swapped && ((uintptr_t)m.out & 15u) == 0 && m.channels.rows % (m.dtype == TC_BF16 ? 8 : 4) == 0;
     a.bias = m.bias;
     a.out = m.out;
-    a.partial = plan.splits != 1 ? (float *)workspace : nullptr;
+    a.partial = plan.workspace ? (float *)workspace : nullptr;
     a.status = m.status;
     if (plan.splits > 0) {
         CUtensorMap map_a, map_b;
         if (!tc_tensor_map_codes(&map_a, ra.m.codes, ra.rows, m.cols, ra.m.ld, kRowsM) ||
-            !tc_tensor_map_codes(&map_b, rb.m.codes, rb.rows, m.cols, rb.m.ld, plan.n)) return TC_ERR_CUDA;
-        const tc_status st = m.dtype == TC_BF16 ? launch<__nv_bfloat16>(ctx, a, plan.n, map_a, map_b, s) : launch<float>(ctx, a, plan.n, map_a, map_b, s);
-        if (st != TC_OK || plan.splits == 1) return st;
+            !tc_tensor_map_codes(&map_b, rb.m.codes, rb.rows, m.cols, rb.m.ld, plan.pairs ? kRowsM : plan.n)) return TC_ERR_CUDA;
+        const tc_status st = m.dtype == TC_BF16 ? launch<__nv_bfloat16>(ctx, a, plan.pairs, plan.n, map_a, map_b, s) : launch<float>(ctx, a, plan.pairs, plan.n, map_a, map_b, s);
+        if (st != TC_OK || !a.partial) return st;
     }
     const long long values = (long long)a.tiles_m * a.tiles_n * plan.n * kRowsM;
     const dim3 grid((unsigned int)((values + 255) / 256));

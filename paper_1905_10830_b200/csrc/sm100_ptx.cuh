@@ -1,7 +1,7 @@
 // Thin wrappers over the sm_100a PTX used by the tensor-core kernels: mbarriers with bounded
 // waits, cp.async, tcgen05 (TMEM allocation, MMA, commit, loads) and the shared-memory matrix
-// descriptors, tiled TMA loads.  Everything here is cta_group::1 (one CTA per tile, no clusters,
-// no multicast).
+// descriptors, tiled TMA loads.  Everything here is cta_group::1 (one CTA per tile) but for the section on
+// pairs of CTAs at the end; no load is multicast.
 #pragma once
 
 #include <stdint.h>
@@ -417,6 +417,80 @@ __device__ __forceinline__ void mma_commit_guarded(uint32_t bar, uint32_t issue)
 __device__ __forceinline__ void mma_commit(uint32_t bar)
 {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// ---- pairs of CTAs (a cluster's two neighbours share one MMA; the even one issues it) ---------------
+// Each holds its half of the rows of A and of B in its shared memory, at the same offsets, and its rows of D in its
+// tensor memory.  A kernel uses either these or the forms above.
+__device__ __forceinline__ uint32_t cluster_address(uint32_t smem_addr, uint32_t rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+// mbar_wait for a barrier on which threads of the other CTA arrive.
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity)
+{
+    unsigned long long t0 = 0, t1;
+    for (int i = 0;; ++i) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok) : "r"(bar), "r"(parity), "r"(i ? 100000u : 0u) : "memory");
+        if (ok) return true;
+        if ((i & 63) == 0) {
+            asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t1));
+            if (i == 0) t0 = t1;
+            else if (t1 - t0 > 2000000000ull) return false;
+        }
+    }
+}
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t smem_result, uint32_t columns)
+{
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_result), "r"(columns) : "memory");
+}
+__device__ __forceinline__ void tmem_relinquish_pair() { asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t columns)
+{
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(columns) : "memory");
+}
+// As tma_load_2d, into this CTA's shared memory; the bytes are counted on `cluster_bar`, a barrier of either CTA of the pair.
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t smem_dst, const void *tensor_map, int x, int y, uint32_t cluster_bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(smem_dst), "l"(tensor_map), "r"(x), "r"(y), "r"(cluster_bar)
+        : "memory");
+}
+__device__ __forceinline__ void mma_e4m3_ss_pair_guarded(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi,
+                                                         uint32_t idesc, uint32_t accumulate, uint32_t issue)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, g;\n\t.reg .b64 ad, bd;\n\t"
+        "mov.b64 ad, {%1, %2};\n\t"
+        "mov.b64 bd, {%3, %4};\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "setp.ne.b32 g, %7, 0;\n\t"
+        "@g tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], ad, bd, %5, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(issue)
+        : "memory");
+}
+// One arrival on the barrier at this offset in both CTAs when the MMAs issued so far have finished.
+__device__ __forceinline__ void mma_commit_pair_guarded(uint32_t bar, uint32_t issue)
+{
+    asm volatile(
+        "{\n\t.reg .pred g;\n\t.reg .b16 m;\n\t"
+        "setp.ne.b32 g, %1, 0;\n\t"
+        "mov.b16 m, 3;\n\t"
+        "@g tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t}"
+        ::"r"(bar), "r"(issue)
+        : "memory");
 }
 
 }  // namespace sm100

@@ -1916,7 +1916,7 @@ tc_status tc_matmul_blocks(tc_ctx *ctx, const tc_blocks *a, const tc_blocks *b, 
     CallScratch scratch;
     const tc_status st = call_scratch(ctx, 0, plan.workspace, (cudaStream_t)cuda_stream, &scratch);
     if (st != TC_OK) return st;
-    if (plan.workspace && !scratch.at) plan.splits = 1;
+    if (plan.workspace && !scratch.at) { plan.splits = 1; plan.workspace = 0; }
     return tc_launch_matmul_blocks(ctx, args, plan, scratch.at, (cudaStream_t)cuda_stream);
 }
 

@@ -239,6 +239,25 @@ inline cudaError_t launch_first(bool alone, void (*kernel)(P...), dim3 grid, dim
     return launch_chained(alone && capture == cudaStreamCaptureStatusNone, kernel, grid, block, smem, s, std::forward<A>(args)...);
 }
 
+// launch_first in clusters of `blocks` neighbours along the grid's first dimension.
+template <typename... P, typename... A>
+inline cudaError_t launch_first_cluster(int blocks, void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, A &&...args)
+{
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(s, &capture) != cudaSuccess) { cudaGetLastError(); capture = cudaStreamCaptureStatusActive; }
+    cudaLaunchAttribute attr[2] = {};
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned int)blocks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = s;
+    cfg.attrs = attr; cfg.numAttrs = capture == cudaStreamCaptureStatusNone ? 2 : 1;
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
+    if (err != cudaSuccess) cudaGetLastError();
+    return err;
+}
+
 // launch_chained, always early, in clusters of `blocks` along the grid's second dimension.
 template <typename... P, typename... A>
 inline cudaError_t launch_chained_cluster(int blocks, void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, A &&...args)
@@ -312,6 +331,8 @@ struct MatmulArgs {
 // How a product is cut into the units of its kernel.
 struct MatmulPlan {
     bool swapped = false;             // rows of the MMA are channels
+    bool pairs = false;               // tiles of 256 x 256, by pairs of CTAs
+    bool cluster = false;             // the parts are a cluster's CTAs
     int n = 0;                        // columns of a tile (its rows: 128)
     int splits = 1;                   // parts of the sums' length
     long long tiles = 0;

@@ -142,7 +142,8 @@ def _check_product(out, a, b, bias=None, relu=False, shape=None):
 
 PRODUCTS = [(1, 1, 1), (1, 128, 16), (3, 200, 5), (17, 129, 127), (128, 128, 256), (130, 384, 257), (64, 4096, 300), (257, 1000, 640),
             (1, 4096, 4096), (2, 960, 1000), (33, 512, 2048), (100, 320, 96), (1000, 64, 64), (3000, 130, 130), (16, 16, 20000),
-            (20000, 48, 40), (500, 2000, 500)]
+            (20000, 48, 40), (500, 2000, 500),
+            (2100, 300, 1300), (1500, 1000, 2000), (4096, 130, 4096)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -155,7 +156,8 @@ def test_product(ctx, p, k, o, squares, dtype):
         _check_product(tc.tc_matmul_blocks(ctx, a, b, dtype=dtype, bias=bias, relu=relu), a, b, bias, relu)
 
 
-@pytest.mark.parametrize("n,h,w,k,o", [(37, 7, 7, 320, 96), (3, 14, 14, 256, 257), (1, 5, 7, 64, 300), (700, 2, 3, 48, 16), (1, 1, 333, 96, 128), (2, 56, 56, 24, 144)])
+@pytest.mark.parametrize("n,h,w,k,o", [(37, 7, 7, 320, 96), (3, 14, 14, 256, 257), (1, 5, 7, 64, 300), (700, 2, 3, 48, 16), (1, 1, 333, 96, 128), (2, 56, 56, 24, 144),
+                                       (40, 7, 7, 200, 1100)])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_product_into_maps(ctx, n, h, w, k, o, dtype):
     x = _values((n, k, h, w), 7, dtype)
@@ -171,7 +173,8 @@ def test_product_into_maps(ctx, n, h, w, k, o, dtype):
     assert torch.equal(one, out)
 
 
-@pytest.mark.parametrize("o,c,n,hw", [(40, 56, 3000, 1), (130, 257, 40, 49), (256, 128, 20000, 1), (16, 16, 70000, 1), (300, 520, 1, 1)])
+@pytest.mark.parametrize("o,c,n,hw", [(40, 56, 3000, 1), (130, 257, 40, 49), (256, 128, 20000, 1), (16, 16, 70000, 1), (300, 520, 1, 1),
+                                       (2048, 1500, 700, 1)])
 def test_gradient_of_weights(ctx, o, c, n, hw):
     """Long sums with a scale for each row on both sides, taken in parts where the output is small."""
     side = math.isqrt(hw)
