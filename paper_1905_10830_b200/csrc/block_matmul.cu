@@ -10,7 +10,7 @@
 // shared memory.  With one CTA on a tile of 128 x 256 the operands' way from L2 bounds the kernel (48 KB a block and SM against 32).
 // Small ones: one CTA walks tiles of 128 rows x 16 to 256 columns; where tiles are fewer than SMs the sums' length is cut into
 // parts, by the CTAs of a cluster that add through their shared memory, or, for very long sums, through a workspace.
-#include "device_utils.cuh"
+#include "block_codes.cuh"
 #include "sm100_ptx.cuh"
 #include "tc_internal.h"
 
@@ -39,11 +39,12 @@ template <int kN> struct Shape {
 // Tiles of a pair of CTAs: 256 x 256, 128 rows of each operand a CTA.
 namespace pair {
 constexpr int kN = 256, kRows = 256;
-constexpr int kStageBytes = 2 * kStageA, kStages = kRing / kStageBytes, kBuffers = 2, kTmemCols = 512;
+constexpr int kStageBytes = 2 * kStageA, kStages = 5, kBuffers = 2, kTmemCols = 512;
 constexpr int kSets = 2, kCols = kN / kSets;
+constexpr int kStoreBytes = 4096;                             // a warp's box of a TMA store: 32 rows of 128 bytes
 constexpr int kEpiWarps = 8, kProducer = 8, kMma = 9;         // warps 10 and 11 only give registers away
 constexpr int kThreads = 12 * 32;
-constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes;
+constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpiWarps * kStoreBytes;
 // Registers: 384 threads are launched with 168 each; 256 x 216 + 128 x 72 is the same sum.
 }
 
@@ -57,6 +58,7 @@ struct TileArgs {
     int group;                        // tile rows that are worked on together
     int swapped, cluster;             // cluster: the parts of a tile's length are a cluster's CTAs
     int out_channels, hw, relu, vec;
+    int store_tma;                    // pairs: the output's rows leave by TMA copies
     const float *bias;
     void *out;
     float *partial;                   // [unit][column][128 rows], where the length is split
@@ -189,6 +191,74 @@ __device__ __forceinline__ void store_row(const TileArgs &a, const uint64_t (&su
     }
 }
 
+__device__ __forceinline__ void tmem_ld(uint32_t at, uint32_t (&r)[16]) { tmem_ld_32x32b_x16(at, r); }
+__device__ __forceinline__ void tmem_ld(uint32_t at, uint32_t (&r)[32]) { tmem_ld_32x32b_x32(at, r); }
+
+// Adds a piece of a row's block, kN columns, times the row's scale and the columns'.
+template <int kN, bool kColumnScales>
+__device__ __forceinline__ void add_scaled(uint64_t *sum, const uint32_t *r, uint64_t scale2, const float *cols)
+{
+#pragma unroll
+    for (int j = 0; j < kN / 2; j += 2) {
+        uint64_t f = scale2, g = scale2;
+        if constexpr (kColumnScales) {
+            const float4 c = *reinterpret_cast<const float4 *>(cols + 2 * j);
+            f = mul2(f, pair_of(c.x, c.y));
+            g = mul2(g, pair_of(c.z, c.w));
+        }
+        sum[j] = fma2(pair_of(r[2 * j], r[2 * j + 1]), f, sum[j]);
+        sum[j + 1] = fma2(pair_of(r[2 * j + 2], r[2 * j + 3]), g, sum[j + 1]);
+    }
+}
+
+// The scales of the next blocks on their way to shared memory, for one epilogue warp: of its rows (a lane's own), and either of its kCols
+// columns or the one they share.  Asked for three blocks ahead: they come from L2, in 400 ns and more, and with the registers of one
+// block ahead a block took as long as that (8192x4096 to 8192: 265 us and 205).
+constexpr int kAhead = 3, kScaleSlots = kAhead + 1;
+template <int kCols, bool kColumnScales>
+struct ScaleRing {
+    static constexpr int kSlot = kColumnScales ? 32 + kCols : 64;                  // floats
+    float *slots;
+    const float *at_a, *at_b;
+    long long ld_a, ld_b;
+    bool has_b;
+    int end;
+    __device__ __forceinline__ void ask(int kb, int lane)
+    {
+        if (kb < end) {
+            float *const slot = slots + (kb % kScaleSlots) * kSlot;
+            cp_async_4(smem_u32(slot + lane), at_a + kb * ld_a);
+            if constexpr (kColumnScales) {
+                if (has_b) cp_async_16(smem_u32(slot + 32 + 4 * lane), at_b + kb * ld_b, 16u);
+            } else
+                cp_async_4(smem_u32(slot + 32 + lane), at_b + kb * ld_b);
+        }
+        cp_async_commit();
+    }
+    // Of a tile's row and columns, blocks [first, end_).
+    __device__ __forceinline__ void start(const TileArgs &a, int row, int col0, int first, int end_, int lane)
+    {
+        // (rows behind the last 128 have no scales: they take another's, and nothing of theirs is stored)
+        at_a = a.scale_a + (a.shift_a ? min(row, a.rows_a - 1) >> 7 : min(row, (int)a.scale_a_ld - 1));
+        at_b = kColumnScales ? a.scale_b + col0 + 4 * lane : a.scale_b + min(col0 >> 7, (a.rows_b - 1) >> 7);
+        has_b = 4 * lane < kCols && col0 + 4 * lane < a.scale_b_ld;
+        ld_a = a.scale_a_ld;
+        ld_b = a.scale_b_ld;
+        end = end_;
+        __syncwarp();                                         // the last tile's readers
+        for (int i = 0; i < kAhead; ++i) ask(first + i, lane);
+    }
+    // The block's scales are there (and those of block kb + kAhead asked for).
+    __device__ __forceinline__ const float *next(int kb, int lane)
+    {
+        __syncwarp();                                         // the slot's readers
+        ask(kb + kAhead, lane);
+        cp_async_wait<kAhead>();
+        __syncwarp();
+        return slots + (kb % kScaleSlots) * kSlot;
+    }
+};
+
 // kColumnScales: B has a scale for each row (a column of the tile), else one for each 128.
 template <typename T, int kN, bool kColumnScales>
 __global__ void __launch_bounds__(Shape<kN>::kThreads, 1)
@@ -198,7 +268,7 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) unsigned long long s_full[S::kStages], s_empty[S::kStages], s_tfull[S::kBuffers], s_tempty[S::kBuffers];
     __shared__ uint32_t s_tmem_base;
-    __shared__ __align__(16) float s_scale[kColumnScales ? S::kEpiWarps : 1][2][kColumnScales ? S::kCols : 4];
+    __shared__ __align__(16) float s_scales[S::kEpiWarps][kScaleSlots * ScaleRing<S::kCols, kColumnScales>::kSlot];
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
     chain_next();
@@ -224,7 +294,7 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
             for (int u = blockIdx.x; u < units && alive; u += gridDim.x) {
                 const Unit t = unit_of(a, u);
                 for (int kb = t.k_first; kb < t.k_end; ++kb) {
-                    if (!mbar_wait(smem_u32(&s_empty[s]), phase)) { alive = false; break; }
+                    if (!mbar_wait_soon(smem_u32(&s_empty[s]), phase)) { alive = false; break; }
                     const uint32_t bar = smem_u32(&s_full[s]), dst = ring + (uint32_t)s * S::kStageBytes;
                     mbar_arrive_expect_tx(bar, (uint32_t)S::kStageBytes);
                     tma_load_2d(dst, &map_a, kb * kBlockK, t.tile_m * kRowsM, bar);
@@ -237,7 +307,7 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
                 tc_dev_set_status(a.status, TC_ERR_TIMEOUT);
                 // the copies in flight land before the block's shared memory goes to another
                 const long long first = issued > S::kStages ? issued - S::kStages : 0;
-                for (long long i = first; i < issued; ++i) mbar_wait(smem_u32(&s_full[i % S::kStages]), (uint32_t)(i / S::kStages & 1));
+                for (long long i = first; i < issued; ++i) mbar_wait_soon(smem_u32(&s_full[i % S::kStages]), (uint32_t)(i / S::kStages & 1));
             }
         }
     } else if (warp == S::kMma) {
@@ -251,7 +321,7 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
         for (int u = blockIdx.x; u < units && alive; u += gridDim.x) {
             const Unit t = unit_of(a, u);
             for (int kb = t.k_first; kb < t.k_end; ++kb) {
-                if (!mbar_wait(smem_u32(&s_tempty[b]), tphase) || !mbar_wait(smem_u32(&s_full[s]), phase)) { alive = false; break; }
+                if (!mbar_wait_soon(smem_u32(&s_tempty[b]), tphase) || !mbar_wait_soon(smem_u32(&s_full[s]), phase)) { alive = false; break; }
                 tc_fence_after_sync();
                 const uint32_t a_lo = desc_lo + (uint32_t)s * (S::kStageBytes >> 4), b_lo = a_lo + (kStageA >> 4);
 #pragma unroll
@@ -268,7 +338,8 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
         constexpr int kPieces = S::kCols / 16;
         const int set = warp >> 2, wq = warp & 3;
         const int row_in_tile = wq * 32 + lane;
-        float(*const scales)[kColumnScales ? S::kCols : 4] = s_scale[kColumnScales ? warp : 0];
+        ScaleRing<S::kCols, kColumnScales> scales;
+        scales.slots = s_scales[warp];
         int b = 0;
         uint32_t tphase = 0;
         bool alive = true;
@@ -278,30 +349,12 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
             uint64_t sum[S::kCols / 2];
 #pragma unroll
             for (int i = 0; i < S::kCols / 2; ++i) sum[i] = 0ull;
-            // the scales of a block are asked for while the block before it is added
-            const float *at_a = a.scale_a + (row >> a.shift_a);
-            const float *at_b = kColumnScales ? a.scale_b + col0 + 4 * lane : a.scale_b + min(col0 >> 7, (a.rows_b - 1) >> 7);
-            const bool has_b = kColumnScales && 4 * lane < S::kCols && col0 + 4 * lane < a.scale_b_ld;
-            float next_a = 0.f, next_b = 0.f;
-            float4 next_cols = make_float4(0.f, 0.f, 0.f, 0.f);
-            auto ask = [&](int kb) {
-                next_a = at_a[kb * a.scale_a_ld];
-                if constexpr (kColumnScales) {
-                    if (has_b) next_cols = *reinterpret_cast<const float4 *>(at_b + kb * a.scale_b_ld);
-                } else
-                    next_b = at_b[kb * a.scale_b_ld];
-            };
-            if (t.k_first < t.k_end) ask(t.k_first);
+            scales.start(a, row, col0, t.k_first, t.k_end, lane);
             for (int kb = t.k_first; kb < t.k_end; ++kb) {
-                const float scale = kColumnScales ? next_a : next_a * next_b;
-                float *const cols = scales[kColumnScales ? kb & 1 : 0];
-                if constexpr (kColumnScales) {
-                    if (4 * lane < S::kCols) *reinterpret_cast<float4 *>(cols + 4 * lane) = next_cols;
-                    __syncwarp();
-                }
-                if (kb + 1 < t.k_end) ask(kb + 1);
+                const float *const here = scales.next(kb, lane);
+                const float scale = kColumnScales ? here[lane] : here[lane] * here[32 + lane];
                 // (asked of the whole warp: what follows is done by all its lanes together)
-                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&s_tfull[b]), tphase, 20u))) { alive = false; break; }
+                if (!__all_sync(0xffffffffu, mbar_wait_soon(smem_u32(&s_tfull[b]), tphase))) { alive = false; break; }
                 tc_fence_after_sync();
                 const uint32_t at = tmem_base + b * kN + set * S::kCols + ((uint32_t)(wq * 32) << 16);
                 const uint64_t scale2 = pair_of(scale, scale);
@@ -316,13 +369,7 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
                         __syncwarp();
                         if (lane == 0) mbar_arrive(smem_u32(&s_tempty[b]));
                     }
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const uint64_t v = pair_of(r[i & 1][2 * j], r[i & 1][2 * j + 1]);
-                        uint64_t f = scale2;
-                        if constexpr (kColumnScales) f = mul2(f, *reinterpret_cast<const uint64_t *>(cols + 16 * i + 2 * j));
-                        sum[8 * i + j] = fma2(v, f, sum[8 * i + j]);
-                    }
+                    add_scaled<16, kColumnScales>(&sum[8 * i], r[i & 1], scale2, here + 32 + 16 * i);
                 }
                 if (++b == S::kBuffers) { b = 0; tphase ^= 1u; }
             }
@@ -405,14 +452,15 @@ __global__ void __launch_bounds__(256) block_matmul_join_kernel(TileArgs a, int 
 // ---- pairs of CTAs -------------------------------------------------------------------------
 template <typename T, bool kColumnScales>
 __global__ void __launch_bounds__(pair::kThreads, 1)
-block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b)
+block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                         const __grid_constant__ CUtensorMap map_out)
 {
     using namespace pair;
     extern __shared__ unsigned char smem_raw[];
     // s_full and s_tempty are the even CTA's: both CTAs' copies and epilogues report there; s_empty and s_tfull are each CTA's own.
     __shared__ __align__(8) unsigned long long s_full[kStages], s_empty[kStages], s_tfull[kBuffers], s_tempty[kBuffers];
     __shared__ uint32_t s_tmem_base;
-    __shared__ __align__(16) float s_scale[kColumnScales ? kEpiWarps : 1][2][kColumnScales ? kCols : 4];
+    __shared__ __align__(16) float s_scales[kEpiWarps][kScaleSlots * ScaleRing<kCols, kColumnScales>::kSlot];
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int rank = blockIdx.x & 1;                          // the cluster is two neighbours
@@ -441,7 +489,7 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
             for (int u = blockIdx.x >> 1; u < units && alive; u += step) {
                 const Unit t = unit_of(a, u);
                 for (int kb = 0; kb < a.k_blocks; ++kb) {
-                    if (!mbar_wait(smem_u32(&s_empty[s]), phase)) { alive = false; break; }
+                    if (!mbar_wait_soon(smem_u32(&s_empty[s]), phase)) { alive = false; break; }
                     const uint32_t dst = ring + (uint32_t)s * kStageBytes, bar = cluster_address(smem_u32(&s_full[s]), 0);
                     if (rank == 0) mbar_arrive_expect_tx(smem_u32(&s_full[s]), 2u * kStageBytes);
                     tma_load_2d_pair(dst, &map_a, kb * kBlockK, t.tile_m * kRows + rank * kRowsM, bar);
@@ -452,7 +500,7 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
             }
             if (!alive) tc_dev_set_status(a.status, TC_ERR_TIMEOUT);
             // The copies in flight land before the block ends: with every stage handed back there are none.
-            for (long long i = issued > kStages ? issued - kStages : 0; i < issued; ++i) mbar_wait(smem_u32(&s_empty[i % kStages]), (uint32_t)(i / kStages & 1));
+            for (long long i = issued > kStages ? issued - kStages : 0; i < issued; ++i) mbar_wait_soon(smem_u32(&s_empty[i % kStages]), (uint32_t)(i / kStages & 1));
         } else if (warp == kMma && rank == 0) {
             const uint32_t issuer = lane == 0 ? 1u : 0u;
             const uint32_t idesc = make_idesc_e4m3(kRows, kN);
@@ -463,14 +511,14 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
             bool alive = true;
             for (int u = blockIdx.x >> 1; u < units && alive; u += step) {
                 for (int kb = 0; kb < a.k_blocks; ++kb) {
-                    if (!mbar_wait_cluster(smem_u32(&s_tempty[b]), tphase) || !mbar_wait_cluster(smem_u32(&s_full[s]), phase)) { alive = false; break; }
+                    if (!mbar_wait_soon(smem_u32(&s_full[s]), phase) || !mbar_wait_soon(smem_u32(&s_tempty[b]), tphase)) { alive = false; break; }
                     tc_fence_after_sync();
                     const uint32_t a_lo = desc_lo + (uint32_t)s * (kStageBytes >> 4), b_lo = a_lo + (kStageA >> 4);
 #pragma unroll
                     for (int q = 0; q < kBlockK / 32; ++q)
                         mma_e4m3_ss_pair_guarded(tmem_base + b * kN, a_lo + 2 * q, desc_hi, b_lo + 2 * q, desc_hi, idesc, q ? 1u : 0u, issuer);
-                    mma_commit_pair_guarded(smem_u32(&s_empty[s]), issuer);
                     mma_commit_pair_guarded(smem_u32(&s_tfull[b]), issuer);
+                    mma_commit_pair_guarded(smem_u32(&s_empty[s]), issuer);
                     if (++s == kStages) { s = 0; phase ^= 1u; }
                     if (++b == kBuffers) { b = 0; tphase ^= 1u; }
                 }
@@ -480,72 +528,145 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
         __syncwarp();
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-        constexpr int kPieces = kCols / 32;
         const int set = warp >> 2, wq = warp & 3;
-        float(*const scales)[kColumnScales ? kCols : 4] = s_scale[kColumnScales ? warp : 0];
+        ScaleRing<kCols, kColumnScales> scales;
+        scales.slots = s_scales[warp];
+        const uint32_t box = ring + kStages * kStageBytes + warp * kStoreBytes;
+        const float floor_v = a.relu ? 0.f : __int_as_float((int)0xff800000u);
         uint32_t tempty[kBuffers];
 #pragma unroll
         for (int b = 0; b < kBuffers; ++b) tempty[b] = cluster_address(smem_u32(&s_tempty[b]), 0);
         int b = 0;
         uint32_t tphase = 0;
         bool alive = true;
+        // With scales for the columns a thread reads the fragments' layout, four rows and every fourth pair of columns: 32
+        // columns' scales, where a row's thread has 128 to fetch, which shared memory's 128 bytes a cycle do not give in a block's time
+        // (4096x4096 over 16384: 442 us and 285).
+        const int i = lane >> 2, q = lane & 3;                // row 8 k + i, columns 8 g + 2 q and the next
         for (int u = blockIdx.x >> 1; u < units && alive; u += step) {
             const Unit t = unit_of(a, u);
-            const int row = t.tile_m * kRows + rank * kRowsM + wq * 32 + lane, col0 = t.tile_n * kN + set * kCols;
-            uint64_t sum[kCols / 2];
+            const int first_row = t.tile_m * kRows + rank * kRowsM + wq * 32, col0 = t.tile_n * kN + set * kCols;
+            uint64_t sum[kCols / 2];                          // of a row's columns, or [row k][32 columns' pairs]
 #pragma unroll
-            for (int i = 0; i < kCols / 2; ++i) sum[i] = 0ull;
-            // (rows behind the last 128 have no scales: they take another's, and nothing of theirs is stored)
-            const float *at_a = a.scale_a + (a.shift_a ? min(row, a.rows_a - 1) >> 7 : min(row, (int)a.scale_a_ld - 1));
-            const float *at_b = kColumnScales ? a.scale_b + col0 + 4 * lane : a.scale_b + min(col0 >> 7, (a.rows_b - 1) >> 7);
-            const bool has_b = kColumnScales && col0 + 4 * lane < a.scale_b_ld;
-            float next_a = 0.f, next_b = 0.f;
-            float4 next_cols = make_float4(0.f, 0.f, 0.f, 0.f);
-            auto ask = [&](int kb) {
-                next_a = at_a[kb * a.scale_a_ld];
-                if constexpr (kColumnScales) {
-                    if (has_b) next_cols = *reinterpret_cast<const float4 *>(at_b + kb * a.scale_b_ld);
-                } else
-                    next_b = at_b[kb * a.scale_b_ld];
-            };
-            ask(0);
+            for (int j = 0; j < kCols / 2; ++j) sum[j] = 0ull;
+            scales.start(a, first_row + lane, col0, 0, a.k_blocks, lane);
             for (int kb = 0; kb < a.k_blocks; ++kb) {
-                const float scale = kColumnScales ? next_a : next_a * next_b;
-                float *const cols = scales[kColumnScales ? kb & 1 : 0];
+                const float *const here = scales.next(kb, lane);
+                uint64_t scale2[kColumnScales ? 4 : 1];
                 if constexpr (kColumnScales) {
-                    *reinterpret_cast<float4 *>(cols + 4 * lane) = next_cols;
-                    __syncwarp();
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) scale2[k] = pair_of(here[8 * k + i], here[8 * k + i]);
+                } else {
+                    const float scale = here[lane] * here[32 + lane];
+                    scale2[0] = pair_of(scale, scale);
                 }
-                if (kb + 1 < a.k_blocks) ask(kb + 1);
-                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&s_tfull[b]), tphase, 20u))) { alive = false; break; }
+                // (asked of the whole warp: what follows is done by all its lanes together)
+                if (!__all_sync(0xffffffffu, mbar_wait_soon(smem_u32(&s_tfull[b]), tphase))) { alive = false; break; }
                 tc_fence_after_sync();
                 const uint32_t at = tmem_base + b * kN + set * kCols + ((uint32_t)(wq * 32) << 16);
-                const uint64_t scale2 = pair_of(scale, scale);
-                uint32_t r[2][32];
-                tmem_ld_32x32b_x32(at, r[0]);
+                auto hand_back = [&] {
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(tempty[b]);
+                };
+                if constexpr (kColumnScales) {
+                    uint32_t r[2][16];
+                    uint64_t c[4];
+                    tmem_ld_16x256b_x4(at, r[0]);
 #pragma unroll
-                for (int i = 0; i < kPieces; ++i) {
-                    tmem_ld_wait(r[i & 1]);
-                    if (i + 1 < kPieces) tmem_ld_32x32b_x32(at + 32 * (i + 1), r[(i + 1) & 1]);
-                    else {
-                        tc_fence_before_sync();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive_cluster(tempty[b]);
+                    for (int n = 0; n < kCols / 16; ++n) {    // 32 columns, their first 16 rows, then their last
+                        const int piece = n >> 1, half = n & 1;
+                        if (half == 0)
+#pragma unroll
+                            for (int g = 0; g < 4; ++g) c[g] = *reinterpret_cast<const uint64_t *>(here + 32 + 32 * piece + 8 * g + 2 * q);
+                        tmem_ld_wait(r[n & 1]);
+                        if (n + 1 < kCols / 16) tmem_ld_16x256b_x4(at + 32 * ((n + 1) >> 1) + ((uint32_t)(16 * ((n + 1) & 1)) << 16), r[(n + 1) & 1]);
+                        else hand_back();
+#pragma unroll
+                        for (int g = 0; g < 4; ++g)
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                uint64_t &to = sum[(2 * half + k) * 16 + 4 * piece + g];
+                                to = fma2(pair_of(r[n & 1][4 * g + 2 * k], r[n & 1][4 * g + 2 * k + 1]), mul2(c[g], scale2[2 * half + k]), to);
+                            }
                     }
+                } else {
+                    uint32_t r[2][32];
+                    tmem_ld_32x32b_x32(at, r[0]);
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const uint64_t v = pair_of(r[i & 1][2 * j], r[i & 1][2 * j + 1]);
-                        uint64_t f = scale2;
-                        if constexpr (kColumnScales) f = mul2(f, *reinterpret_cast<const uint64_t *>(cols + 32 * i + 2 * j));
-                        sum[16 * i + j] = fma2(v, f, sum[16 * i + j]);
+                    for (int n = 0; n < kCols / 32; ++n) {
+                        tmem_ld_wait(r[n & 1]);
+                        if (n + 1 < kCols / 32) tmem_ld_32x32b_x32(at + 32 * (n + 1), r[(n + 1) & 1]);
+                        else hand_back();
+                        add_scaled<32, false>(&sum[16 * n], r[n & 1], scale2[0], nullptr);
                     }
                 }
                 if (++b == kBuffers) { b = 0; tphase ^= 1u; }
             }
             if (!alive) break;
-            store_row<T, kCols>(a, sum, row, col0);
+            // Two neighbouring columns' values, with bias and activation.
+            auto finish = [&](uint64_t v, int col, float &x, float &y) {
+                halves(v, x, y);
+                if (a.bias) { x += a.bias[min(col, a.rows_b - 1)]; y += a.bias[min(col + 1, a.rows_b - 1)]; }
+                x = x < floor_v ? floor_v : x;                // (a NaN stays one: a comparison with it fails)
+                y = y < floor_v ? floor_v : y;
+            };
+            if (a.store_tma) {
+                // 32 rows of 128 bytes at a time, 16-byte pieces exchanged by XOR with the row as the copy expects them
+                constexpr int kPer = 128 / (int)sizeof(T);
+#pragma unroll
+                for (int c = 0; c < kCols; c += kPer) {
+                    if (lane == 0) tma_store_wait_read();
+                    __syncwarp();
+                    if constexpr (kColumnScales) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+#pragma unroll
+                            for (int g = 0; g < kPer / 8; ++g) {
+                                float x, y;
+                                finish(sum[k * 16 + c / 8 + g], col0 + c + 8 * g + 2 * q, x, y);
+                                const uint32_t byte = (uint32_t)(8 * g + 2 * q) * sizeof(T), to = box + (uint32_t)(8 * k + i) * 128u + (((byte >> 4) ^ i) << 4) + (byte & 15u);
+                                if constexpr (sizeof(T) == 4) asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(x), "f"(y) : "memory");
+                                else asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(blk::pack_bf16(x, y)) : "memory");
+                            }
+                    } else {
+#pragma unroll
+                        for (int piece = 0; piece < 8; ++piece) {
+                            __align__(16) T w[kPer / 8];
+#pragma unroll
+                            for (int j = 0; j < kPer / 8; j += 2) {
+                                const int k = c + piece * (kPer / 8) + j;
+                                float x, y;
+                                finish(sum[k / 2], col0 + k, x, y);
+                                put(w, j, x);
+                                put(w, j + 1, y);
+                            }
+                            const uint4 v = *reinterpret_cast<const uint4 *>(w);
+                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(box + lane * 128u + ((uint32_t)(piece ^ (lane & 7)) << 4)), "r"(v.x), "r"(v.y),
+                                         "r"(v.z), "r"(v.w) : "memory");
+                        }
+                    }
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0 && first_row < a.rows_a && col0 + c < a.rows_b) tma_store_2d(&map_out, col0 + c, first_row, box);
+                }
+            } else if constexpr (kColumnScales) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int row = first_row + 8 * k + i;
+#pragma unroll
+                    for (int n = 0; n < 16; ++n) {
+                        float v[2];
+                        halves(sum[k * 16 + n], v[0], v[1]);
+                        store_value<T>(a, row, col0 + 8 * n + 2 * q, v[0]);
+                        store_value<T>(a, row, col0 + 8 * n + 2 * q + 1, v[1]);
+                    }
+                }
+            } else
+                store_row<T, kCols>(a, sum, first_row + lane, col0);
             __syncwarp();
         }
+        if (lane == 0) tma_store_wait();
         if (!alive && lane == 0) tc_dev_set_status(a.status, TC_ERR_TIMEOUT);
     }
     tc_fence_before_sync();
@@ -580,20 +701,20 @@ tc_status launch_tiles(const tc_ctx *ctx, const TileArgs &a, const CUtensorMap &
 }
 
 template <typename T, bool kColumnScales>
-tc_status launch_pairs(const tc_ctx *ctx, const TileArgs &a, const CUtensorMap &map_a, const CUtensorMap &map_b, cudaStream_t s)
+tc_status launch_pairs(const tc_ctx *ctx, const TileArgs &a, const CUtensorMap &map_a, const CUtensorMap &map_b, const CUtensorMap &map_out, cudaStream_t s)
 {
     constexpr auto kernel = block_matmul_pair_kernel<T, kColumnScales>;
     if (!allow_shared<kernel>(ctx->device, pair::kSmem)) return TC_ERR_CUDA;
     const long long units = (long long)a.tiles_m * a.tiles_n, pairs = ctx->sm_count / 2;
     const dim3 grid((unsigned int)(2 * (units < pairs ? units : pairs)));
-    return launch_first_cluster(2, kernel, grid, dim3(pair::kThreads), pair::kSmem, s, a, map_a, map_b) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
+    return launch_first_cluster(2, kernel, grid, dim3(pair::kThreads), pair::kSmem, s, a, map_a, map_b, map_out) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
 
 template <typename T>
-tc_status launch(const tc_ctx *ctx, const TileArgs &a, bool pairs, int n, const CUtensorMap &map_a, const CUtensorMap &map_b, cudaStream_t s)
+tc_status launch(const tc_ctx *ctx, const TileArgs &a, bool pairs, int n, const CUtensorMap &map_a, const CUtensorMap &map_b, const CUtensorMap &map_out, cudaStream_t s)
 {
     const bool cols = a.shift_b == 0;
-    if (pairs) return cols ? launch_pairs<T, true>(ctx, a, map_a, map_b, s) : launch_pairs<T, false>(ctx, a, map_a, map_b, s);
+    if (pairs) return cols ? launch_pairs<T, true>(ctx, a, map_a, map_b, map_out, s) : launch_pairs<T, false>(ctx, a, map_a, map_b, map_out, s);
     switch (n) {
     case 16: return cols ? launch_tiles<T, 16, true>(ctx, a, map_a, map_b, s) : TC_ERR_UNSUPPORTED;
     case 32: return cols ? launch_tiles<T, 32, true>(ctx, a, map_a, map_b, s) : TC_ERR_UNSUPPORTED;
@@ -672,10 +793,11 @@ tc_status tc_launch_matmul_blocks(const tc_ctx *ctx, const MatmulArgs &m, const 
     a.partial = plan.workspace ? (float *)workspace : nullptr;
     a.status = m.status;
     if (plan.splits > 0) {
-        CUtensorMap map_a, map_b;
+        CUtensorMap map_a, map_b, map_out{};
         if (!tc_tensor_map_codes(&map_a, ra.m.codes, ra.rows, m.cols, ra.m.ld, kRowsM) ||
             !tc_tensor_map_codes(&map_b, rb.m.codes, rb.rows, m.cols, rb.m.ld, plan.pairs ? kRowsM : plan.n)) return TC_ERR_CUDA;
-        const tc_status st = m.dtype == TC_BF16 ? launch<__nv_bfloat16>(ctx, a, plan.pairs, plan.n, map_a, map_b, s) : launch<float>(ctx, a, plan.pairs, plan.n, map_a, map_b, s);
+        a.store_tma = plan.pairs && a.vec && tc_tensor_map_rows(&map_out, m.out, m.dtype, a.rows_a, a.rows_b, 32);
+        const tc_status st = m.dtype == TC_BF16 ? launch<__nv_bfloat16>(ctx, a, plan.pairs, plan.n, map_a, map_b, map_out, s) : launch<float>(ctx, a, plan.pairs, plan.n, map_a, map_b, map_out, s);
         if (st != TC_OK || !a.partial) return st;
     }
     const long long values = (long long)a.tiles_m * a.tiles_n * plan.n * kRowsM;

@@ -65,6 +65,27 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_
     }
 }
 
+// The same for a wait that is part of a short chain from warp to warp: tries again at once, and reads no clock before it
+// has tried some thousand times (a wait of mbar_wait that does not succeed at once takes 100 ns and a clock's reading more).
+__device__ __forceinline__ bool mbar_wait_soon(uint32_t bar, uint32_t parity)
+{
+    unsigned long long t0 = 0, t1;
+    for (uint32_t i = 1;; ++i) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
+        if ((i & 4095u) == 0) {
+            asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t1));
+            if (t0 == 0) t0 = t1;
+            else if (t1 - t0 > 2000000000ull) return false;
+        }
+    }
+}
+
 // ---- proxies and fences -----------------------------------------------------------------
 // Makes shared-memory writes of the generic proxy (st.shared, cp.async) visible to the async
 // proxy (tcgen05.mma operand reads).
@@ -97,6 +118,10 @@ __device__ __forceinline__ void named_bar_arrive(int id, int threads)
 __device__ __forceinline__ void cp_async_8(uint32_t dst, const void *src, uint32_t src_bytes)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_4(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src, uint32_t src_bytes)
 {
@@ -281,6 +306,16 @@ __device__ __forceinline__ void tma_load_2d(uint32_t smem_dst, const void *tenso
         : "memory");
 }
 
+// The way back: a box from shared memory to the tensor (parts outside it are not written; no coordinate is negative).  The
+// shared memory may be written again after tma_store_wait_read.  Written by st.shared: fence_proxy_async_smem first.
+__device__ __forceinline__ void tma_store_2d(const void *tensor_map, int x, int y, uint32_t smem_src)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];\n\tcp.async.bulk.commit_group;"
+                 ::"l"(tensor_map), "r"(x), "r"(y), "r"(smem_src) : "memory");
+}
+__device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
 // Contiguous bulk copy global -> shared: both addresses 16-byte aligned, the size a multiple of 16.
 __device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void *src, uint32_t bytes, uint32_t bar)
 {
@@ -428,28 +463,11 @@ __device__ __forceinline__ uint32_t cluster_address(uint32_t smem_addr, uint32_t
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr), "r"(rank));
     return r;
 }
+// (Of the pair's tensor memory and copies only, which have fences of their own: a release of the whole cluster's memory takes
+// hundreds of cycles.)
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
-}
-// mbar_wait for a barrier on which threads of the other CTA arrive.
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity)
-{
-    unsigned long long t0 = 0, t1;
-    for (int i = 0;; ++i) {
-        uint32_t ok;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(ok) : "r"(bar), "r"(parity), "r"(i ? 100000u : 0u) : "memory");
-        if (ok) return true;
-        if ((i & 63) == 0) {
-            asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t1));
-            if (i == 0) t0 = t1;
-            else if (t1 - t0 > 2000000000ull) return false;
-        }
-    }
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 __device__ __forceinline__ void tmem_alloc_pair(uint32_t smem_result, uint32_t columns)
 {

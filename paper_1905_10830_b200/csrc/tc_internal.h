@@ -363,7 +363,9 @@ struct NormGradArgs {
 };
 int tc_norm_grad_blocks(long long pixels, int c, int hw, int sm_count);
 tc_status tc_launch_residual_norms_backward(const NormGradArgs &a, int dtype, int blocks, cudaStream_t s);
-// Tensor map of e4m3 codes [rows][ld] of which `cols` count: boxes of 128 codes x box_rows rows, 128-byte swizzle.
+// Tensor map of an fp32 or bf16 matrix [rows][cols] (rows a multiple of 16 bytes): boxes of 128 bytes x box_rows rows, 128-byte swizzle.
+bool tc_tensor_map_rows(CUtensorMap *map, const void *base, int dtype, long long rows, long long cols, int box_rows);
+// The same of e4m3 codes [rows][ld] of which `cols` count: boxes of 128 codes.
 bool tc_tensor_map_codes(CUtensorMap *map, const void *base, long long rows, long long cols, long long ld, int box_rows);
 
 // ---- launchers (defined in the .cu files) ----------------------------------------------
