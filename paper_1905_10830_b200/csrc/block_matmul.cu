@@ -678,18 +678,6 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
     }
 }
 
-// Shared memory of a kernel, asked for once on a device.
-template <auto kKernel>
-bool allow_shared(int device, size_t bytes)
-{
-    static std::atomic<unsigned long long> done{0};
-    const unsigned long long bit = device < 64 ? 1ull << device : 0;
-    if (done.load(std::memory_order_relaxed) & bit) return true;
-    if (cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) { cudaGetLastError(); return false; }
-    done.fetch_or(bit, std::memory_order_relaxed);
-    return true;
-}
-
 template <typename T, int kN, bool kColumnScales>
 tc_status launch_tiles(const tc_ctx *ctx, const TileArgs &a, const CUtensorMap &map_a, const CUtensorMap &map_b, cudaStream_t s)
 {

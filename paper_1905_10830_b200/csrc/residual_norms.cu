@@ -12,6 +12,7 @@
 // a pixel waits for one reduction.  All sums are fp32, in an order that does not depend on the launch's timing; sums over the pixels are first
 // taken by block, and a second kernel adds the blocks' sums in their order.
 #include "block_codes.cuh"
+#include "sm100_ptx.cuh"
 #include "tc_internal.h"
 
 namespace {
@@ -19,7 +20,7 @@ namespace {
 using namespace tcdev;
 using namespace blk;
 
-__device__ __forceinline__ float inv_sqrt(float v) { return __frcp_rn(__fsqrt_rn(v)); }
+__device__ __forceinline__ float inv_sqrt(float v) { return rsqrtf(v); }       // (off by 2^-22 at most)
 
 // ---- single pixels (H W = 1): a pixel's channels are a row in memory ------------------------------
 // kWarps warps a row, kV chunks of eight channels a thread; rows of one warp share a block of eight.
@@ -61,13 +62,26 @@ __device__ __forceinline__ float row_sum(float v, float *s_part)
 #pragma unroll
     for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
     if constexpr (kWarps > 1) {
-        if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = v;
+        const int lane = threadIdx.x & 31;
+        if (lane == 0) s_part[threadIdx.x >> 5] = v;
         __syncthreads();
-        v = 0.f;
+        v = s_part[lane % kWarps];
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) v += s_part[w];
+        for (int d = kWarps / 2; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
     }
     return v;
+}
+
+// Codes of eight values of a row; 16 threads' are a block.
+__device__ __forceinline__ void store_codes(const BlockMatrix &to, const float (&x)[8], long long row, int k, int c, int t)
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, abs_bits(x[j]));
+    const float scale = scale_of(max16(m));
+    if (k >= c) return;
+    *reinterpret_cast<uint2 *>(to.codes + row * to.ld + k) = codes8(x, __frcp_rn(scale));
+    if ((t & 15) == 0) to.scales[(long long)(k / kBlock) * to.scale_ld + row] = scale;
 }
 
 template <typename T, int kWarps, int kV>
@@ -146,16 +160,148 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32) norm_rows_ker
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = s[i][j] * r * w[j];
         if (a.x) store_chunk((T *)a.x + base, w, k, a.c, vec);
-        if (a.codes.codes) {
-            uint32_t m = 0;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) m = max(m, abs_bits(w[j]));
-            const float scale = scale_of(max16(m));           // 16 threads' chunks are a block
-            if (k < a.c) {
-                *reinterpret_cast<uint2 *>(a.codes.codes + row * a.codes.ld + k) = codes8(w, __frcp_rn(scale));
-                if ((t & 15) == 0) a.codes.scales[(long long)(k / kBlock) * a.codes.scale_ld + row] = scale;
-            }
+        if (a.codes.codes) store_codes(a.codes, w, row, k, a.c, t);
+    }
+}
+
+// ---- rows on their way to shared memory ------------------------------------------------------
+// Long aligned rows: a block walks rows gridDim.x apart, whose parts of all inputs one thread brings to a ring in shared memory by bulk
+// copies, several rows ahead, so that the memory is at work while the block waits for a row's sums (with a row's loads in
+// registers, and the vectors read again for each row: gradient of 16384x4096 297 us and RING_GRAD, forward 122 and RING_FWD).
+constexpr int kRingInputs = 5, kRingStages = 8;
+constexpr size_t kRingSm = 200 * 1024;                        // of an SM's shared memory, for all its blocks' rings
+struct RowRing {
+    const char *in[kRingInputs];      // compact: input i is part i of a stage
+    int inputs, stages;
+    uint32_t part_bytes;              // of a row of one input
+};
+struct RowReader {
+    uint32_t ring;
+    unsigned long long *full;
+    bool alive;
+    __device__ __forceinline__ void bring(const RowRing &r, long long row, int slot)
+    {
+        using namespace sm100;
+        const uint32_t bar = smem_u32(full + slot), bytes = r.part_bytes;
+        mbar_arrive_expect_tx(bar, bytes * (uint32_t)r.inputs);
+        for (int i = 0; i < r.inputs; ++i) bulk_load(ring + (uint32_t)(slot * r.inputs + i) * bytes, r.in[i] + row * bytes, bytes, bar);
+    }
+    // The block's first rows; ends with the block in step.
+    __device__ __forceinline__ void start(const RowRing &r, long long rows)
+    {
+        using namespace sm100;
+        if (threadIdx.x == 0) {
+            for (int i = 0; i < r.stages; ++i) mbar_init(smem_u32(full + i), 1);
+            mbar_fence_init();
+            for (int i = 0; i < r.stages && blockIdx.x + (long long)i * gridDim.x < rows; ++i) bring(r, blockIdx.x + (long long)i * gridDim.x, i);
         }
+        alive = true;
+        __syncthreads();
+    }
+    // Where the block's `turn`-th row lies, once it has come.
+    __device__ __forceinline__ uint32_t row(const RowRing &r, int turn, int slot, unsigned int *status)
+    {
+        if (alive && !sm100::mbar_wait_soon(sm100::smem_u32(full + slot), (uint32_t)(turn / r.stages & 1))) {
+            alive = false;                                    // (no wait is waited for twice)
+            tc_dev_set_status(status, TC_ERR_TIMEOUT);
+        }
+        return ring + (uint32_t)(slot * r.inputs) * r.part_bytes;
+    }
+};
+__device__ __forceinline__ uint4 lds16(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void load8_shared(Raw8<__nv_bfloat16> &r, uint32_t at) { r.v = lds16(at); }
+__device__ __forceinline__ void load8_shared(Raw8<float> &r, uint32_t at) { r.v = lds16(at); r.w = lds16(at + 16); }
+
+template <typename T, int kWarps, int kV>
+__global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_ring_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ RowRing r)
+{
+    constexpr int kThreadsRow = kWarps * 32;
+    extern __shared__ __align__(16) unsigned char s_ring[];
+    __shared__ __align__(8) unsigned long long s_full[kRingStages];
+    __shared__ float s_part[2][kWarps];
+    chain_next();
+    chain_wait();
+    const int t = threadIdx.x;
+    RowReader reader;
+    reader.ring = sm100::smem_u32(s_ring);
+    reader.full = s_full;
+    reader.start(r, a.pixels);
+    const float inv_c = 1.0f / (float)a.c, scale = a.scale ? *a.scale : 1.f;
+    float wy[kV][8], wx[kV][8];                               // after times the channels' gate; before
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+        const int k = chunk_at<kThreadsRow>(t, i);
+        float g[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) wy[i][j] = wx[i][j] = g[j] = 1.f;
+        if (a.after) load_vector(wy[i], a.after, k, a.c, true);
+        if (a.gate) load_vector(g, a.gate, k, a.c, true);
+        if (a.before) load_vector(wx[i], a.before, k, a.c, true);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) wy[i][j] *= g[j];
+    }
+    int turn = 0, slot = 0;
+    for (long long row = blockIdx.x; row < a.pixels; row += gridDim.x, ++turn) {
+        const long long base = row * a.c;
+        const uint32_t at = reader.row(r, turn, slot, a.status);
+        Raw8<T> rh[kV], ry[kV], rg[kV];
+        float sum = 0.f, s[kV][8];
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const int k = chunk_at<kThreadsRow>(t, i);
+            zero8(rh[i]); zero8(ry[i]); zero8(rg[i]);
+            if (k < a.c) {
+                load8_shared(rh[i], at + (uint32_t)k * sizeof(T));
+                load8_shared(ry[i], at + r.part_bytes + (uint32_t)k * sizeof(T));
+                if (a.gate_map) load8_shared(rg[i], at + 2 * r.part_bytes + (uint32_t)k * sizeof(T));
+            }
+            float y[8];
+            values8(ry[i], y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum = fmaf(y[j], y[j], sum);
+        }
+        sum = row_sum<kWarps>(sum, s_part[0]);                // (the block is in step here: all have read the slot)
+        if (threadIdx.x == 0 && row + (long long)r.stages * gridDim.x < a.pixels) reader.bring(r, row + (long long)r.stages * gridDim.x, slot);
+        const float f = (a.after ? inv_sqrt(fmaf(sum, inv_c, a.eps)) : 1.f) * scale;
+        sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const int k = chunk_at<kThreadsRow>(t, i);
+            float y[8];
+            values8(ry[i], y);
+            values8(rh[i], s[i]);
+            if (a.gate_map) {
+                float g[8];
+                values8(rg[i], g);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] *= g[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                s[i][j] = fmaf(f, y[j] * wy[i][j], s[i][j]);
+                sum = fmaf(s[i][j], s[i][j], sum);
+            }
+            store_chunk((T *)a.sum + base, s[i], k, a.c, true);
+        }
+        if (a.before) {
+            const float rr = inv_sqrt(fmaf(row_sum<kWarps>(sum, s_part[1]), inv_c, a.eps));
+#pragma unroll
+            for (int i = 0; i < kV; ++i) {
+                const int k = chunk_at<kThreadsRow>(t, i);
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = s[i][j] * rr * wx[i][j];
+                if (a.x) store_chunk((T *)a.x + base, x, k, a.c, true);
+                if (a.codes.codes) store_codes(a.codes, x, row, k, a.c, t);
+            }
+        } else
+            __syncthreads();                                  // the row's partial sums are read before the next row's are written
+        if (++slot == r.stages) slot = 0;
     }
 }
 
@@ -250,7 +396,145 @@ __global__ void __launch_bounds__(256) norm_maps_kernel(NormArgs a)
     }
 }
 
+// The same with a tile of 32 pixels and all channels of the inputs in shared memory, where it fits: each value is fetched once, many at
+// a time, and the vectors once a block (256x14x14 x 1024, bf16: 962 us and MAPS_FWD).
+constexpr int kTilePixels = 32;
+constexpr size_t kTileSm = 220 * 1024;
+
+// [c][32] of a tensor's pixels p0 ...; zeros behind the last.  `vec`: four pixels at a time.
+template <typename T>
+__device__ __forceinline__ void load_tile(T *dst, const T *src, long long p0, long long pixels, int c, int hw, bool vec)
+{
+    using namespace sm100;
+    const int t = threadIdx.x;
+    if (vec) {
+        const int px = (t & 7) * 4;
+        const long long p = p0 + px, img = p / hw;
+        const bool ok = p < pixels;
+        const T *from = ok ? src + img * c * (long long)hw + (p - img * hw) : src;
+        for (int ch = t >> 3; ch < c; ch += 32) {
+            const uint32_t to = smem_u32(dst + ch * kTilePixels + px);
+            const T *at = ok ? from + (long long)ch * hw : from;
+            if constexpr (sizeof(T) == 2) cp_async_8(to, at, ok ? 8u : 0u);
+            else cp_async_16(to, at, ok ? 16u : 0u);
+        }
+    } else {
+        const int px = t & 31;
+        const long long p = p0 + px, img = p / hw;
+        const bool ok = p < pixels;
+        const T *from = src + img * c * (long long)hw + (p - img * hw);
+        for (int ch = t >> 5; ch < c; ch += 128) {
+            T v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                v[i] = T(0.f);
+                if (ok && ch + 8 * i < c) v[i] = from[(long long)(ch + 8 * i) * hw];
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (ch + 8 * i < c) dst[(ch + 8 * i) * kTilePixels + px] = v[i];
+        }
+    }
+}
+// Sum over the block's eight warps, lane by lane.
+__device__ __forceinline__ float over_warps(float (*part)[32], float v)
+{
+    part[threadIdx.x >> 5][threadIdx.x & 31] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) v += part[w][threadIdx.x & 31];
+    return v;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(256) norm_maps_tile_kernel(const __grid_constant__ NormArgs a, int vec)
+{
+    extern __shared__ __align__(16) unsigned char s_tile[];   // after times the channels' gate [c], before [c]; h, y, gate: [c][32]
+    __shared__ float s_part[2][8][32];
+    __shared__ uint32_t s_max[2][8][32];
+    float *const wy = reinterpret_cast<float *>(s_tile), *const wx = wy + a.c;
+    T *const sh = reinterpret_cast<T *>(s_tile + ((2 * a.c * sizeof(float) + 15) & ~15ull)), *const sy = sh + a.c * kTilePixels, *const sg = sy + a.c * kTilePixels;
+    chain_next();
+    chain_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int i = threadIdx.x; i < a.c; i += 256) {
+        wy[i] = (a.after ? a.after[i] : 1.f) * (a.gate ? a.gate[i] : 1.f);
+        wx[i] = a.before ? a.before[i] : 0.f;
+    }
+    const float scale = a.scale ? *a.scale : 1.f, inv_c = 1.0f / (float)a.c;
+    const long long tiles = (a.pixels + kTilePixels - 1) / kTilePixels;
+    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const long long p = tile * kTilePixels + lane, img = p / a.hw, base = img * a.c * (long long)a.hw + (p - img * a.hw);
+        const bool ok = p < a.pixels;
+        __syncthreads();                                      // the last tile's readers
+        load_tile(sh, (const T *)a.h, tile * kTilePixels, a.pixels, a.c, a.hw, vec);
+        if (a.y) load_tile(sy, (const T *)a.y, tile * kTilePixels, a.pixels, a.c, a.hw, vec);
+        if (a.gate_map) load_tile(sg, (const T *)a.gate_map, tile * kTilePixels, a.pixels, a.c, a.hw, vec);
+        sm100::cp_async_wait_all();
+        __syncthreads();
+        float f = scale;
+        if (a.y && a.after) {
+            float sum = 0.f;
+            for (int c0 = warp * 16; c0 < a.c; c0 += kBlock) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float v = c0 + j < a.c ? load1(sy + (c0 + j) * kTilePixels + lane) : 0.f;
+                    sum = fmaf(v, v, sum);
+                }
+            }
+            f *= inv_sqrt(fmaf(over_warps(s_part[0], sum), inv_c, a.eps));
+        }
+        auto sum_at = [&](int ch) {
+            const int at = ch * kTilePixels + lane;
+            const float s = load1(sh + at);
+            if (!a.y) return s;
+            float u = load1(sy + at) * wy[ch];
+            if (a.gate_map) u *= load1(sg + at);
+            return fmaf(f, u, s);
+        };
+        float sum = 0.f;
+        T *to = (T *)a.sum + base;
+        for (int c0 = warp * 16; c0 < a.c; c0 += kBlock) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (c0 + j < a.c) {
+                    const float v = sum_at(c0 + j);
+                    sum = fmaf(v, v, sum);
+                    if (a.y && ok) store1(to + (long long)(c0 + j) * a.hw, v);
+                }
+        }
+        if (!a.before) continue;
+        const float r = inv_sqrt(fmaf(over_warps(s_part[1], sum), inv_c, a.eps));
+        to = (T *)a.x + base;
+        int turn = 0;
+        for (int b0 = 0; b0 < a.c; b0 += kBlock, turn ^= 1) {
+            const int c0 = b0 + warp * 16;
+            float v[16];
+            uint32_t m = 0;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                v[j] = c0 + j < a.c ? sum_at(c0 + j) * r * wx[c0 + j] : 0.f;
+                m = max(m, abs_bits(v[j]));
+                if (a.x && ok && c0 + j < a.c) store1(to + (long long)(c0 + j) * a.hw, v[j]);
+            }
+            if (a.codes.codes) {
+                s_max[turn][warp][lane] = m;
+                __syncthreads();                              // (the other half's readers are past this barrier before it is written again)
+#pragma unroll
+                for (int w = 0; w < 8; ++w) m = max(m, s_max[turn][w][lane]);
+                const float sc = scale_of(m), inv = __frcp_rn(sc);
+                if (ok && c0 < a.c)
+                    *reinterpret_cast<uint4 *>(a.codes.codes + p * a.codes.ld + c0) = make_uint4(
+                        codes4(v[0], v[1], v[2], v[3], inv), codes4(v[4], v[5], v[6], v[7], inv), codes4(v[8], v[9], v[10], v[11], inv), codes4(v[12], v[13], v[14], v[15], inv));
+                if (ok && warp == 0) a.codes.scales[(long long)(b0 / kBlock) * a.codes.scale_ld + p] = sc;
+            }
+        }
+    }
+}
+
 // ---- gradient ----------------------------------------------------------------------------------
+constexpr int kMostChannels = 16384;
 constexpr int kSums = 6;        // s s, t s, y y, and ds, t, s times gate after y
 
 // What a pixel's sums give.
@@ -445,6 +729,140 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32, kWarps == 1 ?
     }
 }
 
+// The same with the rows in a ring, the vectors and the sums over the rows in registers.
+template <typename T, int kWarps, int kV>
+__global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_kernel(const __grid_constant__ NormGradArgs a, const __grid_constant__ RowRing r)
+{
+    constexpr int kThreadsRow = kWarps * 32;
+    extern __shared__ __align__(16) unsigned char s_ring[];
+    __shared__ __align__(8) unsigned long long s_full[kRingStages];
+    __shared__ float s_part[2][kWarps][8];
+    __shared__ float s_scale[kWarps];
+    chain_next();
+    chain_wait();
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    RowReader reader;
+    reader.ring = sm100::smem_u32(s_ring);
+    reader.full = s_full;
+    reader.start(r, a.pixels);
+    // parts of a stage: s and dx (with before), y, ds, gate, those that there are
+    const uint32_t part = r.part_bytes, at_y = a.before ? 2 * part : 0, at_d = at_y + (a.y ? part : 0), at_g = at_d + (a.ds ? part : 0);
+    const float scale = a.y && a.scale ? *a.scale : 1.f;
+    float wy[kV][8], wx[kV][8], sum_y[kV][8], sum_x[kV][8], sum_scale = 0.f;
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+        const int k = chunk_at<kThreadsRow>(t, i);
+        float g[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { wy[i][j] = g[j] = 1.f; wx[i][j] = sum_y[i][j] = sum_x[i][j] = 0.f; }
+        if (a.after) load_vector(wy[i], a.after, k, a.c, true);
+        if (a.gate) load_vector(g, a.gate, k, a.c, true);
+        if (a.before) load_vector(wx[i], a.before, k, a.c, true);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) wy[i][j] *= g[j];
+    }
+    int turn = 0, slot = 0, last = 0;
+    for (long long row = blockIdx.x; row < a.pixels; row += gridDim.x, ++turn) {
+        const long long base = row * a.c;
+        const uint32_t at = reader.row(r, turn, slot, a.status);
+        auto get = [&](bool there, uint32_t where, int k, float (&f)[8]) {
+            Raw8<T> raw;
+            zero8(raw);
+            if (there && k < a.c) load8_shared(raw, at + where + (uint32_t)k * sizeof(T));
+            values8(raw, f);
+        };
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const int k = chunk_at<kThreadsRow>(t, i);
+            float s[8], y[8], dx[8], d[8];
+            get(a.before, 0, k, s);
+            get(a.before, part, k, dx);
+            get(a.y, at_y, k, y);
+            get(a.ds, at_d, k, d);
+            if (a.gate_map) {
+                float g[8];
+                get(true, at_g, k, g);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[2] = fmaf(y[j], y[j], v[2]);
+                    y[j] *= g[j];
+                }
+            } else
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[2] = fmaf(y[j], y[j], v[2]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float tt = dx[j] * wx[i][j], gy = wy[i][j] * y[j];
+                v[0] = fmaf(s[j], s[j], v[0]);
+                v[1] = fmaf(tt, s[j], v[1]);
+                v[3] = fmaf(d[j], gy, v[3]);
+                v[4] = fmaf(tt, gy, v[4]);
+                v[5] = fmaf(s[j], gy, v[5]);
+            }
+        }
+        row_sums<kWarps>(v, s_part[turn & 1]);
+        // (the block is in step: the last row's slot is free)
+        if (t == 0 && turn > 0 && row + (long long)(r.stages - 1) * gridDim.x < a.pixels) reader.bring(r, row + (long long)(r.stages - 1) * gridDim.x, last);
+        const float sums[kSums] = {v[0], v[1], v[2], v[3], v[4], v[5]};
+        const PixelFactors f = pixel_factors(sums, a, scale);
+        const float scale_q = scale * f.q, mean_q = f.mean * f.q * f.q;
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const int k = chunk_at<kThreadsRow>(t, i);
+            float s[8], y[8], d[8], g[8];
+            get(a.ds, at_d, k, d);
+            if (a.before) {
+                float dx[8];
+                get(true, 0, k, s);
+                get(true, part, k, dx);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float rx = f.r * dx[j];
+                    d[j] = fmaf(-f.r3m, s[j], fmaf(rx, wx[i][j], d[j]));
+                    sum_x[i][j] = fmaf(rx, s[j], sum_x[i][j]);
+                }
+            }
+            store_chunk((T *)a.dh + base, d, k, a.c, true);
+            if (a.y) {
+                get(true, at_y, k, y);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) g[j] = 1.f;
+                if (a.gate_map) get(true, at_g, k, g);
+                float dy[8], dg[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float dw = d[j] * wy[i][j], dn = d[j] * (y[j] * f.q);
+                    dg[j] = scale_q * (dw * y[j]);
+                    sum_scale = fmaf(dn * g[j], wy[i][j], sum_scale);
+                    sum_y[i][j] = a.gate_map ? fmaf(dn, g[j], sum_y[i][j]) : sum_y[i][j] + dn;
+                    dy[j] = fmaf(-y[j], mean_q, scale_q * (dw * g[j]));
+                }
+                store_chunk((T *)a.dy + base, dy, k, a.c, true);
+                if (a.gate_map) store_chunk((T *)a.dgate_map + base, dg, k, a.c, true);
+            }
+        }
+        last = slot;
+        if (++slot == r.stages) slot = 0;
+    }
+    float *const to = a.partial + (long long)blockIdx.x * 2 * a.c;
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+        const int k = chunk_at<kThreadsRow>(t, i);
+        store_chunk(to, sum_y[i], k, a.c, true);
+        store_chunk(to + a.c, sum_x[i], k, a.c, true);
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum_scale += __shfl_xor_sync(0xffffffffu, sum_scale, d);
+    if (lane == 0) s_scale[warp] = sum_scale;
+    __syncthreads();
+    if (t == 0) {
+        float v = 0.f;
+        for (int w = 0; w < kWarps; ++w) v += s_scale[w];
+        a.partial_scale[blockIdx.x] = v;
+    }
+}
+
 // Maps: 32 pixels at a time, a lane for each; warps take slices of eight channels in turn.  The sums over the pixels are
 // kept in shared memory, each channel's by the one warp that has it.
 template <typename T>
@@ -539,6 +957,112 @@ __global__ void __launch_bounds__(256) norm_maps_grad_kernel(NormGradArgs a)
     }
 }
 
+// The same with the inputs' tile in shared memory, as in the forward.
+template <typename T>
+__global__ void __launch_bounds__(256) norm_maps_grad_tile_kernel(const __grid_constant__ NormGradArgs a, int vec)
+{
+    extern __shared__ __align__(16) unsigned char s_tile[];   // sums over the pixels [2][c], after times the channels' gate [c], before [c]; s, dx, y, ds, gate: [c][32]
+    __shared__ float s_part[8][kSums][32];
+    __shared__ float s_scale[8];
+    float *const sums_y = reinterpret_cast<float *>(s_tile), *const sums_x = sums_y + a.c, *const wy = sums_x + a.c, *const wx = wy + a.c;
+    const int plane = a.c * kTilePixels;
+    T *const ss = reinterpret_cast<T *>(s_tile + ((4 * a.c * sizeof(float) + 15) & ~15ull)), *const sx = ss + (a.before ? plane : 0), *const sy = sx + (a.before ? plane : 0);
+    T *const sd = sy + (a.y ? plane : 0), *const sg = sd + (a.ds ? plane : 0);
+    chain_next();
+    chain_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int i = threadIdx.x; i < a.c; i += 256) {
+        sums_y[i] = sums_x[i] = 0.f;
+        wy[i] = (a.after ? a.after[i] : 1.f) * (a.gate ? a.gate[i] : 1.f);
+        wx[i] = a.before ? a.before[i] : 0.f;
+    }
+    const float scale = a.y && a.scale ? *a.scale : 1.f;
+    float sum_scale = 0.f;
+    const long long tiles = (a.pixels + kTilePixels - 1) / kTilePixels;
+    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const long long p0 = tile * kTilePixels, p = p0 + lane, img = p / a.hw, base = img * a.c * (long long)a.hw + (p - img * a.hw);
+        const bool ok = p < a.pixels;
+        __syncthreads();                                      // the last tile's readers
+        if (a.before) {
+            load_tile(ss, (const T *)a.s, p0, a.pixels, a.c, a.hw, vec);
+            load_tile(sx, (const T *)a.dx, p0, a.pixels, a.c, a.hw, vec);
+        }
+        if (a.y) load_tile(sy, (const T *)a.y, p0, a.pixels, a.c, a.hw, vec);
+        if (a.ds) load_tile(sd, (const T *)a.ds, p0, a.pixels, a.c, a.hw, vec);
+        if (a.gate_map) load_tile(sg, (const T *)a.gate_map, p0, a.pixels, a.c, a.hw, vec);
+        sm100::cp_async_wait_all();
+        __syncthreads();
+        float sums[kSums] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int c0 = warp * 8; c0 < a.c; c0 += 64) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int ch = c0 + j, at = ch * kTilePixels + lane;
+                if (ch >= a.c) continue;
+                const float s = a.before ? load1(ss + at) : 0.f, t = a.before ? load1(sx + at) * wx[ch] : 0.f;
+                const float y = a.y ? load1(sy + at) : 0.f, ds = a.ds ? load1(sd + at) : 0.f;
+                const float gy = y * wy[ch] * (a.gate_map ? load1(sg + at) : 1.f);
+                sums[0] = fmaf(s, s, sums[0]);
+                sums[1] = fmaf(t, s, sums[1]);
+                sums[2] = fmaf(y, y, sums[2]);
+                sums[3] = fmaf(ds, gy, sums[3]);
+                sums[4] = fmaf(t, gy, sums[4]);
+                sums[5] = fmaf(s, gy, sums[5]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kSums; ++i) s_part[warp][i][lane] = sums[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kSums; ++i) {
+            sums[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) sums[i] += s_part[w][i][lane];
+        }
+        const PixelFactors f = pixel_factors(sums, a, scale);
+        for (int c0 = warp * 8; c0 < a.c; c0 += 64) {
+            float sum_y[8], sum_x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int ch = c0 + j, at = ch * kTilePixels + lane;
+                sum_y[j] = sum_x[j] = 0.f;
+                if (ch >= a.c) continue;
+                const long long to = base + (long long)ch * a.hw;
+                float d = a.ds ? load1(sd + at) : 0.f;
+                if (a.before) {
+                    const float s = load1(ss + at), rx = f.r * load1(sx + at);
+                    d = fmaf(-f.r3m, s, fmaf(rx, wx[ch], d));
+                    sum_x[j] = rx * s;
+                }
+                if (ok) store1((T *)a.dh + to, d);
+                if (a.y) {
+                    const float n = load1(sy + at) * f.q, g = a.gate_map ? load1(sg + at) : 1.f, dn = d * n, dw = d * wy[ch];
+                    sum_scale = fmaf(dn * g, wy[ch], sum_scale);
+                    sum_y[j] = dn * g;
+                    if (ok) {
+                        store1((T *)a.dy + to, f.q * fmaf(-n, f.mean, scale * (dw * g)));
+                        if (a.gate_map) store1((T *)a.dgate_map + to, scale * (dw * n));
+                    }
+                }
+            }
+            const float vy = sum8_over_warp(sum_y, lane), vx = sum8_over_warp(sum_x, lane);
+            if ((lane & 3) == 0 && c0 + (lane >> 2) < a.c) {
+                sums_y[c0 + (lane >> 2)] += vy;
+                sums_x[c0 + (lane >> 2)] += vx;
+            }
+        }
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum_scale += __shfl_xor_sync(0xffffffffu, sum_scale, d);
+    if (lane == 0) s_scale[warp] = sum_scale;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * a.c; i += 256) a.partial[(long long)blockIdx.x * 2 * a.c + i] = sums_y[i];
+    if (threadIdx.x == 0) {
+        float v = 0.f;
+        for (int w = 0; w < 8; ++w) v += s_scale[w];
+        a.partial_scale[blockIdx.x] = v;
+    }
+}
+
 // The blocks' sums, in their order: 32 channels a block, every eighth of the blocks' sums a warp.
 __global__ void __launch_bounds__(256) norm_vectors_kernel(NormGradArgs a, int blocks)
 {
@@ -580,17 +1104,67 @@ tc_status launch_norm_rows(const NormArgs &a, cudaStream_t s)
                ? TC_OK : TC_ERR_CUDA;
 }
 
+// A ring of rows of the given inputs, for `blocks` blocks an SM; none (no stages) where two rows do not fit, and where a block has no more than two rows, which
+// registers hold as soon.
+RowRing make_ring(std::initializer_list<const void *> inputs, int c, size_t size, long long rows, long long grid, int blocks)
+{
+    RowRing r{};
+    for (const void *p : inputs)
+        if (p) r.in[r.inputs++] = (const char *)p;
+    r.part_bytes = (uint32_t)(c * size);
+    const size_t stage = (size_t)r.inputs * r.part_bytes, fit = kRingSm / blocks / stage;
+    r.stages = fit < 2 || rows <= 2 * grid ? 0 : (int)(fit < kRingStages ? fit : kRingStages);
+    return r;
+}
+
+template <auto kKernel, typename A>
+cudaError_t launch_ring(int device, const A &a, const RowRing &r, long long grid, int threads, cudaStream_t s)
+{
+    if (!allow_shared<kKernel>(device, kRingSm)) return cudaErrorInvalidValue;
+    return launch_first(true, kKernel, dim3((unsigned int)grid), dim3(threads), (size_t)r.stages * r.inputs * r.part_bytes, s, a, r);
+}
+
+// Forward with the ring, kBlocks blocks an SM; false where there is none.
+template <typename T, int kWarps, int kV>
+bool launch_norm_ring(const NormArgs &a, cudaStream_t s, tc_status &st)
+{
+    constexpr int kBlocks = 16 / kWarps;
+    if (!a.vec || !a.y) return false;
+    const long long grid = (long long)a.sms * kBlocks;
+    const RowRing r = make_ring({a.h, a.y, a.gate_map}, a.c, sizeof(T), a.pixels, grid, kBlocks);
+    if (r.stages == 0) return false;
+    st = launch_ring<norm_rows_ring_kernel<T, kWarps, kV>>(a.device, a, r, grid, kWarps * 32, s) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
+    return true;
+}
+
+// Whether maps are moved four pixels at a time.
+template <typename T, typename... P>
+bool four_pixels(int hw, P... p)
+{
+    return hw % 4 == 0 && ((((uintptr_t)p) | ...) & (4 * sizeof(T) - 1)) == 0;
+}
+
 template <typename T>
 tc_status norms(const NormArgs &a, cudaStream_t s)
 {
-    if (a.hw > 1)
+    if (a.hw > 1) {
+        const int inputs = 1 + (a.y != nullptr) + (a.gate_map != nullptr);
+        const size_t smem = ((2 * a.c * sizeof(float) + 15) & ~(size_t)15) + (size_t)inputs * a.c * kTilePixels * sizeof(T);
+        if (smem + 6 * 1024 <= kTileSm) {
+            const long long tiles = (a.pixels + kTilePixels - 1) / kTilePixels, fit = kTileSm / (smem + 6 * 1024), most = (fit < 8 ? fit : 8) * a.sms;
+            if (!allow_shared<norm_maps_tile_kernel<T>>(a.device, kTileSm)) return TC_ERR_CUDA;
+            return launch_first(true, norm_maps_tile_kernel<T>, dim3((unsigned int)(tiles < most ? tiles : most)), dim3(256), smem, s, a,
+                                (int)four_pixels<T>(a.hw, a.h, a.y, a.gate_map)) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
+        }
         return launch_first(true, norm_maps_kernel<T>, dim3((unsigned int)((a.pixels + 31) / 32)), dim3(256), 0, s, a) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
+    }
     if (a.c <= 256) return launch_norm_rows<T, 1, 1>(a, s);
     if (a.c <= 512) return launch_norm_rows<T, 1, 2>(a, s);
-    if (a.c <= 1024) return launch_norm_rows<T, 4, 1>(a, s);
-    if (a.c <= 2048) return launch_norm_rows<T, 8, 1>(a, s);
-    if (a.c <= 4096) return launch_norm_rows<T, 8, 2>(a, s);
-    if (a.c <= 8192) return launch_norm_rows<T, 16, 2>(a, s);
+    tc_status st;
+    if (a.c <= 1024) return launch_norm_ring<T, 2, 2>(a, s, st) ? st : launch_norm_rows<T, 4, 1>(a, s);
+    if (a.c <= 2048) return launch_norm_ring<T, 4, 2>(a, s, st) ? st : launch_norm_rows<T, 8, 1>(a, s);
+    if (a.c <= 4096) return launch_norm_ring<T, 8, 2>(a, s, st) ? st : launch_norm_rows<T, 8, 2>(a, s);
+    if (a.c <= 8192) return launch_norm_ring<T, 16, 2>(a, s, st) ? st : launch_norm_rows<T, 16, 2>(a, s);
     return launch_norm_rows<T, 16, 4>(a, s);
 }
 
@@ -601,21 +1175,43 @@ cudaError_t launch_grad_rows(const NormGradArgs &a, int blocks, cudaStream_t s)
     return launch_first(true, norm_rows_grad_kernel<T, kWarps, kV>, dim3((unsigned int)blocks), dim3(kWarps == 1 ? 256 : kWarps * 32), smem, s, a);
 }
 
+// With the ring of rows where there is one: kRingWarps warps of kRingV chunks a thread, as many blocks as an SM's 512 threads.
+template <typename T, int kWarps, int kV, int kRingWarps, int kRingV>
+cudaError_t launch_grad(const NormGradArgs &a, int blocks, cudaStream_t s)
+{
+    if (a.vec) {
+        const RowRing r = make_ring({a.before ? a.s : nullptr, a.before ? a.dx : nullptr, a.y, a.ds, a.gate_map}, a.c, sizeof(T), a.pixels, blocks, 16 / kRingWarps);
+        if (r.stages) return launch_ring<norm_rows_grad_ring_kernel<T, kRingWarps, kRingV>>(a.device, a, r, blocks, kRingWarps * 32, s);
+    }
+    return launch_grad_rows<T, kWarps, kV>(a, blocks, s);
+}
+
+constexpr size_t kTileStatic = 8 * 1024;                      // of the gradient's kernel, and the system's
+size_t grad_tile_bytes(const NormGradArgs &a, size_t size)
+{
+    const int inputs = (a.before ? 2 : 0) + (a.y != nullptr) + (a.ds != nullptr) + (a.gate_map != nullptr);
+    return ((4 * a.c * sizeof(float) + 15) & ~(size_t)15) + (size_t)inputs * a.c * kTilePixels * size;
+}
+
 template <typename T>
 tc_status gradient(const NormGradArgs &a, int blocks, cudaStream_t s)
 {
     cudaError_t err = cudaSuccess;
     if (blocks == 0) {                                        // no pixels: the vectors' gradients are zero
+    } else if (const size_t tile = grad_tile_bytes(a, sizeof(T)); a.hw > 1 && tile + kTileStatic <= kTileSm) {
+        err = allow_shared<norm_maps_grad_tile_kernel<T>>(a.device, kTileSm)
+                  ? launch_first(true, norm_maps_grad_tile_kernel<T>, dim3((unsigned int)blocks), dim3(256), tile, s, a,
+                                 (int)four_pixels<T>(a.hw, a.s, a.dx, a.y, a.ds, a.gate_map)) : cudaErrorInvalidValue;
     } else if (a.hw > 1) {
         const size_t smem = (size_t)2 * a.c * sizeof(float);
-        err = cudaFuncSetAttribute(norm_maps_grad_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (err == cudaSuccess) err = launch_first(true, norm_maps_grad_kernel<T>, dim3((unsigned int)blocks), dim3(256), smem, s, a);
+        err = allow_shared<norm_maps_grad_kernel<T>>(a.device, 2 * kMostChannels * sizeof(float))
+                  ? launch_first(true, norm_maps_grad_kernel<T>, dim3((unsigned int)blocks), dim3(256), smem, s, a) : cudaErrorInvalidValue;
     } else if (a.c <= 256) err = launch_grad_rows<T, 1, 1>(a, blocks, s);
-    else if (a.c <= 512) err = launch_grad_rows<T, 2, 1>(a, blocks, s);
-    else if (a.c <= 1024) err = launch_grad_rows<T, 4, 1>(a, blocks, s);
-    else if (a.c <= 2048) err = launch_grad_rows<T, 8, 1>(a, blocks, s);
-    else if (a.c <= 4096) err = launch_grad_rows<T, 16, 1>(a, blocks, s);
-    else if (a.c <= 8192) err = launch_grad_rows<T, 32, 1>(a, blocks, s);
+    else if (a.c <= 512) err = launch_grad<T, 2, 1, 2, 1>(a, blocks, s);
+    else if (a.c <= 1024) err = launch_grad<T, 4, 1, 2, 2>(a, blocks, s);
+    else if (a.c <= 2048) err = launch_grad<T, 8, 1, 4, 2>(a, blocks, s);
+    else if (a.c <= 4096) err = launch_grad<T, 16, 1, 8, 2>(a, blocks, s);
+    else if (a.c <= 8192) err = launch_grad<T, 32, 1, 16, 2>(a, blocks, s);
     else err = launch_grad_rows<T, 32, 2>(a, blocks, s);
     if (err != cudaSuccess) { cudaGetLastError(); return TC_ERR_CUDA; }
     return launch_chained(blocks > 0, norm_vectors_kernel, dim3((unsigned int)((a.c + 31) / 32)), dim3(256), 0, s, a, blocks) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
@@ -634,8 +1230,9 @@ int tc_norm_grad_blocks(long long pixels, int c, int hw, int sm_count)
     long long rows = pixels, per_sm = 1;
     if (hw > 1) { rows = (pixels + 31) / 32; per_sm = 4; }
     else if (c <= 256) { rows = (pixels + 7) / 8; per_sm = 2; }
-    else for (int w = 2; w < 16 && per_sm == 1; w *= 2)
-        if (c <= 256 * w) per_sm = 16 / w;
+    else if (c <= 1024) per_sm = 8;
+    else if (c <= 2048) per_sm = 4;
+    else if (c <= 4096) per_sm = 2;
     const long long most = per_sm * sm_count;
     return (int)(rows < most ? rows : most);
 }

@@ -1968,6 +1968,9 @@ tc_status tc_residual_norms(tc_ctx *ctx, const tc_tensor *h, const tc_norm_param
     a.c = h->c;
     a.hw = h->h * h->w;
     a.vec = h->c % 8 == 0 && aligned16(a.h, a.y, a.gate_map, a.after, a.gate, a.before, a.sum, a.x);
+    a.sms = ctx->sm_count;
+    a.device = ctx->device;
+    a.status = ctx->d_status;
     return tc_launch_residual_norms(a, h->dtype, (cudaStream_t)cuda_stream);
 }
 
@@ -2021,6 +2024,8 @@ tc_status tc_residual_norms_backward(tc_ctx *ctx, const tc_tensor *s, const tc_n
     const tc_status st = call_scratch(ctx, bytes, bytes, (cudaStream_t)cuda_stream, &scratch);
     if (st != TC_OK) return st;
     a.partial = (float *)scratch.at;
+    a.device = ctx->device;
+    a.status = ctx->d_status;
     a.partial_scale = a.partial + (size_t)blocks * 2 * a.c;
     return tc_launch_residual_norms_backward(a, s->dtype, blocks, (cudaStream_t)cuda_stream);
 }

@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <initializer_list>
 #include <utility>
 #include <vector>
 
@@ -306,6 +307,17 @@ constexpr int kHistCopies = 8;
 constexpr int kExactParallelTilesPerSm = 2;
 
 // ---- block-scaled 8-bit matrices and residual norms -------------------------------------------
+// Shared memory of a kernel, asked for once on a device.
+template <auto kKernel>
+inline bool allow_shared(int device, size_t bytes)
+{
+    static std::atomic<unsigned long long> done{0};
+    const unsigned long long bit = device < 64 ? 1ull << device : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return true;
+    if (cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) { cudaGetLastError(); return false; }
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
 // The kernels' side of tc_blocks: codes [rows][ld], scales [blocks][scale_ld].
 struct BlockMatrix {
     uint8_t *codes = nullptr;
@@ -348,6 +360,8 @@ struct NormArgs {
     BlockMatrix codes;
     long long pixels;
     int c, hw, vec;                   // vec: rows and vectors can be moved 16 bytes at a time
+    int sms, device;
+    unsigned int *status;
 };
 tc_status tc_launch_residual_norms(const NormArgs &a, int dtype, cudaStream_t s);
 struct NormGradArgs {
@@ -360,6 +374,8 @@ struct NormGradArgs {
     int c, hw, vec;
     float *partial;                   // [blocks][2][c]
     float *partial_scale;             // [blocks]
+    int device;
+    unsigned int *status;
 };
 int tc_norm_grad_blocks(long long pixels, int c, int hw, int sm_count);
 tc_status tc_launch_residual_norms_backward(const NormGradArgs &a, int dtype, int blocks, cudaStream_t s);
