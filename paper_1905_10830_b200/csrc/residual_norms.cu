@@ -24,36 +24,68 @@ __device__ __forceinline__ float inv_sqrt(float v) { return rsqrtf(v); }       /
 
 // ---- single pixels (H W = 1): a pixel's channels are a row in memory ------------------------------
 // kWarps warps a row, kV chunks of eight channels a thread; rows of one warp share a block of eight.
-template <typename T, int kV>
-struct RowChunks {
-    Raw8<T> raw[kV];
-};
+// Rows that cannot be moved 16 bytes at a time (kVec false): a thread's eight values lie 32 apart, so that a warp's are neighbours.
 template <int kThreadsRow>
 __device__ __forceinline__ int chunk_at(int t, int i) { return (i * kThreadsRow + t) * 8; }
-
-template <typename T>
-__device__ __forceinline__ void load_chunk(Raw8<T> &r, const T *row, int k, int c, bool vec)
+template <int kThreadsRow, bool kVec>
+__device__ __forceinline__ int value_at(int t, int i, int j)
 {
-    if (k >= c) { zero8(r); return; }
-    if (vec) load8(r, row + k);
-    else load8(r, row + k, min(8, c - k));
+    return kVec ? chunk_at<kThreadsRow>(t, i) + j : i * kThreadsRow * 8 + (t >> 5) * 256 + j * 32 + (t & 31);
 }
-__device__ __forceinline__ void load_vector(float (&f)[8], const float *v, int k, int c, bool vec)
+template <typename T, int kThreadsRow, bool kVec>
+__device__ __forceinline__ void load_values(Raw8<T> &r, const T *row, int t, int i, int c)
 {
-    if (vec && k < c) {
-        const float4 a = reinterpret_cast<const float4 *>(v + k)[0], b = reinterpret_cast<const float4 *>(v + k)[1];
-        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    zero8(r);
+    if constexpr (kVec) {
+        const int k = chunk_at<kThreadsRow>(t, i);
+        if (k < c) load8(r, row + k);
     } else {
+        uint32_t h[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = k + j < c ? v[k + j] : 0.f;
+        for (int j = 0; j < 8; ++j) {
+            const int k = value_at<kThreadsRow, false>(t, i, j);
+            h[j] = 0u;
+            if (k < c) {
+                if constexpr (sizeof(T) == 2) h[j] = reinterpret_cast<const unsigned short *>(row)[k];
+                else h[j] = reinterpret_cast<const uint32_t *>(row)[k];
+            }
+        }
+        if constexpr (sizeof(T) == 2) r.v = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+        else { r.v = make_uint4(h[0], h[1], h[2], h[3]); r.w = make_uint4(h[4], h[5], h[6], h[7]); }
     }
 }
-template <typename T>
-__device__ __forceinline__ void store_chunk(T *row, const float (&f)[8], int k, int c, bool vec)
+template <int kThreadsRow, bool kVec>
+__device__ __forceinline__ void load_weights(float (&f)[8], const float *v, int t, int i, int c)
 {
-    if (k >= c) return;
-    if (vec) store8(row + k, f);
-    else store8(row + k, f, min(8, c - k));
+    if constexpr (kVec) {
+        const int k = chunk_at<kThreadsRow>(t, i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = 0.f;
+        if (k < c) {
+            const float4 a = reinterpret_cast<const float4 *>(v + k)[0], b = reinterpret_cast<const float4 *>(v + k)[1];
+            f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int k = value_at<kThreadsRow, false>(t, i, j);
+            f[j] = k < c ? v[k] : 0.f;
+        }
+    }
+}
+template <typename T, int kThreadsRow, bool kVec>
+__device__ __forceinline__ void store_values(T *row, const float (&f)[8], int t, int i, int c)
+{
+    if constexpr (kVec) {
+        const int k = chunk_at<kThreadsRow>(t, i);
+        if (k < c) store8(row + k, f);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int k = value_at<kThreadsRow, false>(t, i, j);
+            if (k < c) store1(row + k, f[j]);
+        }
+    }
 }
 
 template <int kWarps>
@@ -72,19 +104,38 @@ __device__ __forceinline__ float row_sum(float v, float *s_part)
     return v;
 }
 
-// Codes of eight values of a row; 16 threads' are a block.
-__device__ __forceinline__ void store_codes(const BlockMatrix &to, const float (&x)[8], long long row, int k, int c, int t)
+// Codes of a thread's eight values of a row: 16 threads' are a block, or four of each of a warp's.
+template <int kThreadsRow, bool kVec>
+__device__ __forceinline__ void store_codes(const BlockMatrix &to, const float (&x)[8], long long row, int t, int i, int c)
 {
-    uint32_t m = 0;
+    uint8_t *const codes = to.codes + row * to.ld;
+    if constexpr (kVec) {
+        const int k = chunk_at<kThreadsRow>(t, i);
+        uint32_t m = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, abs_bits(x[j]));
-    const float scale = scale_of(max16(m));
-    if (k >= c) return;
-    *reinterpret_cast<uint2 *>(to.codes + row * to.ld + k) = codes8(x, __frcp_rn(scale));
-    if ((t & 15) == 0) to.scales[(long long)(k / kBlock) * to.scale_ld + row] = scale;
+        for (int j = 0; j < 8; ++j) m = max(m, abs_bits(x[j]));
+        const float scale = scale_of(max16(m));
+        if (k >= c) return;
+        *reinterpret_cast<uint2 *>(codes + k) = codes8(x, __frcp_rn(scale));
+        if ((t & 15) == 0) to.scales[(long long)(k / kBlock) * to.scale_ld + row] = scale;
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int k = value_at<kThreadsRow, false>(t, i, 4 * h);
+            uint32_t m = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) m = max(m, abs_bits(x[4 * h + j]));
+            const float scale = scale_of(__reduce_max_sync(0xffffffffu, m));
+            const uint32_t four = codes4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3], __frcp_rn(scale));
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (k + 32 * j < c) codes[k + 32 * j] = (uint8_t)(four >> 8 * j);
+            if ((t & 31) == 0 && k < c) to.scales[(long long)(k / kBlock) * to.scale_ld + row] = scale;
+        }
+    }
 }
 
-template <typename T, int kWarps, int kV>
+template <typename T, int kWarps, int kV, bool kVec>
 __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32) norm_rows_kernel(NormArgs a)
 {
     constexpr int kThreadsRow = kWarps * 32;
@@ -94,15 +145,13 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32) norm_rows_ker
     const int t = threadIdx.x % kThreadsRow;
     const long long row = kWarps == 1 ? (long long)blockIdx.x * 8 + (threadIdx.x >> 5) : (long long)blockIdx.x;
     if (row >= a.pixels) return;                              // whole warps; with more than one a row, whole blocks
-    const bool vec = a.vec != 0;
     const long long base = row * a.c;
     Raw8<T> rh[kV], ry[kV], rg[kV];
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
-        const int k = chunk_at<kThreadsRow>(t, i);
-        load_chunk(rh[i], (const T *)a.h + base, k, a.c, vec);
-        if (a.y) load_chunk(ry[i], (const T *)a.y + base, k, a.c, vec);
-        if (a.gate_map) load_chunk(rg[i], (const T *)a.gate_map + base, k, a.c, vec);
+        load_values<T, kThreadsRow, kVec>(rh[i], (const T *)a.h + base, t, i, a.c);
+        if (a.y) load_values<T, kThreadsRow, kVec>(ry[i], (const T *)a.y + base, t, i, a.c);
+        if (a.gate_map) load_values<T, kThreadsRow, kVec>(rg[i], (const T *)a.gate_map + base, t, i, a.c);
     }
     float s[kV][8];
 #pragma unroll
@@ -124,25 +173,24 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32) norm_rows_ker
         const float scale = a.scale ? *a.scale : 1.f;
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
-            const int k = chunk_at<kThreadsRow>(t, i);
             float u[8];
             values8(ry[i], u);
             if (a.after) {
                 float w[8];
-                load_vector(w, a.after, k, a.c, vec);
+                load_weights<kThreadsRow, kVec>(w, a.after, t, i, a.c);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) u[j] = u[j] * q * w[j];
             }
             if (a.gate_map || a.gate) {
                 float g[8];
                 if (a.gate_map) values8(rg[i], g);
-                else load_vector(g, a.gate, k, a.c, vec);
+                else load_weights<kThreadsRow, kVec>(g, a.gate, t, i, a.c);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) u[j] *= g[j];
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[i][j] = fmaf(scale, u[j], s[i][j]);
-            store_chunk((T *)a.sum + base, s[i], k, a.c, vec);
+            store_values<T, kThreadsRow, kVec>((T *)a.sum + base, s[i], t, i, a.c);
         }
     }
     if (!a.before) return;
@@ -154,13 +202,12 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32) norm_rows_ker
     const float r = inv_sqrt(fmaf(row_sum<kWarps>(sum, s_part[1]), inv_c, a.eps));
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
-        const int k = chunk_at<kThreadsRow>(t, i);
         float w[8];
-        load_vector(w, a.before, k, a.c, vec);
+        load_weights<kThreadsRow, kVec>(w, a.before, t, i, a.c);
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = s[i][j] * r * w[j];
-        if (a.x) store_chunk((T *)a.x + base, w, k, a.c, vec);
-        if (a.codes.codes) store_codes(a.codes, w, row, k, a.c, t);
+        if (a.x) store_values<T, kThreadsRow, kVec>((T *)a.x + base, w, t, i, a.c);
+        if (a.codes.codes) store_codes<kThreadsRow, kVec>(a.codes, w, row, t, i, a.c);
     }
 }
 
@@ -235,13 +282,12 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_ring_kerne
     float wy[kV][8], wx[kV][8];                               // after times the channels' gate; before
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
-        const int k = chunk_at<kThreadsRow>(t, i);
         float g[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) wy[i][j] = wx[i][j] = g[j] = 1.f;
-        if (a.after) load_vector(wy[i], a.after, k, a.c, true);
-        if (a.gate) load_vector(g, a.gate, k, a.c, true);
-        if (a.before) load_vector(wx[i], a.before, k, a.c, true);
+        if (a.after) load_weights<kThreadsRow, true>(wy[i], a.after, t, i, a.c);
+        if (a.gate) load_weights<kThreadsRow, true>(g, a.gate, t, i, a.c);
+        if (a.before) load_weights<kThreadsRow, true>(wx[i], a.before, t, i, a.c);
 #pragma unroll
         for (int j = 0; j < 8; ++j) wy[i][j] *= g[j];
     }
@@ -271,7 +317,6 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_ring_kerne
         sum = 0.f;
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
-            const int k = chunk_at<kThreadsRow>(t, i);
             float y[8];
             values8(ry[i], y);
             values8(rh[i], s[i]);
@@ -286,18 +331,17 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_ring_kerne
                 s[i][j] = fmaf(f, y[j] * wy[i][j], s[i][j]);
                 sum = fmaf(s[i][j], s[i][j], sum);
             }
-            store_chunk((T *)a.sum + base, s[i], k, a.c, true);
+            store_values<T, kThreadsRow, true>((T *)a.sum + base, s[i], t, i, a.c);
         }
         if (a.before) {
             const float rr = inv_sqrt(fmaf(row_sum<kWarps>(sum, s_part[1]), inv_c, a.eps));
 #pragma unroll
             for (int i = 0; i < kV; ++i) {
-                const int k = chunk_at<kThreadsRow>(t, i);
                 float x[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = s[i][j] * rr * wx[i][j];
-                if (a.x) store_chunk((T *)a.x + base, x, k, a.c, true);
-                if (a.codes.codes) store_codes(a.codes, x, row, k, a.c, t);
+                if (a.x) store_values<T, kThreadsRow, true>((T *)a.x + base, x, t, i, a.c);
+                if (a.codes.codes) store_codes<kThreadsRow, true>(a.codes, x, row, t, i, a.c);
             }
         } else
             __syncthreads();                                  // the row's partial sums are read before the next row's are written
@@ -594,7 +638,7 @@ __device__ __forceinline__ void row_sums(float (&v)[8], float (*s_part)[8])
     for (int i = 0; i < kSums; ++i) v[i] = __shfl_sync(0xffffffffu, mine, 4 * i);
 }
 
-template <typename T, int kWarps, int kV>
+template <typename T, int kWarps, int kV, bool kVec>
 __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32, kWarps == 1 ? 2 : (kWarps >= 16 ? 1 : 16 / kWarps)) norm_rows_grad_kernel(NormGradArgs a)
 {
     constexpr int kThreadsRow = kWarps * 32, kRows = kWarps == 1 ? 8 : 1;
@@ -604,7 +648,6 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32, kWarps == 1 ?
     chain_next();
     chain_wait();
     const int t = threadIdx.x % kThreadsRow, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const bool vec = a.vec != 0;
     const float scale = a.y && a.scale ? *a.scale : 1.f;
     float sum_y[kV][8], sum_x[kV][8], sum_scale = 0.f;        // D n (times a map's gate);  dx s r
 #pragma unroll
@@ -617,31 +660,32 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32, kWarps == 1 ?
         Raw8<T> rs[kV], ry[kV], rx[kV], rd[kV], rg[kV];
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
-            const int k = chunk_at<kThreadsRow>(t, i);
             zero8(rs[i]); zero8(ry[i]); zero8(rx[i]); zero8(rd[i]);
-            if (a.before) { load_chunk(rs[i], (const T *)a.s + base, k, a.c, vec); load_chunk(rx[i], (const T *)a.dx + base, k, a.c, vec); }
-            if (a.y) load_chunk(ry[i], (const T *)a.y + base, k, a.c, vec);
-            if (a.ds) load_chunk(rd[i], (const T *)a.ds + base, k, a.c, vec);
-            if (a.gate_map) load_chunk(rg[i], (const T *)a.gate_map + base, k, a.c, vec);
+            if (a.before) {
+                load_values<T, kThreadsRow, kVec>(rs[i], (const T *)a.s + base, t, i, a.c);
+                load_values<T, kThreadsRow, kVec>(rx[i], (const T *)a.dx + base, t, i, a.c);
+            }
+            if (a.y) load_values<T, kThreadsRow, kVec>(ry[i], (const T *)a.y + base, t, i, a.c);
+            if (a.ds) load_values<T, kThreadsRow, kVec>(rd[i], (const T *)a.ds + base, t, i, a.c);
+            if (a.gate_map) load_values<T, kThreadsRow, kVec>(rg[i], (const T *)a.gate_map + base, t, i, a.c);
         }
         // gate times after of a chunk
-        auto factors = [&](int i, int k, float (&g)[8], float (&w)[8]) {
+        auto factors = [&](int i, float (&g)[8], float (&w)[8]) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) g[j] = w[j] = 1.f;
             if (a.gate_map) values8(rg[i], g);
-            else if (a.gate) load_vector(g, a.gate, k, a.c, vec);
-            if (a.after) load_vector(w, a.after, k, a.c, vec);
+            else if (a.gate) load_weights<kThreadsRow, kVec>(g, a.gate, t, i, a.c);
+            if (a.after) load_weights<kThreadsRow, kVec>(w, a.after, t, i, a.c);
         };
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
-            const int k = chunk_at<kThreadsRow>(t, i);
             float s[8], y[8], dx[8], ds[8], g[8], w[8], b[8];
             values8(rs[i], s); values8(ry[i], y); values8(rx[i], dx); values8(rd[i], ds);
-            factors(i, k, g, w);
+            factors(i, g, w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) b[j] = 0.f;
-            if (a.before) load_vector(b, a.before, k, a.c, vec);
+            if (a.before) load_weights<kThreadsRow, kVec>(b, a.before, t, i, a.c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float tt = dx[j] * b[j], gy = g[j] * w[j] * y[j];
@@ -658,19 +702,18 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32, kWarps == 1 ?
         const PixelFactors f = pixel_factors(sums, a, scale);
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
-            const int k = chunk_at<kThreadsRow>(t, i);
             float s[8], y[8], dx[8], d[8], g[8], w[8], b[8];
             values8(rs[i], s); values8(ry[i], y); values8(rx[i], dx); values8(rd[i], d);
-            factors(i, k, g, w);
+            factors(i, g, w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) b[j] = 0.f;
-            if (a.before) load_vector(b, a.before, k, a.c, vec);
+            if (a.before) load_weights<kThreadsRow, kVec>(b, a.before, t, i, a.c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 d[j] = fmaf(-f.r3m, s[j], fmaf(f.r, dx[j] * b[j], d[j]));
                 sum_x[i][j] = fmaf(dx[j] * f.r, s[j], sum_x[i][j]);
             }
-            store_chunk((T *)a.dh + base, d, k, a.c, vec);
+            store_values<T, kThreadsRow, kVec>((T *)a.dh + base, d, t, i, a.c);
             if (a.y) {
                 float dy[8], dg[8];
 #pragma unroll
@@ -681,8 +724,8 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32, kWarps == 1 ?
                     dg[j] = scale * (dn * w[j]);
                     dy[j] = f.q * fmaf(-n, f.mean, scale * (d[j] * (g[j] * w[j])));
                 }
-                store_chunk((T *)a.dy + base, dy, k, a.c, vec);
-                if (a.gate_map) store_chunk((T *)a.dgate_map + base, dg, k, a.c, vec);
+                store_values<T, kThreadsRow, kVec>((T *)a.dy + base, dy, t, i, a.c);
+                if (a.gate_map) store_values<T, kThreadsRow, kVec>((T *)a.dgate_map + base, dg, t, i, a.c);
             }
         }
     }
@@ -695,8 +738,8 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32, kWarps == 1 ?
         for (int i = 0; i < kV; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                mine[chunk_at<32>(lane, i) + j] = sum_y[i][j];
-                mine[kRow + chunk_at<32>(lane, i) + j] = sum_x[i][j];
+                mine[value_at<32, kVec>(lane, i, j)] = sum_y[i][j];
+                mine[kRow + value_at<32, kVec>(lane, i, j)] = sum_x[i][j];
             }
         __syncthreads();
         for (int i = threadIdx.x; i < 2 * kRow; i += 256) {
@@ -709,13 +752,8 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32, kWarps == 1 ?
     } else {
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
-            const int k = chunk_at<kThreadsRow>(t, i);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (k + j < a.c) {
-                    part[k + j] = sum_y[i][j];
-                    part[a.c + k + j] = sum_x[i][j];
-                }
+            store_values<float, kThreadsRow, kVec>(part, sum_y[i], t, i, a.c);
+            store_values<float, kThreadsRow, kVec>(part + a.c, sum_x[i], t, i, a.c);
         }
     }
 #pragma unroll
@@ -751,13 +789,12 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
     float wy[kV][8], wx[kV][8], sum_y[kV][8], sum_x[kV][8], sum_scale = 0.f;
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
-        const int k = chunk_at<kThreadsRow>(t, i);
         float g[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) { wy[i][j] = g[j] = 1.f; wx[i][j] = sum_y[i][j] = sum_x[i][j] = 0.f; }
-        if (a.after) load_vector(wy[i], a.after, k, a.c, true);
-        if (a.gate) load_vector(g, a.gate, k, a.c, true);
-        if (a.before) load_vector(wx[i], a.before, k, a.c, true);
+        if (a.after) load_weights<kThreadsRow, true>(wy[i], a.after, t, i, a.c);
+        if (a.gate) load_weights<kThreadsRow, true>(g, a.gate, t, i, a.c);
+        if (a.before) load_weights<kThreadsRow, true>(wx[i], a.before, t, i, a.c);
 #pragma unroll
         for (int j = 0; j < 8; ++j) wy[i][j] *= g[j];
     }
@@ -823,7 +860,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
                     sum_x[i][j] = fmaf(rx, s[j], sum_x[i][j]);
                 }
             }
-            store_chunk((T *)a.dh + base, d, k, a.c, true);
+            store_values<T, kThreadsRow, true>((T *)a.dh + base, d, t, i, a.c);
             if (a.y) {
                 get(true, at_y, k, y);
 #pragma unroll
@@ -838,8 +875,8 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
                     sum_y[i][j] = a.gate_map ? fmaf(dn, g[j], sum_y[i][j]) : sum_y[i][j] + dn;
                     dy[j] = fmaf(-y[j], mean_q, scale_q * (dw * g[j]));
                 }
-                store_chunk((T *)a.dy + base, dy, k, a.c, true);
-                if (a.gate_map) store_chunk((T *)a.dgate_map + base, dg, k, a.c, true);
+                store_values<T, kThreadsRow, true>((T *)a.dy + base, dy, t, i, a.c);
+                if (a.gate_map) store_values<T, kThreadsRow, true>((T *)a.dgate_map + base, dg, t, i, a.c);
             }
         }
         last = slot;
@@ -848,9 +885,8 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
     float *const to = a.partial + (long long)blockIdx.x * 2 * a.c;
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
-        const int k = chunk_at<kThreadsRow>(t, i);
-        store_chunk(to, sum_y[i], k, a.c, true);
-        store_chunk(to + a.c, sum_x[i], k, a.c, true);
+        store_values<float, kThreadsRow, true>(to, sum_y[i], t, i, a.c);
+        store_values<float, kThreadsRow, true>(to + a.c, sum_x[i], t, i, a.c);
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1) sum_scale += __shfl_xor_sync(0xffffffffu, sum_scale, d);
@@ -1100,7 +1136,7 @@ template <typename T, int kWarps, int kV>
 tc_status launch_norm_rows(const NormArgs &a, cudaStream_t s)
 {
     const long long blocks = kWarps == 1 ? (a.pixels + 7) / 8 : a.pixels;
-    return launch_first(true, norm_rows_kernel<T, kWarps, kV>, dim3((unsigned int)blocks), dim3(kWarps == 1 ? 256 : kWarps * 32), 0, s, a) == cudaSuccess
+    return launch_first(true, a.vec ? norm_rows_kernel<T, kWarps, kV, true> : norm_rows_kernel<T, kWarps, kV, false>, dim3((unsigned int)blocks), dim3(kWarps == 1 ? 256 : kWarps * 32), 0, s, a) == cudaSuccess
                ? TC_OK : TC_ERR_CUDA;
 }
 
@@ -1172,18 +1208,22 @@ template <typename T, int kWarps, int kV>
 cudaError_t launch_grad_rows(const NormGradArgs &a, int blocks, cudaStream_t s)
 {
     const size_t smem = kWarps == 1 ? 8 * 2 * 256 * kV * sizeof(float) : 0;
-    return launch_first(true, norm_rows_grad_kernel<T, kWarps, kV>, dim3((unsigned int)blocks), dim3(kWarps == 1 ? 256 : kWarps * 32), smem, s, a);
+    return launch_first(true, a.vec ? norm_rows_grad_kernel<T, kWarps, kV, true> : norm_rows_grad_kernel<T, kWarps, kV, false>, dim3((unsigned int)blocks), dim3(kWarps == 1 ? 256 : kWarps * 32), smem, s, a);
 }
 
-// With the ring of rows where there is one: kRingWarps warps of kRingV chunks a thread, as many blocks as an SM's 512 threads.
-template <typename T, int kWarps, int kV, int kRingWarps, int kRingV>
+// With the ring of rows where there is one: two chunks a thread of bf16, whose unpacking and sums bound it (16384x4096 209 us with one
+// and 166); one of fp32, of whose rows two would not fit two blocks' rings.  Blocks of 512 threads an SM in all.
+constexpr int ring_chunks(int warps, int size) { return warps <= 2 ? 1 : warps > 16 ? warps / 16 : size == 2 ? 2 : 1; }
+// Rows of up to 256 kWarps channels.
+template <typename T, int kWarps>
 cudaError_t launch_grad(const NormGradArgs &a, int blocks, cudaStream_t s)
 {
+    constexpr int kRingV = ring_chunks(kWarps, sizeof(T)), kRingWarps = kWarps / kRingV;
     if (a.vec) {
         const RowRing r = make_ring({a.before ? a.s : nullptr, a.before ? a.dx : nullptr, a.y, a.ds, a.gate_map}, a.c, sizeof(T), a.pixels, blocks, 16 / kRingWarps);
         if (r.stages) return launch_ring<norm_rows_grad_ring_kernel<T, kRingWarps, kRingV>>(a.device, a, r, blocks, kRingWarps * 32, s);
     }
-    return launch_grad_rows<T, kWarps, kV>(a, blocks, s);
+    return launch_grad_rows<T, kWarps, 1>(a, blocks, s);
 }
 
 constexpr size_t kTileStatic = 8 * 1024;                      // of the gradient's kernel, and the system's
@@ -1207,11 +1247,11 @@ tc_status gradient(const NormGradArgs &a, int blocks, cudaStream_t s)
         err = allow_shared<norm_maps_grad_kernel<T>>(a.device, 2 * kMostChannels * sizeof(float))
                   ? launch_first(true, norm_maps_grad_kernel<T>, dim3((unsigned int)blocks), dim3(256), smem, s, a) : cudaErrorInvalidValue;
     } else if (a.c <= 256) err = launch_grad_rows<T, 1, 1>(a, blocks, s);
-    else if (a.c <= 512) err = launch_grad<T, 2, 1, 2, 1>(a, blocks, s);
-    else if (a.c <= 1024) err = launch_grad<T, 4, 1, 2, 2>(a, blocks, s);
-    else if (a.c <= 2048) err = launch_grad<T, 8, 1, 4, 2>(a, blocks, s);
-    else if (a.c <= 4096) err = launch_grad<T, 16, 1, 8, 2>(a, blocks, s);
-    else if (a.c <= 8192) err = launch_grad<T, 32, 1, 16, 2>(a, blocks, s);
+    else if (a.c <= 512) err = launch_grad<T, 2>(a, blocks, s);
+    else if (a.c <= 1024) err = launch_grad<T, 4>(a, blocks, s);
+    else if (a.c <= 2048) err = launch_grad<T, 8>(a, blocks, s);
+    else if (a.c <= 4096) err = launch_grad<T, 16>(a, blocks, s);
+    else if (a.c <= 8192) err = launch_grad<T, 32>(a, blocks, s);
     else err = launch_grad_rows<T, 32, 2>(a, blocks, s);
     if (err != cudaSuccess) { cudaGetLastError(); return TC_ERR_CUDA; }
     return launch_chained(blocks > 0, norm_vectors_kernel, dim3((unsigned int)((a.c + 31) / 32)), dim3(256), 0, s, a, blocks) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
@@ -1225,14 +1265,14 @@ tc_status tc_launch_residual_norms(const NormArgs &a, int dtype, cudaStream_t s)
 }
 
 // Blocks of the gradient's kernel: as many as an SM holds of its row's width, four of the maps' kernel.
-int tc_norm_grad_blocks(long long pixels, int c, int hw, int sm_count)
+int tc_norm_grad_blocks(long long pixels, int c, int hw, int dtype, int sm_count)
 {
     long long rows = pixels, per_sm = 1;
     if (hw > 1) { rows = (pixels + 31) / 32; per_sm = 4; }
     else if (c <= 256) { rows = (pixels + 7) / 8; per_sm = 2; }
-    else if (c <= 1024) per_sm = 8;
-    else if (c <= 2048) per_sm = 4;
-    else if (c <= 4096) per_sm = 2;
+    else
+        for (int warps = 2; warps <= 16; warps *= 2)
+            if (c <= 256 * warps) { per_sm = 16 * ring_chunks(warps, dtype == TC_BF16 ? 2 : 4) / warps; break; }
     const long long most = per_sm * sm_count;
     return (int)(rows < most ? rows : most);
 }

@@ -89,31 +89,40 @@ def _check(got, want, tol, name):
     assert not bad.any(), (name, int(bad.sum()), ((got.double() - want).abs() / tol).max().item())
 
 
+def _check_forward(d, s, x):
+    """s and x against the formulas; (x, its error but for the last rounding)."""
+    s64, x64 = _forward64(**_in64(d))
+    k = _chain(s64.shape[1])
+    branch = (s64 - d["h"].double()).abs()
+    # the sum: the branch's own roundings and one of the sum
+    err_s = branch * k + s64.abs() * 2.0 ** -24
+    if d["y"] is None:
+        err_s = torch.zeros_like(s64)
+    else:
+        _check(s, s64, err_s, "s")
+    if d["before"] is None:
+        assert x is None
+        return None, None
+    # x: what the errors of s do to it (through itself and through the mean), and its own roundings
+    r = 1 / torch.sqrt((s64 * s64).mean(1, keepdim=True) + EPS)
+    b = _vec(d["before"]).abs()
+    err_x = b * (err_s * r + s64.abs() * r ** 3 * (s64.abs() * err_s).mean(1, keepdim=True)) + x64.abs() * k
+    _check(x, x64, err_x, "x")
+    return x64, err_x
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("mix", MIXES)
 @pytest.mark.parametrize("shape", SHAPES)
 def test_forward(ctx, shape, mix, dtype):
     d = _mix(shape, dtype, mix)
     keep = {k: None if v is None else v.clone() for k, v in d.items()}
-    s64, x64 = _forward64(**_in64(d))
     s, x = tc.tc_residual_norms(ctx, **d, eps=EPS)
-    k = _chain(shape[1])
-    branch = (s64 - d["h"].double()).abs()
-    # the sum: the branch's own roundings and one of the sum
-    err_s = branch * k + s64.abs() * 2.0 ** -24
     if d["y"] is None:
         assert s is d["h"]
-        err_s = torch.zeros_like(s64)
-    else:
-        _check(s, s64, err_s, "s")
+    x64, err_x = _check_forward(d, s, x)
     if d["before"] is None:
-        assert x is None
         return
-    # x: what the errors of s do to it (through itself and through the mean), and its own roundings
-    r = 1 / torch.sqrt((s64 * s64).mean(1, keepdim=True) + EPS)
-    b = _vec(d["before"]).abs()
-    err_x = b * (err_s * r + s64.abs() * r ** 3 * (s64.abs() * err_s).mean(1, keepdim=True)) + x64.abs() * k
-    _check(x, x64, err_x, "x")
     s2, blocks = tc.tc_residual_norms(ctx, **d, eps=EPS, blocks=True)
     assert torch.equal(s, s2)
     want, err = (t.permute(0, 2, 3, 1).reshape(-1, shape[1]) for t in (x64, err_x))
@@ -245,12 +254,11 @@ def test_views_at_odd_addresses_and_guards(ctx):
                 return flat, flat[1:1 + t.numel()].view(t.shape)
 
             rooms = {k: odd(v) for k, v in d.items()}
-            want = tc.tc_residual_norms(ctx, **d, eps=EPS)
             room_s, s = odd(torch.zeros(shape, dtype=dtype, device="cuda"))
             room_x, x = odd(torch.zeros(shape, dtype=dtype, device="cuda"))
             got = tc.tc_residual_norms(ctx, **{k: v[1] for k, v in rooms.items()}, eps=EPS, sum_out=s, out=x)
             assert got[0] is s and got[1] is x
-            assert torch.equal(want[0], s) and torch.equal(want[1], x)
+            _check_forward(d, s, x)                            # (another order of the sums than at aligned addresses: the same bounds)
             for room in (room_s, room_x):
                 assert room[0] == 2.5 and (room[1 + n:] == 2.5).all()
 
