@@ -500,31 +500,31 @@ tc_status tc_matmul_blocks(tc_ctx *ctx, const tc_blocks *a, const tc_blocks *b, 
  *     x = s / sqrt(mean_c s^2 + eps) * before
  * Statistics, sums and products in fp32; s and x are rounded once, x is computed from the s that is not rounded yet. */
 typedef struct {
-    const tc_tensor *y;        /* layer's output; NULL: s = h, which is not written                     */
+    const void *y;             /* layer's output; NULL: s = h, which is not written                     */
     const float *after;        /* DEVICE [C]; NULL: no norm after the layer                             */
     const float *gate;         /* DEVICE [C]; NULL: none                                                */
-    const tc_tensor *gate_map; /* a gate for each value, of y's shape and type, instead of `gate`; or NULL */
+    const void *gate_map;      /* a gate for each value, instead of `gate`; or NULL                     */
     const float *scale;        /* DEVICE [1]; NULL: 1                                                   */
     const float *before;       /* DEVICE [C]; NULL: no x                                                */
     float eps;                 /* >= 0                                                                  */
 } tc_norm_params;
 
 /* `sum` receives s (required with y), `x` and `codes` (block codes by pixels, not square) receive x; either or both, with `before`.
- * All tensors have the shape and type of `h`; outputs overlap neither inputs nor each other.  May be captured into a graph.
+ * y, gate_map, sum and x are DEVICE tensors of the shape and type of `h`; outputs overlap neither inputs nor each other.  May be captured into a graph.
  * Errors: INVALID_ARG, UNSUPPORTED (more than 16384 channels, more than 2^31 - 256 pixels), CUDA. */
-tc_status tc_residual_norms(tc_ctx *ctx, const tc_tensor *h, const tc_norm_params *params, const tc_tensor *sum, const tc_tensor *x,
-                            const tc_blocks *codes, void *cuda_stream);
+tc_status tc_residual_norms(tc_ctx *ctx, const tc_tensor *h, const tc_norm_params *params, void *sum, void *x, const tc_blocks *codes,
+                            void *cuda_stream);
 
 /* Gradients of tc_residual_norms at the sum `s` it wrote (y = NULL: at h), from those of x (`dx`, NULL exactly without `before`; the same
  * whether x left as a tensor or as codes) and of s (`ds`, NULL = zero).  dh always; dy where y is given; the others where wanted, each only where
- * its input is given (scale's may be asked for with y).  Gradients of vectors are sums over all pixels, in fp32, in an order that does not depend on
+ * its input is given (scale's may be asked for with y).  dx, ds, dh, dy and dgate_map are DEVICE tensors like `s`.  Gradients of vectors are sums over all pixels, in fp32, in an order that does not depend on
  * timing.  Conventions and errors as above. */
 typedef struct {
-    const tc_tensor *dh, *dy;
-    const tc_tensor *dgate_map;                  /* required with gate_map               */
+    void *dh, *dy;
+    void *dgate_map;                             /* required with gate_map               */
     float *dafter, *dgate, *dscale, *dbefore;    /* DEVICE [C], [C], [1], [C], or NULL   */
 } tc_norm_grads;
-tc_status tc_residual_norms_backward(tc_ctx *ctx, const tc_tensor *s, const tc_norm_params *params, const tc_tensor *dx, const tc_tensor *ds,
+tc_status tc_residual_norms_backward(tc_ctx *ctx, const tc_tensor *s, const tc_norm_params *params, const void *dx, const void *ds,
                                      const tc_norm_grads *out, void *cuda_stream);
 
 #ifdef __cplusplus

@@ -633,8 +633,9 @@ class Blocks:
 
     @classmethod
     def empty(cls, rows: int, cols: int, square: bool = False, device="cuda") -> "Blocks":
-        return cls(*_block_buffers(torch.empty(0, dtype=torch.float8_e4m3fn, device=device), torch.empty(0, dtype=torch.float32, device=device),
-                                   rows, cols, square), cols, square)
+        tall = -(-rows // 128)
+        return cls(torch.empty((rows, -(-cols // 16) * 16), dtype=torch.float8_e4m3fn, device=device),
+                   torch.empty((-(-cols // 128), tall if square else tall * 128), dtype=torch.float32, device=device), cols, square)
 
     def dequantize(self) -> torch.Tensor:
         """The values the codes stand for, float32 [rows, cols] (for inspection; no product reads them)."""
@@ -642,31 +643,35 @@ class Blocks:
         return self.codes[:, :self.cols].float() * scales[:, :self.rows].t().repeat_interleave(128, 1)[:, :self.cols]
 
 
-def _block_buffers(codes, scales, rows, cols, square):
-    tall = (rows + 127) // 128
-    return codes.new_empty(rows, (cols + 15) // 16 * 16), scales.new_empty((cols + 127) // 128, tall if square else tall * 128)
+def _empty(ctx: Context, dtype):
+    """An empty tensor on the context's device, to make others of its type from."""
+    if ctx.empty is None:
+        ctx.empty = {}
+    t = ctx.empty.get(dtype)
+    if t is None:
+        t = ctx.empty[dtype] = torch.empty(0, dtype=dtype, device=f"cuda:{ctx.device}")
+    return t
 
 
 def _new_blocks(ctx: Context, rows: int, cols: int, square: bool):
     """Blocks on the context's device, and their C structure."""
-    if ctx.empty is None:
-        ctx.empty = tuple(torch.empty(0, dtype=t, device=f"cuda:{ctx.device}") for t in (torch.float8_e4m3fn, torch.float32))
-    codes, scales = _block_buffers(*ctx.empty, rows, cols, square)
-    return Blocks(codes, scales, cols, square), _Blocks(codes.data_ptr(), scales.data_ptr(), (cols + 15) // 16 * 16, rows, cols, square)
+    ld, tall = (cols + 15) // 16 * 16, (rows + 127) // 128
+    codes = _empty(ctx, torch.float8_e4m3fn).new_empty(rows, ld)
+    scales = _empty(ctx, torch.float32).new_empty((cols + 127) // 128, tall if square else tall * 128)
+    return Blocks(codes, scales, cols, square), _Blocks(codes.data_ptr(), scales.data_ptr(), ld, rows, cols, square)
 
 
 def _blocks(ctx: Context, b: Blocks) -> _Blocks:
-    codes, scales = b.codes, b.scales
-    if codes.get_device() != ctx.device or scales.get_device() != ctx.device:
-        raise ValueError(_ELSEWHERE)
-    if codes.dim() != 2 or scales.dim() != 2 or codes.dtype != torch.float8_e4m3fn or scales.dtype != torch.float32 or \
-            not codes.is_contiguous() or not scales.is_contiguous():
-        raise ValueError("block matrices have contiguous float8_e4m3fn codes [rows, ld] and float32 scales")
+    codes, scales, cols, device = b.codes, b.scales, b.cols, ctx.device
+    if codes.dtype is not torch.float8_e4m3fn or scales.dtype is not torch.float32 or not codes.is_contiguous() or not scales.is_contiguous() or \
+            codes.get_device() != device or scales.get_device() != device:
+        raise ValueError("block matrices have contiguous float8_e4m3fn codes [rows, ld] and float32 scales on the context's device")
     rows, ld = codes.shape
+    high, wide = scales.shape
     tall = (rows + 127) // 128
-    if not 0 <= b.cols <= ld or scales.shape != ((b.cols + 127) // 128, tall if b.square else tall * 128):
+    if not 0 <= cols <= ld or high != (cols + 127) // 128 or wide != (tall if b.square else tall * 128):
         raise ValueError("block matrix: codes, scales and cols do not belong together")
-    return _Blocks(codes.data_ptr(), scales.data_ptr(), ld, rows, b.cols, b.square)
+    return _Blocks(codes.data_ptr(), scales.data_ptr(), ld, rows, cols, b.square)
 
 
 _ELSEWHERE = "expected tensors on the context's device"
@@ -679,12 +684,21 @@ def _local(ctx: Context, x: torch.Tensor) -> _Tensor:
     return t
 
 
-def _vector(ctx: Context, v, n: int, name: str) -> int | None:
+def _vector(device: int, v, n: int, name: str) -> int | None:
     if v is None:
         return None
-    if v.dtype != torch.float32 or v.numel() != n or not v.is_contiguous() or v.get_device() != ctx.device:
+    if v.dtype is not torch.float32 or v.numel() != n or v.get_device() != device or not v.is_contiguous():
         raise ValueError(f"{name}: expected {n} contiguous float32 values on the context's device")
     return v.data_ptr()
+
+
+def _like(v, h: torch.Tensor, device: int, name: str) -> int | None:
+    """The address of a tensor of h's shape and type."""
+    if v is None:
+        return None
+    if v.shape != h.shape or v.dtype is not h.dtype or v.get_device() != device or not v.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor of the shape and type of the first, on the context's device")
+    return v.data_ptr() or 16                     # (a tensor without values has no address, but it is there)
 
 
 def tc_quantize_blocks(ctx: Context, x: torch.Tensor, *, rows: str = "pixels", square: bool = False, out=None):
@@ -718,23 +732,24 @@ def tc_matmul_blocks(ctx: Context, a: Blocks, b: Blocks, *, shape=None, dtype=to
     """Product of a's rows (the output's pixels) and b's rows (its channels), (N, O, H, W) with `shape` = (N, H, W), by default
     (rows of a, 1, 1); `bias` [O], `relu` on the result."""
     ma, mb = _blocks(ctx, a), _blocks(ctx, b)
-    if out is None:
+    rows = mb.rows
+    if out is None and dtype in (torch.bfloat16, torch.float32):
         n, h, w = (ma.rows, 1, 1) if shape is None else shape
-        out = torch.empty((n, mb.rows, h, w), dtype=dtype, device=a.codes.device)
-    t = _local(ctx, out)
-    _check(load_library().tc_matmul_blocks(ctx.ptr, C.addressof(ma), C.addressof(mb), _vector(ctx, bias, mb.rows, "bias"), relu, C.addressof(t),
+        out = _empty(ctx, dtype).new_empty(n, rows, h, w)
+        t = _Tensor(out.data_ptr(), n, rows, h, w, TC_BF16 if dtype is torch.bfloat16 else TC_F32)
+    elif out is None:
+        raise ValueError("dtype must be float32 or bfloat16")
+    else:
+        t = _local(ctx, out)
+    _check(load_library().tc_matmul_blocks(ctx.ptr, C.addressof(ma), C.addressof(mb), _vector(ctx.device, bias, rows, "bias"), relu, C.addressof(t),
                                            _tensor_stream(ctx.device)), "tc_matmul_blocks")
     return out
 
 
-def _norm_params(ctx: Context, h: _Tensor, y, after, gate, scale, before, eps):
-    """The C structure, and the tensors it points to."""
-    c = h.c
-    ty = None if y is None else _local(ctx, y)
-    tg = gate if gate is None or gate.dim() != 4 else _local(ctx, gate)
-    in_channels = tg is gate                      # no gate, or one for each channel
-    return _NormParams(None if ty is None else C.addressof(ty), _vector(ctx, after, c, "after"), _vector(ctx, gate, c, "gate") if in_channels else None,
-                       None if in_channels else C.addressof(tg), _vector(ctx, scale, 1, "scale"), _vector(ctx, before, c, "before"), eps), ty, tg
+def _norm_params(device: int, h: torch.Tensor, c: int, y, after, gate, scale, before, eps):
+    gate_map = gate is not None and gate.dim() == 4
+    return _NormParams(_like(y, h, device, "y"), _vector(device, after, c, "after"), None if gate_map else _vector(device, gate, c, "gate"),
+                       _like(gate, h, device, "gate") if gate_map else None, _vector(device, scale, 1, "scale"), _vector(device, before, c, "before"), eps)
 
 
 def tc_residual_norms(ctx: Context, h: torch.Tensor, y: torch.Tensor | None = None, *, after: torch.Tensor | None = None,
@@ -743,23 +758,26 @@ def tc_residual_norms(ctx: Context, h: torch.Tensor, y: torch.Tensor | None = No
     """(s, x): s = h + scale * gate * norm(y) * after, x = norm(s) * before, norms over the channels of each pixel.  x is a
     tensor like h, or with `blocks` its codes by pixels; without `before` it is None.  Without `y` s is h itself.  `gate` is
     [C], or a tensor like y."""
-    th = _local(ctx, h)
-    p, *keep = _norm_params(ctx, th, y, after, gate, scale, before, eps)
+    t = _local(ctx, h)
+    device, c = ctx.device, t.c
+    p = _norm_params(device, h, c, y, after, gate, scale, before, eps)
     s, at_s, x, at_x, at_b = h, None, None, None, None
     if y is not None:
-        s = torch.empty_like(h) if sum_out is None else sum_out
-        ts = _local(ctx, s)
-        at_s = C.addressof(ts)
+        if sum_out is None:
+            s = torch.empty_like(h)
+            at_s = s.data_ptr()
+        else:
+            s, at_s = sum_out, _like(sum_out, h, device, "sum_out")
     if before is not None:
         if blocks:
-            x, b = _new_blocks(ctx, th.n * th.h * th.w, th.c, False) if out is None else (out, _blocks(ctx, out))
+            x, b = _new_blocks(ctx, t.n * t.h * t.w, c, False) if out is None else (out, _blocks(ctx, out))
             at_b = C.addressof(b)
+        elif out is None:
+            x = torch.empty_like(h)
+            at_x = x.data_ptr()
         else:
-            x = torch.empty_like(h) if out is None else out
-            tx = _local(ctx, x)
-            at_x = C.addressof(tx)
-    _check(load_library().tc_residual_norms(ctx.ptr, C.addressof(th), C.addressof(p), at_s, at_x, at_b, _tensor_stream(ctx.device)), "tc_residual_norms")
-    del keep
+            x, at_x = out, _like(out, h, device, "out")
+    _check(load_library().tc_residual_norms(ctx.ptr, C.addressof(t), C.addressof(p), at_s, at_x, at_b, _tensor_stream(device)), "tc_residual_norms")
     return s, x
 
 
@@ -779,21 +797,14 @@ def tc_residual_norms_backward(ctx: Context, s: torch.Tensor, y: torch.Tensor | 
     """Gradients at the sum `s` that tc_residual_norms returned, from the gradients `dx` of x (None without `before`) and `ds` of s
     (None: zero)."""
     t = _local(ctx, s)
-    p, _, tg = keep = _norm_params(ctx, t, y, after, gate, scale, before, eps)
-    tx, td = None if dx is None else _local(ctx, dx), None if ds is None else _local(ctx, ds)
-    vectors = [v if v is None else torch.empty_like(v) for v in (after, gate, scale, before)]
-    dafter, dgate, dscale, dbefore = [None if v is None else v.data_ptr() for v in vectors]
-    dh, th = torch.empty_like(s), _Tensor(0, t.n, t.c, t.h, t.w, t.dtype)
-    th.data = dh.data_ptr()
-    dy = ty = tgate = None
-    if y is not None:
-        dy = torch.empty_like(y)
-        ty = _Tensor(dy.data_ptr(), *y.shape, t.dtype)
-    if p.gate_map:
-        tgate, dgate = _Tensor(dgate, tg.n, tg.c, tg.h, tg.w, tg.dtype), None
-    at = lambda v: None if v is None else C.addressof(v)                         # noqa: E731
-    out = _NormGrads(C.addressof(th), at(ty), at(tgate), dafter, dgate, dscale, dbefore)
-    _check(load_library().tc_residual_norms_backward(ctx.ptr, C.addressof(t), C.addressof(p), at(tx), at(td), C.addressof(out),
-                                                     _tensor_stream(ctx.device)), "tc_residual_norms_backward")
-    del keep
-    return NormGrads(dh, dy, *vectors)
+    device = ctx.device
+    p = _norm_params(device, s, t.c, y, after, gate, scale, before, eps)
+    at_dx, at_ds = _like(dx, s, device, "dx"), _like(ds, s, device, "ds")
+    dh = torch.empty_like(s)
+    dy, dafter, dgate, dscale, dbefore = [v if v is None else torch.empty_like(v) for v in (y, after, gate, scale, before)]
+    at = [v if v is None else v.data_ptr() for v in (dh, dy, dgate, dafter, dgate, dscale, dbefore)]
+    at[4 if p.gate_map else 2] = None
+    out = _NormGrads(*at)
+    _check(load_library().tc_residual_norms_backward(ctx.ptr, C.addressof(t), C.addressof(p), at_dx, at_ds, C.addressof(out), _tensor_stream(device)),
+           "tc_residual_norms_backward")
+    return NormGrads(dh, dy, dafter, dgate, dscale, dbefore)

@@ -8,6 +8,7 @@
 // memory, both layouts, tiles -- one that turns a tile of 128 x 128 values in shared memory, so that the tensor
 // is read once for both.
 #include "block_codes.cuh"
+#include "sm100_ptx.cuh"
 #include "tc_internal.h"
 
 namespace {
@@ -64,9 +65,13 @@ struct TileArgs {
     BlockMatrix along, across;      // rows = outer (blocks along memory), rows = inner; codes null where not wanted
 };
 
+// The tile comes by asynchronous copies and its values are read from shared memory where they are needed, twice for the layout across:
+// with them in registers (96 a thread) two blocks fitted an SM, and a tile's memory time was hardly hidden (8192x4096, both layouts 38 us
+// and Q_BOTH; maps of 256x14x14 x 1024 56 and Q_MAPS).
 template <typename T, bool kMaps, bool kSquare>
-__global__ void __launch_bounds__(256) quantize_tile_kernel(const T *x, TileArgs a, int vec)
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 5 : 3) quantize_tile_kernel(const T *x, const __grid_constant__ TileArgs a, int vec)
 {
+    using namespace sm100;
     extern __shared__ __align__(16) unsigned char smem[];
     T(*tile)[kBlock] = reinterpret_cast<T(*)[kBlock]>(smem);                       // [outer][inner]
     __shared__ uint32_t s_max[4][kBlock];
@@ -75,65 +80,55 @@ __global__ void __launch_bounds__(256) quantize_tile_kernel(const T *x, TileArgs
     chain_wait();
     const long long outer_n = kMaps ? a.c : a.pixels, inner_n = kMaps ? a.pixels : a.c;
     const long long o0 = (long long)(kMaps ? blockIdx.y : blockIdx.x) * kBlock, i0 = (long long)(kMaps ? blockIdx.x : blockIdx.y) * kBlock;
-    const int t = threadIdx.x, chunk = t & 15, row0 = t >> 4;
-    // A thread's eight inner values are the same ones in each of its eight rows: where they lie is found once.
-    long long off[8];
-    int valid = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const long long i = i0 + chunk * 8 + j;
-        if (i < inner_n) valid = j + 1;
-        off[j] = i;
-        if (kMaps) {
-            if (j == 0 || vec < 8) {
-                const long long img = i / a.hw;
-                off[j] = img * a.c * (long long)a.hw + (i - img * a.hw);
-            } else
-                off[j] = off[0] + j;
-        }
-    }
+    const int t = threadIdx.x;
+    const int rows = (int)min((long long)kBlock, outer_n - o0), cols = (int)min((long long)kBlock, inner_n - i0);
     const long long pitch = kMaps ? a.hw : a.c;
-    Raw8<T> raw[8];
+    // Where inner value i lies in row 0 of the tile.
+    auto inner_at = [&](long long i) {
+        if (!kMaps) return o0 * pitch + i;
+        const long long img = i / a.hw;
+        return img * a.c * (long long)a.hw + (i - img * a.hw) + o0 * pitch;
+    };
+    // Values are moved `vec` at a time (inner_n and the maps' sides are multiples of it), zeros behind the tensor's end.
+    if (vec >= 4) {
+        constexpr int kCopy = 16 / (int)sizeof(T);                                 // eight values of fp32 go as two copies
+        auto copy = [&](uint32_t dst, const T *src, bool ok) {
+            if (vec * (int)sizeof(T) >= 16) cp_async_16(dst, src, ok ? 16u : 0u);
+            else cp_async_8(dst, src, ok ? 8u : 0u);
+        };
+        const int step = vec < kCopy ? vec : kCopy, per_row = kBlock / step, k = t % per_row * step;
+        const T *src = x + (k < cols ? inner_at(i0 + k) : 0);
+        for (int r = t / per_row; r < kBlock; r += 256 / per_row) {
+            const bool ok = r < rows && k < cols;
+            copy(smem_u32(&tile[r][k]), ok ? src + r * pitch : x, ok);
+        }
+    } else {
+        const int k = t & (kBlock - 1);
+        const T *src = x + (k < cols ? inner_at(i0 + k) : 0);
+        for (int r0 = t >> 7; r0 < kBlock; r0 += 32) {
+            T v[16];
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-        const long long o = o0 + row0 + 16 * r;
-        zero8(raw[r]);
-        if (o >= outer_n || valid == 0) continue;
-        const T *src = x + o * pitch;
-        if (vec == 8) load8(raw[r], src + off[0]);                                 // inner_n and the maps' sides are multiples of eight
-        else if (vec == 4) {
-            if constexpr (sizeof(T) == 2) {
-                const uint2 p = *reinterpret_cast<const uint2 *>(src + off[0]);
-                const uint2 q = valid > 4 ? *reinterpret_cast<const uint2 *>(src + off[4]) : make_uint2(0, 0);
-                raw[r].v = make_uint4(p.x, p.y, q.x, q.y);
-            } else {
-                raw[r].v = *reinterpret_cast<const uint4 *>(src + off[0]);
-                if (valid > 4) raw[r].w = *reinterpret_cast<const uint4 *>(src + off[4]);
+            for (int j = 0; j < 16; ++j) {
+                v[j] = T(0.f);
+                if (r0 + 2 * j < rows && k < cols) v[j] = src[(r0 + 2 * j) * pitch];
             }
-        } else {
-            T *dst = reinterpret_cast<T *>(&raw[r]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < valid) dst[j] = src[off[j]];
+            for (int j = 0; j < 16; ++j) tile[r0 + 2 * j][k] = v[j];
         }
     }
-    uint32_t m[8];
-#pragma unroll
-    for (int r = 0; r < 8; ++r) {
-        *reinterpret_cast<Raw8<T> *>(&tile[row0 + 16 * r][chunk * 8]) = raw[r];
-        float v[8];
-        values8(raw[r], v);
-        m[r] = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m[r] = max(m[r], abs_bits(v[j]));
-        m[r] = max16(m[r]);
-    }
+    cp_async_wait_all();
+    __syncthreads();
     float scale = 0.f;
     if constexpr (kSquare) {
         uint32_t all = 0;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) all = max(all, m[r]);
-        all = max(all, __shfl_xor_sync(0xffffffffu, all, 16));
+        for (int r = 0; r < 8; ++r) {
+            float v[8];
+            values8(*reinterpret_cast<const Raw8<T> *>(&tile[(t >> 4) + 16 * r][(t & 15) * 8]), v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) all = max(all, abs_bits(v[j]));
+        }
+        all = __reduce_max_sync(0xffffffffu, all);
         if ((t & 31) == 0) s_warp[t >> 5] = all;
         __syncthreads();
 #pragma unroll
@@ -144,39 +139,50 @@ __global__ void __launch_bounds__(256) quantize_tile_kernel(const T *x, TileArgs
             if (a.across.codes) a.across.scales[o0 / kBlock * a.across.scale_ld + i0 / kBlock] = scale;
         }
     }
-    if (a.along.codes && valid > 0) {
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            const long long o = o0 + row0 + 16 * r;
-            if (o >= outer_n) continue;
-            const float s = kSquare ? scale : scale_of(m[r]);
+    if (a.along.codes) {
+        const int k = (t & 15) * 8;
+        uint8_t *to = a.along.codes + (o0 + (t >> 4)) * a.along.ld + i0 + k;
+#pragma unroll 4
+        for (int r = t >> 4; r < kBlock; r += 16, to += 16 * a.along.ld) {
             float v[8];
-            values8(raw[r], v);
-            *reinterpret_cast<uint2 *>(a.along.codes + o * a.along.ld + i0 + chunk * 8) = codes8(v, __frcp_rn(s));
-            if (!kSquare && chunk == 0) a.along.scales[i0 / kBlock * a.along.scale_ld + o] = s;
+            values8(*reinterpret_cast<const Raw8<T> *>(&tile[r][k]), v);
+            float s = scale;
+            if constexpr (!kSquare) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[j]));
+                s = scale_of(max16(m));
+            }
+            if (r < rows && k < cols) {
+                *reinterpret_cast<uint2 *>(to) = codes8(v, __frcp_rn(s));
+                if (!kSquare && k == 0) a.along.scales[i0 / kBlock * a.along.scale_ld + o0 + r] = s;
+            }
         }
     }
     if (!a.across.codes) return;
-    if (!kSquare) __syncthreads();                                                 // the tile (a square's maximum has waited for it)
     // two inner columns and 32 outer values a thread
     const int pair = t & 63, part = t >> 6;
-    float v0[32], v1[32];
-    uint32_t m0 = 0, m1 = 0;
-#pragma unroll
-    for (int r = 0; r < 32; ++r) {
+    auto two = [&](int r, float &v0, float &v1) {
         if constexpr (sizeof(T) == 2) {
             const uint32_t w = *reinterpret_cast<const uint32_t *>(&tile[part * 32 + r][pair * 2]);
-            v0[r] = __uint_as_float(w << 16);
-            v1[r] = __uint_as_float(w & 0xffff0000u);
+            v0 = __uint_as_float(w << 16);
+            v1 = __uint_as_float(w & 0xffff0000u);
         } else {
             const float2 w = *reinterpret_cast<const float2 *>(&tile[part * 32 + r][pair * 2]);
-            v0[r] = w.x;
-            v1[r] = w.y;
+            v0 = w.x;
+            v1 = w.y;
         }
-        if (!kSquare) { m0 = max(m0, abs_bits(v0[r])); m1 = max(m1, abs_bits(v1[r])); }
-    }
+    };
     float scale0 = scale, scale1 = scale;
     if constexpr (!kSquare) {
+        uint32_t m0 = 0, m1 = 0;
+#pragma unroll 8
+        for (int r = 0; r < 32; ++r) {
+            float v0, v1;
+            two(r, v0, v1);
+            m0 = max(m0, abs_bits(v0));
+            m1 = max(m1, abs_bits(v1));
+        }
         s_max[part][2 * pair] = m0;
         s_max[part][2 * pair + 1] = m1;
         __syncthreads();
@@ -185,22 +191,28 @@ __global__ void __launch_bounds__(256) quantize_tile_kernel(const T *x, TileArgs
         scale0 = scale_of(m0);
         scale1 = scale_of(m1);
     }
-    const long long o_first = o0 + part * 32;
-    if (o_first >= outer_n) return;
-    auto put = [&](long long i, const float (&v)[32], float s) {
-        if (i >= inner_n) return;
-        const float inv = __frcp_rn(s);
-        uint8_t *dst = a.across.codes + i * a.across.ld + o_first;
+    const float inv0 = __frcp_rn(scale0), inv1 = __frcp_rn(scale1);
+    const int c = 2 * pair;
+    uint8_t *const to = a.across.codes + (i0 + c) * a.across.ld + o0 + part * 32;
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
-            if (o_first + 16 * q < outer_n)                                        // rows of codes end at a multiple of 16
-                *reinterpret_cast<uint4 *>(dst + 16 * q) =
-                    make_uint4(codes4(v[16 * q], v[16 * q + 1], v[16 * q + 2], v[16 * q + 3], inv), codes4(v[16 * q + 4], v[16 * q + 5], v[16 * q + 6], v[16 * q + 7], inv),
-                               codes4(v[16 * q + 8], v[16 * q + 9], v[16 * q + 10], v[16 * q + 11], inv), codes4(v[16 * q + 12], v[16 * q + 13], v[16 * q + 14], v[16 * q + 15], inv));
-        if (!kSquare && part == 0) a.across.scales[o0 / kBlock * a.across.scale_ld + i] = s;
-    };
-    put(i0 + 2 * pair, v0, scale0);
-    put(i0 + 2 * pair + 1, v1, scale1);
+    for (int q = 0; q < 2; ++q) {
+        uint32_t w0[4], w1[4];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            float v0[4], v1[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) two(16 * q + 4 * h + j, v0[j], v1[j]);
+            w0[h] = codes4(v0[0], v0[1], v0[2], v0[3], inv0);
+            w1[h] = codes4(v1[0], v1[1], v1[2], v1[3], inv1);
+        }
+        if (part * 32 + 16 * q >= rows) break;                                     // rows of codes end at a multiple of 16
+        if (c < cols) *reinterpret_cast<uint4 *>(to + 16 * q) = make_uint4(w0[0], w0[1], w0[2], w0[3]);
+        if (c + 1 < cols) *reinterpret_cast<uint4 *>(to + a.across.ld + 16 * q) = make_uint4(w1[0], w1[1], w1[2], w1[3]);
+    }
+    if (!kSquare && part == 0) {
+        if (c < cols) a.across.scales[o0 / kBlock * a.across.scale_ld + i0 + c] = scale0;
+        if (c + 1 < cols) a.across.scales[o0 / kBlock * a.across.scale_ld + i0 + c + 1] = scale1;
+    }
 }
 
 template <typename T>
@@ -215,7 +227,7 @@ tc_status launch_rows(const T *x, long long rows, int cols, const BlockMatrix &o
 }
 
 template <typename T>
-tc_status launch_tiles(const T *x, int n, int c, int hw, bool square, const BlockMatrix &pixels, const BlockMatrix &channels, cudaStream_t s)
+tc_status launch_tiles(int device, const T *x, int n, int c, int hw, bool square, const BlockMatrix &pixels, const BlockMatrix &channels, cudaStream_t s)
 {
     TileArgs a;
     a.pixels = (long long)n * hw;
@@ -228,27 +240,28 @@ tc_status launch_tiles(const T *x, int n, int c, int hw, bool square, const Bloc
     const int vec = inner % 8 == 0 && at % 16 == 0 ? 8 : inner % 4 == 0 && at % (4 * sizeof(T)) == 0 ? 4 : 1;
     const dim3 grid((unsigned int)((a.pixels + kBlock - 1) / kBlock), (unsigned int)((c + kBlock - 1) / kBlock));
     constexpr size_t smem = kBlock * kBlock * sizeof(T);
-    auto launch = [&](auto kernel) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) { cudaGetLastError(); return TC_ERR_CUDA; }
-        return launch_first(true, kernel, grid, dim3(256), smem, s, x, a, vec) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
+    auto launch = [&](bool allowed, auto kernel) {
+        return allowed && launch_first(true, kernel, grid, dim3(256), smem, s, x, a, vec) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
     };
-    if (hw > 1) return square ? launch(quantize_tile_kernel<T, true, true>) : launch(quantize_tile_kernel<T, true, false>);
-    return square ? launch(quantize_tile_kernel<T, false, true>) : launch(quantize_tile_kernel<T, false, false>);
+#define TC_TILES(maps, squares) launch(allow_shared<quantize_tile_kernel<T, maps, squares>>(device, smem), quantize_tile_kernel<T, maps, squares>)
+    if (hw > 1) return square ? TC_TILES(true, true) : TC_TILES(true, false);
+    return square ? TC_TILES(false, true) : TC_TILES(false, false);
+#undef TC_TILES
 }
 
 template <typename T>
-tc_status quantize(const T *x, int n, int c, int hw, bool square, const BlockMatrix &pixels, const BlockMatrix &channels, cudaStream_t s)
+tc_status quantize(int device, const T *x, int n, int c, int hw, bool square, const BlockMatrix &pixels, const BlockMatrix &channels, cudaStream_t s)
 {
     if (!square && !channels.codes && hw == 1) return launch_rows(x, n, c, pixels, s);
     if (!square && !pixels.codes && n == 1) return launch_rows(x, c, hw, channels, s);
-    return launch_tiles(x, n, c, hw, square, pixels, channels, s);
+    return launch_tiles(device, x, n, c, hw, square, pixels, channels, s);
 }
 
 }  // namespace
 
-tc_status tc_launch_quantize_blocks(const void *x, int dtype, int n, int c, int hw, bool square, const BlockMatrix &pixels, const BlockMatrix &channels,
+tc_status tc_launch_quantize_blocks(int device, const void *x, int dtype, int n, int c, int hw, bool square, const BlockMatrix &pixels, const BlockMatrix &channels,
                                     cudaStream_t s)
 {
-    return dtype == TC_BF16 ? quantize((const __nv_bfloat16 *)x, n, c, hw, square, pixels, channels, s)
-                            : quantize((const float *)x, n, c, hw, square, pixels, channels, s);
+    return dtype == TC_BF16 ? quantize(device, (const __nv_bfloat16 *)x, n, c, hw, square, pixels, channels, s)
+                            : quantize(device, (const float *)x, n, c, hw, square, pixels, channels, s);
 }

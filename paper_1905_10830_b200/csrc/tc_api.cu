@@ -1817,7 +1817,6 @@ constexpr int kMostNormChannels = 16384;                // a row's channels in t
 size_t element_size(int dtype) { return dtype == TC_BF16 ? 2 : 4; }
 bool aligned_tensor(const tc_tensor *t) { return valid_tensor(t) && ((uintptr_t)t->data & (element_size(t->dtype) - 1)) == 0; }
 long long pixels_of(const tc_tensor *t) { return (long long)t->n * t->h * t->w; }
-bool same_shape(const tc_tensor *a, const tc_tensor *b) { return a->n == b->n && a->c == b->c && a->h == b->h && a->w == b->w && a->dtype == b->dtype; }
 
 bool valid_blocks(const tc_blocks *b)
 {
@@ -1857,24 +1856,22 @@ struct Ranges {
     }
 };
 
-// The parameters both directions share, against the tensor they belong to.
+// The parameters both directions share; `aligned`: of the tensors that are given, all others too.
+template <typename... P>
+bool aligned_to(size_t bytes, P... p) { return ((((uintptr_t)p) | ...) & (bytes - 1)) == 0; }
 bool valid_norm_params(const tc_tensor *h, const tc_norm_params *p)
 {
     if (!aligned_tensor(h) || !p || !(p->eps >= 0.f) || (!p->y && !p->before)) return false;
-    if (p->y ? !aligned_tensor(p->y) || !same_shape(h, p->y) : p->after || p->gate || p->gate_map || p->scale) return false;
-    return !p->gate_map || (!p->gate && aligned_tensor(p->gate_map) && same_shape(h, p->gate_map));
+    if (!p->y && (p->after || p->gate || p->gate_map || p->scale)) return false;
+    return !(p->gate && p->gate_map) && aligned_to(element_size(h->dtype), p->y, p->gate_map) && aligned_to(4, p->after, p->gate, p->scale, p->before);
 }
+size_t tensor_bytes(const tc_tensor *t) { return (size_t)pixels_of(t) * t->c * element_size(t->dtype); }
 void add_norm_params(Ranges &r, const tc_tensor *h, const tc_norm_params *p)
 {
-    r.add(h, false);
-    r.add(p->y, false);
-    r.add(p->gate_map, false);
+    for (const void *t : {(const void *)h->data, p->y, p->gate_map}) r.add(t, tensor_bytes(h), false);
     for (const float *v : {p->after, p->gate, p->before}) r.add(v, (size_t)h->c * sizeof(float), false);
     r.add(p->scale, sizeof(float), false);
 }
-template <typename... P>
-bool aligned16(P... p) { return ((((uintptr_t)p) | ...) & 15u) == 0; }
-const void *data_of(const tc_tensor *t) { return t ? t->data : nullptr; }
 
 }  // namespace
 
@@ -1896,7 +1893,7 @@ tc_status tc_quantize_blocks(tc_ctx *ctx, const tc_tensor *x, const tc_blocks *p
     if (p == 0) return TC_OK;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return TC_ERR_CUDA;
-    return tc_launch_quantize_blocks(x->data, x->dtype, x->n, x->c, x->h * x->w, (pixels ? pixels : channels)->square != 0, block_matrix(pixels),
+    return tc_launch_quantize_blocks(ctx->device, x->data, x->dtype, x->n, x->c, x->h * x->w, (pixels ? pixels : channels)->square != 0, block_matrix(pixels),
                                      block_matrix(channels), (cudaStream_t)cuda_stream);
 }
 
@@ -1933,20 +1930,19 @@ tc_status tc_matmul_blocks(tc_ctx *ctx, const tc_blocks *a, const tc_blocks *b, 
     return tc_launch_matmul_blocks(ctx, args, plan, scratch.at, (cudaStream_t)cuda_stream);
 }
 
-tc_status tc_residual_norms(tc_ctx *ctx, const tc_tensor *h, const tc_norm_params *params, const tc_tensor *sum, const tc_tensor *x, const tc_blocks *codes,
-                            void *cuda_stream)
+tc_status tc_residual_norms(tc_ctx *ctx, const tc_tensor *h, const tc_norm_params *params, void *sum, void *x, const tc_blocks *codes, void *cuda_stream)
 {
     if (!ctx || !valid_norm_params(h, params)) return TC_ERR_INVALID_ARG;
-    if (params->y ? !aligned_tensor(sum) || !same_shape(h, sum) : sum != nullptr) return TC_ERR_INVALID_ARG;
-    if ((params->before != nullptr) != (x || codes)) return TC_ERR_INVALID_ARG;
-    if (x && (!aligned_tensor(x) || !same_shape(h, x))) return TC_ERR_INVALID_ARG;
     const long long p = pixels_of(h);
+    if ((params->y != nullptr) != (sum != nullptr) && p > 0) return TC_ERR_INVALID_ARG;
+    if ((params->before != nullptr) != (x || codes) && p > 0) return TC_ERR_INVALID_ARG;
+    if (!aligned_to(element_size(h->dtype), sum, x)) return TC_ERR_INVALID_ARG;
     if (p > kMostRows || h->c > kMostNormChannels) return TC_ERR_UNSUPPORTED;
     if (codes && (!valid_blocks(codes) || codes->rows != p || codes->cols != h->c || codes->square)) return TC_ERR_INVALID_ARG;
     Ranges ranges;
     add_norm_params(ranges, h, params);
-    ranges.add(sum, true);
-    ranges.add(x, true);
+    ranges.add(sum, tensor_bytes(h), true);
+    ranges.add(x, tensor_bytes(h), true);
     ranges.add(codes, true);
     if (!ranges.apart()) return TC_ERR_INVALID_ARG;
     if (p == 0) return TC_OK;
@@ -1954,43 +1950,42 @@ tc_status tc_residual_norms(tc_ctx *ctx, const tc_tensor *h, const tc_norm_param
     if (!guard.ok) return TC_ERR_CUDA;
     NormArgs a{};
     a.h = h->data;
-    a.y = data_of(params->y);
-    a.gate_map = data_of(params->gate_map);
+    a.y = params->y;
+    a.gate_map = params->gate_map;
     a.after = params->after;
     a.gate = params->gate;
     a.scale = params->scale;
     a.before = params->before;
     a.eps = params->eps;
-    a.sum = (void *)data_of(sum);
-    a.x = (void *)data_of(x);
+    a.sum = sum;
+    a.x = x;
     a.codes = block_matrix(codes);
     a.pixels = p;
     a.c = h->c;
     a.hw = h->h * h->w;
-    a.vec = h->c % 8 == 0 && aligned16(a.h, a.y, a.gate_map, a.after, a.gate, a.before, a.sum, a.x);
+    a.vec = h->c % 8 == 0 && aligned_to(16, a.h, a.y, a.gate_map, a.after, a.gate, a.before, a.sum, a.x);
     a.sms = ctx->sm_count;
     a.device = ctx->device;
     a.status = ctx->d_status;
     return tc_launch_residual_norms(a, h->dtype, (cudaStream_t)cuda_stream);
 }
 
-tc_status tc_residual_norms_backward(tc_ctx *ctx, const tc_tensor *s, const tc_norm_params *params, const tc_tensor *dx, const tc_tensor *ds,
+tc_status tc_residual_norms_backward(tc_ctx *ctx, const tc_tensor *s, const tc_norm_params *params, const void *dx, const void *ds,
                                      const tc_norm_grads *out, void *cuda_stream)
 {
     if (!ctx || !valid_norm_params(s, params) || !out) return TC_ERR_INVALID_ARG;
-    if ((params->before != nullptr) != (dx != nullptr) || (dx && (!aligned_tensor(dx) || !same_shape(s, dx)))) return TC_ERR_INVALID_ARG;
-    if (ds && (!aligned_tensor(ds) || !same_shape(s, ds))) return TC_ERR_INVALID_ARG;
-    if (!aligned_tensor(out->dh) || !same_shape(s, out->dh)) return TC_ERR_INVALID_ARG;
-    if (params->y ? !aligned_tensor(out->dy) || !same_shape(s, out->dy) : out->dy || out->dscale) return TC_ERR_INVALID_ARG;
-    if (params->gate_map ? !aligned_tensor(out->dgate_map) || !same_shape(s, out->dgate_map) : out->dgate_map != nullptr) return TC_ERR_INVALID_ARG;
-    if ((out->dafter && !params->after) || (out->dgate && !params->gate) || (out->dbefore && !params->before)) return TC_ERR_INVALID_ARG;
     const long long p = pixels_of(s);
+    if (p > 0 && ((params->before != nullptr) != (dx != nullptr) || !out->dh)) return TC_ERR_INVALID_ARG;
+    if (params->y ? p > 0 && !out->dy : out->dy || out->dscale) return TC_ERR_INVALID_ARG;
+    if (params->gate_map ? p > 0 && !out->dgate_map : out->dgate_map != nullptr) return TC_ERR_INVALID_ARG;
+    if (!aligned_to(element_size(s->dtype), dx, ds, out->dh, out->dy, out->dgate_map) || !aligned_to(4, out->dafter, out->dgate, out->dscale, out->dbefore))
+        return TC_ERR_INVALID_ARG;
+    if ((out->dafter && !params->after) || (out->dgate && !params->gate) || (out->dbefore && !params->before)) return TC_ERR_INVALID_ARG;
     if (p > kMostRows || s->c > kMostNormChannels) return TC_ERR_UNSUPPORTED;
     Ranges ranges;
     add_norm_params(ranges, s, params);
-    ranges.add(dx, false);
-    ranges.add(ds, false);
-    for (const tc_tensor *t : {out->dh, out->dy, out->dgate_map}) ranges.add(t, true);
+    for (const void *t : {dx, ds}) ranges.add(t, tensor_bytes(s), false);
+    for (void *t : {out->dh, out->dy, out->dgate_map}) ranges.add(t, tensor_bytes(s), true);
     for (const float *v : {out->dafter, out->dgate, out->dbefore}) ranges.add(v, (size_t)s->c * sizeof(float), true);
     ranges.add(out->dscale, sizeof(float), true);
     if (!ranges.apart()) return TC_ERR_INVALID_ARG;
@@ -1998,18 +1993,18 @@ tc_status tc_residual_norms_backward(tc_ctx *ctx, const tc_tensor *s, const tc_n
     if (!guard.ok) return TC_ERR_CUDA;
     NormGradArgs a{};
     a.s = s->data;
-    a.y = data_of(params->y);
-    a.dx = data_of(dx);
-    a.ds = data_of(ds);
-    a.gate_map = data_of(params->gate_map);
+    a.y = params->y;
+    a.dx = dx;
+    a.ds = ds;
+    a.gate_map = params->gate_map;
     a.after = params->after;
     a.gate = params->gate;
     a.scale = params->scale;
     a.before = params->before;
     a.eps = params->eps;
-    a.dh = out->dh->data;
-    a.dy = (void *)data_of(out->dy);
-    a.dgate_map = (void *)data_of(out->dgate_map);
+    a.dh = out->dh;
+    a.dy = out->dy;
+    a.dgate_map = out->dgate_map;
     a.dafter = out->dafter;
     a.dgate = out->dgate;
     a.dscale = out->dscale;
@@ -2017,7 +2012,7 @@ tc_status tc_residual_norms_backward(tc_ctx *ctx, const tc_tensor *s, const tc_n
     a.pixels = p;
     a.c = s->c;
     a.hw = p ? s->h * s->w : 1;
-    a.vec = s->c % 8 == 0 && aligned16(a.s, a.y, a.dx, a.ds, a.gate_map, a.after, a.gate, a.before, a.dh, a.dy, a.dgate_map);
+    a.vec = s->c % 8 == 0 && aligned_to(16, a.s, a.y, a.dx, a.ds, a.gate_map, a.after, a.gate, a.before, a.dh, a.dy, a.dgate_map);
     const int blocks = tc_norm_grad_blocks(p, a.c, a.hw, s->dtype, ctx->sm_count);
     CallScratch scratch;
     const size_t bytes = ((size_t)blocks * (2 * (size_t)a.c + 1) + 1) * sizeof(float);

@@ -324,7 +324,7 @@ struct BlockMatrix {
     float *scales = nullptr;
     long long ld = 0, scale_ld = 0;
 };
-tc_status tc_launch_quantize_blocks(const void *x, int dtype, int n, int c, int hw, bool square, const BlockMatrix &pixels, const BlockMatrix &channels,
+tc_status tc_launch_quantize_blocks(int device, const void *x, int dtype, int n, int c, int hw, bool square, const BlockMatrix &pixels, const BlockMatrix &channels,
                                     cudaStream_t s);
 struct MatmulOperand {
     BlockMatrix m;

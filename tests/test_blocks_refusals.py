@@ -70,55 +70,50 @@ def test_matmul(lib, ctx):
 
 def params(**k):
     v = {"y": None, "after": None, "gate": None, "gate_map": None, "scale": None, "before": None, "eps": 1e-6, **k}
-    p = B._NormParams(at(v["y"]), v["after"], v["gate"], at(v["gate_map"]), v["scale"], v["before"], v["eps"])
-    p.keep = v
-    return p
+    return B._NormParams(v["y"], v["after"], v["gate"], v["gate_map"], v["scale"], v["before"], v["eps"])
 
 
 def test_norms(lib, ctx):
-    call = lambda h, p, s, x, b=None, cx=ctx: lib.tc_residual_norms(cx, at(h), at(p), at(s), at(x), at(b), None)   # noqa: E731
-    t = lambda i, **k: tensor(**{"n": 8, "c": 64, "at": i * AT, **k})                     # noqa: E731
-    whole = dict(y=t(2), after=3 * AT, gate=4 * AT, scale=5 * AT, before=6 * AT)
-    assert call(t(1), params(**whole), t(7), t(8), None, None) == INVALID
-    assert call(t(1), None, t(7), t(8)) == INVALID
-    assert call(None, params(**whole), t(7), t(8)) == INVALID
-    for change in (dict(eps=-1.0), dict(eps=float("nan")), dict(y=t(2, n=7)), dict(y=t(2, dtype=B.TC_BF16)), dict(gate_map=t(9)), dict(y=None),
-                   dict(before=None), dict(gate=None, gate_map=t(9, c=32))):
-        assert call(t(1), params(**{**whole, **change}), t(7), t(8)) == INVALID
+    call = lambda h, p, s, x, b=None, cx=ctx: lib.tc_residual_norms(cx, at(h), at(p), s, x, at(b), None)                # noqa: E731
+    h = tensor(8, 64)
+    whole = dict(y=2 * AT, after=3 * AT, gate=4 * AT, scale=5 * AT, before=6 * AT)
+    s, x = 7 * AT, 8 * AT
+    assert call(h, params(**whole), s, x, None, None) == INVALID
+    assert call(h, None, s, x) == INVALID
+    assert call(None, params(**whole), s, x) == INVALID
+    for change in (dict(eps=-1.0), dict(eps=float("nan")), dict(gate_map=9 * AT), dict(y=None), dict(before=None), dict(y=2 * AT + 2), dict(after=3 * AT + 1)):
+        assert call(h, params(**{**whole, **change}), s, x) == INVALID
     p = params(**whole)
-    for s, x in ((None, t(8)), (t(7), None), (t(1), t(8)), (t(2), t(8)), (t(7), t(7)), (t(7), t(3)), (t(7, n=9), t(8)), (t(7), t(8, c=65))):
-        assert call(t(1), p, s, x) == INVALID
-    for b in (blocks(8, 64, True, 9 * AT), blocks(8, 65, False, 9 * AT), blocks(8, 64, False, 7 * AT)):
-        assert call(t(1), p, t(7), None, b) == INVALID
-    assert call(t(1), params(before=6 * AT), t(7), t(8)) == INVALID                       # a sum of nothing
-    wide = dict(c=16385)
-    assert call(t(1, **wide), params(before=6 * AT), None, t(8, **wide)) == UNSUPPORTED
-    assert call(t(1, n=0), params(before=6 * AT), None, t(8, n=0)) == OK
+    for to, norm in ((None, x), (s, None), (AT, x), (2 * AT, x), (s, s), (s, 3 * AT), (AT + 8 * 64 * 4 - 4, x), (s + 2, x), (s, x + 1)):
+        assert call(h, p, to, norm) == INVALID
+    for b in (blocks(8, 64, True, 9 * AT), blocks(8, 65, False, 9 * AT), blocks(8, 64, False, 7 * AT), blocks(9, 64, False, 9 * AT)):
+        assert call(h, p, s, None, b) == INVALID
+    assert call(h, params(before=6 * AT), s, x) == INVALID                                # a sum of nothing
+    assert call(tensor(8, 16385), params(before=6 * AT), None, x) == UNSUPPORTED
+    assert call(tensor(0, 64), params(before=6 * AT), None, x) == OK
+    assert call(tensor(8, 64, dtype=B.TC_INT8), p, s, x) == INVALID
 
 
 def test_norms_backward(lib, ctx):
-    t = lambda i, **k: tensor(**{"n": 8, "c": 64, "at": i * AT, **k})                     # noqa: E731
-
     def grads(dh=None, dy=None, dgate_map=None, dafter=None, dgate=None, dscale=None, dbefore=None):
-        g = B._NormGrads(at(dh), at(dy), at(dgate_map), dafter, dgate, dscale, dbefore)
-        g.keep = dh, dy, dgate_map
-        return g
+        return B._NormGrads(dh, dy, dgate_map, dafter, dgate, dscale, dbefore)
 
-    call = lambda s, p, dx, ds, g, cx=ctx: lib.tc_residual_norms_backward(cx, at(s), at(p), at(dx), at(ds), at(g), None)   # noqa: E731
-    whole = dict(y=t(2), after=3 * AT, gate=4 * AT, scale=5 * AT, before=6 * AT)
-    out = dict(dh=t(10), dy=t(11), dafter=12 * AT, dgate=13 * AT, dscale=14 * AT, dbefore=15 * AT)
+    call = lambda s, p, dx, ds, g, cx=ctx: lib.tc_residual_norms_backward(cx, at(s), at(p), dx, ds, at(g), None)        # noqa: E731
+    s, dx, ds = tensor(8, 64), 7 * AT, 8 * AT
+    whole = dict(y=2 * AT, after=3 * AT, gate=4 * AT, scale=5 * AT, before=6 * AT)
+    out = dict(dh=10 * AT, dy=11 * AT, dafter=12 * AT, dgate=13 * AT, dscale=14 * AT, dbefore=15 * AT)
     p = params(**whole)
-    assert call(t(1), p, t(7), t(8), grads(**out), None) == INVALID
-    assert call(t(1), p, t(7), t(8), None) == INVALID
-    assert call(t(1), p, None, t(8), grads(**out)) == INVALID                             # before, and no gradient of x
-    assert call(t(1), params(**{**whole, "before": None}), t(7), t(8), grads(**out)) == INVALID
-    for change in (dict(dh=None), dict(dy=None), dict(dh=t(1)), dict(dh=t(7)), dict(dy=t(10)), dict(dh=t(10, n=7)), dict(dgate_map=t(16)), dict(dafter=10 * AT)):
-        assert call(t(1), p, t(7), t(8), grads(**{**out, **change})) == INVALID
-    for without, extra in ((dict(after=None), "dafter"), (dict(gate=None), "dgate")):
-        assert call(t(1), params(**{**whole, **without}), t(7), t(8), grads(**out)) == INVALID, extra
-    assert call(t(1), params(**{**whole, "gate": None, "gate_map": t(9)}), t(7), t(8), grads(**{**out, "dgate": None})) == INVALID   # its gradient is required
+    assert call(s, p, dx, ds, grads(**out), None) == INVALID
+    assert call(s, p, dx, ds, None) == INVALID
+    assert call(s, p, None, ds, grads(**out)) == INVALID                                  # before, and no gradient of x
+    assert call(s, params(**{**whole, "before": None}), dx, ds, grads(**out)) == INVALID
+    for change in (dict(dh=None), dict(dy=None), dict(dh=AT), dict(dh=dx), dict(dy=10 * AT), dict(dgate_map=16 * AT), dict(dafter=10 * AT), dict(dh=10 * AT + 2),
+                   dict(dscale=14 * AT + 1)):
+        assert call(s, p, dx, ds, grads(**{**out, **change})) == INVALID
+    for without in (dict(after=None), dict(gate=None)):
+        assert call(s, params(**{**whole, **without}), dx, ds, grads(**out)) == INVALID
+    assert call(s, params(**{**whole, "gate": None, "gate_map": 9 * AT}), dx, ds, grads(**{**out, "dgate": None})) == INVALID   # its gradient is required
     alone = params(before=6 * AT)
-    for bad in (dict(dh=t(10), dy=t(11)), dict(dh=t(10), dscale=14 * AT)):
-        assert call(t(1), alone, t(7), None, grads(**bad)) == INVALID
-    wide = dict(c=16385)
-    assert call(t(1, **wide), alone, t(7, **wide), None, grads(dh=t(10, **wide))) == UNSUPPORTED
+    for bad in (dict(dh=10 * AT, dy=11 * AT), dict(dh=10 * AT, dscale=14 * AT)):
+        assert call(s, alone, dx, None, grads(**bad)) == INVALID
+    assert call(tensor(8, 16385), alone, dx, None, grads(dh=10 * AT)) == UNSUPPORTED

@@ -293,10 +293,12 @@ def test_refusals(ctx):
         tc.tc_residual_norms(ctx, d["h"])                                          # nothing to do
     with pytest.raises(tc.TcError):
         tc.tc_residual_norms(ctx, d["h"], before=d["before"], gate=d["gate"])      # a gate of nothing
-    with pytest.raises(tc.TcError):
+    with pytest.raises(ValueError):
         tc.tc_residual_norms(ctx, d["h"], d["y"][:3], after=d["after"])
-    with pytest.raises(tc.TcError):
+    with pytest.raises(ValueError):
         tc.tc_residual_norms(ctx, d["h"], d["y"].to(BF16), after=d["after"])
+    with pytest.raises(ValueError):
+        tc.tc_residual_norms(ctx, d["h"], d["y"].cpu(), after=d["after"])
     with pytest.raises(tc.TcError):
         tc.tc_residual_norms(ctx, d["h"], d["y"], after=d["after"], sum_out=d["h"])    # in place
     with pytest.raises(tc.TcError):
