@@ -26,10 +26,15 @@ __device__ __forceinline__ float scale_of(uint32_t amax_bits)
 // Codes of four values: rounded to the nearest e4m3 value, ties to even, beyond the range the largest.
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv)
 {
-    uint16_t lo, hi;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(__fmul_rn(b, inv)), "f"(__fmul_rn(a, inv)));
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(__fmul_rn(d, inv)), "f"(__fmul_rn(c, inv)));
-    return (uint32_t)lo | (uint32_t)hi << 16;
+    uint32_t codes;
+    asm("{\n\t.reg .b64 p, q, s;\n\t.reg .f32 x, y, z, w;\n\t.reg .b16 lo, hi;\n\t"
+        "mov.b64 p, {%1, %2};\n\tmov.b64 q, {%3, %4};\n\tmov.b64 s, {%5, %5};\n\t"
+        "mul.rn.f32x2 p, p, s;\n\tmul.rn.f32x2 q, q, s;\n\t"
+        "mov.b64 {x, y}, p;\n\tmov.b64 {z, w}, q;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 lo, y, x;\n\tcvt.rn.satfinite.e4m3x2.f32 hi, w, z;\n\t"
+        "mov.b32 %0, {lo, hi};\n\t}"
+        : "=r"(codes) : "f"(a), "f"(b), "f"(c), "f"(d), "f"(inv));
+    return codes;
 }
 __device__ __forceinline__ uint2 codes8(const float (&v)[8], float inv)
 {
@@ -43,11 +48,51 @@ __device__ __forceinline__ uint32_t max16(uint32_t v)
     return v;
 }
 
+// Two fp32 values in a register pair, on which one instruction works.
+__device__ __forceinline__ uint64_t pair_of(float a, float b)
+{
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    return v;
+}
+__device__ __forceinline__ uint64_t pair_of(uint32_t a, uint32_t b)
+{
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(a), "r"(b));
+    return v;
+}
+__device__ __forceinline__ void halves(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
 // Eight consecutive values as they lie in memory.
 template <typename T> struct Raw8;
 template <> struct Raw8<__nv_bfloat16> { uint4 v; };
 template <> struct Raw8<float> { uint4 v, w; };
 
+// Bits of the largest magnitude of two bf16 values with those of two others, as fp32's.
+__device__ __forceinline__ uint32_t max_pairs(uint32_t m, uint32_t w) { return __vmaxu2(m, w & 0x7fff7fffu); }
+__device__ __forceinline__ uint32_t max_of_pair(uint32_t m) { return max(m << 16, m & 0xffff0000u); }
+// Bits of the largest magnitude of eight values.
+__device__ __forceinline__ uint32_t max8(const Raw8<__nv_bfloat16> &r)
+{
+    return max_of_pair(max_pairs(max_pairs(max_pairs(r.v.x & 0x7fff7fffu, r.v.y), r.v.z), r.v.w));
+}
+__device__ __forceinline__ uint32_t max8(const Raw8<float> &r)
+{
+    const uint32_t k = 0x7fffffffu;
+    return max(max(max(r.v.x & k, r.v.y & k), max(r.v.z & k, r.v.w & k)), max(max(r.w.x & k, r.w.y & k), max(r.w.z & k, r.w.w & k)));
+}
 __device__ __forceinline__ void zero8(Raw8<__nv_bfloat16> &r) { r.v = make_uint4(0, 0, 0, 0); }
 __device__ __forceinline__ void zero8(Raw8<float> &r) { r.v = r.w = make_uint4(0, 0, 0, 0); }
 __device__ __forceinline__ void load8(Raw8<__nv_bfloat16> &r, const __nv_bfloat16 *p) { r.v = *reinterpret_cast<const uint4 *>(p); }

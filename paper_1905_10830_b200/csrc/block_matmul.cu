@@ -18,6 +18,7 @@ namespace {
 
 using namespace tcdev;
 using namespace sm100;
+using namespace blk;
 
 constexpr int kBlockK = 128;
 constexpr int kRowsM = 128;
@@ -64,32 +65,6 @@ struct TileArgs {
     float *partial;                   // [unit][column][128 rows], where the length is split
     unsigned int *status;
 };
-
-__device__ __forceinline__ uint64_t pair_of(float a, float b)
-{
-    uint64_t v;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
-    return v;
-}
-__device__ __forceinline__ uint64_t pair_of(uint32_t a, uint32_t b)
-{
-    uint64_t v;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(a), "r"(b));
-    return v;
-}
-__device__ __forceinline__ void halves(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
-{
-    uint64_t d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 
 struct Unit {
     int tile_m, tile_n, k_first, k_end;
@@ -627,7 +602,7 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
                                 finish(sum[k * 16 + c / 8 + g], col0 + c + 8 * g + 2 * q, x, y);
                                 const uint32_t byte = (uint32_t)(8 * g + 2 * q) * sizeof(T), to = box + (uint32_t)(8 * k + i) * 128u + (((byte >> 4) ^ i) << 4) + (byte & 15u);
                                 if constexpr (sizeof(T) == 4) asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(x), "f"(y) : "memory");
-                                else asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(blk::pack_bf16(x, y)) : "memory");
+                                else asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(pack_bf16(x, y)) : "memory");
                             }
                     } else {
 #pragma unroll

@@ -46,10 +46,7 @@ __global__ void __launch_bounds__(kRowThreads) quantize_rows_kernel(const T *x, 
     for (int i = 0; i < kInFlight; ++i) {
         float v[8];
         values8(raw[i], v);
-        uint32_t m = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[j]));
-        const float scale = scale_of(max16(m));
+        const float scale = scale_of(max16(max8(raw[i])));
         if (first + i * (kRowThreads / 16) >= items) continue;
         const int k = (int)kb[i] * kBlock + k_lane;
         if (k < cols) *reinterpret_cast<uint2 *>(out.codes + (long long)row[i] * out.ld + k) = codes8(v, __frcp_rn(scale));
@@ -68,14 +65,16 @@ struct TileArgs {
 // The tile comes by asynchronous copies and its values are read from shared memory where they are needed, twice for the layout across:
 // with them in registers (96 a thread) two blocks fitted an SM, and a tile's memory time was hardly hidden (8192x4096, both layouts 38 us
 // and Q_BOTH; maps of 256x14x14 x 1024 56 and Q_MAPS).
+constexpr int kTileThreads = 256;
 template <typename T, bool kMaps, bool kSquare>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 5 : 3) quantize_tile_kernel(const T *x, const __grid_constant__ TileArgs a, int vec)
+__global__ void __launch_bounds__(kTileThreads, sizeof(T) == 2 ? 5 : 3) quantize_tile_kernel(const T *x, const __grid_constant__ TileArgs a, int vec)
 {
     using namespace sm100;
+    constexpr int kThreads = kTileThreads, kParts = kThreads / 64, kPart = kBlock / kParts;
     extern __shared__ __align__(16) unsigned char smem[];
     T(*tile)[kBlock] = reinterpret_cast<T(*)[kBlock]>(smem);                       // [outer][inner]
-    __shared__ uint32_t s_max[4][kBlock];
-    __shared__ uint32_t s_warp[8];
+    __shared__ uint32_t s_max[kParts][kBlock];
+    __shared__ uint32_t s_warp[kThreads / 32];
     chain_next();
     chain_wait();
     const long long outer_n = kMaps ? a.c : a.pixels, inner_n = kMaps ? a.pixels : a.c;
@@ -98,22 +97,23 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 5 : 3) quantize_tile_ker
         };
         const int step = vec < kCopy ? vec : kCopy, per_row = kBlock / step, k = t % per_row * step;
         const T *src = x + (k < cols ? inner_at(i0 + k) : 0);
-        for (int r = t / per_row; r < kBlock; r += 256 / per_row) {
+        for (int r = t / per_row; r < kBlock; r += kThreads / per_row) {
             const bool ok = r < rows && k < cols;
             copy(smem_u32(&tile[r][k]), ok ? src + r * pitch : x, ok);
         }
     } else {
         const int k = t & (kBlock - 1);
         const T *src = x + (k < cols ? inner_at(i0 + k) : 0);
-        for (int r0 = t >> 7; r0 < kBlock; r0 += 32) {
+        constexpr int kRows = kThreads / kBlock;
+        for (int r0 = t >> 7; r0 < kBlock; r0 += 16 * kRows) {
             T v[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 v[j] = T(0.f);
-                if (r0 + 2 * j < rows && k < cols) v[j] = src[(r0 + 2 * j) * pitch];
+                if (r0 + kRows * j < rows && k < cols) v[j] = src[(r0 + kRows * j) * pitch];
             }
 #pragma unroll
-            for (int j = 0; j < 16; ++j) tile[r0 + 2 * j][k] = v[j];
+            for (int j = 0; j < 16; ++j) tile[r0 + kRows * j][k] = v[j];
         }
     }
     cp_async_wait_all();
@@ -122,17 +122,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 5 : 3) quantize_tile_ker
     if constexpr (kSquare) {
         uint32_t all = 0;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            float v[8];
-            values8(*reinterpret_cast<const Raw8<T> *>(&tile[(t >> 4) + 16 * r][(t & 15) * 8]), v);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) all = max(all, abs_bits(v[j]));
-        }
+        for (int r = t >> 4; r < kBlock; r += kThreads / 16) all = max(all, max8(*reinterpret_cast<const Raw8<T> *>(&tile[r][(t & 15) * 8])));
         all = __reduce_max_sync(0xffffffffu, all);
         if ((t & 31) == 0) s_warp[t >> 5] = all;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < 8; ++w) all = max(all, s_warp[w]);
+        for (int w = 0; w < kThreads / 32; ++w) all = max(all, s_warp[w]);
         scale = scale_of(all);
         if (t == 0) {
             if (a.along.codes) a.along.scales[i0 / kBlock * a.along.scale_ld + o0 / kBlock] = scale;
@@ -143,16 +138,11 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 5 : 3) quantize_tile_ker
         const int k = (t & 15) * 8;
         uint8_t *to = a.along.codes + (o0 + (t >> 4)) * a.along.ld + i0 + k;
 #pragma unroll 4
-        for (int r = t >> 4; r < kBlock; r += 16, to += 16 * a.along.ld) {
+        for (int r = t >> 4; r < kBlock; r += kThreads / 16, to += kThreads / 16 * a.along.ld) {
+            const Raw8<T> raw = *reinterpret_cast<const Raw8<T> *>(&tile[r][k]);
             float v[8];
-            values8(*reinterpret_cast<const Raw8<T> *>(&tile[r][k]), v);
-            float s = scale;
-            if constexpr (!kSquare) {
-                uint32_t m = 0;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[j]));
-                s = scale_of(max16(m));
-            }
+            values8(raw, v);
+            const float s = kSquare ? scale : scale_of(max16(max8(raw)));
             if (r < rows && k < cols) {
                 *reinterpret_cast<uint2 *>(to) = codes8(v, __frcp_rn(s));
                 if (!kSquare && k == 0) a.along.scales[i0 / kBlock * a.along.scale_ld + o0 + r] = s;
@@ -160,15 +150,15 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 5 : 3) quantize_tile_ker
         }
     }
     if (!a.across.codes) return;
-    // two inner columns and 32 outer values a thread
+    // two inner columns and kPart outer values a thread
     const int pair = t & 63, part = t >> 6;
     auto two = [&](int r, float &v0, float &v1) {
         if constexpr (sizeof(T) == 2) {
-            const uint32_t w = *reinterpret_cast<const uint32_t *>(&tile[part * 32 + r][pair * 2]);
+            const uint32_t w = *reinterpret_cast<const uint32_t *>(&tile[part * kPart + r][pair * 2]);
             v0 = __uint_as_float(w << 16);
             v1 = __uint_as_float(w & 0xffff0000u);
         } else {
-            const float2 w = *reinterpret_cast<const float2 *>(&tile[part * 32 + r][pair * 2]);
+            const float2 w = *reinterpret_cast<const float2 *>(&tile[part * kPart + r][pair * 2]);
             v0 = w.x;
             v1 = w.y;
         }
@@ -177,25 +167,32 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 5 : 3) quantize_tile_ker
     if constexpr (!kSquare) {
         uint32_t m0 = 0, m1 = 0;
 #pragma unroll 8
-        for (int r = 0; r < 32; ++r) {
-            float v0, v1;
-            two(r, v0, v1);
-            m0 = max(m0, abs_bits(v0));
-            m1 = max(m1, abs_bits(v1));
+        for (int r = 0; r < kPart; ++r) {
+            if constexpr (sizeof(T) == 2) m0 = max_pairs(m0, *reinterpret_cast<const uint32_t *>(&tile[part * kPart + r][pair * 2]));
+            else {
+                float v0, v1;
+                two(r, v0, v1);
+                m0 = max(m0, abs_bits(v0));
+                m1 = max(m1, abs_bits(v1));
+            }
+        }
+        if constexpr (sizeof(T) == 2) {                       // both columns' in one word
+            m1 = m0 & 0xffff0000u;
+            m0 <<= 16;
         }
         s_max[part][2 * pair] = m0;
         s_max[part][2 * pair + 1] = m1;
         __syncthreads();
 #pragma unroll
-        for (int q = 0; q < 4; ++q) { m0 = max(m0, s_max[q][2 * pair]); m1 = max(m1, s_max[q][2 * pair + 1]); }
+        for (int q = 0; q < kParts; ++q) { m0 = max(m0, s_max[q][2 * pair]); m1 = max(m1, s_max[q][2 * pair + 1]); }
         scale0 = scale_of(m0);
         scale1 = scale_of(m1);
     }
     const float inv0 = __frcp_rn(scale0), inv1 = __frcp_rn(scale1);
     const int c = 2 * pair;
-    uint8_t *const to = a.across.codes + (i0 + c) * a.across.ld + o0 + part * 32;
+    uint8_t *const to = a.across.codes + (i0 + c) * a.across.ld + o0 + part * kPart;
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
+    for (int q = 0; q < kPart / 16; ++q) {
         uint32_t w0[4], w1[4];
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
@@ -205,7 +202,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 5 : 3) quantize_tile_ker
             w0[h] = codes4(v0[0], v0[1], v0[2], v0[3], inv0);
             w1[h] = codes4(v1[0], v1[1], v1[2], v1[3], inv1);
         }
-        if (part * 32 + 16 * q >= rows) break;                                     // rows of codes end at a multiple of 16
+        if (part * kPart + 16 * q >= rows) break;                                     // rows of codes end at a multiple of 16
         if (c < cols) *reinterpret_cast<uint4 *>(to + 16 * q) = make_uint4(w0[0], w0[1], w0[2], w0[3]);
         if (c + 1 < cols) *reinterpret_cast<uint4 *>(to + a.across.ld + 16 * q) = make_uint4(w1[0], w1[1], w1[2], w1[3]);
     }
@@ -241,7 +238,7 @@ tc_status launch_tiles(int device, const T *x, int n, int c, int hw, bool square
     const dim3 grid((unsigned int)((a.pixels + kBlock - 1) / kBlock), (unsigned int)((c + kBlock - 1) / kBlock));
     constexpr size_t smem = kBlock * kBlock * sizeof(T);
     auto launch = [&](bool allowed, auto kernel) {
-        return allowed && launch_first(true, kernel, grid, dim3(256), smem, s, x, a, vec) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
+        return allowed && launch_first(true, kernel, grid, dim3(kTileThreads), smem, s, x, a, vec) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
     };
 #define TC_TILES(maps, squares) launch(allow_shared<quantize_tile_kernel<T, maps, squares>>(device, smem), quantize_tile_kernel<T, maps, squares>)
     if (hw > 1) return square ? TC_TILES(true, true) : TC_TILES(true, false);

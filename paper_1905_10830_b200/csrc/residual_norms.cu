@@ -440,138 +440,244 @@ __global__ void __launch_bounds__(256) norm_maps_kernel(NormArgs a)
     }
 }
 
-// The same with a tile of 32 pixels and all channels of the inputs in shared memory, where it fits: each value is fetched once, many at
-// a time, and the vectors once a block (256x14x14 x 1024, bf16: 962 us and MAPS_FWD).
-constexpr int kTilePixels = 32;
-constexpr size_t kTileSm = 220 * 1024;
-
-// [c][32] of a tensor's pixels p0 ...; zeros behind the last.  `vec`: four pixels at a time.
-template <typename T>
-__device__ __forceinline__ void load_tile(T *dst, const T *src, long long p0, long long pixels, int c, int hw, bool vec)
-{
-    using namespace sm100;
-    const int t = threadIdx.x;
-    if (vec) {
-        const int px = (t & 7) * 4;
-        const long long p = p0 + px, img = p / hw;
-        const bool ok = p < pixels;
-        const T *from = ok ? src + img * c * (long long)hw + (p - img * hw) : src;
-        for (int ch = t >> 3; ch < c; ch += 32) {
-            const uint32_t to = smem_u32(dst + ch * kTilePixels + px);
-            const T *at = ok ? from + (long long)ch * hw : from;
-            if constexpr (sizeof(T) == 2) cp_async_8(to, at, ok ? 8u : 0u);
-            else cp_async_16(to, at, ok ? 16u : 0u);
-        }
-    } else {
-        const int px = t & 31;
-        const long long p = p0 + px, img = p / hw;
-        const bool ok = p < pixels;
-        const T *from = src + img * c * (long long)hw + (p - img * hw);
-        for (int ch = t >> 5; ch < c; ch += 128) {
-            T v[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                v[i] = T(0.f);
-                if (ok && ch + 8 * i < c) v[i] = from[(long long)(ch + 8 * i) * hw];
+// The same with all channels of a tile of kPx pixels in shared memory, where they fit: each value is fetched once, many at a time, and
+// the vectors once a block (256x14x14 x 1024, bf16: 962 us and MAPS_FWD).  A lane has two pixels, whose values one instruction works on, and
+// eight channels in a row of every kStep.
+constexpr size_t kTileSm = 220 * 1024, kTileStatic = 10 * 1024;       // of an SM's shared memory; what a block has beside its tile
+template <typename T, int kPx>
+struct MapTile {
+    static constexpr int kPairs = kPx / 2, kSubs = 32 / kPairs, kStep = 8 * kSubs * 8;
+    static constexpr int kMask = 128 / (kPx * (int)sizeof(T)) - 1;    // rows that share 128 bytes, less one
+    // Row of a channel: lanes that read rows eight apart read them in different banks.
+    static __device__ __forceinline__ int row(int c) { return (c ^ ((c >> 3) & kMask)) * kPx; }
+    static __device__ __forceinline__ uint64_t load(const T *tile, int c, int pair)
+    {
+        const T *at = tile + row(c) + 2 * pair;
+        if constexpr (sizeof(T) == 2) {
+            const uint32_t w = *reinterpret_cast<const uint32_t *>(at);
+            return pair_of(w << 16, w & 0xffff0000u);
+        } else
+            return *reinterpret_cast<const uint64_t *>(at);
+    }
+    // A tensor's pixels p0 ...; zeros behind the last.  `vec`: four pixels at a time.
+    static __device__ __forceinline__ void fill(T *dst, const T *src, long long p0, long long pixels, int c, int hw, bool vec)
+    {
+        using namespace sm100;
+        const int t = threadIdx.x;
+        if (vec) {
+            constexpr int kQuads = kPx / 4;
+            const int px = t % kQuads * 4;
+            const long long p = p0 + px, img = p / hw;
+            const bool ok = p < pixels;
+            const T *from = ok ? src + img * c * (long long)hw + (p - img * hw) : src;
+            for (int ch = t / kQuads; ch < c; ch += 256 / kQuads) {
+                const uint32_t to = smem_u32(dst + row(ch) + px);
+                const T *at = ok ? from + (long long)ch * hw : from;
+                if constexpr (sizeof(T) == 2) cp_async_8(to, at, ok ? 8u : 0u);
+                else cp_async_16(to, at, ok ? 16u : 0u);
             }
+        } else {
+            constexpr int kRows = 256 / kPx;
+            const int px = t % kPx;
+            const long long p = p0 + px, img = p / hw;
+            const bool ok = p < pixels;
+            const T *from = src + img * c * (long long)hw + (p - img * hw);
+            for (int ch = t / kPx; ch < c; ch += 8 * kRows) {
+                T v[8];
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (ch + 8 * i < c) dst[(ch + 8 * i) * kTilePixels + px] = v[i];
+                for (int i = 0; i < 8; ++i) {
+                    v[i] = T(0.f);
+                    if (ok && ch + kRows * i < c) v[i] = from[(long long)(ch + kRows * i) * hw];
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (ch + kRows * i < c) dst[row(ch + kRows * i) + px] = v[i];
+            }
         }
     }
-}
-// Sum over the block's eight warps, lane by lane.
-__device__ __forceinline__ float over_warps(float (*part)[32], float v)
-{
-    part[threadIdx.x >> 5][threadIdx.x & 31] = v;
-    __syncthreads();
-    v = 0.f;
+    // Sum over the block's lanes that share this lane's pixels.
+    static __device__ __forceinline__ uint64_t over_block(float2 (*part)[kPairs], uint64_t v)
+    {
+        float x, y;
+        halves(v, x, y);
 #pragma unroll
-    for (int w = 0; w < 8; ++w) v += part[w][threadIdx.x & 31];
-    return v;
+        for (int d = kPairs; d < 32; d *= 2) {
+            x += __shfl_xor_sync(0xffffffffu, x, d);
+            y += __shfl_xor_sync(0xffffffffu, y, d);
+        }
+        const int lane = threadIdx.x & 31;
+        if (lane < kPairs) part[threadIdx.x >> 5][lane] = make_float2(x, y);
+        __syncthreads();
+        x = y = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            const float2 q = part[w][lane % kPairs];
+            x += q.x;
+            y += q.y;
+        }
+        return pair_of(x, y);
+    }
+};
+// Where a lane's two pixels lie in a map, and how they are written.
+struct MapPixels {
+    long long at0, at1;
+    bool ok0, ok1, both;              // both: neighbours that one store writes
+    __device__ __forceinline__ MapPixels(long long p, long long pixels, int c, int hw, bool pairs)
+    {
+        ok0 = p < pixels;
+        ok1 = p + 1 < pixels;
+        const long long img = p / hw;
+        at0 = img * c * (long long)hw + (p - img * hw);
+        at1 = p + 1 == (img + 1) * hw ? (img + 1) * c * (long long)hw : at0 + 1;
+        both = pairs && ok1;
+    }
+    template <typename T>
+    __device__ __forceinline__ void store(T *map, long long channel, uint64_t v) const
+    {
+        float x, y;
+        halves(v, x, y);
+        if (both) {
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t *>(map + at0 + channel) = pack_bf16(x, y);
+            else *reinterpret_cast<float2 *>(map + at0 + channel) = make_float2(x, y);
+        } else {
+            if (ok0) store1(map + at0 + channel, x);
+            if (ok1) store1(map + at1 + channel, y);
+        }
+    }
+};
+__device__ __forceinline__ void weights8(float (&f)[8], const float *v)
+{
+    const float4 a = reinterpret_cast<const float4 *>(v)[0], b = reinterpret_cast<const float4 *>(v)[1];
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) norm_maps_tile_kernel(const __grid_constant__ NormArgs a, int vec)
+template <typename T, int kPx>
+__global__ void __launch_bounds__(256) norm_maps_tile_kernel(const __grid_constant__ NormArgs a, int vec, int pairs)
 {
-    extern __shared__ __align__(16) unsigned char s_tile[];   // after times the channels' gate [c], before [c]; h, y, gate: [c][32]
-    __shared__ float s_part[2][8][32];
-    __shared__ uint32_t s_max[2][8][32];
-    float *const wy = reinterpret_cast<float *>(s_tile), *const wx = wy + a.c;
-    T *const sh = reinterpret_cast<T *>(s_tile + ((2 * a.c * sizeof(float) + 15) & ~15ull)), *const sy = sh + a.c * kTilePixels, *const sg = sy + a.c * kTilePixels;
+    using M = MapTile<T, kPx>;
+    extern __shared__ __align__(16) unsigned char s_tile[];   // with c8 channels, c rounded up to eight: after times the channels' gate, before; h, y, gate [c8][kPx]
+    __shared__ float2 s_part[2][8][M::kPairs];
+    __shared__ uint2 s_max[2][8][M::kPairs];
+    const int c8 = (a.c + 7) & ~7;
+    float *const wy = reinterpret_cast<float *>(s_tile), *const wx = wy + c8;
+    T *const sh = reinterpret_cast<T *>(wx + c8), *const sy = sh + c8 * kPx, *const sg = sy + (a.y ? c8 * kPx : 0);
     chain_next();
     chain_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int i = threadIdx.x; i < a.c; i += 256) {
-        wy[i] = (a.after ? a.after[i] : 1.f) * (a.gate ? a.gate[i] : 1.f);
-        wx[i] = a.before ? a.before[i] : 0.f;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pair = lane % M::kPairs, slice = warp * M::kSubs + lane / M::kPairs;
+    for (int i = threadIdx.x; i < c8; i += 256) {
+        wy[i] = i < a.c ? (a.after ? a.after[i] : 1.f) * (a.gate ? a.gate[i] : 1.f) : 0.f;
+        wx[i] = i < a.c && a.before ? a.before[i] : 0.f;
+    }
+    const int inputs = 1 + (a.y != nullptr) + (a.gate_map != nullptr);
+    for (int i = threadIdx.x; i < inputs * (c8 - a.c) * kPx; i += 256) {           // channels that there are not
+        const int ch = a.c + i / kPx % (c8 - a.c);
+        sh[(i / (kPx * (c8 - a.c))) * c8 * kPx + M::row(ch) + i % kPx] = T(0.f);
     }
     const float scale = a.scale ? *a.scale : 1.f, inv_c = 1.0f / (float)a.c;
-    const long long tiles = (a.pixels + kTilePixels - 1) / kTilePixels;
+    const long long tiles = (a.pixels + kPx - 1) / kPx;
     for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const long long p = tile * kTilePixels + lane, img = p / a.hw, base = img * a.c * (long long)a.hw + (p - img * a.hw);
-        const bool ok = p < a.pixels;
+        const long long p0 = tile * kPx, p = p0 + 2 * pair;
+        const MapPixels px(p, a.pixels, a.c, a.hw, pairs);
         __syncthreads();                                      // the last tile's readers
-        load_tile(sh, (const T *)a.h, tile * kTilePixels, a.pixels, a.c, a.hw, vec);
-        if (a.y) load_tile(sy, (const T *)a.y, tile * kTilePixels, a.pixels, a.c, a.hw, vec);
-        if (a.gate_map) load_tile(sg, (const T *)a.gate_map, tile * kTilePixels, a.pixels, a.c, a.hw, vec);
+        M::fill(sh, (const T *)a.h, p0, a.pixels, a.c, a.hw, vec);
+        if (a.y) M::fill(sy, (const T *)a.y, p0, a.pixels, a.c, a.hw, vec);
+        if (a.gate_map) M::fill(sg, (const T *)a.gate_map, p0, a.pixels, a.c, a.hw, vec);
         sm100::cp_async_wait_all();
         __syncthreads();
-        float f = scale;
+        uint64_t f = pair_of(scale, scale);
         if (a.y && a.after) {
-            float sum = 0.f;
-            for (int c0 = warp * 16; c0 < a.c; c0 += kBlock) {
+            uint64_t sum = 0ull;
+            for (int c0 = slice * 8; c0 < a.c; c0 += M::kStep) {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const float v = c0 + j < a.c ? load1(sy + (c0 + j) * kTilePixels + lane) : 0.f;
-                    sum = fmaf(v, v, sum);
+                for (int j = 0; j < 8; ++j) {
+                    const uint64_t v = M::load(sy, c0 + j, pair);
+                    sum = fma2(v, v, sum);
                 }
             }
-            f *= inv_sqrt(fmaf(over_warps(s_part[0], sum), inv_c, a.eps));
+            float x, y;
+            halves(M::over_block(s_part[0], sum), x, y);
+            f = pair_of(scale * inv_sqrt(fmaf(x, inv_c, a.eps)), scale * inv_sqrt(fmaf(y, inv_c, a.eps)));
         }
-        auto sum_at = [&](int ch) {
-            const int at = ch * kTilePixels + lane;
-            const float s = load1(sh + at);
-            if (!a.y) return s;
-            float u = load1(sy + at) * wy[ch];
-            if (a.gate_map) u *= load1(sg + at);
-            return fmaf(f, u, s);
-        };
-        float sum = 0.f;
-        T *to = (T *)a.sum + base;
-        for (int c0 = warp * 16; c0 < a.c; c0 += kBlock) {
+        // s of eight channels from c0 on
+        auto sums_at = [&](int c0, uint64_t (&v)[8]) {
+            if (!a.y) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (c0 + j < a.c) {
-                    const float v = sum_at(c0 + j);
-                    sum = fmaf(v, v, sum);
-                    if (a.y && ok) store1(to + (long long)(c0 + j) * a.hw, v);
-                }
+                for (int j = 0; j < 8; ++j) v[j] = M::load(sh, c0 + j, pair);
+                return;
+            }
+            float w[8];
+            weights8(w, wy + c0);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                uint64_t u = mul2(M::load(sy, c0 + j, pair), pair_of(w[j], w[j]));
+                if (a.gate_map) u = mul2(u, M::load(sg, c0 + j, pair));
+                v[j] = fma2(f, u, M::load(sh, c0 + j, pair));
+            }
+        };
+        uint64_t sum = 0ull;
+        for (int c0 = slice * 8; c0 < a.c; c0 += M::kStep) {
+            uint64_t v[8];
+            sums_at(c0, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                sum = fma2(v[j], v[j], sum);
+                if (a.y && c0 + j < a.c) px.store((T *)a.sum, (long long)(c0 + j) * a.hw, v[j]);
+            }
         }
         if (!a.before) continue;
-        const float r = inv_sqrt(fmaf(over_warps(s_part[1], sum), inv_c, a.eps));
-        to = (T *)a.x + base;
+        float rx, ry;
+        halves(M::over_block(s_part[1], sum), rx, ry);
+        const uint64_t r = pair_of(inv_sqrt(fmaf(rx, inv_c, a.eps)), inv_sqrt(fmaf(ry, inv_c, a.eps)));
         int turn = 0;
-        for (int b0 = 0; b0 < a.c; b0 += kBlock, turn ^= 1) {
-            const int c0 = b0 + warp * 16;
-            float v[16];
-            uint32_t m = 0;
+        for (int b0 = 0; b0 < a.c; b0 += M::kStep, turn ^= 1) {                    // (the same for all lanes: the codes' barrier)
+            const int c0 = b0 + slice * 8;
+            uint64_t v[8];
+            uint32_t m0 = 0, m1 = 0;
+            if (c0 < a.c) {
+                float w[8];
+                sums_at(c0, v);
+                weights8(w, wx + c0);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                v[j] = c0 + j < a.c ? sum_at(c0 + j) * r * wx[c0 + j] : 0.f;
-                m = max(m, abs_bits(v[j]));
-                if (a.x && ok && c0 + j < a.c) store1(to + (long long)(c0 + j) * a.hw, v[j]);
+                for (int j = 0; j < 8; ++j) {
+                    v[j] = mul2(mul2(v[j], r), pair_of(w[j], w[j]));
+                    float x, y;
+                    halves(v[j], x, y);
+                    m0 = max(m0, abs_bits(x));
+                    m1 = max(m1, abs_bits(y));
+                    if (a.x && c0 + j < a.c) px.store((T *)a.x, (long long)(c0 + j) * a.hw, v[j]);
+                }
             }
             if (a.codes.codes) {
-                s_max[turn][warp][lane] = m;
+                constexpr int kBlockWarps = 8 * kBlock / M::kStep;                 // warps whose slices are a block of 128
+#pragma unroll
+                for (int d = M::kPairs; d < 32; d *= 2) {
+                    m0 = max(m0, __shfl_xor_sync(0xffffffffu, m0, d));
+                    m1 = max(m1, __shfl_xor_sync(0xffffffffu, m1, d));
+                }
+                if (lane < M::kPairs) s_max[turn][warp][lane] = make_uint2(m0, m1);
                 __syncthreads();                              // (the other half's readers are past this barrier before it is written again)
 #pragma unroll
-                for (int w = 0; w < 8; ++w) m = max(m, s_max[turn][w][lane]);
-                const float sc = scale_of(m), inv = __frcp_rn(sc);
-                if (ok && c0 < a.c)
-                    *reinterpret_cast<uint4 *>(a.codes.codes + p * a.codes.ld + c0) = make_uint4(
-                        codes4(v[0], v[1], v[2], v[3], inv), codes4(v[4], v[5], v[6], v[7], inv), codes4(v[8], v[9], v[10], v[11], inv), codes4(v[12], v[13], v[14], v[15], inv));
-                if (ok && warp == 0) a.codes.scales[(long long)(b0 / kBlock) * a.codes.scale_ld + p] = sc;
+                for (int w = 0; w < kBlockWarps; ++w) {
+                    const uint2 q = s_max[turn][warp / kBlockWarps * kBlockWarps + w][pair];
+                    m0 = max(m0, q.x);
+                    m1 = max(m1, q.y);
+                }
+                if (c0 < a.c) {
+                    const float sc0 = scale_of(m0), sc1 = scale_of(m1);
+                    float x[8], y[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) halves(v[j], x[j], y[j]);
+                    uint8_t *const to = a.codes.codes + p * a.codes.ld + c0;
+                    float *const scales = a.codes.scales + (long long)(c0 / kBlock) * a.codes.scale_ld + p;
+                    if (px.ok0) {
+                        *reinterpret_cast<uint2 *>(to) = codes8(x, __frcp_rn(sc0));
+                        if (c0 % kBlock == 0) scales[0] = sc0;
+                    }
+                    if (px.ok1) {
+                        *reinterpret_cast<uint2 *>(to + a.codes.ld) = codes8(y, __frcp_rn(sc1));
+                        if (c0 % kBlock == 0) scales[1] = sc1;
+                    }
+                }
             }
         }
     }
@@ -994,104 +1100,181 @@ __global__ void __launch_bounds__(256) norm_maps_grad_kernel(NormGradArgs a)
 }
 
 // The same with the inputs' tile in shared memory, as in the forward.
-template <typename T>
-__global__ void __launch_bounds__(256) norm_maps_grad_tile_kernel(const __grid_constant__ NormGradArgs a, int vec)
+// Sums of eight values over kLanes neighbouring lanes: a lane has those of values first .. first + 8 / kLanes (one at least; lanes of the same
+// value have the same).
+template <int kLanes>
+__device__ __forceinline__ int sum8_over_lanes(float (&v)[8], int lane)
 {
-    extern __shared__ __align__(16) unsigned char s_tile[];   // sums over the pixels [2][c], after times the channels' gate [c], before [c]; s, dx, y, ds, gate: [c][32]
-    __shared__ float s_part[8][kSums][32];
+    int n = 8, first = 0;
+#pragma unroll
+    for (int d = kLanes / 2; d; d /= 2) {
+        if (n > 1) {
+            n /= 2;
+            const bool high = lane & d;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j < n) {
+                    const float keep = high ? v[n + j] : v[j], give = high ? v[j] : v[n + j];
+                    v[j] = keep + __shfl_xor_sync(0xffffffffu, give, d);
+                }
+            first += high ? n : 0;
+        } else
+            v[0] += __shfl_xor_sync(0xffffffffu, v[0], d);
+    }
+    return first;
+}
+
+template <typename T, int kPx>
+__global__ void __launch_bounds__(256) norm_maps_grad_tile_kernel(const __grid_constant__ NormGradArgs a, int vec, int pairs)
+{
+    using M = MapTile<T, kPx>;
+    extern __shared__ __align__(16) unsigned char s_tile[];   // sums over the pixels [2][c8], after times the channels' gate, before; s, dx, y, ds, gate [c8][kPx]
+    __shared__ float2 s_part[kSums][8][M::kPairs];
     __shared__ float s_scale[8];
-    float *const sums_y = reinterpret_cast<float *>(s_tile), *const sums_x = sums_y + a.c, *const wy = sums_x + a.c, *const wx = wy + a.c;
-    const int plane = a.c * kTilePixels;
-    T *const ss = reinterpret_cast<T *>(s_tile + ((4 * a.c * sizeof(float) + 15) & ~15ull)), *const sx = ss + (a.before ? plane : 0), *const sy = sx + (a.before ? plane : 0);
+    const int c8 = (a.c + 7) & ~7, plane = c8 * kPx;
+    float *const sums_y = reinterpret_cast<float *>(s_tile), *const sums_x = sums_y + c8, *const wy = sums_x + c8, *const wx = wy + c8;
+    T *const ss = reinterpret_cast<T *>(wx + c8), *const sx = ss + (a.before ? plane : 0), *const sy = sx + (a.before ? plane : 0);
     T *const sd = sy + (a.y ? plane : 0), *const sg = sd + (a.ds ? plane : 0);
     chain_next();
     chain_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int i = threadIdx.x; i < a.c; i += 256) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pair = lane % M::kPairs, slice = warp * M::kSubs + lane / M::kPairs;
+    for (int i = threadIdx.x; i < c8; i += 256) {
         sums_y[i] = sums_x[i] = 0.f;
-        wy[i] = (a.after ? a.after[i] : 1.f) * (a.gate ? a.gate[i] : 1.f);
-        wx[i] = a.before ? a.before[i] : 0.f;
+        wy[i] = i < a.c ? (a.after ? a.after[i] : 1.f) * (a.gate ? a.gate[i] : 1.f) : 0.f;
+        wx[i] = i < a.c && a.before ? a.before[i] : 0.f;
+    }
+    const int inputs = (a.before ? 2 : 0) + (a.y != nullptr) + (a.ds != nullptr) + (a.gate_map != nullptr);
+    for (int i = threadIdx.x; i < inputs * (c8 - a.c) * kPx; i += 256) {           // channels that there are not
+        const int ch = a.c + i / kPx % (c8 - a.c);
+        ss[(i / (kPx * (c8 - a.c))) * plane + M::row(ch) + i % kPx] = T(0.f);
     }
     const float scale = a.y && a.scale ? *a.scale : 1.f;
-    float sum_scale = 0.f;
-    const long long tiles = (a.pixels + kTilePixels - 1) / kTilePixels;
+    uint64_t sum_scale = 0ull;
+    const long long tiles = (a.pixels + kPx - 1) / kPx;
     for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const long long p0 = tile * kTilePixels, p = p0 + lane, img = p / a.hw, base = img * a.c * (long long)a.hw + (p - img * a.hw);
-        const bool ok = p < a.pixels;
+        const long long p0 = tile * kPx;
+        const MapPixels px(p0 + 2 * pair, a.pixels, a.c, a.hw, pairs);
         __syncthreads();                                      // the last tile's readers
         if (a.before) {
-            load_tile(ss, (const T *)a.s, p0, a.pixels, a.c, a.hw, vec);
-            load_tile(sx, (const T *)a.dx, p0, a.pixels, a.c, a.hw, vec);
+            M::fill(ss, (const T *)a.s, p0, a.pixels, a.c, a.hw, vec);
+            M::fill(sx, (const T *)a.dx, p0, a.pixels, a.c, a.hw, vec);
         }
-        if (a.y) load_tile(sy, (const T *)a.y, p0, a.pixels, a.c, a.hw, vec);
-        if (a.ds) load_tile(sd, (const T *)a.ds, p0, a.pixels, a.c, a.hw, vec);
-        if (a.gate_map) load_tile(sg, (const T *)a.gate_map, p0, a.pixels, a.c, a.hw, vec);
+        if (a.y) M::fill(sy, (const T *)a.y, p0, a.pixels, a.c, a.hw, vec);
+        if (a.ds) M::fill(sd, (const T *)a.ds, p0, a.pixels, a.c, a.hw, vec);
+        if (a.gate_map) M::fill(sg, (const T *)a.gate_map, p0, a.pixels, a.c, a.hw, vec);
         sm100::cp_async_wait_all();
         __syncthreads();
-        float sums[kSums] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (int c0 = warp * 8; c0 < a.c; c0 += 64) {
+        uint64_t sums[kSums] = {0ull, 0ull, 0ull, 0ull, 0ull, 0ull};
+        for (int c0 = slice * 8; c0 < a.c; c0 += M::kStep) {
+            float w[8], b[8];
+            weights8(w, wy + c0);
+            weights8(b, wx + c0);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int ch = c0 + j, at = ch * kTilePixels + lane;
-                if (ch >= a.c) continue;
-                const float s = a.before ? load1(ss + at) : 0.f, t = a.before ? load1(sx + at) * wx[ch] : 0.f;
-                const float y = a.y ? load1(sy + at) : 0.f, ds = a.ds ? load1(sd + at) : 0.f;
-                const float gy = y * wy[ch] * (a.gate_map ? load1(sg + at) : 1.f);
-                sums[0] = fmaf(s, s, sums[0]);
-                sums[1] = fmaf(t, s, sums[1]);
-                sums[2] = fmaf(y, y, sums[2]);
-                sums[3] = fmaf(ds, gy, sums[3]);
-                sums[4] = fmaf(t, gy, sums[4]);
-                sums[5] = fmaf(s, gy, sums[5]);
+                uint64_t s = 0ull, t = 0ull;
+                if (a.before) {
+                    s = M::load(ss, c0 + j, pair);
+                    t = mul2(M::load(sx, c0 + j, pair), pair_of(b[j], b[j]));
+                    sums[0] = fma2(s, s, sums[0]);
+                    sums[1] = fma2(t, s, sums[1]);
+                }
+                if (a.y) {
+                    const uint64_t y = M::load(sy, c0 + j, pair);
+                    uint64_t gy = mul2(y, pair_of(w[j], w[j]));
+                    if (a.gate_map) gy = mul2(gy, M::load(sg, c0 + j, pair));
+                    sums[2] = fma2(y, y, sums[2]);
+                    if (a.ds) sums[3] = fma2(M::load(sd, c0 + j, pair), gy, sums[3]);
+                    sums[4] = fma2(t, gy, sums[4]);
+                    sums[5] = fma2(s, gy, sums[5]);
+                }
             }
         }
+        float sum0[kSums], sum1[kSums];
 #pragma unroll
-        for (int i = 0; i < kSums; ++i) s_part[warp][i][lane] = sums[i];
+        for (int i = 0; i < kSums; ++i) {
+            halves(sums[i], sum0[i], sum1[i]);
+#pragma unroll
+            for (int d = M::kPairs; d < 32; d *= 2) {
+                sum0[i] += __shfl_xor_sync(0xffffffffu, sum0[i], d);
+                sum1[i] += __shfl_xor_sync(0xffffffffu, sum1[i], d);
+            }
+            if (lane < M::kPairs) s_part[i][warp][lane] = make_float2(sum0[i], sum1[i]);
+        }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kSums; ++i) {
-            sums[i] = 0.f;
+            sum0[i] = sum1[i] = 0.f;
 #pragma unroll
-            for (int w = 0; w < 8; ++w) sums[i] += s_part[w][i][lane];
+            for (int w = 0; w < 8; ++w) {
+                const float2 q = s_part[i][w][pair];
+                sum0[i] += q.x;
+                sum1[i] += q.y;
+            }
         }
-        const PixelFactors f = pixel_factors(sums, a, scale);
-        for (int c0 = warp * 8; c0 < a.c; c0 += 64) {
-            float sum_y[8], sum_x[8];
+        const PixelFactors f0 = pixel_factors(sum0, a, scale), f1 = pixel_factors(sum1, a, scale);
+        const uint64_t r = pair_of(f0.r, f1.r), r3m = pair_of(-f0.r3m, -f1.r3m), q = pair_of(f0.q, f1.q), scale_q = pair_of(scale * f0.q, scale * f1.q);
+        const uint64_t mean_q = pair_of(-f0.mean * f0.q * f0.q, -f1.mean * f1.q * f1.q);
+        for (int c0 = slice * 8; c0 - slice * 8 < a.c; c0 += M::kStep) {           // (the same for all lanes: their sums go together)
+            float sum_y[8], sum_x[8], w[8], b[8];
+            const bool some = c0 < a.c;
+            if (some) {
+                weights8(w, wy + c0);
+                weights8(b, wx + c0);
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int ch = c0 + j, at = ch * kTilePixels + lane;
                 sum_y[j] = sum_x[j] = 0.f;
-                if (ch >= a.c) continue;
-                const long long to = base + (long long)ch * a.hw;
-                float d = a.ds ? load1(sd + at) : 0.f;
+                if (!some) continue;
+                const long long to = (long long)(c0 + j) * a.hw;
+                const bool there = c0 + j < a.c;
+                uint64_t d = a.ds ? M::load(sd, c0 + j, pair) : 0ull;
+                float x, y;
                 if (a.before) {
-                    const float s = load1(ss + at), rx = f.r * load1(sx + at);
-                    d = fmaf(-f.r3m, s, fmaf(rx, wx[ch], d));
-                    sum_x[j] = rx * s;
+                    const uint64_t s = M::load(ss, c0 + j, pair), t = mul2(r, M::load(sx, c0 + j, pair));
+                    d = fma2(r3m, s, fma2(t, pair_of(b[j], b[j]), d));
+                    halves(mul2(t, s), x, y);
+                    sum_x[j] = x + y;
                 }
-                if (ok) store1((T *)a.dh + to, d);
+                if (there) px.store((T *)a.dh, to, d);
                 if (a.y) {
-                    const float n = load1(sy + at) * f.q, g = a.gate_map ? load1(sg + at) : 1.f, dn = d * n, dw = d * wy[ch];
-                    sum_scale = fmaf(dn * g, wy[ch], sum_scale);
-                    sum_y[j] = dn * g;
-                    if (ok) {
-                        store1((T *)a.dy + to, f.q * fmaf(-n, f.mean, scale * (dw * g)));
-                        if (a.gate_map) store1((T *)a.dgate_map + to, scale * (dw * n));
+                    const uint64_t yy = M::load(sy, c0 + j, pair), ww = pair_of(w[j], w[j]), dw = mul2(d, ww);
+                    uint64_t dn = mul2(d, mul2(yy, q)), dwg = dw;
+                    if (a.gate_map) {
+                        const uint64_t g = M::load(sg, c0 + j, pair);
+                        dn = mul2(dn, g);
+                        dwg = mul2(dw, g);
+                        if (there) px.store((T *)a.dgate_map, to, mul2(scale_q, mul2(dw, yy)));
                     }
+                    sum_scale = fma2(dn, ww, sum_scale);
+                    halves(dn, x, y);
+                    sum_y[j] = x + y;
+                    if (there) px.store((T *)a.dy, to, fma2(yy, mean_q, mul2(scale_q, dwg)));
                 }
             }
-            const float vy = sum8_over_warp(sum_y, lane), vx = sum8_over_warp(sum_x, lane);
-            if ((lane & 3) == 0 && c0 + (lane >> 2) < a.c) {
-                sums_y[c0 + (lane >> 2)] += vy;
-                sums_x[c0 + (lane >> 2)] += vx;
+            const int first = sum8_over_lanes<M::kPairs>(sum_y, lane);
+            sum8_over_lanes<M::kPairs>(sum_x, lane);
+            constexpr int kEach = 8 / M::kPairs > 1 ? 8 / M::kPairs : 1, kSame = M::kPairs > 8 ? M::kPairs / 8 : 1;
+            if (some && lane % kSame == 0) {
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) {
+                    sums_y[c0 + first + j] += sum_y[j];
+                    sums_x[c0 + first + j] += sum_x[j];
+                }
             }
         }
     }
+    float x, y;
+    halves(sum_scale, x, y);
+    x += y;
 #pragma unroll
-    for (int d = 16; d; d >>= 1) sum_scale += __shfl_xor_sync(0xffffffffu, sum_scale, d);
-    if (lane == 0) s_scale[warp] = sum_scale;
+    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+    if (lane == 0) s_scale[warp] = x;
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * a.c; i += 256) a.partial[(long long)blockIdx.x * 2 * a.c + i] = sums_y[i];
+    float *const to = a.partial + (long long)blockIdx.x * 2 * a.c;
+    for (int i = threadIdx.x; i < a.c; i += 256) {
+        to[i] = sums_y[i];
+        to[a.c + i] = sums_x[i];
+    }
     if (threadIdx.x == 0) {
         float v = 0.f;
         for (int w = 0; w < 8; ++w) v += s_scale[w];
@@ -1179,19 +1362,55 @@ bool four_pixels(int hw, P... p)
 {
     return hw % 4 == 0 && ((((uintptr_t)p) | ...) & (4 * sizeof(T) - 1)) == 0;
 }
+// Whether two neighbouring pixels are written at once.
+template <typename T, typename... P>
+bool pixel_pairs(int hw, P... p)
+{
+    return hw % 2 == 0 && ((((uintptr_t)p) | ...) & (2 * sizeof(T) - 1)) == 0;
+}
+
+// Tile of a maps' kernel: as many pixels as fit, but no more than 16 while the tiles are fewer than two an SM; 0 where not even eight do.
+struct MapPlan {
+    int px = 0;
+    size_t smem = 0;
+    long long blocks = 0;
+};
+MapPlan plan_maps(int inputs, int vectors, int c, size_t size, long long pixels, int sms)
+{
+    MapPlan m;
+    const size_t c8 = (size_t)((c + 7) & ~7);
+    for (int px = 32; px >= 8; px /= 2) {
+        const size_t smem = c8 * (vectors * sizeof(float) + inputs * px * size);
+        if (smem + kTileStatic > kTileSm || (px > 16 && pixels <= 2ll * sms * px)) continue;
+        const long long fit = (long long)(kTileSm / (smem + kTileStatic)), tiles = (pixels + px - 1) / px, most = (fit < 4 ? fit : 4) * sms;
+        m.px = px;
+        m.smem = smem;
+        m.blocks = tiles < most ? tiles : most;
+        break;
+    }
+    return m;
+}
+MapPlan plan_grad_maps(const NormGradArgs &a, size_t size, int sms)
+{
+    return plan_maps((a.before ? 2 : 0) + (a.y != nullptr) + (a.ds != nullptr) + (a.gate_map != nullptr), 4, a.c, size, a.pixels, sms);
+}
+
+template <auto kKernel, typename A>
+cudaError_t launch_maps(const A &a, const MapPlan &m, long long blocks, bool vec, bool pairs, cudaStream_t s)
+{
+    if (!allow_shared<kKernel>(a.device, kTileSm)) return cudaErrorInvalidValue;
+    return launch_first(true, kKernel, dim3((unsigned int)blocks), dim3(256), m.smem, s, a, (int)vec, (int)pairs);
+}
 
 template <typename T>
 tc_status norms(const NormArgs &a, cudaStream_t s)
 {
     if (a.hw > 1) {
-        const int inputs = 1 + (a.y != nullptr) + (a.gate_map != nullptr);
-        const size_t smem = ((2 * a.c * sizeof(float) + 15) & ~(size_t)15) + (size_t)inputs * a.c * kTilePixels * sizeof(T);
-        if (smem + 6 * 1024 <= kTileSm) {
-            const long long tiles = (a.pixels + kTilePixels - 1) / kTilePixels, fit = kTileSm / (smem + 6 * 1024), most = (fit < 8 ? fit : 8) * a.sms;
-            if (!allow_shared<norm_maps_tile_kernel<T>>(a.device, kTileSm)) return TC_ERR_CUDA;
-            return launch_first(true, norm_maps_tile_kernel<T>, dim3((unsigned int)(tiles < most ? tiles : most)), dim3(256), smem, s, a,
-                                (int)four_pixels<T>(a.hw, a.h, a.y, a.gate_map)) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
-        }
+        const MapPlan m = plan_maps(1 + (a.y != nullptr) + (a.gate_map != nullptr), 2, a.c, sizeof(T), a.pixels, a.sms);
+        const bool vec = four_pixels<T>(a.hw, a.h, a.y, a.gate_map), pairs = pixel_pairs<T>(a.hw, a.sum, a.x);
+        if (m.px == 32) return launch_maps<norm_maps_tile_kernel<T, 32>>(a, m, m.blocks, vec, pairs, s) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
+        if (m.px == 16) return launch_maps<norm_maps_tile_kernel<T, 16>>(a, m, m.blocks, vec, pairs, s) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
+        if (m.px == 8) return launch_maps<norm_maps_tile_kernel<T, 8>>(a, m, m.blocks, vec, pairs, s) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
         return launch_first(true, norm_maps_kernel<T>, dim3((unsigned int)((a.pixels + 31) / 32)), dim3(256), 0, s, a) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
     }
     if (a.c <= 256) return launch_norm_rows<T, 1, 1>(a, s);
@@ -1226,22 +1445,16 @@ cudaError_t launch_grad(const NormGradArgs &a, int blocks, cudaStream_t s)
     return launch_grad_rows<T, kWarps, 1>(a, blocks, s);
 }
 
-constexpr size_t kTileStatic = 8 * 1024;                      // of the gradient's kernel, and the system's
-size_t grad_tile_bytes(const NormGradArgs &a, size_t size)
-{
-    const int inputs = (a.before ? 2 : 0) + (a.y != nullptr) + (a.ds != nullptr) + (a.gate_map != nullptr);
-    return ((4 * a.c * sizeof(float) + 15) & ~(size_t)15) + (size_t)inputs * a.c * kTilePixels * size;
-}
-
 template <typename T>
-tc_status gradient(const NormGradArgs &a, int blocks, cudaStream_t s)
+tc_status gradient(const NormGradArgs &a, int blocks, int sms, cudaStream_t s)
 {
     cudaError_t err = cudaSuccess;
     if (blocks == 0) {                                        // no pixels: the vectors' gradients are zero
-    } else if (const size_t tile = grad_tile_bytes(a, sizeof(T)); a.hw > 1 && tile + kTileStatic <= kTileSm) {
-        err = allow_shared<norm_maps_grad_tile_kernel<T>>(a.device, kTileSm)
-                  ? launch_first(true, norm_maps_grad_tile_kernel<T>, dim3((unsigned int)blocks), dim3(256), tile, s, a,
-                                 (int)four_pixels<T>(a.hw, a.s, a.dx, a.y, a.ds, a.gate_map)) : cudaErrorInvalidValue;
+    } else if (const MapPlan m = plan_grad_maps(a, sizeof(T), sms); a.hw > 1 && m.px) {
+        const bool vec = four_pixels<T>(a.hw, a.s, a.dx, a.y, a.ds, a.gate_map), pairs = pixel_pairs<T>(a.hw, a.dh, a.dy, a.dgate_map);
+        err = m.px == 32   ? launch_maps<norm_maps_grad_tile_kernel<T, 32>>(a, m, blocks, vec, pairs, s)
+              : m.px == 16 ? launch_maps<norm_maps_grad_tile_kernel<T, 16>>(a, m, blocks, vec, pairs, s)
+                           : launch_maps<norm_maps_grad_tile_kernel<T, 8>>(a, m, blocks, vec, pairs, s);
     } else if (a.hw > 1) {
         const size_t smem = (size_t)2 * a.c * sizeof(float);
         err = allow_shared<norm_maps_grad_kernel<T>>(a.device, 2 * kMostChannels * sizeof(float))
@@ -1264,20 +1477,23 @@ tc_status tc_launch_residual_norms(const NormArgs &a, int dtype, cudaStream_t s)
     return dtype == TC_BF16 ? norms<__nv_bfloat16>(a, s) : norms<float>(a, s);
 }
 
-// Blocks of the gradient's kernel: as many as an SM holds of its row's width, four of the maps' kernel.
-int tc_norm_grad_blocks(long long pixels, int c, int hw, int dtype, int sm_count)
+// Blocks of the gradient's kernel: as many as an SM holds of its row's or tile's size.
+int tc_norm_grad_blocks(const NormGradArgs &a, int dtype, int sm_count)
 {
-    long long rows = pixels, per_sm = 1;
-    if (hw > 1) { rows = (pixels + 31) / 32; per_sm = 4; }
-    else if (c <= 256) { rows = (pixels + 7) / 8; per_sm = 2; }
+    const size_t size = dtype == TC_BF16 ? 2 : 4;
+    if (a.hw > 1)
+        if (const MapPlan m = plan_grad_maps(a, size, sm_count); m.px) return (int)m.blocks;
+    long long rows = a.pixels, per_sm = 1;
+    if (a.hw > 1) { rows = (a.pixels + 31) / 32; per_sm = 4; }
+    else if (a.c <= 256) { rows = (a.pixels + 7) / 8; per_sm = 2; }
     else
         for (int warps = 2; warps <= 16; warps *= 2)
-            if (c <= 256 * warps) { per_sm = 16 * ring_chunks(warps, dtype == TC_BF16 ? 2 : 4) / warps; break; }
+            if (a.c <= 256 * warps) { per_sm = 16 * ring_chunks(warps, (int)size) / warps; break; }
     const long long most = per_sm * sm_count;
     return (int)(rows < most ? rows : most);
 }
 
-tc_status tc_launch_residual_norms_backward(const NormGradArgs &a, int dtype, int blocks, cudaStream_t s)
+tc_status tc_launch_residual_norms_backward(const NormGradArgs &a, int dtype, int blocks, int sm_count, cudaStream_t s)
 {
-    return dtype == TC_BF16 ? gradient<__nv_bfloat16>(a, blocks, s) : gradient<float>(a, blocks, s);
+    return dtype == TC_BF16 ? gradient<__nv_bfloat16>(a, blocks, sm_count, s) : gradient<float>(a, blocks, sm_count, s);
 }

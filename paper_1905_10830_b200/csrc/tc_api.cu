@@ -2013,7 +2013,7 @@ tc_status tc_residual_norms_backward(tc_ctx *ctx, const tc_tensor *s, const tc_n
     a.c = s->c;
     a.hw = p ? s->h * s->w : 1;
     a.vec = s->c % 8 == 0 && aligned_to(16, a.s, a.y, a.dx, a.ds, a.gate_map, a.after, a.gate, a.before, a.dh, a.dy, a.dgate_map);
-    const int blocks = tc_norm_grad_blocks(p, a.c, a.hw, s->dtype, ctx->sm_count);
+    const int blocks = tc_norm_grad_blocks(a, s->dtype, ctx->sm_count);
     CallScratch scratch;
     const size_t bytes = ((size_t)blocks * (2 * (size_t)a.c + 1) + 1) * sizeof(float);
     const tc_status st = call_scratch(ctx, bytes, bytes, (cudaStream_t)cuda_stream, &scratch);
@@ -2022,7 +2022,7 @@ tc_status tc_residual_norms_backward(tc_ctx *ctx, const tc_tensor *s, const tc_n
     a.device = ctx->device;
     a.status = ctx->d_status;
     a.partial_scale = a.partial + (size_t)blocks * 2 * a.c;
-    return tc_launch_residual_norms_backward(a, s->dtype, blocks, (cudaStream_t)cuda_stream);
+    return tc_launch_residual_norms_backward(a, s->dtype, blocks, ctx->sm_count, (cudaStream_t)cuda_stream);
 }
 
 }  // extern "C"

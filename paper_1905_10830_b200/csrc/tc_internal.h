@@ -377,8 +377,8 @@ struct NormGradArgs {
     int device;
     unsigned int *status;
 };
-int tc_norm_grad_blocks(long long pixels, int c, int hw, int dtype, int sm_count);
-tc_status tc_launch_residual_norms_backward(const NormGradArgs &a, int dtype, int blocks, cudaStream_t s);
+int tc_norm_grad_blocks(const NormGradArgs &a, int dtype, int sm_count);
+tc_status tc_launch_residual_norms_backward(const NormGradArgs &a, int dtype, int blocks, int sm_count, cudaStream_t s);
 // Tensor map of an fp32 or bf16 matrix [rows][cols] (rows a multiple of 16 bytes): boxes of 128 bytes x box_rows rows, 128-byte swizzle.
 bool tc_tensor_map_rows(CUtensorMap *map, const void *base, int dtype, long long rows, long long cols, int box_rows);
 // The same of e4m3 codes [rows][ld] of which `cols` count: boxes of 128 codes.
