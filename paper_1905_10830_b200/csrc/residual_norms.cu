@@ -443,55 +443,59 @@ __global__ void __launch_bounds__(256) norm_maps_kernel(NormArgs a)
 // The same with all channels of a tile of kPx pixels in shared memory, where they fit: each value is fetched once, many at a time, and
 // the vectors once a block (256x14x14 x 1024, bf16: 962 us and MAPS_FWD).  A lane has two pixels, whose values one instruction works on, and
 // eight channels in a row of every kStep.
-constexpr size_t kTileSm = 220 * 1024, kTileStatic = 10 * 1024;       // of an SM's shared memory; what a block has beside its tile
+constexpr size_t kTileSm = 220 * 1024, kTileStatic = 14 * 1024;       // of an SM's shared memory; what a block has beside its tile
 template <typename T, int kPx>
 struct MapTile {
     static constexpr int kPairs = kPx / 2, kSubs = 32 / kPairs, kStep = 8 * kSubs * 8;
-    static constexpr int kMask = 128 / (kPx * (int)sizeof(T)) - 1;    // rows that share 128 bytes, less one
-    // Row of a channel: lanes that read rows eight apart read them in different banks.
-    static __device__ __forceinline__ int row(int c) { return (c ^ ((c >> 3) & kMask)) * kPx; }
-    static __device__ __forceinline__ uint64_t load(const T *tile, int c, int pair)
+    // Eight channels' rows lie together, a row apart from the next eight's where rows are shorter than 128 bytes: lanes that read rows eight
+    // apart read them in different banks.
+    static constexpr int kEight = 8 * kPx + (kPx * (int)sizeof(T) < 128 ? kPx : 0);
+    static __host__ __device__ constexpr int values(int c8) { return c8 / 8 * kEight; }
+    static __device__ __forceinline__ int row(int c) { return (c >> 3) * kEight + (c & 7) * kPx; }
+    // Of a tile's eight rows (from a channel that is a multiple of eight on, at this lane's pixels) the j-th's two values.
+    static __device__ __forceinline__ const T *eight(const T *tile, int c0, int pair) { return tile + (c0 >> 3) * kEight + 2 * pair; }
+    static __device__ __forceinline__ uint64_t load(const T *rows, int j)
     {
-        const T *at = tile + row(c) + 2 * pair;
         if constexpr (sizeof(T) == 2) {
-            const uint32_t w = *reinterpret_cast<const uint32_t *>(at);
+            const uint32_t w = *reinterpret_cast<const uint32_t *>(rows + j * kPx);
             return pair_of(w << 16, w & 0xffff0000u);
         } else
-            return *reinterpret_cast<const uint64_t *>(at);
+            return *reinterpret_cast<const uint64_t *>(rows + j * kPx);
     }
     // A tensor's pixels p0 ...; zeros behind the last.  `vec`: four pixels at a time.
-    static __device__ __forceinline__ void fill(T *dst, const T *src, long long p0, long long pixels, int c, int hw, bool vec)
+    static __device__ __forceinline__ void fill(T *dst, const T *src, uint32_t p0, uint32_t pixels, int c, int hw, bool vec)
     {
         using namespace sm100;
         const int t = threadIdx.x;
         if (vec) {
-            constexpr int kQuads = kPx / 4;
-            const int px = t % kQuads * 4;
-            const long long p = p0 + px, img = p / hw;
-            const bool ok = p < pixels;
-            const T *from = ok ? src + img * c * (long long)hw + (p - img * hw) : src;
-            for (int ch = t / kQuads; ch < c; ch += 256 / kQuads) {
-                const uint32_t to = smem_u32(dst + row(ch) + px);
-                const T *at = ok ? from + (long long)ch * hw : from;
-                if constexpr (sizeof(T) == 2) cp_async_8(to, at, ok ? 8u : 0u);
-                else cp_async_16(to, at, ok ? 16u : 0u);
+            constexpr int kQuads = kPx / 4, kRows = 256 / kQuads;     // (rows a multiple of eight: each step is as far)
+            const int ch0 = t / kQuads;
+            const uint32_t p = p0 + t % kQuads * 4, img = p / (uint32_t)hw, bytes = p < pixels ? 4u * sizeof(T) : 0u;
+            const T *from = bytes ? src + (long long)img * c * hw + (p - img * (uint32_t)hw) + (long long)ch0 * hw : src;
+            const long long step = bytes ? (long long)kRows * hw : 0;
+            uint32_t to = smem_u32(dst + row(ch0) + t % kQuads * 4);
+#pragma unroll 4
+            for (int ch = ch0; ch < c; ch += kRows, from += step, to += kRows / 8 * kEight * (int)sizeof(T)) {
+                if constexpr (sizeof(T) == 2) cp_async_8(to, from, bytes);
+                else cp_async_16(to, from, bytes);
             }
         } else {
             constexpr int kRows = 256 / kPx;
-            const int px = t % kPx;
-            const long long p = p0 + px, img = p / hw;
+            const int ch0 = t / kPx;
+            const uint32_t p = p0 + t % kPx, img = p / (uint32_t)hw;
             const bool ok = p < pixels;
-            const T *from = src + img * c * (long long)hw + (p - img * hw);
-            for (int ch = t / kPx; ch < c; ch += 8 * kRows) {
-                T v[8];
+            const T *from = src + (long long)img * c * hw + (p - img * (uint32_t)hw) + (long long)ch0 * hw;
+            T *to = dst + t % kPx;
+            for (int ch = ch0; ch < c; ch += 16 * kRows, from += 16ll * kRows * hw) {
+                T v[16];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+                for (int i = 0; i < 16; ++i) {
                     v[i] = T(0.f);
-                    if (ok && ch + kRows * i < c) v[i] = from[(long long)(ch + kRows * i) * hw];
+                    if (ok && ch + kRows * i < c) v[i] = from[(long long)(kRows * i) * hw];
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (ch + kRows * i < c) dst[row(ch + kRows * i) + px] = v[i];
+                for (int i = 0; i < 16; ++i)
+                    if (ch + kRows * i < c) to[row(ch + kRows * i)] = v[i];
             }
         }
     }
@@ -518,79 +522,127 @@ struct MapTile {
         return pair_of(x, y);
     }
 };
-// Where a lane's two pixels lie in a map, and how they are written.
+// Where a lane's two pixels lie in a map, and how they are written: one store for both where they are neighbours at an even place.
 struct MapPixels {
     long long at0, at1;
-    bool ok0, ok1, both;              // both: neighbours that one store writes
-    __device__ __forceinline__ MapPixels(long long p, long long pixels, int c, int hw, bool pairs)
+    bool ok0, ok1, both;
+    __device__ __forceinline__ MapPixels(uint32_t p, uint32_t pixels, int c, int hw, bool pairs)
     {
         ok0 = p < pixels;
         ok1 = p + 1 < pixels;
-        const long long img = p / hw;
-        at0 = img * c * (long long)hw + (p - img * hw);
-        at1 = p + 1 == (img + 1) * hw ? (img + 1) * c * (long long)hw : at0 + 1;
+        const uint32_t img = p / (uint32_t)hw, in = p - img * (uint32_t)hw;
+        at0 = (long long)img * c * hw + in;
+        at1 = in + 1 == (uint32_t)hw ? (long long)(img + 1) * c * hw : at0 + 1;
         both = pairs && ok1;
     }
-    template <typename T>
-    __device__ __forceinline__ void store(T *map, long long channel, uint64_t v) const
+};
+// Eight channels of them, from c0 on, those there are.
+template <typename T>
+struct MapRows {
+    T *to0;
+    long long apart;
+    int hw, there;
+    bool ok0, ok1, both;
+    __device__ __forceinline__ MapRows(T *map, const MapPixels &px, int c0, int c, int hw_) : hw(hw_), ok0(px.ok0), ok1(px.ok1), both(px.both)
     {
-        float x, y;
-        halves(v, x, y);
+        to0 = map + px.at0 + (long long)c0 * hw_;
+        apart = px.at1 - px.at0;
+        there = c - c0;
+    }
+    __device__ __forceinline__ void store1of(int j, float x, float y) const
+    {
+        T *const to = to0 + (uint32_t)(j * hw);
         if (both) {
-            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t *>(map + at0 + channel) = pack_bf16(x, y);
-            else *reinterpret_cast<float2 *>(map + at0 + channel) = make_float2(x, y);
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t *>(to) = pack_bf16(x, y);
+            else *reinterpret_cast<float2 *>(to) = make_float2(x, y);
         } else {
-            if (ok0) store1(map + at0 + channel, x);
-            if (ok1) store1(map + at1 + channel, y);
+            if (ok0) store1(to, x);
+            if (ok1) store1(to + apart, y);
+        }
+    }
+    // Channels j0 ... j0 + 3: with one test for all of them where they are all there (a test for each took as many instructions as the values).
+    __device__ __forceinline__ void store4(int j0, const uint64_t (&v)[4]) const
+    {
+        float x[4], y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) halves(v[j], x[j], y[j]);
+        if (both && there >= 8) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                T *const to = to0 + (uint32_t)((j0 + j) * hw);
+                if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t *>(to) = pack_bf16(x[j], y[j]);
+                else *reinterpret_cast<float2 *>(to) = make_float2(x[j], y[j]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j0 + j < there) store1of(j0 + j, x[j], y[j]);
         }
     }
 };
-__device__ __forceinline__ void weights8(float (&f)[8], const float *v)
+// Each channel's vector value twice, as it multiplies two pixels.
+__device__ __forceinline__ void weights8(uint64_t (&f)[8], const uint64_t *v)
 {
-    const float4 a = reinterpret_cast<const float4 *>(v)[0], b = reinterpret_cast<const float4 *>(v)[1];
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const ulonglong2 w = reinterpret_cast<const ulonglong2 *>(v)[j];
+        f[2 * j] = w.x;
+        f[2 * j + 1] = w.y;
+    }
+}
+__device__ __forceinline__ void fill_weights(uint64_t *wy, uint64_t *wx, const float *after, const float *gate, const float *before, int c, int c8)
+{
+    for (int i = threadIdx.x; i < c8; i += 256) {
+        const float y = i < c ? (after ? after[i] : 1.f) * (gate ? gate[i] : 1.f) : 0.f, x = i < c && before ? before[i] : 0.f;
+        wy[i] = pair_of(y, y);
+        wx[i] = pair_of(x, x);
+    }
+}
+
+// Zeros in the rows of channels that there are not.
+template <typename M, typename T>
+__device__ __forceinline__ void zero_rows(T *tiles, int inputs, int plane, int c, int c8, int px)
+{
+    for (int n = 0; n < inputs; ++n)
+        for (int i = threadIdx.x; i < (c8 - c) * px; i += 256) tiles[n * plane + M::row(c + i / px) + i % px] = T(0.f);
 }
 
 template <typename T, int kPx>
-__global__ void __launch_bounds__(256) norm_maps_tile_kernel(const __grid_constant__ NormArgs a, int vec, int pairs)
+__global__ void __launch_bounds__(256, 3) norm_maps_tile_kernel(const __grid_constant__ NormArgs a, int vec, int pairs)
 {
     using M = MapTile<T, kPx>;
     extern __shared__ __align__(16) unsigned char s_tile[];   // with c8 channels, c rounded up to eight: after times the channels' gate, before; h, y, gate [c8][kPx]
     __shared__ float2 s_part[2][8][M::kPairs];
     __shared__ uint2 s_max[2][8][M::kPairs];
     const int c8 = (a.c + 7) & ~7;
-    float *const wy = reinterpret_cast<float *>(s_tile), *const wx = wy + c8;
-    T *const sh = reinterpret_cast<T *>(wx + c8), *const sy = sh + c8 * kPx, *const sg = sy + (a.y ? c8 * kPx : 0);
+    uint64_t *const wy = reinterpret_cast<uint64_t *>(s_tile), *const wx = wy + c8;
+    const int plane = M::values(c8);
+    T *const sh = reinterpret_cast<T *>(wx + c8), *const sy = sh + plane, *const sg = sy + (a.y ? plane : 0);
     chain_next();
     chain_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pair = lane % M::kPairs, slice = warp * M::kSubs + lane / M::kPairs;
-    for (int i = threadIdx.x; i < c8; i += 256) {
-        wy[i] = i < a.c ? (a.after ? a.after[i] : 1.f) * (a.gate ? a.gate[i] : 1.f) : 0.f;
-        wx[i] = i < a.c && a.before ? a.before[i] : 0.f;
-    }
-    const int inputs = 1 + (a.y != nullptr) + (a.gate_map != nullptr);
-    for (int i = threadIdx.x; i < inputs * (c8 - a.c) * kPx; i += 256) {           // channels that there are not
-        const int ch = a.c + i / kPx % (c8 - a.c);
-        sh[(i / (kPx * (c8 - a.c))) * c8 * kPx + M::row(ch) + i % kPx] = T(0.f);
-    }
+    fill_weights(wy, wx, a.after, a.gate, a.before, a.c, c8);
+    zero_rows<M>(sh, 1 + (a.y != nullptr) + (a.gate_map != nullptr), plane, a.c, c8, kPx);
     const float scale = a.scale ? *a.scale : 1.f, inv_c = 1.0f / (float)a.c;
     const long long tiles = (a.pixels + kPx - 1) / kPx;
     for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const long long p0 = tile * kPx, p = p0 + 2 * pair;
-        const MapPixels px(p, a.pixels, a.c, a.hw, pairs);
+        const uint32_t p0 = (uint32_t)tile * kPx, pixels = (uint32_t)a.pixels;
+        const long long p = (long long)p0 + 2 * pair;
+        const MapPixels px((uint32_t)p, pixels, a.c, a.hw, pairs);
         __syncthreads();                                      // the last tile's readers
-        M::fill(sh, (const T *)a.h, p0, a.pixels, a.c, a.hw, vec);
-        if (a.y) M::fill(sy, (const T *)a.y, p0, a.pixels, a.c, a.hw, vec);
-        if (a.gate_map) M::fill(sg, (const T *)a.gate_map, p0, a.pixels, a.c, a.hw, vec);
+        M::fill(sh, (const T *)a.h, p0, pixels, a.c, a.hw, vec);
+        if (a.y) M::fill(sy, (const T *)a.y, p0, pixels, a.c, a.hw, vec);
+        if (a.gate_map) M::fill(sg, (const T *)a.gate_map, p0, pixels, a.c, a.hw, vec);
         sm100::cp_async_wait_all();
         __syncthreads();
         uint64_t f = pair_of(scale, scale);
         if (a.y && a.after) {
             uint64_t sum = 0ull;
             for (int c0 = slice * 8; c0 < a.c; c0 += M::kStep) {
+                const T *const y = M::eight(sy, c0, pair);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const uint64_t v = M::load(sy, c0 + j, pair);
+                    const uint64_t v = M::load(y, j);
                     sum = fma2(v, v, sum);
                 }
             }
@@ -600,28 +652,31 @@ __global__ void __launch_bounds__(256) norm_maps_tile_kernel(const __grid_consta
         }
         // s of eight channels from c0 on
         auto sums_at = [&](int c0, uint64_t (&v)[8]) {
+            const T *const h = M::eight(sh, c0, pair), *const y = M::eight(sy, c0, pair), *const g = M::eight(sg, c0, pair);
             if (!a.y) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = M::load(sh, c0 + j, pair);
+                for (int j = 0; j < 8; ++j) v[j] = M::load(h, j);
                 return;
             }
-            float w[8];
-            weights8(w, wy + c0);
+            weights8(v, wy + c0);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                uint64_t u = mul2(M::load(sy, c0 + j, pair), pair_of(w[j], w[j]));
-                if (a.gate_map) u = mul2(u, M::load(sg, c0 + j, pair));
-                v[j] = fma2(f, u, M::load(sh, c0 + j, pair));
-            }
+            for (int j = 0; j < 8; ++j) v[j] = mul2(M::load(y, j), v[j]);
+            if (a.gate_map)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = mul2(v[j], M::load(g, j));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = fma2(f, v[j], M::load(h, j));
         };
         uint64_t sum = 0ull;
         for (int c0 = slice * 8; c0 < a.c; c0 += M::kStep) {
             uint64_t v[8];
             sums_at(c0, v);
+            const MapRows<T> to((T *)a.sum, px, c0, a.c, a.hw);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                sum = fma2(v[j], v[j], sum);
-                if (a.y && c0 + j < a.c) px.store((T *)a.sum, (long long)(c0 + j) * a.hw, v[j]);
+            for (int j = 0; j < 8; ++j) sum = fma2(v[j], v[j], sum);
+            if (a.y) {
+                to.store4(0, {v[0], v[1], v[2], v[3]});
+                to.store4(4, {v[4], v[5], v[6], v[7]});
             }
         }
         if (!a.before) continue;
@@ -634,21 +689,26 @@ __global__ void __launch_bounds__(256) norm_maps_tile_kernel(const __grid_consta
             uint64_t v[8];
             uint32_t m0 = 0, m1 = 0;
             if (c0 < a.c) {
-                float w[8];
+                uint64_t w[8];
                 sums_at(c0, v);
                 weights8(w, wx + c0);
 #pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = mul2(mul2(v[j], r), w[j]);
+                if (a.x) {
+                    const MapRows<T> to((T *)a.x, px, c0, a.c, a.hw);
+                    to.store4(0, {v[0], v[1], v[2], v[3]});
+                    to.store4(4, {v[4], v[5], v[6], v[7]});
+                }
+#pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    v[j] = mul2(mul2(v[j], r), pair_of(w[j], w[j]));
                     float x, y;
                     halves(v[j], x, y);
                     m0 = max(m0, abs_bits(x));
                     m1 = max(m1, abs_bits(y));
-                    if (a.x && c0 + j < a.c) px.store((T *)a.x, (long long)(c0 + j) * a.hw, v[j]);
                 }
             }
             if (a.codes.codes) {
-                constexpr int kBlockWarps = 8 * kBlock / M::kStep;                 // warps whose slices are a block of 128
+                constexpr int kBlockWarps = kPx == 64 ? 8 : 8 * kBlock / M::kStep; // warps whose slices are a block of 128 (tiles of 64 pixels: up to 64 channels)
 #pragma unroll
                 for (int d = M::kPairs; d < 32; d *= 2) {
                     m0 = max(m0, __shfl_xor_sync(0xffffffffu, m0, d));
@@ -1125,67 +1185,76 @@ __device__ __forceinline__ int sum8_over_lanes(float (&v)[8], int lane)
 }
 
 template <typename T, int kPx>
-__global__ void __launch_bounds__(256) norm_maps_grad_tile_kernel(const __grid_constant__ NormGradArgs a, int vec, int pairs)
+__global__ void __launch_bounds__(256, 2) norm_maps_grad_tile_kernel(const __grid_constant__ NormGradArgs a, int vec, int pairs)
 {
     using M = MapTile<T, kPx>;
     extern __shared__ __align__(16) unsigned char s_tile[];   // sums over the pixels [2][c8], after times the channels' gate, before; s, dx, y, ds, gate [c8][kPx]
     __shared__ float2 s_part[kSums][8][M::kPairs];
     __shared__ float s_scale[8];
-    const int c8 = (a.c + 7) & ~7, plane = c8 * kPx;
-    float *const sums_y = reinterpret_cast<float *>(s_tile), *const sums_x = sums_y + c8, *const wy = sums_x + c8, *const wx = wy + c8;
-    T *const ss = reinterpret_cast<T *>(wx + c8), *const sx = ss + (a.before ? plane : 0), *const sy = sx + (a.before ? plane : 0);
+    const int c8 = (a.c + 7) & ~7, plane = M::values(c8);
+    uint64_t *const wy = reinterpret_cast<uint64_t *>(s_tile), *const wx = wy + c8;
+    float *const sums_y = reinterpret_cast<float *>(wx + c8), *const sums_x = sums_y + c8;
+    T *const ss = reinterpret_cast<T *>(sums_x + c8), *const sx = ss + (a.before ? plane : 0), *const sy = sx + (a.before ? plane : 0);
     T *const sd = sy + (a.y ? plane : 0), *const sg = sd + (a.ds ? plane : 0);
     chain_next();
     chain_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pair = lane % M::kPairs, slice = warp * M::kSubs + lane / M::kPairs;
-    for (int i = threadIdx.x; i < c8; i += 256) {
-        sums_y[i] = sums_x[i] = 0.f;
-        wy[i] = i < a.c ? (a.after ? a.after[i] : 1.f) * (a.gate ? a.gate[i] : 1.f) : 0.f;
-        wx[i] = i < a.c && a.before ? a.before[i] : 0.f;
-    }
-    const int inputs = (a.before ? 2 : 0) + (a.y != nullptr) + (a.ds != nullptr) + (a.gate_map != nullptr);
-    for (int i = threadIdx.x; i < inputs * (c8 - a.c) * kPx; i += 256) {           // channels that there are not
-        const int ch = a.c + i / kPx % (c8 - a.c);
-        ss[(i / (kPx * (c8 - a.c))) * plane + M::row(ch) + i % kPx] = T(0.f);
-    }
+    fill_weights(wy, wx, a.after, a.gate, a.before, a.c, c8);
+    for (int i = threadIdx.x; i < 2 * c8; i += 256) sums_y[i] = 0.f;
+    zero_rows<M>(ss, (a.before ? 2 : 0) + (a.y != nullptr) + (a.ds != nullptr) + (a.gate_map != nullptr), plane, a.c, c8, kPx);
     const float scale = a.y && a.scale ? *a.scale : 1.f;
     uint64_t sum_scale = 0ull;
     const long long tiles = (a.pixels + kPx - 1) / kPx;
     for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const long long p0 = tile * kPx;
-        const MapPixels px(p0 + 2 * pair, a.pixels, a.c, a.hw, pairs);
+        const uint32_t p0 = (uint32_t)tile * kPx, pixels = (uint32_t)a.pixels;
+        const MapPixels px(p0 + 2 * pair, pixels, a.c, a.hw, pairs);
         __syncthreads();                                      // the last tile's readers
         if (a.before) {
-            M::fill(ss, (const T *)a.s, p0, a.pixels, a.c, a.hw, vec);
-            M::fill(sx, (const T *)a.dx, p0, a.pixels, a.c, a.hw, vec);
+            M::fill(ss, (const T *)a.s, p0, pixels, a.c, a.hw, vec);
+            M::fill(sx, (const T *)a.dx, p0, pixels, a.c, a.hw, vec);
         }
-        if (a.y) M::fill(sy, (const T *)a.y, p0, a.pixels, a.c, a.hw, vec);
-        if (a.ds) M::fill(sd, (const T *)a.ds, p0, a.pixels, a.c, a.hw, vec);
-        if (a.gate_map) M::fill(sg, (const T *)a.gate_map, p0, a.pixels, a.c, a.hw, vec);
+        if (a.y) M::fill(sy, (const T *)a.y, p0, pixels, a.c, a.hw, vec);
+        if (a.ds) M::fill(sd, (const T *)a.ds, p0, pixels, a.c, a.hw, vec);
+        if (a.gate_map) M::fill(sg, (const T *)a.gate_map, p0, pixels, a.c, a.hw, vec);
         sm100::cp_async_wait_all();
         __syncthreads();
         uint64_t sums[kSums] = {0ull, 0ull, 0ull, 0ull, 0ull, 0ull};
         for (int c0 = slice * 8; c0 < a.c; c0 += M::kStep) {
-            float w[8], b[8];
+            const T *const s = M::eight(ss, c0, pair), *const x = M::eight(sx, c0, pair), *const y = M::eight(sy, c0, pair), *const d = M::eight(sd, c0, pair),
+                    *const g = M::eight(sg, c0, pair);
+            uint64_t w[8], b[8];
             weights8(w, wy + c0);
             weights8(b, wx + c0);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                uint64_t s = 0ull, t = 0ull;
-                if (a.before) {
-                    s = M::load(ss, c0 + j, pair);
-                    t = mul2(M::load(sx, c0 + j, pair), pair_of(b[j], b[j]));
-                    sums[0] = fma2(s, s, sums[0]);
-                    sums[1] = fma2(t, s, sums[1]);
-                }
+            for (int h = 0; h < 8; h += 4) {
+                uint64_t sv[4] = {0ull, 0ull, 0ull, 0ull}, tv[4] = {0ull, 0ull, 0ull, 0ull};
+                if (a.before)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        sv[j] = M::load(s, h + j);
+                        tv[j] = mul2(M::load(x, h + j), b[h + j]);
+                        sums[0] = fma2(sv[j], sv[j], sums[0]);
+                        sums[1] = fma2(tv[j], sv[j], sums[1]);
+                    }
                 if (a.y) {
-                    const uint64_t y = M::load(sy, c0 + j, pair);
-                    uint64_t gy = mul2(y, pair_of(w[j], w[j]));
-                    if (a.gate_map) gy = mul2(gy, M::load(sg, c0 + j, pair));
-                    sums[2] = fma2(y, y, sums[2]);
-                    if (a.ds) sums[3] = fma2(M::load(sd, c0 + j, pair), gy, sums[3]);
-                    sums[4] = fma2(t, gy, sums[4]);
-                    sums[5] = fma2(s, gy, sums[5]);
+                    uint64_t gy[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint64_t yv = M::load(y, h + j);
+                        gy[j] = mul2(yv, w[h + j]);
+                        sums[2] = fma2(yv, yv, sums[2]);
+                    }
+                    if (a.gate_map)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) gy[j] = mul2(gy[j], M::load(g, h + j));
+                    if (a.ds)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) sums[3] = fma2(M::load(d, h + j), gy[j], sums[3]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        sums[4] = fma2(tv[j], gy[j], sums[4]);
+                        sums[5] = fma2(sv[j], gy[j], sums[5]);
+                    }
                 }
             }
         }
@@ -1215,40 +1284,61 @@ __global__ void __launch_bounds__(256) norm_maps_grad_tile_kernel(const __grid_c
         const uint64_t r = pair_of(f0.r, f1.r), r3m = pair_of(-f0.r3m, -f1.r3m), q = pair_of(f0.q, f1.q), scale_q = pair_of(scale * f0.q, scale * f1.q);
         const uint64_t mean_q = pair_of(-f0.mean * f0.q * f0.q, -f1.mean * f1.q * f1.q);
         for (int c0 = slice * 8; c0 - slice * 8 < a.c; c0 += M::kStep) {           // (the same for all lanes: their sums go together)
-            float sum_y[8], sum_x[8], w[8], b[8];
+            float sum_y[8], sum_x[8];
             const bool some = c0 < a.c;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum_y[j] = sum_x[j] = 0.f;
             if (some) {
+                const T *const s = M::eight(ss, c0, pair), *const x = M::eight(sx, c0, pair), *const y = M::eight(sy, c0, pair), *const dd = M::eight(sd, c0, pair),
+                        *const g = M::eight(sg, c0, pair);
+                const MapRows<T> to_h((T *)a.dh, px, c0, a.c, a.hw), to_y((T *)a.dy, px, c0, a.c, a.hw), to_g((T *)a.dgate_map, px, c0, a.c, a.hw);
+                uint64_t w[8], b[8];
                 weights8(w, wy + c0);
                 weights8(b, wx + c0);
-            }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                sum_y[j] = sum_x[j] = 0.f;
-                if (!some) continue;
-                const long long to = (long long)(c0 + j) * a.hw;
-                const bool there = c0 + j < a.c;
-                uint64_t d = a.ds ? M::load(sd, c0 + j, pair) : 0ull;
-                float x, y;
-                if (a.before) {
-                    const uint64_t s = M::load(ss, c0 + j, pair), t = mul2(r, M::load(sx, c0 + j, pair));
-                    d = fma2(r3m, s, fma2(t, pair_of(b[j], b[j]), d));
-                    halves(mul2(t, s), x, y);
-                    sum_x[j] = x + y;
-                }
-                if (there) px.store((T *)a.dh, to, d);
-                if (a.y) {
-                    const uint64_t yy = M::load(sy, c0 + j, pair), ww = pair_of(w[j], w[j]), dw = mul2(d, ww);
-                    uint64_t dn = mul2(d, mul2(yy, q)), dwg = dw;
-                    if (a.gate_map) {
-                        const uint64_t g = M::load(sg, c0 + j, pair);
-                        dn = mul2(dn, g);
-                        dwg = mul2(dw, g);
-                        if (there) px.store((T *)a.dgate_map, to, mul2(scale_q, mul2(dw, yy)));
+                for (int h = 0; h < 8; h += 4) {
+                    uint64_t d[4] = {0ull, 0ull, 0ull, 0ull};
+                    float u, v;
+                    if (a.ds)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) d[j] = M::load(dd, h + j);
+                    if (a.before)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint64_t sv = M::load(s, h + j), tv = mul2(r, M::load(x, h + j));
+                            d[j] = fma2(r3m, sv, fma2(tv, b[h + j], d[j]));
+                            halves(mul2(tv, sv), u, v);
+                            sum_x[h + j] = u + v;
+                        }
+                    to_h.store4(h, d);
+                    if (a.y) {
+                        uint64_t yv[4], dw[4], dn[4], dwg[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            yv[j] = M::load(y, h + j);
+                            dw[j] = dwg[j] = mul2(d[j], w[h + j]);
+                            dn[j] = mul2(d[j], mul2(yv[j], q));
+                        }
+                        if (a.gate_map) {
+                            uint64_t dg[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const uint64_t gv = M::load(g, h + j);
+                                dn[j] = mul2(dn[j], gv);
+                                dwg[j] = mul2(dw[j], gv);
+                                dg[j] = mul2(scale_q, mul2(dw[j], yv[j]));
+                            }
+                            to_g.store4(h, dg);
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            sum_scale = fma2(dn[j], w[h + j], sum_scale);
+                            halves(dn[j], u, v);
+                            sum_y[h + j] = u + v;
+                            dwg[j] = fma2(yv[j], mean_q, mul2(scale_q, dwg[j]));
+                        }
+                        to_y.store4(h, dwg);
                     }
-                    sum_scale = fma2(dn, ww, sum_scale);
-                    halves(dn, x, y);
-                    sum_y[j] = x + y;
-                    if (there) px.store((T *)a.dy, to, fma2(yy, mean_q, mul2(scale_q, dwg)));
                 }
             }
             const int first = sum8_over_lanes<M::kPairs>(sum_y, lane);
@@ -1282,16 +1372,19 @@ __global__ void __launch_bounds__(256) norm_maps_grad_tile_kernel(const __grid_c
     }
 }
 
-// The blocks' sums, in their order: 32 channels a block, every eighth of the blocks' sums a warp.
-__global__ void __launch_bounds__(256) norm_vectors_kernel(NormGradArgs a, int blocks)
+// The blocks' sums, in their order: 32 channels a block, every kVectorWarps-th of the blocks' sums a warp (of up to 592: what it waits for is
+// memory, one sum after the other).
+constexpr int kVectorWarps = 32;
+__global__ void __launch_bounds__(kVectorWarps * 32) norm_vectors_kernel(NormGradArgs a, int blocks)
 {
-    __shared__ float s_sum[2][8][32];
+    __shared__ float s_sum[2][kVectorWarps][32];
     chain_next();
     chain_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, ch = blockIdx.x * 32 + lane;
     float vy = 0.f, vx = 0.f;
     if (ch < a.c)
-        for (int b = warp; b < blocks; b += 8) {
+        #pragma unroll 4
+        for (int b = warp; b < blocks; b += kVectorWarps) {
             vy += a.partial[(long long)b * 2 * a.c + ch];
             vx += a.partial[(long long)b * 2 * a.c + a.c + ch];
         }
@@ -1300,7 +1393,7 @@ __global__ void __launch_bounds__(256) norm_vectors_kernel(NormGradArgs a, int b
     __syncthreads();
     if (warp == 0 && ch < a.c) {
         vy = vx = 0.f;
-        for (int w = 0; w < 8; ++w) { vy += s_sum[0][w][lane]; vx += s_sum[1][w][lane]; }
+        for (int w = 0; w < kVectorWarps; ++w) { vy += s_sum[0][w][lane]; vx += s_sum[1][w][lane]; }
         const float scale = a.y && a.scale ? *a.scale : 1.f;
         if (a.dafter) a.dafter[ch] = scale * vy * (a.gate ? a.gate[ch] : 1.f);
         if (a.dgate) a.dgate[ch] = scale * vy * (a.after ? a.after[ch] : 1.f);
@@ -1369,7 +1462,8 @@ bool pixel_pairs(int hw, P... p)
     return hw % 2 == 0 && ((((uintptr_t)p) | ...) & (2 * sizeof(T) - 1)) == 0;
 }
 
-// Tile of a maps' kernel: as many pixels as fit, but no more than 16 while the tiles are fewer than two an SM; 0 where not even eight do.
+// Tile of a maps' kernel: as many pixels as fit, but no more than 16 while the tiles are fewer than two an SM, and 64 only of up to 64 channels,
+// which leave half of the warps idle with 32; 0 where not even eight fit.
 struct MapPlan {
     int px = 0;
     size_t smem = 0;
@@ -1379,10 +1473,10 @@ MapPlan plan_maps(int inputs, int vectors, int c, size_t size, long long pixels,
 {
     MapPlan m;
     const size_t c8 = (size_t)((c + 7) & ~7);
-    for (int px = 32; px >= 8; px /= 2) {
-        const size_t smem = c8 * (vectors * sizeof(float) + inputs * px * size);
+    for (int px = c <= 64 ? 64 : 32; px >= 8; px /= 2) {
+        const size_t rows = px * size < 128 ? 9 : 8, smem = c8 * vectors * sizeof(float) + inputs * (c8 / 8) * rows * px * size;
         if (smem + kTileStatic > kTileSm || (px > 16 && pixels <= 2ll * sms * px)) continue;
-        const long long fit = (long long)(kTileSm / (smem + kTileStatic)), tiles = (pixels + px - 1) / px, most = (fit < 4 ? fit : 4) * sms;
+        const long long fit = (long long)(kTileSm / (smem + kTileStatic)), tiles = (pixels + px - 1) / px, most = (fit < 3 ? fit : 3) * sms;
         m.px = px;
         m.smem = smem;
         m.blocks = tiles < most ? tiles : most;
@@ -1392,13 +1486,13 @@ MapPlan plan_maps(int inputs, int vectors, int c, size_t size, long long pixels,
 }
 MapPlan plan_grad_maps(const NormGradArgs &a, size_t size, int sms)
 {
-    return plan_maps((a.before ? 2 : 0) + (a.y != nullptr) + (a.ds != nullptr) + (a.gate_map != nullptr), 4, a.c, size, a.pixels, sms);
+    return plan_maps((a.before ? 2 : 0) + (a.y != nullptr) + (a.ds != nullptr) + (a.gate_map != nullptr), 6, a.c, size, a.pixels, sms);
 }
 
 template <auto kKernel, typename A>
 cudaError_t launch_maps(const A &a, const MapPlan &m, long long blocks, bool vec, bool pairs, cudaStream_t s)
 {
-    if (!allow_shared<kKernel>(a.device, kTileSm)) return cudaErrorInvalidValue;
+    if (!allow_shared<kKernel>(a.device, kTileSm - kTileStatic)) return cudaErrorInvalidValue;
     return launch_first(true, kKernel, dim3((unsigned int)blocks), dim3(256), m.smem, s, a, (int)vec, (int)pairs);
 }
 
@@ -1406,8 +1500,9 @@ template <typename T>
 tc_status norms(const NormArgs &a, cudaStream_t s)
 {
     if (a.hw > 1) {
-        const MapPlan m = plan_maps(1 + (a.y != nullptr) + (a.gate_map != nullptr), 2, a.c, sizeof(T), a.pixels, a.sms);
+        const MapPlan m = plan_maps(1 + (a.y != nullptr) + (a.gate_map != nullptr), 4, a.c, sizeof(T), a.pixels, a.sms);
         const bool vec = four_pixels<T>(a.hw, a.h, a.y, a.gate_map), pairs = pixel_pairs<T>(a.hw, a.sum, a.x);
+        if (m.px == 64) return launch_maps<norm_maps_tile_kernel<T, 64>>(a, m, m.blocks, vec, pairs, s) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
         if (m.px == 32) return launch_maps<norm_maps_tile_kernel<T, 32>>(a, m, m.blocks, vec, pairs, s) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
         if (m.px == 16) return launch_maps<norm_maps_tile_kernel<T, 16>>(a, m, m.blocks, vec, pairs, s) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
         if (m.px == 8) return launch_maps<norm_maps_tile_kernel<T, 8>>(a, m, m.blocks, vec, pairs, s) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
@@ -1452,7 +1547,8 @@ tc_status gradient(const NormGradArgs &a, int blocks, int sms, cudaStream_t s)
     if (blocks == 0) {                                        // no pixels: the vectors' gradients are zero
     } else if (const MapPlan m = plan_grad_maps(a, sizeof(T), sms); a.hw > 1 && m.px) {
         const bool vec = four_pixels<T>(a.hw, a.s, a.dx, a.y, a.ds, a.gate_map), pairs = pixel_pairs<T>(a.hw, a.dh, a.dy, a.dgate_map);
-        err = m.px == 32   ? launch_maps<norm_maps_grad_tile_kernel<T, 32>>(a, m, blocks, vec, pairs, s)
+        err = m.px == 64   ? launch_maps<norm_maps_grad_tile_kernel<T, 64>>(a, m, blocks, vec, pairs, s)
+              : m.px == 32 ? launch_maps<norm_maps_grad_tile_kernel<T, 32>>(a, m, blocks, vec, pairs, s)
               : m.px == 16 ? launch_maps<norm_maps_grad_tile_kernel<T, 16>>(a, m, blocks, vec, pairs, s)
                            : launch_maps<norm_maps_grad_tile_kernel<T, 8>>(a, m, blocks, vec, pairs, s);
     } else if (a.hw > 1) {
@@ -1467,7 +1563,7 @@ tc_status gradient(const NormGradArgs &a, int blocks, int sms, cudaStream_t s)
     else if (a.c <= 8192) err = launch_grad<T, 32>(a, blocks, s);
     else err = launch_grad_rows<T, 32, 2>(a, blocks, s);
     if (err != cudaSuccess) { cudaGetLastError(); return TC_ERR_CUDA; }
-    return launch_chained(blocks > 0, norm_vectors_kernel, dim3((unsigned int)((a.c + 31) / 32)), dim3(256), 0, s, a, blocks) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
+    return launch_chained(blocks > 0, norm_vectors_kernel, dim3((unsigned int)((a.c + 31) / 32)), dim3(kVectorWarps * 32), 0, s, a, blocks) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
 
 }  // namespace
