@@ -206,7 +206,6 @@ class Context(_Handle):
     def __init__(self, ptr: int, device: int):
         super().__init__(ptr)
         self.device = device
-        self.empty = None          # tensors without values that new ones are made from
 
 
 class Model(_Handle):
@@ -615,8 +614,8 @@ def tc_stats(ctx: Context, model: Model, cb: Codebook | None, x: torch.Tensor, *
 
 
 # ---- layers between coded maps ---------------------------------------------------------------
-# A single token's calls take the GPU a few microseconds, so the host's part is kept short: pointers are passed as addresses (a
-# ctypes pointer object costs 0.3 us), and buffers are made from an empty tensor of their type (1.0 us instead of torch.empty's 2.4).
+# A single token's calls take the GPU a few microseconds, so their arguments are read and checked, and their tensors made, by a compiled
+# module (binding_layers.cpp) instead of ctypes: a call's host time is 5 to 11 us with it and 10 to 23 without.
 
 @dataclass
 class Blocks:
@@ -643,113 +642,34 @@ class Blocks:
         return self.codes[:, :self.cols].float() * scales[:, :self.rows].t().repeat_interleave(128, 1)[:, :self.cols]
 
 
-def _empty(ctx: Context, dtype):
-    """An empty tensor on the context's device, to make others of its type from."""
-    if ctx.empty is None:
-        ctx.empty = {}
-    t = ctx.empty.get(dtype)
-    if t is None:
-        t = ctx.empty[dtype] = torch.empty(0, dtype=dtype, device=f"cuda:{ctx.device}")
-    return t
+_layers = None
 
 
-def _new_blocks(ctx: Context, rows: int, cols: int, square: bool):
-    """Blocks on the context's device, and their C structure."""
-    ld, tall = (cols + 15) // 16 * 16, (rows + 127) // 128
-    codes = _empty(ctx, torch.float8_e4m3fn).new_empty(rows, ld)
-    scales = _empty(ctx, torch.float32).new_empty((cols + 127) // 128, tall if square else tall * 128)
-    return Blocks(codes, scales, cols, square), _Blocks(codes.data_ptr(), scales.data_ptr(), ld, rows, cols, square)
-
-
-def _blocks(ctx: Context, b: Blocks) -> _Blocks:
-    codes, scales, cols, device = b.codes, b.scales, b.cols, ctx.device
-    if codes.dtype is not torch.float8_e4m3fn or scales.dtype is not torch.float32 or not codes.is_contiguous() or not scales.is_contiguous() or \
-            codes.get_device() != device or scales.get_device() != device:
-        raise ValueError("block matrices have contiguous float8_e4m3fn codes [rows, ld] and float32 scales on the context's device")
-    rows, ld = codes.shape
-    high, wide = scales.shape
-    tall = (rows + 127) // 128
-    if not 0 <= cols <= ld or high != (cols + 127) // 128 or wide != (tall if b.square else tall * 128):
-        raise ValueError("block matrix: codes, scales and cols do not belong together")
-    return _Blocks(codes.data_ptr(), scales.data_ptr(), ld, rows, cols, b.square)
-
-
-_ELSEWHERE = "expected tensors on the context's device"
-
-
-def _local(ctx: Context, x: torch.Tensor) -> _Tensor:
-    t = _tensor(x)
-    if x.get_device() != ctx.device:
-        raise ValueError(_ELSEWHERE)
-    return t
-
-
-def _vector(device: int, v, n: int, name: str) -> int | None:
-    if v is None:
-        return None
-    if v.dtype is not torch.float32 or v.numel() != n or v.get_device() != device or not v.is_contiguous():
-        raise ValueError(f"{name}: expected {n} contiguous float32 values on the context's device")
-    return v.data_ptr()
-
-
-def _like(v, h: torch.Tensor, device: int, name: str) -> int | None:
-    """The address of a tensor of h's shape and type."""
-    if v is None:
-        return None
-    if v.shape != h.shape or v.dtype is not h.dtype or v.get_device() != device or not v.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous tensor of the shape and type of the first, on the context's device")
-    return v.data_ptr() or 16                     # (a tensor without values has no address, but it is there)
+def _layer_calls():
+    global _layers
+    if _layers is None:
+        lib = load_library()
+        try:
+            from . import _layers as module
+        except ImportError as e:
+            raise ImportError(f"{_PKG}/_layers.so cannot be loaded ({e}): run `python -m paper_1905_10830_b200.build`") from e
+        module.init(*[C.cast(getattr(lib, name), C.c_void_p).value
+                      for name in ("tc_quantize_blocks", "tc_matmul_blocks", "tc_residual_norms", "tc_residual_norms_backward")], TcError, Blocks)
+        _layers = module
+    return _layers
 
 
 def tc_quantize_blocks(ctx: Context, x: torch.Tensor, *, rows: str = "pixels", square: bool = False, out=None):
     """Codes of `x` (N, C, H, W): a row for each pixel ("pixels", blocks along the channels), for each channel ("channels",
     blocks along the pixels), or "both" as a pair.  `out` reuses the Blocks of an earlier call."""
-    t = _local(ctx, x)
-    p = t.n * t.h * t.w
-    if rows == "pixels":
-        shapes = ((p, t.c),)
-    elif rows == "channels":
-        shapes = ((t.c, p),)
-    elif rows == "both":
-        shapes = ((p, t.c), (t.c, p))
-    else:
-        raise ValueError('rows: "pixels", "channels" or "both"')
-    if out is None:
-        made = [_new_blocks(ctx, r, c, square) for r, c in shapes]
-    else:
-        given = tuple(out) if rows == "both" else (out,)
-        if len(given) != len(shapes) or any(bool(b.square) != bool(square) for b in given):
-            raise ValueError("out: Blocks as this call returns them")
-        made = [(b, _blocks(ctx, b)) for b in given]
-    at = C.addressof(made[0][1])
-    pixels, channels = (at, C.addressof(made[1][1])) if rows == "both" else (at, None) if rows == "pixels" else (None, at)
-    _check(load_library().tc_quantize_blocks(ctx.ptr, C.addressof(t), pixels, channels, _tensor_stream(ctx.device)), "tc_quantize_blocks")
-    return (made[0][0], made[1][0]) if rows == "both" else made[0][0]
+    return (_layers or _layer_calls()).quantize(ctx.ptr.value, ctx.device, _tensor_stream(ctx.device), x, rows, square, out)
 
 
 def tc_matmul_blocks(ctx: Context, a: Blocks, b: Blocks, *, shape=None, dtype=torch.bfloat16, bias: torch.Tensor | None = None,
                      relu: bool = False, out: torch.Tensor | None = None) -> torch.Tensor:
     """Product of a's rows (the output's pixels) and b's rows (its channels), (N, O, H, W) with `shape` = (N, H, W), by default
     (rows of a, 1, 1); `bias` [O], `relu` on the result."""
-    ma, mb = _blocks(ctx, a), _blocks(ctx, b)
-    rows = mb.rows
-    if out is None and dtype in (torch.bfloat16, torch.float32):
-        n, h, w = (ma.rows, 1, 1) if shape is None else shape
-        out = _empty(ctx, dtype).new_empty(n, rows, h, w)
-        t = _Tensor(out.data_ptr(), n, rows, h, w, TC_BF16 if dtype is torch.bfloat16 else TC_F32)
-    elif out is None:
-        raise ValueError("dtype must be float32 or bfloat16")
-    else:
-        t = _local(ctx, out)
-    _check(load_library().tc_matmul_blocks(ctx.ptr, C.addressof(ma), C.addressof(mb), _vector(ctx.device, bias, rows, "bias"), relu, C.addressof(t),
-                                           _tensor_stream(ctx.device)), "tc_matmul_blocks")
-    return out
-
-
-def _norm_params(device: int, h: torch.Tensor, c: int, y, after, gate, scale, before, eps):
-    gate_map = gate is not None and gate.dim() == 4
-    return _NormParams(_like(y, h, device, "y"), _vector(device, after, c, "after"), None if gate_map else _vector(device, gate, c, "gate"),
-                       _like(gate, h, device, "gate") if gate_map else None, _vector(device, scale, 1, "scale"), _vector(device, before, c, "before"), eps)
+    return (_layers or _layer_calls()).matmul(ctx.ptr.value, ctx.device, _tensor_stream(ctx.device), a, b, shape, dtype, bias, relu, out)
 
 
 def tc_residual_norms(ctx: Context, h: torch.Tensor, y: torch.Tensor | None = None, *, after: torch.Tensor | None = None,
@@ -758,27 +678,7 @@ def tc_residual_norms(ctx: Context, h: torch.Tensor, y: torch.Tensor | None = No
     """(s, x): s = h + scale * gate * norm(y) * after, x = norm(s) * before, norms over the channels of each pixel.  x is a
     tensor like h, or with `blocks` its codes by pixels; without `before` it is None.  Without `y` s is h itself.  `gate` is
     [C], or a tensor like y."""
-    t = _local(ctx, h)
-    device, c = ctx.device, t.c
-    p = _norm_params(device, h, c, y, after, gate, scale, before, eps)
-    s, at_s, x, at_x, at_b = h, None, None, None, None
-    if y is not None:
-        if sum_out is None:
-            s = torch.empty_like(h)
-            at_s = s.data_ptr()
-        else:
-            s, at_s = sum_out, _like(sum_out, h, device, "sum_out")
-    if before is not None:
-        if blocks:
-            x, b = _new_blocks(ctx, t.n * t.h * t.w, c, False) if out is None else (out, _blocks(ctx, out))
-            at_b = C.addressof(b)
-        elif out is None:
-            x = torch.empty_like(h)
-            at_x = x.data_ptr()
-        else:
-            x, at_x = out, _like(out, h, device, "out")
-    _check(load_library().tc_residual_norms(ctx.ptr, C.addressof(t), C.addressof(p), at_s, at_x, at_b, _tensor_stream(device)), "tc_residual_norms")
-    return s, x
+    return (_layers or _layer_calls()).norms(ctx.ptr.value, ctx.device, _tensor_stream(ctx.device), h, y, after, gate, scale, before, eps, blocks, sum_out, out)
 
 
 class NormGrads(NamedTuple):
@@ -796,15 +696,4 @@ def tc_residual_norms_backward(ctx: Context, s: torch.Tensor, y: torch.Tensor | 
                                before: torch.Tensor | None = None, eps: float = 1e-6) -> NormGrads:
     """Gradients at the sum `s` that tc_residual_norms returned, from the gradients `dx` of x (None without `before`) and `ds` of s
     (None: zero)."""
-    t = _local(ctx, s)
-    device = ctx.device
-    p = _norm_params(device, s, t.c, y, after, gate, scale, before, eps)
-    at_dx, at_ds = _like(dx, s, device, "dx"), _like(ds, s, device, "ds")
-    dh = torch.empty_like(s)
-    dy, dafter, dgate, dscale, dbefore = [v if v is None else torch.empty_like(v) for v in (y, after, gate, scale, before)]
-    at = [v if v is None else v.data_ptr() for v in (dh, dy, dgate, dafter, dgate, dscale, dbefore)]
-    at[4 if p.gate_map else 2] = None
-    out = _NormGrads(*at)
-    _check(load_library().tc_residual_norms_backward(ctx.ptr, C.addressof(t), C.addressof(p), at_dx, at_ds, C.addressof(out), _tensor_stream(device)),
-           "tc_residual_norms_backward")
-    return NormGrads(dh, dy, dafter, dgate, dscale, dbefore)
+    return NormGrads._make((_layers or _layer_calls()).backward(ctx.ptr.value, ctx.device, _tensor_stream(ctx.device), s, dx, ds, y, after, gate, scale, before, eps))

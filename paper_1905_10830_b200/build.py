@@ -1,7 +1,8 @@
 """Builds the codec library (CUDA, sm_100a only) in-tree with nvcc.
 
 `python -m paper_1905_10830_b200.build` compiles every source under csrc/ into
-`paper_1905_10830_b200/libtc_b200.so`.  Objects are cached under `_build/` by mtime.
+`paper_1905_10830_b200/libtc_b200.so` and the layer calls' Python module into `_layers.so`.
+Objects are cached under `_build/` by mtime.
 """
 from __future__ import annotations
 
@@ -10,12 +11,14 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libtc_b200.so")
+LAYERS_SRC, LAYERS = os.path.join(PKG, "binding_layers.cpp"), os.path.join(PKG, "_layers.so")
 
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 COMMON = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
@@ -48,14 +51,35 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
+def build_layers(force: bool = False) -> str:
+    """The module of the layer calls, against this torch's headers; its libraries are loaded by `import torch`."""
+    newest = max(os.path.getmtime(LAYERS_SRC), os.path.getmtime(os.path.join(ROOT, "include", "tc.h")))
+    if not force and os.path.exists(LAYERS) and os.path.getmtime(LAYERS) >= newest:
+        return LAYERS
+    import torch
+    base = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(NVCC))
+    tmp = LAYERS + f".{os.getpid()}.tmp"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
+           "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(base, "include"), "-isystem", os.path.join(cuda, "include"),
+           LAYERS_SRC, "-o", tmp, "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-lc10"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"g++ failed for {LAYERS_SRC}:\n{res.stdout}\n{res.stderr}")
+    os.replace(tmp, LAYERS)
+    return LAYERS
+
+
 def build_library(force: bool = False, verbose: bool = False) -> str:
     os.makedirs(OBJ_DIR, exist_ok=True)
     if force:
         for f in glob.glob(os.path.join(OBJ_DIR, "*.o")):
             os.remove(f)
     srcs = _sources()
-    with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(srcs))) as pool:
+    with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(srcs) + 1)) as pool:
+        layers = pool.submit(build_layers, force)
         objs = list(pool.map(lambda s: _compile(s, verbose), srcs))
+        layers.result()
     if (not os.path.exists(LIB)) or any(os.path.getmtime(o) > os.path.getmtime(LIB) for o in objs):
         tmp = LIB + f".{os.getpid()}.tmp"
         subprocess.check_call([NVCC, "-shared", "-gencode", "arch=compute_100a,code=sm_100a",
