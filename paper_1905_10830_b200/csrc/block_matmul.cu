@@ -31,7 +31,9 @@ template <int kN> struct Shape {
     static constexpr int kEpiWarps = 4 * kSets, kProducer = kEpiWarps, kMma = kEpiWarps + 1;
     static constexpr int kThreads = (kEpiWarps + 2) * 32;
     static constexpr int kStageBytes = kStageA + kN * kBlockK;
-    static constexpr int kStages = kRing / kStageBytes > 10 ? 10 : kRing / kStageBytes;
+    // up to 64 columns (few tokens): rings of which two fit an SM; of clusters of eight with one block an SM not all find a place at a time
+    // (one row of 8192 by 2048: 15.0 us and 9.4)
+    static constexpr int kStages = (kN <= 64 ? 98304 : kRing) / kStageBytes;
     static constexpr int kBuffers = kN == 256 ? 2 : 4;        // of tensor memory
     static constexpr int kTmemCols = kN * kBuffers < 32 ? 32 : kN * kBuffers;
     static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes;
@@ -58,6 +60,7 @@ struct TileArgs {
     int shift_a, shift_b;             // 0: a scale for each row, 7: for each 128
     int group;                        // tile rows that are worked on together
     int swapped, cluster;             // cluster: the parts of a tile's length are a cluster's CTAs
+    int join_rows;                    // and a pixel's channels are neighbours in a row of the tile
     int out_channels, hw, relu, vec;
     int store_tma;                    // pairs: the output's rows leave by TMA copies
     const float *bias;
@@ -104,6 +107,26 @@ __device__ __forceinline__ void store_value(const TileArgs &a, int row, int col,
     if (a.bias) v += a.bias[o];
     if (a.relu && v < 0.f) v = 0.f;                           // (a NaN stays one: a comparison with it fails)
     put((T *)a.out, pixel_at(a, p) + (long long)o * a.hw, v);
+}
+
+// Four neighbouring channels of a pixel.
+template <typename T>
+__device__ __forceinline__ void store_four(const TileArgs &a, int row, int col, float (&v)[4])
+{
+    if (a.vec && col + 4 <= a.rows_b) {
+        __align__(16) T w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (a.bias) v[j] += a.bias[col + j];
+            if (a.relu && v[j] < 0.f) v[j] = 0.f;
+            put(w, j, v[j]);
+        }
+        T *const to = (T *)a.out + (long long)row * a.out_channels + col;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(w);
+        else *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(w);
+    } else
+#pragma unroll
+        for (int j = 0; j < 4; ++j) store_value<T>(a, row, col + j, v[j]);
 }
 
 // The sums of a thread's row and kCols columns from `col0` on, to the output.
@@ -236,7 +259,7 @@ struct ScaleRing {
 
 // kColumnScales: B has a scale for each row (a column of the tile), else one for each 128.
 template <typename T, int kN, bool kColumnScales>
-__global__ void __launch_bounds__(Shape<kN>::kThreads, 1)
+__global__ void __launch_bounds__(Shape<kN>::kThreads, kN <= 64 ? 2 : 1)
 block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b)
 {
     using S = Shape<kN>;
@@ -247,6 +270,7 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
     chain_next();
+    if (tid == S::kProducer * 32) { tensormap_prefetch(&map_a); tensormap_prefetch(&map_b); }
     if (tid == 0) {
         for (int s = 0; s < S::kStages; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
         for (int b = 0; b < S::kBuffers; ++b) { mbar_init(smem_u32(&s_tfull[b]), 1); mbar_init(smem_u32(&s_tempty[b]), S::kEpiWarps); }
@@ -350,14 +374,27 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
             }
             if (!alive) break;
             if (a.cluster) {
-                // this part's sums, [column][128 rows], in the ring, which the tensor cores are done with
-                float *dst = reinterpret_cast<float *>(smem_raw + (ring - smem_u32(smem_raw))) + set * S::kCols * kRowsM + row_in_tile;
+                // this part's sums in the ring, which the tensor cores are done with: [column][128 rows], or where a pixel's channels are neighbours
+                // [row][kN + 4 columns]
+                float *const parts = reinterpret_cast<float *>(smem_raw + (ring - smem_u32(smem_raw)));
+                if (a.join_rows) {
+                    float4 *dst = reinterpret_cast<float4 *>(parts + row_in_tile * (kN + 4) + set * S::kCols);
 #pragma unroll
-                for (int i = 0; i < S::kCols / 2; ++i) {
-                    float x, y;
-                    halves(sum[i], x, y);
-                    dst[(2 * i) * kRowsM] = x;
-                    dst[(2 * i + 1) * kRowsM] = y;
+                    for (int i = 0; i < S::kCols / 4; ++i) {
+                        float4 v;
+                        halves(sum[2 * i], v.x, v.y);
+                        halves(sum[2 * i + 1], v.z, v.w);
+                        dst[i] = v;
+                    }
+                } else {
+                    float *dst = parts + set * S::kCols * kRowsM + row_in_tile;
+#pragma unroll
+                    for (int i = 0; i < S::kCols / 2; ++i) {
+                        float x, y;
+                        halves(sum[i], x, y);
+                        dst[(2 * i) * kRowsM] = x;
+                        dst[(2 * i + 1) * kRowsM] = y;
+                    }
                 }
                 break;                                        // a CTA has one part
             }
@@ -384,20 +421,32 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
         tmem_dealloc(tmem_base, S::kTmemCols);
     }
     if (a.cluster) {
-        // The cluster's CTAs each add their share of the columns over all parts, in the parts' order.
-        cluster_sync();
-        const int u = blockIdx.x, rank = u % a.splits, share = (kN + a.splits - 1) / a.splits;
+        // The cluster's CTAs each add their share of the rows (columns) over all parts, in the parts' order, four values at a time.
+        const int u = blockIdx.x, rank = u % a.splits;
         const Unit t = unit_of(a, u);
-        const int first = rank * share, end = min(kN, first + share);
-        for (int i = first * kRowsM + tid; i < end * kRowsM; i += S::kThreads) {
-            const int row = t.tile_m * kRowsM + (i & (kRowsM - 1)), col = t.tile_n * kN + (i >> 7);
-            float v = 0.f;
-            for (int part = 0; part < a.splits; ++part) {
-                float x;
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(cluster_address(ring + 4u * (uint32_t)i, (uint32_t)part)));
-                v += x;
-            }
-            store_value<T>(a, row, col, v);
+        const int rows = min(kRowsM, a.rows_a - t.tile_m * kRowsM), cols = min(kN, a.rows_b - t.tile_n * kN);
+        const int lines = a.join_rows ? rows : cols, fours = ((a.join_rows ? cols : rows) + 3) / 4, share = (lines + a.splits - 1) / a.splits;
+        const int first = rank * share, count = (min(lines, first + share) - first) * fours;
+        const uint32_t pitch = 4u * (a.join_rows ? kN + 4 : kRowsM);
+        cluster_sync();
+        for (int i = tid; i < count; i += S::kThreads) {
+            const int line = first + i / fours, four = i - i / fours * fours;
+            const uint32_t at = ring + (uint32_t)line * pitch + 16u * (uint32_t)four;
+            float4 v[8];
+#pragma unroll
+            for (int part = 0; part < 8; ++part)
+                if (part < a.splits)
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[part].x), "=f"(v[part].y), "=f"(v[part].z), "=f"(v[part].w)
+                                 : "r"(cluster_address(at, (uint32_t)part)));
+            float r[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+            for (int part = 1; part < 8; ++part)
+                if (part < a.splits) { r[0] += v[part].x; r[1] += v[part].y; r[2] += v[part].z; r[3] += v[part].w; }
+            const int row = t.tile_m * kRowsM + (a.join_rows ? line : 4 * four), col = t.tile_n * kN + (a.join_rows ? 4 * four : line);
+            if (a.join_rows) store_four<T>(a, row, col, r);
+            else
+#pragma unroll
+                for (int j = 0; j < 4; ++j) store_value<T>(a, row + j, col, r[j]);
         }
         cluster_sync();                                       // this block's shared memory is read no more
     }
@@ -440,6 +489,7 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int rank = blockIdx.x & 1;                          // the cluster is two neighbours
     chain_next();
+    if (tid == kProducer * 32) { tensormap_prefetch(&map_a); tensormap_prefetch(&map_b); }
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
         for (int b = 0; b < kBuffers; ++b) { mbar_init(smem_u32(&s_tfull[b]), 1); mbar_init(smem_u32(&s_tempty[b]), 2 * kEpiWarps); }
@@ -739,6 +789,7 @@ tc_status tc_launch_matmul_blocks(const tc_ctx *ctx, const MatmulArgs &m, const 
     a.tiles_m = (ra.rows + rows_tile - 1) / rows_tile;
     a.group = plan.pairs ? 8 : 16;
     a.cluster = plan.cluster;
+    a.join_rows = m.hw == 1 && !plan.swapped;
     a.tiles_n = (rb.rows + plan.n - 1) / plan.n;
     a.scale_a = ra.m.scales;
     a.scale_b = rb.m.scales;

@@ -306,6 +306,10 @@ __device__ __forceinline__ void tma_load_2d(uint32_t smem_dst, const void *tenso
         : "memory");
 }
 
+__device__ __forceinline__ void tensormap_prefetch(const void *tensor_map)
+{
+    asm volatile("prefetch.tensormap [%0];" ::"l"(tensor_map) : "memory");
+}
 // The way back: a box from shared memory to the tensor (parts outside it are not written; no coordinate is negative).  The
 // shared memory may be written again after tma_store_wait_read.  Written by st.shared: fence_proxy_async_smem first.
 __device__ __forceinline__ void tma_store_2d(const void *tensor_map, int x, int y, uint32_t smem_src)
