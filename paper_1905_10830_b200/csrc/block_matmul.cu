@@ -8,7 +8,7 @@
 //
 // Large products: pairs of CTAs (cta_group::2) walk tiles of 256 x 256, each CTA with half the rows of both operands in its
 // shared memory.  With one CTA on a tile of 128 x 256 the operands' way from L2 bounds the kernel (48 KB a block and SM against 32).
-// Small ones: one CTA walks tiles of 128 rows x 16 to 256 columns; where tiles are fewer than SMs the sums' length is cut into
+// Small ones: one CTA walks tiles of 128 rows x 16 to 128 columns; where tiles are fewer than SMs the sums' length is cut into
 // parts, by the CTAs of a cluster that add through their shared memory, or, for very long sums, through a workspace.
 #include "block_codes.cuh"
 #include "sm100_ptx.cuh"
@@ -23,7 +23,7 @@ using namespace blk;
 constexpr int kBlockK = 128;
 constexpr int kRowsM = 128;
 constexpr int kStageA = kRowsM * kBlockK;
-constexpr int kRing = 196608;                                 // bytes of the ring at most
+constexpr int kBoxBytes = 4096;                               // what a warp turns on the way to the output: 32 rows of 128 bytes
 
 template <int kN> struct Shape {
     static constexpr int kSets = kN >= 128 ? 2 : 1;           // sets of four epilogue warps, each with its share of the columns
@@ -33,10 +33,11 @@ template <int kN> struct Shape {
     static constexpr int kStageBytes = kStageA + kN * kBlockK;
     // up to 64 columns (few tokens): rings of which two fit an SM; of clusters of eight with one block an SM not all find a place at a time
     // (one row of 8192 by 2048: 15.0 us and 9.4)
-    static constexpr int kStages = (kN <= 64 ? 98304 : kRing) / kStageBytes;
-    static constexpr int kBuffers = kN == 256 ? 2 : 4;        // of tensor memory
+    static constexpr int kStages = kN == 128 ? 5 : kN == 64 ? 3 : kN == 32 ? 4 : 5;
+    static constexpr bool kBoxes = kN >= 64;
+    static constexpr int kBuffers = 4;                        // of tensor memory
     static constexpr int kTmemCols = kN * kBuffers < 32 ? 32 : kN * kBuffers;
-    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes;
+    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + (kBoxes ? kEpiWarps * kBoxBytes : 0);
 };
 
 // Tiles of a pair of CTAs: 256 x 256, 128 rows of each operand a CTA.
@@ -44,10 +45,9 @@ namespace pair {
 constexpr int kN = 256, kRows = 256;
 constexpr int kStageBytes = 2 * kStageA, kStages = 5, kBuffers = 2, kTmemCols = 512;
 constexpr int kSets = 2, kCols = kN / kSets;
-constexpr int kStoreBytes = 4096;                             // a warp's box of a TMA store: 32 rows of 128 bytes
 constexpr int kEpiWarps = 8, kProducer = 8, kMma = 9;         // warps 10 and 11 only give registers away
 constexpr int kThreads = 12 * 32;
-constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpiWarps * kStoreBytes;
+constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpiWarps * kBoxBytes;
 // Registers: 384 threads are launched with 168 each; 256 x 216 + 128 x 72 is the same sum.
 }
 
@@ -62,7 +62,8 @@ struct TileArgs {
     int swapped, cluster;             // cluster: the parts of a tile's length are a cluster's CTAs
     int join_rows;                    // and a pixel's channels are neighbours in a row of the tile
     int out_channels, hw, relu, vec;
-    int store_tma;                    // pairs: the output's rows leave by TMA copies
+    int by_rows;                      // a row's columns are neighbours in the output, else the rows of a column are
+    int store_tma;                    // pairs: rows leave by TMA copies
     const float *bias;
     void *out;
     float *partial;                   // [unit][column][128 rows], where the length is split
@@ -129,68 +130,121 @@ __device__ __forceinline__ void store_four(const TileArgs &a, int row, int col, 
         for (int j = 0; j < 4; ++j) store_value<T>(a, row, col + j, v[j]);
 }
 
-// The sums of a thread's row and kCols columns from `col0` on, to the output.
+// The sums of a thread's row and kCols columns from `col0` on, a column at a time: where the lanes' rows are neighbours in the output.
 template <typename T, int kCols>
-__device__ __forceinline__ void store_row(const TileArgs &a, const uint64_t (&sum)[kCols / 2], int row, int col0)
+__device__ __forceinline__ void store_lanes(const TileArgs &a, const uint64_t (&sum)[kCols / 2], int row, int col0)
 {
     if (row >= a.rows_a) return;
-    T *const out = (T *)a.out;
-    const float floor_v = a.relu ? 0.f : __int_as_float((int)0xff800000u);
-    const int cols_here = min(kCols, a.rows_b - col0);
-    if (!a.swapped) {
-        long long dst = pixel_at(a, row) + (long long)col0 * a.hw;
-        if (a.vec && cols_here == kCols) {
-            constexpr int kPer = 16 / (int)sizeof(T);
+    const int cols = min(kCols, a.rows_b - col0);
+    const float *const bias = a.swapped ? nullptr : a.bias;
+    const float of_row = a.swapped && a.bias ? a.bias[row] : 0.f, floor_v = a.relu ? 0.f : __int_as_float((int)0xff800000u);
+    auto value = [&](int i, float v) {
+        v += of_row;
+        if (bias) v += bias[col0 + i];
+        return v < floor_v ? floor_v : v;                     // (a NaN stays one: a comparison with it fails)
+    };
+    const bool apart = a.swapped && a.hw > 1;                 // (few pixels: their places are looked up)
+    T *const to = (T *)a.out + (a.swapped ? (long long)row * a.hw + (apart ? 0 : (long long)col0 * a.out_channels) : pixel_at(a, row) + (long long)col0 * a.hw);
+    const int pitch = a.swapped ? a.out_channels : a.hw;
 #pragma unroll
-            for (int i = 0; i < kCols; i += kPer) {
-                float v[kPer];
-#pragma unroll
-                for (int j = 0; j < kPer; j += 2) {
-                    halves(sum[(i + j) / 2], v[j], v[j + 1]);
-                    if (a.bias) { v[j] += a.bias[col0 + i + j]; v[j + 1] += a.bias[col0 + i + j + 1]; }
-                    // (a NaN stays one: a comparison with it fails)
-                    v[j] = v[j] < floor_v ? floor_v : v[j];
-                    v[j + 1] = v[j + 1] < floor_v ? floor_v : v[j + 1];
-                }
-                __align__(16) T w[kPer];
-#pragma unroll
-                for (int j = 0; j < kPer; ++j) put(w, j, v[j]);
-                *reinterpret_cast<uint4 *>(out + dst + i) = *reinterpret_cast<const uint4 *>(w);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < kCols / 2; ++i) {
-                float x, y;
-                halves(sum[i], x, y);
-                if (2 * i < cols_here) {
-                    if (a.bias) x += a.bias[col0 + 2 * i];
-                    put(out, dst + (long long)(2 * i) * a.hw, x < floor_v ? floor_v : x);
-                }
-                if (2 * i + 1 < cols_here) {
-                    if (a.bias) y += a.bias[col0 + 2 * i + 1];
-                    put(out, dst + (long long)(2 * i + 1) * a.hw, y < floor_v ? floor_v : y);
-                }
-            }
-        }
-    } else {
-        const float bias = a.bias ? a.bias[row] : 0.f;
-        const long long ch = (long long)row * a.hw;
-#pragma unroll
-        for (int i = 0; i < kCols / 2; ++i) {
-            float v[2];
-            halves(sum[i], v[0], v[1]);
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                if (2 * i + j < cols_here) {
-                    const float x = v[j] + bias;
-                    put(out, ch + pixel_at(a, col0 + 2 * i + j), x < floor_v ? floor_v : x);
-                }
-        }
+    for (int i = 0; i < kCols / 2; ++i) {
+        float x, y;
+        halves(sum[i], x, y);
+        if (2 * i < cols) put(to, apart ? pixel_at(a, col0 + 2 * i) : (long long)(2 * i) * pitch, value(2 * i, x));
+        if (2 * i + 1 < cols) put(to, apart ? pixel_at(a, col0 + 2 * i + 1) : (long long)(2 * i + 1) * pitch, value(2 * i + 1, y));
     }
 }
 
-__device__ __forceinline__ void tmem_ld(uint32_t at, uint32_t (&r)[16]) { tmem_ld_32x32b_x16(at, r); }
-__device__ __forceinline__ void tmem_ld(uint32_t at, uint32_t (&r)[32]) { tmem_ld_32x32b_x32(at, r); }
+// Where a row's columns are neighbours in the output a warp turns them in shared memory: a box of 32 rows x 128 bytes, 16-byte pieces
+// exchanged by XOR with the row.  (Stored by their threads, 16 bytes or a value at a time, each store meets 32 rows: 2000x1000 to 1000 took 14 us
+// and BOXES.)
+template <typename T> constexpr int kBoxCols = 128 / (int)sizeof(T);
+// Two neighbouring columns' values, with bias and activation.
+__device__ __forceinline__ void finish(const TileArgs &a, uint64_t v, int row, int col, float &x, float &y)
+{
+    halves(v, x, y);
+    if (a.bias) {
+        x += a.bias[a.swapped ? min(row, a.rows_a - 1) : min(col, a.rows_b - 1)];
+        y += a.bias[a.swapped ? min(row, a.rows_a - 1) : min(col + 1, a.rows_b - 1)];
+    }
+    if (a.relu) {                                             // (a NaN stays one: a comparison with it fails)
+        x = x < 0.f ? 0.f : x;
+        y = y < 0.f ? 0.f : y;
+    }
+}
+// A thread's row of the box from the sums of its columns c ...
+template <typename T>
+__device__ __forceinline__ void fill_box(const TileArgs &a, uint32_t box, const uint64_t *sum, int row, int col, int lane)
+{
+#pragma unroll
+    for (int piece = 0; piece < 8; ++piece) {
+        constexpr int kPer = 16 / (int)sizeof(T);
+        __align__(16) T w[kPer];
+#pragma unroll
+        for (int j = 0; j < kPer; j += 2) {
+            float x, y;
+            finish(a, sum[(piece * kPer + j) / 2], row, col + piece * kPer + j, x, y);
+            put(w, j, x);
+            put(w, j + 1, y);
+        }
+        const uint4 v = *reinterpret_cast<const uint4 *>(w);
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(box + lane * 128u + ((uint32_t)(piece ^ (lane & 7)) << 4)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
+                     : "memory");
+    }
+}
+// The box to the output, its lanes along the columns.
+template <typename T>
+__device__ __forceinline__ void store_box(const TileArgs &a, uint32_t box, int first_row, int col, int lane)
+{
+    const int rows = min(32, a.rows_a - first_row), cols = min(kBoxCols<T>, a.rows_b - col);
+    T *const out = (T *)a.out;
+    if (a.vec) {
+        const int piece = lane & 7;
+        if (piece * (16 / (int)sizeof(T)) < cols)             // (rows end at a multiple of 16 bytes)
+#pragma unroll
+            for (int r = lane >> 3; r < 32; r += 4)
+                if (r < rows) {
+                    uint4 v;
+                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                                 : "r"(box + (uint32_t)r * 128u + ((uint32_t)(piece ^ (r & 7)) << 4)));
+                    *reinterpret_cast<uint4 *>(out + (long long)(first_row + r) * a.out_channels + col + piece * (16 / (int)sizeof(T))) = v;
+                }
+        return;
+    }
+#pragma unroll
+    for (int h = 0; h < kBoxCols<T> / 32; ++h) {
+        const int c = 32 * h + lane;
+        if (c >= cols) continue;
+        const uint32_t byte = (uint32_t)c * sizeof(T);
+        T *to = out + (a.swapped ? pixel_at(a, col + c) + (long long)first_row * a.hw : (long long)first_row * a.out_channels + col + c);
+        const long long pitch = a.swapped ? a.hw : a.out_channels;
+#pragma unroll 8
+        for (int r = 0; r < rows; ++r, to += pitch) {
+            const uint32_t at = box + (uint32_t)r * 128u + (((byte >> 4) ^ (uint32_t)(r & 7)) << 4) + (byte & 15u);
+            if constexpr (sizeof(T) == 2) {
+                unsigned short v;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
+                *reinterpret_cast<unsigned short *>(to) = v;
+            } else {
+                uint32_t v;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at));
+                *reinterpret_cast<uint32_t *>(to) = v;
+            }
+        }
+    }
+}
+template <typename T, int kCols>
+__device__ __forceinline__ void store_by_rows(const TileArgs &a, uint32_t box, const uint64_t (&sum)[kCols / 2], int first_row, int col0, int lane)
+{
+    static_assert(kCols % kBoxCols<T> == 0, "whole boxes");
+#pragma unroll
+    for (int c = 0; c < kCols; c += kBoxCols<T>) {
+        __syncwarp();                                         // the last box's readers
+        fill_box<T>(a, box, sum + c / 2, first_row + lane, col0 + c, lane);
+        __syncwarp();
+        if (first_row < a.rows_a && col0 + c < a.rows_b) store_box<T>(a, box, first_row, col0 + c, lane);
+    }
+}
 
 // Adds a piece of a row's block, kN columns, times the row's scale and the columns'.
 template <int kN, bool kColumnScales>
@@ -211,7 +265,7 @@ __device__ __forceinline__ void add_scaled(uint64_t *sum, const uint32_t *r, uin
 
 // The scales of the next blocks on their way to shared memory, for one epilogue warp: of its rows (a lane's own), and either of its kCols
 // columns or the one they share.  Asked for three blocks ahead: they come from L2, in 400 ns and more, and with the registers of one
-// block ahead a block took as long as that (8192x4096 to 8192: 265 us and 205).
+// block ahead a block of few columns took as long as that (one row of 4096 by 4096: 11.2 us and 8.9).
 constexpr int kAhead = 3, kScaleSlots = kAhead + 1;
 template <int kCols, bool kColumnScales>
 struct ScaleRing {
@@ -409,7 +463,11 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
                 }
                 continue;
             }
-            store_row<T, S::kCols>(a, sum, row, col0);
+            if constexpr (S::kBoxes) {
+                if (a.by_rows) store_by_rows<T, S::kCols>(a, ring + S::kStages * S::kStageBytes + warp * kBoxBytes, sum, row - lane, col0, lane);
+                else store_lanes<T, S::kCols>(a, sum, row, col0);
+            } else
+                store_lanes<T, S::kCols>(a, sum, row, col0);
             __syncwarp();
         }
         if (!alive && lane == 0) tc_dev_set_status(a.status, TC_ERR_TIMEOUT);
@@ -556,8 +614,7 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
         const int set = warp >> 2, wq = warp & 3;
         ScaleRing<kCols, kColumnScales> scales;
         scales.slots = s_scales[warp];
-        const uint32_t box = ring + kStages * kStageBytes + warp * kStoreBytes;
-        const float floor_v = a.relu ? 0.f : __int_as_float((int)0xff800000u);
+        const uint32_t box = ring + kStages * kStageBytes + warp * kBoxBytes;
         uint32_t tempty[kBuffers];
 #pragma unroll
         for (int b = 0; b < kBuffers; ++b) tempty[b] = cluster_address(smem_u32(&s_tempty[b]), 0);
@@ -566,7 +623,7 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
         bool alive = true;
         // With scales for the columns a thread reads the fragments' layout, four rows and every fourth pair of columns: 32
         // columns' scales, where a row's thread has 128 to fetch, which shared memory's 128 bytes a cycle do not give in a block's time
-        // (4096x4096 over 16384: 442 us and 285).
+        // (4096x4096 over 16384: 442 us and 391).
         const int i = lane >> 2, q = lane & 3;                // row 8 k + i, columns 8 g + 2 q and the next
         for (int u = blockIdx.x >> 1; u < units && alive; u += step) {
             const Unit t = unit_of(a, u);
@@ -629,66 +686,43 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
                 if (++b == kBuffers) { b = 0; tphase ^= 1u; }
             }
             if (!alive) break;
-            // Two neighbouring columns' values, with bias and activation.
-            auto finish = [&](uint64_t v, int col, float &x, float &y) {
-                halves(v, x, y);
-                if (a.bias) { x += a.bias[min(col, a.rows_b - 1)]; y += a.bias[min(col + 1, a.rows_b - 1)]; }
-                x = x < floor_v ? floor_v : x;                // (a NaN stays one: a comparison with it fails)
-                y = y < floor_v ? floor_v : y;
-            };
-            if (a.store_tma) {
-                // 32 rows of 128 bytes at a time, 16-byte pieces exchanged by XOR with the row as the copy expects them
-                constexpr int kPer = 128 / (int)sizeof(T);
+            if (a.by_rows) {
 #pragma unroll
-                for (int c = 0; c < kCols; c += kPer) {
-                    if (lane == 0) tma_store_wait_read();
-                    __syncwarp();
+                for (int c = 0; c < kCols; c += kBoxCols<T>) {
+                    if (a.store_tma && lane == 0) tma_store_wait_read();
+                    __syncwarp();                             // the last box's readers
                     if constexpr (kColumnScales) {
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
 #pragma unroll
-                            for (int g = 0; g < kPer / 8; ++g) {
+                            for (int g = 0; g < kBoxCols<T> / 8; ++g) {
                                 float x, y;
-                                finish(sum[k * 16 + c / 8 + g], col0 + c + 8 * g + 2 * q, x, y);
+                                finish(a, sum[k * 16 + c / 8 + g], first_row + 8 * k + i, col0 + c + 8 * g + 2 * q, x, y);
                                 const uint32_t byte = (uint32_t)(8 * g + 2 * q) * sizeof(T), to = box + (uint32_t)(8 * k + i) * 128u + (((byte >> 4) ^ i) << 4) + (byte & 15u);
                                 if constexpr (sizeof(T) == 4) asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(x), "f"(y) : "memory");
                                 else asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(pack_bf16(x, y)) : "memory");
                             }
-                    } else {
-#pragma unroll
-                        for (int piece = 0; piece < 8; ++piece) {
-                            __align__(16) T w[kPer / 8];
-#pragma unroll
-                            for (int j = 0; j < kPer / 8; j += 2) {
-                                const int k = c + piece * (kPer / 8) + j;
-                                float x, y;
-                                finish(sum[k / 2], col0 + k, x, y);
-                                put(w, j, x);
-                                put(w, j + 1, y);
-                            }
-                            const uint4 v = *reinterpret_cast<const uint4 *>(w);
-                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(box + lane * 128u + ((uint32_t)(piece ^ (lane & 7)) << 4)), "r"(v.x), "r"(v.y),
-                                         "r"(v.z), "r"(v.w) : "memory");
-                        }
-                    }
-                    fence_proxy_async_smem();
+                    } else
+                        fill_box<T>(a, box, sum + c / 2, first_row + lane, col0 + c, lane);
+                    if (a.store_tma) fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0 && first_row < a.rows_a && col0 + c < a.rows_b) tma_store_2d(&map_out, col0 + c, first_row, box);
+                    if (first_row < a.rows_a && col0 + c < a.rows_b) {
+                        if (!a.store_tma) store_box<T>(a, box, first_row, col0 + c, lane);
+                        else if (lane == 0) tma_store_2d(&map_out, col0 + c, first_row, box);
+                    }
                 }
             } else if constexpr (kColumnScales) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int row = first_row + 8 * k + i;
+                for (int k = 0; k < 4; ++k)
 #pragma unroll
                     for (int n = 0; n < 16; ++n) {
                         float v[2];
                         halves(sum[k * 16 + n], v[0], v[1]);
-                        store_value<T>(a, row, col0 + 8 * n + 2 * q, v[0]);
-                        store_value<T>(a, row, col0 + 8 * n + 2 * q + 1, v[1]);
+                        store_value<T>(a, first_row + 8 * k + i, col0 + 8 * n + 2 * q, v[0]);
+                        store_value<T>(a, first_row + 8 * k + i, col0 + 8 * n + 2 * q + 1, v[1]);
                     }
-                }
             } else
-                store_row<T, kCols>(a, sum, first_row + lane, col0);
+                store_lanes<T, kCols>(a, sum, first_row + lane, col0);
             __syncwarp();
         }
         if (lane == 0) tma_store_wait();
@@ -733,7 +767,7 @@ tc_status launch(const tc_ctx *ctx, const TileArgs &a, bool pairs, int n, const 
     case 32: return cols ? launch_tiles<T, 32, true>(ctx, a, map_a, map_b, s) : TC_ERR_UNSUPPORTED;
     case 64: return cols ? launch_tiles<T, 64, true>(ctx, a, map_a, map_b, s) : launch_tiles<T, 64, false>(ctx, a, map_a, map_b, s);
     case 128: return cols ? launch_tiles<T, 128, true>(ctx, a, map_a, map_b, s) : launch_tiles<T, 128, false>(ctx, a, map_a, map_b, s);
-    default: return cols ? launch_tiles<T, 256, true>(ctx, a, map_a, map_b, s) : launch_tiles<T, 256, false>(ctx, a, map_a, map_b, s);
+    default: return TC_ERR_UNSUPPORTED;                       // (no plan has it: a tile's size is a kernel's)
     }
 }
 
@@ -744,19 +778,23 @@ MatmulPlan tc_plan_matmul(const MatmulArgs &a, int sm_count)
     MatmulPlan best;
     const int k_blocks = (a.cols + kBlockK - 1) / kBlockK;
     double best_cost = 0.0;
-    auto consider = [&](bool swapped, bool pairs, int n) {
+    auto consider = [&](bool swapped, bool pairs, int n, int splits) {
         const MatmulOperand &m = swapped ? a.channels : a.pixels, &c = swapped ? a.pixels : a.channels;
         const int rows = pairs ? pair::kRows : kRowsM, workers = pairs ? sm_count / 2 : sm_count;
         const long long tiles = (long long)((m.rows + rows - 1) / rows) * ((c.rows + n - 1) / n);
-        int splits = 1;
-        if (!pairs && tiles * 2 <= sm_count && k_blocks > 1) splits = (int)(sm_count / tiles < (k_blocks + 1) / 2 ? sm_count / tiles : (k_blocks + 1) / 2);
-        if (splits > 8 && splits < 17) splits = 8;
+        // Clusters run all at once: two blocks an SM with up to 64 columns, one with 128, of which clusters of more than four do not all
+        // find a place (512x512 over 8192: 22.6 us in eight parts, 14.2 in six).
         const bool cluster = splits > 1 && splits <= 8;
-        const long long rounds = (tiles * splits + workers - 1) / workers;
-        // a block's cycles: its operands from L2, or its sums; a tile's: its store
-        const double load = pairs ? 870 : (kRowsM + n) * 3.4, add = n * (c.square ? 3.2 : pairs ? 4.5 : 9.6);
-        const double cost = (double)rounds * ((double)((k_blocks + splits - 1) / splits) * (load > add ? load : add) + 600 + 8 * n) +
-                            (cluster ? 2000 + n * 16 : splits > 1 ? 6000 + (double)tiles * splits * n * 0.5 : 0);
+        const long long units = tiles * splits;
+        if (splits > 1 && (splits * 2 > k_blocks + 1 || (cluster ? units > (n <= 64 ? 2 : 1) * sm_count || (n > 64 && splits > 4) : units > sm_count))) return;
+        const double rounds = cluster ? std::max(1.0, (double)units / sm_count) : (double)((units + workers - 1) / workers);
+        // Cycles, fitted to the times of 130 forced plans: of a block (its operands from L2, or its sums), of a tile (its store, dearest where its
+        // columns lie apart in memory), of joining parts.
+        const double block = pairs ? (c.square ? 1100 : 1430) : std::max(600 + 3.4 * n, c.square ? 0.0 : 300 + 7.2 * n);
+        const bool by_rows = swapped ? a.hw > 1 : a.hw == 1;
+        const double store = pairs ? 6000 : (by_rows ? (n >= 64 ? 20.0 : 60.0) : 45.0) * n;
+        const double cost = rounds * ((double)((k_blocks + splits - 1) / splits) * block + 600 + store) +
+                            (cluster ? 5000 + n * 22 : splits > 1 ? 9000 + (double)units * n * 0.5 : 0);
         if (best.n == 0 || cost < best_cost) {
             best_cost = cost;
             best.swapped = swapped;
@@ -769,9 +807,10 @@ MatmulPlan tc_plan_matmul(const MatmulArgs &a, int sm_count)
         }
     };
     for (int swapped = 0; swapped < 2; ++swapped) {
-        for (int n = 16; n <= 256; n *= 2)
-            if (n >= 64 || (swapped && !a.pixels.square)) consider(swapped, false, n);
-        if (sm_count > 1) consider(swapped, true, pair::kN);
+        for (int n = 16; n <= 128; n *= 2)
+            if (n >= 64 || (swapped && !a.pixels.square))
+                for (const int splits : {1, 2, 3, 4, 6, 8, 16, 32, 64, 128}) consider(swapped, false, n, splits);
+        if (sm_count > 1) consider(swapped, true, pair::kN, 1);
     }
     if (k_blocks == 0) { best.splits = 0; best.pairs = best.cluster = false; best.workspace = 0; }
     return best;
@@ -789,7 +828,8 @@ tc_status tc_launch_matmul_blocks(const tc_ctx *ctx, const MatmulArgs &m, const 
     a.tiles_m = (ra.rows + rows_tile - 1) / rows_tile;
     a.group = plan.pairs ? 8 : 16;
     a.cluster = plan.cluster;
-    a.join_rows = m.hw == 1 && !plan.swapped;
+    a.by_rows = plan.swapped ? m.hw > 1 : m.hw == 1;
+    a.join_rows = a.by_rows && !plan.swapped;
     a.tiles_n = (rb.rows + plan.n - 1) / plan.n;
     a.scale_a = ra.m.scales;
     a.scale_b = rb.m.scales;
