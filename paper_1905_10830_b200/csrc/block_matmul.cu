@@ -48,7 +48,8 @@ constexpr int kSets = 2, kCols = kN / kSets;
 constexpr int kEpiWarps = 8, kProducer = 8, kMma = 9;         // warps 10 and 11 only give registers away
 constexpr int kThreads = 12 * 32;
 constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpiWarps * kBoxBytes;
-// Registers: 384 threads are launched with 168 each; 256 x 216 + 128 x 72 is the same sum.
+// Registers: 384 threads are launched with 168 each; 256 x 224 + 128 x 56 is the same sum, and so is 256 x 216 + 128 x 72
+// (the kernel with scales for the columns: 4096x4096 over 16384 takes 477 us with the first and 441 with the second).
 }
 
 struct TileArgs {
@@ -61,7 +62,8 @@ struct TileArgs {
     int group;                        // tile rows that are worked on together
     int swapped, cluster;             // cluster: the parts of a tile's length are a cluster's CTAs
     int join_rows;                    // and a pixel's channels are neighbours in a row of the tile
-    int out_channels, hw, relu, vec;
+    int out_channels, hw, relu;
+    int vec;                          // bytes of a store by rows, 0: values one by one
     int by_rows;                      // a row's columns are neighbours in the output, else the rows of a column are
     int store_tma;                    // pairs: rows leave by TMA copies
     const float *bias;
@@ -114,7 +116,7 @@ __device__ __forceinline__ void store_value(const TileArgs &a, int row, int col,
 template <typename T>
 __device__ __forceinline__ void store_four(const TileArgs &a, int row, int col, float (&v)[4])
 {
-    if (a.vec && col + 4 <= a.rows_b) {
+    if (a.vec == 16 && !a.swapped && a.hw == 1 && col + 4 <= a.rows_b) {
         __align__(16) T w[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -130,19 +132,40 @@ __device__ __forceinline__ void store_four(const TileArgs &a, int row, int col, 
         for (int j = 0; j < 4; ++j) store_value<T>(a, row, col + j, v[j]);
 }
 
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+// Bias and activation, in a pass of their own: the stores, of which a warp's time between two tiles consists, stay short.  The j-th pair is of
+// row and column place(j).
+template <int kPairs, typename F>
+__device__ __forceinline__ void finish(const TileArgs &a, uint64_t (&sum)[kPairs], F place)
+{
+    if (a.bias) {
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) {
+            const int2 at = place(j);
+            const int last = a.out_channels - 1, o = a.swapped ? at.x : at.y;
+            sum[j] = add2(sum[j], pair_of(a.bias[min(o, last)], a.bias[min(a.swapped ? o : o + 1, last)]));
+        }
+    }
+    if (a.relu)
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) {
+            float x, y;
+            halves(sum[j], x, y);
+            sum[j] = pair_of(x < 0.f ? 0.f : x, y < 0.f ? 0.f : y);            // (a NaN stays one: a comparison with it fails)
+        }
+}
+
 // The sums of a thread's row and kCols columns from `col0` on, a column at a time: where the lanes' rows are neighbours in the output.
 template <typename T, int kCols>
 __device__ __forceinline__ void store_lanes(const TileArgs &a, const uint64_t (&sum)[kCols / 2], int row, int col0)
 {
     if (row >= a.rows_a) return;
     const int cols = min(kCols, a.rows_b - col0);
-    const float *const bias = a.swapped ? nullptr : a.bias;
-    const float of_row = a.swapped && a.bias ? a.bias[row] : 0.f, floor_v = a.relu ? 0.f : __int_as_float((int)0xff800000u);
-    auto value = [&](int i, float v) {
-        v += of_row;
-        if (bias) v += bias[col0 + i];
-        return v < floor_v ? floor_v : v;                     // (a NaN stays one: a comparison with it fails)
-    };
     const bool apart = a.swapped && a.hw > 1;                 // (few pixels: their places are looked up)
     T *const to = (T *)a.out + (a.swapped ? (long long)row * a.hw + (apart ? 0 : (long long)col0 * a.out_channels) : pixel_at(a, row) + (long long)col0 * a.hw);
     const int pitch = a.swapped ? a.out_channels : a.hw;
@@ -150,31 +173,18 @@ __device__ __forceinline__ void store_lanes(const TileArgs &a, const uint64_t (&
     for (int i = 0; i < kCols / 2; ++i) {
         float x, y;
         halves(sum[i], x, y);
-        if (2 * i < cols) put(to, apart ? pixel_at(a, col0 + 2 * i) : (long long)(2 * i) * pitch, value(2 * i, x));
-        if (2 * i + 1 < cols) put(to, apart ? pixel_at(a, col0 + 2 * i + 1) : (long long)(2 * i + 1) * pitch, value(2 * i + 1, y));
+        if (2 * i < cols) put(to, apart ? pixel_at(a, col0 + 2 * i) : (long long)(2 * i) * pitch, x);
+        if (2 * i + 1 < cols) put(to, apart ? pixel_at(a, col0 + 2 * i + 1) : (long long)(2 * i + 1) * pitch, y);
     }
 }
 
 // Where a row's columns are neighbours in the output a warp turns them in shared memory: a box of 32 rows x 128 bytes, 16-byte pieces
 // exchanged by XOR with the row.  (Stored by their threads, 16 bytes or a value at a time, each store meets 32 rows: 2000x1000 to 1000 took 14 us
-// and BOXES.)
+// and 8.8.)
 template <typename T> constexpr int kBoxCols = 128 / (int)sizeof(T);
-// Two neighbouring columns' values, with bias and activation.
-__device__ __forceinline__ void finish(const TileArgs &a, uint64_t v, int row, int col, float &x, float &y)
-{
-    halves(v, x, y);
-    if (a.bias) {
-        x += a.bias[a.swapped ? min(row, a.rows_a - 1) : min(col, a.rows_b - 1)];
-        y += a.bias[a.swapped ? min(row, a.rows_a - 1) : min(col + 1, a.rows_b - 1)];
-    }
-    if (a.relu) {                                             // (a NaN stays one: a comparison with it fails)
-        x = x < 0.f ? 0.f : x;
-        y = y < 0.f ? 0.f : y;
-    }
-}
-// A thread's row of the box from the sums of its columns c ...
+// A thread's row of the box from the sums of its columns.
 template <typename T>
-__device__ __forceinline__ void fill_box(const TileArgs &a, uint32_t box, const uint64_t *sum, int row, int col, int lane)
+__device__ __forceinline__ void fill_box(uint32_t box, const uint64_t *sum, int lane)
 {
 #pragma unroll
     for (int piece = 0; piece < 8; ++piece) {
@@ -183,7 +193,7 @@ __device__ __forceinline__ void fill_box(const TileArgs &a, uint32_t box, const 
 #pragma unroll
         for (int j = 0; j < kPer; j += 2) {
             float x, y;
-            finish(a, sum[(piece * kPer + j) / 2], row, col + piece * kPer + j, x, y);
+            halves(sum[(piece * kPer + j) / 2], x, y);
             put(w, j, x);
             put(w, j + 1, y);
         }
@@ -198,17 +208,26 @@ __device__ __forceinline__ void store_box(const TileArgs &a, uint32_t box, int f
 {
     const int rows = min(32, a.rows_a - first_row), cols = min(kBoxCols<T>, a.rows_b - col);
     T *const out = (T *)a.out;
+    constexpr int kPer = 16 / (int)sizeof(T);
     if (a.vec) {
-        const int piece = lane & 7;
-        if (piece * (16 / (int)sizeof(T)) < cols)             // (rows end at a multiple of 16 bytes)
+        const int piece = lane & 7, c = piece * kPer;
+        if (c >= cols) return;                                // (rows, or four or eight pixels of a map, end at a multiple of a store)
+        const bool half = c + kPer / 2 >= cols;
+        const long long pitch = a.swapped ? a.hw : a.out_channels;
+        T *to = out + (a.swapped ? pixel_at(a, col + c) : (long long)(col + c)) + (long long)(first_row + (lane >> 3)) * pitch;
+        const long long second = a.swapped && !half ? pixel_at(a, col + c + kPer / 2) - pixel_at(a, col + c) : kPer / 2;
 #pragma unroll
-            for (int r = lane >> 3; r < 32; r += 4)
-                if (r < rows) {
-                    uint4 v;
-                    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                                 : "r"(box + (uint32_t)r * 128u + ((uint32_t)(piece ^ (r & 7)) << 4)));
-                    *reinterpret_cast<uint4 *>(out + (long long)(first_row + r) * a.out_channels + col + piece * (16 / (int)sizeof(T))) = v;
+        for (int r = lane >> 3; r < 32; r += 4, to += 4 * pitch)
+            if (r < rows) {
+                uint4 v;
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                             : "r"(box + (uint32_t)r * 128u + ((uint32_t)(piece ^ (r & 7)) << 4)));
+                if (a.vec == 16) *reinterpret_cast<uint4 *>(to) = v;
+                else {
+                    *reinterpret_cast<uint2 *>(to) = make_uint2(v.x, v.y);
+                    if (!half) *reinterpret_cast<uint2 *>(to + second) = make_uint2(v.z, v.w);
                 }
+            }
         return;
     }
 #pragma unroll
@@ -240,7 +259,7 @@ __device__ __forceinline__ void store_by_rows(const TileArgs &a, uint32_t box, c
 #pragma unroll
     for (int c = 0; c < kCols; c += kBoxCols<T>) {
         __syncwarp();                                         // the last box's readers
-        fill_box<T>(a, box, sum + c / 2, first_row + lane, col0 + c, lane);
+        fill_box<T>(box, sum + c / 2, lane);
         __syncwarp();
         if (first_row < a.rows_a && col0 + c < a.rows_b) store_box<T>(a, box, first_row, col0 + c, lane);
     }
@@ -402,7 +421,7 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
             uint64_t sum[S::kCols / 2];
 #pragma unroll
             for (int i = 0; i < S::kCols / 2; ++i) sum[i] = 0ull;
-            scales.start(a, row, col0, t.k_first, t.k_end, lane);
+            if (u == (int)blockIdx.x) scales.start(a, row, col0, t.k_first, t.k_end, lane);
             for (int kb = t.k_first; kb < t.k_end; ++kb) {
                 const float *const here = scales.next(kb, lane);
                 const float scale = kColumnScales ? here[lane] : here[lane] * here[32 + lane];
@@ -427,6 +446,10 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
                 if (++b == S::kBuffers) { b = 0; tphase ^= 1u; }
             }
             if (!alive) break;
+            if (u + (int)gridDim.x < units) {                 // the next unit's scales are on their way while this one is stored
+                const Unit next = unit_of(a, u + gridDim.x);
+                scales.start(a, next.tile_m * kRowsM + row_in_tile, next.tile_n * kN + set * S::kCols, next.k_first, next.k_end, lane);
+            }
             if (a.cluster) {
                 // this part's sums in the ring, which the tensor cores are done with: [column][128 rows], or where a pixel's channels are neighbours
                 // [row][kN + 4 columns]
@@ -463,6 +486,7 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
                 }
                 continue;
             }
+            finish(a, sum, [&](int j) { return make_int2(row, col0 + 2 * j); });
             if constexpr (S::kBoxes) {
                 if (a.by_rows) store_by_rows<T, S::kCols>(a, ring + S::kStages * S::kStageBytes + warp * kBoxBytes, sum, row - lane, col0, lane);
                 else store_lanes<T, S::kCols>(a, sum, row, col0);
@@ -563,7 +587,8 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
     const int units = a.tiles_m * a.tiles_n, step = gridDim.x >> 1;
 
     if (warp >= kEpiWarps) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if constexpr (kColumnScales) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        else asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp == kProducer && lane == 0) {
             int s = 0;
             long long issued = 0;
@@ -610,7 +635,8 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
         }
         __syncwarp();
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        if constexpr (kColumnScales) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        else asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int set = warp >> 2, wq = warp & 3;
         ScaleRing<kCols, kColumnScales> scales;
         scales.slots = s_scales[warp];
@@ -631,7 +657,7 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
             uint64_t sum[kCols / 2];                          // of a row's columns, or [row k][32 columns' pairs]
 #pragma unroll
             for (int j = 0; j < kCols / 2; ++j) sum[j] = 0ull;
-            scales.start(a, first_row + lane, col0, 0, a.k_blocks, lane);
+            if (u == (int)(blockIdx.x >> 1)) scales.start(a, first_row + lane, col0, 0, a.k_blocks, lane);
             for (int kb = 0; kb < a.k_blocks; ++kb) {
                 const float *const here = scales.next(kb, lane);
                 uint64_t scale2[kColumnScales ? 4 : 1];
@@ -686,6 +712,13 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
                 if (++b == kBuffers) { b = 0; tphase ^= 1u; }
             }
             if (!alive) break;
+            if (u + step < units) {                           // the next tile's scales are on their way while this one is stored
+                const Unit next = unit_of(a, u + step);
+                scales.start(a, next.tile_m * kRows + rank * kRowsM + wq * 32 + lane, next.tile_n * kN + set * kCols, 0, a.k_blocks, lane);
+            }
+            finish(a, sum, [&](int j) {
+                return kColumnScales ? make_int2(first_row + 8 * (j >> 4) + i, col0 + 8 * (j & 15) + 2 * q) : make_int2(first_row + lane, col0 + 2 * j);
+            });
             if (a.by_rows) {
 #pragma unroll
                 for (int c = 0; c < kCols; c += kBoxCols<T>) {
@@ -697,13 +730,13 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
 #pragma unroll
                             for (int g = 0; g < kBoxCols<T> / 8; ++g) {
                                 float x, y;
-                                finish(a, sum[k * 16 + c / 8 + g], first_row + 8 * k + i, col0 + c + 8 * g + 2 * q, x, y);
+                                halves(sum[k * 16 + c / 8 + g], x, y);
                                 const uint32_t byte = (uint32_t)(8 * g + 2 * q) * sizeof(T), to = box + (uint32_t)(8 * k + i) * 128u + (((byte >> 4) ^ i) << 4) + (byte & 15u);
                                 if constexpr (sizeof(T) == 4) asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(x), "f"(y) : "memory");
                                 else asm volatile("st.shared.u32 [%0], %1;" ::"r"(to), "r"(pack_bf16(x, y)) : "memory");
                             }
                     } else
-                        fill_box<T>(a, box, sum + c / 2, first_row + lane, col0 + c, lane);
+                        fill_box<T>(box, sum + c / 2, lane);
                     if (a.store_tma) fence_proxy_async_smem();
                     __syncwarp();
                     if (first_row < a.rows_a && col0 + c < a.rows_b) {
@@ -718,8 +751,11 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
                     for (int n = 0; n < 16; ++n) {
                         float v[2];
                         halves(sum[k * 16 + n], v[0], v[1]);
-                        store_value<T>(a, first_row + 8 * k + i, col0 + 8 * n + 2 * q, v[0]);
-                        store_value<T>(a, first_row + 8 * k + i, col0 + 8 * n + 2 * q + 1, v[1]);
+                        const int row = first_row + 8 * k + i, col = col0 + 8 * n + 2 * q;
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            if (row < a.rows_a && col + j < a.rows_b)
+                                put((T *)a.out, pixel_at(a, a.swapped ? col + j : row) + (long long)(a.swapped ? row : col + j) * a.hw, v[j]);
                     }
             } else
                 store_lanes<T, kCols>(a, sum, first_row + lane, col0);
@@ -743,7 +779,8 @@ tc_status launch_tiles(const tc_ctx *ctx, const TileArgs &a, const CUtensorMap &
     constexpr auto kernel = block_matmul_kernel<T, kN, kColumnScales>;
     if (!allow_shared<kernel>(ctx->device, Shape<kN>::kSmem)) return TC_ERR_CUDA;
     const long long units = (long long)a.tiles_m * a.tiles_n * a.splits;
-    const dim3 grid((unsigned int)(units < ctx->sm_count || a.cluster ? units : ctx->sm_count));
+    const long long most = (kN <= 64 ? 2 : 1) * ctx->sm_count;
+    const dim3 grid((unsigned int)(units < most || a.cluster ? units : most));
     return launch_first_cluster(a.cluster ? a.splits : 1, kernel, grid, dim3(Shape<kN>::kThreads), Shape<kN>::kSmem, s, a, map_a, map_b) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
 
@@ -792,7 +829,7 @@ MatmulPlan tc_plan_matmul(const MatmulArgs &a, int sm_count)
         // columns lie apart in memory), of joining parts.
         const double block = pairs ? (c.square ? 1100 : 1430) : std::max(600 + 3.4 * n, c.square ? 0.0 : 300 + 7.2 * n);
         const bool by_rows = swapped ? a.hw > 1 : a.hw == 1;
-        const double store = pairs ? 6000 : (by_rows ? (n >= 64 ? 20.0 : 60.0) : 45.0) * n;
+        const double store = splits > 1 ? 8 * n : by_rows ? (pairs ? 6000 : n >= 64 ? 25 * n : 60 * n) : pairs ? 30000 : n == 128 ? 110 * n : 180 * n;
         const double cost = rounds * ((double)((k_blocks + splits - 1) / splits) * block + 600 + store) +
                             (cluster ? 5000 + n * 22 : splits > 1 ? 9000 + (double)units * n * 0.5 : 0);
         if (best.n == 0 || cost < best_cost) {
@@ -841,7 +878,9 @@ tc_status tc_launch_matmul_blocks(const tc_ctx *ctx, const MatmulArgs &m, const 
     a.out_channels = m.channels.rows;
     a.hw = m.hw;
     a.relu = m.relu;
-    a.vec = m.hw == 1 && !plan.swapped && ((uintptr_t)m.out & 15u) == 0 && m.channels.rows % (m.dtype == TC_BF16 ? 8 : 4) == 0;
+    // bytes that a store by rows moves: neighbouring channels of a pixel, or pixels of a map
+    const int line = m.hw == 1 ? m.channels.rows : m.hw, size = m.dtype == TC_BF16 ? 2 : 4;
+    a.vec = !a.by_rows ? 0 : line * size % 16 == 0 && ((uintptr_t)m.out & 15u) == 0 ? 16 : line * size % 8 == 0 && ((uintptr_t)m.out & 7u) == 0 ? 8 : 0;
     a.bias = m.bias;
     a.out = m.out;
     a.partial = plan.workspace ? (float *)workspace : nullptr;
@@ -850,7 +889,7 @@ tc_status tc_launch_matmul_blocks(const tc_ctx *ctx, const MatmulArgs &m, const 
         CUtensorMap map_a, map_b, map_out{};
         if (!tc_tensor_map_codes(&map_a, ra.m.codes, ra.rows, m.cols, ra.m.ld, kRowsM) ||
             !tc_tensor_map_codes(&map_b, rb.m.codes, rb.rows, m.cols, rb.m.ld, plan.pairs ? kRowsM : plan.n)) return TC_ERR_CUDA;
-        a.store_tma = plan.pairs && a.vec && tc_tensor_map_rows(&map_out, m.out, m.dtype, a.rows_a, a.rows_b, 32);
+        a.store_tma = plan.pairs && a.vec == 16 && m.hw == 1 && tc_tensor_map_rows(&map_out, m.out, m.dtype, a.rows_a, a.rows_b, 32);
         const tc_status st = m.dtype == TC_BF16 ? launch<__nv_bfloat16>(ctx, a, plan.pairs, plan.n, map_a, map_b, map_out, s) : launch<float>(ctx, a, plan.pairs, plan.n, map_a, map_b, map_out, s);
         if (st != TC_OK || !a.partial) return st;
     }

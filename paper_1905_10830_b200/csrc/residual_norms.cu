@@ -551,7 +551,7 @@ struct MapRows {
     }
     __device__ __forceinline__ void store1of(int j, float x, float y) const
     {
-        T *const to = to0 + (uint32_t)(j * hw);
+        T *const to = to0 + (long long)j * hw;
         if (both) {
             if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t *>(to) = pack_bf16(x, y);
             else *reinterpret_cast<float2 *>(to) = make_float2(x, y);
@@ -569,7 +569,7 @@ struct MapRows {
         if (both && there >= 8) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                T *const to = to0 + (uint32_t)((j0 + j) * hw);
+                T *const to = to0 + (long long)(j0 + j) * hw;
                 if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t *>(to) = pack_bf16(x[j], y[j]);
                 else *reinterpret_cast<float2 *>(to) = make_float2(x[j], y[j]);
             }

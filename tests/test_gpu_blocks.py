@@ -157,7 +157,7 @@ def test_product(ctx, p, k, o, squares, dtype):
 
 
 @pytest.mark.parametrize("n,h,w,k,o", [(37, 7, 7, 320, 96), (3, 14, 14, 256, 257), (1, 5, 7, 64, 300), (700, 2, 3, 48, 16), (1, 1, 333, 96, 128), (2, 56, 56, 24, 144),
-                                       (40, 7, 7, 200, 1100)])
+                                       (40, 7, 7, 200, 1100), (30, 14, 14, 130, 200), (9, 16, 16, 64, 333), (70, 19, 19, 80, 48), (11, 2, 6, 300, 500)])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_product_into_maps(ctx, n, h, w, k, o, dtype):
     x = _values((n, k, h, w), 7, dtype)
