@@ -64,7 +64,7 @@ struct TileArgs {
 
 // The tile comes by asynchronous copies and its values are read from shared memory where they are needed, twice for the layout across:
 // with them in registers (96 a thread) two blocks fitted an SM, and a tile's memory time was hardly hidden (8192x4096, both layouts 38 us
-// and Q_BOTH; maps of 256x14x14 x 1024 56 and Q_MAPS).
+// and 33; maps of 256x14x14 x 1024 56 and 41).
 constexpr int kTileThreads = 256;
 template <typename T, bool kMaps, bool kSquare>
 __global__ void __launch_bounds__(kTileThreads, sizeof(T) == 2 ? 5 : 3) quantize_tile_kernel(const T *x, const __grid_constant__ TileArgs a, int vec)

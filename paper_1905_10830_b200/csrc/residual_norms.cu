@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32) norm_rows_ker
 // ---- rows on their way to shared memory ------------------------------------------------------
 // Long rows: a block walks rows gridDim.x apart, whose parts of all inputs one thread brings to a ring in shared memory by bulk
 // copies, several rows ahead, so that the memory is at work while the block waits for a row's sums (with a row's loads in
-// registers, and the vectors read again for each row: gradient of 16384x4096 297 us and RING_GRAD, forward 122 and RING_FWD).
+// registers, and the vectors read again for each row: gradient of 16384x4096 in bf16 297 us and 157, forward 122 and 106).
 constexpr int kRingInputs = 5, kRingStages = 8;
 constexpr size_t kRingSm = 200 * 1024;                        // of an SM's shared memory, for all its blocks' rings
 struct RowRing {
@@ -484,7 +484,7 @@ __global__ void __launch_bounds__(256) norm_maps_kernel(NormArgs a)
 }
 
 // The same with all channels of a tile of kPx pixels in shared memory, where they fit: each value is fetched once, many at a time, and
-// the vectors once a block (256x14x14 x 1024, bf16: 962 us and MAPS_FWD).  A lane has two pixels, whose values one instruction works on, and
+// the vectors once a block (256x14x14 x 1024, bf16: 962 us and 169).  A lane has two pixels, whose values one instruction works on, and
 // eight channels in a row of every kStep.
 constexpr size_t kTileSm = 220 * 1024, kTileStatic = 14 * 1024;       // of an SM's shared memory; what a block has beside its tile
 template <typename T, int kPx, int kWarps>
@@ -1226,7 +1226,6 @@ __global__ void __launch_bounds__(256) norm_maps_grad_kernel(NormGradArgs a)
     }
 }
 
-// The same with the inputs' tile in shared memory, as in the forward.
 // Sums of eight values over kLanes neighbouring lanes: a lane has those of values first .. first + 8 / kLanes (one at least; lanes of the same
 // value have the same).
 template <int kLanes>
@@ -1251,6 +1250,7 @@ __device__ __forceinline__ int sum8_over_lanes(float (&v)[8], int lane)
     return first;
 }
 
+// The same with the inputs' tile in shared memory, as in the forward.
 template <typename T, int kPx, int kWarps>
 __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) norm_maps_grad_tile_kernel(const __grid_constant__ NormGradArgs a, int vec, int pairs)
 {
@@ -1540,19 +1540,21 @@ bool pixel_pairs(int hw, P... p)
 }
 
 // Tile of a maps' kernel: as many pixels as fit, but no more than 16 while the tiles are fewer than two an SM, and 64 only of up to 64 channels,
-// which leave half of the warps idle with 32; 0 where not even eight fit.
+// which leave half of the warps idle with 32; 0 where not even eight fit.  `two`: rather tiles of which two fit an SM, the forward's (431x7x7 x 944
+// in bf16 181 us and 122, 60x28x28 x 512 in fp32 105 and 77; the gradient has no use of them: 256x14x14 x 1024 in bf16 290 us and 518).  Up to 32 channels
+// keep four warps busy: more blocks of those (437x20x20 x 25 in bf16, forward 24 us and 16, gradient 65 and 33).
 struct MapPlan {
     int px = 0, warps = 8;
     size_t smem = 0;
     long long blocks = 0;
 };
-MapPlan plan_maps(int inputs, int vectors, int c, size_t size, long long pixels, int sms, int warps_sm)
+MapPlan plan_maps(int inputs, int vectors, int c, size_t size, long long pixels, int sms, int warps_sm, bool two)
 {
     MapPlan m;
     const size_t c8 = (size_t)((c + 7) & ~7);
     for (int px = c <= 64 ? 64 : 32; px >= 8; px /= 2) {
         const size_t rows = px * size < 128 ? 9 : 8, smem = c8 * vectors * sizeof(float) + inputs * (c8 / 8) * rows * px * size;
-        if (smem + kTileStatic > kTileSm || (px > 16 && pixels <= 2ll * sms * px)) continue;
+        if (smem + kTileStatic > kTileSm || (px > 16 && pixels <= 2ll * sms * px) || (two && px > 8 && 2 * (smem + kTileStatic) > kTileSm)) continue;
         m.warps = px == 64 && c <= 32 ? 4 : 8;
         const long long fit = (long long)(kTileSm / (smem + kTileStatic * m.warps / 8)), held = warps_sm / m.warps, tiles = (pixels + px - 1) / px, most = (fit < held ? fit : held) * sms;
         m.px = px;
@@ -1564,7 +1566,7 @@ MapPlan plan_maps(int inputs, int vectors, int c, size_t size, long long pixels,
 }
 MapPlan plan_grad_maps(const NormGradArgs &a, size_t size, int sms)
 {
-    return plan_maps((a.before ? 2 : 0) + (a.y != nullptr) + (a.ds != nullptr) + (a.gate_map != nullptr), 6, a.c, size, a.pixels, sms, 16);
+    return plan_maps((a.before ? 2 : 0) + (a.y != nullptr) + (a.ds != nullptr) + (a.gate_map != nullptr), 6, a.c, size, a.pixels, sms, 16, false);
 }
 
 template <auto kKernel, typename A>
@@ -1578,7 +1580,7 @@ template <typename T>
 tc_status norms(const NormArgs &a, cudaStream_t s)
 {
     if (a.hw > 1) {
-        const MapPlan m = plan_maps(1 + (a.y != nullptr) + (a.gate_map != nullptr), 4, a.c, sizeof(T), a.pixels, a.sms, 24);
+        const MapPlan m = plan_maps(1 + (a.y != nullptr) + (a.gate_map != nullptr), 4, a.c, sizeof(T), a.pixels, a.sms, 24, true);
         const bool vec = four_pixels<T>(a.hw, a.h, a.y, a.gate_map), pairs = pixel_pairs<T>(a.hw, a.sum, a.x);
         if (m.px == 64 && m.warps == 4) return launch_maps<norm_maps_tile_kernel<T, 64, 4>>(a, m, m.blocks, vec, pairs, s) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
         if (m.px == 64) return launch_maps<norm_maps_tile_kernel<T, 64, 8>>(a, m, m.blocks, vec, pairs, s) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
@@ -1605,7 +1607,7 @@ cudaError_t launch_grad_rows(const NormGradArgs &a, int blocks, cudaStream_t s)
 }
 
 // With the ring of rows where there is one: two chunks a thread of bf16, whose unpacking and sums bound it (16384x4096 209 us with one
-// and 166); one of fp32, of whose rows two would not fit two blocks' rings.  Blocks of 512 threads an SM in all.
+// and 157); one of fp32, of whose rows two would not fit two blocks' rings.  Blocks of 512 threads an SM in all.
 constexpr int ring_chunks(int warps, int size) { return warps <= 2 ? 1 : warps > 16 ? warps / 16 : size == 2 ? 2 : 1; }
 // Rows of up to 256 kWarps channels.
 template <typename T, int kWarps>
