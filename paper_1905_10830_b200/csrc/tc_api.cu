@@ -1817,6 +1817,8 @@ constexpr int kMostNormChannels = 16384;                // a row's channels in t
 size_t element_size(int dtype) { return dtype == TC_BF16 ? 2 : 4; }
 bool aligned_tensor(const tc_tensor *t) { return valid_tensor(t) && ((uintptr_t)t->data & (element_size(t->dtype) - 1)) == 0; }
 long long pixels_of(const tc_tensor *t) { return (long long)t->n * t->h * t->w; }
+template <typename... P>
+bool aligned_to(size_t bytes, P... p) { return ((((uintptr_t)p) | ...) & (bytes - 1)) == 0; }
 
 bool valid_blocks(const tc_blocks *b)
 {
@@ -1856,9 +1858,7 @@ struct Ranges {
     }
 };
 
-// The parameters both directions share; `aligned`: of the tensors that are given, all others too.
-template <typename... P>
-bool aligned_to(size_t bytes, P... p) { return ((((uintptr_t)p) | ...) & (bytes - 1)) == 0; }
+// The parameters both directions share.
 bool valid_norm_params(const tc_tensor *h, const tc_norm_params *p)
 {
     if (!aligned_tensor(h) || !p || !(p->eps >= 0.f) || (!p->y && !p->before)) return false;
@@ -1899,7 +1899,7 @@ tc_status tc_quantize_blocks(tc_ctx *ctx, const tc_tensor *x, const tc_blocks *p
 
 tc_status tc_matmul_blocks(tc_ctx *ctx, const tc_blocks *a, const tc_blocks *b, const float *bias, int32_t relu, const tc_tensor *out, void *cuda_stream)
 {
-    if (!ctx || !valid_blocks(a) || !valid_blocks(b) || !aligned_tensor(out)) return TC_ERR_INVALID_ARG;
+    if (!ctx || !valid_blocks(a) || !valid_blocks(b) || !aligned_tensor(out) || !aligned_to(sizeof(float), bias)) return TC_ERR_INVALID_ARG;
     if (a->cols != b->cols || pixels_of(out) != a->rows || out->c != b->rows) return TC_ERR_INVALID_ARG;
     if (a->rows > kMostRows || b->rows > kMostRows || a->cols > kMostRows) return TC_ERR_UNSUPPORTED;
     Ranges ranges;

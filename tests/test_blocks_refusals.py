@@ -65,6 +65,7 @@ def test_matmul(lib, ctx):
                  (a, b, tensor(4, 16, 3, 1)), (a, b, tensor(8, 16, at=2 * AT)), (a, b, tensor(8, 16, at=AT + 1)), (a, blocks(16, 64, True, 3 * AT + 4), out)):
         assert call(*args) == INVALID
     assert call(a, b, out, bias=AT) == INVALID                                            # the bias in the output's memory
+    assert call(a, b, out, bias=5 * AT + 2) == INVALID
     assert call(blocks(0, 64), b, tensor(0, 16)) == OK
 
 
