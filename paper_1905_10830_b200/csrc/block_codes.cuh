@@ -40,11 +40,12 @@ __device__ __forceinline__ uint2 codes8(const float (&v)[8], float inv)
 {
     return make_uint2(codes4(v[0], v[1], v[2], v[3], inv), codes4(v[4], v[5], v[6], v[7], inv));
 }
-// Largest of a value over the 16 lanes of a half warp.
-__device__ __forceinline__ uint32_t max16(uint32_t v)
+// Largest of a value over kLanes neighbouring lanes.
+template <int kLanes>
+__device__ __forceinline__ uint32_t max_over(uint32_t v)
 {
 #pragma unroll
-    for (int d = 8; d; d >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, d));
+    for (int d = kLanes / 2; d; d >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, d));
     return v;
 }
 

@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(kRowThreads) quantize_rows_kernel(const T *x, 
     for (int i = 0; i < kInFlight; ++i) {
         float v[8];
         values8(raw[i], v);
-        const float scale = scale_of(max16(max8(raw[i])));
+        const float scale = scale_of(max_over<16>(max8(raw[i])));
         if (first + i * (kRowThreads / 16) >= items) continue;
         const int k = (int)kb[i] * kBlock + k_lane;
         if (k < cols) *reinterpret_cast<uint2 *>(out.codes + (long long)row[i] * out.ld + k) = codes8(v, __frcp_rn(scale));
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(kTileThreads, sizeof(T) == 2 ? 5 : 3) quantize
             const Raw8<T> raw = *reinterpret_cast<const Raw8<T> *>(&tile[r][k]);
             float v[8];
             values8(raw, v);
-            const float s = kSquare ? scale : scale_of(max16(max8(raw)));
+            const float s = kSquare ? scale : scale_of(max_over<16>(max8(raw)));
             if (r < rows && k < cols) {
                 *reinterpret_cast<uint2 *>(to) = codes8(v, __frcp_rn(s));
                 if (!kSquare && k == 0) a.along.scales[i0 / kBlock * a.along.scale_ld + o0 + r] = s;

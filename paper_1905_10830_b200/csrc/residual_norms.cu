@@ -23,7 +23,8 @@ using namespace blk;
 __device__ __forceinline__ float inv_sqrt(float v) { return rsqrtf(v); }       // (off by 2^-22 at most)
 
 // ---- single pixels (H W = 1): a pixel's channels are a row in memory ------------------------------
-// kWarps warps a row, kV chunks of eight channels a thread; rows of one warp share a block of eight.
+// kThreadsRow threads a row, kV chunks of eight channels a thread; rows of one warp share a block of eight, and aligned ones of up to 128 channels a
+// warp (a warp each, 200000x64 in bf16: 72 us and 20, gradient 142 and 44).
 // Rows that cannot be moved 16 bytes at a time (kVec false): a thread's eight values lie 32 apart, so that a warp's are neighbours.
 template <int kThreadsRow>
 __device__ __forceinline__ int chunk_at(int t, int i) { return (i * kThreadsRow + t) * 8; }
@@ -88,11 +89,12 @@ __device__ __forceinline__ void store_values(T *row, const float (&f)[8], int t,
     }
 }
 
-template <int kWarps>
+template <int kThreadsRow>
 __device__ __forceinline__ float row_sum(float v, float *s_part)
 {
+    constexpr int kWarps = kThreadsRow / 32;
 #pragma unroll
-    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    for (int d = kThreadsRow < 32 ? kThreadsRow / 2 : 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
     if constexpr (kWarps > 1) {
         const int lane = threadIdx.x & 31;
         if (lane == 0) s_part[threadIdx.x >> 5] = v;
@@ -114,7 +116,7 @@ __device__ __forceinline__ void store_codes(const BlockMatrix &to, const float (
         uint32_t m = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) m = max(m, abs_bits(x[j]));
-        const float scale = scale_of(max16(m));
+        const float scale = scale_of(max_over<kThreadsRow < 16 ? kThreadsRow : 16>(m));
         if (k >= c) return;
         *reinterpret_cast<uint2 *>(codes + k) = codes8(x, __frcp_rn(scale));
         if ((t & 15) == 0) to.scales[(long long)(k / kBlock) * to.scale_ld + row] = scale;
@@ -135,23 +137,24 @@ __device__ __forceinline__ void store_codes(const BlockMatrix &to, const float (
     }
 }
 
-template <typename T, int kWarps, int kV, bool kVec>
-__global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32) norm_rows_kernel(NormArgs a)
+template <typename T, int kThreadsRow, int kV, bool kVec>
+__global__ void __launch_bounds__(kThreadsRow <= 32 ? 256 : kThreadsRow) norm_rows_kernel(NormArgs a)
 {
-    constexpr int kThreadsRow = kWarps * 32;
-    __shared__ float s_part[2][kWarps];
+    constexpr int kRows = kThreadsRow <= 32 ? 256 / kThreadsRow : 1;
+    __shared__ float s_part[2][kThreadsRow <= 32 ? 1 : kThreadsRow / 32];
     chain_next();
     chain_wait();
     const int t = threadIdx.x % kThreadsRow;
-    const long long row = kWarps == 1 ? (long long)blockIdx.x * 8 + (threadIdx.x >> 5) : (long long)blockIdx.x;
-    if (row >= a.pixels) return;                              // whole warps; with more than one a row, whole blocks
+    const long long row = (long long)blockIdx.x * kRows + (kRows > 1 ? threadIdx.x / kThreadsRow : 0);
+    if (kThreadsRow >= 32 && row >= a.pixels) return;         // whole warps; with more than one a row, whole blocks
+    const int c = kThreadsRow < 32 && row >= a.pixels ? 0 : a.c;                   // (of several rows of a warp each has its lanes' share of its sums to take)
     const long long base = row * a.c;
     Raw8<T> rh[kV], ry[kV], rg[kV];
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
-        load_values<T, kThreadsRow, kVec>(rh[i], (const T *)a.h + base, t, i, a.c);
-        if (a.y) load_values<T, kThreadsRow, kVec>(ry[i], (const T *)a.y + base, t, i, a.c);
-        if (a.gate_map) load_values<T, kThreadsRow, kVec>(rg[i], (const T *)a.gate_map + base, t, i, a.c);
+        load_values<T, kThreadsRow, kVec>(rh[i], (const T *)a.h + base, t, i, c);
+        if (a.y) load_values<T, kThreadsRow, kVec>(ry[i], (const T *)a.y + base, t, i, c);
+        if (a.gate_map) load_values<T, kThreadsRow, kVec>(rg[i], (const T *)a.gate_map + base, t, i, c);
     }
     float s[kV][8];
 #pragma unroll
@@ -168,7 +171,7 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32) norm_rows_ker
 #pragma unroll
                 for (int j = 0; j < 8; ++j) sum = fmaf(y[j], y[j], sum);
             }
-            q = inv_sqrt(fmaf(row_sum<kWarps>(sum, s_part[0]), inv_c, a.eps));
+            q = inv_sqrt(fmaf(row_sum<kThreadsRow>(sum, s_part[0]), inv_c, a.eps));
         }
         const float scale = a.scale ? *a.scale : 1.f;
 #pragma unroll
@@ -177,20 +180,20 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32) norm_rows_ker
             values8(ry[i], u);
             if (a.after) {
                 float w[8];
-                load_weights<kThreadsRow, kVec>(w, a.after, t, i, a.c);
+                load_weights<kThreadsRow, kVec>(w, a.after, t, i, c);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) u[j] = u[j] * q * w[j];
             }
             if (a.gate_map || a.gate) {
                 float g[8];
                 if (a.gate_map) values8(rg[i], g);
-                else load_weights<kThreadsRow, kVec>(g, a.gate, t, i, a.c);
+                else load_weights<kThreadsRow, kVec>(g, a.gate, t, i, c);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) u[j] *= g[j];
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[i][j] = fmaf(scale, u[j], s[i][j]);
-            store_values<T, kThreadsRow, kVec>((T *)a.sum + base, s[i], t, i, a.c);
+            store_values<T, kThreadsRow, kVec>((T *)a.sum + base, s[i], t, i, c);
         }
     }
     if (!a.before) return;
@@ -199,15 +202,15 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32) norm_rows_ker
     for (int i = 0; i < kV; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum = fmaf(s[i][j], s[i][j], sum);
-    const float r = inv_sqrt(fmaf(row_sum<kWarps>(sum, s_part[1]), inv_c, a.eps));
+    const float r = inv_sqrt(fmaf(row_sum<kThreadsRow>(sum, s_part[1]), inv_c, a.eps));
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
         float w[8];
-        load_weights<kThreadsRow, kVec>(w, a.before, t, i, a.c);
+        load_weights<kThreadsRow, kVec>(w, a.before, t, i, c);
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = s[i][j] * r * w[j];
-        if (a.x) store_values<T, kThreadsRow, kVec>((T *)a.x + base, w, t, i, a.c);
-        if (a.codes.codes) store_codes<kThreadsRow, kVec>(a.codes, w, row, t, i, a.c);
+        if (a.x) store_values<T, kThreadsRow, kVec>((T *)a.x + base, w, t, i, c);
+        if (a.codes.codes) store_codes<kThreadsRow, kVec>(a.codes, w, row, t, i, c);
     }
 }
 
@@ -354,7 +357,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_ring_kerne
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum = fmaf(y[j], y[j], sum);
         }
-        sum = row_sum<kWarps>(sum, s_part[0]);                // (the block is in step here: all have read the slot)
+        sum = row_sum<kThreadsRow>(sum, s_part[0]);                // (the block is in step here: all have read the slot)
         if (threadIdx.x == 0 && row + (long long)r.stages * gridDim.x < a.pixels) reader.bring(r, row + (long long)r.stages * gridDim.x, slot);
         const float f = (a.after ? inv_sqrt(fmaf(sum, inv_c, a.eps)) : 1.f) * scale;
         sum = 0.f;
@@ -377,7 +380,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_ring_kerne
             store_values<T, kThreadsRow, true>((T *)a.sum + base, s[i], t, i, a.c);
         }
         if (a.before) {
-            const float rr = inv_sqrt(fmaf(row_sum<kWarps>(sum, s_part[1]), inv_c, a.eps));
+            const float rr = inv_sqrt(fmaf(row_sum<kThreadsRow>(sum, s_part[1]), inv_c, a.eps));
 #pragma unroll
             for (int i = 0; i < kV; ++i) {
                 float x[8];
@@ -853,11 +856,43 @@ __device__ __forceinline__ float sum8_over_warp(const float (&v)[8], int lane)
     return c;
 }
 
+// Sums of eight values over kLanes neighbouring lanes: a lane has those of values first .. first + 8 / kLanes (one at least; lanes of the same
+// value have the same).
+template <int kLanes>
+__device__ __forceinline__ int sum8_over_lanes(float (&v)[8], int lane)
+{
+    int n = 8, first = 0;
+#pragma unroll
+    for (int d = kLanes / 2; d; d /= 2) {
+        if (n > 1) {
+            n /= 2;
+            const bool high = lane & d;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j < n) {
+                    const float keep = high ? v[n + j] : v[j], give = high ? v[j] : v[n + j];
+                    v[j] = keep + __shfl_xor_sync(0xffffffffu, give, d);
+                }
+            first += high ? n : 0;
+        } else
+            v[0] += __shfl_xor_sync(0xffffffffu, v[0], d);
+    }
+    return first;
+}
+
 // The row's six sums in every thread.
-template <int kWarps>
+template <int kThreadsRow>
 __device__ __forceinline__ void row_sums(float (&v)[8], float (*s_part)[8])
 {
+    constexpr int kWarps = kThreadsRow / 32;
     const int lane = threadIdx.x & 31;
+    if constexpr (kThreadsRow < 32) {
+        sum8_over_lanes<kThreadsRow>(v, lane);                // lane l of a row: value l / (kThreadsRow / 8)
+        const float mine = v[0];
+#pragma unroll
+        for (int i = 0; i < kSums; ++i) v[i] = __shfl_sync(0xffffffffu, mine, i * (kThreadsRow / 8), kThreadsRow);
+        return;
+    }
     float mine = sum8_over_warp(v, lane);
     if constexpr (kWarps > 1) {
         if ((lane & 3) == 0) s_part[threadIdx.x >> 5][lane >> 2] = mine;
@@ -873,12 +908,13 @@ __device__ __forceinline__ void row_sums(float (&v)[8], float (*s_part)[8])
     for (int i = 0; i < kSums; ++i) v[i] = __shfl_sync(0xffffffffu, mine, 4 * i);
 }
 
-template <typename T, int kWarps, int kV, bool kVec>
-__global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32, kWarps == 1 ? 2 : (kWarps >= 16 ? 1 : 16 / kWarps)) norm_rows_grad_kernel(NormGradArgs a)
+template <typename T, int kThreadsRow, int kV, bool kVec>
+__global__ void __launch_bounds__(kThreadsRow <= 32 ? 256 : kThreadsRow, kThreadsRow <= 32 ? 2 : (kThreadsRow >= 512 ? 1 : 512 / kThreadsRow))
+norm_rows_grad_kernel(NormGradArgs a)
 {
-    constexpr int kThreadsRow = kWarps * 32, kRows = kWarps == 1 ? 8 : 1;
-    extern __shared__ float s_dyn[];                          // rows of one warp: [8][2][256 kV] sums of the warps
-    __shared__ float s_part[2][kWarps][8];
+    constexpr int kRows = kThreadsRow <= 32 ? 256 / kThreadsRow : 1, kWarpRows = kThreadsRow < 32 ? 32 / kThreadsRow : 1;
+    extern __shared__ float s_dyn[];                          // rows of a warp or less: [kRows][2][8 kThreadsRow kV] their threads' sums
+    __shared__ float s_part[2][kThreadsRow <= 32 ? 1 : kThreadsRow / 32][8];
     __shared__ float s_scale[32];
     chain_next();
     chain_wait();
@@ -890,27 +926,28 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32, kWarps == 1 ?
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum_y[i][j] = sum_x[i][j] = 0.f;
     int turn = 0;
-    for (long long row = (long long)blockIdx.x * kRows + (kRows > 1 ? warp : 0); row < a.pixels; row += (long long)gridDim.x * kRows, turn ^= 1) {
-        const long long base = row * a.c;
+    for (long long first = (long long)blockIdx.x * kRows + (kRows > 1 ? warp * kWarpRows : 0); first < a.pixels; first += (long long)gridDim.x * kRows, turn ^= 1) {
+        const long long row = first + (kWarpRows > 1 ? lane / kThreadsRow : 0), base = row * a.c;
+        const int c = kThreadsRow < 32 && row >= a.pixels ? 0 : a.c;               // (the rows of a warp keep in step)
         Raw8<T> rs[kV], ry[kV], rx[kV], rd[kV], rg[kV];
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
             zero8(rs[i]); zero8(ry[i]); zero8(rx[i]); zero8(rd[i]);
             if (a.before) {
-                load_values<T, kThreadsRow, kVec>(rs[i], (const T *)a.s + base, t, i, a.c);
-                load_values<T, kThreadsRow, kVec>(rx[i], (const T *)a.dx + base, t, i, a.c);
+                load_values<T, kThreadsRow, kVec>(rs[i], (const T *)a.s + base, t, i, c);
+                load_values<T, kThreadsRow, kVec>(rx[i], (const T *)a.dx + base, t, i, c);
             }
-            if (a.y) load_values<T, kThreadsRow, kVec>(ry[i], (const T *)a.y + base, t, i, a.c);
-            if (a.ds) load_values<T, kThreadsRow, kVec>(rd[i], (const T *)a.ds + base, t, i, a.c);
-            if (a.gate_map) load_values<T, kThreadsRow, kVec>(rg[i], (const T *)a.gate_map + base, t, i, a.c);
+            if (a.y) load_values<T, kThreadsRow, kVec>(ry[i], (const T *)a.y + base, t, i, c);
+            if (a.ds) load_values<T, kThreadsRow, kVec>(rd[i], (const T *)a.ds + base, t, i, c);
+            if (a.gate_map) load_values<T, kThreadsRow, kVec>(rg[i], (const T *)a.gate_map + base, t, i, c);
         }
         // gate times after of a chunk
         auto factors = [&](int i, float (&g)[8], float (&w)[8]) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) g[j] = w[j] = 1.f;
             if (a.gate_map) values8(rg[i], g);
-            else if (a.gate) load_weights<kThreadsRow, kVec>(g, a.gate, t, i, a.c);
-            if (a.after) load_weights<kThreadsRow, kVec>(w, a.after, t, i, a.c);
+            else if (a.gate) load_weights<kThreadsRow, kVec>(g, a.gate, t, i, c);
+            if (a.after) load_weights<kThreadsRow, kVec>(w, a.after, t, i, c);
         };
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -920,7 +957,7 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32, kWarps == 1 ?
             factors(i, g, w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) b[j] = 0.f;
-            if (a.before) load_weights<kThreadsRow, kVec>(b, a.before, t, i, a.c);
+            if (a.before) load_weights<kThreadsRow, kVec>(b, a.before, t, i, c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float tt = dx[j] * b[j], gy = g[j] * w[j] * y[j];
@@ -932,9 +969,10 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32, kWarps == 1 ?
                 v[5] = fmaf(s[j], gy, v[5]);
             }
         }
-        row_sums<kWarps>(v, s_part[turn]);
+        row_sums<kThreadsRow>(v, s_part[turn]);
         const float sums[kSums] = {v[0], v[1], v[2], v[3], v[4], v[5]};
         const PixelFactors f = pixel_factors(sums, a, scale);
+        if (kWarpRows > 1 && c == 0) continue;
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
             float s[8], y[8], dx[8], d[8], g[8], w[8], b[8];
@@ -942,13 +980,13 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32, kWarps == 1 ?
             factors(i, g, w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) b[j] = 0.f;
-            if (a.before) load_weights<kThreadsRow, kVec>(b, a.before, t, i, a.c);
+            if (a.before) load_weights<kThreadsRow, kVec>(b, a.before, t, i, c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 d[j] = fmaf(-f.r3m, s[j], fmaf(f.r, dx[j] * b[j], d[j]));
                 sum_x[i][j] = fmaf(dx[j] * f.r, s[j], sum_x[i][j]);
             }
-            store_values<T, kThreadsRow, kVec>((T *)a.dh + base, d, t, i, a.c);
+            store_values<T, kThreadsRow, kVec>((T *)a.dh + base, d, t, i, c);
             if (a.y) {
                 float dy[8], dg[8];
 #pragma unroll
@@ -959,29 +997,29 @@ __global__ void __launch_bounds__(kWarps == 1 ? 256 : kWarps * 32, kWarps == 1 ?
                     dg[j] = scale * (dn * w[j]);
                     dy[j] = f.q * fmaf(-n, f.mean, scale * (d[j] * (g[j] * w[j])));
                 }
-                store_values<T, kThreadsRow, kVec>((T *)a.dy + base, dy, t, i, a.c);
-                if (a.gate_map) store_values<T, kThreadsRow, kVec>((T *)a.dgate_map + base, dg, t, i, a.c);
+                store_values<T, kThreadsRow, kVec>((T *)a.dy + base, dy, t, i, c);
+                if (a.gate_map) store_values<T, kThreadsRow, kVec>((T *)a.dgate_map + base, dg, t, i, c);
             }
         }
     }
     // the block's sums
     float *const part = a.partial + (long long)blockIdx.x * 2 * a.c;
     if constexpr (kRows > 1) {
-        constexpr int kRow = 256 * kV;
-        float *const mine = s_dyn + warp * 2 * kRow;
+        constexpr int kRow = 8 * kThreadsRow * kV;
+        float *const mine = s_dyn + threadIdx.x / kThreadsRow * 2 * kRow;
 #pragma unroll
         for (int i = 0; i < kV; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                mine[value_at<32, kVec>(lane, i, j)] = sum_y[i][j];
-                mine[kRow + value_at<32, kVec>(lane, i, j)] = sum_x[i][j];
+                mine[value_at<kThreadsRow, kVec>(t, i, j)] = sum_y[i][j];
+                mine[kRow + value_at<kThreadsRow, kVec>(t, i, j)] = sum_x[i][j];
             }
         __syncthreads();
         for (int i = threadIdx.x; i < 2 * kRow; i += 256) {
             const int k = i % kRow;
             float v = 0.f;
 #pragma unroll
-            for (int w = 0; w < 8; ++w) v += s_dyn[w * 2 * kRow + i];
+            for (int w = 0; w < kRows; ++w) v += s_dyn[w * 2 * kRow + i];
             if (k < a.c) part[(i / kRow) * (long long)a.c + k] = v;
         }
     } else {
@@ -1072,7 +1110,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
                 v[5] = fmaf(s[j], gy, v[5]);
             }
         }
-        row_sums<kWarps>(v, s_part[turn & 1]);
+        row_sums<kThreadsRow>(v, s_part[turn & 1]);
         // (the block is in step: the last row's slot is free)
         if (t == 0 && turn > 0 && row + (long long)(r.stages - 1) * gridDim.x < a.pixels) reader.bring(r, row + (long long)(r.stages - 1) * gridDim.x, last);
         const float sums[kSums] = {v[0], v[1], v[2], v[3], v[4], v[5]};
@@ -1224,30 +1262,6 @@ __global__ void __launch_bounds__(256) norm_maps_grad_kernel(NormGradArgs a)
         for (int w = 0; w < 8; ++w) v += s_scale[w];
         a.partial_scale[blockIdx.x] = v;
     }
-}
-
-// Sums of eight values over kLanes neighbouring lanes: a lane has those of values first .. first + 8 / kLanes (one at least; lanes of the same
-// value have the same).
-template <int kLanes>
-__device__ __forceinline__ int sum8_over_lanes(float (&v)[8], int lane)
-{
-    int n = 8, first = 0;
-#pragma unroll
-    for (int d = kLanes / 2; d; d /= 2) {
-        if (n > 1) {
-            n /= 2;
-            const bool high = lane & d;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j < n) {
-                    const float keep = high ? v[n + j] : v[j], give = high ? v[j] : v[n + j];
-                    v[j] = keep + __shfl_xor_sync(0xffffffffu, give, d);
-                }
-            first += high ? n : 0;
-        } else
-            v[0] += __shfl_xor_sync(0xffffffffu, v[0], d);
-    }
-    return first;
 }
 
 // The same with the inputs' tile in shared memory, as in the forward.
@@ -1480,12 +1494,14 @@ __global__ void __launch_bounds__(kVectorWarps * 32) norm_vectors_kernel(NormGra
     }
 }
 
-template <typename T, int kWarps, int kV>
+template <typename T, int kThreadsRow, int kV>
 tc_status launch_norm_rows(const NormArgs &a, cudaStream_t s)
 {
-    const long long blocks = kWarps == 1 ? (a.pixels + 7) / 8 : a.pixels;
-    return launch_first(true, a.vec ? norm_rows_kernel<T, kWarps, kV, true> : norm_rows_kernel<T, kWarps, kV, false>, dim3((unsigned int)blocks), dim3(kWarps == 1 ? 256 : kWarps * 32), 0, s, a) == cudaSuccess
-               ? TC_OK : TC_ERR_CUDA;
+    constexpr int kRows = kThreadsRow <= 32 ? 256 / kThreadsRow : 1;
+    auto kernel = norm_rows_kernel<T, kThreadsRow, kV, true>;
+    if constexpr (kThreadsRow >= 32)
+        if (!a.vec) kernel = norm_rows_kernel<T, kThreadsRow, kV, false>;
+    return launch_first(true, kernel, dim3((unsigned int)((a.pixels + kRows - 1) / kRows)), dim3(kThreadsRow <= 32 ? 256 : kThreadsRow), 0, s, a) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
 
 // A ring of rows of the given inputs, for `blocks` blocks an SM; none (no stages) where two rows do not fit, and where a block has no more than two rows, which
@@ -1589,22 +1605,29 @@ tc_status norms(const NormArgs &a, cudaStream_t s)
         if (m.px == 8) return launch_maps<norm_maps_tile_kernel<T, 8, 8>>(a, m, m.blocks, vec, pairs, s) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
         return launch_first(true, norm_maps_kernel<T>, dim3((unsigned int)((a.pixels + 31) / 32)), dim3(256), 0, s, a) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
     }
-    if (a.c <= 256) return launch_norm_rows<T, 1, 1>(a, s);
-    if (a.c <= 512) return launch_norm_rows<T, 1, 2>(a, s);
+    if (a.c <= 64 && a.vec) return launch_norm_rows<T, 8, 1>(a, s);
+    if (a.c <= 128 && a.vec) return launch_norm_rows<T, 16, 1>(a, s);
+    if (a.c <= 256) return launch_norm_rows<T, 32, 1>(a, s);
+    if (a.c <= 512) return launch_norm_rows<T, 32, 2>(a, s);
     tc_status st;
-    if (a.c <= 1024) return launch_norm_ring<T, 2, 2>(a, s, st) ? st : launch_norm_rows<T, 4, 1>(a, s);
-    if (a.c <= 2048) return launch_norm_ring<T, 4, 2>(a, s, st) ? st : launch_norm_rows<T, 8, 1>(a, s);
-    if (a.c <= 4096) return launch_norm_ring<T, 8, 2>(a, s, st) ? st : launch_norm_rows<T, 8, 2>(a, s);
-    if (a.c <= 8192) return launch_norm_ring<T, 16, 2>(a, s, st) ? st : launch_norm_rows<T, 16, 2>(a, s);
-    return launch_norm_rows<T, 16, 4>(a, s);
+    if (a.c <= 1024) return launch_norm_ring<T, 2, 2>(a, s, st) ? st : launch_norm_rows<T, 128, 1>(a, s);
+    if (a.c <= 2048) return launch_norm_ring<T, 4, 2>(a, s, st) ? st : launch_norm_rows<T, 256, 1>(a, s);
+    if (a.c <= 4096) return launch_norm_ring<T, 8, 2>(a, s, st) ? st : launch_norm_rows<T, 256, 2>(a, s);
+    if (a.c <= 8192) return launch_norm_ring<T, 16, 2>(a, s, st) ? st : launch_norm_rows<T, 512, 2>(a, s);
+    return launch_norm_rows<T, 512, 4>(a, s);
 }
 
-template <typename T, int kWarps, int kV>
+template <typename T, int kThreadsRow, int kV>
 cudaError_t launch_grad_rows(const NormGradArgs &a, int blocks, cudaStream_t s)
 {
-    const size_t smem = kWarps == 1 ? 8 * 2 * 256 * kV * sizeof(float) : 0;
-    return launch_first(true, a.vec ? norm_rows_grad_kernel<T, kWarps, kV, true> : norm_rows_grad_kernel<T, kWarps, kV, false>, dim3((unsigned int)blocks), dim3(kWarps == 1 ? 256 : kWarps * 32), smem, s, a);
+    const size_t smem = kThreadsRow <= 32 ? 2 * 8 * 256 * kV * sizeof(float) : 0;
+    auto kernel = norm_rows_grad_kernel<T, kThreadsRow, kV, true>;
+    if constexpr (kThreadsRow >= 32)
+        if (!a.vec) kernel = norm_rows_grad_kernel<T, kThreadsRow, kV, false>;
+    return launch_first(true, kernel, dim3((unsigned int)blocks), dim3(kThreadsRow <= 32 ? 256 : kThreadsRow), smem, s, a);
 }
+// Threads of a row of up to 256 channels.
+int short_row_threads(const NormGradArgs &a) { return !a.vec || a.c > 128 ? 32 : a.c > 64 ? 16 : 8; }
 
 // With the ring of rows where there is one: two chunks a thread of bf16, whose unpacking and sums bound it (16384x4096 209 us with one
 // and 157); one of fp32, of whose rows two would not fit two blocks' rings.  Blocks of 512 threads an SM in all.
@@ -1618,7 +1641,7 @@ cudaError_t launch_grad(const NormGradArgs &a, int blocks, cudaStream_t s)
     if (r.stages && a.vec) return launch_ring<norm_rows_grad_ring_kernel<T, kRingWarps, kRingV, true>>(a.device, a, r, blocks, kRingWarps * 32, s);
     if constexpr (kWarps > 2)                                 // (unaligned rows of up to 512 channels: 20000x301 47 us without and 55 with)
         if (r.stages) return launch_ring<norm_rows_grad_ring_kernel<T, kRingWarps, kRingV, false>>(a.device, a, r, blocks, kRingWarps * 32, s);
-    return launch_grad_rows<T, kWarps, 1>(a, blocks, s);
+    return launch_grad_rows<T, 32 * kWarps, 1>(a, blocks, s);
 }
 
 template <typename T>
@@ -1637,13 +1660,16 @@ tc_status gradient(const NormGradArgs &a, int blocks, int sms, cudaStream_t s)
         const size_t smem = (size_t)2 * a.c * sizeof(float);
         err = allow_shared<norm_maps_grad_kernel<T>>(a.device, 2 * kMostChannels * sizeof(float))
                   ? launch_first(true, norm_maps_grad_kernel<T>, dim3((unsigned int)blocks), dim3(256), smem, s, a) : cudaErrorInvalidValue;
-    } else if (a.c <= 256) err = launch_grad_rows<T, 1, 1>(a, blocks, s);
+    } else if (a.c <= 256) {
+        const int threads = short_row_threads(a);
+        err = threads == 8 ? launch_grad_rows<T, 8, 1>(a, blocks, s) : threads == 16 ? launch_grad_rows<T, 16, 1>(a, blocks, s) : launch_grad_rows<T, 32, 1>(a, blocks, s);
+    }
     else if (a.c <= 512) err = launch_grad<T, 2>(a, blocks, s);
     else if (a.c <= 1024) err = launch_grad<T, 4>(a, blocks, s);
     else if (a.c <= 2048) err = launch_grad<T, 8>(a, blocks, s);
     else if (a.c <= 4096) err = launch_grad<T, 16>(a, blocks, s);
     else if (a.c <= 8192) err = launch_grad<T, 32>(a, blocks, s);
-    else err = launch_grad_rows<T, 32, 2>(a, blocks, s);
+    else err = launch_grad_rows<T, 1024, 2>(a, blocks, s);
     if (err != cudaSuccess) { cudaGetLastError(); return TC_ERR_CUDA; }
     return launch_chained(blocks > 0, norm_vectors_kernel, dim3((unsigned int)((a.c + 31) / 32)), dim3(kVectorWarps * 32), 0, s, a, blocks) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
@@ -1663,7 +1689,7 @@ int tc_norm_grad_blocks(const NormGradArgs &a, int dtype, int sm_count)
         if (const MapPlan m = plan_grad_maps(a, size, sm_count); m.px) return (int)m.blocks;
     long long rows = a.pixels, per_sm = 1;
     if (a.hw > 1) { rows = (a.pixels + 31) / 32; per_sm = 4; }
-    else if (a.c <= 256) { rows = (a.pixels + 7) / 8; per_sm = 2; }
+    else if (a.c <= 256) { const int each = 256 / short_row_threads(a); rows = (a.pixels + each - 1) / each; per_sm = 2; }
     else
         for (int warps = 2; warps <= 16; warps *= 2)
             if (a.c <= 256 * warps) { per_sm = 16 * ring_chunks(warps, (int)size) / warps; break; }

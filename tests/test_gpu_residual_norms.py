@@ -69,7 +69,7 @@ def _chain(c):
     return (c / 8 + 100) * 2.0 ** -24
 
 
-SHAPES = [(1, 1, 1, 1), (1, 4096, 1, 1), (3, 130, 1, 1), (300, 256, 1, 1), (17, 512, 1, 1), (9, 1000, 1, 1), (40, 1024, 1, 1), (5, 2048, 1, 1),
+SHAPES = [(1, 1, 1, 1), (1, 16, 1, 1), (3, 64, 1, 1), (1001, 64, 1, 1), (10007, 24, 1, 1), (77, 128, 1, 1), (5003, 104, 1, 1), (1, 4096, 1, 1), (3, 130, 1, 1), (300, 256, 1, 1), (17, 512, 1, 1), (9, 1000, 1, 1), (40, 1024, 1, 1), (5, 2048, 1, 1),
           (3, 2051, 1, 1), (2500, 400, 1, 1), (1900, 776, 1, 1), (1301, 2048, 1, 1), (700, 4096, 1, 1), (601, 4104, 1, 1), (2501, 301, 1, 1), (1303, 1021, 1, 1), (1201, 1538, 1, 1), (700, 4095, 1, 1), (603, 4130, 1, 1), (4, 8192, 1, 1), (2, 16384, 1, 1), (2, 9000, 1, 1), (3, 20, 7, 7), (2, 256, 14, 14), (1, 33, 5, 13), (2, 1000, 1, 33), (70, 16, 2, 2),
           (200, 48, 8, 8), (300, 100, 7, 7), (64, 500, 14, 14), (3, 1030, 6, 7), (1, 3000, 5, 5), (40, 264, 1, 30)]
 MIXES = [("channel", ()), ("tensor", ()), ("none", ()), ("none", ("scale",)), ("channel", ("before",)), ("channel", ("after",)),
