@@ -1558,21 +1558,23 @@ bool pixel_pairs(int hw, P... p)
 // Tile of a maps' kernel: as many pixels as fit, but no more than 16 while the tiles are fewer than two an SM, and 64 only of up to 64 channels,
 // which leave half of the warps idle with 32; 0 where not even eight fit.  `two`: rather tiles of which two fit an SM, the forward's (431x7x7 x 944
 // in bf16 181 us and 122, 60x28x28 x 512 in fp32 105 and 77; the gradient has no use of them: 256x14x14 x 1024 in bf16 290 us and 518).  Up to 32 channels
-// keep four warps busy: more blocks of those (437x20x20 x 25 in bf16, forward 24 us and 16, gradient 65 and 33).
+// keep four warps busy: more blocks of those (437x20x20 x 25 in bf16, forward 24 us and 16, gradient 65 and 33).  Where one tile of the
+// gradient's fits an SM and its pixels come one at a time, sixteen warps work on it (431x7x7 x 944 in bf16 243 us and 190; by
+// fours it costs time: 256x14x14 x 1024 in fp32 394 and 445).
 struct MapPlan {
     int px = 0, warps = 8;
     size_t smem = 0;
     long long blocks = 0;
 };
-MapPlan plan_maps(int inputs, int vectors, int c, size_t size, long long pixels, int sms, int warps_sm, bool two)
+MapPlan plan_maps(int inputs, int vectors, int c, int hw, size_t size, long long pixels, int sms, int warps_sm, bool two)
 {
     MapPlan m;
     const size_t c8 = (size_t)((c + 7) & ~7);
     for (int px = c <= 64 ? 64 : 32; px >= 8; px /= 2) {
         const size_t rows = px * size < 128 ? 9 : 8, smem = c8 * vectors * sizeof(float) + inputs * (c8 / 8) * rows * px * size;
         if (smem + kTileStatic > kTileSm || (px > 16 && pixels <= 2ll * sms * px) || (two && px > 8 && 2 * (smem + kTileStatic) > kTileSm)) continue;
-        m.warps = px == 64 && c <= 32 ? 4 : 8;
-        const long long fit = (long long)(kTileSm / (smem + kTileStatic * m.warps / 8)), held = warps_sm / m.warps, tiles = (pixels + px - 1) / px, most = (fit < held ? fit : held) * sms;
+        m.warps = px == 64 && c <= 32 ? 4 : !two && hw % 4 && c > 256 && 2 * (smem + kTileStatic) > kTileSm ? 16 : 8;
+        const long long fit = (long long)(kTileSm / (smem + kTileStatic / (m.warps < 8 ? 2 : 1))), held = warps_sm / m.warps, tiles = (pixels + px - 1) / px, most = (fit < held ? fit : held) * sms;
         m.px = px;
         m.smem = smem;
         m.blocks = tiles < most ? tiles : most;
@@ -1582,7 +1584,7 @@ MapPlan plan_maps(int inputs, int vectors, int c, size_t size, long long pixels,
 }
 MapPlan plan_grad_maps(const NormGradArgs &a, size_t size, int sms)
 {
-    return plan_maps((a.before ? 2 : 0) + (a.y != nullptr) + (a.ds != nullptr) + (a.gate_map != nullptr), 6, a.c, size, a.pixels, sms, 16, false);
+    return plan_maps((a.before ? 2 : 0) + (a.y != nullptr) + (a.ds != nullptr) + (a.gate_map != nullptr), 6, a.c, a.hw, size, a.pixels, sms, 16, false);
 }
 
 template <auto kKernel, typename A>
@@ -1596,7 +1598,7 @@ template <typename T>
 tc_status norms(const NormArgs &a, cudaStream_t s)
 {
     if (a.hw > 1) {
-        const MapPlan m = plan_maps(1 + (a.y != nullptr) + (a.gate_map != nullptr), 4, a.c, sizeof(T), a.pixels, a.sms, 24, true);
+        const MapPlan m = plan_maps(1 + (a.y != nullptr) + (a.gate_map != nullptr), 4, a.c, a.hw, sizeof(T), a.pixels, a.sms, 24, true);
         const bool vec = four_pixels<T>(a.hw, a.h, a.y, a.gate_map), pairs = pixel_pairs<T>(a.hw, a.sum, a.x);
         if (m.px == 64 && m.warps == 4) return launch_maps<norm_maps_tile_kernel<T, 64, 4>>(a, m, m.blocks, vec, pairs, s) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
         if (m.px == 64) return launch_maps<norm_maps_tile_kernel<T, 64, 8>>(a, m, m.blocks, vec, pairs, s) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
@@ -1651,11 +1653,13 @@ tc_status gradient(const NormGradArgs &a, int blocks, int sms, cudaStream_t s)
     if (blocks == 0) {                                        // no pixels: the vectors' gradients are zero
     } else if (const MapPlan m = plan_grad_maps(a, sizeof(T), sms); a.hw > 1 && m.px) {
         const bool vec = four_pixels<T>(a.hw, a.s, a.dx, a.y, a.ds, a.gate_map), pairs = pixel_pairs<T>(a.hw, a.dh, a.dy, a.dgate_map);
-        err = m.px == 64 && m.warps == 4 ? launch_maps<norm_maps_grad_tile_kernel<T, 64, 4>>(a, m, blocks, vec, pairs, s)
-              : m.px == 64 ? launch_maps<norm_maps_grad_tile_kernel<T, 64, 8>>(a, m, blocks, vec, pairs, s)
-              : m.px == 32 ? launch_maps<norm_maps_grad_tile_kernel<T, 32, 8>>(a, m, blocks, vec, pairs, s)
-              : m.px == 16 ? launch_maps<norm_maps_grad_tile_kernel<T, 16, 8>>(a, m, blocks, vec, pairs, s)
-                           : launch_maps<norm_maps_grad_tile_kernel<T, 8, 8>>(a, m, blocks, vec, pairs, s);
+        auto run = [&](auto px, auto warps) { return launch_maps<norm_maps_grad_tile_kernel<T, px.value, warps.value>>(a, m, blocks, vec, pairs, s); };
+        using std::integral_constant;
+        constexpr integral_constant<int, 4> w4; constexpr integral_constant<int, 8> w8; constexpr integral_constant<int, 16> w16;
+        err = m.px == 64   ? m.warps == 4 ? run(integral_constant<int, 64>(), w4) : run(integral_constant<int, 64>(), w8)
+              : m.px == 32 ? m.warps == 16 ? run(integral_constant<int, 32>(), w16) : run(integral_constant<int, 32>(), w8)
+              : m.px == 16 ? m.warps == 16 ? run(integral_constant<int, 16>(), w16) : run(integral_constant<int, 16>(), w8)
+                           : m.warps == 16 ? run(integral_constant<int, 8>(), w16) : run(integral_constant<int, 8>(), w8);
     } else if (a.hw > 1) {
         const size_t smem = (size_t)2 * a.c * sizeof(float);
         err = allow_shared<norm_maps_grad_kernel<T>>(a.device, 2 * kMostChannels * sizeof(float))
