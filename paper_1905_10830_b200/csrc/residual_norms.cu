@@ -822,6 +822,19 @@ constexpr int kSums = 6;        // s s, t s, y y, and ds, t, s times gate after 
 // What a pixel's sums give.
 struct PixelFactors {
     float r, r3m, q, mean;      // D = ds + r t - r3m s;  dy = q (v - y q mean)
+    float e;                    // sum D gate n after: the pixel's part of scale's gradient
+};
+// A sum of one value a pixel that carries what its additions round off: scale's gradient is a sum over all values of the maps, whose terms cancel and long
+// chains of fp32 additions showed in it.
+struct CarriedSum {
+    float sum = 0.f, off = 0.f;
+    __device__ __forceinline__ void add(float v)
+    {
+        const float w = v - off, t = sum + w;
+        off = fabsf(t) <= 3.4e38f ? (t - sum) - w : 0.f;      // (infinities stay ones)
+        sum = t;
+    }
+    __device__ __forceinline__ float value() const { return sum - off; }
 };
 __device__ __forceinline__ PixelFactors pixel_factors(const float (&sums)[kSums], const NormGradArgs &a, float scale)
 {
@@ -831,7 +844,8 @@ __device__ __forceinline__ PixelFactors pixel_factors(const float (&sums)[kSums]
     f.r3m = f.r * f.r * f.r * (sums[1] * inv_c);
     f.q = a.after ? inv_sqrt(fmaf(sums[2], inv_c, a.eps)) : 1.f;
     const float dot = fmaf(-f.r3m, sums[5], fmaf(f.r, sums[4], sums[3]));           // sum D gate after y
-    f.mean = a.after ? scale * f.q * dot * inv_c : 0.f;
+    f.e = f.q * dot;
+    f.mean = a.after ? scale * f.e * inv_c : 0.f;
     return f;
 }
 
@@ -920,11 +934,12 @@ norm_rows_grad_kernel(NormGradArgs a)
     chain_wait();
     const int t = threadIdx.x % kThreadsRow, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const float scale = a.y && a.scale ? *a.scale : 1.f;
-    float sum_y[kV][8], sum_x[kV][8], sum_scale = 0.f;        // D n (times a map's gate);  dx s r
+    float sum_y[kV][8], sum_x[kV][8];                         // D n (times a map's gate);  dx s r
 #pragma unroll
     for (int i = 0; i < kV; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum_y[i][j] = sum_x[i][j] = 0.f;
+    CarriedSum total;
     int turn = 0;
     for (long long first = (long long)blockIdx.x * kRows + (kRows > 1 ? warp * kWarpRows : 0); first < a.pixels; first += (long long)gridDim.x * kRows, turn ^= 1) {
         const long long row = first + (kWarpRows > 1 ? lane / kThreadsRow : 0), base = row * a.c;
@@ -973,6 +988,7 @@ norm_rows_grad_kernel(NormGradArgs a)
         const float sums[kSums] = {v[0], v[1], v[2], v[3], v[4], v[5]};
         const PixelFactors f = pixel_factors(sums, a, scale);
         if (kWarpRows > 1 && c == 0) continue;
+        total.add(f.e);
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
             float s[8], y[8], dx[8], d[8], g[8], w[8], b[8];
@@ -991,8 +1007,7 @@ norm_rows_grad_kernel(NormGradArgs a)
                 float dy[8], dg[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float n = y[j] * f.q, dn = d[j] * n, e = dn * g[j] * w[j];
-                    sum_scale += e;
+                    const float n = y[j] * f.q, dn = d[j] * n;
                     sum_y[i][j] += a.gate ? dn : dn * g[j];
                     dg[j] = scale * (dn * w[j]);
                     dy[j] = f.q * fmaf(-n, f.mean, scale * (d[j] * (g[j] * w[j])));
@@ -1029,6 +1044,7 @@ norm_rows_grad_kernel(NormGradArgs a)
             store_values<float, kThreadsRow, kVec>(part + a.c, sum_x[i], t, i, a.c);
         }
     }
+    float sum_scale = t == 0 ? total.value() : 0.f;
 #pragma unroll
     for (int d = 16; d; d >>= 1) sum_scale += __shfl_xor_sync(0xffffffffu, sum_scale, d);
     if (lane == 0) s_scale[warp] = sum_scale;
@@ -1048,7 +1064,6 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
     extern __shared__ __align__(16) unsigned char s_ring[];
     __shared__ __align__(8) unsigned long long s_full[kRingStages];
     __shared__ float s_part[2][kWarps][8];
-    __shared__ float s_scale[kWarps];
     chain_next();
     chain_wait();
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
@@ -1059,7 +1074,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
     // parts of a stage: s and dx (with before), y, ds, gate, those that there are
     const uint32_t part = r.part_bytes, at_y = a.before ? 2 * part : 0, at_d = at_y + (a.y ? part : 0), at_g = at_d + (a.ds ? part : 0);
     const float scale = a.y && a.scale ? *a.scale : 1.f;
-    float wy[kV][8], wx[kV][8], sum_y[kV][8], sum_x[kV][8], sum_scale = 0.f;
+    float wy[kV][8], wx[kV][8], sum_y[kV][8], sum_x[kV][8];
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
         float g[8];
@@ -1071,6 +1086,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
 #pragma unroll
         for (int j = 0; j < 8; ++j) wy[i][j] *= g[j];
     }
+    CarriedSum total;
     int turn = 0, slot = 0, last = 0;
     for (long long row = blockIdx.x; row < a.pixels; row += gridDim.x, ++turn) {
         const long long base = row * a.c;
@@ -1115,6 +1131,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
         if (t == 0 && turn > 0 && row + (long long)(r.stages - 1) * gridDim.x < a.pixels) reader.bring(r, row + (long long)(r.stages - 1) * gridDim.x, last);
         const float sums[kSums] = {v[0], v[1], v[2], v[3], v[4], v[5]};
         const PixelFactors f = pixel_factors(sums, a, scale);
+        total.add(f.e);
         const float scale_q = scale * f.q, mean_q = f.mean * f.q * f.q;
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
@@ -1142,7 +1159,6 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
                 for (int j = 0; j < 8; ++j) {
                     const float dw = d[j] * wy[i][j], dn = d[j] * (y[j] * f.q);
                     dg[j] = scale_q * (dw * y[j]);
-                    sum_scale = fmaf(dn * g[j], wy[i][j], sum_scale);
                     sum_y[i][j] = a.gate_map ? fmaf(dn, g[j], sum_y[i][j]) : sum_y[i][j] + dn;
                     dy[j] = fmaf(-y[j], mean_q, scale_q * (dw * g[j]));
                 }
@@ -1159,15 +1175,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
         store_values<float, kThreadsRow, kVec>(to, sum_y[i], t, i, a.c);
         store_values<float, kThreadsRow, kVec>(to + a.c, sum_x[i], t, i, a.c);
     }
-#pragma unroll
-    for (int d = 16; d; d >>= 1) sum_scale += __shfl_xor_sync(0xffffffffu, sum_scale, d);
-    if (lane == 0) s_scale[warp] = sum_scale;
-    __syncthreads();
-    if (t == 0) {
-        float v = 0.f;
-        for (int w = 0; w < kWarps; ++w) v += s_scale[w];
-        a.partial_scale[blockIdx.x] = v;
-    }
+    if (t == 0) a.partial_scale[blockIdx.x] = total.value();
 }
 
 // Maps: 32 pixels at a time, a lane for each; warps take slices of eight channels in turn.  The sums over the pixels are
@@ -1177,13 +1185,12 @@ __global__ void __launch_bounds__(256) norm_maps_grad_kernel(NormGradArgs a)
 {
     extern __shared__ float s_dyn[];                          // [2][c]
     __shared__ float s_part[8][kSums][32];
-    __shared__ float s_scale[8];
     chain_next();
     chain_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const float scale = a.y && a.scale ? *a.scale : 1.f;
     for (int i = threadIdx.x; i < 2 * a.c; i += 256) s_dyn[i] = 0.f;
-    float sum_scale = 0.f;
+    CarriedSum total;
     const long long groups = (a.pixels + 31) / 32;
     for (long long group = blockIdx.x; group < groups; group += gridDim.x) {
         const long long p = group * 32 + lane;
@@ -1221,6 +1228,7 @@ __global__ void __launch_bounds__(256) norm_maps_grad_kernel(NormGradArgs a)
             for (int w = 0; w < 8; ++w) sums[i] += s_part[w][i][lane];
         }
         const PixelFactors f = pixel_factors(sums, a, scale);
+        if (ok) total.add(f.e);
         for (int c0 = warp * 8; c0 < a.c; c0 += 64) {
             float sum_y[8], sum_x[8];
 #pragma unroll
@@ -1239,7 +1247,6 @@ __global__ void __launch_bounds__(256) norm_maps_grad_kernel(NormGradArgs a)
                 if (a.y) {
                     const float n = load1((const T *)a.y + at) * f.q, w = a.after ? a.after[ch] : 1.f;
                     const float g = a.gate_map ? load1((const T *)a.gate_map + at) : a.gate ? a.gate[ch] : 1.f, dn = d * n;
-                    sum_scale += dn * g * w;
                     sum_y[j] = a.gate ? dn : dn * g;
                     store1((T *)a.dy + at, f.q * fmaf(-n, f.mean, scale * (d * (g * w))));
                     if (a.gate_map) store1((T *)a.dgate_map + at, scale * (dn * w));
@@ -1252,16 +1259,12 @@ __global__ void __launch_bounds__(256) norm_maps_grad_kernel(NormGradArgs a)
             }
         }
     }
+    float sum_scale = total.value();                          // (every warp has the same pixels')
 #pragma unroll
     for (int d = 16; d; d >>= 1) sum_scale += __shfl_xor_sync(0xffffffffu, sum_scale, d);
-    if (lane == 0) s_scale[warp] = sum_scale;
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * a.c; i += 256) a.partial[(long long)blockIdx.x * 2 * a.c + i] = s_dyn[i];
-    if (threadIdx.x == 0) {
-        float v = 0.f;
-        for (int w = 0; w < 8; ++w) v += s_scale[w];
-        a.partial_scale[blockIdx.x] = v;
-    }
+    if (threadIdx.x == 0) a.partial_scale[blockIdx.x] = sum_scale;
 }
 
 // The same with the inputs' tile in shared memory, as in the forward.
@@ -1271,7 +1274,6 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) norm_maps_grad_tile_
     using M = MapTile<T, kPx, kWarps>;
     extern __shared__ __align__(16) unsigned char s_tile[];   // sums over the pixels [2][c8], after times the channels' gate, before; s, dx, y, ds, gate [c8][kPx]
     __shared__ float2 s_part[kSums][kWarps][M::kPairs];
-    __shared__ float s_scale[kWarps];
     const int c8 = (a.c + 7) & ~7, plane = M::values(c8);
     uint64_t *const wy = reinterpret_cast<uint64_t *>(s_tile), *const wx = wy + c8;
     float *const sums_y = reinterpret_cast<float *>(wx + c8), *const sums_x = sums_y + c8;
@@ -1284,7 +1286,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) norm_maps_grad_tile_
     for (int i = threadIdx.x; i < 2 * c8; i += M::kThreads) sums_y[i] = 0.f;
     zero_rows<M>(ss, (a.before ? 2 : 0) + (a.y != nullptr) + (a.ds != nullptr) + (a.gate_map != nullptr), plane, a.c, c8, kPx);
     const float scale = a.y && a.scale ? *a.scale : 1.f;
-    uint64_t sum_scale = 0ull;
+    CarriedSum total0, total1;
     const long long tiles = (a.pixels + kPx - 1) / kPx;
     for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const uint32_t p0 = (uint32_t)tile * kPx, pixels = (uint32_t)a.pixels;
@@ -1367,6 +1369,8 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) norm_maps_grad_tile_
             }
         }
         const PixelFactors f0 = pixel_factors(sum0, a, scale), f1 = pixel_factors(sum1, a, scale);
+        if (px.ok0) total0.add(f0.e);
+        if (px.ok1) total1.add(f1.e);
         const uint64_t r = pair_of(f0.r, f1.r), r3m = pair_of(-f0.r3m, -f1.r3m), q = pair_of(f0.q, f1.q), scale_q = pair_of(scale * f0.q, scale * f1.q);
         const uint64_t mean_q = pair_of(-f0.mean * f0.q * f0.q, -f1.mean * f1.q * f1.q);
         for (int c0 = slice * 8; c0 - slice * 8 < a.c; c0 += M::kStep) {           // (the same for all lanes: their sums go together)
@@ -1418,7 +1422,6 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) norm_maps_grad_tile_
                         }
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            sum_scale = fma2(dn[j], w[h + j], sum_scale);
                             halves(dn[j], u, v);
                             sum_y[h + j] = u + v;
                             dwg[j] = fma2(yv[j], mean_q, mul2(scale_q, dwg[j]));
@@ -1439,23 +1442,16 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) norm_maps_grad_tile_
             }
         }
     }
-    float x, y;
-    halves(sum_scale, x, y);
-    x += y;
+    float sum_scale = lane < M::kPairs ? total0.value() + total1.value() : 0.f;      // (every warp has the same pixels')
 #pragma unroll
-    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    if (lane == 0) s_scale[warp] = x;
+    for (int d = 16; d; d >>= 1) sum_scale += __shfl_xor_sync(0xffffffffu, sum_scale, d);
     __syncthreads();
     float *const to = a.partial + (long long)blockIdx.x * 2 * a.c;
     for (int i = threadIdx.x; i < a.c; i += M::kThreads) {
         to[i] = sums_y[i];
         to[a.c + i] = sums_x[i];
     }
-    if (threadIdx.x == 0) {
-        float v = 0.f;
-        for (int w = 0; w < kWarps; ++w) v += s_scale[w];
-        a.partial_scale[blockIdx.x] = v;
-    }
+    if (threadIdx.x == 0) a.partial_scale[blockIdx.x] = sum_scale;
 }
 
 // The blocks' sums, in their order: 32 channels a block, every kVectorWarps-th of the blocks' sums a warp (of up to 592: what it waits for is

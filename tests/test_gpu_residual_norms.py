@@ -398,3 +398,22 @@ def test_captured_with_other_calls_between(ctx):
         assert torch.equal(s, want_s) and torch.equal(x, want_x)
         for a, b in zip(g, want):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("shape", [(4_000_000, 16, 1, 1), (4_000_000, 20, 1, 1), (20_000, 1024, 1, 1), (1000, 16, 28, 28)])
+def test_scale_gradient_of_many_pixels(ctx, shape):
+    """Equal terms v = 1 + 0.45 * 2^-13, one a pixel (y = +-1 has the norm 1, ds is v in one channel): added one after the other in fp32, a chain of more than
+    1024 of them loses nearly half of a unit in the last place each time."""
+    n, c, h, w = shape
+    pixels = n * h * w
+    y = torch.ones(shape, device="cuda")
+    y[:, 1::2] = -1
+    ds = torch.zeros(shape, device="cuda")
+    v = torch.tensor(1 + 0.45 * 2.0 ** -13, device="cuda")
+    ds[:, 0] = v
+    got = tc.tc_residual_norms_backward(ctx, y, y, None, ds, after=torch.ones(c, device="cuda"), scale=torch.ones(1, device="cuda"), eps=0.0)
+    want = pixels * v.double()
+    # A block's own sum carries its roundings: one (2^-24) where it leaves.  Of a warp's eight rows, or a lane's pixels: a sum over 32 lanes, 5 roundings, and one of two pixels.
+    # Blocks: at most 592, by 32 lanes 19 in a row and 5 for the lanes'.  1 / sqrt(1) may be off by 2^-22 (twice: for y and in the pixel's part), the sum of 1 / c times c ones by 2^-23.
+    tol = want * ((1 + 6 + 19 + 5) * 2.0 ** -24 + 2 * 2.0 ** -22 + 2.0 ** -23)
+    assert (got.scale.double() - want).abs().item() <= tol.item(), ((got.scale.double() - want) / want).item()
