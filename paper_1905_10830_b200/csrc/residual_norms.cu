@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(kThreadsRow <= 32 ? 256 : kThreadsRow) norm_ro
 // ---- rows on their way to shared memory ------------------------------------------------------
 // Long rows: a block walks rows gridDim.x apart, whose parts of all inputs one thread brings to a ring in shared memory by bulk
 // copies, several rows ahead, so that the memory is at work while the block waits for a row's sums (with a row's loads in
-// registers, and the vectors read again for each row: gradient of 16384x4096 in bf16 297 us and 157, forward 122 and 106).
+// registers, and the vectors read again for each row: gradient of 16384x4096 in bf16 297 us and 151, forward 122 and 106).
 constexpr int kRingInputs = 5, kRingStages = 8;
 constexpr size_t kRingSm = 200 * 1024;                        // of an SM's shared memory, for all its blocks' rings
 struct RowRing {
