@@ -1482,11 +1482,11 @@ __global__ void __launch_bounds__(kVectorWarps * 32) norm_vectors_kernel(NormGra
         if (a.dbefore) a.dbefore[ch] = vx;
     }
     if (warp == 1 && blockIdx.x == 0 && a.dscale) {
-        float v = 0.f;
+        double v = 0.0;                                       // (one warp, and the blocks' sums cancel like their pixels')
         for (int b = lane; b < blocks; b += 32) v += a.partial_scale[b];
 #pragma unroll
         for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-        if (lane == 0) *a.dscale = v;
+        if (lane == 0) *a.dscale = (float)v;
     }
 }
 
@@ -1628,7 +1628,7 @@ cudaError_t launch_grad_rows(const NormGradArgs &a, int blocks, cudaStream_t s)
 int short_row_threads(const NormGradArgs &a) { return !a.vec || a.c > 128 ? 32 : a.c > 64 ? 16 : 8; }
 
 // With the ring of rows where there is one: two chunks a thread of bf16, whose unpacking and sums bound it (16384x4096 209 us with one
-// and 157); one of fp32, of whose rows two would not fit two blocks' rings.  Blocks of 512 threads an SM in all.
+// and 151); one of fp32, of whose rows two would not fit two blocks' rings.  Blocks of 512 threads an SM in all.
 constexpr int ring_chunks(int warps, int size) { return warps <= 2 ? 1 : warps > 16 ? warps / 16 : size == 2 ? 2 : 1; }
 // Rows of up to 256 kWarps channels.
 template <typename T, int kWarps>
