@@ -821,9 +821,11 @@ constexpr int kSums = 6;        // s s, t s, y y, and ds, t, s times gate after 
 
 // What a pixel's sums give.
 struct PixelFactors {
-    float r, r3m, q, mean;      // D = ds + r t - r3m s;  dy = q (v - y q mean)
+    float r, m, q, mean;        // D = ds + r (t - s r m);  dy = q (v - y q mean)
     float e;                    // sum D gate n after: the pixel's part of scale's gradient
 };
+// Values are multiplied by r and by q first, one factor after the other: products of two or three factors leave fp32's range long before the values
+// do (r^3 of values above 1e13 is subnormal, of those below 1e-13 infinite).
 // A sum of one value a pixel that carries what its additions round off: scale's gradient is a sum over all values of the maps, whose terms cancel and long
 // chains of fp32 additions showed in it.
 struct CarriedSum {
@@ -841,9 +843,9 @@ __device__ __forceinline__ PixelFactors pixel_factors(const float (&sums)[kSums]
     const float inv_c = 1.0f / (float)a.c;
     PixelFactors f;
     f.r = a.before ? inv_sqrt(fmaf(sums[0], inv_c, a.eps)) : 0.f;
-    f.r3m = f.r * f.r * f.r * (sums[1] * inv_c);
+    f.m = f.r * (sums[1] * inv_c);
     f.q = a.after ? inv_sqrt(fmaf(sums[2], inv_c, a.eps)) : 1.f;
-    const float dot = fmaf(-f.r3m, sums[5], fmaf(f.r, sums[4], sums[3]));           // sum D gate after y
+    const float dot = fmaf(f.r, fmaf(-f.m, f.r * sums[5], sums[4]), sums[3]);       // sum D gate after y
     f.e = f.q * dot;
     f.mean = a.after ? scale * f.e * inv_c : 0.f;
     return f;
@@ -999,8 +1001,9 @@ norm_rows_grad_kernel(NormGradArgs a)
             if (a.before) load_weights<kThreadsRow, kVec>(b, a.before, t, i, c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                d[j] = fmaf(-f.r3m, s[j], fmaf(f.r, dx[j] * b[j], d[j]));
-                sum_x[i][j] = fmaf(dx[j] * f.r, s[j], sum_x[i][j]);
+                const float sr = s[j] * f.r;
+                d[j] = fmaf(f.r, fmaf(-sr, f.m, dx[j] * b[j]), d[j]);
+                sum_x[i][j] = fmaf(dx[j], sr, sum_x[i][j]);
             }
             store_values<T, kThreadsRow, kVec>((T *)a.dh + base, d, t, i, c);
             if (a.y) {
@@ -1132,7 +1135,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
         const float sums[kSums] = {v[0], v[1], v[2], v[3], v[4], v[5]};
         const PixelFactors f = pixel_factors(sums, a, scale);
         total.add(f.e);
-        const float scale_q = scale * f.q, mean_q = f.mean * f.q * f.q;
+        const float scale_q = scale * f.q, mean_q = f.mean * f.q;
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
             float s[8], y[8], d[8], g[8];
@@ -1143,9 +1146,9 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
                 get(true, part, i, dx);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float rx = f.r * dx[j];
-                    d[j] = fmaf(-f.r3m, s[j], fmaf(rx, wx[i][j], d[j]));
-                    sum_x[i][j] = fmaf(rx, s[j], sum_x[i][j]);
+                    const float sr = s[j] * f.r;
+                    d[j] = fmaf(f.r, fmaf(-sr, f.m, dx[j] * wx[i][j]), d[j]);
+                    sum_x[i][j] = fmaf(dx[j], sr, sum_x[i][j]);
                 }
             }
             store_values<T, kThreadsRow, kVec>((T *)a.dh + base, d, t, i, a.c);
@@ -1157,10 +1160,10 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
                 float dy[8], dg[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float dw = d[j] * wy[i][j], dn = d[j] * (y[j] * f.q);
-                    dg[j] = scale_q * (dw * y[j]);
+                    const float n = y[j] * f.q, dw = d[j] * wy[i][j], dn = d[j] * n;
+                    dg[j] = scale * (dw * n);
                     sum_y[i][j] = a.gate_map ? fmaf(dn, g[j], sum_y[i][j]) : sum_y[i][j] + dn;
-                    dy[j] = fmaf(-y[j], mean_q, scale_q * (dw * g[j]));
+                    dy[j] = fmaf(-n, mean_q, scale_q * (dw * g[j]));
                 }
                 store_values<T, kThreadsRow, kVec>((T *)a.dy + base, dy, t, i, a.c);
                 if (a.gate_map) store_values<T, kThreadsRow, kVec>((T *)a.dgate_map + base, dg, t, i, a.c);
@@ -1240,8 +1243,9 @@ __global__ void __launch_bounds__(256) norm_maps_grad_kernel(NormGradArgs a)
                 float d = a.ds ? load1((const T *)a.ds + at) : 0.f;
                 if (a.before) {
                     const float s = load1((const T *)a.s + at), dx = load1((const T *)a.dx + at);
-                    d = fmaf(-f.r3m, s, fmaf(f.r, dx * a.before[ch], d));
-                    sum_x[j] = dx * f.r * s;
+                    const float sr = s * f.r;
+                    d = fmaf(f.r, fmaf(-sr, f.m, dx * a.before[ch]), d);
+                    sum_x[j] = dx * sr;
                 }
                 store1((T *)a.dh + at, d);
                 if (a.y) {
@@ -1372,8 +1376,8 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) norm_maps_grad_tile_
         const PixelFactors f0 = px.ok0 ? pixel_factors(sum0, a, scale) : PixelFactors{}, f1 = px.ok1 ? pixel_factors(sum1, a, scale) : PixelFactors{};
         if (px.ok0) total0.add(f0.e);
         if (px.ok1) total1.add(f1.e);
-        const uint64_t r = pair_of(f0.r, f1.r), r3m = pair_of(-f0.r3m, -f1.r3m), q = pair_of(f0.q, f1.q), scale_q = pair_of(scale * f0.q, scale * f1.q);
-        const uint64_t mean_q = pair_of(-f0.mean * f0.q * f0.q, -f1.mean * f1.q * f1.q);
+        const uint64_t r = pair_of(f0.r, f1.r), m = pair_of(-f0.m, -f1.m), q = pair_of(f0.q, f1.q), scale_q = pair_of(scale * f0.q, scale * f1.q);
+        const uint64_t mean_q = pair_of(-f0.mean * f0.q, -f1.mean * f1.q), scales = pair_of(scale, scale);
         for (int c0 = slice * 8; c0 - slice * 8 < a.c; c0 += M::kStep) {           // (the same for all lanes: their sums go together)
             float sum_y[8], sum_x[8];
             const bool some = c0 < a.c;
@@ -1396,19 +1400,19 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) norm_maps_grad_tile_
                     if (a.before)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            const uint64_t sv = M::load(s, h + j), tv = mul2(r, M::load(x, h + j));
-                            d[j] = fma2(r3m, sv, fma2(tv, b[h + j], d[j]));
-                            halves(mul2(tv, sv), u, v);
+                            const uint64_t sr = mul2(r, M::load(s, h + j)), xv = M::load(x, h + j);
+                            d[j] = fma2(r, fma2(sr, m, mul2(xv, b[h + j])), d[j]);
+                            halves(mul2(xv, sr), u, v);
                             sum_x[h + j] = u + v;
                         }
                     to_h.store4(h, d);
                     if (a.y) {
-                        uint64_t yv[4], dw[4], dn[4], dwg[4];
+                        uint64_t n[4], dw[4], dn[4], dwg[4];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            yv[j] = M::load(y, h + j);
+                            n[j] = mul2(M::load(y, h + j), q);
                             dw[j] = dwg[j] = mul2(d[j], w[h + j]);
-                            dn[j] = mul2(d[j], mul2(yv[j], q));
+                            dn[j] = mul2(d[j], n[j]);
                         }
                         if (a.gate_map) {
                             uint64_t dg[4];
@@ -1417,7 +1421,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) norm_maps_grad_tile_
                                 const uint64_t gv = M::load(g, h + j);
                                 dn[j] = mul2(dn[j], gv);
                                 dwg[j] = mul2(dw[j], gv);
-                                dg[j] = mul2(scale_q, mul2(dw[j], yv[j]));
+                                dg[j] = mul2(scales, mul2(dw[j], n[j]));
                             }
                             to_g.store4(h, dg);
                         }
@@ -1425,7 +1429,7 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) norm_maps_grad_tile_
                         for (int j = 0; j < 4; ++j) {
                             halves(dn[j], u, v);
                             sum_y[h + j] = u + v;
-                            dwg[j] = fma2(yv[j], mean_q, mul2(scale_q, dwg[j]));
+                            dwg[j] = fma2(n[j], mean_q, mul2(scale_q, dwg[j]));
                         }
                         to_y.store4(h, dwg);
                     }

@@ -94,3 +94,18 @@ def _run(ctx, d, eps):
 def test_without_eps(ctx, shape, dtype, gate, before, eps):
     d = _inputs(shape, dtype, gate, before, 3)
     _check(d, _run(ctx, d, eps), eps)
+
+
+# The forward takes such values exactly (their squares and the sum over 64 to 520 channels stay within fp32), and so do the gradients.  1e17: r^2 times
+# a gradient of 1e-6 and less is subnormal.
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape", [(37, 64, 14, 14), (40, 264, 7, 7), (1, 3000, 5, 5), (301, 64, 1, 1), (301, 201, 1, 1), (2500, 520, 1, 1), (2500, 521, 1, 1)])
+@pytest.mark.parametrize("gate", ["none", "channel", "tensor"])
+@pytest.mark.parametrize("size,eps", [(1e12, 1e-6), (1e15, 1e-6), (1e17, 0.0), (1e-14, 0.0), (1e-17, 0.0)])
+@pytest.mark.parametrize("with_ds", [True, False])
+def test_values_far_from_one(ctx, shape, dtype, gate, size, eps, with_ds):
+    d = _inputs(shape, dtype, gate, True, 4, size, with_ds)
+    if gate == "tensor":
+        d["gate"] = _inputs(shape, dtype, gate, True, 5)["s"]
+    d["dx"] = (d["dx"].float() * 1e-3).to(dtype)
+    _check(d, _run(ctx, d, eps), eps)
