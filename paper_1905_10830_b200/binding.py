@@ -674,10 +674,10 @@ def tc_matmul_blocks(ctx: Context, a: Blocks, b: Blocks, *, shape=None, dtype=to
 
 def tc_residual_norms(ctx: Context, h: torch.Tensor, y: torch.Tensor | None = None, *, after: torch.Tensor | None = None,
                       gate: torch.Tensor | None = None, scale: torch.Tensor | None = None, before: torch.Tensor | None = None,
-                      eps: float = 1e-6, blocks: bool = False, sum_out: torch.Tensor | None = None, out=None):
+                      eps: float = 1e-6, blocks: bool | str = False, sum_out: torch.Tensor | None = None, out=None):
     """(s, x): s = h + scale * gate * norm(y) * after, x = norm(s) * before, norms over the channels of each pixel.  x is a
-    tensor like h, or with `blocks` its codes by pixels; without `before` it is None.  Without `y` s is h itself.  `gate` is
-    [C], or a tensor like y."""
+    tensor like h, or with `blocks` its codes by pixels, or with blocks="both" the pair of them (the codes are those of x before it is
+    rounded to h's type); without `before` it is None.  Without `y` s is h itself.  `gate` is [C], or a tensor like y."""
     return (_layers or _layer_calls()).norms(ctx.ptr.value, ctx.device, _tensor_stream(ctx.device), h, y, after, gate, scale, before, eps, blocks, sum_out, out)
 
 

@@ -257,30 +257,39 @@ PyObject *norms(PyObject *, PyObject *const *args, Py_ssize_t n)
         const at::Tensor &h = tensor_of(a[0]);
         const tc_tensor t = map_of(h, c.device);
         const tc_norm_params p = norm_params(a + 1, h, c.device);
-        const int blocks = PyObject_IsTrue(a[7]);
-        if (blocks < 0) throw Raised{};
-        Ref sum, x;
+        const bool both = PyUnicode_Check(a[7]) && PyUnicode_CompareWithASCIIString(a[7], "both") == 0;
+        const int blocks = both || PyObject_IsTrue(a[7]);
+        if (PyErr_Occurred()) throw Raised{};
+        Ref sum, x, pair;
         void *at_sum = nullptr, *at_x = nullptr;
         BlocksRef codes;
         const bool has_y = a[1] != Py_None, has_x = a[5] != Py_None;
+        PyObject *out_x = a[9], *out_codes = a[9];
+        if (both && has_x && a[9] != Py_None) {
+            pair = Ref(PySequence_Tuple(a[9]));
+            if (PyTuple_GET_SIZE(pair.p) != 2) throw Bad{"out: a tensor and Blocks as this call returns them"};
+            out_x = PyTuple_GET_ITEM(pair.p, 0);
+            out_codes = PyTuple_GET_ITEM(pair.p, 1);
+        }
         if (has_y) {
             if (a[8] == Py_None) sum = wrap(make_like(h));
             else { Py_INCREF(a[8]); sum = Ref(a[8]); }
             at_sum = like(sum.p, h, c.device, "sum_out");
         } else { Py_INCREF(a[0]); sum = Ref(a[0]); }
-        if (has_x && blocks) {
-            if (a[9] == Py_None) codes = new_blocks(pixels_of(t), t.c, false, c.device);
-            else {
-                codes.blocks = given_blocks(a[9], c.device);
-                Py_INCREF(a[9]);
-                codes.object = Ref(a[9]);
-            }
-            x = std::move(codes.object);
-        } else if (has_x) {
-            if (a[9] == Py_None) x = wrap(make_like(h));
-            else { Py_INCREF(a[9]); x = Ref(a[9]); }
+        if (has_x && (both || !blocks)) {
+            if (out_x == Py_None) x = wrap(make_like(h));
+            else { Py_INCREF(out_x); x = Ref(out_x); }
             at_x = like(x.p, h, c.device, "out");
-        } else x = Ref(none());
+        }
+        if (has_x && blocks) {
+            if (out_codes == Py_None) codes = new_blocks(pixels_of(t), t.c, false, c.device);
+            else {
+                codes.blocks = given_blocks(out_codes, c.device);
+                Py_INCREF(out_codes);
+                codes.object = Ref(out_codes);
+            }
+            x = both ? Ref(PyTuple_Pack(2, x.p, codes.object.p)) : std::move(codes.object);
+        } else if (!has_x) x = Ref(none());
         c.check(unlocked([&] { return call_norms(c.ctx, &t, &p, at_sum, at_x, has_x && blocks ? &codes.blocks : nullptr, c.stream); }), "tc_residual_norms");
         return PyTuple_Pack(2, sum.p, x.p);
     });

@@ -102,10 +102,10 @@ class ResidualBlock:
 
     def gradients(self, h: torch.Tensor, ds: torch.Tensor) -> dict:
         """Gradients to `h`, the weight (float32) and the vectors, from the gradient `ds` of the block's output; the forward
-        pass is computed again, the products' operands in both directions are 8-bit blocks."""
+        pass is computed again (the same bits), the products' operands in both directions are 8-bit blocks."""
         n, c, hh, ww = h.shape
-        _, x = tc.tc_residual_norms(self.ctx, h, before=self.before, eps=self.eps)
-        x_pixels, x_channels = tc.tc_quantize_blocks(self.ctx, x, rows="both")
+        _, (x, x_pixels) = tc.tc_residual_norms(self.ctx, h, before=self.before, eps=self.eps, blocks="both")
+        x_channels = tc.tc_quantize_blocks(self.ctx, x, rows="channels")
         y = tc.tc_matmul_blocks(self.ctx, x_pixels, self.rows, shape=(n, hh, ww), dtype=h.dtype)
         s = tc.tc_residual_norms(self.ctx, h, y, eps=self.eps, **self.around)[0]
         outer = tc.tc_residual_norms_backward(self.ctx, s, y, None, ds, eps=self.eps, **self.around)
