@@ -342,7 +342,6 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
     __shared__ __align__(16) float s_scales[S::kEpiWarps][kScaleSlots * ScaleRing<S::kCols, kColumnScales>::kSlot];
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    chain_next();
     if (tid == S::kProducer * 32) { tensormap_prefetch(&map_a); tensormap_prefetch(&map_b); }
     if (tid == 0) {
         for (int s = 0; s < S::kStages; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
@@ -353,6 +352,7 @@ block_matmul_kernel(const __grid_constant__ TileArgs a, const __grid_constant__ 
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
+    chain_next();                                             // (behind the allocation of tensor memory)
     const uint32_t tmem_base = __shfl_sync(0xffffffffu, s_tmem_base, 0);
     chain_wait();
     const int units = a.tiles_m * a.tiles_n * a.splits;
@@ -570,7 +570,6 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int rank = blockIdx.x & 1;                          // the cluster is two neighbours
-    chain_next();
     if (tid == kProducer * 32) { tensormap_prefetch(&map_a); tensormap_prefetch(&map_b); }
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
@@ -582,6 +581,7 @@ block_matmul_pair_kernel(const __grid_constant__ TileArgs a, const __grid_consta
     __syncthreads();
     cluster_sync();                                           // the other CTA's barriers are there
     tc_fence_after_sync();
+    chain_next();                                             // (behind the allocation of tensor memory)
     const uint32_t tmem_base = __shfl_sync(0xffffffffu, s_tmem_base, 0);
     chain_wait();
     const int units = a.tiles_m * a.tiles_n, step = gridDim.x >> 1;

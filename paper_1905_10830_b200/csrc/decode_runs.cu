@@ -293,7 +293,6 @@ __device__ __forceinline__ void decode_tiles(const DecodeArgs &a, const SmemLayo
     const int items = n_blocks;                                // work items per tile: its channel blocks
 
     // ---- set-up ---------------------------------------------------------------------
-    chain_next();
     if (tid < G * (kMaxPanels + 1)) {
         const int g = tid / (kMaxPanels + 1), p = tid - g * (kMaxPanels + 1);
         if (p < kMaxPanels) mbar_init(smem_u32(&s_empty[g][p]), 1);                     // the commit of the tile's last item
@@ -316,6 +315,7 @@ __device__ __forceinline__ void decode_tiles(const DecodeArgs &a, const SmemLayo
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
+    chain_next();                                             // (behind the allocation of tensor memory)
     const uint32_t tmem_base = __shfl_sync(0xffffffffu, s_tmem_base, 0);
     if (warp >= kEpiWarp0 && warp < kMmaWarp) {
         // Transposed basis -> tensor memory: row c of block b (channel 128 b + c) goes to lane c,

@@ -287,7 +287,6 @@ __device__ __forceinline__ void encode_tiles(const EncodeArgs &a, const Plan &pl
     const int n_panels = (a.c + kPanelCh - 1) / kPanelCh;
 
     // ---- set-up ---------------------------------------------------------------------
-    chain_next();                                             // (a decoder that follows is set up meanwhile)
     if (tid < kGroups) s_overflow[tid] = 0;
     if (tid == 0) {
         for (int s = 0; s < n_stages; ++s) { mbar_init(smem_u32(&s_full[s]), 128); mbar_init(smem_u32(&s_empty[s]), 1); }
@@ -343,6 +342,7 @@ __device__ __forceinline__ void encode_tiles(const EncodeArgs &a, const Plan &pl
         tc_fence_before_sync();
         named_bar_sync(kSetupBar, kSetupThreads);
         tc_fence_after_sync();
+        chain_next();                                         // (a decoder that follows is set up meanwhile; behind the allocation of tensor memory)
     }
     const uint32_t tmem_base = __shfl_sync(0xffffffffu, s_tmem_base, 0);
 

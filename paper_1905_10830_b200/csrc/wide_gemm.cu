@@ -67,7 +67,6 @@ __global__ void __launch_bounds__(kThreads, 1) wide_gemm_kernel(GemmArgs a, cons
     // (taken from lane 0: the compiler knows that the branches between the roles are the same for a whole warp)
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const uint32_t ring = smem_u32(smem);
-    chain_next();
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&s_full[s]), 1); mbar_init(smem_u32(&s_empty[s]), 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&s_tfull[b]), 1); mbar_init(smem_u32(&s_tempty[b]), kEpiWarps); }
@@ -77,6 +76,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_gemm_kernel(GemmArgs a, cons
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
+    chain_next();                                             // (behind the allocation of tensor memory)
     const uint32_t tmem_base = __shfl_sync(0xffffffffu, s_tmem_base, 0);
     chain_wait();                                             // the workspace operand; earlier readers of what this kernel writes
     // rows of both operands of unit u: (tile of pixels, block)
