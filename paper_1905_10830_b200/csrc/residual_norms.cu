@@ -233,11 +233,14 @@ struct RowRing {
 template <bool kVec>
 struct RowReader {
     uint32_t ring;
-    unsigned long long *full;
+    unsigned long long *full;         // [kRingStages]
+    int *brought;                     // rows asked for so far (the first thread's)
     bool alive;
+    // The block's next row to a slot that its readers are done with, by the first thread, as long as that is alive: the slot's last copy has landed.
     __device__ __forceinline__ void bring(const RowRing &r, long long row, int slot)
     {
         using namespace sm100;
+        ++*brought;
         const uint32_t bar = smem_u32(full + slot), to = ring + (uint32_t)(slot * r.inputs) * r.part_bytes;
         const long long first = row * r.row_bytes, from = first & ~15ll;
         uint32_t bytes = r.row_bytes;
@@ -260,6 +263,7 @@ struct RowReader {
     {
         using namespace sm100;
         if (threadIdx.x == 0) {
+            *brought = 0;
             for (int i = 0; i < r.stages; ++i) mbar_init(smem_u32(full + i), 1);
             mbar_fence_init();
             for (int i = 0; i < r.stages && blockIdx.x + (long long)i * gridDim.x < rows; ++i) bring(r, blockIdx.x + (long long)i * gridDim.x, i);
@@ -275,6 +279,12 @@ struct RowReader {
             tc_dev_set_status(status, TC_ERR_TIMEOUT);
         }
         return ring + (uint32_t)(slot * r.inputs) * r.part_bytes + (kVec ? 0u : (uint32_t)(at * r.row_bytes & 15));
+    }
+    // Behind the last row: where a wait ran out, the copies in flight land before the block's shared memory goes to another.
+    __device__ __forceinline__ void finish(const RowRing &r)
+    {
+        if (threadIdx.x != 0 || alive) return;
+        for (int i = max(0, *brought - r.stages); i < *brought; ++i) sm100::mbar_wait_soon(sm100::smem_u32(full + i % r.stages), (uint32_t)(i / r.stages & 1));
     }
 };
 __device__ __forceinline__ uint4 lds16(uint32_t at)
@@ -320,6 +330,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_ring_kerne
     constexpr int kThreadsRow = kWarps * 32;
     extern __shared__ __align__(16) unsigned char s_ring[];
     __shared__ __align__(8) unsigned long long s_full[kRingStages];
+    __shared__ int s_brought;
     __shared__ float s_part[2][kWarps];
     chain_next();
     chain_wait();
@@ -327,6 +338,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_ring_kerne
     RowReader<true> reader;
     reader.ring = sm100::smem_u32(s_ring);
     reader.full = s_full;
+    reader.brought = &s_brought;
     reader.start(r, a.pixels);
     const float inv_c = 1.0f / (float)a.c, scale = a.scale ? *a.scale : 1.f;
     float wy[kV][8], wx[kV][8];                               // after times the channels' gate; before
@@ -358,7 +370,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_ring_kerne
             for (int j = 0; j < 8; ++j) sum = fmaf(y[j], y[j], sum);
         }
         sum = row_sum<kThreadsRow>(sum, s_part[0]);                // (the block is in step here: all have read the slot)
-        if (threadIdx.x == 0 && row + (long long)r.stages * gridDim.x < a.pixels) reader.bring(r, row + (long long)r.stages * gridDim.x, slot);
+        if (threadIdx.x == 0 && reader.alive && row + (long long)r.stages * gridDim.x < a.pixels) reader.bring(r, row + (long long)r.stages * gridDim.x, slot);
         const float f = (a.after ? inv_sqrt(fmaf(sum, inv_c, a.eps)) : 1.f) * scale;
         sum = 0.f;
 #pragma unroll
@@ -393,6 +405,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_ring_kerne
             __syncthreads();                                  // the row's partial sums are read before the next row's are written
         if (++slot == r.stages) slot = 0;
     }
+    reader.finish(r);
 }
 
 // ---- maps: a pixel's channels lie H W apart ------------------------------------------------------
@@ -1066,6 +1079,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
     constexpr int kThreadsRow = kWarps * 32;
     extern __shared__ __align__(16) unsigned char s_ring[];
     __shared__ __align__(8) unsigned long long s_full[kRingStages];
+    __shared__ int s_brought;
     __shared__ float s_part[2][kWarps][8];
     chain_next();
     chain_wait();
@@ -1073,6 +1087,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
     RowReader<kVec> reader;
     reader.ring = sm100::smem_u32(s_ring);
     reader.full = s_full;
+    reader.brought = &s_brought;
     reader.start(r, a.pixels);
     // parts of a stage: s and dx (with before), y, ds, gate, those that there are
     const uint32_t part = r.part_bytes, at_y = a.before ? 2 * part : 0, at_d = at_y + (a.y ? part : 0), at_g = at_d + (a.ds ? part : 0);
@@ -1131,7 +1146,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
         }
         row_sums<kThreadsRow>(v, s_part[turn & 1]);
         // (the block is in step: the last row's slot is free)
-        if (t == 0 && turn > 0 && row + (long long)(r.stages - 1) * gridDim.x < a.pixels) reader.bring(r, row + (long long)(r.stages - 1) * gridDim.x, last);
+        if (t == 0 && reader.alive && turn > 0 && row + (long long)(r.stages - 1) * gridDim.x < a.pixels) reader.bring(r, row + (long long)(r.stages - 1) * gridDim.x, last);
         const float sums[kSums] = {v[0], v[1], v[2], v[3], v[4], v[5]};
         const PixelFactors f = pixel_factors(sums, a, scale);
         total.add(f.e);
@@ -1172,6 +1187,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) norm_rows_grad_ring_
         last = slot;
         if (++slot == r.stages) slot = 0;
     }
+    reader.finish(r);
     float *const to = a.partial + (long long)blockIdx.x * 2 * a.c;
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
