@@ -648,7 +648,11 @@ _layers = None
 def _layer_calls():
     global _layers
     if _layers is None:
+        from . import build
         lib = load_library()
+        built_for, here = build.layers_built_for()
+        if built_for not in (None, here):
+            raise ImportError(f"{_PKG}/_layers.so was built for {built_for}, this is {here}: run `python -m paper_1905_10830_b200.build`")
         try:
             from . import _layers as module
         except ImportError as e:

@@ -2,7 +2,8 @@
 
 `python -m paper_1905_10830_b200.build` compiles every source under csrc/ into
 `paper_1905_10830_b200/libtc_b200.so` and the layer calls' Python module into `_layers.so`.
-Objects are cached under `_build/` by mtime.
+Objects are cached under `_build/` by mtime, the module by mtime and by the torch and Python it was
+built for.  The codec and the C ABI do not need the module: where it cannot be compiled the library is built all the same.
 """
 from __future__ import annotations
 
@@ -12,6 +13,7 @@ import os
 import subprocess
 import sys
 import sysconfig
+import warnings
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -51,10 +53,22 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
+def layers_built_for() -> tuple[str | None, str]:
+    """The torch and Python that the module of the layer calls was built for (None: not known), and those that run."""
+    import torch
+    here = f"torch {torch.__version__}, {sys.implementation.cache_tag}"
+    try:
+        with open(LAYERS + ".built") as f:
+            return f.read(), here
+    except OSError:
+        return None, here
+
+
 def build_layers(force: bool = False) -> str:
     """The module of the layer calls, against this torch's headers; its libraries are loaded by `import torch`."""
+    built_for, here = layers_built_for()
     newest = max(os.path.getmtime(LAYERS_SRC), os.path.getmtime(os.path.join(ROOT, "include", "tc.h")))
-    if not force and os.path.exists(LAYERS) and os.path.getmtime(LAYERS) >= newest:
+    if not force and os.path.exists(LAYERS) and os.path.getmtime(LAYERS) >= newest and built_for == here:
         return LAYERS
     import torch
     base = os.path.dirname(torch.__file__)
@@ -67,6 +81,8 @@ def build_layers(force: bool = False) -> str:
     if res.returncode != 0:
         raise RuntimeError(f"g++ failed for {LAYERS_SRC}:\n{res.stdout}\n{res.stderr}")
     os.replace(tmp, LAYERS)
+    with open(LAYERS + ".built", "w") as f:
+        f.write(here)
     return LAYERS
 
 
@@ -79,14 +95,27 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(srcs) + 1)) as pool:
         layers = pool.submit(build_layers, force)
         objs = list(pool.map(lambda s: _compile(s, verbose), srcs))
-        layers.result()
     if (not os.path.exists(LIB)) or any(os.path.getmtime(o) > os.path.getmtime(LIB) for o in objs):
         tmp = LIB + f".{os.getpid()}.tmp"
         subprocess.check_call([NVCC, "-shared", "-gencode", "arch=compute_100a,code=sm_100a",
                                "-o", tmp, *objs])
         os.replace(tmp, LIB)
+    try:
+        layers.result()
+    except (RuntimeError, OSError, ImportError) as e:
+        warnings.warn(f"the layer calls' module was not built, the library was: {e}", RuntimeWarning, stacklevel=2)
     return LIB
 
 
+def main(args: list[str]) -> int:
+    print(build_library(force="--force" in args, verbose="-v" in args))
+    try:
+        build_layers()
+    except (RuntimeError, OSError, ImportError) as e:
+        print(e, file=sys.stderr)
+        return 1
+    return 0
+
+
 if __name__ == "__main__":
-    print(build_library(force="--force" in sys.argv, verbose="-v" in sys.argv))
+    sys.exit(main(sys.argv[1:]))
