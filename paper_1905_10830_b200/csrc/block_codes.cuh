@@ -149,12 +149,5 @@ __device__ __forceinline__ void store1(__nv_bfloat16 *p, float f) { *p = __float
 __device__ __forceinline__ void store1(float *p, float f) { *p = f; }
 __device__ __forceinline__ float load1(const __nv_bfloat16 *p) { return __uint_as_float((uint32_t) * reinterpret_cast<const unsigned short *>(p) << 16); }
 __device__ __forceinline__ float load1(const float *p) { return *p; }
-template <typename T>
-__device__ __forceinline__ void store8(T *p, const float (&f)[8], int count)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < count) store1(p + i, f[i]);
-}
 
 }  // namespace blk
