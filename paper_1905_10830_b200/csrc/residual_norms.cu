@@ -1388,8 +1388,10 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) norm_maps_grad_tile_
                 sum1[i] += q.y;
             }
         }
-        // (of a pixel behind the last one all factors are zero: without eps its zeros have infinite ones, and the vectors' sums NaN)
-        const PixelFactors f0 = px.ok0 ? pixel_factors(sum0, a, scale) : PixelFactors{}, f1 = px.ok1 ? pixel_factors(sum1, a, scale) : PixelFactors{};
+        // (the zeros of a pixel behind the last one would have infinite factors without eps, and the vectors' sums be NaN)
+        if (!px.ok0) sum0[0] = sum0[2] = 1.f;
+        if (!px.ok1) sum1[0] = sum1[2] = 1.f;
+        const PixelFactors f0 = pixel_factors(sum0, a, scale), f1 = pixel_factors(sum1, a, scale);
         if (px.ok0) total0.add(f0.e);
         if (px.ok1) total1.add(f1.e);
         const uint64_t r = pair_of(f0.r, f1.r), m = pair_of(-f0.m, -f1.m), q = pair_of(f0.q, f1.q), scale_q = pair_of(scale * f0.q, scale * f1.q);
