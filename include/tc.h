@@ -485,7 +485,8 @@ tc_status tc_quantize_blocks(tc_ctx *ctx, const tc_tensor *x, const tc_blocks *p
 /* out[p][o] = act(bias[o] + sum_k a[p][k] b[o][k]), a [P][K] and b [O][K] block matrices (square or not, each), `out` a tensor of P pixels and
  * O channels, fp32 or bf16; `bias` DEVICE [O] or NULL; act = max(., 0) if `relu`, else none.  Codes are multiplied exactly, each block of 128 is
  * summed by the tensor cores in fp32, scaled, and added in fp32 in ascending order; sums of few, long rows are cut into parts that are added in
- * their order, so a call's result depends on its sizes, types and alignment, not on timing.
+ * their order, so a call's result depends on its sizes, types and alignment, not on timing.  The product of two blocks' scales is taken in fp32 too: it loses bits
+ * below 2^-126, where the largest magnitudes of both blocks multiply to less than 2e-33, and overflows from 2^128 on, 7e43.
  *   layer            a = codes of x by pixels,  b = codes of W (C_out, C_in) by pixels
  *   gradient to x    a = codes of dy by pixels, b = codes of W by channels
  *   gradient to W    a = codes of dy by channels, b = codes of x by channels, out (C_out, C_in, 1, 1)
@@ -498,7 +499,8 @@ tc_status tc_matmul_blocks(tc_ctx *ctx, const tc_blocks *a, const tc_blocks *b, 
 /* The norm after a layer, its gate and scale, the residual sum, and the norm before the next layer, over each pixel's channels:
  *     n = y / sqrt(mean_c y^2 + eps), u = n * after (no `after`: u = y);   s = h + scale * gate * u;
  *     x = s / sqrt(mean_c s^2 + eps) * before
- * Statistics, sums and products in fp32; s and x are rounded once, x is computed from the s that is not rounded yet. */
+ * Statistics, sums and products in fp32; s and x are rounded once, x is computed from the s that is not rounded yet.  The sums of squares have to
+ * stay within fp32's range: magnitudes up to about 1e17, and without eps from 1e-18 on. */
 typedef struct {
     const void *y;             /* layer's output; NULL: s = h, which is not written                     */
     const float *after;        /* DEVICE [C]; NULL: no norm after the layer                             */
@@ -518,7 +520,7 @@ tc_status tc_residual_norms(tc_ctx *ctx, const tc_tensor *h, const tc_norm_param
 /* Gradients of tc_residual_norms at the sum `s` it wrote (y = NULL: at h), from those of x (`dx`, NULL exactly without `before`; the same
  * whether x left as a tensor or as codes) and of s (`ds`, NULL = zero).  dh always; dy where y is given; the others where wanted, each only where
  * its input is given (scale's may be asked for with y).  dx, ds, dh, dy and dgate_map are DEVICE tensors like `s`.  Gradients of vectors are sums over all pixels, in fp32, in an order that does not depend on
- * timing.  Conventions and errors as above. */
+ * timing; scale's carries what its additions round off, and adds the blocks' parts in fp64.  Conventions and errors as above. */
 typedef struct {
     void *dh, *dy;
     void *dgate_map;                             /* required with gate_map               */

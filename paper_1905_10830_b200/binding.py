@@ -616,6 +616,8 @@ def tc_stats(ctx: Context, model: Model, cb: Codebook | None, x: torch.Tensor, *
 # ---- layers between coded maps ---------------------------------------------------------------
 # A single token's calls take the GPU a few microseconds, so their arguments are read and checked, and their tensors made, by a compiled
 # module (binding_layers.cpp) instead of ctypes: a call's host time is 5 to 11 us with it and 10 to 23 without.
+# Like the codec's calls they record nothing for autograd: tensors that require gradients are taken as values, and the gradients are calls of
+# their own (tc_residual_norms_backward; the products' are products of the other codes).
 
 @dataclass
 class Blocks:
@@ -672,7 +674,7 @@ def tc_quantize_blocks(ctx: Context, x: torch.Tensor, *, rows: str = "pixels", s
 def tc_matmul_blocks(ctx: Context, a: Blocks, b: Blocks, *, shape=None, dtype=torch.bfloat16, bias: torch.Tensor | None = None,
                      relu: bool = False, out: torch.Tensor | None = None) -> torch.Tensor:
     """Product of a's rows (the output's pixels) and b's rows (its channels), (N, O, H, W) with `shape` = (N, H, W), by default
-    (rows of a, 1, 1); `bias` [O], `relu` on the result."""
+    (rows of a, 1, 1), or into `out`, whose shape and type count then; `bias` [O], `relu` on the result.  Nothing is recorded for autograd."""
     return (_layers or _layer_calls()).matmul(ctx.ptr.value, ctx.device, _tensor_stream(ctx.device), a, b, shape, dtype, bias, relu, out)
 
 
@@ -681,7 +683,8 @@ def tc_residual_norms(ctx: Context, h: torch.Tensor, y: torch.Tensor | None = No
                       eps: float = 1e-6, blocks: bool | str = False, sum_out: torch.Tensor | None = None, out=None):
     """(s, x): s = h + scale * gate * norm(y) * after, x = norm(s) * before, norms over the channels of each pixel.  x is a
     tensor like h, or with `blocks` its codes by pixels, or with blocks="both" the pair of them (the codes are those of x before it is
-    rounded to h's type); without `before` it is None.  Without `y` s is h itself.  `gate` is [C], or a tensor like y."""
+    rounded to h's type); without `before` it is None.  Without `y` s is h itself.  `gate` is [C], or a tensor like y.  `sum_out` and
+    `out` receive s and x where there are such.  Nothing is recorded for autograd: the gradients are tc_residual_norms_backward's."""
     return (_layers or _layer_calls()).norms(ctx.ptr.value, ctx.device, _tensor_stream(ctx.device), h, y, after, gate, scale, before, eps, blocks, sum_out, out)
 
 

@@ -9,8 +9,9 @@
 //
 // Bound by the bytes of the maps: each is read once and written once.  The gradient's mean_c v n is a sum of D's three parts, so
 // that all sums over a pixel's channels -- s s, t s, y y, and ds, t and s times g after y -- are taken together and
-// a pixel waits for one reduction.  All sums are fp32, in an order that does not depend on the launch's timing; sums over the pixels are first
-// taken by block, and a second kernel adds the blocks' sums in their order.
+// a pixel waits for one reduction.  Sums are fp32, in an order that does not depend on the launch's timing; sums over the pixels are first
+// taken by block, and a second kernel adds the blocks' sums in their order.  scale's gradient, a sum over all values, carries what its additions round
+// off within a block, and its blocks' parts are added in fp64.
 #include "block_codes.cuh"
 #include "sm100_ptx.cuh"
 #include "tc_internal.h"
@@ -24,7 +25,7 @@ __device__ __forceinline__ float inv_sqrt(float v) { return rsqrtf(v); }       /
 
 // ---- single pixels (H W = 1): a pixel's channels are a row in memory ------------------------------
 // kThreadsRow threads a row, kV chunks of eight channels a thread; rows of one warp share a block of eight, and aligned ones of up to 128 channels a
-// warp (a warp each, 200000x64 in bf16: 72 us and 20, gradient 142 and 44).
+// warp (a warp each, 200000x64 in bf16: 72 us and 22, gradient 151 and 51).
 // Rows that cannot be moved 16 bytes at a time (kVec false): a thread's eight values lie 32 apart, so that a warp's are neighbours.
 template <int kThreadsRow>
 __device__ __forceinline__ int chunk_at(int t, int i) { return (i * kThreadsRow + t) * 8; }
@@ -217,7 +218,7 @@ __global__ void __launch_bounds__(kThreadsRow <= 32 ? 256 : kThreadsRow) norm_ro
 // ---- rows on their way to shared memory ------------------------------------------------------
 // Long rows: a block walks rows gridDim.x apart, whose parts of all inputs one thread brings to a ring in shared memory by bulk
 // copies, several rows ahead, so that the memory is at work while the block waits for a row's sums (with a row's loads in
-// registers, and the vectors read again for each row: gradient of 16384x4096 in bf16 297 us and 151, forward 122 and 106).
+// registers, and the vectors read again for each row: gradient of 16384x4096 in bf16 278 us and 158, forward 113 and 107).
 constexpr int kRingInputs = 5, kRingStages = 8;
 constexpr size_t kRingSm = 200 * 1024;                        // of an SM's shared memory, for all its blocks' rings
 struct RowRing {
@@ -228,7 +229,7 @@ struct RowRing {
     long long rows;
 };
 // Rows that do not begin at a multiple of 16 bytes (kVec false; the inputs do) come with the bytes around them up to one, and are read
-// value by value from where they begin: the gradient only (16000x4095 in bf16 350 us without the ring and 221; the forward, whose
+// value by value from where they begin: the gradient only (16000x4095 in bf16 419 us without the ring and 225; the forward, whose
 // instructions bound it with such rows, 40000x1001 106 and 111).
 template <bool kVec>
 struct RowReader {
@@ -500,7 +501,7 @@ __global__ void __launch_bounds__(256) norm_maps_kernel(NormArgs a)
 }
 
 // The same with all channels of a tile of kPx pixels in shared memory, where they fit: each value is fetched once, many at a time, and
-// the vectors once a block (256x14x14 x 1024, bf16: 962 us and 169).  A lane has two pixels, whose values one instruction works on, and
+// the vectors once a block (256x14x14 x 1024, bf16: 970 us and 138, the gradient 516 and 239).  A lane has two pixels, whose values one instruction works on, and
 // eight channels in a row of every kStep.
 constexpr size_t kTileSm = 220 * 1024, kTileStatic = 14 * 1024;       // of an SM's shared memory; what a block has beside its tile
 template <typename T, int kPx, int kWarps>
@@ -1477,8 +1478,8 @@ __global__ void __launch_bounds__(32 * kWarps, 16 / kWarps) norm_maps_grad_tile_
     if (threadIdx.x == 0) a.partial_scale[blockIdx.x] = sum_scale;
 }
 
-// The blocks' sums, in their order: 32 channels a block, every kVectorWarps-th of the blocks' sums a warp (of up to 592: what it waits for is
-// memory, one sum after the other).
+// The blocks' sums, in their order: 32 channels a block, every kVectorWarps-th of the blocks' sums a warp (of up to eight an SM, 1184 on
+// 148: what it waits for is memory, one sum after the other).
 constexpr int kVectorWarps = 32;
 __global__ void __launch_bounds__(kVectorWarps * 32) norm_vectors_kernel(NormGradArgs a, int blocks)
 {
@@ -1575,11 +1576,14 @@ bool pixel_pairs(int hw, P... p)
 }
 
 // Tile of a maps' kernel: as many pixels as fit, but no more than 16 while the tiles are fewer than two an SM, and 64 only of up to 64 channels,
-// which leave half of the warps idle with 32; 0 where not even eight fit.  `two`: rather tiles of which two fit an SM, the forward's (431x7x7 x 944
-// in bf16 181 us and 122, 60x28x28 x 512 in fp32 105 and 77; the gradient has no use of them: 256x14x14 x 1024 in bf16 290 us and 518).  Up to 32 channels
-// keep four warps busy: more blocks of those (437x20x20 x 25 in bf16, forward 24 us and 16, gradient 65 and 33).  Where one tile of the
-// gradient's fits an SM and its pixels come one at a time, sixteen warps work on it (431x7x7 x 944 in bf16 243 us and 190; by
-// fours it costs time: 256x14x14 x 1024 in fp32 394 and 445).
+// which leave half of the warps idle with 32.  0 where not even eight fit, of about 1250 channels on for the gradient in fp32 (1030 with a gate for
+// each value), 2200 (1850) in bf16, 2390 (1700) and 4060 (3010) for the forward: those maps take the kernels that read them again for each pass, 1.5 to five
+// times as long (gradient of 1248x7x7 x 128 in fp32 163 us, of 1256 310; forward of 4056x1x8192 in bf16 225, of 4064 1166).
+// `two`: rather tiles of which two fit an SM, the forward's (944x7x7 x 431 in bf16 185 us and 127, 512x28x28 x 60 in fp32 105 and 78; the
+// gradient of the first takes 204 with one and 223 with two, though even sides in fp32 would gain: 256x14x14 x 1024 345 and 302).  Up to 32 channels
+// keep four warps busy: more blocks of those (25x20x20 x 437 in bf16, forward 26 us and 17, gradient 57 and 37).  Where one tile of the
+// gradient's fits an SM and its pixels come one at a time, sixteen warps work on it (944x7x7 x 431 in bf16 260 us and 204; by
+// fours it costs time in fp32, 512x28x28 x 60 172 and 195, and gains a little in bf16, 944x8x8 x 200 83 and 79).
 struct MapPlan {
     int px = 0, warps = 8;
     size_t smem = 0;
@@ -1650,8 +1654,8 @@ cudaError_t launch_grad_rows(const NormGradArgs &a, int blocks, cudaStream_t s)
 // Threads of a row of up to 256 channels.
 int short_row_threads(const NormGradArgs &a) { return !a.vec || a.c > 128 ? 32 : a.c > 64 ? 16 : 8; }
 
-// With the ring of rows where there is one: two chunks a thread of bf16, whose unpacking and sums bound it (16384x4096 209 us with one
-// and 151); one of fp32, of whose rows two would not fit two blocks' rings.  Blocks of 512 threads an SM in all.
+// With the ring of rows where there is one: two chunks a thread of bf16, whose unpacking and sums bound it (16384x4096 205 us with one
+// and 158); one of fp32, of whose rows two would not fit two blocks' rings.  Blocks of 512 threads an SM in all.
 constexpr int ring_chunks(int warps, int size) { return warps <= 2 ? 1 : warps > 16 ? warps / 16 : size == 2 ? 2 : 1; }
 // Rows of up to 256 kWarps channels.
 template <typename T, int kWarps>
@@ -1660,7 +1664,7 @@ cudaError_t launch_grad(const NormGradArgs &a, int blocks, cudaStream_t s)
     constexpr int kRingV = ring_chunks(kWarps, sizeof(T)), kRingWarps = kWarps / kRingV;
     const RowRing r = make_ring({a.before ? a.s : nullptr, a.before ? a.dx : nullptr, a.y, a.ds, a.gate_map}, a.c, sizeof(T), a.pixels, blocks, 16 / kRingWarps, a.vec);
     if (r.stages && a.vec) return launch_ring<norm_rows_grad_ring_kernel<T, kRingWarps, kRingV, true>>(a.device, a, r, blocks, kRingWarps * 32, s);
-    if constexpr (kWarps > 2)                                 // (unaligned rows of up to 512 channels: 20000x301 47 us without and 55 with)
+    if constexpr (kWarps > 2)                                 // (unaligned rows of up to 512 channels: 20000x301 in fp32 51 us without and 55 with, in bf16 61 and 56)
         if (r.stages) return launch_ring<norm_rows_grad_ring_kernel<T, kRingWarps, kRingV, false>>(a.device, a, r, blocks, kRingWarps * 32, s);
     return launch_grad_rows<T, 32 * kWarps, 1>(a, blocks, s);
 }

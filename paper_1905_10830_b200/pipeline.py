@@ -80,7 +80,8 @@ def run_chain(ctx: tc.Context, stages: Sequence[Callable[[torch.Tensor], torch.T
 class ResidualBlock:
     """A residual block on the pixels' vectors, to stand between two coded maps (a stage of the functions above) or to be
     trained: s = h + scale * gate * norm(W norm(h) before) after, the 1 x 1 convolution W [C][C] as a product of 8-bit blocks.
-    Vectors are float32 CUDA tensors [C] (`scale`: one value); `gate` and `scale` may be None."""
+    Vectors are float32 CUDA tensors [C] (`scale`: one value); `gate` and `scale` may be None.  Nothing is recorded for autograd: a
+    training step takes its gradients from `gradients`."""
 
     def __init__(self, ctx: tc.Context, weight: torch.Tensor, *, before: torch.Tensor, after: torch.Tensor,
                  gate: torch.Tensor | None = None, scale: torch.Tensor | None = None, eps: float = 1e-6):
