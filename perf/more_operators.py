@@ -163,7 +163,7 @@ def _rows(x, kind):
 def _codes(m):
     """Codes [R][C] and scales [R] of a matrix: scale = max|x| / 127 rounded to 32 bits, code = the integer nearest to x / scale."""
     m = m.float()
-    scale = m.abs().amax(1).clamp_min(SMALLEST) / 127.0
+    scale = (m.abs().amax(1).clamp_min(SMALLEST).double() / 127.0).float()     # (a quotient of 32 bits by a constant is a product)
     return (m.double() / scale.double()[:, None]).round().to(torch.int8), scale
 
 
