@@ -529,6 +529,37 @@ typedef struct {
 tc_status tc_residual_norms_backward(tc_ctx *ctx, const tc_tensor *s, const tc_norm_params *params, const void *dx, const void *ds,
                                      const tc_norm_grads *out, void *cuda_stream);
 
+/* ---------------------------------------------------------------------------------------
+ * The same layers on 8-bit integers (the paper quantises weights and activations so, Table C.1), with one scale a row.
+ *
+ * tc_rows: a matrix of integers of -128 to 127 with a scale for each row; a value is code * scale.
+ *   codes   DEVICE [rows][ld] bytes, 16-byte aligned; ld >= cols, a multiple of 16.  Bytes behind a row's `cols` are never used.
+ *   scales  DEVICE float [rows]
+ * ------------------------------------------------------------------------------------- */
+typedef struct {
+    void *codes;
+    float *scales;
+    int64_t ld;
+    int32_t rows, cols;
+} tc_rows;
+
+/* Codes of `x`, by its pixels ([P][C]), by its channels ([C][P]), or both; either may be NULL (see tc_quantize_blocks for what reads which).
+ *     scale = fl(max|x| / 127) over the row (max|x| at least 2^-100), code = the integer nearest to x / scale (the quotient of the real numbers,
+ * ties to even), -127 to 127.  A row that holds an infinity or a NaN gets a NaN for its scale and zeros for its codes: everything computed from
+ * it is NaN.  A tensor whose channels are neighbours in memory is one of P pixels of 1 x 1.  Rows that do not lie one after the other in memory have
+ * their maxima in the context's arena.  May be captured into a graph.
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 - 256 pixels, more than 2^22 channels), CUDA. */
+tc_status tc_quantize_rows(tc_ctx *ctx, const tc_tensor *x, const tc_rows *pixels, const tc_rows *channels, void *cuda_stream);
+
+/* out[p][o] = act(fl(fl(fl(sum_k a[p][k] b[o][k]) sa[p]) sb[o]) + bias[o]), a [P][K] and b [O][K], `out` a tensor of P pixels and O channels, fp32 or
+ * bf16 (a tensor whose channels are neighbours in memory is one of P pixels of 1 x 1); `bias` DEVICE [O] or NULL; act = max(., 0) if `relu`, else
+ * none.  The sum is exact and rounded to fp32 once, each further step to fp32, the result to the output's type: it depends on the values alone, not on sizes,
+ * alignment or timing.  Operands by layer and gradient as with tc_matmul_blocks.  With K = 0 the sums are empty (no scale is read).  `out` must not
+ * overlap the operands.  Partial sums live in the context's arena (where that memory cannot be had, each sum is taken in one part; sums
+ * of more than 130944 codes fail then: CUDA).  May be captured into a graph.
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 - 256 rows, more than 2^30 tiles), CUDA; TIMEOUT by tc_get_status. */
+tc_status tc_matmul_rows(tc_ctx *ctx, const tc_rows *a, const tc_rows *b, const float *bias, int32_t relu, const tc_tensor *out, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -65,6 +65,10 @@ class _Blocks(C.Structure):
                 ("square", C.c_int32)]
 
 
+class _Rows(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("ld", C.c_int64), ("rows", C.c_int32), ("cols", C.c_int32)]
+
+
 class _NormParams(C.Structure):
     _fields_ = [("y", C.c_void_p), ("after", C.c_void_p), ("gate", C.c_void_p), ("gate_map", C.c_void_p),
                 ("scale", C.c_void_p), ("before", C.c_void_p), ("eps", C.c_float)]
@@ -152,6 +156,8 @@ def load_library() -> C.CDLL:
         lib.tc_matmul_blocks.argtypes = [vp, vp, vp, vp, i32, vp, vp]
         lib.tc_residual_norms.argtypes = [vp] * 7
         lib.tc_residual_norms_backward.argtypes = [vp] * 7
+        lib.tc_quantize_rows.argtypes = [vp] * 5
+        lib.tc_matmul_rows.argtypes = [vp, vp, vp, vp, i32, vp, vp]
         _lib = lib
     return _lib
 
@@ -644,6 +650,26 @@ class Blocks:
         return self.codes[:, :self.cols].float() * scales[:, :self.rows].t().repeat_interleave(128, 1)[:, :self.cols]
 
 
+@dataclass
+class Rows:
+    """A matrix of 8-bit integers with a scale for each row: a value is code * scale (tc_rows in include/tc.h has the layout)."""
+    codes: torch.Tensor        # int8 [rows, cols rounded up to a multiple of 16]
+    scales: torch.Tensor       # float32 [rows]
+    cols: int
+
+    @property
+    def rows(self) -> int:
+        return self.codes.shape[0]
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device="cuda") -> "Rows":
+        return cls(torch.empty((rows, -(-cols // 16) * 16), dtype=torch.int8, device=device), torch.empty(rows, dtype=torch.float32, device=device), cols)
+
+    def dequantize(self) -> torch.Tensor:
+        """The values the codes stand for, float32 [rows, cols] (for inspection; no product reads them)."""
+        return self.codes[:, :self.cols].float() * self.scales[:, None]
+
+
 _layers = None
 
 
@@ -659,8 +685,7 @@ def _layer_calls():
             from . import _layers as module
         except ImportError as e:
             raise ImportError(f"{_PKG}/_layers.so cannot be loaded ({e}): run `python -m paper_1905_10830_b200.build`") from e
-        module.init(*[C.cast(getattr(lib, name), C.c_void_p).value
-                      for name in ("tc_quantize_blocks", "tc_matmul_blocks", "tc_residual_norms", "tc_residual_norms_backward")], TcError, Blocks)
+        module.init({name: C.cast(getattr(lib, name), C.c_void_p).value for name in module.entry_points}, TcError, Blocks, Rows)
         _layers = module
     return _layers
 
@@ -704,3 +729,20 @@ def tc_residual_norms_backward(ctx: Context, s: torch.Tensor, y: torch.Tensor | 
     """Gradients at the sum `s` that tc_residual_norms returned, from the gradients `dx` of x (None without `before`) and `ds` of s
     (None: zero)."""
     return NormGrads._make((_layers or _layer_calls()).backward(ctx.ptr.value, ctx.device, _tensor_stream(ctx.device), s, dx, ds, y, after, gate, scale, before, eps))
+
+
+# ---- layers on 8-bit integers ----------------------------------------------------------------
+# Tensors of these calls are dense NCHW, or have their channels as neighbours in memory (torch.channels_last), in which a pixel's row is.
+
+def tc_quantize_rows(ctx: Context, x: torch.Tensor, *, rows: str = "pixels", out=None):
+    """Codes of `x` (N, C, H, W), contiguous or channels_last, with one scale a row: a row for each pixel ("pixels"), for each channel ("channels"), or "both" as
+    a pair.  `out` reuses the Rows of an earlier call."""
+    return (_layers or _layer_calls()).quantize_rows(ctx.ptr.value, ctx.device, _tensor_stream(ctx.device), x, rows, out)
+
+
+def tc_matmul_rows(ctx: Context, a: Rows, b: Rows, *, shape=None, dtype=torch.bfloat16, bias: torch.Tensor | None = None, relu: bool = False,
+                   channels_last: bool = False, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Product of a's rows (the output's pixels) and b's rows (its channels), (N, O, H, W) with `shape` = (N, H, W), by default (rows of a, 1, 1), contiguous
+    or `channels_last`; or into `out`, contiguous or channels_last, whose shape and type count then; `bias` [O], `relu` on the result.  Nothing is recorded for
+    autograd: the gradients are products of the other codes."""
+    return (_layers or _layer_calls()).matmul_rows(ctx.ptr.value, ctx.device, _tensor_stream(ctx.device), a, b, shape, dtype, bias, relu, channels_last, out)

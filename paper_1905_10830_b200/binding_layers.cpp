@@ -1,4 +1,4 @@
-// The Python side of the layer calls (tc_quantize_blocks, tc_matmul_blocks, tc_residual_norms and its backward), as a module of
+// The Python side of the layer calls (codes, their products, norms and their gradients), as a module of
 // CPython functions: a single token's call takes the GPU 2 to 7 us, and reading, checking and making its tensors took
 // Python and ctypes 6 to 19 us.  It checks tensors, makes those that are returned and calls the C ABI, whose entry points it is
 // given as addresses; nothing is computed here.
@@ -19,7 +19,13 @@ decltype(&tc_quantize_blocks) call_quantize = nullptr;
 decltype(&tc_matmul_blocks) call_matmul = nullptr;
 decltype(&tc_residual_norms) call_norms = nullptr;
 decltype(&tc_residual_norms_backward) call_backward = nullptr;
+decltype(&tc_quantize_rows) call_quantize_rows = nullptr;
+decltype(&tc_matmul_rows) call_matmul_rows = nullptr;
+struct EntryPoint { const char *name; void *at; };                   // of the C ABI, and the pointer that keeps it
+const EntryPoint entry_points[] = {{"tc_quantize_blocks", &call_quantize}, {"tc_matmul_blocks", &call_matmul}, {"tc_residual_norms", &call_norms},
+                                   {"tc_residual_norms_backward", &call_backward}, {"tc_quantize_rows", &call_quantize_rows}, {"tc_matmul_rows", &call_matmul_rows}};
 PyObject *error_type = nullptr, *blocks_type = nullptr;              // TcError(code, where); Blocks(codes, scales, cols, square)
+PyObject *rows_type = nullptr;                                       // Rows(codes, scales, cols)
 PyObject *name_codes = nullptr, *name_scales = nullptr, *name_cols = nullptr, *name_square = nullptr;
 
 struct Bad { std::string what; };                                    // a ValueError
@@ -77,6 +83,18 @@ tc_tensor map_of(const at::Tensor &x, int device)
     for (int i = 0; i < 4; ++i)
         if (x.size(i) > INT32_MAX) throw Bad{"tensor sides must fit 32 bits"};
     return tc_tensor{x.data_ptr(), (int32_t)x.size(0), (int32_t)x.size(1), (int32_t)x.size(2), (int32_t)x.size(3), type == at::kFloat ? TC_F32 : TC_BF16};
+}
+bool channels_last(const at::Tensor &x) { return x.dim() == 4 && x.is_contiguous(at::MemoryFormat::ChannelsLast); }
+// The same of a tensor whose channels may be neighbours in memory: pixels of 1 x 1 then.
+tc_tensor map_of_either(const at::Tensor &x, int device)
+{
+    if (x.dim() == 4 && !x.is_contiguous() && channels_last(x)) {
+        tc_tensor t = map_of(x.permute({0, 2, 3, 1}), device);       // (its sides and type are checked; the C dimension is the last)
+        const int64_t pixels = (int64_t)t.n * t.c * t.h;
+        if (pixels > INT32_MAX) throw Bad{"a channels_last tensor's pixels must fit 32 bits"};
+        return tc_tensor{t.data, (int32_t)pixels, t.w, 1, 1, t.dtype};
+    }
+    return map_of(x, device);
 }
 int64_t pixels_of(const tc_tensor &t) { return (int64_t)t.n * t.h * t.w; }
 
@@ -146,6 +164,37 @@ tc_blocks given_blocks(PyObject *o, int device)
     return tc_blocks{codes.data_ptr(), (float *)scales.data_ptr(), codes.size(1), (int32_t)codes.size(0), (int32_t)cols, square};
 }
 
+// Rows: the same.
+struct RowsRef {
+    Ref object;
+    tc_rows rows{};
+};
+RowsRef new_rows(int64_t rows, int64_t cols, int device)
+{
+    RowsRef r;
+    if (rows > INT32_MAX || cols > INT32_MAX) throw Bad{"matrix of integers: rows and cols must fit 32 bits"};
+    const int64_t ld = (cols + 15) / 16 * 16;
+    const at::Tensor codes = make({rows, ld}, at::kChar, device), scales = make({rows}, at::kFloat, device);
+    Ref c = wrap(codes), s = wrap(scales), n(PyLong_FromLongLong(cols));
+    PyObject *const args[3] = {c.p, s.p, n.p};
+    r.object = Ref(PyObject_Vectorcall(rows_type, args, 3, nullptr));
+    r.rows = tc_rows{codes.data_ptr(), (float *)scales.data_ptr(), ld, (int32_t)rows, (int32_t)cols};
+    return r;
+}
+tc_rows given_rows(PyObject *o, int device)
+{
+    Ref c(PyObject_GetAttr(o, name_codes)), s(PyObject_GetAttr(o, name_scales)), n(PyObject_GetAttr(o, name_cols));
+    const at::Tensor &codes = tensor_of(c.p), &scales = tensor_of(s.p);
+    const int64_t cols = PyLong_AsLongLong(n.p);
+    if (PyErr_Occurred()) throw Raised{};
+    if (!on_device(codes, device) || !on_device(scales, device) || codes.dim() != 2 || scales.dim() != 1 || codes.scalar_type() != at::kChar ||
+        scales.scalar_type() != at::kFloat)
+        throw Bad{"matrices of integers have contiguous int8 codes [rows, ld] and float32 scales [rows] on the context's device"};
+    if (cols < 0 || cols > codes.size(1) || scales.size(0) != codes.size(0) || codes.size(0) > INT32_MAX || codes.size(1) > INT32_MAX)
+        throw Bad{"matrix of integers: codes, scales and cols do not belong together"};
+    return tc_rows{codes.data_ptr(), (float *)scales.data_ptr(), codes.size(1), (int32_t)codes.size(0), (int32_t)cols};
+}
+
 template <typename F>
 PyObject *guarded(PyObject *const *args, Py_ssize_t given, Py_ssize_t wanted, F body)
 {
@@ -207,6 +256,24 @@ PyObject *quantize(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// A new tensor (N, O, H, W) for rows of the given number, by the caller's shape (N, H, W) or None and dtype.
+at::Tensor make_output(PyObject *shape_arg, PyObject *dtype, int64_t rows, int64_t channels, bool last, int device)
+{
+    int64_t shape[3] = {rows, 1, 1};
+    if (shape_arg != Py_None) {
+        Ref s(PySequence_Tuple(shape_arg));
+        if (PyTuple_GET_SIZE(s.p) != 3) throw Bad{"shape: expected (N, H, W)"};
+        for (int i = 0; i < 3; ++i) shape[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(s.p, i));
+        if (PyErr_Occurred()) throw Raised{};
+    }
+    const at::ScalarType type = THPDtype_Check(dtype) ? ((THPDtype *)dtype)->scalar_type : at::kInt;
+    if (type != at::kFloat && type != at::kBFloat16) throw Bad{"dtype must be float32 or bfloat16"};
+    for (const int64_t v : shape)
+        if (v < 0 || v > INT32_MAX) throw Bad{"shape: expected (N, H, W)"};
+    if (last) return make({shape[0], shape[1], shape[2], channels}, type, device).permute({0, 3, 1, 2});
+    return make({shape[0], channels, shape[1], shape[2]}, type, device);
+}
+
 // a, b, shape, dtype, bias, relu, out
 PyObject *matmul(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -217,18 +284,7 @@ PyObject *matmul(PyObject *, PyObject *const *args, Py_ssize_t n)
         Ref made;
         PyObject *out = a[6];
         if (out == Py_None) {
-            int64_t shape[3] = {ma.rows, 1, 1};
-            if (a[2] != Py_None) {
-                Ref s(PySequence_Tuple(a[2]));
-                if (PyTuple_GET_SIZE(s.p) != 3) throw Bad{"shape: expected (N, H, W)"};
-                for (int i = 0; i < 3; ++i) shape[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(s.p, i));
-                if (PyErr_Occurred()) throw Raised{};
-            }
-            const at::ScalarType type = THPDtype_Check(a[3]) ? ((THPDtype *)a[3])->scalar_type : at::kInt;
-            if (type != at::kFloat && type != at::kBFloat16) throw Bad{"dtype must be float32 or bfloat16"};
-            for (const int64_t v : shape)
-                if (v < 0 || v > INT32_MAX) throw Bad{"shape: expected (N, H, W)"};
-            made = wrap(make({shape[0], mb.rows, shape[1], shape[2]}, type, c.device));
+            made = wrap(make_output(a[2], a[3], ma.rows, mb.rows, false, c.device));
             out = made.p;
         }
         const tc_tensor t = map_of(tensor_of(out), c.device);
@@ -322,18 +378,76 @@ PyObject *backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
-// addresses of the four entry points, TcError, Blocks
+// x, rows, out
+PyObject *quantize_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded(args, n, 6, [](const Call &c, PyObject *const *a) -> PyObject * {
+        const tc_tensor x = map_of_either(tensor_of(a[0]), c.device);
+        const char *kind = PyUnicode_Check(a[1]) ? PyUnicode_AsUTF8(a[1]) : "";
+        if (!kind) throw Raised{};
+        const bool both = !strcmp(kind, "both"), pixels = both || !strcmp(kind, "pixels"), channels = both || !strcmp(kind, "channels");
+        if (!pixels && !channels) throw Bad{"rows: \"pixels\", \"channels\" or \"both\""};
+        PyObject *outs[2] = {a[2], a[2]};
+        Ref pair;
+        if (a[2] != Py_None && both) {
+            pair = Ref(PySequence_Tuple(a[2]));
+            if (PyTuple_GET_SIZE(pair.p) != 2) throw Bad{"out: Rows as this call returns them"};
+            outs[0] = PyTuple_GET_ITEM(pair.p, 0);
+            outs[1] = PyTuple_GET_ITEM(pair.p, 1);
+        }
+        RowsRef r[2];
+        const int64_t p = pixels_of(x);
+        for (int i = 0; i < 2; ++i) {
+            if (!(i ? channels : pixels)) continue;
+            if (a[2] == Py_None) r[i] = new_rows(i ? x.c : p, i ? p : x.c, c.device);
+            else {
+                r[i].rows = given_rows(outs[i], c.device);
+                Py_INCREF(outs[i]);
+                r[i].object = Ref(outs[i]);
+            }
+        }
+        c.check(unlocked([&] { return call_quantize_rows(c.ctx, &x, pixels ? &r[0].rows : nullptr, channels ? &r[1].rows : nullptr, c.stream); }), "tc_quantize_rows");
+        if (both) return PyTuple_Pack(2, r[0].object.p, r[1].object.p);
+        return r[pixels ? 0 : 1].object.give();
+    });
+}
+
+// a, b, shape, dtype, bias, relu, channels_last, out
+PyObject *matmul_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded(args, n, 11, [](const Call &c, PyObject *const *a) -> PyObject * {
+        const tc_rows ma = given_rows(a[0], c.device), mb = given_rows(a[1], c.device);
+        const int relu = PyObject_IsTrue(a[5]), last = PyObject_IsTrue(a[6]);
+        if (relu < 0 || last < 0) throw Raised{};
+        Ref made;
+        PyObject *out = a[7];
+        if (out == Py_None) {
+            made = wrap(make_output(a[2], a[3], ma.rows, mb.rows, last, c.device));
+            out = made.p;
+        }
+        const at::Tensor &to = tensor_of(out);
+        const tc_tensor t = map_of_either(to, c.device);
+        if (out != made.p && to.size(1) != mb.rows) throw Bad{"out: expected a tensor whose channels are b's rows"};
+        const float *bias = vector(a[4], mb.rows, c.device, "bias");
+        c.check(unlocked([&] { return call_matmul_rows(c.ctx, &ma, &mb, bias, relu, &t, c.stream); }), "tc_matmul_rows");
+        Py_INCREF(out);
+        return out;
+    });
+}
+
+// addresses of the entry points by name, TcError, Blocks, Rows
 PyObject *init(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
-    if (n != 6) { PyErr_SetString(PyExc_ValueError, "wrong number of arguments"); return nullptr; }
-    call_quantize = (decltype(call_quantize))PyLong_AsVoidPtr(args[0]);
-    call_matmul = (decltype(call_matmul))PyLong_AsVoidPtr(args[1]);
-    call_norms = (decltype(call_norms))PyLong_AsVoidPtr(args[2]);
-    call_backward = (decltype(call_backward))PyLong_AsVoidPtr(args[3]);
-    Py_INCREF(args[4]);
-    Py_INCREF(args[5]);
-    error_type = args[4];
-    blocks_type = args[5];
+    if (n != 4 || !PyDict_Check(args[0])) { PyErr_SetString(PyExc_ValueError, "wrong arguments"); return nullptr; }
+    for (const EntryPoint &e : entry_points) {
+        PyObject *const at = PyDict_GetItemString(args[0], e.name);
+        if (!at) { PyErr_SetString(PyExc_ValueError, e.name); return nullptr; }
+        *(void **)e.at = PyLong_AsVoidPtr(at);
+    }
+    for (int i = 1; i < 4; ++i) Py_INCREF(args[i]);
+    error_type = args[1];
+    blocks_type = args[2];
+    rows_type = args[3];
     name_codes = PyUnicode_InternFromString("codes");
     name_scales = PyUnicode_InternFromString("scales");
     name_cols = PyUnicode_InternFromString("cols");
@@ -347,9 +461,17 @@ PyMethodDef methods[] = {{"init", (PyCFunction)(void *)init, METH_FASTCALL, null
                          {"matmul", (PyCFunction)(void *)matmul, METH_FASTCALL, nullptr},
                          {"norms", (PyCFunction)(void *)norms, METH_FASTCALL, nullptr},
                          {"backward", (PyCFunction)(void *)backward, METH_FASTCALL, nullptr},
+                         {"quantize_rows", (PyCFunction)(void *)quantize_rows, METH_FASTCALL, nullptr},
+                         {"matmul_rows", (PyCFunction)(void *)matmul_rows, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_layers", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__layers(void) { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__layers(void)
+{
+    PyObject *const m = PyModule_Create(&module), *const names = PyTuple_New(sizeof entry_points / sizeof *entry_points);
+    for (size_t i = 0; names && i < sizeof entry_points / sizeof *entry_points; ++i) PyTuple_SET_ITEM(names, i, PyUnicode_FromString(entry_points[i].name));
+    if (!m || !names || PyErr_Occurred() || PyModule_AddObject(m, "entry_points", names) < 0) { Py_XDECREF(names); Py_XDECREF(m); return nullptr; }
+    return m;
+}

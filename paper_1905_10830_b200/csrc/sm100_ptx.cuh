@@ -351,6 +351,18 @@ __device__ __forceinline__ uint32_t make_idesc_e4m3(int m, int n)
     return d;
 }
 
+// Instruction descriptor for kind::i8 with signed 8-bit operands, both K-major, and 32-bit integer accumulation (which wraps).
+__device__ __forceinline__ uint32_t make_idesc_s8(int m, int n)
+{
+    uint32_t d = 0;
+    d |= 2u << 4;                          // accumulator format: s32
+    d |= 1u << 7;                          // A: signed
+    d |= 1u << 10;                         // B: signed
+    d |= (uint32_t)(n >> 3) << 17;
+    d |= (uint32_t)(m >> 4) << 24;
+    return d;
+}
+
 // D[tmem] (+)= A[smem] * B[smem]; issued by one thread.
 __device__ __forceinline__ void mma_bf16_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
                                             uint32_t accumulate)
@@ -443,6 +455,20 @@ __device__ __forceinline__ void mma_e4m3_ss_guarded(uint32_t d_tmem, uint32_t a_
         ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(issue)
         : "memory");
 }
+// The same of signed 8-bit integers.
+__device__ __forceinline__ void mma_s8_ss_guarded(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi,
+                                                  uint32_t idesc, uint32_t accumulate, uint32_t issue)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, g;\n\t.reg .b64 ad, bd;\n\t"
+        "mov.b64 ad, {%1, %2};\n\t"
+        "mov.b64 bd, {%3, %4};\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "setp.ne.b32 g, %7, 0;\n\t"
+        "@g tcgen05.mma.cta_group::1.kind::i8 [%0], ad, bd, %5, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(issue)
+        : "memory");
+}
 __device__ __forceinline__ void mma_commit_guarded(uint32_t bar, uint32_t issue)
 {
     asm volatile(
@@ -500,6 +526,19 @@ __device__ __forceinline__ void mma_e4m3_ss_pair_guarded(uint32_t d_tmem, uint32
         "setp.ne.b32 p, %6, 0;\n\t"
         "setp.ne.b32 g, %7, 0;\n\t"
         "@g tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], ad, bd, %5, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(issue)
+        : "memory");
+}
+__device__ __forceinline__ void mma_s8_ss_pair_guarded(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi,
+                                                       uint32_t idesc, uint32_t accumulate, uint32_t issue)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, g;\n\t.reg .b64 ad, bd;\n\t"
+        "mov.b64 ad, {%1, %2};\n\t"
+        "mov.b64 bd, {%3, %4};\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "setp.ne.b32 g, %7, 0;\n\t"
+        "@g tcgen05.mma.cta_group::2.kind::i8 [%0], ad, bd, %5, p;\n\t}"
         ::"r"(d_tmem), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(issue)
         : "memory");
 }

@@ -1836,6 +1836,22 @@ BlockMatrix block_matrix(const tc_blocks *b)
     return m;
 }
 
+bool valid_rows(const tc_rows *r)
+{
+    return r && r->rows >= 0 && r->cols >= 0 && r->ld >= r->cols && r->ld % 16 == 0 &&
+           (((r->codes && r->scales) && ((uintptr_t)r->codes & 15u) == 0 && ((uintptr_t)r->scales & 3u) == 0) || r->rows == 0 || r->cols == 0);
+}
+RowMatrix row_matrix(const tc_rows *r)
+{
+    RowMatrix m;
+    if (!r) return m;
+    m.codes = (uint8_t *)r->codes;
+    m.scales = r->scales;
+    m.ld = r->ld;
+    m.rows = r->rows;
+    return m;
+}
+
 // Byte ranges of a call's buffers: its outputs overlap neither one another nor its inputs.
 struct Ranges {
     struct Range { const char *first, *end; bool out; };
@@ -1848,6 +1864,12 @@ struct Ranges {
         if (!b) return;
         add(b->codes, (size_t)b->rows * b->ld, out);
         add(b->scales, (size_t)((b->cols + 127ll) / 128) * block_matrix(b).scale_ld * sizeof(float), out);
+    }
+    void add(const tc_rows *r, bool out)
+    {
+        if (!r) return;
+        add(r->codes, (size_t)r->rows * r->ld, out);
+        add(r->scales, r->cols ? (size_t)r->rows * sizeof(float) : 0, out);
     }
     bool apart() const
     {
@@ -2023,6 +2045,53 @@ tc_status tc_residual_norms_backward(tc_ctx *ctx, const tc_tensor *s, const tc_n
     a.status = ctx->d_status;
     a.partial_scale = a.partial + (size_t)blocks * 2 * a.c;
     return tc_launch_residual_norms_backward(a, s->dtype, blocks, ctx->sm_count, (cudaStream_t)cuda_stream);
+}
+
+tc_status tc_quantize_rows(tc_ctx *ctx, const tc_tensor *x, const tc_rows *pixels, const tc_rows *channels, void *cuda_stream)
+{
+    if (!ctx || !aligned_tensor(x) || (!pixels && !channels)) return TC_ERR_INVALID_ARG;
+    const long long p = pixels_of(x);
+    if (p > kMostRows || x->c > 1 << 22) return TC_ERR_UNSUPPORTED;
+    if (pixels && (!valid_rows(pixels) || pixels->rows != p || pixels->cols != x->c)) return TC_ERR_INVALID_ARG;
+    if (channels && (!valid_rows(channels) || channels->rows != x->c || channels->cols != p)) return TC_ERR_INVALID_ARG;
+    Ranges ranges;
+    ranges.add(x, false);
+    ranges.add(pixels, true);
+    ranges.add(channels, true);
+    if (!ranges.apart()) return TC_ERR_INVALID_ARG;
+    if (p == 0) return TC_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return TC_ERR_CUDA;
+    RowQuantizeArgs a{x->data, x->dtype, x->n, x->c, x->h * x->w, row_matrix(pixels), row_matrix(channels)};
+    const size_t bytes = tc_quantize_rows_workspace(a);
+    CallScratch scratch;
+    const tc_status st = call_scratch(ctx, bytes, bytes, (cudaStream_t)cuda_stream, &scratch);
+    if (st != TC_OK) return st;
+    return tc_launch_quantize_rows(ctx->device, a, scratch.at, (cudaStream_t)cuda_stream);
+}
+
+tc_status tc_matmul_rows(tc_ctx *ctx, const tc_rows *a, const tc_rows *b, const float *bias, int32_t relu, const tc_tensor *out, void *cuda_stream)
+{
+    if (!ctx || !valid_rows(a) || !valid_rows(b) || !aligned_tensor(out) || !aligned_to(sizeof(float), bias)) return TC_ERR_INVALID_ARG;
+    if (a->cols != b->cols || pixels_of(out) != a->rows || out->c != b->rows) return TC_ERR_INVALID_ARG;
+    if (a->rows > kMostRows || b->rows > kMostRows || a->cols > kMostRows) return TC_ERR_UNSUPPORTED;
+    Ranges ranges;
+    ranges.add(a, false);
+    ranges.add(b, false);
+    ranges.add(bias, (size_t)b->rows * sizeof(float), false);
+    ranges.add(out, true);
+    if (!ranges.apart()) return TC_ERR_INVALID_ARG;
+    if (a->rows == 0) return TC_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return TC_ERR_CUDA;
+    RowMatmulArgs args{row_matrix(a), row_matrix(b), a->cols, bias, relu != 0, out->data, out->dtype, out->h * out->w, ctx->d_status};
+    MatmulPlan plan = tc_plan_matmul_rows(args, ctx->sm_count);
+    if (plan.tiles * std::max(1, plan.splits) > 1 << 30) return TC_ERR_UNSUPPORTED;
+    CallScratch scratch;
+    const tc_status st = call_scratch(ctx, plan.needs_workspace ? plan.workspace : 0, plan.workspace, (cudaStream_t)cuda_stream, &scratch);
+    if (st != TC_OK) return st;
+    if (plan.workspace && !scratch.at) { plan.splits = 1; plan.workspace = 0; }
+    return tc_launch_matmul_rows(ctx, args, plan, scratch.at, (cudaStream_t)cuda_stream);
 }
 
 }  // extern "C"

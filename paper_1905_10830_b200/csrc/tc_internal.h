@@ -350,9 +350,37 @@ struct MatmulPlan {
     int splits = 1;                   // parts of the sums' length
     long long tiles = 0;
     size_t workspace = 0;             // bytes for the parts' sums
+    bool needs_workspace = false;     // there is no way without it
 };
 MatmulPlan tc_plan_matmul(const MatmulArgs &a, int sm_count);
 tc_status tc_launch_matmul_blocks(const tc_ctx *ctx, const MatmulArgs &a, const MatmulPlan &plan, void *workspace, cudaStream_t s);
+// ---- 8-bit integers with a scale for each row ----------------------------------------------------
+// The kernels' side of tc_rows: codes [rows][ld], scales [rows].
+struct RowMatrix {
+    uint8_t *codes = nullptr;
+    float *scales = nullptr;
+    long long ld = 0;
+    int rows = 0;
+};
+struct RowQuantizeArgs {
+    const void *x;
+    int dtype, n, c, hw;
+    RowMatrix pixels, channels;       // codes null where not wanted
+};
+size_t tc_quantize_rows_workspace(const RowQuantizeArgs &a);
+tc_status tc_launch_quantize_rows(int device, const RowQuantizeArgs &a, void *workspace, cudaStream_t s);
+struct RowMatmulArgs {
+    RowMatrix pixels, channels;       // rows of the output's pixels, of its channels
+    int cols;                         // length of the sums
+    const float *bias;                // [channels.rows], or null
+    int relu;
+    void *out;
+    int dtype, hw;
+    unsigned int *status;
+};
+MatmulPlan tc_plan_matmul_rows(const RowMatmulArgs &a, int sm_count);
+tc_status tc_launch_matmul_rows(const tc_ctx *ctx, const RowMatmulArgs &a, const MatmulPlan &plan, void *workspace, cudaStream_t s);
+
 struct NormArgs {
     const void *h, *y, *gate_map;     // y null: nothing is added to h;  gate_map: a gate for each value
     const float *after, *gate, *scale, *before;     // null: no norm, no gate, 1, no output x

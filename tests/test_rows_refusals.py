@@ -1,0 +1,52 @@
+"""Arguments that the layer calls on 8-bit integers refuse, found on the host before anything is launched: the C ABI with a context that no
+check looks into, so that no device is needed."""
+import ctypes as C
+
+import pytest
+
+import paper_1905_10830_b200 as tc
+from paper_1905_10830_b200 import binding as B
+from tests.test_blocks_refusals import AT, INVALID, OK, UNSUPPORTED, at, ctx, lib, tensor  # noqa: F401
+
+
+def rows(n, cols, at=2 * AT, ld=None):
+    return B._Rows(at, at + (1 << 36), -(-cols // 16) * 16 if ld is None else ld, n, cols)
+
+
+def test_quantize(lib, ctx):  # noqa: F811
+    call = lambda x, p, c, cx=ctx: lib.tc_quantize_rows(cx, at(x), at(p), at(c), None)                # noqa: E731
+    x = tensor(8, 64)
+    assert call(x, rows(8, 64), None, None) == INVALID
+    assert call(x, None, None) == INVALID
+    assert call(None, rows(8, 64), None) == INVALID
+    for bad in (rows(9, 64), rows(8, 65), rows(64, 8), rows(8, 64, at=2 * AT + 8), rows(8, 64, ld=72), rows(8, 64, ld=48),
+                B._Rows(None, 3 * AT, 64, 8, 64), B._Rows(3 * AT, None, 64, 8, 64), B._Rows(2 * AT, 3 * AT + 2, 64, 8, 64), rows(8, 64, at=AT + 1024)):
+        assert call(x, bad, None) == INVALID
+    assert call(x, None, rows(8, 64)) == INVALID
+    assert call(x, rows(8, 64), rows(64, 8, 2 * AT)) == INVALID                           # the same memory
+    assert call(tensor(8, 64, at=AT + 2), rows(8, 64), None) == INVALID                   # not aligned to an element
+    assert call(tensor(8, 64, dtype=B.TC_INT8), rows(8, 64), None) == INVALID
+    assert call(tensor(2**21, 1, 64, 64), rows(8, 64), None) == UNSUPPORTED
+    assert call(tensor(1, 2**22 + 1), rows(1, 2**22 + 1), None) == UNSUPPORTED
+    assert call(tensor(0, 64), rows(0, 64), rows(64, 0, 3 * AT)) == OK                    # nothing to do
+
+
+def test_matmul(lib, ctx):  # noqa: F811
+    call = lambda a, b, out, cx=ctx, bias=None: lib.tc_matmul_rows(cx, at(a), at(b), bias, 0, at(out), None)   # noqa: E731
+    a, b, out = rows(8, 64), rows(16, 64, 3 * AT), tensor(8, 16)
+    assert call(a, b, out, None) == INVALID
+    for args in ((None, b, out), (a, None, out), (a, b, None), (a, rows(16, 48, 3 * AT), out), (a, b, tensor(8, 15)), (a, b, tensor(7, 16)),
+                 (a, b, tensor(4, 16, 3, 1)), (a, b, tensor(8, 16, at=2 * AT)), (a, b, tensor(8, 16, at=AT + 1)), (a, rows(16, 64, 3 * AT + 4), out)):
+        assert call(*args) == INVALID
+    assert call(a, b, out, bias=AT) == INVALID                                            # the bias in the output's memory
+    assert call(a, b, out, bias=5 * AT + 2) == INVALID
+    assert call(rows(0, 64), b, tensor(0, 16)) == OK
+
+
+def test_the_library_has_what_the_module_asks_for(lib):  # noqa: F811
+    module = B._layer_calls()
+    assert all(hasattr(lib, name) for name in module.entry_points) and len(set(module.entry_points)) == len(module.entry_points)
+    assert {"Rows", "tc_quantize_rows", "tc_matmul_rows"} <= set(dir(tc))
+    assert C.sizeof(B._Rows) == 32
+    with pytest.raises(ValueError):
+        module.init({}, tc.TcError, tc.Blocks, tc.Rows)
