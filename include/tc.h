@@ -560,6 +560,32 @@ tc_status tc_quantize_rows(tc_ctx *ctx, const tc_tensor *x, const tc_rows *pixel
  * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 - 256 rows, more than 2^30 tiles), CUDA; TIMEOUT by tc_get_status. */
 tc_status tc_matmul_rows(tc_ctx *ctx, const tc_rows *a, const tc_rows *b, const float *bias, int32_t relu, const tc_tensor *out, void *cuda_stream);
 
+/* Group norm with an activation, of maps whose channels are neighbours in memory: value (i, c, y, x) of the tensor lies at
+ * ((i h + y) w + x) C + c, C being its number of channels.  Over a map's pixels and the C / groups channels of a group
+ *     y = act((x - mean) rstd weight_c + bias_c),   rstd = 1 / sqrt(mean (x - mean)^2 + eps)
+ * act: none, max(., 0), or z / (1 + e^-z).  Statistics, sums and products in fp32 (moments of parts of a map are put together as mean and sum of squares about
+ * it); y is rounded once. */
+typedef enum { TC_ACT_NONE = 0, TC_ACT_RELU = 1, TC_ACT_SILU = 2 } tc_activation;
+typedef struct {
+    int32_t groups;            /* a divisor of C                                                        */
+    int32_t activation;        /* tc_activation                                                         */
+    const float *weight;       /* DEVICE [C]; NULL: 1                                                   */
+    const float *bias;         /* DEVICE [C]; NULL: 0                                                   */
+    float eps;                 /* >= 0; the gradient takes it from the statistics                       */
+} tc_group_params;
+
+/* `y` (DEVICE, as x) and `codes` (by pixels, of y before it is rounded: what tc_matmul_rows reads) receive y; either or both.  `stats` DEVICE float [n][groups][2]
+ * receives mean and rstd, or NULL.  Outputs overlap neither inputs nor each other.  Larger maps' moments live in the context's arena.  May be
+ * captured into a graph.
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 8192 channels, more than 2^31 - 256 pixels), CUDA; TIMEOUT by tc_get_status. */
+tc_status tc_group_norm(tc_ctx *ctx, const tc_tensor *x, const tc_group_params *params, void *y, const tc_rows *codes, float *stats, void *cuda_stream);
+
+/* Gradients from `dy` (DEVICE, as x) and the statistics that tc_group_norm wrote: `dx` (DEVICE, as x), and where they are wanted `dweight` and `dbias`
+ * (DEVICE float [C], or NULL; only where the vector is given).  The ReLU's derivative at 0 is 0.  Gradients of vectors are sums over all pixels, within a block in fp32, over blocks
+ * in fp64, in an order that depends on sizes, type and alignment alone.  Conventions and errors as above. */
+tc_status tc_group_norm_backward(tc_ctx *ctx, const tc_tensor *x, const tc_group_params *params, const float *stats, const void *dy, void *dx, float *dweight,
+                                 float *dbias, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

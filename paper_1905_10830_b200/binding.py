@@ -69,6 +69,10 @@ class _Rows(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("ld", C.c_int64), ("rows", C.c_int32), ("cols", C.c_int32)]
 
 
+class _GroupParams(C.Structure):
+    _fields_ = [("groups", C.c_int32), ("activation", C.c_int32), ("weight", C.c_void_p), ("bias", C.c_void_p), ("eps", C.c_float)]
+
+
 class _NormParams(C.Structure):
     _fields_ = [("y", C.c_void_p), ("after", C.c_void_p), ("gate", C.c_void_p), ("gate_map", C.c_void_p),
                 ("scale", C.c_void_p), ("before", C.c_void_p), ("eps", C.c_float)]
@@ -158,6 +162,8 @@ def load_library() -> C.CDLL:
         lib.tc_residual_norms_backward.argtypes = [vp] * 7
         lib.tc_quantize_rows.argtypes = [vp] * 5
         lib.tc_matmul_rows.argtypes = [vp, vp, vp, vp, i32, vp, vp]
+        lib.tc_group_norm.argtypes = [vp] * 7
+        lib.tc_group_norm_backward.argtypes = [vp] * 9
         _lib = lib
     return _lib
 
@@ -746,3 +752,25 @@ def tc_matmul_rows(ctx: Context, a: Rows, b: Rows, *, shape=None, dtype=torch.bf
     or `channels_last`; or into `out`, contiguous or channels_last, whose shape and type count then; `bias` [O], `relu` on the result.  Nothing is recorded for
     autograd: the gradients are products of the other codes."""
     return (_layers or _layer_calls()).matmul_rows(ctx.ptr.value, ctx.device, _tensor_stream(ctx.device), a, b, shape, dtype, bias, relu, channels_last, out)
+
+
+def tc_group_norm(ctx: Context, x: torch.Tensor, groups: int, *, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, eps: float = 1e-5,
+                  activation: str | None = None, codes: bool | str = False, out=None, stats_out: torch.Tensor | None = None):
+    """(y, stats): y = act((x - mean) rstd weight + bias) of channels_last maps `x` (N, C, H, W), over each map's pixels and the C / groups channels of a group;
+    `activation` None, "relu" or "silu"; `weight` and `bias` float32 [C].  y is a tensor like x, or with `codes` its Rows by pixels (of the values before they are rounded to x's
+    type), or with codes="both" the pair of them.  stats, float32 [N, groups, 2], are mean and rstd, which the gradient takes.  `out` and `stats_out`
+    receive them where they are given.  Nothing is recorded for autograd: the gradients are tc_group_norm_backward's."""
+    return (_layers or _layer_calls()).group_norm(ctx.ptr.value, ctx.device, _tensor_stream(ctx.device), x, groups, weight, bias, eps, activation, codes, out, stats_out)
+
+
+class GroupNormGrads(NamedTuple):
+    """Gradients of tc_group_norm by its arguments' names; None where an argument was not given."""
+    x: torch.Tensor
+    weight: torch.Tensor | None
+    bias: torch.Tensor | None
+
+
+def tc_group_norm_backward(ctx: Context, x: torch.Tensor, dy: torch.Tensor, stats: torch.Tensor, *, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                           activation: str | None = None) -> GroupNormGrads:
+    """Gradients from that of y, `dy`, at the maps `x` and the statistics that tc_group_norm returned (channels_last tensors)."""
+    return GroupNormGrads._make((_layers or _layer_calls()).group_backward(ctx.ptr.value, ctx.device, _tensor_stream(ctx.device), x, dy, stats, weight, bias, activation))

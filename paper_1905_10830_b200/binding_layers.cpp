@@ -21,9 +21,12 @@ decltype(&tc_residual_norms) call_norms = nullptr;
 decltype(&tc_residual_norms_backward) call_backward = nullptr;
 decltype(&tc_quantize_rows) call_quantize_rows = nullptr;
 decltype(&tc_matmul_rows) call_matmul_rows = nullptr;
+decltype(&tc_group_norm) call_group_norm = nullptr;
+decltype(&tc_group_norm_backward) call_group_backward = nullptr;
 struct EntryPoint { const char *name; void *at; };                   // of the C ABI, and the pointer that keeps it
 const EntryPoint entry_points[] = {{"tc_quantize_blocks", &call_quantize}, {"tc_matmul_blocks", &call_matmul}, {"tc_residual_norms", &call_norms},
-                                   {"tc_residual_norms_backward", &call_backward}, {"tc_quantize_rows", &call_quantize_rows}, {"tc_matmul_rows", &call_matmul_rows}};
+                                   {"tc_residual_norms_backward", &call_backward}, {"tc_quantize_rows", &call_quantize_rows}, {"tc_matmul_rows", &call_matmul_rows},
+                                   {"tc_group_norm", &call_group_norm}, {"tc_group_norm_backward", &call_group_backward}};
 PyObject *error_type = nullptr, *blocks_type = nullptr;              // TcError(code, where); Blocks(codes, scales, cols, square)
 PyObject *rows_type = nullptr;                                       // Rows(codes, scales, cols)
 PyObject *name_codes = nullptr, *name_scales = nullptr, *name_cols = nullptr, *name_square = nullptr;
@@ -435,6 +438,109 @@ PyObject *matmul_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// A channels_last tensor, as the C structure names its sides.
+tc_tensor last_map_of(const at::Tensor &x, int device)
+{
+    if (!x.is_cuda() || !channels_last(x)) throw Bad{"expected a 4-d CUDA tensor in channels_last order"};
+    const tc_tensor t = map_of(x.permute({0, 2, 3, 1}), device);
+    return tc_tensor{t.data, t.n, t.w, t.c, t.h, t.dtype};
+}
+// A channels_last tensor of the shape and type of `x`.
+void *last_like(PyObject *o, const at::Tensor &x, int device, const char *name)
+{
+    const at::Tensor &t = tensor_of(o);
+    if (!t.is_cuda() || t.get_device() != device || t.scalar_type() != x.scalar_type() || t.sizes() != x.sizes() || !channels_last(t))
+        throw Bad{std::string(name) + ": expected a channels_last tensor of the shape and type of the first, on the context's device"};
+    return t.numel() ? t.data_ptr() : (void *)16;
+}
+at::Tensor make_last(const at::Tensor &x) { return make({x.size(0), x.size(2), x.size(3), x.size(1)}, x.scalar_type(), x.get_device()).permute({0, 3, 1, 2}); }
+float *stats_of(PyObject *o, int64_t n, int64_t groups, int device)
+{
+    const at::Tensor &t = tensor_of(o);
+    if (!on_device(t, device) || t.scalar_type() != at::kFloat || t.dim() != 3 || t.size(0) != n || (groups >= 0 && t.size(1) != groups) || t.size(2) != 2 || t.size(1) > INT32_MAX)
+        throw Bad{"stats: expected contiguous float32 values [N, groups, 2] on the context's device"};
+    return t.numel() ? (float *)t.data_ptr() : (float *)16;
+}
+int activation_of(PyObject *o)
+{
+    if (o == Py_None) return TC_ACT_NONE;
+    if (PyUnicode_Check(o) && PyUnicode_CompareWithASCIIString(o, "relu") == 0) return TC_ACT_RELU;
+    if (PyUnicode_Check(o) && PyUnicode_CompareWithASCIIString(o, "silu") == 0) return TC_ACT_SILU;
+    throw Bad{"activation: None, \"relu\" or \"silu\""};
+}
+
+// x, groups, weight, bias, eps, activation, codes, out, stats_out
+PyObject *group_norm(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded(args, n, 12, [](const Call &c, PyObject *const *a) -> PyObject * {
+        const at::Tensor &x = tensor_of(a[0]);
+        const tc_tensor t = last_map_of(x, c.device);
+        const int64_t groups = PyLong_AsLongLong(a[1]);
+        const double eps = PyFloat_AsDouble(a[4]);
+        if (PyErr_Occurred()) throw Raised{};
+        if (groups < 1 || t.c % groups) throw Bad{"groups: expected a divisor of the number of channels"};
+        const tc_group_params p{(int32_t)groups, activation_of(a[5]), vector(a[2], t.c, c.device, "weight"), vector(a[3], t.c, c.device, "bias"), (float)eps};
+        const bool both = PyUnicode_Check(a[6]) && PyUnicode_CompareWithASCIIString(a[6], "both") == 0;
+        const int codes = both || PyObject_IsTrue(a[6]);
+        if (PyErr_Occurred()) throw Raised{};
+        PyObject *out_y = a[7], *out_codes = a[7];
+        Ref pair, y, result, stats;
+        if (both && a[7] != Py_None) {
+            pair = Ref(PySequence_Tuple(a[7]));
+            if (PyTuple_GET_SIZE(pair.p) != 2) throw Bad{"out: a tensor and Rows as this call returns them"};
+            out_y = PyTuple_GET_ITEM(pair.p, 0);
+            out_codes = PyTuple_GET_ITEM(pair.p, 1);
+        }
+        void *at_y = nullptr;
+        if (both || !codes) {
+            if (out_y == Py_None) y = wrap(make_last(x));
+            else { Py_INCREF(out_y); y = Ref(out_y); }
+            at_y = last_like(y.p, x, c.device, "out");
+        }
+        RowsRef r;
+        if (codes) {
+            if (out_codes == Py_None) r = new_rows(pixels_of(t), t.c, c.device);
+            else {
+                r.rows = given_rows(out_codes, c.device);
+                Py_INCREF(out_codes);
+                r.object = Ref(out_codes);
+            }
+            result = both ? Ref(PyTuple_Pack(2, y.p, r.object.p)) : std::move(r.object);
+        } else
+            result = std::move(y);
+        if (a[8] == Py_None) stats = wrap(make({t.n, groups, 2}, at::kFloat, c.device));
+        else { Py_INCREF(a[8]); stats = Ref(a[8]); }
+        float *const at_stats = stats_of(stats.p, t.n, groups, c.device);
+        c.check(unlocked([&] { return call_group_norm(c.ctx, &t, &p, at_y, codes ? &r.rows : nullptr, at_stats, c.stream); }), "tc_group_norm");
+        return PyTuple_Pack(2, result.p, stats.p);
+    });
+}
+
+// x, dy, stats, weight, bias, activation: (x, weight, bias)
+PyObject *group_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded(args, n, 9, [](const Call &c, PyObject *const *a) -> PyObject * {
+        const at::Tensor &x = tensor_of(a[0]);
+        const tc_tensor t = last_map_of(x, c.device);
+        const void *const dy = last_like(a[1], x, c.device, "dy");
+        const float *const stats = stats_of(a[2], t.n, -1, c.device);
+        const int64_t groups = tensor_of(a[2]).size(1);
+        if (groups < 1 || t.c % groups) throw Bad{"stats: as tc_group_norm returned them for these maps"};
+        const tc_group_params p{(int32_t)groups, activation_of(a[5]), vector(a[3], t.c, c.device, "weight"), vector(a[4], t.c, c.device, "bias"), 0.f};
+        Ref dx = wrap(make_last(x)), vectors[2];
+        float *at[2] = {};
+        for (int i = 0; i < 2; ++i) {
+            if (a[3 + i] == Py_None) { vectors[i] = Ref(none()); continue; }
+            const at::Tensor g = make({t.c}, at::kFloat, c.device);
+            at[i] = (float *)g.data_ptr();
+            vectors[i] = wrap(g);
+        }
+        void *const to = THPVariable_Unpack(dx.p).numel() ? THPVariable_Unpack(dx.p).data_ptr() : nullptr;
+        c.check(unlocked([&] { return call_group_backward(c.ctx, &t, &p, stats, dy, to, at[0], at[1], c.stream); }), "tc_group_norm_backward");
+        return PyTuple_Pack(3, dx.p, vectors[0].p, vectors[1].p);
+    });
+}
+
 // addresses of the entry points by name, TcError, Blocks, Rows
 PyObject *init(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -463,6 +569,8 @@ PyMethodDef methods[] = {{"init", (PyCFunction)(void *)init, METH_FASTCALL, null
                          {"backward", (PyCFunction)(void *)backward, METH_FASTCALL, nullptr},
                          {"quantize_rows", (PyCFunction)(void *)quantize_rows, METH_FASTCALL, nullptr},
                          {"matmul_rows", (PyCFunction)(void *)matmul_rows, METH_FASTCALL, nullptr},
+                         {"group_norm", (PyCFunction)(void *)group_norm, METH_FASTCALL, nullptr},
+                         {"group_backward", (PyCFunction)(void *)group_backward, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_layers", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,66 @@
+// Codes of 8-bit integers with one scale a row: scale = fl(max|x| / 127), code = the integer nearest to x / scale (the quotient of
+// the real numbers), ties to even.
+#pragma once
+
+#include "block_codes.cuh"
+
+namespace rowcodes {
+
+using namespace blk;
+
+// Scale of a row from the bits of its largest magnitude; NaN where the row holds an infinity or a NaN.
+__device__ __forceinline__ float row_scale(uint32_t amax_bits)
+{
+    if (amax_bits >= 0x7f800000u) return __int_as_float(0x7fffffff);
+    return __fdiv_rn(fmaxf(__uint_as_float(amax_bits), kSmallest), 127.0f);
+}
+
+// A row's scale and what its codes are computed with.
+struct Coder {
+    float scale, inv;
+    __device__ __forceinline__ explicit Coder(float s)
+    {
+        scale = s;
+        inv = s == s ? __frcp_rn(s) : 0.f;
+    }
+};
+constexpr float kInteger = 12582912.0f;                       // 1.5 x 2^23: added to a value of up to 2^22 it leaves the nearest integer in the low bits
+constexpr float kNearBorder = 0.5f - 1.0f / 32768.0f;
+
+// The code next to `near_code` where x / scale comes close to the border between two.
+__device__ __noinline__ static int code_at_border(float x, float scale, int near_code, float rest)
+{
+    const int other = near_code + (rest > 0.f ? 1 : -1);
+    const float border = 0.5f * (float)(near_code + other);
+    const float past = fmaf(-border, scale, x) * (rest > 0.f ? 1.f : -1.f);         // the sign is exact
+    if (past != 0.f) return past > 0.f ? other : near_code;
+    return near_code & 1 ? other : near_code;
+}
+// Codes of four values, packed.  With a NaN for its scale a row's codes are zeros.  Found with 1 / scale in fp32, whose product with x is off by
+// less than 127 x 2^-23; those that come near a border between two codes are looked at again with the border's exact difference.
+__device__ __forceinline__ uint32_t codes_of4(const float *v, const Coder &c)
+{
+    float t[4], d[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        t[i] = fmaf(v[i], c.inv, kInteger);
+        d[i] = fmaf(v[i], c.inv, -(t[i] - kInteger));
+    }
+    const float most = fmaxf(fmaxf(fabsf(d[0]), fabsf(d[1])), fmaxf(fabsf(d[2]), fabsf(d[3])));
+    if (most > kNearBorder)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (fabsf(d[i]) > kNearBorder) t[i] = kInteger + (float)code_at_border(v[i], c.scale, (int)(t[i] - kInteger), d[i]);
+    const uint32_t lo = __byte_perm(__float_as_uint(t[0]), __float_as_uint(t[1]), 0x0040), hi = __byte_perm(__float_as_uint(t[2]), __float_as_uint(t[3]), 0x0040);
+    const uint32_t w = __byte_perm(lo, hi, 0x5410);
+    return c.scale == c.scale ? w : 0u;
+}
+__device__ __forceinline__ uint2 codes_of8(const float (&v)[8], const Coder &c) { return make_uint2(codes_of4(v, c), codes_of4(v + 4, c)); }
+// One code (of the low byte).
+__device__ __forceinline__ uint8_t code_of(float x, const Coder &c)
+{
+    const float v[4] = {x, 0.f, 0.f, 0.f};
+    return (uint8_t)codes_of4(v, c);
+}
+
+}  // namespace rowcodes

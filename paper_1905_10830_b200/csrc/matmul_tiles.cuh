@@ -92,12 +92,6 @@ __device__ __forceinline__ void store_four(const TileArgs &a, int row, int col, 
         for (int j = 0; j < 4; ++j) store_value<T>(a, row, col + j, v[j]);
 }
 
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
-{
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 // Bias and activation, in a pass of their own: the stores, of which a warp's time between two tiles consists, stay short.  The j-th pair is of
 // row and column place(j).
 template <int kPairs, typename F>

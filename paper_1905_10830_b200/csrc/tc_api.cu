@@ -1813,6 +1813,7 @@ namespace {
 
 constexpr long long kMostRows = (1ll << 31) - 256;      // rows that 32-bit row numbers, rounded up to a tile, hold
 constexpr int kMostNormChannels = 16384;                // a row's channels in the registers of a block
+constexpr int kMostGroupChannels = 8192;                // sums of channels and groups in a block's shared memory
 
 size_t element_size(int dtype) { return dtype == TC_BF16 ? 2 : 4; }
 bool aligned_tensor(const tc_tensor *t) { return valid_tensor(t) && ((uintptr_t)t->data & (element_size(t->dtype) - 1)) == 0; }
@@ -1893,6 +1894,21 @@ void add_norm_params(Ranges &r, const tc_tensor *h, const tc_norm_params *p)
     for (const void *t : {(const void *)h->data, p->y, p->gate_map}) r.add(t, tensor_bytes(h), false);
     for (const float *v : {p->after, p->gate, p->before}) r.add(v, (size_t)h->c * sizeof(float), false);
     r.add(p->scale, sizeof(float), false);
+}
+
+// What both directions of the group norm share.
+bool valid_group_params(const tc_tensor *x, const tc_group_params *p)
+{
+    return aligned_tensor(x) && p && p->groups > 0 && x->c % p->groups == 0 && aligned_to(4, p->weight, p->bias) && p->activation >= TC_ACT_NONE && p->activation <= TC_ACT_SILU;
+}
+bool supported_groups(const tc_tensor *x, const tc_group_params *p)
+{
+    return pixels_of(x) <= kMostRows && x->c <= kMostGroupChannels && (long long)x->n * p->groups <= 1ll << 33;
+}
+void add_group_params(Ranges &r, const tc_tensor *x, const tc_group_params *p)
+{
+    r.add(x, false);
+    for (const float *v : {p->weight, p->bias}) r.add(v, (size_t)x->c * sizeof(float), false);
 }
 
 }  // namespace
@@ -2092,6 +2108,58 @@ tc_status tc_matmul_rows(tc_ctx *ctx, const tc_rows *a, const tc_rows *b, const 
     if (st != TC_OK) return st;
     if (plan.workspace && !scratch.at) { plan.splits = 1; plan.workspace = 0; }
     return tc_launch_matmul_rows(ctx, args, plan, scratch.at, (cudaStream_t)cuda_stream);
+}
+
+tc_status tc_group_norm(tc_ctx *ctx, const tc_tensor *x, const tc_group_params *params, void *y, const tc_rows *codes, float *stats, void *cuda_stream)
+{
+    if (!ctx || !valid_group_params(x, params) || !aligned_to(element_size(x->dtype), y) || !aligned_to(8, stats)) return TC_ERR_INVALID_ARG;
+    const long long p = pixels_of(x);
+    if (!(params->eps >= 0.f) || (!y && !codes && p > 0)) return TC_ERR_INVALID_ARG;
+    if (!supported_groups(x, params)) return TC_ERR_UNSUPPORTED;
+    if (codes && (!valid_rows(codes) || codes->rows != p || codes->cols != x->c)) return TC_ERR_INVALID_ARG;
+    Ranges ranges;
+    add_group_params(ranges, x, params);
+    ranges.add(y, tensor_bytes(x), true);
+    ranges.add(codes, true);
+    ranges.add(stats, (size_t)x->n * params->groups * 2 * sizeof(float), true);
+    if (!ranges.apart()) return TC_ERR_INVALID_ARG;
+    if (p == 0) return TC_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return TC_ERR_CUDA;
+    const GroupNormArgs a{x->data, x->dtype, x->n, x->c, x->h * x->w, params->groups, params->activation, params->weight, params->bias, params->eps,
+                          y, row_matrix(codes), stats, aligned_to(16, x->data, y), ctx->d_status};
+    const GroupPlan plan = tc_plan_group_norm(a, ctx->sm_count);
+    CallScratch scratch;
+    const tc_status st = call_scratch(ctx, plan.workspace, plan.workspace, (cudaStream_t)cuda_stream, &scratch);
+    if (st != TC_OK) return st;
+    return tc_launch_group_norm(ctx->device, a, plan, scratch.at, (cudaStream_t)cuda_stream);
+}
+
+tc_status tc_group_norm_backward(tc_ctx *ctx, const tc_tensor *x, const tc_group_params *params, const float *stats, const void *dy, void *dx, float *dweight,
+                                 float *dbias, void *cuda_stream)
+{
+    if (!ctx || !valid_group_params(x, params) || !aligned_to(element_size(x->dtype), dy, dx) || !aligned_to(8, stats) || !aligned_to(4, dweight, dbias))
+        return TC_ERR_INVALID_ARG;
+    const long long p = pixels_of(x);
+    if ((p > 0 && (!stats || !dy || !dx)) || (dweight && !params->weight) || (dbias && !params->bias)) return TC_ERR_INVALID_ARG;
+    if (!supported_groups(x, params)) return TC_ERR_UNSUPPORTED;
+    Ranges ranges;
+    add_group_params(ranges, x, params);
+    ranges.add(stats, (size_t)x->n * params->groups * 2 * sizeof(float), false);
+    ranges.add(dy, tensor_bytes(x), false);
+    ranges.add(dx, tensor_bytes(x), true);
+    for (float *v : {dweight, dbias}) ranges.add(v, (size_t)x->c * sizeof(float), true);
+    if (!ranges.apart()) return TC_ERR_INVALID_ARG;
+    if (p == 0 && !dweight && !dbias) return TC_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return TC_ERR_CUDA;
+    const GroupGradArgs a{x->data, dy, x->dtype, x->n, x->c, x->h * x->w, params->groups, params->activation, params->weight, params->bias, stats,
+                          dx, dweight, dbias, aligned_to(16, x->data, dy, dx), ctx->d_status};
+    const GroupPlan plan = p ? tc_plan_group_norm_backward(a, ctx->sm_count) : GroupPlan{};
+    CallScratch scratch;
+    const tc_status st = call_scratch(ctx, plan.workspace, plan.workspace, (cudaStream_t)cuda_stream, &scratch);
+    if (st != TC_OK) return st;
+    return tc_launch_group_norm_backward(ctx->device, a, plan, scratch.at, (cudaStream_t)cuda_stream);
 }
 
 }  // extern "C"

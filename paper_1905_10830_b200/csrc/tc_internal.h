@@ -381,6 +381,44 @@ struct RowMatmulArgs {
 MatmulPlan tc_plan_matmul_rows(const RowMatmulArgs &a, int sm_count);
 tc_status tc_launch_matmul_rows(const tc_ctx *ctx, const RowMatmulArgs &a, const MatmulPlan &plan, void *workspace, cudaStream_t s);
 
+// ---- group norms of maps whose channels are neighbours in memory ------------------------------------
+struct GroupNormArgs {
+    const void *x;
+    int dtype;
+    long long n;
+    int c, hw, groups, act;
+    const float *weight, *bias;       // null: 1, 0
+    float eps;
+    void *y;                          // or null, with codes
+    RowMatrix codes;
+    float *stats;                     // [n][groups][2], or null
+    bool aligned;                     // tensors begin at 16 bytes
+    unsigned int *status;
+};
+struct GroupGradArgs {
+    const void *x, *dy;
+    int dtype;
+    long long n;
+    int c, hw, groups, act;
+    const float *weight, *bias;
+    const float *stats;
+    void *dx;
+    float *dweight, *dbias;           // null: not wanted
+    bool aligned;
+    unsigned int *status;
+};
+// How maps are cut: `shared` bytes of a block where a map lies in a cluster's shared memory, else 0.
+struct GroupPlan {
+    int vector = 1, threads = 256;
+    int share = 0, shares = 1;        // pixels of a block, blocks of a map
+    size_t shared = 0, workspace = 0;
+};
+int tc_group_threads(int columns);
+GroupPlan tc_plan_group_norm(const GroupNormArgs &a, int sm_count);
+tc_status tc_launch_group_norm(int device, const GroupNormArgs &a, const GroupPlan &plan, void *workspace, cudaStream_t s);
+GroupPlan tc_plan_group_norm_backward(const GroupGradArgs &a, int sm_count);
+tc_status tc_launch_group_norm_backward(int device, const GroupGradArgs &a, const GroupPlan &plan, void *workspace, cudaStream_t s);
+
 struct NormArgs {
     const void *h, *y, *gate_map;     // y null: nothing is added to h;  gate_map: a gate for each value
     const float *after, *gate, *scale, *before;     // null: no norm, no gate, 1, no output x

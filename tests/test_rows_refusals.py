@@ -50,3 +50,36 @@ def test_the_library_has_what_the_module_asks_for(lib):  # noqa: F811
     assert C.sizeof(B._Rows) == 32
     with pytest.raises(ValueError):
         module.init({}, tc.TcError, tc.Blocks, tc.Rows)
+
+
+def group_params(groups=4, act=0, weight=None, bias=None, eps=1e-5):
+    return B._GroupParams(groups, act, weight, bias, eps)
+
+
+def test_group_norm(lib, ctx):  # noqa: F811
+    call = lambda x, p, y, codes=None, stats=None, cx=ctx: lib.tc_group_norm(cx, at(x), at(p), y, at(codes), stats, None)      # noqa: E731
+    x, y, p = tensor(8, 64, 3, 3), 2 * AT, group_params()
+    assert call(x, p, y, None, None, None) == INVALID
+    for args in ((None, p, y), (x, None, y), (x, p, None), (x, p, AT), (x, p, y + 2), (tensor(8, 64, 3, 3, at=AT + 2), p, y), (x, p, y, rows(72, 65, 3 * AT)), (x, p, y, rows(71, 64, 3 * AT)),
+                 (x, p, y, rows(72, 64, 2 * AT)), (x, p, y, None, y), (x, p, y, None, 3 * AT + 4), (x, p, None, rows(72, 64, AT))):
+        assert call(*args) == INVALID, args
+    for bad in (group_params(0), group_params(-1), group_params(5), group_params(128), group_params(act=3), group_params(act=-1), group_params(eps=-1.0), group_params(eps=float("nan")),
+                group_params(weight=3 * AT + 2), group_params(bias=2 * AT), group_params(weight=2 * AT + 64)):
+        assert call(x, bad, y) == INVALID
+    assert call(tensor(1, 8256), p, y) == UNSUPPORTED
+    assert call(tensor(2**21, 4, 64, 64), p, 2**20 * AT) == UNSUPPORTED
+    assert call(tensor(0, 64, 3, 3), p, None) == OK
+
+
+def test_group_norm_backward(lib, ctx):  # noqa: F811
+    def call(x, p, stats, dy, dx, dw=None, db=None, cx=ctx):
+        return lib.tc_group_norm_backward(cx, at(x), at(p), stats, dy, dx, dw, db, None)
+
+    x, p, stats, dy, dx = tensor(8, 64, 3, 3), group_params(weight=5 * AT, bias=6 * AT), 2 * AT, 3 * AT, 4 * AT
+    assert call(x, p, stats, dy, dx, cx=None) == INVALID
+    for args in ((None, p, stats, dy, dx), (x, None, stats, dy, dx), (x, p, None, dy, dx), (x, p, stats, None, dx), (x, p, stats, dy, None), (x, p, stats, dy, AT), (x, p, stats, dy, dy),
+                 (x, p, stats, dy, stats), (x, p, stats + 4, dy, dx), (x, p, stats, dy + 2, dx), (x, p, stats, dy, dx, dx), (x, p, stats, dy, dx, 5 * AT), (x, p, stats, dy, dx, 7 * AT + 2),
+                 (x, p, stats, dy, dx, 7 * AT, 7 * AT), (x, group_params(bias=6 * AT), stats, dy, dx, 7 * AT), (x, group_params(weight=5 * AT), stats, dy, dx, 7 * AT, 8 * AT)):
+        assert call(*args) == INVALID, args
+    assert call(tensor(1, 8256), group_params(), stats, dy, dx) == UNSUPPORTED
+    assert call(tensor(0, 64, 3, 3), group_params(), None, None, None) == OK
