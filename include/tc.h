@@ -586,6 +586,23 @@ tc_status tc_group_norm(tc_ctx *ctx, const tc_tensor *x, const tc_group_params *
 tc_status tc_group_norm_backward(tc_ctx *ctx, const tc_tensor *x, const tc_group_params *params, const float *stats, const void *dy, void *dx, float *dweight,
                                  float *dbias, void *cuda_stream);
 
+/* The norm of many gradients together, and their clipping by it:
+ *     norm = sqrt(sum over all values of all tensors of x^2),   out = x min(1, max_norm / norm)
+ * for a list of tensors of any number and sizes, fp32 and bf16 mixed.  Squares are summed in fp64 (a few at a time in fp32 where that loses nothing), in an order that
+ * the sizes and alignments decide; max_norm / norm and the products are fp32, rounded once to the tensor's type.  Where norm <= max_norm or is not finite
+ * the values keep their bits.  `out` may be the tensor itself (then nothing is written unless it is scaled), otherwise outputs overlap neither one another nor
+ * inputs; tc_gradient_norm does not look at it.  `list` is HOST memory, read before the call returns; `norm` DEVICE float [1] receives the norm
+ * before clipping.  May be captured into a graph.
+ * Errors: INVALID_ARG (max_norm negative or NaN among them), UNSUPPORTED (more than 2^42 values), CUDA. */
+typedef struct {
+    const void *data;          /* DEVICE, aligned to its element size */
+    void *out;                 /* DEVICE, of the same size and type   */
+    int64_t count;             /* values                              */
+    int32_t dtype;             /* tc_dtype                            */
+} tc_gradient;
+tc_status tc_gradient_norm(tc_ctx *ctx, const tc_gradient *list, int32_t n, float *norm, void *cuda_stream);
+tc_status tc_clip_gradients(tc_ctx *ctx, const tc_gradient *list, int32_t n, float max_norm, float *norm, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

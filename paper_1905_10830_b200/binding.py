@@ -69,6 +69,10 @@ class _Rows(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("ld", C.c_int64), ("rows", C.c_int32), ("cols", C.c_int32)]
 
 
+class _Gradient(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("count", C.c_int64), ("dtype", C.c_int32)]
+
+
 class _GroupParams(C.Structure):
     _fields_ = [("groups", C.c_int32), ("activation", C.c_int32), ("weight", C.c_void_p), ("bias", C.c_void_p), ("eps", C.c_float)]
 
@@ -163,6 +167,8 @@ def load_library() -> C.CDLL:
         lib.tc_quantize_rows.argtypes = [vp] * 5
         lib.tc_matmul_rows.argtypes = [vp, vp, vp, vp, i32, vp, vp]
         lib.tc_group_norm.argtypes = [vp] * 7
+        lib.tc_gradient_norm.argtypes = [vp, vp, i32, vp, vp]
+        lib.tc_clip_gradients.argtypes = [vp, vp, i32, C.c_float, vp, vp]
         lib.tc_group_norm_backward.argtypes = [vp] * 9
         _lib = lib
     return _lib
@@ -774,3 +780,16 @@ def tc_group_norm_backward(ctx: Context, x: torch.Tensor, dy: torch.Tensor, stat
                            activation: str | None = None) -> GroupNormGrads:
     """Gradients from that of y, `dy`, at the maps `x` and the statistics that tc_group_norm returned (channels_last tensors)."""
     return GroupNormGrads._make((_layers or _layer_calls()).group_backward(ctx.ptr.value, ctx.device, _tensor_stream(ctx.device), x, dy, stats, weight, bias, activation))
+
+
+# ---- gradients of a whole network ---------------------------------------------------------------
+
+def tc_gradient_norm(ctx: Context, tensors, *, norm_out: torch.Tensor | None = None) -> torch.Tensor:
+    """sqrt of the sum of the squares of all values of `tensors` (float32 and bfloat16 CUDA tensors, dense in any order of their sides), float32 [1]."""
+    return (_layers or _layer_calls()).gradients(ctx.ptr.value, ctx.device, _tensor_stream(ctx.device), tensors, None, None, norm_out)
+
+
+def tc_clip_gradients(ctx: Context, tensors, max_norm: float, *, out=None, norm_out: torch.Tensor | None = None) -> torch.Tensor:
+    """Scales `tensors` by min(1, max_norm / norm), in place or into the tensors `out` (of the same shapes, strides and types); returns the norm before that, float32 [1].
+    A norm that is not finite leaves the values as they are."""
+    return (_layers or _layer_calls()).gradients(ctx.ptr.value, ctx.device, _tensor_stream(ctx.device), tensors, float(max_norm), out, norm_out)

@@ -10,6 +10,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <string>
+#include <vector>
 
 #include "tc.h"
 
@@ -23,10 +24,13 @@ decltype(&tc_quantize_rows) call_quantize_rows = nullptr;
 decltype(&tc_matmul_rows) call_matmul_rows = nullptr;
 decltype(&tc_group_norm) call_group_norm = nullptr;
 decltype(&tc_group_norm_backward) call_group_backward = nullptr;
+decltype(&tc_gradient_norm) call_gradient_norm = nullptr;
+decltype(&tc_clip_gradients) call_clip_gradients = nullptr;
 struct EntryPoint { const char *name; void *at; };                   // of the C ABI, and the pointer that keeps it
 const EntryPoint entry_points[] = {{"tc_quantize_blocks", &call_quantize}, {"tc_matmul_blocks", &call_matmul}, {"tc_residual_norms", &call_norms},
                                    {"tc_residual_norms_backward", &call_backward}, {"tc_quantize_rows", &call_quantize_rows}, {"tc_matmul_rows", &call_matmul_rows},
-                                   {"tc_group_norm", &call_group_norm}, {"tc_group_norm_backward", &call_group_backward}};
+                                   {"tc_group_norm", &call_group_norm}, {"tc_group_norm_backward", &call_group_backward},
+                                   {"tc_gradient_norm", &call_gradient_norm}, {"tc_clip_gradients", &call_clip_gradients}};
 PyObject *error_type = nullptr, *blocks_type = nullptr;              // TcError(code, where); Blocks(codes, scales, cols, square)
 PyObject *rows_type = nullptr;                                       // Rows(codes, scales, cols)
 PyObject *name_codes = nullptr, *name_scales = nullptr, *name_cols = nullptr, *name_square = nullptr;
@@ -541,6 +545,44 @@ PyObject *group_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// tensors, max_norm or None (the norm alone), out, norm_out
+PyObject *gradients(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded(args, n, 7, [](const Call &c, PyObject *const *a) -> PyObject * {
+        const bool clip = a[1] != Py_None;
+        const double max_norm = clip ? PyFloat_AsDouble(a[1]) : 0.0;
+        Ref tensors(PySequence_Fast(a[0], "expected a list of tensors")), outs;
+        if (a[2] != Py_None) outs = Ref(PySequence_Fast(a[2], "out: expected a list of tensors"));
+        if (PyErr_Occurred()) throw Raised{};
+        const Py_ssize_t count = PySequence_Fast_GET_SIZE(tensors.p);
+        if (count > INT32_MAX || (outs.p && PySequence_Fast_GET_SIZE(outs.p) != count)) throw Bad{"out: expected as many tensors"};
+        std::vector<tc_gradient> list((size_t)count);
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            const at::Tensor &t = tensor_of(PySequence_Fast_GET_ITEM(tensors.p, i));
+            if (!t.is_cuda() || t.get_device() != c.device) throw Bad{"expected tensors on the context's device"};
+            if (t.scalar_type() != at::kFloat && t.scalar_type() != at::kBFloat16) throw Bad{"dtype must be float32 or bfloat16"};
+            if (!t.is_non_overlapping_and_dense()) throw Bad{"expected tensors whose values lie one behind the other"};
+            void *out = t.data_ptr();
+            if (outs.p) {
+                const at::Tensor &o = tensor_of(PySequence_Fast_GET_ITEM(outs.p, i));
+                if (!o.is_cuda() || o.get_device() != c.device || o.scalar_type() != t.scalar_type() || o.sizes() != t.sizes() || o.strides() != t.strides())
+                    throw Bad{"out: expected tensors of the shapes, strides and types of the first, on the context's device"};
+                out = o.data_ptr();
+            }
+            list[i] = tc_gradient{t.data_ptr(), out, t.numel(), t.scalar_type() == at::kFloat ? TC_F32 : TC_BF16};
+        }
+        Ref norm;
+        if (a[3] == Py_None) norm = wrap(make({1}, at::kFloat, c.device));
+        else { Py_INCREF(a[3]); norm = Ref(a[3]); }
+        float *const at = vector(norm.p, 1, c.device, "norm_out");
+        c.check(unlocked([&] {
+                    return clip ? call_clip_gradients(c.ctx, list.data(), (int32_t)count, (float)max_norm, at, c.stream) : call_gradient_norm(c.ctx, list.data(), (int32_t)count, at, c.stream);
+                }),
+                clip ? "tc_clip_gradients" : "tc_gradient_norm");
+        return norm.give();
+    });
+}
+
 // addresses of the entry points by name, TcError, Blocks, Rows
 PyObject *init(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -570,6 +612,7 @@ PyMethodDef methods[] = {{"init", (PyCFunction)(void *)init, METH_FASTCALL, null
                          {"quantize_rows", (PyCFunction)(void *)quantize_rows, METH_FASTCALL, nullptr},
                          {"matmul_rows", (PyCFunction)(void *)matmul_rows, METH_FASTCALL, nullptr},
                          {"group_norm", (PyCFunction)(void *)group_norm, METH_FASTCALL, nullptr},
+                         {"gradients", (PyCFunction)(void *)gradients, METH_FASTCALL, nullptr},
                          {"group_backward", (PyCFunction)(void *)group_backward, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_layers", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1911,6 +1911,59 @@ void add_group_params(Ranges &r, const tc_tensor *x, const tc_group_params *p)
     for (const float *v : {p->weight, p->bias}) r.add(v, (size_t)x->c * sizeof(float), false);
 }
 
+// The outputs of a list of gradients overlap neither one another nor an input, but for a tensor that is scaled where it is.
+bool gradients_apart(const tc_gradient *g, int n, const float *norm)
+{
+    struct Range { const char *first, *end; bool out; };
+    const auto bytes = [&](int i) { return (size_t)g[i].count * element_size(g[i].dtype); };
+    const char *const at_norm = (const char *)norm;
+    std::vector<Range> all;
+    all.reserve(2 * (size_t)n + 1);
+    all.push_back({at_norm, at_norm + sizeof(float), true});
+    for (int i = 0; i < n; ++i) {
+        if (!g[i].count) continue;
+        const char *const in = (const char *)g[i].data, *const out = (const char *)g[i].out;
+        if (in != out) all.push_back({in, in + bytes(i), false});
+        if (out) all.push_back({out, out + bytes(i), true});
+    }
+    const auto before = [](const Range &a, const Range &b) { return a.first < b.first; };
+    if (!std::is_sorted(all.begin(), all.end(), before)) std::sort(all.begin(), all.end(), before);
+    const char *end_out = nullptr, *end_any = nullptr;        // of the ranges so far
+    for (const Range &r : all) {
+        if (r.first < (r.out ? end_any : end_out)) return false;
+        if (r.end > end_any) end_any = r.end;
+        if (r.out && r.end > end_out) end_out = r.end;
+    }
+    return true;
+}
+tc_status gradients(tc_ctx *ctx, const tc_gradient *list, int32_t n, bool clip, float max_norm, float *norm, void *cuda_stream)
+try {
+    if (!ctx || n < 0 || (n > 0 && !list) || !norm || !aligned_to(4, norm) || (clip && !(max_norm >= 0.f))) return TC_ERR_INVALID_ARG;
+    long long values = 0;
+    std::vector<tc_gradient> reads;
+    for (int i = 0; i < n; ++i) {
+        const tc_gradient &g = list[i];
+        if ((g.dtype != TC_F32 && g.dtype != TC_BF16) || g.count < 0) return TC_ERR_INVALID_ARG;
+        if (g.count > 0 && (!g.data || (clip && !g.out) || !aligned_to(element_size(g.dtype), g.data, g.out))) return TC_ERR_INVALID_ARG;
+        if (g.count > 1ll << 42 || (values += g.count) > 1ll << 42) return TC_ERR_UNSUPPORTED;
+    }
+    if (!clip) {                                              // (the norm writes none)
+        reads.assign(list, list + n);
+        for (tc_gradient &g : reads) g.out = nullptr;
+        list = reads.data();
+    }
+    if (!gradients_apart(list, n, norm)) return TC_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return TC_ERR_CUDA;
+    const size_t bytes = tc_gradient_norm_workspace(n, ctx->sm_count);
+    CallScratch scratch;
+    const tc_status st = call_scratch(ctx, bytes, bytes, (cudaStream_t)cuda_stream, &scratch);
+    if (st != TC_OK) return st;
+    return tc_launch_clip_gradients(list, n, clip, max_norm, norm, ctx->sm_count, scratch.at, (cudaStream_t)cuda_stream);
+} catch (...) {                                               // no memory for the host's lists
+    return TC_ERR_CUDA;
+}
+
 }  // namespace
 
 extern "C" {
@@ -2160,6 +2213,16 @@ tc_status tc_group_norm_backward(tc_ctx *ctx, const tc_tensor *x, const tc_group
     const tc_status st = call_scratch(ctx, plan.workspace, plan.workspace, (cudaStream_t)cuda_stream, &scratch);
     if (st != TC_OK) return st;
     return tc_launch_group_norm_backward(ctx->device, a, plan, scratch.at, (cudaStream_t)cuda_stream);
+}
+
+tc_status tc_gradient_norm(tc_ctx *ctx, const tc_gradient *list, int32_t n, float *norm, void *cuda_stream)
+{
+    return gradients(ctx, list, n, false, 0.f, norm, cuda_stream);
+}
+
+tc_status tc_clip_gradients(tc_ctx *ctx, const tc_gradient *list, int32_t n, float max_norm, float *norm, void *cuda_stream)
+{
+    return gradients(ctx, list, n, true, max_norm, norm, cuda_stream);
 }
 
 }  // extern "C"

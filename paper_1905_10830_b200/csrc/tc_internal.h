@@ -419,6 +419,10 @@ tc_status tc_launch_group_norm(int device, const GroupNormArgs &a, const GroupPl
 GroupPlan tc_plan_group_norm_backward(const GroupGradArgs &a, int sm_count);
 tc_status tc_launch_group_norm_backward(int device, const GroupGradArgs &a, const GroupPlan &plan, void *workspace, cudaStream_t s);
 
+// ---- the norm of a list of tensors ------------------------------------------------------------------
+size_t tc_gradient_norm_workspace(int tensors, int sm_count);
+tc_status tc_launch_clip_gradients(const tc_gradient *list, int n, bool clip, float max_norm, float *norm, int sm_count, void *workspace, cudaStream_t s);
+
 struct NormArgs {
     const void *h, *y, *gate_map;     // y null: nothing is added to h;  gate_map: a gate for each value
     const float *after, *gate, *scale, *before;     // null: no norm, no gate, 1, no output x

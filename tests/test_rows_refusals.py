@@ -83,3 +83,26 @@ def test_group_norm_backward(lib, ctx):  # noqa: F811
         assert call(*args) == INVALID, args
     assert call(tensor(1, 8256), group_params(), stats, dy, dx) == UNSUPPORTED
     assert call(tensor(0, 64, 3, 3), group_params(), None, None, None) == OK
+
+
+def test_gradients(lib, ctx):  # noqa: F811
+    def call(items, max_norm=1.0, norm=8 * AT, cx=ctx, n=None):
+        g = (B._Gradient * max(1, len(items)))(*items)
+        return lib.tc_clip_gradients(cx, C.addressof(g), len(items) if n is None else n, max_norm, norm, None)
+
+    ok = B._Gradient(AT, 2 * AT, 100, B.TC_F32)
+    assert call([ok], cx=None) == INVALID
+    for bad in (B._Gradient(AT, 2 * AT, -1, B.TC_F32), B._Gradient(AT, 2 * AT, 100, B.TC_INT8), B._Gradient(AT + 2, 2 * AT, 100, B.TC_F32), B._Gradient(AT, 2 * AT + 1, 100, B.TC_BF16),
+                B._Gradient(None, 2 * AT, 100, B.TC_F32), B._Gradient(AT, None, 100, B.TC_F32), B._Gradient(AT, AT + 4, 100, B.TC_F32), B._Gradient(AT, AT - 396, 100, B.TC_F32)):
+        assert call([bad]) == INVALID
+        assert call([B._Gradient(3 * AT, 4 * AT, 8, B.TC_BF16), bad]) == INVALID
+    assert call([ok], n=-1) == INVALID and call([ok], norm=None) == INVALID and call([ok], norm=8 * AT + 2) == INVALID
+    assert call([ok], max_norm=-1.0) == INVALID and call([ok], max_norm=float("nan")) == INVALID
+    assert call([ok], norm=AT + 40) == INVALID and call([ok], norm=2 * AT + 396) == INVALID
+    for other in (B._Gradient(3 * AT, 2 * AT + 396, 100, B.TC_F32), B._Gradient(2 * AT, 3 * AT, 100, B.TC_F32), B._Gradient(3 * AT, AT, 100, B.TC_F32)):
+        assert call([ok, other]) == INVALID and call([other, ok]) == INVALID
+    assert call([B._Gradient(AT, AT, 1 << 43, B.TC_BF16)]) == UNSUPPORTED
+    assert lib.tc_clip_gradients(ctx, None, 1, 1.0, 8 * AT, None) == INVALID
+    assert lib.tc_gradient_norm(ctx, None, 1, 8 * AT, None) == INVALID
+    g = B._Gradient(AT, None, 100, B.TC_F32)
+    assert lib.tc_gradient_norm(ctx, C.addressof(g), 1, AT + 8, None) == INVALID           # the norm in what is read
