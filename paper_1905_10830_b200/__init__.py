@@ -12,4 +12,4 @@ from .binding import (  # noqa: F401
     Blocks, NormGrads, tc_quantize_blocks, tc_matmul_blocks, tc_residual_norms, tc_residual_norms_backward,
     tc_get_status, tc_force_exact_path, tc_force_jacobi, tc_last_path, tc_host_huffman_lengths, tc_host_eigh, tc_device_eigh, TC_EIG_DEVICE, TC_EIG_HOST, library_path, load_library,
 )
-from .pipeline import CodedLayer, ResidualBlock, calibrate_layer_by_layer, run_chain, code_layer  # noqa: F401,E402
+from .pipeline import CodedLayer, ResidualBlock, IntegerBlock, calibrate_layer_by_layer, run_chain, code_layer, chain_gradients  # noqa: F401,E402

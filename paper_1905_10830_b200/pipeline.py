@@ -115,3 +115,67 @@ class ResidualBlock:
         dw = tc.tc_matmul_blocks(self.ctx, dy_channels, x_channels, dtype=torch.float32)
         inner = tc.tc_residual_norms_backward(self.ctx, h, None, dx, outer.h, before=self.before, eps=self.eps)
         return dict(h=inner.h, weight=dw.reshape(c, c), before=inner.before, after=outer.after, gate=outer.gate, scale=outer.scale)
+
+
+def _pixels(x: torch.Tensor) -> torch.Tensor:
+    """A channels_last tensor's pixels as a list of tokens, (N H W, C, 1, 1): a view."""
+    return x.permute(0, 2, 3, 1).reshape(-1, x.shape[1], 1, 1)
+
+
+class IntegerBlock:
+    """A residual block on 8-bit integers, as the paper's networks run their layers, to stand between two coded maps or to be trained:
+    s = h + W act(group_norm(h)), the 1 x 1 convolution W [C][C] as a product of integers with a scale for each pixel and each row of W.  Maps go in and
+    come out in the same order, contiguous (as the codec's are; the block's own are channels_last, which costs one copy) or channels_last.
+    Vectors are float32 CUDA tensors [C] or None.  Nothing is recorded for autograd: a training step takes its gradients from `gradients`."""
+
+    def __init__(self, ctx: tc.Context, weight: torch.Tensor, *, groups: int, norm_weight: torch.Tensor | None = None, norm_bias: torch.Tensor | None = None,
+                 eps: float = 1e-5, activation: str | None = "relu"):
+        if weight.dim() != 2 or weight.shape[0] != weight.shape[1]:
+            raise ValueError("weight: expected [C][C]")
+        self.ctx, self.groups, self.eps = ctx, groups, eps
+        self.norm = dict(weight=norm_weight, bias=norm_bias, activation=activation)
+        self.set_weight(weight)
+
+    def set_weight(self, weight: torch.Tensor) -> None:
+        """New values of W: its codes, by rows for the product and by columns for the gradient to its input."""
+        self.rows, self.columns = tc.tc_quantize_rows(self.ctx, weight[:, :, None, None].contiguous(), rows="both")
+
+    def _sum(self, a: torch.Tensor, b: torch.Tensor) -> torch.Tensor:
+        if a.is_contiguous():
+            return tc.tc_residual_norms(self.ctx, a, b.contiguous())[0]
+        n, c, h, w = a.shape
+        return tc.tc_residual_norms(self.ctx, _pixels(a), _pixels(b))[0].view(n, h, w, c).permute(0, 3, 1, 2)
+
+    def __call__(self, h: torch.Tensor) -> torch.Tensor:
+        n, _, hh, ww = h.shape
+        x = h.contiguous(memory_format=torch.channels_last)
+        codes, _ = tc.tc_group_norm(self.ctx, x, self.groups, eps=self.eps, codes=True, **self.norm)
+        y = tc.tc_matmul_rows(self.ctx, codes, self.rows, shape=(n, hh, ww), dtype=h.dtype, channels_last=not h.is_contiguous())
+        return self._sum(h if h.is_contiguous() else x, y)
+
+    def gradients(self, h: torch.Tensor, ds: torch.Tensor) -> dict:
+        """Gradients to `h`, the weight (float32) and the vectors, from the gradient `ds` of the block's output; the norm is computed again, the
+        products' operands in both directions are 8-bit integers."""
+        n, c, hh, ww = h.shape
+        x, d = (t.contiguous(memory_format=torch.channels_last) for t in (h, ds))
+        xn, stats = tc.tc_group_norm(self.ctx, x, self.groups, eps=self.eps, **self.norm)
+        d_pixels, d_channels = tc.tc_quantize_rows(self.ctx, d, rows="both")
+        dxn = tc.tc_matmul_rows(self.ctx, d_pixels, self.columns, shape=(n, hh, ww), dtype=h.dtype, channels_last=True)
+        dw = tc.tc_matmul_rows(self.ctx, d_channels, tc.tc_quantize_rows(self.ctx, xn, rows="channels"), dtype=torch.float32)
+        inner = tc.tc_group_norm_backward(self.ctx, x, dxn, stats, **self.norm)
+        return dict(h=self._sum(ds if ds.is_contiguous() else d, inner.x), weight=dw.reshape(c, c), norm_weight=inner.weight, norm_bias=inner.bias)
+
+
+def chain_gradients(ctx: tc.Context, blocks: Sequence, h: torch.Tensor, ds: torch.Tensor, max_norm: float):
+    """A training step's gradients through blocks that follow one another (ResidualBlock, IntegerBlock): each block's by its names and without its
+    input's, all of them clipped to `max_norm` together, and their norm before that (float32 [1])."""
+    inputs = [h]
+    for block in blocks[:-1]:
+        inputs.append(block(inputs[-1]))
+    grads = []
+    for block, x in zip(reversed(blocks), reversed(inputs)):
+        g = block.gradients(x, ds)
+        ds = g.pop("h")
+        grads.insert(0, g)
+    norm = tc.tc_clip_gradients(ctx, [v for g in grads for v in g.values() if v is not None], max_norm)
+    return grads, norm
