@@ -577,7 +577,7 @@ typedef struct {
 /* `y` (DEVICE, as x) and `codes` (by pixels, of y before it is rounded: what tc_matmul_rows reads) receive y; either or both.  `stats` DEVICE float [n][groups][2]
  * receives mean and rstd, or NULL.  Outputs overlap neither inputs nor each other.  Larger maps' moments live in the context's arena.  May be
  * captured into a graph.
- * Errors: INVALID_ARG, UNSUPPORTED (more than 8192 channels, more than 2^31 - 256 pixels), CUDA; TIMEOUT by tc_get_status. */
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 8192 channels, 2^31 - 256 pixels or 2^29 maps), CUDA; TIMEOUT by tc_get_status. */
 tc_status tc_group_norm(tc_ctx *ctx, const tc_tensor *x, const tc_group_params *params, void *y, const tc_rows *codes, float *stats, void *cuda_stream);
 
 /* Gradients from `dy` (DEVICE, as x) and the statistics that tc_group_norm wrote: `dx` (DEVICE, as x), and where they are wanted `dweight` and `dbias`

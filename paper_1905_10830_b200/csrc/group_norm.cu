@@ -5,123 +5,157 @@
 // Bound by the bytes moved, x once and y once.  Where a map fits the shared memory of a cluster's blocks (up to eight) it is read once: each block
 // takes its pixels there by bulk copies, finds its mean and then its squares about that mean, the blocks' moments are put together through
 // the cluster's shared memory, and the values leave from where they lie.  Larger maps, and rows that do not begin at 16 bytes, take
-// three kernels: moments of runs of pixels, their joining, and the values (last runs first: they are the likeliest to be in L2 still).
+// two kernels: moments of runs of pixels, and the values.
 //
 // Moments are put together as (n, mean, M2): no sum of squares is taken about a mean far from its own.
 #include "group_norm.cuh"
 #include "integer_codes.cuh"
-#include "sm100_ptx.cuh"
 
 namespace {
 
 using namespace groups;
 using rowcodes::Coder;
 
-// Mean and M2 (sum of squares about it) of each group over `pixels` pixels at `src`, to moments[group].
-template <typename T, int V>
-__device__ __forceinline__ void block_moments(const T *src, int pixels, const GroupArgs &a, const Lay &lay, float *red, float2 *moments)
-{
-    const int per_group = a.c / a.groups;
-    const float count = (float)pixels * (float)per_group;
-    for (int g = threadIdx.x; g < a.groups; g += blockDim.x) moments[g] = make_float2(0.f, 0.f);
-    for (int b = 0; b < lay.blocks; ++b) {
-        Pairs<V> sum = {};
-        if (lay.at(b)) {
-            const T *p = src + (long long)lay.row * a.c + (b * lay.lanes + lay.lane) * V;
-#pragma unroll 4
-            for (int i = lay.row; i < pixels; i += lay.rows, p += (long long)lay.rows * a.c) {
-                Pairs<V> v;
-                load_pairs<V>(p, v);
-#pragma unroll
-                for (int k = 0; k < kPairs<V>; ++k) sum[k] = add2(sum[k], v[k]);
-            }
-        }
-        add_groups<V>(lay, b, per_group, a.groups, sum, red, [&](int g, float s) { moments[g].x += s; });
-    }
-    __syncthreads();
-    for (int g = threadIdx.x; g < a.groups; g += blockDim.x) moments[g].x = pixels ? moments[g].x / count : 0.f;
-    __syncthreads();
-    for (int b = 0; b < lay.blocks; ++b) {
-        Pairs<V> sum = {};
-        if (lay.at(b)) {
-            const int c = (b * lay.lanes + lay.lane) * V;
-            const T *p = src + (long long)lay.row * a.c + c;
-            Pairs<V> minus, unused;
-            stats_pairs<V>(moments, c, per_group, minus, unused);
-#pragma unroll 4
-            for (int i = lay.row; i < pixels; i += lay.rows, p += (long long)lay.rows * a.c) {
-                Pairs<V> v;
-                load_pairs<V>(p, v);
-#pragma unroll
-                for (int k = 0; k < kPairs<V>; ++k) {
-                    const uint64_t d = add2(v[k], minus[k]);
-                    sum[k] = fma2(d, d, sum[k]);
-                }
-            }
-        }
-        add_groups<V>(lay, b, per_group, a.groups, sum, red, [&](int g, float s) { moments[g].y += s; });
-    }
-    __syncthreads();
-}
+constexpr int kBatch = 4;
 
-// Joins the moments of `parts` runs of pixels: of(i) = (mean, M2), run i having pixels(i).
-template <typename F, typename G>
-__device__ __forceinline__ float2 joined(int parts, float count, int per_group, float eps, G pixels, F of)
+// Mean and M2 (sum of squares about it) of each group over the pixels at `src`, in one pass: sums of the distances d of a channel's values from the
+// first pixel's, p, and of their squares; the channel's mean is m = p + sum d / n, its squares about that sum d^2 - (sum d)^2 / n.  p being one of the n
+// values, (p - m)^2 is at most n times the mean square distance: the difference loses no more than a factor of n.
+// to(group, (mean, M2)) by one thread each.  red: red_values() float2; channels: c float2 of (m, squares).
+template <typename T, int V, typename F>
+__device__ __forceinline__ void block_moments(const T *src, const Pieces &pieces, const GroupArgs &a, const Lay &lay, float2 *red, float2 *channels, F to)
 {
-    float mean = 0.f, m2 = 0.f;
-    for (int i = 0; i < parts; ++i) mean += of(i).x * ((float)pixels(i) * (float)per_group / count);
-    for (int i = 0; i < parts; ++i) {
-        const float2 m = of(i);
-        const float d = m.x - mean;
-        m2 += m.y + (float)pixels(i) * (float)per_group * d * d;
-    }
-    return make_float2(mean, 1.0f / sqrtf(m2 / count + eps));
-}
-
-// The values of `pixels` pixels at `src`, the first of them pixel `first` of the tensor; stats[group] as they are found in shared memory.
-template <typename T, int V, int kAct>
-__device__ __forceinline__ void write_values(const T *src, int pixels, long long first, const GroupArgs &a, const Lay &lay, const float2 *stats)
-{
-    const int per_group = a.c / a.groups;
+    const int per_group = a.c / a.groups, pixels = pieces.pixels;
+    const float per_pixel = 1.0f / (float)pixels, per_channel = 1.0f / (float)per_group, n = (float)pixels;
+    const bool in_warps = groups_in_warps(lay, per_group);
     for (int b = 0; b < lay.blocks; ++b) {
-        if (!lay.at(b)) continue;
+        Pairs<V> from = {}, sum = {}, squares = {};
+        const bool here = lay.at(b) && pixels > 0;
         const int c = (b * lay.lanes + lay.lane) * V;
-        Pairs<V> minus, slope, w, bias;
-        stats_pairs<V>(stats, c, per_group, minus, slope);
+        if (here) {
+            const T *const p = src + c;
+            for (int piece = 0; piece < pieces.count(); ++piece) {
+                pieces.wait(piece);
+                if (piece == 0) {
+                    load_pairs<V>(p, from);
+#pragma unroll
+                    for (int k = 0; k < kPairs<V>; ++k) from[k] ^= kMinus;
+                }
+                Raw<T, V> raw[kBatch];
+                in_batches<kBatch>(
+                    pieces.first(piece) + lay.row, pieces.end(piece), lay.rows, [&](int k, int i) { load_raw<V>(raw[k], p + i * a.c); },
+                    [&](int k, int, int second) {
+                        for (int h = 0; h < (second < 0 ? 1 : 2); ++h) {
+                            Pairs<V> v;
+                            pairs_of<V>(raw[k + h], v);
+#pragma unroll
+                            for (int j = 0; j < kPairs<V>; ++j) {
+                                const uint64_t d = add2(v[j], from[j]);
+                                sum[j] = add2(sum[j], d);
+                                squares[j] = fma2(d, d, squares[j]);
+                            }
+                        }
+                    });
+            }
+        }
+        float s[2 * kPairs<V>], q[2 * kPairs<V>];
+#pragma unroll
+        for (int k = 0; k < kPairs<V>; ++k) {
+            halves(sum[k], s[2 * k], s[2 * k + 1]);
+            halves(squares[k], q[2 * k], q[2 * k + 1]);
+        }
+        // a channel's mean and squares, and in warps its group's
+        channel_sums<V>(lay, b, s, q, red, [&](int ch, float sum_d, float sum_q) {
+            const float d = sum_d * per_pixel;
+            float mean = ch >= 0 && pixels > 0 ? load1(src + ch) + d : 0.f, m2 = ch >= 0 && pixels > 0 ? fmaf(-sum_d, d, sum_q) : 0.f;
+            if (in_warps) {
+                const float m = sum_over(mean, per_group) * per_channel;
+                m2 = sum_over(fmaf(n * (mean - m), mean - m, m2), per_group);
+                if (ch >= 0 && (ch & (per_group - 1)) == 0) to(ch / per_group, make_float2(m, m2));
+            } else if (ch >= 0)
+                channels[ch] = make_float2(mean, m2);
+        });
+    }
+    if (in_warps) return;
+    lay.sync();
+    // groups of so many channels: their means' mean, and what the channels' means are off it
+    const Team team(per_group, lay.threads);
+    for (int base = 0; base < a.groups; base += team.step) {
+        const int g = base + team.first;
+        const float2 *const at = channels + g * per_group;
+        const int count = g < a.groups ? per_group : 0;
+        float mean = 0.f, m2 = 0.f;
+        for (int i = team.rank; i < count; i += team.size) mean += at[i].x;
+        mean = team.sum(mean) * per_channel;
+        for (int i = team.rank; i < count; i += team.size) {
+            const float2 t = at[i];
+            m2 += fmaf(n * (t.x - mean), t.x - mean, t.y);
+        }
+        m2 = team.sum(m2);
+        if (g < a.groups && team.rank == 0) to(g, make_float2(mean, m2));
+    }
+}
+
+// What a thread's values are computed with: y = act((x + minus) slope + bias).
+template <int V> struct Affine {
+    Pairs<V> minus, slope, bias;
+    // stats(group): mean and 1 / deviation
+    template <typename F>
+    __device__ __forceinline__ Affine(const GroupArgs &a, int c, F stats)
+    {
+        stats_pairs<V>(c, a.c / a.groups, minus, slope, stats);
+        Pairs<V> w;
         vector_pairs<V>(a.weight, c, 1.f, w);
         vector_pairs<V>(a.bias, c, 0.f, bias);
 #pragma unroll
         for (int k = 0; k < kPairs<V>; ++k) slope[k] = mul2(slope[k], w[k]);
-        const long long at = (long long)lay.row * a.c + c, step = (long long)lay.rows * a.c;
-        const T *p = src + at;
-        T *q = (T *)a.out + first * a.c + at;
-#pragma unroll 4
-        for (int i = lay.row; i < pixels; i += lay.rows, p += step, q += step) {
-            Pairs<V> v;
-            load_pairs<V>(p, v);
+    }
+};
+// The values of `pixels` pixels at `src`, the first of them pixel `first` of the tensor.
+template <typename T, int V, int kAct, typename F>
+__device__ __forceinline__ void write_values(const T *src, int pixels, long long first, const GroupArgs &a, const Lay &lay, F stats)
+{
+    for (int b = 0; b < lay.blocks; ++b) {
+        if (!lay.at(b)) continue;
+        const int c = (b * lay.lanes + lay.lane) * V;
+        const Affine<V> f(a, c, stats);
+        const T *const p = src + c;
+        T *const q = (T *)a.out + first * a.c + c;
+        Raw<T, V> raw[kBatch];
+        in_batches<kBatch>(
+            lay.row, pixels, lay.rows, [&](int k, int i) { load_raw<V>(raw[k], p + i * a.c); },
+            [&](int k, int i, int second) {
+                Pairs<V> v, w;
+                pairs_of<V>(raw[k], v);
+                pairs_of<V>(raw[k + 1], w);
 #pragma unroll
-            for (int k = 0; k < kPairs<V>; ++k) v[k] = activate2<kAct>(fma2(add2(v[k], minus[k]), slope[k], bias[k]));
-            store_pairs<V>(q, v);
-        }
+                for (int j = 0; j < kPairs<V>; ++j) {
+                    v[j] = activate2<kAct>(fma2(add2(v[j], f.minus[j]), f.slope[j], f.bias[j]));
+                    w[j] = activate2<kAct>(fma2(add2(w[j], f.minus[j]), f.slope[j], f.bias[j]));
+                }
+                store_pairs<V>(q + i * a.c, v);
+                if (second >= 0) store_pairs<V>(q + second * a.c, w);
+            });
     }
 }
 
 // The same as codes, and as values too where they are wanted: a team of lanes a pixel, its largest magnitude first.  `table`: [3][c] floats of shared memory.
-template <typename T, int V, int kAct>
-__device__ __forceinline__ void write_codes(const T *src, int pixels, long long first, const GroupArgs &a, const float2 *stats, float *table)
+template <typename T, int V, int kAct, typename F>
+__device__ __forceinline__ void write_codes(const T *src, int pixels, long long first, const GroupArgs &a, const Lay &lay, F stats, float *table)
 {
     const int per_group = a.c / a.groups;
-    for (int c = threadIdx.x; c < a.c; c += blockDim.x) {
-        const float2 s = stats[c / per_group];
+    lay.sync();                                               // the last table's readers
+    for (int c = threadIdx.x; c < a.c; c += lay.threads) {
+        const float2 s = stats(c / per_group);
         table[c] = -s.x;
         table[a.c + c] = s.y * (a.weight ? a.weight[c] : 1.f);
         table[2 * a.c + c] = a.bias ? a.bias[c] : 0.f;
     }
-    __syncthreads();
+    lay.sync();
     const int columns = a.c / V;
     int size = 1;
     while (size < 32 && size < columns) size *= 2;
-    const int rank = threadIdx.x & (size - 1), step = blockDim.x / size;
+    const int rank = threadIdx.x & (size - 1), step = lay.threads / size;
     auto values = [&](int pixel, int c, Pairs<V> &v) {
         load_pairs<V>(src + (long long)pixel * a.c + c, v);
         Pairs<V> minus, slope, bias;
@@ -166,23 +200,26 @@ __device__ __forceinline__ void write_codes(const T *src, int pixels, long long 
 }
 
 // ---- maps in a cluster's shared memory --------------------------------------------------------
-// [data, to 16 bytes][red: threads x V floats][moments: groups float2][stats: groups float2][table of the codes: 3 c floats, room for which there
-// always is: a map is cut the same way, and has the same statistics to the last bit, whatever is asked for]
+// [data, to 16 bytes][red: red_values() float2][moments: groups float2][stats: groups float2][table of the codes: 3 c floats, room for which there
+// always is: a map is cut the same way, and has the same statistics to the last bit, whatever is asked for; before it, the channels' c float2]
 size_t shared_bytes(const GroupArgs &a, int pixels, int element, int v, int threads)
 {
-    return ((size_t)pixels * a.c * element + 15) / 16 * 16 + (size_t)threads * v * 4 + 16 * (size_t)a.groups + 12 * (size_t)a.c;
+    return ((size_t)pixels * a.c * element + 15) / 16 * 16 + 8 * (size_t)red_values(a.c / v, threads, v) + 16 * (size_t)a.groups + 12 * (size_t)a.c;
 }
 
 template <typename T, int V, int kAct, bool kCodes>
-__global__ void __launch_bounds__(512) group_norm_map_kernel(const __grid_constant__ GroupArgs a)
+__global__ void __launch_bounds__(512, 2) group_norm_map_kernel(const __grid_constant__ GroupArgs a)
 {
     using namespace sm100;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ __align__(8) unsigned long long s_full;
+    __shared__ __align__(8) unsigned long long s_full[kPieces];
     T *const data = reinterpret_cast<T *>(smem);
-    float *const red = reinterpret_cast<float *>(smem + ((size_t)a.share * a.c * sizeof(T) + 15) / 16 * 16);
-    float2 *const moments = reinterpret_cast<float2 *>(red + blockDim.x * V), *const stats = moments + a.groups;
-    if (threadIdx.x == 0) { mbar_init(smem_u32(&s_full), 1); mbar_fence_init(); }
+    float2 *const red = reinterpret_cast<float2 *>(smem + ((size_t)a.share * a.c * sizeof(T) + 15) / 16 * 16);
+    float2 *const moments = red + red_values(a.c / V, blockDim.x, V), *const stats = moments + a.groups, *const table = stats + a.groups;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kPieces; ++i) mbar_init(smem_u32(&s_full[i]), 1);
+        mbar_fence_init();
+    }
     __syncthreads();
     chain_next();
     chain_wait();
@@ -190,126 +227,165 @@ __global__ void __launch_bounds__(512) group_norm_map_kernel(const __grid_consta
     const long long map = blockIdx.x / a.shares;
     const int p0 = rank * a.share, pixels = max(0, min(a.share, a.hw - p0)), per_group = a.c / a.groups;
     const long long first = map * a.hw + p0;
-    if (pixels) {
-        if (threadIdx.x == 0) {
-            const uint32_t bytes = (uint32_t)pixels * a.c * sizeof(T);
-            mbar_arrive_expect_tx(smem_u32(&s_full), bytes);
-            const char *const src = (const char *)((const T *)a.x + first * a.c);
-            for (uint32_t at = 0; at < bytes; at += 16384) bulk_load(smem_u32(smem) + at, src + at, min(16384u, bytes - at), smem_u32(&s_full));
+    const Lay lay(a.c / V, blockDim.x);
+    const Pieces pieces(pixels, lay.rows, s_full, a.status);
+    if (threadIdx.x == 0) {
+        const char *const src = (const char *)((const T *)a.x + first * a.c);
+        const uint32_t row = (uint32_t)a.c * sizeof(T);
+        for (int i = 0; i < kPieces; ++i) {
+            const uint32_t from = pieces.first(i) * row, to = pieces.end(i) * row;
+            if (from == to) break;
+            mbar_arrive_expect_tx(smem_u32(&s_full[i]), to - from);
+            for (uint32_t at = from; at < to; at += 16384) bulk_load(smem_u32(smem) + at, src + at, min(16384u, to - at), smem_u32(&s_full[i]));
         }
-        // (a wait that runs out is reported; the values are wrong then, nothing else)
-        if (!mbar_wait_soon(smem_u32(&s_full), 0) && !mbar_wait_soon(smem_u32(&s_full), 0)) tc_dev_set_status(a.status, TC_ERR_TIMEOUT);
     }
-    const Lay lay(a.c / V);
-    block_moments<T, V>(data, pixels, a, lay, red, moments);
+    block_moments<T, V>(data, pieces, a, lay, red, table, [&](int g, float2 m) { moments[g] = m; });
     if (a.shares > 1) cluster_sync();
+    else __syncthreads();
     const float count = (float)a.hw * (float)per_group;
     for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
-        const float2 s = joined(a.shares, count, per_group, a.eps, [&](int i) { return max(0, min(a.share, a.hw - i * a.share)); }, [&](int i) {
-            float2 m;
-            asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(m.x), "=f"(m.y) : "r"(peer_address(&moments[g], (uint32_t)i)));
-            return m;
-        });
+        float2 m[kMostShares];
+        if (a.shares > 1) of_cluster(&moments[g], a.shares, m);
+        else m[0] = moments[g];
+        float mean = 0.f, m2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < kMostShares; ++i)
+            if (i < a.shares) mean += m[i].x * ((float)max(0, min(a.share, a.hw - i * a.share)) * (float)per_group / count);
+#pragma unroll
+        for (int i = 0; i < kMostShares; ++i)
+            if (i < a.shares) {
+                const float d = m[i].x - mean;
+                m2 += m[i].y + (float)max(0, min(a.share, a.hw - i * a.share)) * (float)per_group * d * d;
+            }
+        const float2 s = make_float2(mean, 1.0f / sqrtf(m2 / count + a.eps));
         stats[g] = s;
         if (rank == 0 && a.stats) a.stats[map * a.groups + g] = s;
     }
     __syncthreads();
     if (a.shares > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    if constexpr (kCodes) write_codes<T, V, kAct>(data, pixels, first, a, stats, reinterpret_cast<float *>(stats + a.groups));
-    else write_values<T, V, kAct>(data, pixels, first, a, lay, stats);
+    auto of = [&](int g) { return stats[g]; };
+    if constexpr (kCodes) write_codes<T, V, kAct>(data, pixels, first, a, lay, of, reinterpret_cast<float *>(table));
+    else write_values<T, V, kAct>(data, pixels, first, a, lay, of);
     if (a.shares > 1) {
         __syncwarp();
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");       // the others have read this block's moments
     }
 }
 
-// ---- any maps ----------------------------------------------------------------------------------
-// part[map][share][group]: moments of a run of pixels.
-template <typename T, int V>
-__global__ void __launch_bounds__(512) group_moments_kernel(const __grid_constant__ GroupArgs a)
+// ---- maps in runs of pixels ----------------------------------------------------------------------
+// A group's mean and 1 / deviation from its runs' moments, by a team of `size` lanes, as block_moments about the first run's mean.
+__device__ __forceinline__ float2 join_runs(const GroupArgs &a, long long map, int g, int rank, int size)
 {
-    extern __shared__ __align__(128) unsigned char smem[];
-    float *const red = reinterpret_cast<float *>(smem);
-    float2 *const moments = reinterpret_cast<float2 *>(red + blockDim.x * V);
-    chain_next();
-    chain_wait();
-    const long long map = blockIdx.x / a.shares;
-    const int p0 = (int)(blockIdx.x % a.shares) * a.share, pixels = max(0, min(a.share, a.hw - p0));
-    const Lay lay(a.c / V);
-    block_moments<T, V>((const T *)a.x + (map * a.hw + p0) * a.c, pixels, a, lay, red, moments);
-    for (int g = threadIdx.x; g < a.groups; g += blockDim.x) a.part[(long long)blockIdx.x * a.groups + g] = moments[g];
+    const int per_group = a.c / a.groups;
+    const float2 *const at = a.part + map * a.shares * a.groups + g;
+    const float from = at->x;
+    float s = 0.f, q = 0.f;                                   // in units of a run's values
+#pragma unroll 4
+    for (int r = rank; r < a.shares; r += size) {
+        const float2 m = at[(long long)r * a.groups];
+        const float n = (float)min(a.share, a.hw - r * a.share), d = m.x - from;
+        s = fmaf(n, d, s);
+        q += fmaf(n * (float)per_group * d, d, m.y);
+    }
+    s = sum_over(s, size);
+    q = sum_over(q, size);
+    const float d = s / (float)a.hw;
+    return make_float2(from + d, 1.0f / sqrtf(fmaxf(fmaf(-s * (float)per_group, d, q), 0.f) / ((float)a.hw * (float)per_group) + a.eps));
 }
 
-// sums[map][group]: mean and 1 / deviation of a map's groups, a warp each.
+// Maps of many runs: sums[map][group], a warp each.
 __global__ void __launch_bounds__(256) group_join_kernel(const __grid_constant__ GroupArgs a)
 {
     chain_next();
     chain_wait();
     const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) / 32;
-    const int lane = threadIdx.x & 31, per_group = a.c / a.groups;
     if (i >= a.n * a.groups) return;
-    const long long map = i / a.groups;
-    const int g = (int)(i - map * a.groups);
-    const float count = (float)a.hw * (float)per_group;
-    auto pixels = [&](int s) { return (float)max(0, min(a.share, a.hw - s * a.share)); };
-    auto of = [&](int s) { return a.part[(map * a.shares + s) * a.groups + g]; };
-    float mean = 0.f, m2 = 0.f;
-    for (int s = lane; s < a.shares; s += 32) mean += of(s).x * (pixels(s) * (float)per_group / count);
-    for (int d = 16; d; d >>= 1) mean += __shfl_xor_sync(0xffffffffu, mean, d);
-    for (int s = lane; s < a.shares; s += 32) {
-        const float2 m = of(s);
-        m2 += m.y + pixels(s) * (float)per_group * (m.x - mean) * (m.x - mean);
-    }
-    for (int d = 16; d; d >>= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, d);
-    if (lane) return;
-    const float2 s = make_float2(mean, 1.0f / sqrtf(m2 / count + a.eps));
-    a.sums[i] = s;
-    if (a.stats) a.stats[i] = s;
+    const float2 v = join_runs(a, i / a.groups, (int)(i % a.groups), threadIdx.x & 31, 32);
+    if (threadIdx.x & 31) return;
+    a.sums[i] = v;
+    if (a.stats) a.stats[i] = v;
 }
 
-template <typename T, int V, int kAct, bool kCodes>
-__global__ void __launch_bounds__(512) group_values_kernel(const __grid_constant__ GroupArgs a)
+// part[map][run][group]: moments of a run of pixels.  [red: red_values() float2][channels: c float2]
+template <typename T, int V>
+__global__ void __launch_bounds__(kRunThreads, 4) group_moments_kernel(const __grid_constant__ GroupArgs a)
 {
     extern __shared__ __align__(128) unsigned char smem[];
-    float2 *const stats = reinterpret_cast<float2 *>(smem);
+    float2 *const red = reinterpret_cast<float2 *>(smem), *const channels = red + red_values(a.c / V, kRunThreads, V);
     chain_next();
     chain_wait();
-    const long long block = (long long)gridDim.x - 1 - blockIdx.x, map = block / a.shares;
-    const int p0 = (int)(block % a.shares) * a.share, pixels = max(0, min(a.share, a.hw - p0));
-    for (int g = threadIdx.x; g < a.groups; g += blockDim.x) stats[g] = a.sums[map * a.groups + g];
+    const Lay lay(a.c / V, kRunThreads);
+    const Run run(a, blockIdx.x);
+    float2 *const part = a.part + (long long)run.index * a.groups;
+    block_moments<T, V>((const T *)a.x + run.first * a.c, Pieces(run.pixels, lay.rows, nullptr, a.status), a, lay, red, channels, [&](int g, float2 m) { part[g] = m; });
+}
+
+// The values, the last runs first: they are the likeliest to be in L2 still.  [stats: groups float2][table of the codes: 3 c floats]
+template <typename T, int V, int kAct, bool kCodes>
+__global__ void __launch_bounds__(kRunThreads, 4) group_values_kernel(const __grid_constant__ GroupArgs a)
+{
+    extern __shared__ __align__(128) unsigned char smem[];
+    float2 *const own = reinterpret_cast<float2 *>(smem);
+    chain_next();
+    chain_wait();
+    const Lay lay(a.c / V, kRunThreads);
+    const Run run(a, gridDim.x - 1 - blockIdx.x);
+    if (a.sums)
+        for (int g = threadIdx.x; g < a.groups; g += kRunThreads) own[g] = a.sums[run.map * a.groups + g];
+    else {
+        const Team team(a.shares, kRunThreads);
+        for (int base = 0; base < a.groups; base += team.step) {
+            const int g = base + team.first;
+            const float2 v = join_runs(a, run.map, min(g, a.groups - 1), team.rank, team.size);
+            if (g < a.groups && team.rank == 0) {
+                own[g] = v;
+                if (a.stats && run.run == 0) a.stats[run.map * a.groups + g] = v;
+            }
+        }
+    }
     __syncthreads();
-    const long long first = map * a.hw + p0;
-    const T *const src = (const T *)a.x + first * a.c;
-    const Lay lay(a.c / V);
-    if constexpr (kCodes) write_codes<T, V, kAct>(src, pixels, first, a, stats, reinterpret_cast<float *>(stats + a.groups));
-    else write_values<T, V, kAct>(src, pixels, first, a, lay, stats);
+    const T *const src = (const T *)a.x + run.first * a.c;
+    auto stats = [&](int g) { return own[g]; };
+    if constexpr (kCodes) write_codes<T, V, kAct>(src, run.pixels, run.first, a, lay, stats, reinterpret_cast<float *>(own + a.groups));
+    else write_values<T, V, kAct>(src, run.pixels, run.first, a, lay, stats);
 }
 
 template <typename T, int V, int kAct, bool kCodes>
 tc_status launch_map(int device, const GroupArgs &a, int threads, size_t smem, cudaStream_t s)
 {
     constexpr auto kernel = group_norm_map_kernel<T, V, kAct, kCodes>;
-    if (!allow_shared<kernel>(device, 225 * 1024)) return TC_ERR_CUDA;
+    if (!allow_shared<kernel>(device, kMostShared) || !allow_large_clusters<kernel>(device)) return TC_ERR_CUDA;
     return launch_first_cluster(a.shares, kernel, dim3((unsigned int)(a.n * a.shares)), dim3(threads), smem, s, a) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
 template <typename T, int V, int kAct, bool kCodes>
-tc_status launch_any(int device, const GroupArgs &a, int threads, cudaStream_t s)
+tc_status launch_runs(int device, const GroupArgs &a, cudaStream_t s)
 {
-    const size_t first = (size_t)threads * V * 4 + 8 * (size_t)a.groups, last = 8 * (size_t)a.groups + (kCodes ? 12 * (size_t)a.c : 0);
-    if (!allow_shared<group_moments_kernel<T, V>>(device, 225 * 1024) || !allow_shared<group_values_kernel<T, V, kAct, kCodes>>(device, 225 * 1024)) return TC_ERR_CUDA;
-    const dim3 grid((unsigned int)(a.n * a.shares)), block(threads);
+    const size_t first = 8 * (size_t)red_values(a.c / V, kRunThreads, V) + 8 * (size_t)a.c, last = 8 * (size_t)a.groups + (kCodes ? 12 * (size_t)a.c : 0);
+    if (!allow_shared<group_moments_kernel<T, V>>(device, kMostShared) || !allow_shared<group_values_kernel<T, V, kAct, kCodes>>(device, kMostShared)) return TC_ERR_CUDA;
+    const dim3 grid((unsigned int)(a.n * a.shares)), block(kRunThreads);
     if (launch_first(true, group_moments_kernel<T, V>, grid, block, first, s, a) != cudaSuccess) return TC_ERR_CUDA;
-    if (launch_chained(true, group_join_kernel, dim3((unsigned int)((a.n * a.groups + 7) / 8)), dim3(256), 0, s, a) != cudaSuccess) return TC_ERR_CUDA;
+    if (a.sums && launch_chained(true, group_join_kernel, dim3((unsigned int)((a.n * a.groups + 7) / 8)), dim3(256), 0, s, a) != cudaSuccess) return TC_ERR_CUDA;
     return launch_chained(true, group_values_kernel<T, V, kAct, kCodes>, grid, block, last, s, a) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
 
 template <typename T, int V>
-tc_status launch(int device, const GroupArgs &a, int act, int threads, size_t smem, cudaStream_t s)
+tc_status launch(int device, const GroupArgs &a, const GroupPlan &p, int act, cudaStream_t s)
 {
-#define TC_NORM(kAct) \
-    (smem ? a.codes.codes ? launch_map<T, V, kAct, true>(device, a, threads, smem, s) : launch_map<T, V, kAct, false>(device, a, threads, smem, s) \
-          : a.codes.codes ? launch_any<T, V, kAct, true>(device, a, threads, s) : launch_any<T, V, kAct, false>(device, a, threads, s))
-    return act == kRelu ? TC_NORM(kRelu) : act == kSilu ? TC_NORM(kSilu) : TC_NORM(kNoAct);
+    // (maps of single values never lie in shared memory: bulk copies begin at 16 bytes)
+#define TC_NORM(kAct, kCodes) \
+    do { \
+        if constexpr (V > 1) \
+            if (p.shared) return launch_map<T, V, kAct, kCodes>(device, a, p.threads, p.shared, s); \
+        return launch_runs<T, V, kAct, kCodes>(device, a, s); \
+    } while (0)
+    if (a.codes.codes) {
+        if (act == kRelu) TC_NORM(kRelu, true);
+        if (act == kSilu) TC_NORM(kSilu, true);
+        TC_NORM(kNoAct, true);
+    }
+    if (act == kRelu) TC_NORM(kRelu, false);
+    if (act == kSilu) TC_NORM(kSilu, false);
+    TC_NORM(kNoAct, false);
 #undef TC_NORM
 }
 
@@ -326,6 +402,34 @@ int tc_group_threads(int columns)
     return best;
 }
 
+// Runs of pixels (of `row` bytes in each of `tensors`) of a map.
+void cut_runs(GroupPlan &p, long long n, int hw, long long row, int tensors, int sm_count)
+{
+    // of eight pixels at least where their channels' sums are written too; shorter than kRunBytes where SMs would be idle
+    long long share = std::max(tensors > 1 ? 8ll : 1ll, kRunBytes / (row * tensors));
+    while (share > 1 && n * ((hw + share - 1) / share) < 2ll * sm_count) share = (share + 1) / 2;
+    share = std::max(share, ((long long)hw * n + (1ll << 29) - 1) >> 29);
+    const long long runs = (hw + std::min<long long>(share, hw) - 1) / std::min<long long>(share, hw);
+    p.share = (int)((hw + runs - 1) / runs);                  // (of one size but for the last)
+    p.shares = (hw + p.share - 1) / p.share;
+    p.join = p.shares > kInlineRuns;
+}
+
+// Blocks of a map where maps lie in clusters' shared memory; 0: they do not.  As few as let two share an SM, then as few as fit one, where all of them are `most` at
+// most, and more where SMs would be idle.  More maps than find a place at a time take the other kernels: a block's phases (wait, sums, cluster, values) follow one another,
+// and little of the next one's waiting falls into them (1024 maps of 256x14x14 bf16: 64 us and 70, their gradient 173 and 168; 64 of 512x28x28 45 and 53, 125 and 77).
+int shares_on_chip(long long n, int hw, long long most, int sm_count, const std::function<size_t(int)> &bytes)
+{
+    for (const size_t room : {kTwoBlocks, kMostShared}) {
+        int shares = 1;
+        while (shares < groups::kMostShares && bytes(shares) > room) shares *= 2;
+        if (bytes(shares) > room || n * shares > most) continue;
+        while (shares < 8 && n * shares * 2 <= sm_count && hw / shares >= 16) shares *= 2;
+        return shares;
+    }
+    return 0;
+}
+
 GroupPlan tc_plan_group_norm(const GroupNormArgs &m, int sm_count)
 {
     GroupPlan p;
@@ -337,25 +441,16 @@ GroupPlan tc_plan_group_norm(const GroupNormArgs &m, int sm_count)
     a.groups = m.groups;
     auto bytes = [&](int shares) { return shared_bytes(a, (m.hw + shares - 1) / shares, element, p.vector, p.threads); };
     if (p.vector > 1) {
-        // as few blocks a map as let three share an SM (one loads while the others work), then as many as the SMs take
-        int shares = 1;
-        while (shares < 8 && bytes(shares) > 73 * 1024) shares *= 2;
-        while (shares < 8 && (long long)m.n * shares * 2 <= sm_count && m.hw / shares >= 16) shares *= 2;
-        if (bytes(shares) <= 225 * 1024 && (long long)m.n * shares < 1ll << 31) {
+        const int shares = shares_on_chip(m.n, m.hw, 2ll * sm_count, sm_count, bytes);
+        if (shares) {
             p.shares = shares;
             p.share = (m.hw + shares - 1) / shares;
             p.shared = bytes(shares);
             return p;
         }
     }
-    // runs of about 64 KB, as many as let every SM have several
-    const long long row = (long long)m.c * element;
-    long long share = std::max(1ll, 65536 / row);
-    while (share > 1 && (long long)m.n * ((m.hw + share - 1) / share) < 4ll * sm_count) share = (share + 1) / 2;
-    share = std::max(share, ((long long)m.hw * m.n + (1ll << 30) - 1) >> 30);
-    p.share = (int)std::min<long long>(share, m.hw);
-    p.shares = (m.hw + p.share - 1) / p.share;
-    p.workspace = (size_t)m.n * m.groups * sizeof(float2) * (p.shares + 1);
+    cut_runs(p, m.n, m.hw, (long long)m.c * element, 1, sm_count);
+    p.workspace = (size_t)m.n * m.groups * sizeof(float2) * (p.shares + (p.join ? 1 : 0));
     return p;
 }
 
@@ -377,9 +472,9 @@ tc_status tc_launch_group_norm(int device, const GroupNormArgs &m, const GroupPl
     a.shares = p.shares;
     a.status = m.status;
     if (!p.shared) {
-        a.sums = (float2 *)workspace;
-        a.part = a.sums + (long long)a.n * a.groups;
+        a.part = (float2 *)workspace;
+        if (p.join) a.sums = a.part + (long long)a.n * a.groups * a.shares;
     }
-    if (m.dtype == TC_BF16) return p.vector == 8 ? launch<__nv_bfloat16, 8>(device, a, m.act, p.threads, p.shared, s) : launch<__nv_bfloat16, 1>(device, a, m.act, p.threads, p.shared, s);
-    return p.vector == 4 ? launch<float, 4>(device, a, m.act, p.threads, p.shared, s) : launch<float, 1>(device, a, m.act, p.threads, p.shared, s);
+    if (m.dtype == TC_BF16) return p.vector == 8 ? launch<__nv_bfloat16, 8>(device, a, p, m.act, s) : launch<__nv_bfloat16, 1>(device, a, p, m.act, s);
+    return p.vector == 4 ? launch<float, 4>(device, a, p, m.act, s) : launch<float, 1>(device, a, p, m.act, s);
 }

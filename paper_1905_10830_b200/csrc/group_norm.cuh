@@ -7,13 +7,18 @@
 // column blocks.
 #pragma once
 
+#include <functional>
+
 #include "block_codes.cuh"
+#include "sm100_ptx.cuh"
 #include "tc_internal.h"
 
 namespace groups {
 
 using namespace tcdev;
 using namespace blk;
+
+constexpr int kRunThreads = 256;                               // of the kernels that work on runs of pixels
 
 enum { kNoAct = 0, kRelu = 1, kSilu = 2 };
 
@@ -33,30 +38,57 @@ struct GroupArgs {
     unsigned int *status;
 };
 
-// V values as pairs (one value: a pair with a zero).
+// V values as they lie in memory, and as pairs (one value: a pair with a zero).  Loops load some vectors before they work on the first: a store between two loads
+// would keep the second back, for all the compiler knows of what overlaps.
 template <int V> constexpr int kPairs = (V + 1) / 2;
 template <int V> using Pairs = uint64_t[kPairs<V>];
+template <typename T, int V> struct Raw { uint4 v; };
+template <typename T> struct Raw<T, 1> { float v; };
 
-template <int V>
-__device__ __forceinline__ void load_pairs(const __nv_bfloat16 *p, Pairs<V> &v)
+template <int V, typename T>
+__device__ __forceinline__ void load_raw(Raw<T, V> &r, const T *p)
+{
+    if constexpr (V > 1) r.v = *reinterpret_cast<const uint4 *>(p);
+    else r.v = load1(p);
+}
+template <int V, typename T>
+__device__ __forceinline__ void pairs_of(const Raw<T, V> &r, Pairs<V> &v)
 {
     if constexpr (V == 8) {
-        const uint4 r = *reinterpret_cast<const uint4 *>(p);
-        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+        const uint32_t w[4] = {r.v.x, r.v.y, r.v.z, r.v.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = pair_of(w[i] << 16, w[i] & 0xffff0000u);
+    } else if constexpr (V == 4) {
+        v[0] = pair_of(r.v.x, r.v.y);
+        v[1] = pair_of(r.v.z, r.v.w);
     } else
-        v[0] = pair_of(load1(p), 0.f);
+        v[0] = pair_of(r.v, 0.f);
 }
-template <int V>
-__device__ __forceinline__ void load_pairs(const float *p, Pairs<V> &v)
+template <int V, typename T>
+__device__ __forceinline__ void load_pairs(const T *p, Pairs<V> &v)
 {
-    if constexpr (V == 4) {
-        const uint4 r = *reinterpret_cast<const uint4 *>(p);
-        v[0] = pair_of(r.x, r.y);
-        v[1] = pair_of(r.z, r.w);
-    } else
-        v[0] = pair_of(*p, 0.f);
+    Raw<T, V> r;
+    load_raw<V>(r, p);
+    pairs_of<V>(r, v);
+}
+// load(place, i) and then work(place, i, i2) for pairs of the pixels i and i2 of a thread, from `first` on in steps of `rows`, kBatch (even) loaded at a time; an odd last one comes
+// with i2 = -1, and loaded(place) of the place behind it is what load left there before.
+template <int kBatch, typename L, typename W>
+__device__ __forceinline__ void in_batches(int first, int end, int rows, L load, W work)
+{
+    int i = first;
+    for (; i + (kBatch - 1) * rows < end; i += kBatch * rows) {
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) load(k, i + k * rows);
+#pragma unroll
+        for (int k = 0; k < kBatch; k += 2) work(k, i + k * rows, i + (k + 1) * rows);
+    }
+    for (; i < end; i += 2 * rows) {
+        const bool two = i + rows < end;
+        load(0, i);
+        load(1, two ? i + rows : i);
+        work(0, i, two ? i + rows : -1);
+    }
 }
 template <int V, typename T>
 __device__ __forceinline__ void store_pairs(T *p, const Pairs<V> &v)
@@ -72,71 +104,150 @@ __device__ __forceinline__ void store_pairs(T *p, const Pairs<V> &v)
 template <int V>
 __device__ __forceinline__ void vector_pairs(const float *p, int c, float other, Pairs<V> &v)
 {
+    if constexpr (V % 4 == 0) {
+        if (p && ((uintptr_t)p & 15u) == 0) {
+#pragma unroll
+            for (int i = 0; i < V; i += 4) {
+                const float4 f = *reinterpret_cast<const float4 *>(p + c + i);
+                v[i / 2] = pair_of(f.x, f.y);
+                v[i / 2 + 1] = pair_of(f.z, f.w);
+            }
+            return;
+        }
+    }
     float f[2 * kPairs<V>] = {};
 #pragma unroll
     for (int i = 0; i < V; ++i) f[i] = p ? p[c + i] : other;
 #pragma unroll
     for (int i = 0; i < kPairs<V>; ++i) v[i] = pair_of(f[2 * i], f[2 * i + 1]);
 }
-// Means (negated) and 1 / deviations of V channels' groups.
-template <int V>
-__device__ __forceinline__ void stats_pairs(const float2 *stats, int c, int per_group, Pairs<V> &minus_mean, Pairs<V> &rstd)
+// First (negated) and second value of V channels' groups: of(group).
+template <int V, typename F>
+__device__ __forceinline__ void stats_pairs(int c, int per_group, Pairs<V> &minus, Pairs<V> &second, F of)
 {
+    int g = c / per_group, rest = c - g * per_group;
+    float2 s = of(g);
+    if (rest + V <= per_group) {
+#pragma unroll
+        for (int i = 0; i < kPairs<V>; ++i) {
+            minus[i] = pair_of(-s.x, -s.x);
+            second[i] = pair_of(s.y, s.y);
+        }
+        return;
+    }
     float m[2 * kPairs<V>] = {}, r[2 * kPairs<V>] = {};
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const float2 s = stats[(c + i) / per_group];
+        if (i && ++rest == per_group) {
+            rest = 0;
+            s = of(++g);
+        }
         m[i] = -s.x;
         r[i] = s.y;
     }
 #pragma unroll
     for (int i = 0; i < kPairs<V>; ++i) {
-        minus_mean[i] = pair_of(m[2 * i], m[2 * i + 1]);
-        rstd[i] = pair_of(r[2 * i], r[2 * i + 1]);
+        minus[i] = pair_of(m[2 * i], m[2 * i + 1]);
+        second[i] = pair_of(r[2 * i], r[2 * i + 1]);
     }
 }
+constexpr uint64_t kMinus = 0x8000000080000000ull;             // a pair's signs
 __device__ __forceinline__ uint64_t both(float v) { return pair_of(v, v); }
 
-// 1 / (1 + e^-z): an fp32 exponential and quotient of a few roundings each; 0 where e^-z is beyond fp32.
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
-template <int kAct>
-__device__ __forceinline__ float activate(float z)
+__device__ __forceinline__ float max_nan(float a, float b)    // (a NaN stays one)
 {
-    return kAct == kRelu ? (z < 0.f ? 0.f : z) : kAct == kSilu ? z * sigmoid(z) : z;
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
 }
+// 1 / (1 + e^-z) of two pixels' pairs a and b, each value's two reciprocals from one of their product: the functions' unit takes three operations for two values instead of four,
+// and it is what bounds the gradient.  The two are of one channel, so a NaN stays in its group.  z is taken as -44 at least, where the result is 8e-20 and products of two
+// denominators stay in range.  The fast exponential and reciprocal, a few steps of 2^-23 each.
+__device__ __forceinline__ float exp2_fast(float v)
+{
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v));
+    return e;
+}
+__device__ __forceinline__ float reciprocal_fast(float v)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t at_least(uint64_t z, float least)
+{
+    float x, y;
+    halves(z, x, y);
+    return pair_of(max_nan(x, least), max_nan(y, least));
+}
+__device__ __forceinline__ uint64_t denominator(uint64_t z)
+{
+    float x, y;
+    halves(mul2(z, both(-1.4426950408889634f)), x, y);
+    return add2(pair_of(exp2_fast(x), exp2_fast(y)), both(1.0f));
+}
+__device__ __forceinline__ void sigmoids(uint64_t &za, uint64_t &zb, uint64_t &sa, uint64_t &sb)
+{
+    za = at_least(za, -44.0f);
+    zb = at_least(zb, -44.0f);
+    const uint64_t da = denominator(za), db = denominator(zb);
+    float x, y;
+    halves(mul2(da, db), x, y);
+    const uint64_t r = pair_of(reciprocal_fast(x), reciprocal_fast(y));
+    sa = mul2(r, db);
+    sb = mul2(r, da);
+}
+// The activation.  (Each value's reciprocal its own: memory bounds the forward pass, and a value's bits do not depend on its neighbour.)
 template <int kAct>
 __device__ __forceinline__ uint64_t activate2(uint64_t z)
 {
     if constexpr (kAct == kNoAct) return z;
-    float a, b;
-    halves(z, a, b);
-    return pair_of(activate<kAct>(a), activate<kAct>(b));
+    if constexpr (kAct == kRelu) return at_least(z, 0.f);
+    float x, y;
+    halves(denominator(z), x, y);                             // (e^-z beyond 2^126: 0)
+    return mul2(z, pair_of(reciprocal_fast(x), reciprocal_fast(y)));
 }
-// The activation's derivative at z, times d.
+// Its derivatives at za and zb, times da and db.
 template <int kAct>
-__device__ __forceinline__ uint64_t slope2(uint64_t z, uint64_t d)
+__device__ __forceinline__ void slope2(uint64_t za, uint64_t zb, uint64_t &da, uint64_t &db)
 {
-    if constexpr (kAct == kNoAct) return d;
-    float a, b;
-    halves(z, a, b);
     if constexpr (kAct == kRelu) {
-        float x, y;
-        halves(d, x, y);
-        return pair_of(a > 0.f ? x : 0.f, b > 0.f ? y : 0.f);
-    } else {
-        const uint64_t s = pair_of(sigmoid(a), sigmoid(b));
-        // s + z s (1 - s)
-        const uint64_t t = fma2(mul2(z, s), add2(both(1.0f), s ^ 0x8000000080000000ull), s);
-        return mul2(t, d);
+        auto one = [](uint64_t z, uint64_t &d) {
+            float a, b, x, y;
+            halves(z, a, b);
+            halves(d, x, y);
+            d = pair_of(a > 0.f ? x : 0.f, b > 0.f ? y : 0.f);
+        };
+        one(za, da);
+        one(zb, db);
+    } else if constexpr (kAct == kSilu) {
+        uint64_t sa, sb;
+        sigmoids(za, zb, sa, sb);
+        // s (1 + z (1 - s))
+        const uint64_t one = both(1.0f);
+        da = mul2(da, mul2(sa, fma2(za, add2(one, sa ^ kMinus), one)));
+        db = mul2(db, mul2(sb, fma2(zb, add2(one, sb ^ kMinus), one)));
     }
 }
 
-// A block's threads over `columns` lanes of channels.
+// Moments or totals of group `g` that the blocks of a cluster left at `mine` in their shared memory, asked for all at once (one after the other they cost
+// a microsecond for each two blocks).
+constexpr int kMostShares = 16;
+__device__ __forceinline__ void of_cluster(const float2 *mine, int shares, float2 (&m)[kMostShares])
+{
+#pragma unroll
+    for (int i = 0; i < kMostShares; ++i)
+        if (i < shares)
+            asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(m[i].x), "=f"(m[i].y) : "r"(peer_address(mine, (uint32_t)i)));
+}
+
+// A block's first `threads` threads over `columns` lanes of channels.
 struct Lay {
-    int columns, lanes, rows, lane, row, blocks;
-    __device__ __forceinline__ explicit Lay(int columns_)
+    int threads, columns, lanes, rows, lane, row, blocks;
+    __device__ __forceinline__ explicit Lay(int columns_, int threads_)
     {
-        const int threads = blockDim.x;
+        threads = threads_;
         columns = columns_;
         blocks = (columns + threads - 1) / threads;
         lanes = (columns + blocks - 1) / blocks;
@@ -145,18 +256,68 @@ struct Lay {
         lane = threadIdx.x - row * lanes;
     }
     __device__ __forceinline__ bool at(int block) const { return row < rows && block * lanes + lane < columns; }
+    __device__ __forceinline__ void sync() const { sm100::named_bar_sync(1, threads); }
 };
+
+// A block's pixels come in pieces, so that the first can be worked on while the others are on their way: pieces of whole rounds of the block's rows.
+constexpr int kPieces = 4;
+struct Pieces {
+    int pixels, each;
+    unsigned long long *full;         // null: they are where they are (global memory)
+    unsigned int *status;
+    __device__ __forceinline__ Pieces(int pixels_, int rows, unsigned long long *full_, unsigned int *status_)
+    {
+        pixels = pixels_;
+        each = full_ ? ((pixels + kPieces - 1) / kPieces + rows - 1) / rows * rows : pixels;
+        full = full_;
+        status = status_;
+    }
+    __device__ __forceinline__ int first(int piece) const { return min(piece * each, pixels); }
+    __device__ __forceinline__ int end(int piece) const { return min((piece + 1) * each, pixels); }
+    __device__ __forceinline__ int count() const { return full ? kPieces : 1; }
+    // (a wait that runs out is reported; the values are wrong then, nothing else)
+    __device__ __forceinline__ void wait(int piece) const
+    {
+        if (!full || first(piece) == end(piece)) return;
+        const uint32_t bar = sm100::smem_u32(&full[piece]);
+        if (!sm100::mbar_try_wait(bar, 0, 1000u) && !sm100::mbar_wait_soon(bar, 0) && !sm100::mbar_wait_soon(bar, 0)) tc_dev_set_status(status, TC_ERR_TIMEOUT);
+    }
+};
+
+// The run of pixels that a block works on.
+struct Run {
+    unsigned int index;               // of all maps' runs
+    long long map;
+    int run, pixels;
+    long long first;                  // pixel of the tensor
+    __device__ __forceinline__ Run(const GroupArgs &a, unsigned int index_)
+    {
+        index = index_;
+        const unsigned int m = index / (unsigned int)a.shares;
+        run = (int)(index - m * (unsigned int)a.shares);
+        map = m;
+        pixels = min(a.share, a.hw - run * a.share);
+        first = map * a.hw + run * a.share;
+    }
+};
+
+// Room that channel_sums takes: of the lower half of the rows.
+__host__ __device__ inline int red_values(int columns, int threads, int v)
+{
+    const int blocks = (columns + threads - 1) / threads, lanes = (columns + blocks - 1) / blocks, rows = threads / lanes;
+    return ((rows + 1) / 2 * lanes * v + 1) / 2 * 2;
+}
 
 // Sums of runs of a group's entries, by as many neighbouring lanes as they are worth.
 struct Team {
     int size, rank, first, step;      // lanes of a group; this thread's; its first group, and how many groups the block works on at a time
-    __device__ __forceinline__ explicit Team(int entries)
+    __device__ __forceinline__ Team(int entries, int threads)
     {
         size = 1;
         while (size < 32 && size * 4 < entries) size *= 2;
         rank = threadIdx.x & (size - 1);
         first = threadIdx.x / size;
-        step = blockDim.x / size;
+        step = threads / size;
     }
     __device__ __forceinline__ float sum(float v) const
     {
@@ -165,48 +326,65 @@ struct Team {
     }
 };
 
-// Adds, for each group, what the threads hold for its channels in column block `block`: to(group, total), by one thread, blocks in their order.
-// `red`: blockDim x V floats of shared memory.
+// Sums over the block's rows of what its threads hold for V channels each (a[i], b[i]); each(channel, a, b) by one thread for each of column block `block`, by
+// neighbouring threads for neighbouring channels, whole warps together (channel -1: none).  red: red_values() float2.
 template <int V, typename F>
-__device__ __forceinline__ void add_groups(const Lay &lay, int block, int per_group, int group_count, const Pairs<V> &v, float *red, F to)
+__device__ __forceinline__ void channel_sums(const Lay &lay, int block, const float (&a)[2 * kPairs<V>], const float (&b)[2 * kPairs<V>], float2 *red, F each)
 {
-    const bool whole = V > 1 && per_group % V == 0;           // a thread's channels are of one group
-    const int per_lane = whole ? 1 : V, pitch = lay.lanes * per_lane;
-    __syncthreads();                                          // the readers of the last sums
-    if (lay.at(block)) {
-        float f[2 * kPairs<V>];
+    // the upper half of the rows leaves its values, the lower half adds its own
+    constexpr int kPer = V > 1 ? V / 2 : 1;
+    const int half = (lay.rows + 1) / 2, lanes = lay.lanes;
+    const bool here = lay.at(block);
+    lay.sync();                                               // the last sums' readers
+    float4 *const at = reinterpret_cast<float4 *>(red) + (lay.row >= half ? lay.row - half : lay.row) * kPer * lanes + lay.lane;
+    float2 *const at1 = red + (lay.row >= half ? lay.row - half : lay.row) * lanes + lay.lane;
+    if (here && lay.row >= half) {
+        if constexpr (V > 1)
 #pragma unroll
-        for (int i = 0; i < kPairs<V>; ++i) halves(v[i], f[2 * i], f[2 * i + 1]);
-        float *const at = red + lay.row * pitch + lay.lane * per_lane;
-        if (whole) {
-            float s = f[0];
-#pragma unroll
-            for (int i = 1; i < V; ++i) s += f[i];
-            at[0] = s;
-        } else
-#pragma unroll
-            for (int i = 0; i < V; ++i) at[i] = f[i];
+            for (int i = 0; i < kPer; ++i) at[i * lanes] = make_float4(a[2 * i], b[2 * i], a[2 * i + 1], b[2 * i + 1]);
+        else *at1 = make_float2(a[0], b[0]);
     }
-    __syncthreads();
-    const int per = whole ? per_group / V : per_group;        // entries of a group in a row
-    const int c0 = block * pitch, c1 = min(c0 + pitch, whole ? lay.columns : lay.columns * V);
-    const int g0 = c0 / per, g1 = min(group_count, (c1 + per - 1) / per);
-    const Team team(lay.rows * per);
-    for (int base = g0; base < g1; base += team.step) {       // (all threads go round together: the sums are taken by whole warps)
-        const int g = base + team.first;
-        float s = 0.f;
-        if (g < g1) {
-            const int from = max(g * per, c0) - c0, count = min((g + 1) * per, c1) - c0 - from;
-            if (count == 1) for (int r = team.rank; r < lay.rows; r += team.size) s += red[r * pitch + from];
-            else
-                for (int i = team.rank; i < lay.rows * count; i += team.size) {
-                    const int r = i / count;
-                    s += red[r * pitch + from + i - r * count];
-                }
+    lay.sync();
+    if (here && lay.row < half) {
+        const bool two = lay.row + half < lay.rows;
+        if constexpr (V > 1) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const float4 t = two ? at[i * lanes] : make_float4(0.f, 0.f, 0.f, 0.f);
+                at[i * lanes] = make_float4(a[2 * i] + t.x, b[2 * i] + t.y, a[2 * i + 1] + t.z, b[2 * i + 1] + t.w);
+            }
+        } else {
+            const float2 t = two ? *at1 : make_float2(0.f, 0.f);
+            *at1 = make_float2(a[0] + t.x, b[0] + t.y);
         }
-        s = team.sum(s);
-        if (g < g1 && team.rank == 0) to(g, s);
     }
+    lay.sync();
+    const int first = block * lanes, channels = min(lanes, lay.columns - first) * V;
+    for (int base = 0; base < channels; base += lay.threads) {
+        const int j = base + threadIdx.x;
+        float2 s = make_float2(0.f, 0.f);
+        if (j < channels) {
+            const float2 *from = red + (V > 1 ? 2 * (((j % V) / 2) * lanes + j / V) + (j & 1) : j);
+            const int pitch = V * lanes;
+#pragma unroll 4
+            for (int r = 0; r < half; ++r) {
+                const float2 t = from[r * pitch];
+                s.x += t.x;
+                s.y += t.y;
+            }
+        }
+        each(j < channels ? first * V + j : -1, s.x, s.y);
+    }
+}
+// Where a block's channels have a thread each and a group's are a power of two that a warp holds, sums over groups need no shared memory.
+__device__ __forceinline__ bool groups_in_warps(const Lay &lay, int per_group) { return lay.blocks == 1 && per_group <= 32 && (per_group & (per_group - 1)) == 0; }
+__device__ __forceinline__ float sum_over(float v, int lanes)
+{
+    for (int d = lanes / 2; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
 }
 
 }  // namespace groups
+
+int shares_on_chip(long long n, int hw, long long most, int sm_count, const std::function<size_t(int)> &bytes);
+void cut_runs(GroupPlan &p, long long n, int hw, long long row, int tensors, int sm_count);

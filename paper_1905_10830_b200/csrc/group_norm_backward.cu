@@ -7,135 +7,157 @@
 // blocks they are read once, else by two kernels; dz is computed for the sums and again for dx (it does not fit beside them).  Each block leaves its
 // A and B, which the last kernel adds over maps in a fixed order.
 #include "group_norm.cuh"
-#include "sm100_ptx.cuh"
 
 namespace {
 
 using namespace groups;
 
-// What a thread needs of its channels.
+// Blocks an SM, and vectors in flight: registers enough for both pixels' values (three blocks with two vectors: 156 us where this takes 140, with four 142).
+constexpr int kGradientBlocks = 2, kBatch = 4;
+
+// What a thread needs of its channels: z = (x + minus) slope + b, slope = rstd w.
 template <int V> struct Channel {
-    Pairs<V> minus, rstd, w, b;
-    __device__ __forceinline__ void load(const GroupArgs &a, const float2 *stats, int c)
+    Pairs<V> minus, slope, b, rstd;
+    template <typename S>
+    __device__ __forceinline__ Channel(const GroupArgs &a, S stats, int c)
     {
-        stats_pairs<V>(stats, c, a.c / a.groups, minus, rstd);
-        vector_pairs<V>(a.weight, c, 1.f, w);
+        stats_pairs<V>(c, a.c / a.groups, minus, rstd, stats);
+        vector_pairs<V>(a.weight, c, 1.f, slope);
         vector_pairs<V>(a.bias, c, 0.f, b);
+#pragma unroll
+        for (int k = 0; k < kPairs<V>; ++k) slope[k] = mul2(slope[k], rstd[k]);
     }
 };
 
-// sums[c] = (A, B) over `pixels` pixels; x and dy at `src` and `grad`.  red: blockDim x V float2.
-template <typename T, int V, int kAct>
-__device__ __forceinline__ void block_sums(const T *src, const T *grad, int pixels, const GroupArgs &a, const Lay &lay, const float2 *stats, float2 *red, float2 *sums)
-{
-    for (int b = 0; b < lay.blocks; ++b) {
-        __syncthreads();                                      // the readers of the last block's sums
-        if (lay.at(b)) {
-            const int c = (b * lay.lanes + lay.lane) * V;
-            Channel<V> ch;
-            ch.load(a, stats, c);
-            Pairs<V> sum_a = {}, sum_b = {};
-            const long long at = (long long)lay.row * a.c + c, step = (long long)lay.rows * a.c;
-            const T *p = src + at, *q = grad + at;
-#pragma unroll 2
-            for (int i = lay.row; i < pixels; i += lay.rows, p += step, q += step) {
-                Pairs<V> v, d;
-                load_pairs<V>(p, v);
-                load_pairs<V>(q, d);
-#pragma unroll
-                for (int k = 0; k < kPairs<V>; ++k) {
-                    const uint64_t n = mul2(add2(v[k], ch.minus[k]), ch.rstd[k]);
-                    const uint64_t dz = slope2<kAct>(fma2(n, ch.w[k], ch.b[k]), d[k]);
-                    sum_a[k] = add2(sum_a[k], dz);
-                    sum_b[k] = fma2(dz, n, sum_b[k]);
-                }
-            }
-            float fa[2 * kPairs<V>], fb[2 * kPairs<V>];
-#pragma unroll
-            for (int k = 0; k < kPairs<V>; ++k) {
-                halves(sum_a[k], fa[2 * k], fa[2 * k + 1]);
-                halves(sum_b[k], fb[2 * k], fb[2 * k + 1]);
-            }
-#pragma unroll
-            for (int i = 0; i < V; ++i) red[(lay.row * V + i) * lay.lanes + lay.lane] = make_float2(fa[i], fb[i]);
-        }
-        __syncthreads();
-        const int first = b * lay.lanes, lanes = min(lay.lanes, lay.columns - first);
-        for (int j = threadIdx.x; j < lanes * V; j += blockDim.x) {
-            const int i = j / lanes, lane = j - i * lanes;
-            float2 s = red[i * lay.lanes + lane];
-            for (int r = 1; r < lay.rows; ++r) {
-                const float2 t = red[(r * V + i) * lay.lanes + lane];
-                s.x += t.x;
-                s.y += t.y;
-            }
-            sums[(first + lane) * V + i] = s;
-        }
-    }
-    __syncthreads();
-}
-
-// totals[g] = (s1, s2) from sums of channels: of(c).
-template <typename F>
-__device__ __forceinline__ void group_totals(const GroupArgs &a, F of, float2 *totals)
+// A and B of the channels over the pixels at `src` and `grad`, to part[c] (or null), and to(group, (s1, s2)) by one thread each.  stats(group): the map's.
+// red: red_values() float2; sums: c float2.
+template <typename T, int V, int kAct, typename S, typename F>
+__device__ __forceinline__ void block_sums(const T *src, const T *grad, const Pieces &pieces, const GroupArgs &a, const Lay &lay, S stats, float2 *red, float2 *sums, float2 *part, F to)
 {
     const int per_group = a.c / a.groups;
-    const Team team(per_group);
+    const bool in_warps = groups_in_warps(lay, per_group);
+    for (int b = 0; b < lay.blocks; ++b) {
+        Pairs<V> sum_a = {}, sum_b = {};
+        const int c = (b * lay.lanes + lay.lane) * V;
+        if (lay.at(b)) {
+            const Channel<V> ch(a, stats, c);
+            const T *const p = src + c, *const q = grad + c;
+            for (int piece = 0; piece < pieces.count(); ++piece) {
+                pieces.wait(piece);
+                Raw<T, V> x[kBatch], dy[kBatch];
+                in_batches<kBatch>(
+                    pieces.first(piece) + lay.row, pieces.end(piece), lay.rows,
+                    [&](int k, int i) {
+                        load_raw<V>(x[k], p + i * a.c);
+                        load_raw<V>(dy[k], q + i * a.c);
+                    },
+                    [&](int k, int, int second) {
+                        Pairs<V> v, w, d, e;
+                        pairs_of<V>(x[k], v);
+                        pairs_of<V>(x[k + 1], w);
+                        pairs_of<V>(dy[k], d);
+                        pairs_of<V>(dy[k + 1], e);
+#pragma unroll
+                        for (int j = 0; j < kPairs<V>; ++j) {
+                            if (second < 0) e[j] = 0;         // (adds nothing, and with the first one's x nothing that is not there already)
+                            v[j] = add2(v[j], ch.minus[j]);
+                            w[j] = add2(w[j], ch.minus[j]);
+                            slope2<kAct>(fma2(v[j], ch.slope[j], ch.b[j]), fma2(w[j], ch.slope[j], ch.b[j]), d[j], e[j]);
+                            sum_a[j] = add2(sum_a[j], add2(d[j], e[j]));
+                            sum_b[j] = fma2(d[j], v[j], fma2(e[j], w[j], sum_b[j]));
+                        }
+                    });
+            }
+            // the distances from the mean in units of the deviation
+#pragma unroll
+            for (int j = 0; j < kPairs<V>; ++j) sum_b[j] = mul2(sum_b[j], ch.rstd[j]);
+        }
+        float fa[2 * kPairs<V>], fb[2 * kPairs<V>];
+#pragma unroll
+        for (int k = 0; k < kPairs<V>; ++k) {
+            halves(sum_a[k], fa[2 * k], fa[2 * k + 1]);
+            halves(sum_b[k], fb[2 * k], fb[2 * k + 1]);
+        }
+        channel_sums<V>(lay, b, fa, fb, red, [&](int ch, float sa, float sb) {
+            if (ch >= 0 && part) part[ch] = make_float2(sa, sb);
+            const float w = ch >= 0 && a.weight ? a.weight[ch] : 1.f;
+            sa *= w;
+            sb *= w;
+            if (in_warps) {
+                sa = sum_over(sa, per_group);
+                sb = sum_over(sb, per_group);
+                if (ch >= 0 && (ch & (per_group - 1)) == 0) to(ch / per_group, make_float2(sa, sb));
+            } else if (ch >= 0)
+                sums[ch] = make_float2(sa, sb);
+        });
+    }
+    if (in_warps) return;
+    lay.sync();
+    const Team team(per_group, lay.threads);
     for (int base = 0; base < a.groups; base += team.step) {
         const int g = base + team.first;
         float s1 = 0.f, s2 = 0.f;
         if (g < a.groups)
             for (int i = team.rank; i < per_group; i += team.size) {
-                const int c = g * per_group + i;
-                const float w = a.weight ? a.weight[c] : 1.f;
-                const float2 s = of(c);
-                s1 += w * s.x;
-                s2 += w * s.y;
+                s1 += sums[g * per_group + i].x;
+                s2 += sums[g * per_group + i].y;
             }
         s1 = team.sum(s1);
         s2 = team.sum(s2);
-        if (g < a.groups && team.rank == 0) totals[g] = make_float2(s1, s2);
+        if (g < a.groups && team.rank == 0) to(g, make_float2(s1, s2));
     }
-    __syncthreads();
 }
 
-// dx of `pixels` pixels; totals[g] = (s1, s2) / m.
-template <typename T, int V, int kAct>
-__device__ __forceinline__ void write_gradients(const T *src, const T *grad, int pixels, long long first, const GroupArgs &a, const Lay &lay, const float2 *stats, const float2 *totals)
+// dx of `pixels` pixels; totals(group) = (s1, s2) / m.
+template <typename T, int V, int kAct, typename S, typename F>
+__device__ __forceinline__ void write_gradients(const T *src, const T *grad, int pixels, long long first, const GroupArgs &a, const Lay &lay, S stats, F totals)
 {
     for (int b = 0; b < lay.blocks; ++b) {
         if (!lay.at(b)) continue;
         const int c = (b * lay.lanes + lay.lane) * V;
-        Channel<V> ch;
-        ch.load(a, stats, c);
-        Pairs<V> minus_s1, s2;
-        stats_pairs<V>(totals, c, a.c / a.groups, minus_s1, s2);
-        const long long at = (long long)lay.row * a.c + c, step = (long long)lay.rows * a.c;
-        const T *p = src + at, *q = grad + at;
-        T *to = (T *)a.out + first * a.c + at;
-#pragma unroll 2
-        for (int i = lay.row; i < pixels; i += lay.rows, p += step, q += step, to += step) {
-            Pairs<V> v, d;
-            load_pairs<V>(p, v);
-            load_pairs<V>(q, d);
+        const Channel<V> ch(a, stats, c);
+        // dx = w rstd dz - rstd s1 - (x - mean) rstd (rstd s2)
+        Pairs<V> by_one, by_x;
+        stats_pairs<V>(c, a.c / a.groups, by_one, by_x, totals);
 #pragma unroll
-            for (int k = 0; k < kPairs<V>; ++k) {
-                const uint64_t n = mul2(add2(v[k], ch.minus[k]), ch.rstd[k]);
-                const uint64_t dz = slope2<kAct>(fma2(n, ch.w[k], ch.b[k]), d[k]);
-                // w dz - s1 - n s2
-                const uint64_t rest = fma2(n, s2[k] ^ 0x8000000080000000ull, fma2(dz, ch.w[k], minus_s1[k]));
-                v[k] = mul2(rest, ch.rstd[k]);
-            }
-            store_pairs<V>(to, v);
+        for (int j = 0; j < kPairs<V>; ++j) {
+            by_one[j] = mul2(by_one[j], ch.rstd[j]);
+            by_x[j] = mul2(mul2(by_x[j], ch.rstd[j]), ch.rstd[j]) ^ kMinus;
         }
+        const T *const p = src + c, *const q = grad + c;
+        T *const to = (T *)a.out + first * a.c + c;
+        Raw<T, V> x[kBatch], dy[kBatch];
+        in_batches<kBatch>(
+            lay.row, pixels, lay.rows,
+            [&](int k, int i) {
+                load_raw<V>(x[k], p + i * a.c);
+                load_raw<V>(dy[k], q + i * a.c);
+            },
+            [&](int k, int i, int second) {
+                Pairs<V> v, w, d, e;
+                pairs_of<V>(x[k], v);
+                pairs_of<V>(x[k + 1], w);
+                pairs_of<V>(dy[k], d);
+                pairs_of<V>(dy[k + 1], e);
+#pragma unroll
+                for (int j = 0; j < kPairs<V>; ++j) {
+                    v[j] = add2(v[j], ch.minus[j]);
+                    w[j] = add2(w[j], ch.minus[j]);
+                    slope2<kAct>(fma2(v[j], ch.slope[j], ch.b[j]), fma2(w[j], ch.slope[j], ch.b[j]), d[j], e[j]);
+                    v[j] = fma2(d[j], ch.slope[j], fma2(v[j], by_x[j], by_one[j]));
+                    w[j] = fma2(e[j], ch.slope[j], fma2(w[j], by_x[j], by_one[j]));
+                }
+                store_pairs<V>(to + i * a.c, v);
+                if (second >= 0) store_pairs<V>(to + second * a.c, w);
+            });
     }
 }
 
 // ---- maps in a cluster's shared memory --------------------------------------------------------
-// [x][dy][red: threads x V float2][sums: c float2][stats: groups float2][own: groups float2][totals: groups float2]
+// [x][dy][red: red_values() float2][sums: c float2][own: groups float2][totals: groups float2]
 size_t shared_bytes(const GroupArgs &a, int pixels, int element, int v, int threads)
 {
-    return 2 * (((size_t)pixels * a.c * element + 15) / 16 * 16) + (size_t)threads * v * 8 + 8 * (size_t)a.c + 24 * (size_t)a.groups;
+    return 2 * (((size_t)pixels * a.c * element + 15) / 16 * 16) + 8 * (size_t)red_values(a.c / v, threads, v) + 8 * (size_t)a.c + 16 * (size_t)a.groups;
 }
 
 template <typename T, int V, int kAct>
@@ -143,12 +165,15 @@ __global__ void __launch_bounds__(512) group_gradient_map_kernel(const __grid_co
 {
     using namespace sm100;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ __align__(8) unsigned long long s_full;
+    __shared__ __align__(8) unsigned long long s_full[kPieces];
     const size_t room = ((size_t)a.share * a.c * sizeof(T) + 15) / 16 * 16;
     const T *const data = reinterpret_cast<const T *>(smem), *const grad = reinterpret_cast<const T *>(smem + room);
-    float2 *const red = reinterpret_cast<float2 *>(smem + 2 * room), *const sums = red + blockDim.x * V;
-    float2 *const stats = sums + a.c, *const own = stats + a.groups, *const totals = own + a.groups;
-    if (threadIdx.x == 0) { mbar_init(smem_u32(&s_full), 1); mbar_fence_init(); }
+    float2 *const red = reinterpret_cast<float2 *>(smem + 2 * room), *const sums = red + red_values(a.c / V, blockDim.x, V);
+    float2 *const own = sums + a.c, *const totals = own + a.groups;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kPieces; ++i) mbar_init(smem_u32(&s_full[i]), 1);
+        mbar_fence_init();
+    }
     __syncthreads();
     chain_next();
     chain_wait();
@@ -156,110 +181,117 @@ __global__ void __launch_bounds__(512) group_gradient_map_kernel(const __grid_co
     const long long map = blockIdx.x / a.shares;
     const int p0 = rank * a.share, pixels = max(0, min(a.share, a.hw - p0)), per_group = a.c / a.groups;
     const long long first = map * a.hw + p0;
-    if (pixels && threadIdx.x == 0) {
-        const uint32_t bytes = (uint32_t)pixels * a.c * sizeof(T);
-        mbar_arrive_expect_tx(smem_u32(&s_full), 2 * bytes);
+    const Lay lay(a.c / V, blockDim.x);
+    const Pieces pieces(pixels, lay.rows, s_full, a.status);
+    if (threadIdx.x == 0) {
         const char *const src = (const char *)((const T *)a.x + first * a.c), *const dy = (const char *)((const T *)a.dy + first * a.c);
-        for (uint32_t at = 0; at < bytes; at += 16384) {
-            bulk_load(smem_u32(smem) + at, src + at, min(16384u, bytes - at), smem_u32(&s_full));
-            bulk_load(smem_u32(smem) + (uint32_t)room + at, dy + at, min(16384u, bytes - at), smem_u32(&s_full));
+        const uint32_t row = (uint32_t)a.c * sizeof(T);
+        for (int i = 0; i < kPieces; ++i) {
+            const uint32_t from = pieces.first(i) * row, to = pieces.end(i) * row;
+            if (from == to) break;
+            mbar_arrive_expect_tx(smem_u32(&s_full[i]), 2 * (to - from));
+            for (uint32_t at = from; at < to; at += 16384) {
+                bulk_load(smem_u32(smem) + at, src + at, min(16384u, to - at), smem_u32(&s_full[i]));
+                bulk_load(smem_u32(smem) + (uint32_t)room + at, dy + at, min(16384u, to - at), smem_u32(&s_full[i]));
+            }
         }
     }
-    for (int g = threadIdx.x; g < a.groups; g += blockDim.x) stats[g] = a.stats[map * a.groups + g];
-    // (a wait that runs out is reported; the values are wrong then, nothing else)
-    if (pixels && !mbar_wait_soon(smem_u32(&s_full), 0) && !mbar_wait_soon(smem_u32(&s_full), 0)) tc_dev_set_status(a.status, TC_ERR_TIMEOUT);
-    const Lay lay(a.c / V);
-    block_sums<T, V, kAct>(data, grad, pixels, a, lay, stats, red, sums);
-    if (a.part)
-        for (int c = threadIdx.x; c < a.c; c += blockDim.x) a.part[(long long)blockIdx.x * a.c + c] = sums[c];
-    group_totals(a, [&](int c) { return sums[c]; }, own);
+    auto stats = [&](int g) { return a.stats[map * a.groups + g]; };
+    block_sums<T, V, kAct>(data, grad, pieces, a, lay, stats, red, sums, a.part ? a.part + (long long)blockIdx.x * a.c : nullptr, [&](int g, float2 t) { own[g] = t; });
     if (a.shares > 1) cluster_sync();
+    else __syncthreads();
     const float per_value = 1.0f / ((float)a.hw * (float)per_group);
     for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
-        float2 t = make_float2(0.f, 0.f);
-        for (int i = 0; i < a.shares; ++i) {
-            float2 m;
-            asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(m.x), "=f"(m.y) : "r"(peer_address(&own[g], (uint32_t)i)));
-            t.x += m.x;
-            t.y += m.y;
-        }
+        float2 m[kMostShares], t = make_float2(0.f, 0.f);
+        if (a.shares > 1) of_cluster(&own[g], a.shares, m);
+        else m[0] = own[g];
+#pragma unroll
+        for (int i = 0; i < kMostShares; ++i)
+            if (i < a.shares) {
+                t.x += m[i].x;
+                t.y += m[i].y;
+            }
         totals[g] = make_float2(t.x * per_value, t.y * per_value);
     }
     __syncthreads();
     if (a.shares > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    write_gradients<T, V, kAct>(data, grad, pixels, first, a, lay, stats, totals);
+    write_gradients<T, V, kAct>(data, grad, pixels, first, a, lay, stats, [&](int g) { return totals[g]; });
     if (a.shares > 1) {
         __syncwarp();
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");       // the others have read this block's totals
     }
 }
 
-// ---- any maps ----------------------------------------------------------------------------------
-// part[map][share][channel]: A and B of a run of pixels; runs[map][share][group]: its s1 and s2.
-template <typename T, int V, int kAct>
-__global__ void __launch_bounds__(512) group_sums_kernel(const __grid_constant__ GroupArgs a)
+// ---- maps in runs of pixels ----------------------------------------------------------------------
+// A group's (s1, s2) / m from its runs', by a team of `size` lanes.
+__device__ __forceinline__ float2 join_runs(const GroupArgs &a, long long map, int g, int rank, int size)
 {
-    extern __shared__ __align__(128) unsigned char smem[];
-    float2 *const red = reinterpret_cast<float2 *>(smem), *const sums = red + blockDim.x * V, *const stats = sums + a.c;
-    chain_next();
-    chain_wait();
-    const long long map = blockIdx.x / a.shares;
-    const int p0 = (int)(blockIdx.x % a.shares) * a.share, pixels = max(0, min(a.share, a.hw - p0));
-    for (int g = threadIdx.x; g < a.groups; g += blockDim.x) stats[g] = a.stats[map * a.groups + g];
-    __syncthreads();
-    const Lay lay(a.c / V);
-    const long long at = (map * a.hw + p0) * a.c;
-    block_sums<T, V, kAct>((const T *)a.x + at, (const T *)a.dy + at, pixels, a, lay, stats, red, sums);
-    if (a.part)
-        for (int c = threadIdx.x; c < a.c; c += blockDim.x) a.part[(long long)blockIdx.x * a.c + c] = sums[c];
-    group_totals(a, [&](int c) { return sums[c]; }, a.runs + (long long)blockIdx.x * a.groups);
+    const float2 *const at = a.runs + map * a.shares * a.groups + g;
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll 4
+    for (int r = rank; r < a.shares; r += size) {
+        const float2 t = at[(long long)r * a.groups];
+        s1 += t.x;
+        s2 += t.y;
+    }
+    const float per_value = 1.0f / ((float)a.hw * (float)(a.c / a.groups));
+    return make_float2(sum_over(s1, size) * per_value, sum_over(s2, size) * per_value);
 }
 
-// sums[map][group] = (s1, s2) / m: a warp a group.
+// Maps of many runs: sums[map][group], a warp each.
 __global__ void __launch_bounds__(256) group_totals_kernel(const __grid_constant__ GroupArgs a)
 {
     chain_next();
     chain_wait();
     const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) / 32;
-    const int lane = threadIdx.x & 31, per_group = a.c / a.groups;
     if (i >= a.n * a.groups) return;
-    const long long map = i / a.groups;
-    const int g = (int)(i - map * a.groups);
-    float s1 = 0.f, s2 = 0.f;
-    for (int k = lane; k < a.shares; k += 32) {
-        const float2 s = a.runs[(map * a.shares + k) * a.groups + g];
-        s1 += s.x;
-        s2 += s.y;
-    }
-    for (int d = 16; d; d >>= 1) {
-        s1 += __shfl_xor_sync(0xffffffffu, s1, d);
-        s2 += __shfl_xor_sync(0xffffffffu, s2, d);
-    }
-    const float per_value = 1.0f / ((float)a.hw * (float)per_group);
-    if (lane == 0) a.sums[i] = make_float2(s1 * per_value, s2 * per_value);
+    const float2 v = join_runs(a, i / a.groups, (int)(i % a.groups), threadIdx.x & 31, 32);
+    if ((threadIdx.x & 31) == 0) a.sums[i] = v;
 }
 
+// part[map][run][channel]: A and B of a run of pixels; runs[map][run][group]: its s1 and s2.  [red: red_values() float2][sums: c float2]
 template <typename T, int V, int kAct>
-__global__ void __launch_bounds__(512) group_gradients_kernel(const __grid_constant__ GroupArgs a)
+__global__ void __launch_bounds__(kRunThreads, kGradientBlocks) group_sums_kernel(const __grid_constant__ GroupArgs a)
 {
     extern __shared__ __align__(128) unsigned char smem[];
-    float2 *const stats = reinterpret_cast<float2 *>(smem), *const totals = stats + a.groups;
+    float2 *const red = reinterpret_cast<float2 *>(smem), *const sums = red + red_values(a.c / V, kRunThreads, V);
     chain_next();
     chain_wait();
-    const long long block = (long long)gridDim.x - 1 - blockIdx.x, map = block / a.shares;
-    const int p0 = (int)(block % a.shares) * a.share, pixels = max(0, min(a.share, a.hw - p0));
-    for (int g = threadIdx.x; g < a.groups; g += blockDim.x) {
-        stats[g] = a.stats[map * a.groups + g];
-        totals[g] = a.sums[map * a.groups + g];
+    const Lay lay(a.c / V, kRunThreads);
+    const Run run(a, blockIdx.x);
+    auto stats = [&](int g) { return a.stats[run.map * a.groups + g]; };
+    float2 *const to = a.runs + (long long)run.index * a.groups;
+    block_sums<T, V, kAct>((const T *)a.x + run.first * a.c, (const T *)a.dy + run.first * a.c, Pieces(run.pixels, lay.rows, nullptr, a.status), a, lay, stats, red, sums,
+                           a.part ? a.part + (long long)run.index * a.c : nullptr, [&](int g, float2 t) { to[g] = t; });
+}
+
+// dx, the last runs first: they are the likeliest to be in L2 still.  [totals: groups float2]
+template <typename T, int V, int kAct>
+__global__ void __launch_bounds__(kRunThreads, kGradientBlocks) group_gradients_kernel(const __grid_constant__ GroupArgs a)
+{
+    extern __shared__ __align__(128) unsigned char smem[];
+    float2 *const own = reinterpret_cast<float2 *>(smem);
+    chain_next();
+    chain_wait();
+    const Lay lay(a.c / V, kRunThreads);
+    const Run run(a, gridDim.x - 1 - blockIdx.x);
+    if (a.sums)
+        for (int g = threadIdx.x; g < a.groups; g += kRunThreads) own[g] = a.sums[run.map * a.groups + g];
+    else {
+        const Team team(a.shares, kRunThreads);
+        for (int base = 0; base < a.groups; base += team.step) {
+            const int g = base + team.first;
+            const float2 v = join_runs(a, run.map, min(g, a.groups - 1), team.rank, team.size);
+            if (g < a.groups && team.rank == 0) own[g] = v;
+        }
     }
     __syncthreads();
-    const Lay lay(a.c / V);
-    const long long first = map * a.hw + p0, at = first * a.c;
-    write_gradients<T, V, kAct>((const T *)a.x + at, (const T *)a.dy + at, pixels, first, a, lay, stats, totals);
+    auto stats = [&](int g) { return a.stats[run.map * a.groups + g]; };
+    write_gradients<T, V, kAct>((const T *)a.x + run.first * a.c, (const T *)a.dy + run.first * a.c, run.pixels, run.first, a, lay, stats, [&](int g) { return own[g]; });
 }
 
 // db and dw: sums over the blocks' A and B, 8 channels a block, in 64 bits (there may be many).
-constexpr int kVectorThreads = 512, kVectorChannels = 8;
+constexpr int kVectorThreads = 1024, kVectorChannels = 8;
 __global__ void __launch_bounds__(kVectorThreads) group_vectors_kernel(const __grid_constant__ GroupArgs a, long long rows)
 {
     chain_next();
@@ -268,7 +300,7 @@ __global__ void __launch_bounds__(kVectorThreads) group_vectors_kernel(const __g
     const int c = blockIdx.x * kVectorChannels + (threadIdx.x & (kVectorChannels - 1));
     double2 s = make_double2(0.0, 0.0);
     if (c < a.c)
-#pragma unroll 4
+#pragma unroll 8
         for (long long r = threadIdx.x / kVectorChannels; r < rows; r += kVectorThreads / kVectorChannels) {
             const float2 t = a.part[r * a.c + c];
             s.x += t.x;
@@ -292,25 +324,33 @@ template <typename T, int V, int kAct>
 tc_status launch_map(int device, const GroupArgs &a, int threads, size_t smem, cudaStream_t s)
 {
     constexpr auto kernel = group_gradient_map_kernel<T, V, kAct>;
-    if (!allow_shared<kernel>(device, 225 * 1024)) return TC_ERR_CUDA;
+    if (!allow_shared<kernel>(device, kMostShared) || !allow_large_clusters<kernel>(device)) return TC_ERR_CUDA;
     return launch_first_cluster(a.shares, kernel, dim3((unsigned int)(a.n * a.shares)), dim3(threads), smem, s, a) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
 template <typename T, int V, int kAct>
-tc_status launch_any(int device, const GroupArgs &a, int threads, cudaStream_t s)
+tc_status launch_runs(int device, const GroupArgs &a, cudaStream_t s)
 {
-    const size_t first = (size_t)threads * V * 8 + 8 * (size_t)a.c + 8 * (size_t)a.groups, last = 16 * (size_t)a.groups;
-    if (!allow_shared<group_sums_kernel<T, V, kAct>>(device, 225 * 1024) || !allow_shared<group_gradients_kernel<T, V, kAct>>(device, 225 * 1024)) return TC_ERR_CUDA;
-    const dim3 grid((unsigned int)(a.n * a.shares)), block(threads);
+    const size_t first = 8 * (size_t)red_values(a.c / V, kRunThreads, V) + 8 * (size_t)a.c, last = 8 * (size_t)a.groups;
+    if (!allow_shared<group_sums_kernel<T, V, kAct>>(device, kMostShared) || !allow_shared<group_gradients_kernel<T, V, kAct>>(device, kMostShared)) return TC_ERR_CUDA;
+    const dim3 grid((unsigned int)(a.n * a.shares)), block(kRunThreads);
     if (launch_first(true, group_sums_kernel<T, V, kAct>, grid, block, first, s, a) != cudaSuccess) return TC_ERR_CUDA;
-    if (launch_chained(true, group_totals_kernel, dim3((unsigned int)((a.n * a.groups + 7) / 8)), dim3(256), 0, s, a) != cudaSuccess) return TC_ERR_CUDA;
+    if (a.sums && launch_chained(true, group_totals_kernel, dim3((unsigned int)((a.n * a.groups + 7) / 8)), dim3(256), 0, s, a) != cudaSuccess) return TC_ERR_CUDA;
     return launch_chained(true, group_gradients_kernel<T, V, kAct>, grid, block, last, s, a) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
 
 template <typename T, int V>
-tc_status launch(int device, const GroupArgs &a, int act, int threads, size_t smem, cudaStream_t s)
+tc_status launch(int device, const GroupArgs &a, const GroupPlan &p, int act, cudaStream_t s)
 {
-#define TC_GRADIENT(kAct) (smem ? launch_map<T, V, kAct>(device, a, threads, smem, s) : launch_any<T, V, kAct>(device, a, threads, s))
-    return act == kRelu ? TC_GRADIENT(kRelu) : act == kSilu ? TC_GRADIENT(kSilu) : TC_GRADIENT(kNoAct);
+    // (maps of single values never lie in shared memory: bulk copies begin at 16 bytes)
+#define TC_GRADIENT(kAct) \
+    do { \
+        if constexpr (V > 1) \
+            if (p.shared) return launch_map<T, V, kAct>(device, a, p.threads, p.shared, s); \
+        return launch_runs<T, V, kAct>(device, a, s); \
+    } while (0)
+    if (act == kRelu) TC_GRADIENT(kRelu);
+    if (act == kSilu) TC_GRADIENT(kSilu);
+    TC_GRADIENT(kNoAct);
 #undef TC_GRADIENT
 }
 
@@ -328,10 +368,8 @@ GroupPlan tc_plan_group_norm_backward(const GroupGradArgs &m, int sm_count)
     a.groups = m.groups;
     auto bytes = [&](int shares) { return shared_bytes(a, (m.hw + shares - 1) / shares, element, p.vector, p.threads); };
     if (p.vector > 1) {
-        int shares = 1;
-        while (shares < 8 && bytes(shares) > 110 * 1024) shares *= 2;
-        while (shares < 8 && (long long)m.n * shares * 2 <= sm_count && m.hw / shares >= 16) shares *= 2;
-        if (bytes(shares) <= 225 * 1024 && (long long)m.n * shares < 1ll << 31) {
+        const int shares = shares_on_chip(m.n, m.hw, sm_count, sm_count, bytes);
+        if (shares) {
             p.shares = shares;
             p.share = (m.hw + shares - 1) / shares;
             p.shared = bytes(shares);
@@ -339,13 +377,8 @@ GroupPlan tc_plan_group_norm_backward(const GroupGradArgs &m, int sm_count)
             return p;
         }
     }
-    const long long row = (long long)m.c * element;
-    long long share = std::max(1ll, 65536 / row);
-    while (share > 1 && (long long)m.n * ((m.hw + share - 1) / share) < 4ll * sm_count) share = (share + 1) / 2;
-    share = std::max(share, ((long long)m.hw * m.n + (1ll << 30) - 1) >> 30);
-    p.share = (int)std::min<long long>(share, m.hw);
-    p.shares = (m.hw + p.share - 1) / p.share;
-    p.workspace = ((vectors ? (size_t)m.n * p.shares * m.c : 0) + (size_t)m.n * m.groups * (p.shares + 1)) * sizeof(float2);
+    cut_runs(p, m.n, m.hw, (long long)m.c * element, 2, sm_count);
+    p.workspace = ((vectors ? (size_t)m.n * p.shares * m.c : 0) + (size_t)m.n * m.groups * (p.shares + (p.join ? 1 : 0))) * sizeof(float2);
     return p;
 }
 
@@ -370,13 +403,14 @@ tc_status tc_launch_group_norm_backward(int device, const GroupGradArgs &m, cons
     tc_status st = TC_OK;
     if (m.n) {
         if (!p.shared) {
-            a.sums = (float2 *)workspace;
-            a.runs = a.sums + (long long)a.n * a.groups;
-            if (a.dweight || a.dbias) a.part = a.runs + (long long)a.n * a.shares * a.groups;
+            a.runs = (float2 *)workspace;
+            float2 *const rest = a.runs + (long long)a.n * a.shares * a.groups;
+            if (p.join) a.sums = rest;
+            if (a.dweight || a.dbias) a.part = rest + (p.join ? (long long)a.n * a.groups : 0);
         } else if (p.workspace)
             a.part = (float2 *)workspace;
-        if (m.dtype == TC_BF16) st = p.vector == 8 ? launch<__nv_bfloat16, 8>(device, a, m.act, p.threads, p.shared, s) : launch<__nv_bfloat16, 1>(device, a, m.act, p.threads, p.shared, s);
-        else st = p.vector == 4 ? launch<float, 4>(device, a, m.act, p.threads, p.shared, s) : launch<float, 1>(device, a, m.act, p.threads, p.shared, s);
+        if (m.dtype == TC_BF16) st = p.vector == 8 ? launch<__nv_bfloat16, 8>(device, a, p, m.act, s) : launch<__nv_bfloat16, 1>(device, a, p, m.act, s);
+        else st = p.vector == 4 ? launch<float, 4>(device, a, p, m.act, s) : launch<float, 1>(device, a, p, m.act, s);
     }
     if (st != TC_OK || (!a.dweight && !a.dbias)) return st;
     const dim3 grid((unsigned int)((a.c + kVectorChannels - 1) / kVectorChannels));

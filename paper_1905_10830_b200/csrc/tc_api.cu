@@ -1901,9 +1901,9 @@ bool valid_group_params(const tc_tensor *x, const tc_group_params *p)
 {
     return aligned_tensor(x) && p && p->groups > 0 && x->c % p->groups == 0 && aligned_to(4, p->weight, p->bias) && p->activation >= TC_ACT_NONE && p->activation <= TC_ACT_SILU;
 }
-bool supported_groups(const tc_tensor *x, const tc_group_params *p)
+bool supported_groups(const tc_tensor *x)
 {
-    return pixels_of(x) <= kMostRows && x->c <= kMostGroupChannels && (long long)x->n * p->groups <= 1ll << 33;
+    return pixels_of(x) <= kMostRows && x->n <= 1 << 29 && x->c <= kMostGroupChannels;
 }
 void add_group_params(Ranges &r, const tc_tensor *x, const tc_group_params *p)
 {
@@ -2168,7 +2168,7 @@ tc_status tc_group_norm(tc_ctx *ctx, const tc_tensor *x, const tc_group_params *
     if (!ctx || !valid_group_params(x, params) || !aligned_to(element_size(x->dtype), y) || !aligned_to(8, stats)) return TC_ERR_INVALID_ARG;
     const long long p = pixels_of(x);
     if (!(params->eps >= 0.f) || (!y && !codes && p > 0)) return TC_ERR_INVALID_ARG;
-    if (!supported_groups(x, params)) return TC_ERR_UNSUPPORTED;
+    if (!supported_groups(x)) return TC_ERR_UNSUPPORTED;
     if (codes && (!valid_rows(codes) || codes->rows != p || codes->cols != x->c)) return TC_ERR_INVALID_ARG;
     Ranges ranges;
     add_group_params(ranges, x, params);
@@ -2195,7 +2195,7 @@ tc_status tc_group_norm_backward(tc_ctx *ctx, const tc_tensor *x, const tc_group
         return TC_ERR_INVALID_ARG;
     const long long p = pixels_of(x);
     if ((p > 0 && (!stats || !dy || !dx)) || (dweight && !params->weight) || (dbias && !params->bias)) return TC_ERR_INVALID_ARG;
-    if (!supported_groups(x, params)) return TC_ERR_UNSUPPORTED;
+    if (!supported_groups(x)) return TC_ERR_UNSUPPORTED;
     Ranges ranges;
     add_group_params(ranges, x, params);
     ranges.add(stats, (size_t)x->n * params->groups * 2 * sizeof(float), false);

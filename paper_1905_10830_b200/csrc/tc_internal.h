@@ -319,6 +319,18 @@ inline bool allow_shared(int device, size_t bytes)
     done.fetch_or(bit, std::memory_order_relaxed);
     return true;
 }
+// Clusters of up to sixteen blocks, asked for once on a device.
+template <auto kKernel>
+inline bool allow_large_clusters(int device)
+{
+    static std::atomic<unsigned long long> done{0};
+    const unsigned long long bit = device < 64 ? 1ull << device : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return true;
+    if (cudaFuncSetAttribute(kKernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) { cudaGetLastError(); return false; }
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
+constexpr size_t kTwoBlocks = 112 * 1024;     // shared memory of a block of which two find a place on an SM
 // The kernels' side of tc_blocks: codes [rows][ld], scales [blocks][scale_ld].
 struct BlockMatrix {
     uint8_t *codes = nullptr;
@@ -410,9 +422,13 @@ struct GroupGradArgs {
 // How maps are cut: `shared` bytes of a block where a map lies in a cluster's shared memory, else 0.
 struct GroupPlan {
     int vector = 1, threads = 256;
-    int share = 0, shares = 1;        // pixels of a block, blocks of a map
+    int share = 0, shares = 1;        // pixels of a block (a run), blocks (runs) of a map
+    bool join = false;                // runs' sums are joined by a kernel of their own
     size_t shared = 0, workspace = 0;
 };
+constexpr size_t kMostShared = 225 * 1024;       // of a block
+constexpr long long kRunBytes = 192 * 1024;
+constexpr int kInlineRuns = 64;                 // of a map, whose sums every run's block joins
 int tc_group_threads(int columns);
 GroupPlan tc_plan_group_norm(const GroupNormArgs &a, int sm_count);
 tc_status tc_launch_group_norm(int device, const GroupNormArgs &a, const GroupPlan &plan, void *workspace, cudaStream_t s);
