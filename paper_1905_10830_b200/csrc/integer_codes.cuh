@@ -36,8 +36,45 @@ __device__ __noinline__ static int code_at_border(float x, float scale, int near
     if (past != 0.f) return past > 0.f ? other : near_code;
     return near_code & 1 ? other : near_code;
 }
-// Codes of four values, packed.  With a NaN for its scale a row's codes are zeros.  Found with 1 / scale in fp32, whose product with x is off by
+// The largest magnitude of three values.
+__device__ __forceinline__ float most_of(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(fabsf(a)), "f"(fabsf(b)), "f"(fabsf(c)));
+    return d;
+}
+// Codes of eight values in pairs, packed.  With a NaN for its scale a row's codes are zeros.  Found with 1 / scale in fp32, whose product with x is off by
 // less than 127 x 2^-23; those that come near a border between two codes are looked at again with the border's exact difference.
+__device__ __forceinline__ uint2 codes_of_pairs(const uint64_t (&v)[4], const Coder &c)
+{
+    const uint64_t inv = pair_of(c.inv, c.inv), integer = pair_of(kInteger, kInteger), minus = pair_of(-1.0f, -1.0f);
+    float t[8], d[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t near_code = fma2(v[i], inv, integer);
+        halves(near_code, t[2 * i], t[2 * i + 1]);
+        halves(fma2(v[i], inv, fma2(near_code, minus, integer)), d[2 * i], d[2 * i + 1]);
+    }
+    if (most_of(most_of(most_of(d[0], d[1], d[2]), d[3], d[4]), most_of(d[5], d[6], d[7]), 0.f) > kNearBorder)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float x, y;
+            halves(v[i / 2], x, y);
+            if (fabsf(d[i]) > kNearBorder) t[i] = kInteger + (float)code_at_border(i & 1 ? y : x, c.scale, (int)(t[i] - kInteger), d[i]);
+        }
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        w[h] = __byte_perm(__byte_perm(__float_as_uint(t[4 * h]), __float_as_uint(t[4 * h + 1]), 0x0040),
+                           __byte_perm(__float_as_uint(t[4 * h + 2]), __float_as_uint(t[4 * h + 3]), 0x0040), 0x5410);
+    return c.scale == c.scale ? make_uint2(w[0], w[1]) : make_uint2(0u, 0u);
+}
+__device__ __forceinline__ uint2 codes_of8(const float (&v)[8], const Coder &c)
+{
+    const uint64_t p[4] = {pair_of(v[0], v[1]), pair_of(v[2], v[3]), pair_of(v[4], v[5]), pair_of(v[6], v[7])};
+    return codes_of_pairs(p, c);
+}
+// The same of four values.
 __device__ __forceinline__ uint32_t codes_of4(const float *v, const Coder &c)
 {
     float t[4], d[4];
@@ -46,8 +83,7 @@ __device__ __forceinline__ uint32_t codes_of4(const float *v, const Coder &c)
         t[i] = fmaf(v[i], c.inv, kInteger);
         d[i] = fmaf(v[i], c.inv, -(t[i] - kInteger));
     }
-    const float most = fmaxf(fmaxf(fabsf(d[0]), fabsf(d[1])), fmaxf(fabsf(d[2]), fabsf(d[3])));
-    if (most > kNearBorder)
+    if (fmaxf(most_of(d[0], d[1], d[2]), fabsf(d[3])) > kNearBorder)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (fabsf(d[i]) > kNearBorder) t[i] = kInteger + (float)code_at_border(v[i], c.scale, (int)(t[i] - kInteger), d[i]);
@@ -55,7 +91,6 @@ __device__ __forceinline__ uint32_t codes_of4(const float *v, const Coder &c)
     const uint32_t w = __byte_perm(lo, hi, 0x5410);
     return c.scale == c.scale ? w : 0u;
 }
-__device__ __forceinline__ uint2 codes_of8(const float (&v)[8], const Coder &c) { return make_uint2(codes_of4(v, c), codes_of4(v + 4, c)); }
 // One code (of the low byte).
 __device__ __forceinline__ uint8_t code_of(float x, const Coder &c)
 {

@@ -2131,12 +2131,12 @@ tc_status tc_quantize_rows(tc_ctx *ctx, const tc_tensor *x, const tc_rows *pixel
     if (p == 0) return TC_OK;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return TC_ERR_CUDA;
-    RowQuantizeArgs a{x->data, x->dtype, x->n, x->c, x->h * x->w, row_matrix(pixels), row_matrix(channels)};
-    const size_t bytes = tc_quantize_rows_workspace(a);
+    const RowQuantizeArgs a{x->data, x->dtype, x->n, x->c, x->h * x->w, row_matrix(pixels), row_matrix(channels), ctx->d_status};
+    const size_t bytes = tc_quantize_rows_workspace(a, ctx->sm_count);
     CallScratch scratch;
     const tc_status st = call_scratch(ctx, bytes, bytes, (cudaStream_t)cuda_stream, &scratch);
     if (st != TC_OK) return st;
-    return tc_launch_quantize_rows(ctx->device, a, scratch.at, (cudaStream_t)cuda_stream);
+    return tc_launch_quantize_rows(ctx->device, ctx->sm_count, a, scratch.at, (cudaStream_t)cuda_stream);
 }
 
 tc_status tc_matmul_rows(tc_ctx *ctx, const tc_rows *a, const tc_rows *b, const float *bias, int32_t relu, const tc_tensor *out, void *cuda_stream)

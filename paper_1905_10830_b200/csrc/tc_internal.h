@@ -331,6 +331,7 @@ inline bool allow_large_clusters(int device)
     return true;
 }
 constexpr size_t kTwoBlocks = 112 * 1024;     // shared memory of a block of which two find a place on an SM
+constexpr size_t kMostShared = 225 * 1024;       // of a block
 // The kernels' side of tc_blocks: codes [rows][ld], scales [blocks][scale_ld].
 struct BlockMatrix {
     uint8_t *codes = nullptr;
@@ -378,9 +379,10 @@ struct RowQuantizeArgs {
     const void *x;
     int dtype, n, c, hw;
     RowMatrix pixels, channels;       // codes null where not wanted
+    unsigned int *status;
 };
-size_t tc_quantize_rows_workspace(const RowQuantizeArgs &a);
-tc_status tc_launch_quantize_rows(int device, const RowQuantizeArgs &a, void *workspace, cudaStream_t s);
+size_t tc_quantize_rows_workspace(const RowQuantizeArgs &a, int sm_count);
+tc_status tc_launch_quantize_rows(int device, int sm_count, const RowQuantizeArgs &a, void *workspace, cudaStream_t s);
 struct RowMatmulArgs {
     RowMatrix pixels, channels;       // rows of the output's pixels, of its channels
     int cols;                         // length of the sums
@@ -426,7 +428,6 @@ struct GroupPlan {
     bool join = false;                // runs' sums are joined by a kernel of their own
     size_t shared = 0, workspace = 0;
 };
-constexpr size_t kMostShared = 225 * 1024;       // of a block
 constexpr long long kRunBytes = 192 * 1024;
 constexpr int kInlineRuns = 64;                 // of a map, whose sums every run's block joins
 int tc_group_threads(int columns);
