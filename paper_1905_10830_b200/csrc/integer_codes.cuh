@@ -12,20 +12,24 @@ using namespace blk;
 __device__ __forceinline__ float row_scale(uint32_t amax_bits)
 {
     if (amax_bits >= 0x7f800000u) return __int_as_float(0x7fffffff);
-    return __fdiv_rn(fmaxf(__uint_as_float(amax_bits), kSmallest), 127.0f);
+    // fl(a / 127): the product with fl(1 / 127), corrected by its residual (Markstein's step for quotients); equal to the quotient for all of fp32's significands
+    const float a = fmaxf(__uint_as_float(amax_bits), kSmallest), q = a * (1.0f / 127.0f);
+    return fmaf(fmaf(-127.0f, q, a), 1.0f / 127.0f, q);
 }
 
 // A row's scale and what its codes are computed with.
 struct Coder {
     float scale, inv;
+    uint32_t mask;
     __device__ __forceinline__ explicit Coder(float s)
     {
         scale = s;
-        inv = s == s ? __frcp_rn(s) : 0.f;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));                       // (one step off at most)
+        mask = s == s ? 0xffffffffu : 0u;
     }
 };
 constexpr float kInteger = 12582912.0f;                       // 1.5 x 2^23: added to a value of up to 2^22 it leaves the nearest integer in the low bits
-constexpr float kNearBorder = 0.5f - 1.0f / 32768.0f;
+constexpr float kNearBorder = 0.5f - 1.0f / 16384.0f;
 
 // The code next to `near_code` where x / scale comes close to the border between two.
 __device__ __noinline__ static int code_at_border(float x, float scale, int near_code, float rest)
@@ -44,7 +48,7 @@ __device__ __forceinline__ float most_of(float a, float b, float c)
     return d;
 }
 // Codes of eight values in pairs, packed.  With a NaN for its scale a row's codes are zeros.  Found with 1 / scale in fp32, whose product with x is off by
-// less than 127 x 2^-23; those that come near a border between two codes are looked at again with the border's exact difference.
+// less than 127 x 2^-22; those that come near a border between two codes are looked at again with the border's exact difference.
 __device__ __forceinline__ uint2 codes_of_pairs(const uint64_t (&v)[4], const Coder &c)
 {
     const uint64_t inv = pair_of(c.inv, c.inv), integer = pair_of(kInteger, kInteger), minus = pair_of(-1.0f, -1.0f);
@@ -67,7 +71,7 @@ __device__ __forceinline__ uint2 codes_of_pairs(const uint64_t (&v)[4], const Co
     for (int h = 0; h < 2; ++h)
         w[h] = __byte_perm(__byte_perm(__float_as_uint(t[4 * h]), __float_as_uint(t[4 * h + 1]), 0x0040),
                            __byte_perm(__float_as_uint(t[4 * h + 2]), __float_as_uint(t[4 * h + 3]), 0x0040), 0x5410);
-    return c.scale == c.scale ? make_uint2(w[0], w[1]) : make_uint2(0u, 0u);
+    return make_uint2(w[0] & c.mask, w[1] & c.mask);
 }
 __device__ __forceinline__ uint2 codes_of8(const float (&v)[8], const Coder &c)
 {
@@ -83,13 +87,13 @@ __device__ __forceinline__ uint32_t codes_of4(const float *v, const Coder &c)
         t[i] = fmaf(v[i], c.inv, kInteger);
         d[i] = fmaf(v[i], c.inv, -(t[i] - kInteger));
     }
-    if (fmaxf(most_of(d[0], d[1], d[2]), fabsf(d[3])) > kNearBorder)
+    if (fmaxf(fmaxf(fabsf(d[0]), fabsf(d[1])), fmaxf(fabsf(d[2]), fabsf(d[3]))) > kNearBorder)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (fabsf(d[i]) > kNearBorder) t[i] = kInteger + (float)code_at_border(v[i], c.scale, (int)(t[i] - kInteger), d[i]);
     const uint32_t lo = __byte_perm(__float_as_uint(t[0]), __float_as_uint(t[1]), 0x0040), hi = __byte_perm(__float_as_uint(t[2]), __float_as_uint(t[3]), 0x0040);
     const uint32_t w = __byte_perm(lo, hi, 0x5410);
-    return c.scale == c.scale ? w : 0u;
+    return w & c.mask;
 }
 // One code (of the low byte).
 __device__ __forceinline__ uint8_t code_of(float x, const Coder &c)

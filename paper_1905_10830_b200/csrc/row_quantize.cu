@@ -376,7 +376,7 @@ struct StripArgs {
     RowMatrix out;
     unsigned int *status;
 };
-constexpr int kStripThreads = 256;
+constexpr int kStripThreads = 512;                            // of a block that has an image; of strips half (64 of 128x56x56 bf16: 36 us, 57 with all)
 constexpr size_t kMostStrip = kMostShared - 4096;             // (static variables beside it)
 template <typename T, int kTogether>
 __global__ void __launch_bounds__(kStripThreads) pixel_strip_kernel(const T *x, const __grid_constant__ StripArgs a)
@@ -385,6 +385,7 @@ __global__ void __launch_bounds__(kStripThreads) pixel_strip_kernel(const T *x, 
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ __align__(8) unsigned long long s_full;
     __shared__ uint32_t s_max[2][kStripThreads];
+    const int threads = blockDim.x;
     T *const values = reinterpret_cast<T *>(smem);
     float *const scales = reinterpret_cast<float *>(smem + ((size_t)a.c * a.width * sizeof(T) + 15) / 16 * 16);
     if (threadIdx.x == 0) { mbar_init(smem_u32(&s_full), 1); mbar_fence_init(); }
@@ -405,8 +406,8 @@ __global__ void __launch_bounds__(kStripThreads) pixel_strip_kernel(const T *x, 
     } else {
         constexpr int kPer = 16 / (int)sizeof(T);
         const int per_row = a.width / kPer, k = (int)(threadIdx.x % per_row) * kPer;
-        if (threadIdx.x < kStripThreads / per_row * per_row)
-            for (int c = threadIdx.x / per_row; c < a.c; c += kStripThreads / per_row)
+        if (threadIdx.x < threads / per_row * per_row)
+            for (int c = threadIdx.x / per_row; c < a.c; c += threads / per_row)
                 cp_async_16(smem_u32(values + c * a.width + k), k < pixels ? src + (long long)c * a.hw + k : x, k < pixels ? 16u : 0u);
         cp_async_wait_all();
         __syncthreads();
@@ -424,8 +425,8 @@ __global__ void __launch_bounds__(kStripThreads) pixel_strip_kernel(const T *x, 
             v1 = w.y;
         }
     };
-    const int columns = a.width / kTogether, parts = max(1, kStripThreads / columns);
-    for (int base = 0; base < columns; base += kStripThreads) {
+    const int columns = a.width / kTogether, parts = max(1, threads / columns);
+    for (int base = 0; base < columns; base += threads) {
         const int part = parts > 1 ? threadIdx.x / columns : 0, q = base + (parts > 1 ? threadIdx.x - part * columns : threadIdx.x), p = q * kTogether;
         uint32_t m0 = 0, m1 = 0;
         if (q < columns && part < parts) {
@@ -465,7 +466,7 @@ __global__ void __launch_bounds__(kStripThreads) pixel_strip_kernel(const T *x, 
     __syncthreads();
     const int pieces = (a.c + 15) / 16;
     int piece = threadIdx.x / columns, q = threadIdx.x - piece * columns;
-    const int more_pieces = kStripThreads / columns, more = kStripThreads - more_pieces * columns;
+    const int more_pieces = threads / columns, more = threads - more_pieces * columns;
     for (; piece < pieces; piece += more_pieces, q += more) {
         if (q >= columns) {
             q -= columns;
@@ -510,9 +511,11 @@ tc_status launch_rows(const T *x, long long rows, int cols, const RowMatrix &out
     if (cols <= 256) return TC_ROWS(32, 1);
     if (cols <= 512) return TC_ROWS(32, 2);
     if (cols <= 1024) return TC_ROWS(32, 4);
-    if (cols <= 2048) return TC_ROWS(256, 1);
-    if (cols <= 4096) return TC_ROWS(256, 2);
-    if (cols <= 8192) return TC_ROWS(512, 2);
+    // (a row's maximum and scale are work of every warp: few warps, but for few rows, whose latency is their threads')
+    const bool few = rows < 592;
+    if (cols <= 2048) return few ? TC_ROWS(256, 1) : TC_ROWS(128, 2);
+    if (cols <= 4096) return few ? TC_ROWS(512, 1) : TC_ROWS(128, 4);
+    if (cols <= 8192) return few ? TC_ROWS(512, 2) : TC_ROWS(256, 4);
     if (cols <= 16384) return TC_ROWS(512, 4);
 #undef TC_ROWS
     return launch_first(true, vec ? long_rows_kernel<T, true> : long_rows_kernel<T, false>, dim3((unsigned int)rows), dim3(1024), 0, s, x, cols, out) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
@@ -523,9 +526,9 @@ bool in_memory(const RowQuantizeArgs &a, bool channels) { return channels ? a.hw
 // Whether the rows that lie in memory and the columns go through one kernel, and its blocks.
 bool rows_with_columns(const RowQuantizeArgs &a)
 {
-    return a.hw == 1 && a.pixels.codes && a.channels.codes && a.c % 8 == 0 && ((uintptr_t)a.x & 15u) == 0 && a.c > 1024 && a.c <= 8192;
+    return a.hw == 1 && a.pixels.codes && a.channels.codes && a.c % 8 == 0 && ((uintptr_t)a.x & 15u) == 0 && a.c > 1024 && a.c <= 4096;
 }
-int rows_blocks(const RowQuantizeArgs &a, int sm_count) { return (int)std::min<long long>(a.n, (a.c <= 4096 ? 4ll : 2ll) * sm_count); }
+int rows_blocks(const RowQuantizeArgs &a, int sm_count) { return (int)std::min<long long>(a.n, 4ll * sm_count); }
 
 // Parts of the maxima of the columns (rows = the inner index), or of the channels of maps.
 int parts_across(const RowQuantizeArgs &a, int vec, int sm_count)
@@ -580,8 +583,7 @@ tc_status quantize(int device, int sm_count, const RowQuantizeArgs &a, uint32_t 
         const long long rows = pixels;
         bool ok;
         if (a.c <= 2048) ok = launch(rows_and_columns_kernel<T, 256, 1>, dim3(blocks), 256, 0, x, rows, a.c, a.pixels, workspace);
-        else if (a.c <= 4096) ok = launch(rows_and_columns_kernel<T, 256, 2>, dim3(blocks), 256, 0, x, rows, a.c, a.pixels, workspace);
-        else ok = launch(rows_and_columns_kernel<T, 512, 2>, dim3(blocks), 512, 0, x, rows, a.c, a.pixels, workspace);
+        else ok = launch(rows_and_columns_kernel<T, 256, 2>, dim3(blocks), 256, 0, x, rows, a.c, a.pixels, workspace);
         if (!ok || !join(blocks, a.c, a.channels.scales)) return TC_ERR_CUDA;
         left[0] = RowMatrix{};
         t.across = left[1];
@@ -597,8 +599,9 @@ tc_status quantize(int device, int sm_count, const RowQuantizeArgs &a, uint32_t 
             const StripArgs strip{a.c, a.hw, width, (a.hw + width - 1) / width, left[0], a.status};
             const size_t smem = ((size_t)a.c * width * sizeof(T) + 15) / 16 * 16 + width * sizeof(float);
             const dim3 grid((unsigned int)(a.n * strip.strips));
+            const int threads = strip.strips > 1 ? kStripThreads / 2 : kStripThreads;
             if (!allow_shared<pixel_strip_kernel<T, 1>>(device, kMostStrip) || !allow_shared<pixel_strip_kernel<T, 2>>(device, kMostStrip) ||
-                !(width % 2 ? launch(pixel_strip_kernel<T, 1>, grid, kStripThreads, smem, x, strip) : launch(pixel_strip_kernel<T, 2>, grid, kStripThreads, smem, x, strip))) return TC_ERR_CUDA;
+                !(width % 2 ? launch(pixel_strip_kernel<T, 1>, grid, threads, smem, x, strip) : launch(pixel_strip_kernel<T, 2>, grid, threads, smem, x, strip))) return TC_ERR_CUDA;
             left[0] = RowMatrix{};
         }
         if (!left[0].codes && !left[1].codes) return TC_OK;
