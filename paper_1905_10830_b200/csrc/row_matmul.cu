@@ -41,11 +41,16 @@ template <int kN> struct Shape {
 // Tiles of a pair of CTAs: 256 x 256, 128 rows of each operand a CTA.
 namespace pair {
 constexpr int kN = 256, kRows = 256;
-constexpr int kStageBytes = 2 * kStageA, kStages = 5, kBuffers = 2, kTmemCols = 512;
+constexpr int kStageBytes = 2 * kStageA, kBuffers = 2, kTmemCols = 512;
 constexpr int kSets = 2, kCols = kN / kSets;
 constexpr int kEpiWarps = 8, kProducer = 8, kMma = 9;
 constexpr int kThreads = 10 * 32;
-constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kEpiWarps * kBoxBytes;
+// Long sums: a ring of five stages, a box a warp on the way out; short ones, whose stores are most of their time: four stages and two boxes (4096 to 8192 of 8192 rows 177 us
+// with the first, 184 with the second; 256 to 256 of 200704 46 and 42).
+template <bool kLong> constexpr int kStages = kLong ? 5 : 4;
+template <bool kLong> constexpr int kBoxes = kLong ? 1 : 2;
+template <bool kLong> constexpr size_t kSmem = 1024 + (size_t)kStages<kLong> * kStageBytes + kEpiWarps * kBoxes<kLong> * kBoxBytes;
+constexpr int kLongBlocks = 8;
 }
 
 struct RowArgs : TileArgs {
@@ -63,28 +68,46 @@ __device__ __forceinline__ float scaled(const TileArgs &a, int row, int col, flo
     return a.swapped ? v * of_col * of_row : v * of_row * of_col;
 }
 
-// What an epilogue warp needs of its columns: their scales and, where the columns are channels, their bias, in its slot of shared memory.
+// What an epilogue warp needs of a tile: its columns' scales and, where the columns are channels, their bias, in its slot of shared memory; its row's scale and
+// bias.  Asked for while the tile before is stored (with sums of one or two blocks the wait for them was a quarter of a tile's time).
 template <int kCols>
-struct Columns {
+struct Scales {
+    static constexpr int kMine = (kCols + 31) / 32;           // columns of a lane
     float *slot;                                              // [2][kCols]
-    __device__ __forceinline__ void fetch(const TileArgs &a, int col0, int lane) const
+    float of_column[kMine], bias[kMine], row_next, row_bias_next;
+    float row, row_bias;
+    __device__ __forceinline__ void ask(const TileArgs &a, int my_row, int col0, int lane)
+    {
+        const int at_row = min(my_row, a.rows_a - 1);
+        row_next = a.scale_a[at_row];
+        row_bias_next = a.bias && a.swapped ? a.bias[at_row] : 0.f;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int at = min(col0 + 32 * i + lane, a.rows_b - 1);                // (columns behind the last take its scale; nothing of theirs is stored)
+            of_column[i] = a.scale_b[at];
+            bias[i] = a.bias && !a.swapped ? a.bias[at] : 0.f;
+        }
+    }
+    __device__ __forceinline__ void take(int lane)
     {
         __syncwarp();                                         // the last tile's readers
 #pragma unroll
-        for (int c = lane; c < kCols; c += 32) {
-            const int at = min(col0 + c, a.rows_b - 1);       // (columns behind the last take its scale; nothing of theirs is stored)
-            slot[c] = a.scale_b[at];
-            if (a.bias && !a.swapped) slot[kCols + c] = a.bias[at];
-        }
+        for (int i = 0; i < kMine; ++i)
+            if (32 * i + lane < kCols) {
+                slot[32 * i + lane] = of_column[i];
+                slot[kCols + 32 * i + lane] = bias[i];
+            }
+        row = row_next;
+        row_bias = row_bias_next;
         __syncwarp();
     }
 };
 // kPairs pairs of neighbouring columns' sums to values, with bias and activation.
 template <int kCols, int kPairs>
-__device__ __forceinline__ void finish_rows(const TileArgs &a, const uint32_t *r, uint64_t *out, const Columns<kCols> &cols, int c, float row_scale, float row_bias)
+__device__ __forceinline__ void finish_rows(const TileArgs &a, const uint32_t *r, uint64_t *out, const Scales<kCols> &scales, int c)
 {
-    const uint64_t rs = pair_of(row_scale, row_scale), rb = pair_of(row_bias, row_bias);
-    const uint64_t *const cs = reinterpret_cast<const uint64_t *>(cols.slot + c), *const cb = reinterpret_cast<const uint64_t *>(cols.slot + kCols + c);
+    const uint64_t rs = pair_of(scales.row, scales.row), rb = pair_of(scales.row_bias, scales.row_bias);
+    const uint64_t *const cs = reinterpret_cast<const uint64_t *>(scales.slot + c), *const cb = reinterpret_cast<const uint64_t *>(scales.slot + kCols + c);
 #pragma unroll
     for (int j = 0; j < kPairs; ++j) {
         uint64_t v = pair_of((float)(int)r[2 * j], (float)(int)r[2 * j + 1]);
@@ -178,20 +201,21 @@ row_matmul_kernel(const __grid_constant__ RowArgs a, const __grid_constant__ CUt
     } else {
         const int set = warp >> 2, wq = warp & 3;
         const int row_in_tile = wq * 32 + lane;
-        const Columns<S::kCols> columns{s_columns[warp]};
+        Scales<S::kCols> scales;
+        scales.slot = s_columns[warp];
         int b = 0;
         uint32_t tphase = 0;
         bool alive = true;
+        const bool whole = !a.cluster && !a.parts;
+        Unit next = unit_of(a, a.first_unit + blockIdx.x);
+        if (whole) scales.ask(a, next.tile_m * kRowsM + row_in_tile, next.tile_n * kN + set * S::kCols, lane);
         for (int u = a.first_unit + blockIdx.x; u < a.end_unit; u += gridDim.x) {
-            const Unit t = unit_of(a, u);
+            const Unit t = next;
             const int row = t.tile_m * kRowsM + row_in_tile, col0 = t.tile_n * kN + set * S::kCols;
-            const bool whole = !a.cluster && !a.parts;
-            float row_scale = 0.f, row_bias = 0.f;
-            if (whole) {
-                columns.fetch(a, col0, lane);
-                const int at = min(row, a.rows_a - 1);
-                row_scale = a.scale_a[at];
-                if (a.bias && a.swapped) row_bias = a.bias[at];
+            if (whole) scales.take(lane);
+            if (u + (int)gridDim.x < a.end_unit) {
+                next = unit_of(a, u + gridDim.x);
+                if (whole) scales.ask(a, next.tile_m * kRowsM + row_in_tile, next.tile_n * kN + set * S::kCols, lane);
             }
             // (asked of the whole warp: what follows is done by all its lanes together)
             if (!__all_sync(0xffffffffu, mbar_wait_soon(smem_u32(&s_tfull[b]), tphase))) { alive = false; break; }
@@ -235,7 +259,7 @@ row_matmul_kernel(const __grid_constant__ RowArgs a, const __grid_constant__ CUt
                             tmem_ld_32x32b_x32(at + c + h, r);
                             tmem_ld_wait(r);
                             if (c + h + 32 == S::kCols) hand_back();
-                            finish_rows<S::kCols, 16>(a, r, v + h / 2, columns, c + h, row_scale, row_bias);
+                            finish_rows<S::kCols, 16>(a, r, v + h / 2, scales, c + h);
                         }
                         __syncwarp();                         // the last box's readers
                         fill_box<T>(box, v, lane);
@@ -251,7 +275,7 @@ row_matmul_kernel(const __grid_constant__ RowArgs a, const __grid_constant__ CUt
                     tmem_ld_32x32b_x16(at + c, r);
                     tmem_ld_wait(r);
                     if (c + 16 == S::kCols) hand_back();
-                    finish_rows<S::kCols, 8>(a, r, v, columns, c, row_scale, row_bias);
+                    finish_rows<S::kCols, 8>(a, r, v, scales, c);
                     store_lanes<T, 16>(a, v, row, col0 + c);
                 }
             }
@@ -324,12 +348,13 @@ __global__ void __launch_bounds__(256) row_matmul_join_kernel(RowArgs a, int n, 
 }
 
 // ---- pairs of CTAs -------------------------------------------------------------------------
-template <typename T>
+template <typename T, bool kLong>
 __global__ void __launch_bounds__(pair::kThreads, 1)
 row_matmul_pair_kernel(const __grid_constant__ RowArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                        const __grid_constant__ CUtensorMap map_out)
 {
     using namespace pair;
+    constexpr int kStages = pair::kStages<kLong>, kBoxes = pair::kBoxes<kLong>;
     extern __shared__ unsigned char smem_raw[];
     // s_full and s_tempty are the even CTA's: both CTAs' copies and epilogues report there; s_empty and s_tfull are each CTA's own.
     __shared__ __align__(8) unsigned long long s_full[kStages], s_empty[kStages], s_tfull[kBuffers], s_tempty[kBuffers];
@@ -404,20 +429,24 @@ row_matmul_pair_kernel(const __grid_constant__ RowArgs a, const __grid_constant_
         __syncwarp();
     } else {
         const int set = warp >> 2, wq = warp & 3;
-        const Columns<kCols> columns{s_columns[warp]};
-        const uint32_t box = ring + kStages * kStageBytes + warp * kBoxBytes;
+        Scales<kCols> scales;
+        scales.slot = s_columns[warp];
+        const uint32_t boxes = ring + kStages * kStageBytes + warp * kBoxes * kBoxBytes;
+        int turn = 0;
         uint32_t tempty[kBuffers];
 #pragma unroll
         for (int b = 0; b < kBuffers; ++b) tempty[b] = cluster_address(smem_u32(&s_tempty[b]), 0);
         int b = 0;
         uint32_t tphase = 0;
         bool alive = true;
+        auto ask = [&](const Unit &t) { scales.ask(a, t.tile_m * kRows + rank * kRowsM + wq * 32 + lane, t.tile_n * kN + set * kCols, lane); };
+        Unit next = unit_of(a, blockIdx.x >> 1);
+        ask(next);
         for (int u = blockIdx.x >> 1; u < units; u += step) {
-            const Unit t = unit_of(a, u);
+            const Unit t = next;
             const int first_row = t.tile_m * kRows + rank * kRowsM + wq * 32, col0 = t.tile_n * kN + set * kCols;
-            columns.fetch(a, col0, lane);
-            const int mine = min(first_row + lane, a.rows_a - 1);
-            const float row_scale = a.scale_a[mine], row_bias = a.bias && a.swapped ? a.bias[mine] : 0.f;
+            scales.take(lane);
+            if (u + step < units) ask(next = unit_of(a, u + step));
             // (asked of the whole warp: what follows is done by all its lanes together)
             if (!__all_sync(0xffffffffu, mbar_wait_soon(smem_u32(&s_tfull[b]), tphase))) { alive = false; break; }
             tc_fence_after_sync();
@@ -437,10 +466,16 @@ row_matmul_pair_kernel(const __grid_constant__ RowArgs a, const __grid_constant_
                         tmem_ld_32x32b_x32(at + c + h, r);
                         tmem_ld_wait(r);
                         if (c + h + 32 == kCols) hand_back();
-                        finish_rows<kCols, 16>(a, r, v + h / 2, columns, c + h, row_scale, row_bias);
+                        finish_rows<kCols, 16>(a, r, v + h / 2, scales, c + h);
                     }
-                    if (a.store_tma && lane == 0) tma_store_wait_read();
-                    __syncwarp();                             // the last box's readers
+                    // boxes in turn: one may still be on its way out
+                    const uint32_t box = boxes + turn * kBoxBytes;
+                    turn = (turn + 1) % kBoxes;
+                    if (a.store_tma && lane == 0) {
+                        if constexpr (kBoxes == 2) tma_store_wait_read_but_one();
+                        else tma_store_wait_read();
+                    }
+                    __syncwarp();                             // the last readers of this box
                     fill_box<T>(box, v, lane);
                     if (a.store_tma) fence_proxy_async_smem();
                     __syncwarp();
@@ -457,7 +492,7 @@ row_matmul_pair_kernel(const __grid_constant__ RowArgs a, const __grid_constant_
                     tmem_ld_32x32b_x32(at + c, r);
                     tmem_ld_wait(r);
                     if (c + 32 == kCols) hand_back();
-                    finish_rows<kCols, 16>(a, r, v, columns, c, row_scale, row_bias);
+                    finish_rows<kCols, 16>(a, r, v, scales, c);
                     store_lanes<T, 32>(a, v, first_row + lane, col0 + c);
                 }
             }
@@ -486,20 +521,20 @@ tc_status launch_tiles(const tc_ctx *ctx, const RowArgs &a, const CUtensorMap &m
     return launch_first_cluster(a.cluster ? a.splits : 1, kernel, grid, dim3(Shape<kN>::kThreads), Shape<kN>::kSmem, s, a, map_a, map_b) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
 
-template <typename T>
+template <typename T, bool kLong>
 tc_status launch_pairs(const tc_ctx *ctx, const RowArgs &a, const CUtensorMap &map_a, const CUtensorMap &map_b, const CUtensorMap &map_out, cudaStream_t s)
 {
-    constexpr auto kernel = row_matmul_pair_kernel<T>;
-    if (!allow_shared<kernel>(ctx->device, pair::kSmem)) return TC_ERR_CUDA;
+    constexpr auto kernel = row_matmul_pair_kernel<T, kLong>;
+    if (!allow_shared<kernel>(ctx->device, pair::kSmem<kLong>)) return TC_ERR_CUDA;
     const int units = a.end_unit - a.first_unit, pairs = ctx->sm_count / 2;
     const dim3 grid((unsigned int)(2 * (units < pairs ? units : pairs)));
-    return launch_first_cluster(2, kernel, grid, dim3(pair::kThreads), pair::kSmem, s, a, map_a, map_b, map_out) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
+    return launch_first_cluster(2, kernel, grid, dim3(pair::kThreads), pair::kSmem<kLong>, s, a, map_a, map_b, map_out) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
 
 template <typename T>
 tc_status launch(const tc_ctx *ctx, const RowArgs &a, bool pairs, int n, const CUtensorMap &map_a, const CUtensorMap &map_b, const CUtensorMap &map_out, cudaStream_t s)
 {
-    if (pairs) return launch_pairs<T>(ctx, a, map_a, map_b, map_out, s);
+    if (pairs) return a.k_blocks >= pair::kLongBlocks ? launch_pairs<T, true>(ctx, a, map_a, map_b, map_out, s) : launch_pairs<T, false>(ctx, a, map_a, map_b, map_out, s);
     switch (n) {
     case 16: return launch_tiles<T, 16>(ctx, a, map_a, map_b, s);
     case 32: return launch_tiles<T, 32>(ctx, a, map_a, map_b, s);

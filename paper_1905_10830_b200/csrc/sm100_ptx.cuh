@@ -318,6 +318,7 @@ __device__ __forceinline__ void tma_store_2d(const void *tensor_map, int x, int 
                  ::"l"(tensor_map), "r"(x), "r"(y), "r"(smem_src) : "memory");
 }
 __device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void tma_store_wait_read_but_one() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
 __device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // Contiguous bulk copy global -> shared: both addresses 16-byte aligned, the size a multiple of 16.
