@@ -81,9 +81,9 @@ const at::Tensor &tensor_of(PyObject *o)
 }
 bool on_device(const at::Tensor &t, int device) { return t.is_cuda() && t.get_device() == device && t.is_contiguous(); }
 
-tc_tensor map_of(const at::Tensor &x, int device)
+// Checks of type, device and sides that all 4-d tensors have in common.
+tc_tensor sides_of(const at::Tensor &x, int device)
 {
-    if (!x.is_cuda() || !x.is_contiguous() || x.dim() != 4) throw Bad{"expected a contiguous 4-d CUDA tensor (NCHW)"};
     if (x.get_device() != device) throw Bad{"expected tensors on the context's device"};
     const auto type = x.scalar_type();
     if (type != at::kFloat && type != at::kBFloat16) throw Bad{"dtype must be float32 or bfloat16"};
@@ -91,15 +91,19 @@ tc_tensor map_of(const at::Tensor &x, int device)
         if (x.size(i) > INT32_MAX) throw Bad{"tensor sides must fit 32 bits"};
     return tc_tensor{x.data_ptr(), (int32_t)x.size(0), (int32_t)x.size(1), (int32_t)x.size(2), (int32_t)x.size(3), type == at::kFloat ? TC_F32 : TC_BF16};
 }
+tc_tensor map_of(const at::Tensor &x, int device)
+{
+    if (!x.is_cuda() || !x.is_contiguous() || x.dim() != 4) throw Bad{"expected a contiguous 4-d CUDA tensor (NCHW)"};
+    return sides_of(x, device);
+}
 bool channels_last(const at::Tensor &x) { return x.dim() == 4 && x.is_contiguous(at::MemoryFormat::ChannelsLast); }
 // The same of a tensor whose channels may be neighbours in memory: pixels of 1 x 1 then.
 tc_tensor map_of_either(const at::Tensor &x, int device)
 {
-    if (x.dim() == 4 && !x.is_contiguous() && channels_last(x)) {
-        tc_tensor t = map_of(x.permute({0, 2, 3, 1}), device);       // (its sides and type are checked; the C dimension is the last)
-        const int64_t pixels = (int64_t)t.n * t.c * t.h;
-        if (pixels > INT32_MAX) throw Bad{"a channels_last tensor's pixels must fit 32 bits"};
-        return tc_tensor{t.data, (int32_t)pixels, t.w, 1, 1, t.dtype};
+    if (x.is_cuda() && !x.is_contiguous() && channels_last(x)) {
+        const tc_tensor t = sides_of(x, device);
+        if ((int64_t)t.h * t.w > INT32_MAX || (int64_t)t.n * (t.h * t.w) > INT32_MAX) throw Bad{"a channels_last tensor's pixels must fit 32 bits"};
+        return tc_tensor{t.data, t.n * t.h * t.w, t.c, 1, 1, t.dtype};
     }
     return map_of(x, device);
 }
@@ -122,9 +126,9 @@ float *vector(PyObject *o, int64_t n, int device, const char *name)
         throw Bad{std::string(name) + ": expected " + std::to_string(n) + " contiguous float32 values on the context's device"};
     return (float *)t.data_ptr();
 }
-at::Tensor make(at::IntArrayRef sizes, at::ScalarType type, int device)
+at::Tensor make(at::IntArrayRef sizes, at::ScalarType type, int device, bool last = false)
 {
-    return at::detail::empty_cuda(sizes, type, at::Device(at::kCUDA, (c10::DeviceIndex)device), c10::nullopt);
+    return at::detail::empty_cuda(sizes, type, at::Device(at::kCUDA, (c10::DeviceIndex)device), last ? c10::optional<at::MemoryFormat>(at::MemoryFormat::ChannelsLast) : c10::nullopt);
 }
 at::Tensor make_like(const at::Tensor &t) { return make(t.sizes(), t.scalar_type(), t.get_device()); }
 Ref wrap(const at::Tensor &t) { return Ref(THPVariable_Wrap(t)); }
@@ -277,8 +281,7 @@ at::Tensor make_output(PyObject *shape_arg, PyObject *dtype, int64_t rows, int64
     if (type != at::kFloat && type != at::kBFloat16) throw Bad{"dtype must be float32 or bfloat16"};
     for (const int64_t v : shape)
         if (v < 0 || v > INT32_MAX) throw Bad{"shape: expected (N, H, W)"};
-    if (last) return make({shape[0], shape[1], shape[2], channels}, type, device).permute({0, 3, 1, 2});
-    return make({shape[0], channels, shape[1], shape[2]}, type, device);
+    return make({shape[0], channels, shape[1], shape[2]}, type, device, last);
 }
 
 // a, b, shape, dtype, bias, relu, out
@@ -446,8 +449,7 @@ PyObject *matmul_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
 tc_tensor last_map_of(const at::Tensor &x, int device)
 {
     if (!x.is_cuda() || !channels_last(x)) throw Bad{"expected a 4-d CUDA tensor in channels_last order"};
-    const tc_tensor t = map_of(x.permute({0, 2, 3, 1}), device);
-    return tc_tensor{t.data, t.n, t.w, t.c, t.h, t.dtype};
+    return sides_of(x, device);
 }
 // A channels_last tensor of the shape and type of `x`.
 void *last_like(PyObject *o, const at::Tensor &x, int device, const char *name)
@@ -457,7 +459,7 @@ void *last_like(PyObject *o, const at::Tensor &x, int device, const char *name)
         throw Bad{std::string(name) + ": expected a channels_last tensor of the shape and type of the first, on the context's device"};
     return t.numel() ? t.data_ptr() : (void *)16;
 }
-at::Tensor make_last(const at::Tensor &x) { return make({x.size(0), x.size(2), x.size(3), x.size(1)}, x.scalar_type(), x.get_device()).permute({0, 3, 1, 2}); }
+at::Tensor make_last(const at::Tensor &x) { return make(x.sizes(), x.scalar_type(), x.get_device(), true); }
 float *stats_of(PyObject *o, int64_t n, int64_t groups, int device)
 {
     const at::Tensor &t = tensor_of(o);
