@@ -66,10 +66,11 @@ __device__ __forceinline__ void block_moments(const T *src, const Pieces &pieces
         }
         // a channel's mean and squares, and in warps its group's
         channel_sums<V>(lay, b, s, q, red, [&](int ch, float sum_d, float sum_q) {
-            const float d = sum_d * per_pixel;
-            float mean = ch >= 0 && pixels > 0 ? load1(src + ch) + d : 0.f, m2 = ch >= 0 && pixels > 0 ? fmaf(-sum_d, d, sum_q) : 0.f;
+            // (products that are not left to be fused: the statistics' bits are the same in every variant of the kernels)
+            const float d = __fmul_rn(sum_d, per_pixel);
+            float mean = ch >= 0 && pixels > 0 ? __fadd_rn(load1(src + ch), d) : 0.f, m2 = ch >= 0 && pixels > 0 ? fmaf(-sum_d, d, sum_q) : 0.f;
             if (in_warps) {
-                const float m = sum_over(mean, per_group) * per_channel;
+                const float m = __fmul_rn(sum_over(mean, per_group), per_channel);
                 m2 = sum_over(fmaf(n * (mean - m), mean - m, m2), per_group);
                 if (ch >= 0 && (ch & (per_group - 1)) == 0) to(ch / per_group, make_float2(m, m2));
             } else if (ch >= 0)
@@ -86,10 +87,10 @@ __device__ __forceinline__ void block_moments(const T *src, const Pieces &pieces
         const int count = g < a.groups ? per_group : 0;
         float mean = 0.f, m2 = 0.f;
         for (int i = team.rank; i < count; i += team.size) mean += at[i].x;
-        mean = team.sum(mean) * per_channel;
+        mean = __fmul_rn(team.sum(mean), per_channel);
         for (int i = team.rank; i < count; i += team.size) {
             const float2 t = at[i];
-            m2 += fmaf(n * (t.x - mean), t.x - mean, t.y);
+            m2 = __fadd_rn(m2, fmaf(n * (t.x - mean), t.x - mean, t.y));
         }
         m2 = team.sum(m2);
         if (g < a.groups && team.rank == 0) to(g, make_float2(mean, m2));
@@ -103,10 +104,10 @@ template <int V> struct Affine {
     template <typename F>
     __device__ __forceinline__ Affine(const GroupArgs &a, int c, F stats)
     {
-        stats_pairs<V>(c, a.c / a.groups, minus, slope, stats);
         Pairs<V> w;
         vector_pairs<V>(a.weight, c, 1.f, w);
         vector_pairs<V>(a.bias, c, 0.f, bias);
+        stats_pairs<V>(c, a.c / a.groups, minus, slope, stats);
 #pragma unroll
         for (int k = 0; k < kPairs<V>; ++k) slope[k] = mul2(slope[k], w[k]);
     }
@@ -250,14 +251,14 @@ __global__ void __launch_bounds__(512, 2) group_norm_map_kernel(const __grid_con
         float mean = 0.f, m2 = 0.f;
 #pragma unroll
         for (int i = 0; i < kMostShares; ++i)
-            if (i < a.shares) mean += m[i].x * ((float)max(0, min(a.share, a.hw - i * a.share)) * (float)per_group / count);
+            if (i < a.shares) mean = fmaf(m[i].x, (float)max(0, min(a.share, a.hw - i * a.share)) * (float)per_group / count, mean);
 #pragma unroll
         for (int i = 0; i < kMostShares; ++i)
             if (i < a.shares) {
                 const float d = m[i].x - mean;
-                m2 += m[i].y + (float)max(0, min(a.share, a.hw - i * a.share)) * (float)per_group * d * d;
+                m2 = __fadd_rn(m2, fmaf((float)max(0, min(a.share, a.hw - i * a.share)) * (float)per_group * d, d, m[i].y));
             }
-        const float2 s = make_float2(mean, 1.0f / sqrtf(m2 / count + a.eps));
+        const float2 s = make_float2(mean, 1.0f / sqrtf(__fadd_rn(m2 / count, a.eps)));
         stats[g] = s;
         if (rank == 0 && a.stats) a.stats[map * a.groups + g] = s;
     }
@@ -285,12 +286,12 @@ __device__ __forceinline__ float2 join_runs(const GroupArgs &a, long long map, i
         const float2 m = at[(long long)r * a.groups];
         const float n = (float)min(a.share, a.hw - r * a.share), d = m.x - from;
         s = fmaf(n, d, s);
-        q += fmaf(n * (float)per_group * d, d, m.y);
+        q = __fadd_rn(q, fmaf(n * (float)per_group * d, d, m.y));
     }
     s = sum_over(s, size);
     q = sum_over(q, size);
     const float d = s / (float)a.hw;
-    return make_float2(from + d, 1.0f / sqrtf(fmaxf(fmaf(-s * (float)per_group, d, q), 0.f) / ((float)a.hw * (float)per_group) + a.eps));
+    return make_float2(__fadd_rn(from, d), 1.0f / sqrtf(__fadd_rn(fmaxf(fmaf(-s * (float)per_group, d, q), 0.f) / ((float)a.hw * (float)per_group), a.eps)));
 }
 
 // Maps of many runs: sums[map][group], a warp each.
@@ -424,7 +425,7 @@ int shares_on_chip(long long n, int hw, long long most, int sm_count, const std:
         int shares = 1;
         while (shares < groups::kMostShares && bytes(shares) > room) shares *= 2;
         if (bytes(shares) > room || n * shares > most) continue;
-        while (shares < 8 && n * shares * 2 <= sm_count && hw / shares >= 16) shares *= 2;
+        while (shares < groups::kMostShares && n * shares * 2 <= sm_count && hw / shares >= 12) shares *= 2;
         return shares;
     }
     return 0;
