@@ -99,7 +99,8 @@ EXPORTS = ["tc_create", "tc_destroy", "tc_status_string", "tc_get_status", "tc_f
            "tc_host_huffman_lengths", "tc_host_eigh", "tc_device_eigh", "tc_encode_bound", "tc_encode", "tc_encode_noalloc", "tc_decode", "tc_encode_many", "tc_decode_many", "tc_roundtrip_host",
            "tc_stats", "tc_fit_state_create", "tc_fit_state_free", "tc_fit_state_update", "tc_fit_state_export",
            "tc_fit_state_import", "tc_fit_state_finish", "tc_fold_forward", "tc_fold_inverse",
-           "tc_quantize_blocks", "tc_matmul_blocks", "tc_residual_norms", "tc_residual_norms_backward"]
+           "tc_quantize_blocks", "tc_matmul_blocks", "tc_residual_norms", "tc_residual_norms_backward",
+           "tc_quantize_rows", "tc_matmul_rows", "tc_group_norm", "tc_group_norm_backward", "tc_gradient_norm", "tc_clip_gradients"]
 
 _lib = None
 

@@ -7,8 +7,6 @@
 // column blocks.
 #pragma once
 
-#include <functional>
-
 #include "block_codes.cuh"
 #include "sm100_ptx.cuh"
 #include "tc_internal.h"
@@ -386,5 +384,19 @@ __device__ __forceinline__ float sum_over(float v, int lanes)
 
 }  // namespace groups
 
-int shares_on_chip(long long n, int hw, long long most, int sm_count, const std::function<size_t(int)> &bytes);
+// Blocks of a map where maps lie in clusters' shared memory; 0: they do not.  As few as let two share an SM, then as few as fit one, where all of them are `most` at
+// most, and more where SMs would be idle.  More maps than find a place at a time take the other kernels: a block's phases (wait, sums, cluster, values) follow one another,
+// and little of the next one's waiting falls into them (1024 maps of 256x14x14 bf16: 64 us and 70, their gradient 173 and 168; 64 of 512x28x28 45 and 53, 125 and 77).
+template <typename F>
+int shares_on_chip(long long n, int hw, long long most, int sm_count, F bytes)
+{
+    for (const size_t room : {kTwoBlocks, kMostShared}) {
+        int shares = 1;
+        while (shares < groups::kMostShares && bytes(shares) > room) shares *= 2;
+        if (bytes(shares) > room || n * shares > most) continue;
+        while (shares < groups::kMostShares && n * shares * 2 <= sm_count && hw / shares >= 12) shares *= 2;
+        return shares;
+    }
+    return 0;
+}
 void cut_runs(GroupPlan &p, long long n, int hw, long long row, int tensors, int sm_count);
