@@ -2,10 +2,10 @@
 //
 //   y = act((x - mean) rstd w + b),   mean and rstd = 1 / sqrt(var + eps) over a map's pixels and a group's channels
 //
-// Bound by the bytes moved, x once and y once.  Where a map fits the shared memory of a cluster's blocks (up to eight) it is read once: each block
+// Bound by the bytes moved, x once and y once.  Where a map fits the shared memory of a cluster's blocks (up to sixteen) it is read once: each block
 // takes its pixels there by bulk copies, finds its mean and then its squares about that mean, the blocks' moments are put together through
 // the cluster's shared memory, and the values leave from where they lie.  Larger maps, and rows that do not begin at 16 bytes, take
-// two kernels: moments of runs of pixels, and the values.
+// two kernels: moments of runs of pixels, and the values, the pixels through a ring in shared memory where their rows begin at 16 bytes.
 //
 // Moments are put together as (n, mean, M2): no sum of squares is taken about a mean far from its own.
 #include "group_norm.cuh"
@@ -17,13 +17,15 @@ using namespace groups;
 using rowcodes::Coder;
 
 constexpr int kBatch = 4;
+constexpr int kNormSlots = 3;
+using NormRing = Ring<kNormSlots, 4, 1>;                      // 48 KB, three blocks an SM
 
 // Mean and M2 (sum of squares about it) of each group over the pixels at `src`, in one pass: sums of the distances d of a channel's values from the
 // first pixel's, p, and of their squares; the channel's mean is m = p + sum d / n, its squares about that sum d^2 - (sum d)^2 / n.  p being one of the n
 // values, (p - m)^2 is at most n times the mean square distance: the difference loses no more than a factor of n.
-// to(group, (mean, M2)) by one thread each.  red: red_values() float2; channels: c float2 of (m, squares).
-template <typename T, int V, typename F>
-__device__ __forceinline__ void block_moments(const T *src, const Pieces &pieces, const GroupArgs &a, const Lay &lay, float2 *red, float2 *channels, F to)
+// to(group, (mean, M2)) by one thread each.  red: red_values() float2; channels: c float2 of (p, ), then (m, squares).
+template <typename T, int V, typename P, typename F>
+__device__ __forceinline__ void block_moments(const T *src, P pieces, const GroupArgs &a, const Lay &lay, float2 *red, float2 *channels, F to)
 {
     const int per_group = a.c / a.groups, pixels = pieces.pixels;
     const float per_pixel = 1.0f / (float)pixels, per_channel = 1.0f / (float)per_group, n = (float)pixels;
@@ -32,18 +34,26 @@ __device__ __forceinline__ void block_moments(const T *src, const Pieces &pieces
         Pairs<V> from = {}, sum = {}, squares = {};
         const bool here = lay.at(b) && pixels > 0;
         const int c = (b * lay.lanes + lay.lane) * V;
-        if (here) {
-            const T *const p = src + c;
-            for (int piece = 0; piece < pieces.count(); ++piece) {
-                pieces.wait(piece);
+        for (int piece = 0; piece < pieces.count(); ++piece) {
+            pieces.wait(piece);
+            if (here) {
+                const T *const p = src + pieces.at(piece) * a.c + c;
                 if (piece == 0) {
                     load_pairs<V>(p, from);
 #pragma unroll
-                    for (int k = 0; k < kPairs<V>; ++k) from[k] ^= kMinus;
+                    for (int k = 0; k < kPairs<V>; ++k) {
+                        float x, y;
+                        halves(from[k], x, y);
+                        if (lay.row == 0) {                   // (a ring's first pixel is gone when the channel's mean is computed)
+                            channels[c + 2 * k].x = x;
+                            if (V > 1) channels[c + 2 * k + 1].x = y;
+                        }
+                        from[k] ^= kMinus;
+                    }
                 }
                 Raw<T, V> raw[kBatch];
                 in_batches<kBatch>(
-                    pieces.first(piece) + lay.row, pieces.end(piece), lay.rows, [&](int k, int i) { load_raw<V>(raw[k], p + i * a.c); },
+                    lay.row, pieces.end(piece) - pieces.first(piece), lay.rows, [&](int k, int i) { load_raw<V>(raw[k], p + i * a.c); },
                     [&](int k, int, int second) {
                         for (int h = 0; h < (second < 0 ? 1 : 2); ++h) {
                             Pairs<V> v;
@@ -57,6 +67,7 @@ __device__ __forceinline__ void block_moments(const T *src, const Pieces &pieces
                         }
                     });
             }
+            pieces.done(piece);
         }
         float s[2 * kPairs<V>], q[2 * kPairs<V>];
 #pragma unroll
@@ -68,7 +79,7 @@ __device__ __forceinline__ void block_moments(const T *src, const Pieces &pieces
         channel_sums<V>(lay, b, s, q, red, [&](int ch, float sum_d, float sum_q) {
             // (products that are not left to be fused: the statistics' bits are the same in every variant of the kernels)
             const float d = __fmul_rn(sum_d, per_pixel);
-            float mean = ch >= 0 && pixels > 0 ? __fadd_rn(load1(src + ch), d) : 0.f, m2 = ch >= 0 && pixels > 0 ? fmaf(-sum_d, d, sum_q) : 0.f;
+            float mean = ch >= 0 && pixels > 0 ? __fadd_rn(channels[ch].x, d) : 0.f, m2 = ch >= 0 && pixels > 0 ? fmaf(-sum_d, d, sum_q) : 0.f;
             if (in_warps) {
                 const float m = __fmul_rn(sum_over(mean, per_group), per_channel);
                 m2 = sum_over(fmaf(n * (mean - m), mean - m, m2), per_group);
@@ -112,37 +123,44 @@ template <int V> struct Affine {
         for (int k = 0; k < kPairs<V>; ++k) slope[k] = mul2(slope[k], w[k]);
     }
 };
-// The values of `pixels` pixels at `src`, the first of them pixel `first` of the tensor.
-template <typename T, int V, int kAct, typename F>
-__device__ __forceinline__ void write_values(const T *src, int pixels, long long first, const GroupArgs &a, const Lay &lay, F stats)
+// The values of the pixels at `src`, the first of them pixel `first` of the tensor.
+template <typename T, int V, int kAct, typename P, typename F>
+__device__ __forceinline__ void write_values(const T *src, P pieces, long long first, const GroupArgs &a, const Lay &lay, F stats)
 {
     for (int b = 0; b < lay.blocks; ++b) {
-        if (!lay.at(b)) continue;
-        const int c = (b * lay.lanes + lay.lane) * V;
+        const bool here = lay.at(b);
+        const int c = here ? (b * lay.lanes + lay.lane) * V : 0;
         const Affine<V> f(a, c, stats);
-        const T *const p = src + c;
-        T *const q = (T *)a.out + first * a.c + c;
-        Raw<T, V> raw[kBatch];
-        in_batches<kBatch>(
-            lay.row, pixels, lay.rows, [&](int k, int i) { load_raw<V>(raw[k], p + i * a.c); },
-            [&](int k, int i, int second) {
-                Pairs<V> v, w;
-                pairs_of<V>(raw[k], v);
-                pairs_of<V>(raw[k + 1], w);
+        T *const to = (T *)a.out + first * a.c + c;
+        for (int piece = 0; piece < pieces.count(); ++piece) {
+            pieces.wait(piece);
+            if (here) {
+                const T *const p = src + pieces.at(piece) * a.c + c;
+                T *const q = to + pieces.first(piece) * a.c;
+                Raw<T, V> raw[kBatch];
+                in_batches<kBatch>(
+                    lay.row, pieces.end(piece) - pieces.first(piece), lay.rows, [&](int k, int i) { load_raw<V>(raw[k], p + i * a.c); },
+                    [&](int k, int i, int second) {
+                        Pairs<V> v, w;
+                        pairs_of<V>(raw[k], v);
+                        pairs_of<V>(raw[k + 1], w);
 #pragma unroll
-                for (int j = 0; j < kPairs<V>; ++j) {
-                    v[j] = activate2<kAct>(fma2(add2(v[j], f.minus[j]), f.slope[j], f.bias[j]));
-                    w[j] = activate2<kAct>(fma2(add2(w[j], f.minus[j]), f.slope[j], f.bias[j]));
-                }
-                store_pairs<V>(q + i * a.c, v);
-                if (second >= 0) store_pairs<V>(q + second * a.c, w);
-            });
+                        for (int j = 0; j < kPairs<V>; ++j) {
+                            v[j] = activate2<kAct>(fma2(add2(v[j], f.minus[j]), f.slope[j], f.bias[j]));
+                            w[j] = activate2<kAct>(fma2(add2(w[j], f.minus[j]), f.slope[j], f.bias[j]));
+                        }
+                        store_pairs<V>(q + i * a.c, v);
+                        if (second >= 0) store_pairs<V>(q + second * a.c, w);
+                    });
+            }
+            pieces.done(piece);
+        }
     }
 }
 
 // The same as codes, and as values too where they are wanted: a team of lanes a pixel, its largest magnitude first.  `table`: [3][c] floats of shared memory.
-template <typename T, int V, int kAct, typename F>
-__device__ __forceinline__ void write_codes(const T *src, int pixels, long long first, const GroupArgs &a, const Lay &lay, F stats, float *table)
+template <typename T, int V, int kAct, typename P, typename F>
+__device__ __forceinline__ void write_codes(const T *src, P pieces, long long first, const GroupArgs &a, const Lay &lay, F stats, float *table)
 {
     const int per_group = a.c / a.groups;
     lay.sync();                                               // the last table's readers
@@ -158,7 +176,7 @@ __device__ __forceinline__ void write_codes(const T *src, int pixels, long long 
     while (size < 32 && size < columns) size *= 2;
     const int rank = threadIdx.x & (size - 1), step = lay.threads / size;
     auto values = [&](int pixel, int c, Pairs<V> &v) {
-        load_pairs<V>(src + (long long)pixel * a.c + c, v);
+        load_pairs<V>(src + (long long)pixel * a.c + c, v);   // (pixels as they lie at src)
         Pairs<V> minus, slope, bias;
         vector_pairs<V>(table, c, 0.f, minus);
         vector_pairs<V>(table, a.c + c, 0.f, slope);
@@ -166,37 +184,44 @@ __device__ __forceinline__ void write_codes(const T *src, int pixels, long long 
 #pragma unroll
         for (int k = 0; k < kPairs<V>; ++k) v[k] = activate2<kAct>(fma2(add2(v[k], minus[k]), slope[k], bias[k]));
     };
-    for (int base = 0; base < pixels; base += step) {         // (whole warps go round together)
-        const int pixel = base + threadIdx.x / size;
-        const bool here = pixel < pixels;
-        uint32_t most = 0;
-        if (here)
+    // pixel p of the run is team p % step's, whatever piece it comes in; whole warps go round together
+    for (int piece = 0; piece < pieces.count(); ++piece) {
+        pieces.wait(piece);
+        const int from = pieces.first(piece), end = pieces.end(piece), place = pieces.at(piece) - from;
+        for (int base = from / step * step; base < end; base += step) {
+            const int pixel = base + threadIdx.x / size;
+            const bool here = pixel >= from && pixel < end;
+            if (!__any_sync(0xffffffffu, here)) continue;
+            uint32_t most = 0;
+            if (here)
+                for (int c = rank * V; c < a.c; c += size * V) {
+                    Pairs<V> v;
+                    values(place + pixel, c, v);
+                    if (a.out) store_pairs<V>((T *)a.out + (first + pixel) * a.c + c, v);
+#pragma unroll
+                    for (int k = 0; k < kPairs<V>; ++k) {
+                        float x, y;
+                        halves(v[k], x, y);
+                        most = max(most, max(abs_bits(x), V > 1 ? abs_bits(y) : 0u));
+                    }
+                }
+            for (int d = size / 2; d; d >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
+            const Coder coder(rowcodes::row_scale(most));
+            if (!here) continue;
+            if (rank == 0) a.codes.scales[first + pixel] = coder.scale;
+            uint8_t *const to = a.codes.codes + (first + pixel) * a.codes.ld;
             for (int c = rank * V; c < a.c; c += size * V) {
                 Pairs<V> v;
-                values(pixel, c, v);
-                if (a.out) store_pairs<V>((T *)a.out + (first + pixel) * a.c + c, v);
+                values(place + pixel, c, v);
+                float f[2 * kPairs<V>];
 #pragma unroll
-                for (int k = 0; k < kPairs<V>; ++k) {
-                    float x, y;
-                    halves(v[k], x, y);
-                    most = max(most, max(abs_bits(x), V > 1 ? abs_bits(y) : 0u));
-                }
+                for (int k = 0; k < kPairs<V>; ++k) halves(v[k], f[2 * k], f[2 * k + 1]);
+                if constexpr (V == 8) *reinterpret_cast<uint2 *>(to + c) = make_uint2(rowcodes::codes_of4(f, coder), rowcodes::codes_of4(f + 4, coder));
+                else if constexpr (V == 4) *reinterpret_cast<uint32_t *>(to + c) = rowcodes::codes_of4(f, coder);
+                else to[c] = rowcodes::code_of(f[0], coder);
             }
-        for (int d = size / 2; d; d >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
-        const Coder coder(rowcodes::row_scale(most));
-        if (!here) continue;
-        if (rank == 0) a.codes.scales[first + pixel] = coder.scale;
-        uint8_t *const to = a.codes.codes + (first + pixel) * a.codes.ld;
-        for (int c = rank * V; c < a.c; c += size * V) {
-            Pairs<V> v;
-            values(pixel, c, v);
-            float f[2 * kPairs<V>];
-#pragma unroll
-            for (int k = 0; k < kPairs<V>; ++k) halves(v[k], f[2 * k], f[2 * k + 1]);
-            if constexpr (V == 8) *reinterpret_cast<uint2 *>(to + c) = make_uint2(rowcodes::codes_of4(f, coder), rowcodes::codes_of4(f + 4, coder));
-            else if constexpr (V == 4) *reinterpret_cast<uint32_t *>(to + c) = rowcodes::codes_of4(f, coder);
-            else to[c] = rowcodes::code_of(f[0], coder);
         }
+        pieces.done(piece);
     }
 }
 
@@ -265,8 +290,8 @@ __global__ void __launch_bounds__(512, 2) group_norm_map_kernel(const __grid_con
     __syncthreads();
     if (a.shares > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     auto of = [&](int g) { return stats[g]; };
-    if constexpr (kCodes) write_codes<T, V, kAct>(data, pixels, first, a, lay, of, reinterpret_cast<float *>(table));
-    else write_values<T, V, kAct>(data, pixels, first, a, lay, of);
+    if constexpr (kCodes) write_codes<T, V, kAct>(data, InPlace{pixels}, first, a, lay, of, reinterpret_cast<float *>(table));
+    else write_values<T, V, kAct>(data, InPlace{pixels}, first, a, lay, of);
     if (a.shares > 1) {
         __syncwarp();
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");       // the others have read this block's moments
@@ -307,48 +332,65 @@ __global__ void __launch_bounds__(256) group_join_kernel(const __grid_constant__
     if (a.stats) a.stats[i] = v;
 }
 
-// part[map][run][group]: moments of a run of pixels.  [red: red_values() float2][channels: c float2]
-template <typename T, int V>
-__global__ void __launch_bounds__(kRunThreads, 4) group_moments_kernel(const __grid_constant__ GroupArgs a)
+// What a kernel on runs begins with: its pixels as pieces, at `src`, for work(src, pieces).  A ring's lies first in shared memory, and threads behind kRunThreads fill it.
+template <typename T, bool kRing, typename F>
+__device__ __forceinline__ void with_run(const GroupArgs &a, const Run &run, const Lay &lay, unsigned char *smem, F work)
+{
+    const T *const src = (const T *)a.x + run.first * a.c;
+    if constexpr (kRing) {
+        __shared__ __align__(8) unsigned long long s_ring[2 * kNormSlots];
+        if (threadIdx.x == 0) NormRing::init(s_ring);
+        __syncthreads();
+        chain_next();
+        chain_wait();
+        const NormRing ring(run.pixels, lay.rows, s_ring, a.status);
+        if (threadIdx.x < kRunThreads) work(reinterpret_cast<const T *>(smem), ring);
+        else if (threadIdx.x == kRunThreads) ring.fill(smem, src, nullptr, a.c * (int)sizeof(T));
+    } else {
+        chain_next();
+        chain_wait();
+        work(src, InPlace{run.pixels});
+    }
+}
+// part[map][run][group]: moments of a run of pixels.  [ring][red: red_values() float2][channels: c float2]
+template <typename T, int V, bool kRing>
+__global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kRing ? 3 : 4) group_moments_kernel(const __grid_constant__ GroupArgs a, int ring)
 {
     extern __shared__ __align__(128) unsigned char smem[];
-    float2 *const red = reinterpret_cast<float2 *>(smem), *const channels = red + red_values(a.c / V, kRunThreads, V);
-    chain_next();
-    chain_wait();
+    float2 *const red = reinterpret_cast<float2 *>(smem + ring), *const channels = red + red_values(a.c / V, kRunThreads, V);
     const Lay lay(a.c / V, kRunThreads);
     const Run run(a, blockIdx.x);
     float2 *const part = a.part + (long long)run.index * a.groups;
-    block_moments<T, V>((const T *)a.x + run.first * a.c, Pieces(run.pixels, lay.rows, nullptr, a.status), a, lay, red, channels, [&](int g, float2 m) { part[g] = m; });
+    with_run<T, kRing>(a, run, lay, smem, [&](const T *src, auto pieces) { block_moments<T, V>(src, pieces, a, lay, red, channels, [&](int g, float2 m) { part[g] = m; }); });
 }
 
-// The values, the last runs first: they are the likeliest to be in L2 still.  [stats: groups float2][table of the codes: 3 c floats]
-template <typename T, int V, int kAct, bool kCodes>
-__global__ void __launch_bounds__(kRunThreads, 4) group_values_kernel(const __grid_constant__ GroupArgs a)
+// The values, the last runs first: they are the likeliest to be in L2 still.  [ring][stats: groups float2][table of the codes: 3 c floats]
+template <typename T, int V, int kAct, bool kCodes, bool kRing>
+__global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kRing ? 3 : 4) group_values_kernel(const __grid_constant__ GroupArgs a, int ring)
 {
     extern __shared__ __align__(128) unsigned char smem[];
-    float2 *const own = reinterpret_cast<float2 *>(smem);
-    chain_next();
-    chain_wait();
+    float2 *const own = reinterpret_cast<float2 *>(smem + ring);
     const Lay lay(a.c / V, kRunThreads);
     const Run run(a, gridDim.x - 1 - blockIdx.x);
-    if (a.sums)
-        for (int g = threadIdx.x; g < a.groups; g += kRunThreads) own[g] = a.sums[run.map * a.groups + g];
-    else {
-        const Team team(a.shares, kRunThreads);
-        for (int base = 0; base < a.groups; base += team.step) {
-            const int g = base + team.first;
-            const float2 v = join_runs(a, run.map, min(g, a.groups - 1), team.rank, team.size);
-            if (g < a.groups && team.rank == 0) {
-                own[g] = v;
-                if (a.stats && run.run == 0) a.stats[run.map * a.groups + g] = v;
+    with_run<T, kRing>(a, run, lay, smem, [&](const T *src, auto pieces) {
+        if (a.sums)
+            for (int g = threadIdx.x; g < a.groups; g += kRunThreads) own[g] = a.sums[run.map * a.groups + g];
+        else {
+            const Team team(a.shares, kRunThreads);
+            for (int base = 0; base < a.groups; base += team.step) {
+                const int g = base + team.first;
+                const float2 v = join_runs(a, run.map, min(g, a.groups - 1), team.rank, team.size);
+                if (g < a.groups && team.rank == 0) {
+                    own[g] = v;
+                    if (a.stats && run.run == 0) a.stats[run.map * a.groups + g] = v;
+                }
             }
         }
-    }
-    __syncthreads();
-    const T *const src = (const T *)a.x + run.first * a.c;
-    auto stats = [&](int g) { return own[g]; };
-    if constexpr (kCodes) write_codes<T, V, kAct>(src, run.pixels, run.first, a, lay, stats, reinterpret_cast<float *>(own + a.groups));
-    else write_values<T, V, kAct>(src, run.pixels, run.first, a, lay, stats);
+        lay.sync();
+        auto stats = [&](int g) { return own[g]; };
+        if constexpr (kCodes) write_codes<T, V, kAct>(src, pieces, run.first, a, lay, stats, reinterpret_cast<float *>(own + a.groups));
+        else write_values<T, V, kAct>(src, pieces, run.first, a, lay, stats);
+    });
 }
 
 template <typename T, int V, int kAct, bool kCodes>
@@ -358,15 +400,18 @@ tc_status launch_map(int device, const GroupArgs &a, int threads, size_t smem, c
     if (!allow_shared<kernel>(device, kMostShared) || !allow_large_clusters<kernel>(device)) return TC_ERR_CUDA;
     return launch_first_cluster(a.shares, kernel, dim3((unsigned int)(a.n * a.shares)), dim3(threads), smem, s, a) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
-template <typename T, int V, int kAct, bool kCodes>
+template <typename T, int V, int kAct, bool kCodes, bool kRing>
 tc_status launch_runs(int device, const GroupArgs &a, cudaStream_t s)
 {
-    const size_t first = 8 * (size_t)red_values(a.c / V, kRunThreads, V) + 8 * (size_t)a.c, last = 8 * (size_t)a.groups + (kCodes ? 12 * (size_t)a.c : 0);
-    if (!allow_shared<group_moments_kernel<T, V>>(device, kMostShared) || !allow_shared<group_values_kernel<T, V, kAct, kCodes>>(device, kMostShared)) return TC_ERR_CUDA;
-    const dim3 grid((unsigned int)(a.n * a.shares)), block(kRunThreads);
-    if (launch_first(true, group_moments_kernel<T, V>, grid, block, first, s, a) != cudaSuccess) return TC_ERR_CUDA;
+    constexpr auto moments = group_moments_kernel<T, V, kRing>;
+    constexpr auto values = group_values_kernel<T, V, kAct, kCodes, kRing>;
+    const size_t ring = kRing ? ring_bytes<NormRing>(a.c / V) : 0;
+    const size_t first = ring + 8 * (size_t)red_values(a.c / V, kRunThreads, V) + 8 * (size_t)a.c, last = ring + 8 * (size_t)a.groups + (kCodes ? 12 * (size_t)a.c : 0);
+    if (!allow_shared<moments>(device, kMostShared) || !allow_shared<values>(device, kMostShared)) return TC_ERR_CUDA;
+    const dim3 grid((unsigned int)(a.n * a.shares)), block(kRing ? kRunThreads + 32 : kRunThreads);
+    if (launch_first(true, moments, grid, block, first, s, a, (int)ring) != cudaSuccess) return TC_ERR_CUDA;
     if (a.sums && launch_chained(true, group_join_kernel, dim3((unsigned int)((a.n * a.groups + 7) / 8)), dim3(256), 0, s, a) != cudaSuccess) return TC_ERR_CUDA;
-    return launch_chained(true, group_values_kernel<T, V, kAct, kCodes>, grid, block, last, s, a) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
+    return launch_chained(true, values, grid, block, last, s, a, (int)ring) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
 
 template <typename T, int V>
@@ -375,9 +420,11 @@ tc_status launch(int device, const GroupArgs &a, const GroupPlan &p, int act, cu
     // (maps of single values never lie in shared memory: bulk copies begin at 16 bytes)
 #define TC_NORM(kAct, kCodes) \
     do { \
-        if constexpr (V > 1) \
+        if constexpr (V > 1) { \
             if (p.shared) return launch_map<T, V, kAct, kCodes>(device, a, p.threads, p.shared, s); \
-        return launch_runs<T, V, kAct, kCodes>(device, a, s); \
+            if (ring_takes(a.c, V)) return launch_runs<T, V, kAct, kCodes, true>(device, a, s); \
+        } \
+        return launch_runs<T, V, kAct, kCodes, false>(device, a, s); \
     } while (0)
     if (a.codes.codes) {
         if (act == kRelu) TC_NORM(kRelu, true);

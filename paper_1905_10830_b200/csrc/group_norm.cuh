@@ -16,7 +16,7 @@ namespace groups {
 using namespace tcdev;
 using namespace blk;
 
-constexpr int kRunThreads = 256;                               // of the kernels that work on runs of pixels
+constexpr int kRunThreads = 256;                               // that work on a run of pixels; a ring has a warp more
 
 enum { kNoAct = 0, kRelu = 1, kSilu = 2 };
 
@@ -257,30 +257,107 @@ struct Lay {
     __device__ __forceinline__ void sync() const { sm100::named_bar_sync(1, threads); }
 };
 
-// A block's pixels come in pieces, so that the first can be worked on while the others are on their way: pieces of whole rounds of the block's rows.
+// A block's pixels, a piece after the other: piece i has the pixels first(i) to end(i), the first of which lies `at(i)` pixels behind the source's address once wait(i) is over, until
+// done(i), both by whole warps.  (A wait that runs out is reported; the values are wrong then, nothing else.)
+// All of them are where they are:
+struct InPlace {
+    int pixels;
+    __device__ __forceinline__ int count() const { return 1; }
+    __device__ __forceinline__ int first(int) const { return 0; }
+    __device__ __forceinline__ int end(int) const { return pixels; }
+    __device__ __forceinline__ int at(int) const { return 0; }
+    __device__ __forceinline__ void wait(int) {}
+    __device__ __forceinline__ void done(int) {}
+};
+__device__ __forceinline__ bool arrived(unsigned long long *barrier, uint32_t parity)
+{
+    const uint32_t bar = sm100::smem_u32(barrier);
+    return sm100::mbar_try_wait(bar, parity, 1000u) || sm100::mbar_wait_soon(bar, parity) || sm100::mbar_wait_soon(bar, parity);
+}
+// On their way to shared memory, so that the first can be worked on while the others come: pieces of whole rounds of the block's rows.
 constexpr int kPieces = 4;
 struct Pieces {
     int pixels, each;
-    unsigned long long *full;         // null: they are where they are (global memory)
+    unsigned long long *full;
     unsigned int *status;
     __device__ __forceinline__ Pieces(int pixels_, int rows, unsigned long long *full_, unsigned int *status_)
     {
         pixels = pixels_;
-        each = full_ ? ((pixels + kPieces - 1) / kPieces + rows - 1) / rows * rows : pixels;
+        each = ((pixels + kPieces - 1) / kPieces + rows - 1) / rows * rows;
         full = full_;
         status = status_;
     }
     __device__ __forceinline__ int first(int piece) const { return min(piece * each, pixels); }
     __device__ __forceinline__ int end(int piece) const { return min((piece + 1) * each, pixels); }
-    __device__ __forceinline__ int count() const { return full ? kPieces : 1; }
-    // (a wait that runs out is reported; the values are wrong then, nothing else)
+    __device__ __forceinline__ int at(int piece) const { return first(piece); }
+    __device__ __forceinline__ int count() const { return kPieces; }
     __device__ __forceinline__ void wait(int piece) const
     {
-        if (!full || first(piece) == end(piece)) return;
-        const uint32_t bar = sm100::smem_u32(&full[piece]);
-        if (!sm100::mbar_try_wait(bar, 0, 1000u) && !sm100::mbar_wait_soon(bar, 0) && !sm100::mbar_wait_soon(bar, 0)) tc_dev_set_status(status, TC_ERR_TIMEOUT);
+        if (first(piece) != end(piece) && !arrived(&full[piece], 0)) tc_dev_set_status(status, TC_ERR_TIMEOUT);
+    }
+    __device__ __forceinline__ void done(int) const {}
+};
+// Of a run that is longer than its block's shared memory: pieces of kRounds rounds of the rows through a ring of kSlots, that a warp of its own fills by bulk copies.  Loads of a block's
+// threads keep too little on its way (128x56x56 x 128 bf16, gradient of silu: 143 us, ring 104; 256x56x56 x 128, forward: 114 and 95).
+template <int kSlots, int kRounds, int kTensors>
+struct Ring {
+    static constexpr int kRows = kTensors * kSlots * kRounds;
+    int pixels, each;
+    unsigned long long *full, *empty;
+    unsigned int *status;
+    bool lost;
+    __device__ __forceinline__ Ring(int pixels_, int rows, unsigned long long *barriers, unsigned int *status_)
+    {
+        pixels = pixels_;
+        each = kRounds * rows;
+        full = barriers;
+        empty = barriers + kSlots;
+        status = status_;
+        lost = false;
+    }
+    __device__ __forceinline__ int count() const { return (pixels + each - 1) / each; }
+    __device__ __forceinline__ int first(int piece) const { return piece * each; }
+    __device__ __forceinline__ int end(int piece) const { return min((piece + 1) * each, pixels); }
+    __device__ __forceinline__ int at(int piece) const { return piece % kSlots * each; }
+    __device__ __forceinline__ void wait(int piece)
+    {
+        if (lost || arrived(&full[piece % kSlots], piece / kSlots & 1)) return;
+        lost = true;
+        tc_dev_set_status(status, TC_ERR_TIMEOUT);
+    }
+    __device__ __forceinline__ void done(int piece) const
+    {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) sm100::mbar_arrive(sm100::smem_u32(&empty[piece % kSlots]));
+    }
+    __device__ __forceinline__ static void init(unsigned long long *barriers)
+    {
+        for (int i = 0; i < 2 * kSlots; ++i) sm100::mbar_init(sm100::smem_u32(&barriers[i]), i < kSlots ? 1 : kRunThreads / 32);
+        sm100::mbar_fence_init();
+    }
+    // By one thread: the run's pixels of `row` bytes from each of the tensors, to rings that follow one another.
+    __device__ __forceinline__ void fill(unsigned char *ring, const void *x, const void *dy, int row) const
+    {
+        const int pieces = count(), room = each * row;
+        for (int i = 0; i < pieces; ++i) {
+            const int slot = i % kSlots;
+            if (i >= kSlots && !arrived(&empty[slot], (i / kSlots + 1) & 1)) {
+                tc_dev_set_status(status, TC_ERR_TIMEOUT);
+                return;
+            }
+            const uint32_t bytes = (uint32_t)(end(i) - first(i)) * row, bar = sm100::smem_u32(&full[slot]), to = sm100::smem_u32(ring) + slot * room;
+            const size_t from = (size_t)first(i) * row;
+            sm100::mbar_arrive_expect_tx(bar, kTensors * bytes);
+            sm100::bulk_load(to, (const char *)x + from, bytes, bar);
+            if (kTensors > 1) sm100::bulk_load(to + kSlots * room, (const char *)dy + from, bytes, bar);
+        }
     }
 };
+// A ring's bytes.  (Rows of a block: as Lay's.)
+template <typename R>
+size_t ring_bytes(int columns) { return (size_t)R::kRows * (kRunThreads / columns) * columns * 16; }
+// Rings are for rows whose vectors have a thread each.
+inline bool ring_takes(int c, int v) { return v > 1 && c / v <= kRunThreads; }
 
 // The run of pixels that a block works on.
 struct Run {

@@ -8,12 +8,17 @@
 // A and B, which the last kernel adds over maps in a fixed order.
 #include "group_norm.cuh"
 
+#include <type_traits>
+
 namespace {
 
 using namespace groups;
 
-// Blocks an SM, and vectors in flight: registers enough for both pixels' values (three blocks with two vectors: 156 us where this takes 140, with four 142).
-constexpr int kGradientBlocks = 2, kBatch = 4;
+// Blocks an SM: registers enough for both pixels' values.
+constexpr int kGradientBlocks = 2, kGradientSlots = 5;
+using GradientRing = Ring<kGradientSlots, 2, 2>;              // 80 KB
+// Vectors that a thread asks for before it works on the first: from shared memory and from global memory.
+template <typename P> constexpr int kBatch = std::is_same_v<P, InPlace> ? 4 : 2;
 
 // What a thread needs of its channels: z = (x + minus) slope + b, slope = rstd w.
 template <int V> struct Channel {
@@ -31,22 +36,24 @@ template <int V> struct Channel {
 
 // A and B of the channels over the pixels at `src` and `grad`, to part[c] (or null), and to(group, (s1, s2)) by one thread each.  stats(group): the map's.
 // red: red_values() float2; sums: c float2.
-template <typename T, int V, int kAct, typename S, typename F>
-__device__ __forceinline__ void block_sums(const T *src, const T *grad, const Pieces &pieces, const GroupArgs &a, const Lay &lay, S stats, float2 *red, float2 *sums, float2 *part, F to)
+template <typename T, int V, int kAct, typename P, typename S, typename F>
+__device__ __forceinline__ void block_sums(const T *src, const T *grad, P pieces, const GroupArgs &a, const Lay &lay, S stats, float2 *red, float2 *sums, float2 *part, F to)
 {
     const int per_group = a.c / a.groups;
     const bool in_warps = groups_in_warps(lay, per_group);
     for (int b = 0; b < lay.blocks; ++b) {
         Pairs<V> sum_a = {}, sum_b = {};
         const int c = (b * lay.lanes + lay.lane) * V;
-        if (lay.at(b)) {
-            const Channel<V> ch(a, stats, c);
-            const T *const p = src + c, *const q = grad + c;
-            for (int piece = 0; piece < pieces.count(); ++piece) {
-                pieces.wait(piece);
-                Raw<T, V> x[kBatch], dy[kBatch];
-                in_batches<kBatch>(
-                    pieces.first(piece) + lay.row, pieces.end(piece), lay.rows,
+        const bool here = lay.at(b);
+        const Channel<V> ch(a, stats, here ? c : 0);
+        for (int piece = 0; piece < pieces.count(); ++piece) {
+            pieces.wait(piece);
+            if (here) {
+                const T *const p = src + pieces.at(piece) * a.c + c, *const q = grad + pieces.at(piece) * a.c + c;
+                constexpr int kAhead = kBatch<P>;
+                Raw<T, V> x[kAhead], dy[kAhead];
+                in_batches<kAhead>(
+                    lay.row, pieces.end(piece) - pieces.first(piece), lay.rows,
                     [&](int k, int i) {
                         load_raw<V>(x[k], p + i * a.c);
                         load_raw<V>(dy[k], q + i * a.c);
@@ -68,10 +75,11 @@ __device__ __forceinline__ void block_sums(const T *src, const T *grad, const Pi
                         }
                     });
             }
-            // the distances from the mean in units of the deviation
-#pragma unroll
-            for (int j = 0; j < kPairs<V>; ++j) sum_b[j] = mul2(sum_b[j], ch.rstd[j]);
+            pieces.done(piece);
         }
+        // the distances from the mean in units of the deviation
+#pragma unroll
+        for (int j = 0; j < kPairs<V>; ++j) sum_b[j] = mul2(sum_b[j], ch.rstd[j]);
         float fa[2 * kPairs<V>], fb[2 * kPairs<V>];
 #pragma unroll
         for (int k = 0; k < kPairs<V>; ++k) {
@@ -108,13 +116,13 @@ __device__ __forceinline__ void block_sums(const T *src, const T *grad, const Pi
     }
 }
 
-// dx of `pixels` pixels; totals(group) = (s1, s2) / m.
-template <typename T, int V, int kAct, typename S, typename F>
-__device__ __forceinline__ void write_gradients(const T *src, const T *grad, int pixels, long long first, const GroupArgs &a, const Lay &lay, S stats, F totals)
+// dx of the pixels; totals(group) = (s1, s2) / m.
+template <typename T, int V, int kAct, typename P, typename S, typename F>
+__device__ __forceinline__ void write_gradients(const T *src, const T *grad, P pieces, long long first, const GroupArgs &a, const Lay &lay, S stats, F totals)
 {
     for (int b = 0; b < lay.blocks; ++b) {
-        if (!lay.at(b)) continue;
-        const int c = (b * lay.lanes + lay.lane) * V;
+        const bool here = lay.at(b);
+        const int c = here ? (b * lay.lanes + lay.lane) * V : 0;
         const Channel<V> ch(a, stats, c);
         // dx = w rstd dz - rstd s1 - (x - mean) rstd (rstd s2)
         Pairs<V> by_one, by_x;
@@ -124,32 +132,40 @@ __device__ __forceinline__ void write_gradients(const T *src, const T *grad, int
             by_one[j] = mul2(by_one[j], ch.rstd[j]);
             by_x[j] = mul2(mul2(by_x[j], ch.rstd[j]), ch.rstd[j]) ^ kMinus;
         }
-        const T *const p = src + c, *const q = grad + c;
-        T *const to = (T *)a.out + first * a.c + c;
-        Raw<T, V> x[kBatch], dy[kBatch];
-        in_batches<kBatch>(
-            lay.row, pixels, lay.rows,
-            [&](int k, int i) {
-                load_raw<V>(x[k], p + i * a.c);
-                load_raw<V>(dy[k], q + i * a.c);
-            },
-            [&](int k, int i, int second) {
-                Pairs<V> v, w, d, e;
-                pairs_of<V>(x[k], v);
-                pairs_of<V>(x[k + 1], w);
-                pairs_of<V>(dy[k], d);
-                pairs_of<V>(dy[k + 1], e);
+        T *const out = (T *)a.out + first * a.c + c;
+        for (int piece = 0; piece < pieces.count(); ++piece) {
+            pieces.wait(piece);
+            if (here) {
+                const T *const p = src + pieces.at(piece) * a.c + c, *const q = grad + pieces.at(piece) * a.c + c;
+                T *const to = out + pieces.first(piece) * a.c;
+                constexpr int kAhead = kBatch<P>;
+                Raw<T, V> x[kAhead], dy[kAhead];
+                in_batches<kAhead>(
+                    lay.row, pieces.end(piece) - pieces.first(piece), lay.rows,
+                    [&](int k, int i) {
+                        load_raw<V>(x[k], p + i * a.c);
+                        load_raw<V>(dy[k], q + i * a.c);
+                    },
+                    [&](int k, int i, int second) {
+                        Pairs<V> v, w, d, e;
+                        pairs_of<V>(x[k], v);
+                        pairs_of<V>(x[k + 1], w);
+                        pairs_of<V>(dy[k], d);
+                        pairs_of<V>(dy[k + 1], e);
 #pragma unroll
-                for (int j = 0; j < kPairs<V>; ++j) {
-                    v[j] = add2(v[j], ch.minus[j]);
-                    w[j] = add2(w[j], ch.minus[j]);
-                    slope2<kAct>(fma2(v[j], ch.slope[j], ch.b[j]), fma2(w[j], ch.slope[j], ch.b[j]), d[j], e[j]);
-                    v[j] = fma2(d[j], ch.slope[j], fma2(v[j], by_x[j], by_one[j]));
-                    w[j] = fma2(e[j], ch.slope[j], fma2(w[j], by_x[j], by_one[j]));
-                }
-                store_pairs<V>(to + i * a.c, v);
-                if (second >= 0) store_pairs<V>(to + second * a.c, w);
-            });
+                        for (int j = 0; j < kPairs<V>; ++j) {
+                            v[j] = add2(v[j], ch.minus[j]);
+                            w[j] = add2(w[j], ch.minus[j]);
+                            slope2<kAct>(fma2(v[j], ch.slope[j], ch.b[j]), fma2(w[j], ch.slope[j], ch.b[j]), d[j], e[j]);
+                            v[j] = fma2(d[j], ch.slope[j], fma2(v[j], by_x[j], by_one[j]));
+                            w[j] = fma2(e[j], ch.slope[j], fma2(w[j], by_x[j], by_one[j]));
+                        }
+                        store_pairs<V>(to + i * a.c, v);
+                        if (second >= 0) store_pairs<V>(to + second * a.c, w);
+                    });
+            }
+            pieces.done(piece);
+        }
     }
 }
 
@@ -215,7 +231,7 @@ __global__ void __launch_bounds__(512) group_gradient_map_kernel(const __grid_co
     }
     __syncthreads();
     if (a.shares > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    write_gradients<T, V, kAct>(data, grad, pixels, first, a, lay, stats, [&](int g) { return totals[g]; });
+    write_gradients<T, V, kAct>(data, grad, InPlace{pixels}, first, a, lay, stats, [&](int g) { return totals[g]; });
     if (a.shares > 1) {
         __syncwarp();
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");       // the others have read this block's totals
@@ -249,45 +265,64 @@ __global__ void __launch_bounds__(256) group_totals_kernel(const __grid_constant
     if ((threadIdx.x & 31) == 0) a.sums[i] = v;
 }
 
-// part[map][run][channel]: A and B of a run of pixels; runs[map][run][group]: its s1 and s2.  [red: red_values() float2][sums: c float2]
-template <typename T, int V, int kAct>
-__global__ void __launch_bounds__(kRunThreads, kGradientBlocks) group_sums_kernel(const __grid_constant__ GroupArgs a)
+// As the forward pass's: the run's pixels as pieces for work(x, dy, pieces).
+template <typename T, bool kRing, typename F>
+__device__ __forceinline__ void with_run(const GroupArgs &a, const Run &run, const Lay &lay, unsigned char *smem, int ring_size, F work)
+{
+    const T *const x = (const T *)a.x + run.first * a.c, *const dy = (const T *)a.dy + run.first * a.c;
+    if constexpr (kRing) {
+        __shared__ __align__(8) unsigned long long s_ring[2 * kGradientSlots];
+        if (threadIdx.x == 0) GradientRing::init(s_ring);
+        __syncthreads();
+        chain_next();
+        chain_wait();
+        const GradientRing ring(run.pixels, lay.rows, s_ring, a.status);
+        if (threadIdx.x < kRunThreads) work(reinterpret_cast<const T *>(smem), reinterpret_cast<const T *>(smem + ring_size / 2), ring);
+        else if (threadIdx.x == kRunThreads) ring.fill(smem, x, dy, a.c * (int)sizeof(T));
+    } else {
+        chain_next();
+        chain_wait();
+        work(x, dy, InPlace{run.pixels});
+    }
+}
+// part[map][run][channel]: A and B of a run of pixels; runs[map][run][group]: its s1 and s2.  [ring of x][ring of dy][red: red_values() float2][sums: c float2]
+template <typename T, int V, int kAct, bool kRing>
+__global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kGradientBlocks) group_sums_kernel(const __grid_constant__ GroupArgs a, int ring)
 {
     extern __shared__ __align__(128) unsigned char smem[];
-    float2 *const red = reinterpret_cast<float2 *>(smem), *const sums = red + red_values(a.c / V, kRunThreads, V);
-    chain_next();
-    chain_wait();
+    float2 *const red = reinterpret_cast<float2 *>(smem + ring), *const sums = red + red_values(a.c / V, kRunThreads, V);
     const Lay lay(a.c / V, kRunThreads);
     const Run run(a, blockIdx.x);
     auto stats = [&](int g) { return a.stats[run.map * a.groups + g]; };
     float2 *const to = a.runs + (long long)run.index * a.groups;
-    block_sums<T, V, kAct>((const T *)a.x + run.first * a.c, (const T *)a.dy + run.first * a.c, Pieces(run.pixels, lay.rows, nullptr, a.status), a, lay, stats, red, sums,
-                           a.part ? a.part + (long long)run.index * a.c : nullptr, [&](int g, float2 t) { to[g] = t; });
+    with_run<T, kRing>(a, run, lay, smem, ring, [&](const T *x, const T *dy, auto pieces) {
+        block_sums<T, V, kAct>(x, dy, pieces, a, lay, stats, red, sums, a.part ? a.part + (long long)run.index * a.c : nullptr, [&](int g, float2 t) { to[g] = t; });
+    });
 }
 
-// dx, the last runs first: they are the likeliest to be in L2 still.  [totals: groups float2]
-template <typename T, int V, int kAct>
-__global__ void __launch_bounds__(kRunThreads, kGradientBlocks) group_gradients_kernel(const __grid_constant__ GroupArgs a)
+// dx, the last runs first: they are the likeliest to be in L2 still.  [ring of x][ring of dy][totals: groups float2]
+template <typename T, int V, int kAct, bool kRing>
+__global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kGradientBlocks) group_gradients_kernel(const __grid_constant__ GroupArgs a, int ring)
 {
     extern __shared__ __align__(128) unsigned char smem[];
-    float2 *const own = reinterpret_cast<float2 *>(smem);
-    chain_next();
-    chain_wait();
+    float2 *const own = reinterpret_cast<float2 *>(smem + ring);
     const Lay lay(a.c / V, kRunThreads);
     const Run run(a, gridDim.x - 1 - blockIdx.x);
-    if (a.sums)
-        for (int g = threadIdx.x; g < a.groups; g += kRunThreads) own[g] = a.sums[run.map * a.groups + g];
-    else {
-        const Team team(a.shares, kRunThreads);
-        for (int base = 0; base < a.groups; base += team.step) {
-            const int g = base + team.first;
-            const float2 v = join_runs(a, run.map, min(g, a.groups - 1), team.rank, team.size);
-            if (g < a.groups && team.rank == 0) own[g] = v;
+    with_run<T, kRing>(a, run, lay, smem, ring, [&](const T *x, const T *dy, auto pieces) {
+        if (a.sums)
+            for (int g = threadIdx.x; g < a.groups; g += kRunThreads) own[g] = a.sums[run.map * a.groups + g];
+        else {
+            const Team team(a.shares, kRunThreads);
+            for (int base = 0; base < a.groups; base += team.step) {
+                const int g = base + team.first;
+                const float2 v = join_runs(a, run.map, min(g, a.groups - 1), team.rank, team.size);
+                if (g < a.groups && team.rank == 0) own[g] = v;
+            }
         }
-    }
-    __syncthreads();
-    auto stats = [&](int g) { return a.stats[run.map * a.groups + g]; };
-    write_gradients<T, V, kAct>((const T *)a.x + run.first * a.c, (const T *)a.dy + run.first * a.c, run.pixels, run.first, a, lay, stats, [&](int g) { return own[g]; });
+        lay.sync();
+        auto stats = [&](int g) { return a.stats[run.map * a.groups + g]; };
+        write_gradients<T, V, kAct>(x, dy, pieces, run.first, a, lay, stats, [&](int g) { return own[g]; });
+    });
 }
 
 // db and dw: sums over the blocks' A and B, 8 channels a block, in 64 bits (there may be many).
@@ -327,15 +362,18 @@ tc_status launch_map(int device, const GroupArgs &a, int threads, size_t smem, c
     if (!allow_shared<kernel>(device, kMostShared) || !allow_large_clusters<kernel>(device)) return TC_ERR_CUDA;
     return launch_first_cluster(a.shares, kernel, dim3((unsigned int)(a.n * a.shares)), dim3(threads), smem, s, a) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
-template <typename T, int V, int kAct>
+template <typename T, int V, int kAct, bool kRing>
 tc_status launch_runs(int device, const GroupArgs &a, cudaStream_t s)
 {
-    const size_t first = 8 * (size_t)red_values(a.c / V, kRunThreads, V) + 8 * (size_t)a.c, last = 8 * (size_t)a.groups;
-    if (!allow_shared<group_sums_kernel<T, V, kAct>>(device, kMostShared) || !allow_shared<group_gradients_kernel<T, V, kAct>>(device, kMostShared)) return TC_ERR_CUDA;
-    const dim3 grid((unsigned int)(a.n * a.shares)), block(kRunThreads);
-    if (launch_first(true, group_sums_kernel<T, V, kAct>, grid, block, first, s, a) != cudaSuccess) return TC_ERR_CUDA;
+    constexpr auto sums = group_sums_kernel<T, V, kAct, kRing>;
+    constexpr auto gradients = group_gradients_kernel<T, V, kAct, kRing>;
+    const size_t ring = kRing ? ring_bytes<GradientRing>(a.c / V) : 0;
+    const size_t first = ring + 8 * (size_t)red_values(a.c / V, kRunThreads, V) + 8 * (size_t)a.c, last = ring + 8 * (size_t)a.groups;
+    if (!allow_shared<sums>(device, kMostShared) || !allow_shared<gradients>(device, kMostShared)) return TC_ERR_CUDA;
+    const dim3 grid((unsigned int)(a.n * a.shares)), block(kRing ? kRunThreads + 32 : kRunThreads);
+    if (launch_first(true, sums, grid, block, first, s, a, (int)ring) != cudaSuccess) return TC_ERR_CUDA;
     if (a.sums && launch_chained(true, group_totals_kernel, dim3((unsigned int)((a.n * a.groups + 7) / 8)), dim3(256), 0, s, a) != cudaSuccess) return TC_ERR_CUDA;
-    return launch_chained(true, group_gradients_kernel<T, V, kAct>, grid, block, last, s, a) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
+    return launch_chained(true, gradients, grid, block, last, s, a, (int)ring) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
 
 template <typename T, int V>
@@ -344,9 +382,11 @@ tc_status launch(int device, const GroupArgs &a, const GroupPlan &p, int act, cu
     // (maps of single values never lie in shared memory: bulk copies begin at 16 bytes)
 #define TC_GRADIENT(kAct) \
     do { \
-        if constexpr (V > 1) \
+        if constexpr (V > 1) { \
             if (p.shared) return launch_map<T, V, kAct>(device, a, p.threads, p.shared, s); \
-        return launch_runs<T, V, kAct>(device, a, s); \
+            if (ring_takes(a.c, V)) return launch_runs<T, V, kAct, true>(device, a, s); \
+        } \
+        return launch_runs<T, V, kAct, false>(device, a, s); \
     } while (0)
     if (act == kRelu) TC_GRADIENT(kRelu);
     if (act == kSilu) TC_GRADIENT(kSilu);
