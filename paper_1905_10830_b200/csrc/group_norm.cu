@@ -17,15 +17,15 @@ using namespace groups;
 using rowcodes::Coder;
 
 constexpr int kBatch = 4;
-constexpr int kNormSlots = 3;
-using NormRing = Ring<kNormSlots, 4, 1>;                      // 48 KB, three blocks an SM
+using NormRing = Ring<2, 8, 1>;                               // 64 KB
+constexpr int kNormBlocks = 3;                                // an SM
 
 // Mean and M2 (sum of squares about it) of each group over the pixels at `src`, in one pass: sums of the distances d of a channel's values from the
 // first pixel's, p, and of their squares; the channel's mean is m = p + sum d / n, its squares about that sum d^2 - (sum d)^2 / n.  p being one of the n
 // values, (p - m)^2 is at most n times the mean square distance: the difference loses no more than a factor of n.
 // to(group, (mean, M2)) by one thread each.  red: red_values() float2; channels: c float2 of (p, ), then (m, squares).
 template <typename T, int V, typename P, typename F>
-__device__ __forceinline__ void block_moments(const T *src, P pieces, const GroupArgs &a, const Lay &lay, float2 *red, float2 *channels, F to)
+__device__ __forceinline__ void block_moments(const T *src, P &pieces, const GroupArgs &a, const Lay &lay, float2 *red, float2 *channels, F to)
 {
     const int per_group = a.c / a.groups, pixels = pieces.pixels;
     const float per_pixel = 1.0f / (float)pixels, per_channel = 1.0f / (float)per_group, n = (float)pixels;
@@ -125,7 +125,7 @@ template <int V> struct Affine {
 };
 // The values of the pixels at `src`, the first of them pixel `first` of the tensor.
 template <typename T, int V, int kAct, typename P, typename F>
-__device__ __forceinline__ void write_values(const T *src, P pieces, long long first, const GroupArgs &a, const Lay &lay, F stats)
+__device__ __forceinline__ void write_values(const T *src, P &pieces, long long first, const GroupArgs &a, const Lay &lay, F stats)
 {
     for (int b = 0; b < lay.blocks; ++b) {
         const bool here = lay.at(b);
@@ -160,7 +160,7 @@ __device__ __forceinline__ void write_values(const T *src, P pieces, long long f
 
 // The same as codes, and as values too where they are wanted: a team of lanes a pixel, its largest magnitude first.  `table`: [3][c] floats of shared memory.
 template <typename T, int V, int kAct, typename P, typename F>
-__device__ __forceinline__ void write_codes(const T *src, P pieces, long long first, const GroupArgs &a, const Lay &lay, F stats, float *table)
+__device__ __forceinline__ void write_codes(const T *src, P &pieces, long long first, const GroupArgs &a, const Lay &lay, F stats, float *table)
 {
     const int per_group = a.c / a.groups;
     lay.sync();                                               // the last table's readers
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(512, 2) group_norm_map_kernel(const __grid_con
     const int p0 = rank * a.share, pixels = max(0, min(a.share, a.hw - p0)), per_group = a.c / a.groups;
     const long long first = map * a.hw + p0;
     const Lay lay(a.c / V, blockDim.x);
-    const Pieces pieces(pixels, lay.rows, s_full, a.status);
+    Pieces pieces(pixels, lay.rows, s_full, a.status);
     if (threadIdx.x == 0) {
         const char *const src = (const char *)((const T *)a.x + first * a.c);
         const uint32_t row = (uint32_t)a.c * sizeof(T);
@@ -290,8 +290,9 @@ __global__ void __launch_bounds__(512, 2) group_norm_map_kernel(const __grid_con
     __syncthreads();
     if (a.shares > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     auto of = [&](int g) { return stats[g]; };
-    if constexpr (kCodes) write_codes<T, V, kAct>(data, InPlace{pixels}, first, a, lay, of, reinterpret_cast<float *>(table));
-    else write_values<T, V, kAct>(data, InPlace{pixels}, first, a, lay, of);
+    InPlace all{pixels};
+    if constexpr (kCodes) write_codes<T, V, kAct>(data, all, first, a, lay, of, reinterpret_cast<float *>(table));
+    else write_values<T, V, kAct>(data, all, first, a, lay, of);
     if (a.shares > 1) {
         __syncwarp();
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");       // the others have read this block's moments
@@ -332,47 +333,29 @@ __global__ void __launch_bounds__(256) group_join_kernel(const __grid_constant__
     if (a.stats) a.stats[i] = v;
 }
 
-// What a kernel on runs begins with: its pixels as pieces, at `src`, for work(src, pieces).  A ring's lies first in shared memory, and threads behind kRunThreads fill it.
-template <typename T, bool kRing, typename F>
-__device__ __forceinline__ void with_run(const GroupArgs &a, const Run &run, const Lay &lay, unsigned char *smem, F work)
-{
-    const T *const src = (const T *)a.x + run.first * a.c;
-    if constexpr (kRing) {
-        __shared__ __align__(8) unsigned long long s_ring[2 * kNormSlots];
-        if (threadIdx.x == 0) NormRing::init(s_ring);
-        __syncthreads();
-        chain_next();
-        chain_wait();
-        const NormRing ring(run.pixels, lay.rows, s_ring, a.status);
-        if (threadIdx.x < kRunThreads) work(reinterpret_cast<const T *>(smem), ring);
-        else if (threadIdx.x == kRunThreads) ring.fill(smem, src, nullptr, a.c * (int)sizeof(T));
-    } else {
-        chain_next();
-        chain_wait();
-        work(src, InPlace{run.pixels});
-    }
-}
 // part[map][run][group]: moments of a run of pixels.  [ring][red: red_values() float2][channels: c float2]
 template <typename T, int V, bool kRing>
-__global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kRing ? 3 : 4) group_moments_kernel(const __grid_constant__ GroupArgs a, int ring)
+__global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kRing ? kNormBlocks : 4) group_moments_kernel(const __grid_constant__ GroupArgs a, int ring_size)
 {
     extern __shared__ __align__(128) unsigned char smem[];
-    float2 *const red = reinterpret_cast<float2 *>(smem + ring), *const channels = red + red_values(a.c / V, kRunThreads, V);
+    float2 *const red = reinterpret_cast<float2 *>(smem + ring_size), *const channels = red + red_values(a.c / V, kRunThreads, V);
     const Lay lay(a.c / V, kRunThreads);
     const Run run(a, blockIdx.x);
     float2 *const part = a.part + (long long)run.index * a.groups;
-    with_run<T, kRing>(a, run, lay, smem, [&](const T *src, auto pieces) { block_moments<T, V>(src, pieces, a, lay, red, channels, [&](int g, float2 m) { part[g] = m; }); });
+    with_run<T, NormRing, kRing>(a, run, lay, smem, ring_size, [&](const T *src, const T *, auto &pieces) {
+        block_moments<T, V>(src, pieces, a, lay, red, channels, [&](int g, float2 m) { part[g] = m; });
+    });
 }
 
 // The values, the last runs first: they are the likeliest to be in L2 still.  [ring][stats: groups float2][table of the codes: 3 c floats]
 template <typename T, int V, int kAct, bool kCodes, bool kRing>
-__global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kRing ? 3 : 4) group_values_kernel(const __grid_constant__ GroupArgs a, int ring)
+__global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kRing ? kNormBlocks : 4) group_values_kernel(const __grid_constant__ GroupArgs a, int ring_size)
 {
     extern __shared__ __align__(128) unsigned char smem[];
-    float2 *const own = reinterpret_cast<float2 *>(smem + ring);
+    float2 *const own = reinterpret_cast<float2 *>(smem + ring_size);
     const Lay lay(a.c / V, kRunThreads);
     const Run run(a, gridDim.x - 1 - blockIdx.x);
-    with_run<T, kRing>(a, run, lay, smem, [&](const T *src, auto pieces) {
+    with_run<T, NormRing, kRing>(a, run, lay, smem, ring_size, [&](const T *src, const T *, auto &pieces) {
         if (a.sums)
             for (int g = threadIdx.x; g < a.groups; g += kRunThreads) own[g] = a.sums[run.map * a.groups + g];
         else {
@@ -450,13 +433,31 @@ int tc_group_threads(int columns)
     return best;
 }
 
-// Runs of pixels (of `row` bytes in each of `tensors`) of a map.
-void cut_runs(GroupPlan &p, long long n, int hw, long long row, int tensors, int sm_count)
+void cut_runs(GroupPlan &p, long long n, int hw, long long row, int tensors, int ring_blocks, int sm_count)
 {
-    // of eight pixels at least where their channels' sums are written too; shorter than kRunBytes where SMs would be idle
-    long long share = std::max(tensors > 1 ? 8ll : 1ll, kRunBytes / (row * tensors));
-    while (share > 1 && n * ((hw + share - 1) / share) < 2ll * sm_count) share = (share + 1) / 2;
-    share = std::max(share, ((long long)hw * n + (1ll << 29) - 1) >> 29);
+    // in all 2^29 runs at most
+    const long long least = std::max(((long long)hw * n + (1ll << 29) - 1) >> 29, 1ll);
+    long long share;
+    if (ring_blocks) {
+        // So many that the blocks' work is least: a run costs as much as kRunCost more of each tensor, and the last ones leave half of the blocks idle.  (Fitted: 128x56x56 x 128 bf16,
+        // gradient, in runs of 128, 242, 349, 448 and 628 pixels: 176, 134, 117, 121 and 118 us; 256x56x56 x 128 forward, 126, 349 and 628: 120, 104 and 108.)
+        const double blocks = (double)ring_blocks * sm_count;
+        const long long shortest = std::max(least, kRunLeast / (row * tensors));
+        double best_cost = 0.0;
+        share = 0;
+        for (long long runs = 1, more; runs <= hw; runs += more) {
+            more = std::max(1ll, runs / 8);
+            const long long of = std::max(shortest, (hw + runs - 1) / runs);
+            const double cost = ((double)n * ((hw + of - 1) / of) / blocks + 0.5) * (double)((of * row + kRunCost) * tensors);
+            if (!share || cost < best_cost) { share = of; best_cost = cost; }
+            if (of == shortest) break;
+        }
+    } else {
+        // of eight pixels at least where their channels' sums are written too; shorter than kRunBytes where SMs would be idle
+        share = std::max(tensors > 1 ? 8ll : 1ll, kRunBytes / (row * tensors));
+        while (share > 1 && n * ((hw + share - 1) / share) < 2ll * sm_count) share = (share + 1) / 2;
+        share = std::max(share, least);
+    }
     const long long runs = (hw + std::min<long long>(share, hw) - 1) / std::min<long long>(share, hw);
     p.share = (int)((hw + runs - 1) / runs);                  // (of one size but for the last)
     p.shares = (hw + p.share - 1) / p.share;
@@ -482,7 +483,7 @@ GroupPlan tc_plan_group_norm(const GroupNormArgs &m, int sm_count)
             return p;
         }
     }
-    cut_runs(p, m.n, m.hw, (long long)m.c * element, 1, sm_count);
+    cut_runs(p, m.n, m.hw, (long long)m.c * element, 1, ring_takes(m.c, p.vector) ? kNormBlocks : 0, sm_count);
     p.workspace = (size_t)m.n * m.groups * sizeof(float2) * (p.shares + (p.join ? 1 : 0));
     return p;
 }

@@ -297,12 +297,13 @@ struct Pieces {
     }
     __device__ __forceinline__ void done(int) const {}
 };
-// Of a run that is longer than its block's shared memory: pieces of kRounds rounds of the rows through a ring of kSlots, that a warp of its own fills by bulk copies.  Loads of a block's
-// threads keep too little on its way (128x56x56 x 128 bf16, gradient of silu: 143 us, ring 104; 256x56x56 x 128, forward: 114 and 95).
-template <int kSlots, int kRounds, int kTensors>
+// Of a run that is longer than its block's shared memory: pieces of kRounds rounds of the rows through a ring of kSlots, that a warp of its own fills by bulk copies.  Loads of the threads
+// keep too little on its way (gradient of silu, 128x56x56 x 128 bf16: 143 us, ring 117; 256x56x56 x 128 forward 114 and 104).  Few long pieces: more and shorter ones, of the
+// same bytes, cost more waits than their earlier refills are worth (125 and 106).
+template <int kSlots_, int kRounds, int kTensors>
 struct Ring {
-    static constexpr int kRows = kTensors * kSlots * kRounds;
-    int pixels, each;
+    static constexpr int kSlots = kSlots_, kRows = kTensors * kSlots * kRounds;
+    int pixels, each;                 // of the run; of a piece
     unsigned long long *full, *empty;
     unsigned int *status;
     bool lost;
@@ -375,6 +376,29 @@ struct Run {
         first = map * a.hw + run * a.share;
     }
 };
+
+// What a kernel on runs does: work(x, dy, pieces) on its block's run, by the threads up to kRunThreads.  With a ring a block has a warp more, and the ring lies first in shared memory, x's
+// and then dy's.
+template <typename T, typename R, bool kRing, typename F>
+__device__ __forceinline__ void with_run(const GroupArgs &a, const Run &run, const Lay &lay, unsigned char *smem, int ring_size, F work)
+{
+    const T *const x = (const T *)a.x + run.first * a.c, *const dy = a.dy ? (const T *)a.dy + run.first * a.c : nullptr;
+    if constexpr (kRing) {
+        __shared__ __align__(8) unsigned long long s_ring[2 * R::kSlots];
+        if (threadIdx.x == 0) R::init(s_ring);
+        __syncthreads();
+        chain_next();
+        chain_wait();
+        R ring(run.pixels, lay.rows, s_ring, a.status);
+        if (threadIdx.x < kRunThreads) work(reinterpret_cast<const T *>(smem), reinterpret_cast<const T *>(smem + ring_size / 2), ring);
+        else if (threadIdx.x == kRunThreads) ring.fill(smem, x, dy, a.c * (int)sizeof(T));
+    } else {
+        chain_next();
+        chain_wait();
+        InPlace pieces{run.pixels};
+        work(x, dy, pieces);
+    }
+}
 
 // Room that channel_sums takes: of the lower half of the rows.
 __host__ __device__ inline int red_values(int columns, int threads, int v)
@@ -476,4 +500,5 @@ int shares_on_chip(long long n, int hw, long long most, int sm_count, F bytes)
     }
     return 0;
 }
-void cut_runs(GroupPlan &p, long long n, int hw, long long row, int tensors, int sm_count);
+// Runs of pixels (of `row` bytes in each of `tensors`) of a map; ring_blocks: blocks of an SM that take them through rings, 0: none do.
+void cut_runs(GroupPlan &p, long long n, int hw, long long row, int tensors, int ring_blocks, int sm_count);

@@ -15,8 +15,8 @@ namespace {
 using namespace groups;
 
 // Blocks an SM: registers enough for both pixels' values.
-constexpr int kGradientBlocks = 2, kGradientSlots = 5;
-using GradientRing = Ring<kGradientSlots, 2, 2>;              // 80 KB
+constexpr int kGradientBlocks = 2;
+using GradientRing = Ring<2, 4, 2>;                           // 64 KB
 // Vectors that a thread asks for before it works on the first: from shared memory and from global memory.
 template <typename P> constexpr int kBatch = std::is_same_v<P, InPlace> ? 4 : 2;
 
@@ -37,7 +37,7 @@ template <int V> struct Channel {
 // A and B of the channels over the pixels at `src` and `grad`, to part[c] (or null), and to(group, (s1, s2)) by one thread each.  stats(group): the map's.
 // red: red_values() float2; sums: c float2.
 template <typename T, int V, int kAct, typename P, typename S, typename F>
-__device__ __forceinline__ void block_sums(const T *src, const T *grad, P pieces, const GroupArgs &a, const Lay &lay, S stats, float2 *red, float2 *sums, float2 *part, F to)
+__device__ __forceinline__ void block_sums(const T *src, const T *grad, P &pieces, const GroupArgs &a, const Lay &lay, S stats, float2 *red, float2 *sums, float2 *part, F to)
 {
     const int per_group = a.c / a.groups;
     const bool in_warps = groups_in_warps(lay, per_group);
@@ -118,7 +118,7 @@ __device__ __forceinline__ void block_sums(const T *src, const T *grad, P pieces
 
 // dx of the pixels; totals(group) = (s1, s2) / m.
 template <typename T, int V, int kAct, typename P, typename S, typename F>
-__device__ __forceinline__ void write_gradients(const T *src, const T *grad, P pieces, long long first, const GroupArgs &a, const Lay &lay, S stats, F totals)
+__device__ __forceinline__ void write_gradients(const T *src, const T *grad, P &pieces, long long first, const GroupArgs &a, const Lay &lay, S stats, F totals)
 {
     for (int b = 0; b < lay.blocks; ++b) {
         const bool here = lay.at(b);
@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(512) group_gradient_map_kernel(const __grid_co
     const int p0 = rank * a.share, pixels = max(0, min(a.share, a.hw - p0)), per_group = a.c / a.groups;
     const long long first = map * a.hw + p0;
     const Lay lay(a.c / V, blockDim.x);
-    const Pieces pieces(pixels, lay.rows, s_full, a.status);
+    Pieces pieces(pixels, lay.rows, s_full, a.status);
     if (threadIdx.x == 0) {
         const char *const src = (const char *)((const T *)a.x + first * a.c), *const dy = (const char *)((const T *)a.dy + first * a.c);
         const uint32_t row = (uint32_t)a.c * sizeof(T);
@@ -231,7 +231,8 @@ __global__ void __launch_bounds__(512) group_gradient_map_kernel(const __grid_co
     }
     __syncthreads();
     if (a.shares > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    write_gradients<T, V, kAct>(data, grad, InPlace{pixels}, first, a, lay, stats, [&](int g) { return totals[g]; });
+    InPlace all{pixels};
+    write_gradients<T, V, kAct>(data, grad, all, first, a, lay, stats, [&](int g) { return totals[g]; });
     if (a.shares > 1) {
         __syncwarp();
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");       // the others have read this block's totals
@@ -265,50 +266,30 @@ __global__ void __launch_bounds__(256) group_totals_kernel(const __grid_constant
     if ((threadIdx.x & 31) == 0) a.sums[i] = v;
 }
 
-// As the forward pass's: the run's pixels as pieces for work(x, dy, pieces).
-template <typename T, bool kRing, typename F>
-__device__ __forceinline__ void with_run(const GroupArgs &a, const Run &run, const Lay &lay, unsigned char *smem, int ring_size, F work)
-{
-    const T *const x = (const T *)a.x + run.first * a.c, *const dy = (const T *)a.dy + run.first * a.c;
-    if constexpr (kRing) {
-        __shared__ __align__(8) unsigned long long s_ring[2 * kGradientSlots];
-        if (threadIdx.x == 0) GradientRing::init(s_ring);
-        __syncthreads();
-        chain_next();
-        chain_wait();
-        const GradientRing ring(run.pixels, lay.rows, s_ring, a.status);
-        if (threadIdx.x < kRunThreads) work(reinterpret_cast<const T *>(smem), reinterpret_cast<const T *>(smem + ring_size / 2), ring);
-        else if (threadIdx.x == kRunThreads) ring.fill(smem, x, dy, a.c * (int)sizeof(T));
-    } else {
-        chain_next();
-        chain_wait();
-        work(x, dy, InPlace{run.pixels});
-    }
-}
 // part[map][run][channel]: A and B of a run of pixels; runs[map][run][group]: its s1 and s2.  [ring of x][ring of dy][red: red_values() float2][sums: c float2]
 template <typename T, int V, int kAct, bool kRing>
-__global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kGradientBlocks) group_sums_kernel(const __grid_constant__ GroupArgs a, int ring)
+__global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kGradientBlocks) group_sums_kernel(const __grid_constant__ GroupArgs a, int ring_size)
 {
     extern __shared__ __align__(128) unsigned char smem[];
-    float2 *const red = reinterpret_cast<float2 *>(smem + ring), *const sums = red + red_values(a.c / V, kRunThreads, V);
+    float2 *const red = reinterpret_cast<float2 *>(smem + ring_size), *const sums = red + red_values(a.c / V, kRunThreads, V);
     const Lay lay(a.c / V, kRunThreads);
     const Run run(a, blockIdx.x);
     auto stats = [&](int g) { return a.stats[run.map * a.groups + g]; };
     float2 *const to = a.runs + (long long)run.index * a.groups;
-    with_run<T, kRing>(a, run, lay, smem, ring, [&](const T *x, const T *dy, auto pieces) {
+    with_run<T, GradientRing, kRing>(a, run, lay, smem, ring_size, [&](const T *x, const T *dy, auto &pieces) {
         block_sums<T, V, kAct>(x, dy, pieces, a, lay, stats, red, sums, a.part ? a.part + (long long)run.index * a.c : nullptr, [&](int g, float2 t) { to[g] = t; });
     });
 }
 
 // dx, the last runs first: they are the likeliest to be in L2 still.  [ring of x][ring of dy][totals: groups float2]
 template <typename T, int V, int kAct, bool kRing>
-__global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kGradientBlocks) group_gradients_kernel(const __grid_constant__ GroupArgs a, int ring)
+__global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kGradientBlocks) group_gradients_kernel(const __grid_constant__ GroupArgs a, int ring_size)
 {
     extern __shared__ __align__(128) unsigned char smem[];
-    float2 *const own = reinterpret_cast<float2 *>(smem + ring);
+    float2 *const own = reinterpret_cast<float2 *>(smem + ring_size);
     const Lay lay(a.c / V, kRunThreads);
     const Run run(a, gridDim.x - 1 - blockIdx.x);
-    with_run<T, kRing>(a, run, lay, smem, ring, [&](const T *x, const T *dy, auto pieces) {
+    with_run<T, GradientRing, kRing>(a, run, lay, smem, ring_size, [&](const T *x, const T *dy, auto &pieces) {
         if (a.sums)
             for (int g = threadIdx.x; g < a.groups; g += kRunThreads) own[g] = a.sums[run.map * a.groups + g];
         else {
@@ -320,8 +301,7 @@ __global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kGradi
             }
         }
         lay.sync();
-        auto stats = [&](int g) { return a.stats[run.map * a.groups + g]; };
-        write_gradients<T, V, kAct>(x, dy, pieces, run.first, a, lay, stats, [&](int g) { return own[g]; });
+        write_gradients<T, V, kAct>(x, dy, pieces, run.first, a, lay, [&](int g) { return a.stats[run.map * a.groups + g]; }, [&](int g) { return own[g]; });
     });
 }
 
@@ -417,7 +397,7 @@ GroupPlan tc_plan_group_norm_backward(const GroupGradArgs &m, int sm_count)
             return p;
         }
     }
-    cut_runs(p, m.n, m.hw, (long long)m.c * element, 2, sm_count);
+    cut_runs(p, m.n, m.hw, (long long)m.c * element, 2, ring_takes(m.c, p.vector) ? kGradientBlocks : 0, sm_count);
     p.workspace = ((vectors ? (size_t)m.n * p.shares * m.c : 0) + (size_t)m.n * m.groups * (p.shares + (p.join ? 1 : 0))) * sizeof(float2);
     return p;
 }
