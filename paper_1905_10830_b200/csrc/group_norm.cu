@@ -445,7 +445,8 @@ void cut_runs(GroupPlan &p, long long n, int hw, long long row, int tensors, int
         const long long shortest = std::max(least, kRunLeast / (row * tensors));
         double best_cost = 0.0;
         share = 0;
-        for (long long runs = 1, more; runs <= hw; runs += more) {
+        // (from as few on as keep a thread's sums short)
+        for (long long runs = (hw * row + kRunMost - 1) / kRunMost, more; runs <= hw; runs += more) {
             more = std::max(1ll, runs / 8);
             const long long of = std::max(shortest, (hw + runs - 1) / runs);
             const double cost = ((double)n * ((hw + of - 1) / of) / blocks + 0.5) * (double)((of * row + kRunCost) * tensors);

@@ -428,7 +428,7 @@ struct GroupPlan {
     bool join = false;                // runs' sums are joined by a kernel of their own
     size_t shared = 0, workspace = 0;
 };
-constexpr long long kRunBytes = 192 * 1024, kRunLeast = 8 * 1024, kRunCost = 32 * 1024;
+constexpr long long kRunBytes = 192 * 1024, kRunLeast = 8 * 1024, kRunMost = 512 * 1024, kRunCost = 32 * 1024;
 constexpr int kInlineRuns = 64;                 // of a map, whose sums every run's block joins
 int tc_group_threads(int columns);
 GroupPlan tc_plan_group_norm(const GroupNormArgs &a, int sm_count);

@@ -7,6 +7,7 @@ import torch
 
 import paper_1905_10830_b200 as tc
 from tests import plain_group_norm as plain
+from tests.test_gpu_group_norm import _check_backward, _check_forward, _maps, _vectors
 from tests.test_gpu_early_launch import late_copy  # noqa: F401
 from tests.test_gpu_layer_calls import TURNS, _room, _untouched
 from tests.test_gpu_rows import _operand, _plain_codes, _same, _want
@@ -89,6 +90,24 @@ def test_norms_of_late_inputs(ctx, late_copy, shape, groups):  # noqa: F811
     _, stats = tc.tc_group_norm(ctx, x, groups, weight=w, bias=w)
     _late(late_copy, make, lambda dy: tc.tc_group_norm_backward(ctx, x, dy, stats, weight=w, bias=w, activation="silu"))
     _late(late_copy, lambda i: stats * (1 + i), lambda st: tc.tc_group_norm_backward(ctx, x, x, st, weight=w, bias=w))
+
+
+# Maps whose runs go through rings: threads that are left over, rows of as many vectors as threads and of one more (no ring), pieces that end inside the last round, codes by teams that share pixels
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shape,groups", [((30, 144, 50, 50), 12), ((200, 520, 19, 21), 65), ((40, 1024, 30, 31), 32), ((20, 1028, 33, 33), 4), ((9, 2048, 41, 41), 32), ((9, 2056, 41, 41), 8),
+                                          ((300, 8, 101, 100), 4), ((1, 24, 700, 700), 3)])
+def test_long_maps(ctx, shape, groups, dtype):
+    x, dy = _maps(shape, sum(shape), dtype), _maps(shape, 7, dtype, 0.1)
+    w, b = _vectors(shape[1], 3)
+    got = tc.tc_group_norm(ctx, x, groups, weight=w, bias=b, activation="silu")
+    (y, codes), stats = tc.tc_group_norm(ctx, x, groups, weight=w, bias=b, activation="silu", codes="both")
+    assert torch.equal(y, got[0]) and torch.equal(stats, got[1])
+    _check_forward(got, x, groups, w, b, 1e-5, "silu")
+    _check_forward((codes, stats), x, groups, w, b, 1e-5, "silu")
+    g = tc.tc_group_norm_backward(ctx, x, dy, stats, weight=w, bias=b, activation="silu")
+    _check_backward(g, x, dy, stats, groups, w, b, "silu")
+    again = tc.tc_group_norm_backward(ctx, x, dy, stats, weight=w, bias=b, activation="silu")
+    assert all(torch.equal(p, q) for p, q in zip(g, again))
 
 
 @pytest.mark.parametrize("n", [1000, 3_000_000])
