@@ -311,8 +311,8 @@ __global__ void __launch_bounds__(kVectorThreads) group_vectors_kernel(const __g
 {
     chain_next();
     chain_wait();
-    __shared__ double2 s_sum[kVectorThreads];
-    const int c = blockIdx.x * kVectorChannels + (threadIdx.x & (kVectorChannels - 1));
+    __shared__ double2 s_sum[kVectorChannels][kVectorThreads / 32 + 1];
+    const int c = blockIdx.x * kVectorChannels + (threadIdx.x & (kVectorChannels - 1)), warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     double2 s = make_double2(0.0, 0.0);
     if (c < a.c)
 #pragma unroll 8
@@ -321,18 +321,23 @@ __global__ void __launch_bounds__(kVectorThreads) group_vectors_kernel(const __g
             s.x += t.x;
             s.y += t.y;
         }
-    s_sum[threadIdx.x] = s;
-    for (int d = kVectorThreads / 2; d >= kVectorChannels; d >>= 1) {
-        __syncthreads();
-        if (threadIdx.x < d) {
-            s.x += s_sum[threadIdx.x + d].x;
-            s.y += s_sum[threadIdx.x + d].y;
-            s_sum[threadIdx.x] = s;
+    auto over_lanes = [&](int least) {
+        for (int d = 16; d >= least; d >>= 1) {
+            s.x += __shfl_xor_sync(0xffffffffu, s.x, d);
+            s.y += __shfl_xor_sync(0xffffffffu, s.y, d);
         }
-    }
-    if (threadIdx.x >= kVectorChannels || c >= a.c) return;
-    if (a.dbias) a.dbias[c] = (float)s.x;
-    if (a.dweight) a.dweight[c] = (float)s.y;
+    };
+    over_lanes(kVectorChannels);
+    if (lane < kVectorChannels) s_sum[lane][warp] = s;
+    __syncthreads();
+    // a channel's 32 warps' sums: a warp each
+    const int mine = blockIdx.x * kVectorChannels + warp;
+    if (warp >= kVectorChannels || mine >= a.c) return;
+    s = s_sum[warp][lane];
+    over_lanes(1);
+    if (lane) return;
+    if (a.dbias) a.dbias[mine] = (float)s.x;
+    if (a.dweight) a.dweight[mine] = (float)s.y;
 }
 
 template <typename T, int V, int kAct>
