@@ -16,7 +16,6 @@ namespace {
 using namespace groups;
 using rowcodes::Coder;
 
-constexpr int kBatch = 4;
 using NormRing = Ring<2, 8, 1>;                               // 64 KB
 constexpr int kNormBlocks = 3;                                // an SM
 
@@ -51,8 +50,8 @@ __device__ __forceinline__ void block_moments(const T *src, P &pieces, const Gro
                         from[k] ^= kMinus;
                     }
                 }
-                Raw<T, V> raw[kBatch];
-                in_batches<kBatch>(
+                Raw<T, V> raw[kAhead<V>];
+                in_batches<kAhead<V>>(
                     lay.row, pieces.end(piece) - pieces.first(piece), lay.rows, [&](int k, int i) { load_raw<V>(raw[k], p + i * a.c); },
                     [&](int k, int, int second) {
                         for (int h = 0; h < (second < 0 ? 1 : 2); ++h) {
@@ -137,8 +136,8 @@ __device__ __forceinline__ void write_values(const T *src, P &pieces, long long 
             if (here) {
                 const T *const p = src + pieces.at(piece) * a.c + c;
                 T *const q = to + pieces.first(piece) * a.c;
-                Raw<T, V> raw[kBatch];
-                in_batches<kBatch>(
+                Raw<T, V> raw[kAhead<V>];
+                in_batches<kAhead<V>>(
                     lay.row, pieces.end(piece) - pieces.first(piece), lay.rows, [&](int k, int i) { load_raw<V>(raw[k], p + i * a.c); },
                     [&](int k, int i, int second) {
                         Pairs<V> v, w;
@@ -218,7 +217,10 @@ __device__ __forceinline__ void write_codes(const T *src, P &pieces, long long f
                 for (int k = 0; k < kPairs<V>; ++k) halves(v[k], f[2 * k], f[2 * k + 1]);
                 if constexpr (V == 8) *reinterpret_cast<uint2 *>(to + c) = make_uint2(rowcodes::codes_of4(f, coder), rowcodes::codes_of4(f + 4, coder));
                 else if constexpr (V == 4) *reinterpret_cast<uint32_t *>(to + c) = rowcodes::codes_of4(f, coder);
-                else to[c] = rowcodes::code_of(f[0], coder);
+                else if constexpr (V == 2) {
+                    const float two[4] = {f[0], f[1], 0.f, 0.f};
+                    *reinterpret_cast<uint16_t *>(to + c) = (uint16_t)rowcodes::codes_of4(two, coder);
+                } else to[c] = rowcodes::code_of(f[0], coder);
             }
         }
         pieces.done(piece);
@@ -400,12 +402,12 @@ tc_status launch_runs(int device, const GroupArgs &a, cudaStream_t s)
 template <typename T, int V>
 tc_status launch(int device, const GroupArgs &a, const GroupPlan &p, int act, cudaStream_t s)
 {
-    // (maps of single values never lie in shared memory: bulk copies begin at 16 bytes)
+    // (maps of other vectors never lie in shared memory: bulk copies begin at 16 bytes)
 #define TC_NORM(kAct, kCodes) \
     do { \
-        if constexpr (V > 1) { \
+        if constexpr (V * sizeof(T) == 16) { \
             if (p.shared) return launch_map<T, V, kAct, kCodes>(device, a, p.threads, p.shared, s); \
-            if (ring_takes(a.c, V)) return launch_runs<T, V, kAct, kCodes, true>(device, a, s); \
+            if (ring_takes(a.c, V, sizeof(T))) return launch_runs<T, V, kAct, kCodes, true>(device, a, s); \
         } \
         return launch_runs<T, V, kAct, kCodes, false>(device, a, s); \
     } while (0)
@@ -469,13 +471,13 @@ GroupPlan tc_plan_group_norm(const GroupNormArgs &m, int sm_count)
 {
     GroupPlan p;
     const int element = m.dtype == TC_BF16 ? 2 : 4;
-    p.vector = m.c * element % 16 == 0 && m.aligned ? 16 / element : 1;
+    p.vector = vector_of(m.c, element, m.aligned);
     p.threads = tc_group_threads(m.c / p.vector);
     GroupArgs a{};
     a.c = m.c;
     a.groups = m.groups;
     auto bytes = [&](int shares) { return shared_bytes(a, (m.hw + shares - 1) / shares, element, p.vector, p.threads); };
-    if (p.vector > 1) {
+    if (p.vector * element == 16) {
         const int shares = shares_on_chip(m.n, m.hw, 2ll * sm_count, sm_count, bytes);
         if (shares) {
             p.shares = shares;
@@ -484,7 +486,7 @@ GroupPlan tc_plan_group_norm(const GroupNormArgs &m, int sm_count)
             return p;
         }
     }
-    cut_runs(p, m.n, m.hw, (long long)m.c * element, 1, ring_takes(m.c, p.vector) ? kNormBlocks : 0, sm_count);
+    cut_runs(p, m.n, m.hw, (long long)m.c * element, 1, ring_takes(m.c, p.vector, element) ? kNormBlocks : 0, sm_count);
     p.workspace = (size_t)m.n * m.groups * sizeof(float2) * (p.shares + (p.join ? 1 : 0));
     return p;
 }
@@ -510,6 +512,6 @@ tc_status tc_launch_group_norm(int device, const GroupNormArgs &m, const GroupPl
         a.part = (float2 *)workspace;
         if (p.join) a.sums = a.part + (long long)a.n * a.groups * a.shares;
     }
-    if (m.dtype == TC_BF16) return p.vector == 8 ? launch<__nv_bfloat16, 8>(device, a, p, m.act, s) : launch<__nv_bfloat16, 1>(device, a, p, m.act, s);
-    return p.vector == 4 ? launch<float, 4>(device, a, p, m.act, s) : launch<float, 1>(device, a, p, m.act, s);
+    if (m.dtype == TC_BF16) return p.vector == 8 ? launch<__nv_bfloat16, 8>(device, a, p, m.act, s) : p.vector == 2 ? launch<__nv_bfloat16, 2>(device, a, p, m.act, s) : launch<__nv_bfloat16, 1>(device, a, p, m.act, s);
+    return p.vector == 4 ? launch<float, 4>(device, a, p, m.act, s) : p.vector == 2 ? launch<float, 2>(device, a, p, m.act, s) : launch<float, 1>(device, a, p, m.act, s);
 }

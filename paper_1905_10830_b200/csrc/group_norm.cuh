@@ -2,7 +2,7 @@
 // sums over a group's channels and a block's pixels.
 //
 // Maps have their channels as neighbours in memory.  A block works on a run of a map's pixels with all their channels, contiguous in memory.
-// Its threads are laid as `rows` x `lanes`: a lane holds V neighbouring channels (16 bytes, or a single value where rows do not begin
+// Its threads are laid as `rows` x `lanes`: a lane holds V neighbouring channels (16 bytes, or two values or one where rows do not begin
 // at 16 bytes), a row every rows-th pixel, so that a thread's weights stay in registers.  More channels than threads are worked through in
 // column blocks.
 #pragma once
@@ -41,12 +41,14 @@ struct GroupArgs {
 template <int V> constexpr int kPairs = (V + 1) / 2;
 template <int V> using Pairs = uint64_t[kPairs<V>];
 template <typename T, int V> struct Raw { uint4 v; };
+template <> struct Raw<__nv_bfloat16, 2> { uint32_t v; };
+template <> struct Raw<float, 2> { float2 v; };
 template <typename T> struct Raw<T, 1> { float v; };
 
 template <int V, typename T>
 __device__ __forceinline__ void load_raw(Raw<T, V> &r, const T *p)
 {
-    if constexpr (V > 1) r.v = *reinterpret_cast<const uint4 *>(p);
+    if constexpr (V > 1) r.v = *reinterpret_cast<const decltype(r.v) *>(p);
     else r.v = load1(p);
 }
 template <int V, typename T>
@@ -59,7 +61,11 @@ __device__ __forceinline__ void pairs_of(const Raw<T, V> &r, Pairs<V> &v)
     } else if constexpr (V == 4) {
         v[0] = pair_of(r.v.x, r.v.y);
         v[1] = pair_of(r.v.z, r.v.w);
-    } else
+    } else if constexpr (V == 2 && sizeof(T) == 2)
+        v[0] = pair_of(r.v << 16, r.v & 0xffff0000u);
+    else if constexpr (V == 2)
+        v[0] = pair_of(r.v.x, r.v.y);
+    else
         v[0] = pair_of(r.v, 0.f);
 }
 template <int V, typename T>
@@ -70,7 +76,7 @@ __device__ __forceinline__ void load_pairs(const T *p, Pairs<V> &v)
     pairs_of<V>(r, v);
 }
 // load(place, i) and then work(place, i, i2) for pairs of the pixels i and i2 of a thread, from `first` on in steps of `rows`, kBatch (even) loaded at a time; an odd last one comes
-// with i2 = -1, and loaded(place) of the place behind it is what load left there before.
+// with i2 = -1, and the place behind it has the same pixel.
 template <int kBatch, typename L, typename W>
 __device__ __forceinline__ void in_batches(int first, int end, int rows, L load, W work)
 {
@@ -81,13 +87,19 @@ __device__ __forceinline__ void in_batches(int first, int end, int rows, L load,
 #pragma unroll
         for (int k = 0; k < kBatch; k += 2) work(k, i + k * rows, i + (k + 1) * rows);
     }
-    for (; i < end; i += 2 * rows) {
-        const bool two = i + rows < end;
-        load(0, i);
-        load(1, two ? i + rows : i);
-        work(0, i, two ? i + rows : -1);
+    if (i >= end) return;
+    int at[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+        at[k] = k == 0 || i + k * rows < end ? i + k * rows : at[k ? k - 1 : 0];
+        load(k, at[k]);
     }
+#pragma unroll
+    for (int k = 0; k < kBatch; k += 2)
+        if (k == 0 || at[k] != at[k ? k - 1 : 0]) work(k, at[k], at[k + 1] != at[k] ? at[k + 1] : -1);
 }
+// Vectors that a thread asks for before it works on the first, of V values from global memory.
+template <int V> constexpr int kAhead = V <= 2 ? 8 : 4;
 template <int V, typename T>
 __device__ __forceinline__ void store_pairs(T *p, const Pairs<V> &v)
 {
@@ -96,6 +108,8 @@ __device__ __forceinline__ void store_pairs(T *p, const Pairs<V> &v)
     for (int i = 0; i < kPairs<V>; ++i) halves(v[i], f[2 * i], f[2 * i + 1]);
     if constexpr (V == 8) *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
     else if constexpr (V == 4) *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    else if constexpr (V == 2 && sizeof(T) == 2) *reinterpret_cast<uint32_t *>(p) = pack_bf16(f[0], f[1]);
+    else if constexpr (V == 2) *reinterpret_cast<float2 *>(p) = make_float2(f[0], f[1]);
     else store1(p, f[0]);
 }
 // A vector's values from channel c on, `other` without the vector.
@@ -358,7 +372,9 @@ struct Ring {
 template <typename R>
 size_t ring_bytes(int columns) { return (size_t)R::kRows * (kRunThreads / columns) * columns * 16; }
 // Rings are for rows whose vectors have a thread each.
-inline bool ring_takes(int c, int v) { return v > 1 && c / v <= kRunThreads; }
+inline bool ring_takes(int c, int v, int element) { return v * element == 16 && c / v <= kRunThreads; }
+// Neighbouring channels that a lane holds: of 16 bytes, else two, else one.
+inline int vector_of(int c, int element, bool aligned) { return !aligned ? 1 : c * element % 16 == 0 ? 16 / element : c % 2 == 0 ? 2 : 1; }
 
 // The run of pixels that a block works on.
 struct Run {

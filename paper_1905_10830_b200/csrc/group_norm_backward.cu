@@ -17,8 +17,8 @@ using namespace groups;
 // Blocks an SM: registers enough for both pixels' values.
 constexpr int kGradientBlocks = 2;
 using GradientRing = Ring<2, 4, 2>;                           // 64 KB
-// Vectors that a thread asks for before it works on the first: from shared memory and from global memory.
-template <typename P> constexpr int kBatch = std::is_same_v<P, InPlace> ? 4 : 2;
+// Vectors that a thread asks for before it works on the first: from shared memory two.
+template <typename P, int V> constexpr int kBatch = std::is_same_v<P, InPlace> ? kAhead<V> : 2;
 
 // What a thread needs of its channels: z = (x + minus) slope + b, slope = rstd w.
 template <int V> struct Channel {
@@ -50,9 +50,9 @@ __device__ __forceinline__ void block_sums(const T *src, const T *grad, P &piece
             pieces.wait(piece);
             if (here) {
                 const T *const p = src + pieces.at(piece) * a.c + c, *const q = grad + pieces.at(piece) * a.c + c;
-                constexpr int kAhead = kBatch<P>;
-                Raw<T, V> x[kAhead], dy[kAhead];
-                in_batches<kAhead>(
+                constexpr int kMany = kBatch<P, V>;
+                Raw<T, V> x[kMany], dy[kMany];
+                in_batches<kMany>(
                     lay.row, pieces.end(piece) - pieces.first(piece), lay.rows,
                     [&](int k, int i) {
                         load_raw<V>(x[k], p + i * a.c);
@@ -138,9 +138,9 @@ __device__ __forceinline__ void write_gradients(const T *src, const T *grad, P &
             if (here) {
                 const T *const p = src + pieces.at(piece) * a.c + c, *const q = grad + pieces.at(piece) * a.c + c;
                 T *const to = out + pieces.first(piece) * a.c;
-                constexpr int kAhead = kBatch<P>;
-                Raw<T, V> x[kAhead], dy[kAhead];
-                in_batches<kAhead>(
+                constexpr int kMany = kBatch<P, V>;
+                Raw<T, V> x[kMany], dy[kMany];
+                in_batches<kMany>(
                     lay.row, pieces.end(piece) - pieces.first(piece), lay.rows,
                     [&](int k, int i) {
                         load_raw<V>(x[k], p + i * a.c);
@@ -364,12 +364,12 @@ tc_status launch_runs(int device, const GroupArgs &a, cudaStream_t s)
 template <typename T, int V>
 tc_status launch(int device, const GroupArgs &a, const GroupPlan &p, int act, cudaStream_t s)
 {
-    // (maps of single values never lie in shared memory: bulk copies begin at 16 bytes)
+    // (maps of other vectors never lie in shared memory: bulk copies begin at 16 bytes)
 #define TC_GRADIENT(kAct) \
     do { \
-        if constexpr (V > 1) { \
+        if constexpr (V * sizeof(T) == 16) { \
             if (p.shared) return launch_map<T, V, kAct>(device, a, p.threads, p.shared, s); \
-            if (ring_takes(a.c, V)) return launch_runs<T, V, kAct, true>(device, a, s); \
+            if (ring_takes(a.c, V, sizeof(T))) return launch_runs<T, V, kAct, true>(device, a, s); \
         } \
         return launch_runs<T, V, kAct, false>(device, a, s); \
     } while (0)
@@ -386,13 +386,13 @@ GroupPlan tc_plan_group_norm_backward(const GroupGradArgs &m, int sm_count)
     GroupPlan p;
     const int element = m.dtype == TC_BF16 ? 2 : 4;
     const bool vectors = m.dweight || m.dbias;
-    p.vector = m.c * element % 16 == 0 && m.aligned ? 16 / element : 1;
+    p.vector = vector_of(m.c, element, m.aligned);
     p.threads = tc_group_threads(m.c / p.vector);
     GroupArgs a{};
     a.c = m.c;
     a.groups = m.groups;
     auto bytes = [&](int shares) { return shared_bytes(a, (m.hw + shares - 1) / shares, element, p.vector, p.threads); };
-    if (p.vector > 1) {
+    if (p.vector * element == 16) {
         const int shares = shares_on_chip(m.n, m.hw, sm_count, sm_count, bytes);
         if (shares) {
             p.shares = shares;
@@ -402,7 +402,7 @@ GroupPlan tc_plan_group_norm_backward(const GroupGradArgs &m, int sm_count)
             return p;
         }
     }
-    cut_runs(p, m.n, m.hw, (long long)m.c * element, 2, ring_takes(m.c, p.vector) ? kGradientBlocks : 0, sm_count);
+    cut_runs(p, m.n, m.hw, (long long)m.c * element, 2, ring_takes(m.c, p.vector, element) ? kGradientBlocks : 0, sm_count);
     p.workspace = ((vectors ? (size_t)m.n * p.shares * m.c : 0) + (size_t)m.n * m.groups * (p.shares + (p.join ? 1 : 0))) * sizeof(float2);
     return p;
 }
@@ -434,8 +434,8 @@ tc_status tc_launch_group_norm_backward(int device, const GroupGradArgs &m, cons
             if (a.dweight || a.dbias) a.part = rest + (p.join ? (long long)a.n * a.groups : 0);
         } else if (p.workspace)
             a.part = (float2 *)workspace;
-        if (m.dtype == TC_BF16) st = p.vector == 8 ? launch<__nv_bfloat16, 8>(device, a, p, m.act, s) : launch<__nv_bfloat16, 1>(device, a, p, m.act, s);
-        else st = p.vector == 4 ? launch<float, 4>(device, a, p, m.act, s) : launch<float, 1>(device, a, p, m.act, s);
+        if (m.dtype == TC_BF16) st = p.vector == 8 ? launch<__nv_bfloat16, 8>(device, a, p, m.act, s) : p.vector == 2 ? launch<__nv_bfloat16, 2>(device, a, p, m.act, s) : launch<__nv_bfloat16, 1>(device, a, p, m.act, s);
+        else st = p.vector == 4 ? launch<float, 4>(device, a, p, m.act, s) : p.vector == 2 ? launch<float, 2>(device, a, p, m.act, s) : launch<float, 1>(device, a, p, m.act, s);
     }
     if (st != TC_OK || (!a.dweight && !a.dbias)) return st;
     const dim3 grid((unsigned int)((a.c + kVectorChannels - 1) / kVectorChannels));
