@@ -157,9 +157,11 @@ __device__ __forceinline__ void write_values(const T *src, P &pieces, long long 
     }
 }
 
-// The same as codes, and as values too where they are wanted: a team of lanes a pixel, its largest magnitude first.  `table`: [3][c] floats of shared memory.
-template <typename T, int V, int kAct, typename P, typename F>
-__device__ __forceinline__ void write_codes(const T *src, P &pieces, long long first, const GroupArgs &a, const Lay &lay, F stats, float *table)
+// The same as codes, and as values too where they are wanted: a team of lanes a pixel, its largest magnitude first.  A pixel's values stay in registers
+// until the codes where a lane has no more than kKeep vectors of them (256x14x14 x 1024 bf16, silu: 112 us, 141 where they are computed again), else they are computed again.  `table`: [3][c] floats of shared memory.
+template <int V> constexpr int kKeep = V == 8 ? 2 : V == 4 ? 4 : 8;
+template <typename T, int V, int kAct, bool kKeeps, typename P, typename F>
+__device__ __forceinline__ void codes_of_run(const T *src, P &pieces, long long first, const GroupArgs &a, const Lay &lay, F stats, float *table)
 {
     const int per_group = a.c / a.groups;
     lay.sync();                                               // the last table's readers
@@ -183,6 +185,27 @@ __device__ __forceinline__ void write_codes(const T *src, P &pieces, long long f
 #pragma unroll
         for (int k = 0; k < kPairs<V>; ++k) v[k] = activate2<kAct>(fma2(add2(v[k], minus[k]), slope[k], bias[k]));
     };
+    auto magnitude = [](const Pairs<V> &v, uint32_t most) {
+#pragma unroll
+        for (int k = 0; k < kPairs<V>; ++k) {
+            float x, y;
+            halves(v[k], x, y);
+            most = max(most, max(abs_bits(x), V > 1 ? abs_bits(y) : 0u));
+        }
+        return most;
+    };
+    auto write = [](uint8_t *to, const Pairs<V> &v, const Coder &coder) {
+        float f[2 * kPairs<V>];
+#pragma unroll
+        for (int k = 0; k < kPairs<V>; ++k) halves(v[k], f[2 * k], f[2 * k + 1]);
+        if constexpr (V == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(rowcodes::codes_of4(f, coder), rowcodes::codes_of4(f + 4, coder));
+        else if constexpr (V == 4) *reinterpret_cast<uint32_t *>(to) = rowcodes::codes_of4(f, coder);
+        else if constexpr (V == 2) {
+            const float two[4] = {f[0], f[1], 0.f, 0.f};
+            *reinterpret_cast<uint16_t *>(to) = (uint16_t)rowcodes::codes_of4(two, coder);
+        } else
+            *to = rowcodes::code_of(f[0], coder);
+    };
     // pixel p of the run is team p % step's, whatever piece it comes in; whole warps go round together
     for (int piece = 0; piece < pieces.count(); ++piece) {
         pieces.wait(piece);
@@ -191,40 +214,52 @@ __device__ __forceinline__ void write_codes(const T *src, P &pieces, long long f
             const int pixel = base + threadIdx.x / size;
             const bool here = pixel >= from && pixel < end;
             if (!__any_sync(0xffffffffu, here)) continue;
+            T *const out = a.out ? (T *)a.out + (first + pixel) * a.c : nullptr;
+            uint8_t *const to = a.codes.codes + (first + pixel) * a.codes.ld;
             uint32_t most = 0;
-            if (here)
+            Pairs<V> kept[kKeeps ? kKeep<V> : 1];
+            if constexpr (kKeeps) {
+#pragma unroll
+                for (int i = 0; i < kKeep<V>; ++i) {
+                    const int c = (i * size + rank) * V;
+                    if (!here || c >= a.c) break;
+                    values(place + pixel, c, kept[i]);
+                    if (out) store_pairs<V>(out + c, kept[i]);
+                    most = magnitude(kept[i], most);
+                }
+            } else if (here)
                 for (int c = rank * V; c < a.c; c += size * V) {
                     Pairs<V> v;
                     values(place + pixel, c, v);
-                    if (a.out) store_pairs<V>((T *)a.out + (first + pixel) * a.c + c, v);
-#pragma unroll
-                    for (int k = 0; k < kPairs<V>; ++k) {
-                        float x, y;
-                        halves(v[k], x, y);
-                        most = max(most, max(abs_bits(x), V > 1 ? abs_bits(y) : 0u));
-                    }
+                    if (out) store_pairs<V>(out + c, v);
+                    most = magnitude(v, most);
                 }
             for (int d = size / 2; d; d >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
             const Coder coder(rowcodes::row_scale(most));
             if (!here) continue;
             if (rank == 0) a.codes.scales[first + pixel] = coder.scale;
-            uint8_t *const to = a.codes.codes + (first + pixel) * a.codes.ld;
-            for (int c = rank * V; c < a.c; c += size * V) {
-                Pairs<V> v;
-                values(place + pixel, c, v);
-                float f[2 * kPairs<V>];
+            if constexpr (kKeeps) {
 #pragma unroll
-                for (int k = 0; k < kPairs<V>; ++k) halves(v[k], f[2 * k], f[2 * k + 1]);
-                if constexpr (V == 8) *reinterpret_cast<uint2 *>(to + c) = make_uint2(rowcodes::codes_of4(f, coder), rowcodes::codes_of4(f + 4, coder));
-                else if constexpr (V == 4) *reinterpret_cast<uint32_t *>(to + c) = rowcodes::codes_of4(f, coder);
-                else if constexpr (V == 2) {
-                    const float two[4] = {f[0], f[1], 0.f, 0.f};
-                    *reinterpret_cast<uint16_t *>(to + c) = (uint16_t)rowcodes::codes_of4(two, coder);
-                } else to[c] = rowcodes::code_of(f[0], coder);
-            }
+                for (int i = 0; i < kKeep<V>; ++i) {
+                    const int c = (i * size + rank) * V;
+                    if (c >= a.c) break;
+                    write(to + c, kept[i], coder);
+                }
+            } else
+                for (int c = rank * V; c < a.c; c += size * V) {
+                    Pairs<V> v;
+                    values(place + pixel, c, v);
+                    write(to + c, v, coder);
+                }
         }
         pieces.done(piece);
     }
+}
+template <typename T, int V, int kAct, typename P, typename F>
+__device__ __forceinline__ void write_codes(const T *src, P &pieces, long long first, const GroupArgs &a, const Lay &lay, F stats, float *table)
+{
+    if (a.c <= 32 * V * kKeep<V>) codes_of_run<T, V, kAct, true>(src, pieces, first, a, lay, stats, table);
+    else codes_of_run<T, V, kAct, false>(src, pieces, first, a, lay, stats, table);
 }
 
 // ---- maps in a cluster's shared memory --------------------------------------------------------
