@@ -548,7 +548,7 @@ typedef struct {
  * ties to even), -127 to 127.  A row that holds an infinity or a NaN gets a NaN for its scale and zeros for its codes: everything computed from
  * it is NaN.  A tensor whose channels are neighbours in memory is one of P pixels of 1 x 1.  Rows that do not lie one after the other in memory have
  * their maxima in the context's arena.  May be captured into a graph.
- * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 - 256 pixels, more than 2^22 channels), CUDA. */
+ * Errors: INVALID_ARG, UNSUPPORTED (more than 2^31 - 256 pixels, more than 2^22 channels), CUDA; TIMEOUT by tc_get_status. */
 tc_status tc_quantize_rows(tc_ctx *ctx, const tc_tensor *x, const tc_rows *pixels, const tc_rows *channels, void *cuda_stream);
 
 /* out[p][o] = act(fl(fl(fl(sum_k a[p][k] b[o][k]) sa[p]) sb[o]) + bias[o]), a [P][K] and b [O][K], `out` a tensor of P pixels and O channels, fp32 or
@@ -581,7 +581,8 @@ typedef struct {
 tc_status tc_group_norm(tc_ctx *ctx, const tc_tensor *x, const tc_group_params *params, void *y, const tc_rows *codes, float *stats, void *cuda_stream);
 
 /* Gradients from `dy` (DEVICE, as x) and the statistics that tc_group_norm wrote: `dx` (DEVICE, as x), and where they are wanted `dweight` and `dbias`
- * (DEVICE float [C], or NULL; only where the vector is given).  The ReLU's derivative at 0 is 0.  Gradients of vectors are sums over all pixels, within a block in fp32, over blocks
+ * (DEVICE float [C], or NULL; only where the vector is given).  The ReLU's derivative at 0 is 0; SiLU's is taken at
+ * z = -44 at least (4e-18).  Gradients of vectors are sums over all pixels, within a block in fp32, over blocks
  * in fp64, in an order that depends on sizes, type and alignment alone.  Conventions and errors as above. */
 tc_status tc_group_norm_backward(tc_ctx *ctx, const tc_tensor *x, const tc_group_params *params, const float *stats, const void *dy, void *dx, float *dweight,
                                  float *dbias, void *cuda_stream);
