@@ -2,10 +2,10 @@
 //
 //   y = act((x - mean) rstd w + b),   mean and rstd = 1 / sqrt(var + eps) over a map's pixels and a group's channels
 //
-// Bound by the bytes moved, x once and y once.  Where a map fits the shared memory of a cluster's blocks (up to sixteen) it is read once: each block
-// takes its pixels there by bulk copies, finds its mean and then its squares about that mean, the blocks' moments are put together through
-// the cluster's shared memory, and the values leave from where they lie.  Larger maps, and rows that do not begin at 16 bytes, take
-// two kernels: moments of runs of pixels, and the values, the pixels through a ring in shared memory where their rows begin at 16 bytes.
+// Bound by the bytes moved, x once and y once.  A map or two, and maps that a block holds, are read once: each of a cluster's blocks (up to sixteen)
+// takes its pixels to shared memory by bulk copies, finds its moments, they are put together through the cluster's shared memory, and the values leave from where
+// they lie.  Others take two kernels: moments of runs of pixels, and the values, the pixels through a ring in shared memory where their rows begin at 16 bytes.
+// 256x56x56 x 128 bf16: 104 us, 5.9 TB/s with the second reading of x; one map of 256x14x14: 6.7 us.
 //
 // Moments are put together as (n, mean, M2): no sum of squares is taken about a mean far from its own.
 #include "group_norm.cuh"
@@ -513,8 +513,10 @@ GroupPlan tc_plan_group_norm(const GroupNormArgs &m, int sm_count)
     a.groups = m.groups;
     auto bytes = [&](int shares) { return shared_bytes(a, (m.hw + shares - 1) / shares, element, p.vector, p.threads); };
     if (p.vector * element == 16) {
-        const int shares = shares_on_chip(m.n, m.hw, 2ll * sm_count, sm_count, bytes);
-        if (shares) {
+        // On chip where a block has a map of some size, or for a map or two.  (Others read x a second time from L2, which costs less than waiting for clusters: 256x14x14 bf16 x 1, 4, 30: 6.8,
+        // 7.2 and 13.2 us on chip, 6.7, 6.4 and 10.4 by runs; 832x19x19 x 2: 10.0 and 11.7; without clusters, 256x14x14 x 290: 21 and 26, 64x7x7 x 290: 9.5 and 8.6.)
+        const int shares = shares_on_chip(m.n, m.hw, 2, sm_count, bytes);
+        if (shares && (m.n <= 2 || (shares == 1 && (long long)m.hw * m.c * element >= kWorthKeeping))) {
             p.shares = shares;
             p.share = (m.hw + shares - 1) / shares;
             p.shared = bytes(shares);

@@ -501,17 +501,20 @@ __device__ __forceinline__ float sum_over(float v, int lanes)
 
 }  // namespace groups
 
-// Blocks of a map where maps lie in clusters' shared memory; 0: they do not.  As few as let two share an SM, then as few as fit one, where all of them are `most` at
-// most, and more where SMs would be idle.  More maps than find a place at a time take the other kernels: a block's phases (wait, sums, cluster, values) follow one another,
-// and little of the next one's waiting falls into them (1024 maps of 256x14x14 bf16: 64 us and 70, their gradient 173 and 168; 64 of 512x28x28 45 and 53, 125 and 77).
+// Clusters of `shares` blocks that run at a time with a block an SM.  Clusters lie within a GPC, and one of the GPCs has fewer than 16 SMs: eight clusters of 16 blocks, or sixteen of 8, take
+// two turns (gradient of 832x19x19 x 8 bf16 in clusters of 16: 26 us, of 8: 19).
+inline long long clusters_at_once(int shares, int sm_count) { return shares <= 4 ? sm_count / shares : sm_count * (shares == 8 ? 14 : 7) / 148; }
+// Blocks of a map where all maps lie in clusters' shared memory at one time, `per_sm` blocks an SM where two fit; 0: they do not.  As few as let two share an SM, then as few as fit one, and
+// more where SMs would be idle.  More maps than find a place at a time take the other kernels: a block's phases (wait, sums, cluster, values) follow one another, and little of the
+// next one's waiting falls into them.
 template <typename F>
-int shares_on_chip(long long n, int hw, long long most, int sm_count, F bytes)
+int shares_on_chip(long long n, int hw, int per_sm, int sm_count, F bytes)
 {
     for (const size_t room : {kTwoBlocks, kMostShared}) {
         int shares = 1;
         while (shares < groups::kMostShares && bytes(shares) > room) shares *= 2;
-        if (bytes(shares) > room || n * shares > most) continue;
-        while (shares < groups::kMostShares && n * shares * 2 <= sm_count && hw / shares >= 12) shares *= 2;
+        if (bytes(shares) > room || n > clusters_at_once(shares, sm_count) * (room == kTwoBlocks ? per_sm : 1)) continue;
+        while (shares < groups::kMostShares && n <= clusters_at_once(2 * shares, sm_count) && hw / shares >= 12) shares *= 2;
         return shares;
     }
     return 0;

