@@ -468,7 +468,9 @@ row_matmul_pair_kernel(const __grid_constant__ RowArgs a, const __grid_constant_
                         if (c + h + 32 == kCols) hand_back();
                         finish_rows<kCols, 16>(a, r, v + h / 2, scales, c + h);
                     }
-                    // boxes in turn: one may still be on its way out
+                    // boxes in turn: one may still be on its way out.  (A box outside the output is not filled either: every turn has its group of copies, so that the one that may
+                    // be pending is the other box's.)
+                    if (first_row >= a.rows_a || col0 + c >= a.rows_b) continue;
                     const uint32_t box = boxes + turn * kBoxBytes;
                     turn = (turn + 1) % kBoxes;
                     if (a.store_tma && lane == 0) {
@@ -479,10 +481,8 @@ row_matmul_pair_kernel(const __grid_constant__ RowArgs a, const __grid_constant_
                     fill_box<T>(box, v, lane);
                     if (a.store_tma) fence_proxy_async_smem();
                     __syncwarp();
-                    if (first_row < a.rows_a && col0 + c < a.rows_b) {
-                        if (!a.store_tma) store_box<T>(a, box, first_row, col0 + c, lane);
-                        else if (lane == 0) tma_store_2d(&map_out, col0 + c, first_row, box);
-                    }
+                    if (!a.store_tma) store_box<T>(a, box, first_row, col0 + c, lane);
+                    else if (lane == 0) tma_store_2d(&map_out, col0 + c, first_row, box);
                 }
             } else {
 #pragma unroll
