@@ -546,13 +546,16 @@ int vector_of(const RowQuantizeArgs &a)
     return inner % 8 == 0 && at % 16 == 0 ? 8 : inner % 4 == 0 && at % (4 * size) == 0 ? 4 : 1;
 }
 
+// Dynamic shared memory of pixel_strip_kernel: the values and a scale for each pixel.
+size_t strip_bytes(int c, int width, size_t size) { return ((size_t)c * width * size + 15) / 16 * 16 + width * sizeof(float); }
 // Pixels of a block of pixel_strip_kernel, 0: it does not take the maps.
 int strip_of(const RowQuantizeArgs &a)
 {
     const size_t size = a.dtype == TC_BF16 ? 2 : 4, at = (uintptr_t)a.x;
     if (a.hw <= 1 || at % 16) return 0;
     const size_t image = (size_t)a.c * a.hw * size;
-    if (image <= kTwoBlocks - 4096 && image % 16 == 0) return a.hw;
+    // (maps of few channels have as many bytes of scales as of values: they count too.  A block an SM is better than strips all the same: 16x56x56 x 128 bf16 13 us, in strips of 64 35)
+    if (image <= kTwoBlocks - 4096 && image % 16 == 0 && strip_bytes(a.c, a.hw, size) <= kMostStrip) return a.hw;
     if (a.hw * size % 16) return image <= kMostStrip - 4096 && image % 16 == 0 && a.hw <= 1024 ? a.hw : 0;
     for (int width = 64; width >= (int)(16 / size); width /= 2)
         if ((size_t)a.c * width * size <= kTwoBlocks - 4096) return width < a.hw ? width : 0;
@@ -597,7 +600,7 @@ tc_status quantize(int device, int sm_count, const RowQuantizeArgs &a, uint32_t 
             }
         if (const int width = left[0].codes ? strip_of(a) : 0) {
             const StripArgs strip{a.c, a.hw, width, (a.hw + width - 1) / width, left[0], a.status};
-            const size_t smem = ((size_t)a.c * width * sizeof(T) + 15) / 16 * 16 + width * sizeof(float);
+            const size_t smem = strip_bytes(a.c, width, sizeof(T));
             const dim3 grid((unsigned int)(a.n * strip.strips));
             const int threads = strip.strips > 1 ? kStripThreads / 2 : kStripThreads;
             if (!allow_shared<pixel_strip_kernel<T, 1>>(device, kMostStrip) || !allow_shared<pixel_strip_kernel<T, 2>>(device, kMostStrip) ||
