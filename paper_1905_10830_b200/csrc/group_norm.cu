@@ -11,6 +11,8 @@
 #include "group_norm.cuh"
 #include "integer_codes.cuh"
 
+#include <type_traits>
+
 namespace {
 
 using namespace groups;
@@ -19,41 +21,140 @@ using rowcodes::Coder;
 using NormRing = Ring<2, 8, 1>;                               // 64 KB
 constexpr int kNormBlocks = 3;                                // an SM
 
-// Mean and M2 (sum of squares about it) of each group over the pixels at `src`, in one pass: sums of the distances d of a channel's values from the
-// first pixel's, p, and of their squares; the channel's mean is m = p + sum d / n, its squares about that sum d^2 - (sum d)^2 / n.  p being one of the n
-// values, (p - m)^2 is at most n times the mean square distance: the difference loses no more than a factor of n.
-// to(group, (mean, M2)) by one thread each.  red: red_values() float2; channels: c float2 of (p, ), then (m, squares).
-template <typename T, int V, typename P, typename F>
-__device__ __forceinline__ void block_moments(const T *src, P &pieces, const GroupArgs &a, const Lay &lay, float2 *red, float2 *channels, F to)
+// A whole run where it is, in steps: each as long as all before it.
+constexpr int kStepRounds = 16;                               // of the block's rows, the first two steps
+struct InSteps {
+    int pixels, each;
+    __device__ __forceinline__ int count() const
+    {
+        int n = 1;
+        while (each << (n - 1) < pixels) ++n;
+        return n;
+    }
+    __device__ __forceinline__ int first(int step) const { return step ? each << (step - 1) : 0; }
+    __device__ __forceinline__ int end(int step) const { return min(each << step, pixels); }
+    __device__ __forceinline__ int at(int step) const { return first(step); }
+    __device__ __forceinline__ void wait(int) {}
+    __device__ __forceinline__ void done(int) {}
+};
+__device__ __forceinline__ InSteps in_steps(InPlace &p, const Lay &lay) { return {p.pixels, kStepRounds * lay.rows}; }
+template <typename P>
+__device__ __forceinline__ P &in_steps(P &p, const Lay &) { return p; }
+
+// Moments that are put together about the first one's mean: what is taken away in the end is at most so many times what stays.
+constexpr int kFew = 8;
+
+// The pixels of a block's rows.
+struct RowCounts {
+    int rows, rest;
+    float full, per_pixel;
+    __device__ __forceinline__ RowCounts(int pixels, const Lay &lay)
+    {
+        rows = lay.rows;
+        rest = pixels % rows;
+        full = (float)(pixels / rows);
+        per_pixel = pixels ? reciprocal_fast((float)pixels) : 0.f;
+    }
+    __device__ __forceinline__ float operator()(int row) const { return row < rest ? full + 1.f : row < rows ? full : 0.f; }
+};
+// Mean and M2 (sum of squares about it) over the block's pixels of column block `block` from its threads' moments of V channels each, as channel_sums hands them out.
+template <int V, typename F>
+__device__ __forceinline__ void channel_moments(const Lay &lay, int block, const RowCounts &count, const float (&mean)[2 * kPairs<V>], const float (&m2)[2 * kPairs<V>], float2 *red, F each)
 {
+    constexpr int kPer = V > 1 ? V / 2 : 1;
+    const int half = (lay.rows + 1) / 2, lanes = lay.lanes;
+    const bool here = lay.at(block);
+    const int place = lay.row >= half ? lay.row - half : lay.row;
+    lay.sync();                                               // the last moments' readers
+    float4 *const at = reinterpret_cast<float4 *>(red) + place * kPer * lanes + lay.lane;
+    float2 *const at1 = red + place * lanes + lay.lane;
+    if (here && lay.row >= half) {
+        if constexpr (V > 1)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) at[i * lanes] = make_float4(mean[2 * i], m2[2 * i], mean[2 * i + 1], m2[2 * i + 1]);
+        else *at1 = make_float2(mean[0], m2[0]);
+    }
+    lay.sync();
+    if (here && lay.row < half) {
+        // the upper half's row added to the lower half's
+        const float n = count(lay.row), more = count(lay.row + half), share = more > 0.f ? more * reciprocal_fast(n + more) : 0.f, weight = n * share;
+        auto joined = [&](float mean_a, float m2_a, float mean_b, float m2_b) {
+            const float d = more > 0.f ? mean_b - mean_a : 0.f;
+            return make_float2(fmaf(d, share, mean_a), more > 0.f ? fmaf(__fmul_rn(d, weight), d, __fadd_rn(m2_a, m2_b)) : m2_a);
+        };
+        if constexpr (V > 1) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const float4 t = at[i * lanes];
+                const float2 x = joined(mean[2 * i], m2[2 * i], t.x, t.y), y = joined(mean[2 * i + 1], m2[2 * i + 1], t.z, t.w);
+                at[i * lanes] = make_float4(x.x, x.y, y.x, y.y);
+            }
+        } else {
+            const float2 t = *at1;
+            *at1 = joined(mean[0], m2[0], t.x, t.y);
+        }
+    }
+    lay.sync();
+    const int first = block * lanes, channels = min(lanes, lay.columns - first) * V;
+    for (int base = 0; base < channels; base += lay.threads) {
+        const int j = base + threadIdx.x;
+        float about = 0.f, off = 0.f, squares = 0.f;
+        if (j < channels) {
+            const float2 *from = red + (V > 1 ? 2 * (((j % V) / 2) * lanes + j / V) + (j & 1) : j);
+            const int pitch = V * lanes;
+            // about the first row's mean, or the mean where there are more than a few: then the squares, and what the mean is off
+            about = from[0].x;
+            if (half > kFew) {
+                about = 0.f;
+#pragma unroll 4
+                for (int r = 0; r < half; ++r) about = fmaf(count(r) + count(r + half), from[r * pitch].x, about);
+                about = __fmul_rn(about, count.per_pixel);
+            }
+#pragma unroll 4
+            for (int r = 0; r < half; ++r) {
+                const float2 t = from[r * pitch];
+                const float d = t.x - about, weighted = __fmul_rn(count(r) + count(r + half), d);
+                off = __fadd_rn(off, weighted);
+                squares = __fadd_rn(squares, fmaf(weighted, d, t.y));
+            }
+        }
+        const float step = __fmul_rn(off, count.per_pixel);
+        each(j < channels ? first * V + j : -1, __fadd_rn(about, step), max_nan(fmaf(-off, step, squares), 0.f));
+    }
+}
+
+// Mean and M2 of each group over the pixels at `src`, in one pass.  A thread sums the distances d of its pixels from a value p and their squares; p is the first of them and moves to the mean of those so far after
+// the first piece and whenever there are twice as many (by t, what the sums are corrected by: sum d - n t, sum d^2 - t (2 sum d - n t)).  (p - mean)^2 of one of n pixels is at most their sum
+// of squares, so what the first correction takes away is no more than n times what stays, n being up to kStepRounds; later ones take away at most as much as stays: no sum of squares is
+// taken about a value far from its values' mean, wherever the pixels lie that are far from the rest.
+// to(group, (mean, M2)) by one thread each.  red: red_values() float2; channels: c float2.
+template <typename T, int V, typename P, typename F>
+__device__ __forceinline__ void block_moments(const T *src, P &given, const GroupArgs &a, const Lay &lay, float2 *red, float2 *channels, F to)
+{
+    decltype(auto) pieces = in_steps(given, lay);
     const int per_group = a.c / a.groups, pixels = pieces.pixels;
-    const float per_pixel = 1.0f / (float)pixels, per_channel = 1.0f / (float)per_group, n = (float)pixels;
-    const bool in_warps = groups_in_warps(lay, per_group);
+    const float per_channel = 1.0f / (float)per_group, n = (float)pixels;
+    const bool in_warps = groups_in_warps(lay, per_group), moves = pixels > kStepRounds * lay.rows;
+    const RowCounts count(pixels, lay);
     for (int b = 0; b < lay.blocks; ++b) {
-        Pairs<V> from = {}, sum = {}, squares = {};
-        const bool here = lay.at(b) && pixels > 0;
+        Pairs<V> from = {}, sum = {}, squares = {};           // (-p)
+        const bool here = lay.at(b) && lay.row < pixels;
         const int c = (b * lay.lanes + lay.lane) * V;
+        int seen = 0;
         for (int piece = 0; piece < pieces.count(); ++piece) {
             pieces.wait(piece);
             if (here) {
                 const T *const p = src + pieces.at(piece) * a.c + c;
-                if (piece == 0) {
-                    load_pairs<V>(p, from);
+                if (piece == 0) {                             // (each row has a pixel in the first piece)
+                    load_pairs<V>(p + lay.row * a.c, from);
 #pragma unroll
-                    for (int k = 0; k < kPairs<V>; ++k) {
-                        float x, y;
-                        halves(from[k], x, y);
-                        if (lay.row == 0) {                   // (a ring's first pixel is gone when the channel's mean is computed)
-                            channels[c + 2 * k].x = x;
-                            if (V > 1) channels[c + 2 * k + 1].x = y;
-                        }
-                        from[k] ^= kMinus;
-                    }
+                    for (int k = 0; k < kPairs<V>; ++k) from[k] ^= kMinus;
                 }
                 Raw<T, V> raw[kAhead<V>];
                 in_batches<kAhead<V>>(
                     lay.row, pieces.end(piece) - pieces.first(piece), lay.rows, [&](int k, int i) { load_raw<V>(raw[k], p + i * a.c); },
                     [&](int k, int, int second) {
+                        seen += second < 0 ? 1 : 2;
                         for (int h = 0; h < (second < 0 ? 1 : 2); ++h) {
                             Pairs<V> v;
                             pairs_of<V>(raw[k + h], v);
@@ -65,23 +166,36 @@ __device__ __forceinline__ void block_moments(const T *src, P &pieces, const Gro
                             }
                         }
                     });
+                if (moves && ((piece & (piece + 1)) == 0 || std::is_same_v<P, InPlace>) && piece + 1 < pieces.count()) {
+                    const uint64_t minus = both(-(float)seen), per = both(reciprocal_fast((float)seen));
+#pragma unroll
+                    for (int j = 0; j < kPairs<V>; ++j) {
+                        const uint64_t moved = fma2(sum[j] ^ kMinus, per, from[j]), t = add2(from[j], moved ^ kMinus), left = fma2(minus, t, sum[j]);          // (t as p moved, rounded)
+                        squares[j] = fma2(t ^ kMinus, add2(sum[j], left), squares[j]);
+                        sum[j] = left;
+                        from[j] = moved;
+                    }
+                }
             }
             pieces.done(piece);
         }
-        float s[2 * kPairs<V>], q[2 * kPairs<V>];
+        // the thread's mean, p + s / n, and M2
+        float mean[2 * kPairs<V>] = {}, m2[2 * kPairs<V>] = {};
+        if (here) {
+            const uint64_t per = both(reciprocal_fast(count(lay.row)));
 #pragma unroll
-        for (int k = 0; k < kPairs<V>; ++k) {
-            halves(sum[k], s[2 * k], s[2 * k + 1]);
-            halves(squares[k], q[2 * k], q[2 * k + 1]);
+            for (int k = 0; k < kPairs<V>; ++k) {
+                const uint64_t step = mul2(sum[k], per);
+                halves(add2(step, from[k] ^ kMinus), mean[2 * k], mean[2 * k + 1]);
+                halves(fma2(sum[k] ^ kMinus, step, squares[k]), m2[2 * k], m2[2 * k + 1]);
+            }
         }
         // a channel's mean and squares, and in warps its group's
-        channel_sums<V>(lay, b, s, q, red, [&](int ch, float sum_d, float sum_q) {
+        channel_moments<V>(lay, b, count, mean, m2, red, [&](int ch, float mean, float m2) {
             // (products that are not left to be fused: the statistics' bits are the same in every variant of the kernels)
-            const float d = __fmul_rn(sum_d, per_pixel);
-            float mean = ch >= 0 && pixels > 0 ? __fadd_rn(channels[ch].x, d) : 0.f, m2 = ch >= 0 && pixels > 0 ? fmaf(-sum_d, d, sum_q) : 0.f;
             if (in_warps) {
                 const float m = __fmul_rn(sum_over(mean, per_group), per_channel);
-                m2 = sum_over(fmaf(n * (mean - m), mean - m, m2), per_group);
+                m2 = sum_over(fmaf(__fmul_rn(n, mean - m), mean - m, m2), per_group);
                 if (ch >= 0 && (ch & (per_group - 1)) == 0) to(ch / per_group, make_float2(m, m2));
             } else if (ch >= 0)
                 channels[ch] = make_float2(mean, m2);
@@ -337,24 +451,44 @@ __global__ void __launch_bounds__(512, 2) group_norm_map_kernel(const __grid_con
 }
 
 // ---- maps in runs of pixels ----------------------------------------------------------------------
-// A group's mean and 1 / deviation from its runs' moments, by a team of `size` lanes, as block_moments about the first run's mean.
+// A group's mean and 1 / deviation from its runs' moments, by a team of `size` lanes, as channel_moments.  A lane has kHeld runs, or more of them (kMore).
+constexpr int kHeld = 4;
+template <bool kMore>
 __device__ __forceinline__ float2 join_runs(const GroupArgs &a, long long map, int g, int rank, int size)
 {
     const int per_group = a.c / a.groups;
     const float2 *const at = a.part + map * a.shares * a.groups + g;
-    const float from = at->x;
-    float s = 0.f, q = 0.f;                                   // in units of a run's values
-#pragma unroll 4
-    for (int r = rank; r < a.shares; r += size) {
-        const float2 m = at[(long long)r * a.groups];
-        const float n = (float)min(a.share, a.hw - r * a.share), d = m.x - from;
-        s = fmaf(n, d, s);
-        q = __fadd_rn(q, fmaf(n * (float)per_group * d, d, m.y));
+    auto pixels_of = [&](int r) { return (float)min(a.share, a.hw - r * a.share); };
+    auto run = [&](int r) { return r < a.shares ? at[(long long)r * a.groups] : make_float2(0.f, 0.f); };
+    const float per_pixel = reciprocal_fast((float)a.hw);
+    float2 held[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) held[i] = run(rank + i * size);
+    float about = at->x, off = 0.f, squares = 0.f;
+    if (a.shares > kFew) {
+        about = 0.f;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (rank + i * size < a.shares) about = fmaf(pixels_of(rank + i * size), held[i].x, about);
+        if constexpr (kMore)
+            for (int r = rank + kHeld * size; r < a.shares; r += size) about = fmaf(pixels_of(r), run(r).x, about);
+        about = __fmul_rn(sum_over(about, size), per_pixel);
     }
-    s = sum_over(s, size);
-    q = sum_over(q, size);
-    const float d = s / (float)a.hw;
-    return make_float2(__fadd_rn(from, d), 1.0f / sqrtf(__fadd_rn(fmaxf(fmaf(-s * (float)per_group, d, q), 0.f) / ((float)a.hw * (float)per_group), a.eps)));
+    auto add = [&](int r, float2 m) {
+        const float d = m.x - about, weighted = __fmul_rn(pixels_of(r), d);
+        off = __fadd_rn(off, weighted);
+        squares = __fadd_rn(squares, fmaf(__fmul_rn(weighted, (float)per_group), d, m.y));
+    };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+        if (rank + i * size < a.shares) add(rank + i * size, held[i]);
+    if constexpr (kMore)
+        for (int r = rank + kHeld * size; r < a.shares; r += size) add(r, run(r));
+    off = sum_over(off, size);
+    squares = sum_over(squares, size);
+    const float step = __fmul_rn(off, per_pixel);
+    squares = max_nan(fmaf(__fmul_rn(-off, (float)per_group), step, squares), 0.f);
+    return make_float2(__fadd_rn(about, step), 1.0f / sqrtf(__fadd_rn(squares / ((float)a.hw * (float)per_group), a.eps)));
 }
 
 // Maps of many runs: sums[map][group], a warp each.
@@ -364,7 +498,7 @@ __global__ void __launch_bounds__(256) group_join_kernel(const __grid_constant__
     chain_wait();
     const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) / 32;
     if (i >= a.n * a.groups) return;
-    const float2 v = join_runs(a, i / a.groups, (int)(i % a.groups), threadIdx.x & 31, 32);
+    const float2 v = join_runs<true>(a, i / a.groups, (int)(i % a.groups), threadIdx.x & 31, 32);
     if (threadIdx.x & 31) return;
     a.sums[i] = v;
     if (a.stats) a.stats[i] = v;
@@ -399,7 +533,7 @@ __global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kRing 
             const Team team(a.shares, kRunThreads);
             for (int base = 0; base < a.groups; base += team.step) {
                 const int g = base + team.first;
-                const float2 v = join_runs(a, run.map, min(g, a.groups - 1), team.rank, team.size);
+                const float2 v = join_runs<false>(a, run.map, min(g, a.groups - 1), team.rank, team.size);
                 if (g < a.groups && team.rank == 0) {
                     own[g] = v;
                     if (a.stats && run.run == 0) a.stats[run.map * a.groups + g] = v;
