@@ -582,7 +582,7 @@ tc_status tc_group_norm(tc_ctx *ctx, const tc_tensor *x, const tc_group_params *
 
 /* Gradients from `dy` (DEVICE, as x) and the statistics that tc_group_norm wrote: `dx` (DEVICE, as x), and where they are wanted `dweight` and `dbias`
  * (DEVICE float [C], or NULL; only where the vector is given).  The ReLU's derivative at 0 is 0; SiLU's is taken at
- * z = -44 at least (4e-18).  Gradients of vectors are sums over all pixels, within a block in fp32, over blocks
+ * z = -43.5 at least (-5e-18).  Gradients of vectors are sums over all pixels, within a block in fp32, over blocks
  * in fp64, in an order that depends on sizes, type and alignment alone.  Conventions and errors as above. */
 tc_status tc_group_norm_backward(tc_ctx *ctx, const tc_tensor *x, const tc_group_params *params, const float *stats, const void *dy, void *dx, float *dweight,
                                  float *dbias, void *cuda_stream);

@@ -172,9 +172,10 @@ __device__ __forceinline__ float max_nan(float a, float b)    // (a NaN stays on
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
     return d;
 }
-// 1 / (1 + e^-z) of two pixels' pairs a and b, each value's two reciprocals from one of their product: the functions' unit takes three operations for two values instead of four,
-// and it is what bounds the gradient.  The two are of one channel, so a NaN stays in its group.  z is taken as -44 at least, where the result is 8e-20 and products of two
-// denominators stay in range.  The fast exponential and reciprocal, a few steps of 2^-23 each.
+// s = 1 / (1 + e^-z) of two pixels' pairs a and b, and rest = e^-z s = 1 - s (the difference would lose the digits that a large z needs).  Each value's two reciprocals come from one of
+// their product: the functions' unit takes three operations for two values instead of four.  The two are of one channel, so a NaN stays in its group.  z is taken as -43.5 at
+// least, where s is 1.3e-19: two denominators' product is 6.1e37 at most, whose reciprocal is a normal number still.  The fast exponential and reciprocal, a few
+// steps of 2^-23 each.
 __device__ __forceinline__ float exp2_fast(float v)
 {
     float e;
@@ -193,22 +194,24 @@ __device__ __forceinline__ uint64_t at_least(uint64_t z, float least)
     halves(z, x, y);
     return pair_of(max_nan(x, least), max_nan(y, least));
 }
-__device__ __forceinline__ uint64_t denominator(uint64_t z)
+__device__ __forceinline__ uint64_t exp_minus(uint64_t z)
 {
     float x, y;
     halves(mul2(z, both(-1.4426950408889634f)), x, y);
-    return add2(pair_of(exp2_fast(x), exp2_fast(y)), both(1.0f));
+    return pair_of(exp2_fast(x), exp2_fast(y));
 }
-__device__ __forceinline__ void sigmoids(uint64_t &za, uint64_t &zb, uint64_t &sa, uint64_t &sb)
+__device__ __forceinline__ void sigmoids(uint64_t &za, uint64_t &zb, uint64_t &sa, uint64_t &sb, uint64_t &rest_a, uint64_t &rest_b)
 {
-    za = at_least(za, -44.0f);
-    zb = at_least(zb, -44.0f);
-    const uint64_t da = denominator(za), db = denominator(zb);
+    za = at_least(za, -43.5f);
+    zb = at_least(zb, -43.5f);
+    const uint64_t ea = exp_minus(za), eb = exp_minus(zb), da = add2(ea, both(1.0f)), db = add2(eb, both(1.0f));
     float x, y;
     halves(mul2(da, db), x, y);
     const uint64_t r = pair_of(reciprocal_fast(x), reciprocal_fast(y));
     sa = mul2(r, db);
     sb = mul2(r, da);
+    rest_a = mul2(ea, sa);
+    rest_b = mul2(eb, sb);
 }
 // The activation.  (Each value's reciprocal its own: memory bounds the forward pass, and a value's bits do not depend on its neighbour.)
 template <int kAct>
@@ -217,7 +220,7 @@ __device__ __forceinline__ uint64_t activate2(uint64_t z)
     if constexpr (kAct == kNoAct) return z;
     if constexpr (kAct == kRelu) return at_least(z, 0.f);
     float x, y;
-    halves(denominator(z), x, y);                             // (e^-z beyond 2^126: 0)
+    halves(add2(exp_minus(z), both(1.0f)), x, y);             // (e^-z beyond 2^126: 0)
     return mul2(z, pair_of(reciprocal_fast(x), reciprocal_fast(y)));
 }
 // Its derivatives at za and zb, times da and db.
@@ -234,12 +237,12 @@ __device__ __forceinline__ void slope2(uint64_t za, uint64_t zb, uint64_t &da, u
         one(za, da);
         one(zb, db);
     } else if constexpr (kAct == kSilu) {
-        uint64_t sa, sb;
-        sigmoids(za, zb, sa, sb);
+        uint64_t sa, sb, rest_a, rest_b;
+        sigmoids(za, zb, sa, sb, rest_a, rest_b);
         // s (1 + z (1 - s))
         const uint64_t one = both(1.0f);
-        da = mul2(da, mul2(sa, fma2(za, add2(one, sa ^ kMinus), one)));
-        db = mul2(db, mul2(sb, fma2(zb, add2(one, sb ^ kMinus), one)));
+        da = mul2(da, mul2(sa, fma2(za, rest_a, one)));
+        db = mul2(db, mul2(sb, fma2(zb, rest_b, one)));
     }
 }
 
