@@ -604,8 +604,11 @@ int tc_group_threads(int columns)
     return best;
 }
 
-void cut_runs(GroupPlan &p, long long n, int hw, long long row, int tensors, int ring_blocks, int sm_count)
+void cut_runs(GroupPlan &p, long long n, int hw, int columns, long long row, int tensors, int ring_blocks, int sm_count)
 {
+    // a thread's sums stay short: so many pixels of a block's rows
+    const int blocks_of_columns = (columns + kRunThreads - 1) / kRunThreads, rows = kRunThreads / ((columns + blocks_of_columns - 1) / blocks_of_columns);
+    const long long longest = (long long)kMostRounds * rows;
     // in all 2^29 runs at most
     const long long least = std::max(((long long)hw * n + (1ll << 29) - 1) >> 29, 1ll);
     long long share;
@@ -616,8 +619,7 @@ void cut_runs(GroupPlan &p, long long n, int hw, long long row, int tensors, int
         const long long shortest = std::max(least, kRunLeast / (row * tensors));
         double best_cost = 0.0;
         share = 0;
-        // (from as few on as keep a thread's sums short)
-        for (long long runs = (hw * row + kRunMost - 1) / kRunMost, more; runs <= hw; runs += more) {
+        for (long long runs = std::max((hw * row + kRunMost - 1) / kRunMost, (hw + longest - 1) / longest), more; runs <= hw; runs += more) {
             more = std::max(1ll, runs / 8);
             const long long of = std::max(shortest, (hw + runs - 1) / runs);
             const double cost = ((double)n * ((hw + of - 1) / of) / blocks + 0.5) * (double)((of * row + kRunCost) * tensors);
@@ -626,7 +628,7 @@ void cut_runs(GroupPlan &p, long long n, int hw, long long row, int tensors, int
         }
     } else {
         // of eight pixels at least where their channels' sums are written too; shorter than kRunBytes where SMs would be idle
-        share = std::max(tensors > 1 ? 8ll : 1ll, kRunBytes / (row * tensors));
+        share = std::max(tensors > 1 ? 8ll : 1ll, std::min(longest, kRunBytes / (row * tensors)));
         while (share > 1 && n * ((hw + share - 1) / share) < 2ll * sm_count) share = (share + 1) / 2;
         share = std::max(share, least);
     }
@@ -657,7 +659,7 @@ GroupPlan tc_plan_group_norm(const GroupNormArgs &m, int sm_count)
             return p;
         }
     }
-    cut_runs(p, m.n, m.hw, (long long)m.c * element, 1, ring_takes(m.c, p.vector, element) ? kNormBlocks : 0, sm_count);
+    cut_runs(p, m.n, m.hw, m.c / p.vector, (long long)m.c * element, 1, ring_takes(m.c, p.vector, element) ? kNormBlocks : 0, sm_count);
     p.workspace = (size_t)m.n * m.groups * sizeof(float2) * (p.shares + (p.join ? 1 : 0));
     return p;
 }

@@ -522,5 +522,5 @@ int shares_on_chip(long long n, int hw, int per_sm, int sm_count, F bytes)
     }
     return 0;
 }
-// Runs of pixels (of `row` bytes in each of `tensors`) of a map; ring_blocks: blocks of an SM that take them through rings, 0: none do.
-void cut_runs(GroupPlan &p, long long n, int hw, long long row, int tensors, int ring_blocks, int sm_count);
+// Runs of pixels (of `columns` vectors, `row` bytes in each of `tensors`) of a map; ring_blocks: blocks of an SM that take them through rings, 0: none do.
+void cut_runs(GroupPlan &p, long long n, int hw, int columns, long long row, int tensors, int ring_blocks, int sm_count);

@@ -403,7 +403,7 @@ GroupPlan tc_plan_group_norm_backward(const GroupGradArgs &m, int sm_count)
             return p;
         }
     }
-    cut_runs(p, m.n, m.hw, (long long)m.c * element, 2, ring_takes(m.c, p.vector, element) ? kGradientBlocks : 0, sm_count);
+    cut_runs(p, m.n, m.hw, m.c / p.vector, (long long)m.c * element, 2, ring_takes(m.c, p.vector, element) ? kGradientBlocks : 0, sm_count);
     p.workspace = ((vectors ? (size_t)m.n * p.shares * m.c : 0) + (size_t)m.n * m.groups * (p.shares + (p.join ? 1 : 0))) * sizeof(float2);
     return p;
 }

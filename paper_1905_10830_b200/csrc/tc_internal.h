@@ -429,6 +429,7 @@ struct GroupPlan {
     size_t shared = 0, workspace = 0;
 };
 constexpr long long kRunBytes = 192 * 1024, kRunLeast = 8 * 1024, kRunMost = 512 * 1024, kRunCost = 32 * 1024;
+constexpr int kMostRounds = 128;                // of a block's rows over a run's pixels
 constexpr long long kWorthKeeping = 64 * 1024;  // bytes of a map
 // Runs of a map whose sums every run's block joins; more are joined by a kernel (4 maps of 256x128x128 bf16, 111 runs: 29 us with it, 39 without; 12 of 256x64x64 f32, 37 runs: 32 and 38; 42 of
 // 114x28x28, 10 runs: 16.5 and 15.8).
