@@ -357,11 +357,12 @@ struct Ring {
     __device__ __forceinline__ void fill(unsigned char *ring, const void *x, const void *dy, int row) const
     {
         const int pieces = count(), room = each * row;
-        for (int i = 0; i < pieces; ++i) {
+        int i = 0;
+        for (; i < pieces; ++i) {
             const int slot = i % kSlots;
             if (i >= kSlots && !arrived(&empty[slot], (i / kSlots + 1) & 1)) {
                 tc_dev_set_status(status, TC_ERR_TIMEOUT);
-                return;
+                break;
             }
             const uint32_t bytes = (uint32_t)(end(i) - first(i)) * row, bar = sm100::smem_u32(&full[slot]), to = sm100::smem_u32(ring) + slot * room;
             const size_t from = (size_t)first(i) * row;
@@ -369,6 +370,8 @@ struct Ring {
             sm100::bulk_load(to, (const char *)x + from, bytes, bar);
             if (kTensors > 1) sm100::bulk_load(to + kSlots * room, (const char *)dy + from, bytes, bar);
         }
+        // The copies in flight land before the block's shared memory goes to another, whoever's wait ran out.
+        for (int last = max(i - kSlots, 0); last < i; ++last) arrived(&full[last % kSlots], last / kSlots & 1);
     }
 };
 // A ring's bytes.  (Rows of a block: as Lay's.)

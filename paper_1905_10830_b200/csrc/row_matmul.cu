@@ -165,12 +165,9 @@ row_matmul_kernel(const __grid_constant__ RowArgs a, const __grid_constant__ CUt
                     if (++s == S::kStages) { s = 0; phase ^= 1u; }
                 }
             }
-            if (!alive) {
-                tc_dev_set_status(a.status, TC_ERR_TIMEOUT);
-                // the copies in flight land before the block's shared memory goes to another
-                const long long first = issued > S::kStages ? issued - S::kStages : 0;
-                for (long long i = first; i < issued; ++i) mbar_wait_soon(smem_u32(&s_full[i % S::kStages]), (uint32_t)(i / S::kStages & 1));
-            }
+            if (!alive) tc_dev_set_status(a.status, TC_ERR_TIMEOUT);
+            // The copies in flight land before the block's shared memory goes to another, whichever warp's wait ran out.
+            for (long long i = issued > S::kStages ? issued - S::kStages : 0; i < issued; ++i) mbar_wait_soon(smem_u32(&s_full[i % S::kStages]), (uint32_t)(i / S::kStages & 1));
         }
     } else if (warp == S::kMma) {
         const uint32_t issuer = lane == 0 ? 1u : 0u;
