@@ -594,7 +594,7 @@ tc_status tc_group_norm_backward(tc_ctx *ctx, const tc_tensor *x, const tc_group
  * the values keep their bits.  `out` may be the tensor itself (then nothing is written unless it is scaled), otherwise outputs overlap neither one another nor
  * inputs; tc_gradient_norm does not look at it.  `list` is HOST memory, read before the call returns; `norm` DEVICE float [1] receives the norm
  * before clipping.  May be captured into a graph.
- * Errors: INVALID_ARG (max_norm negative or NaN among them), UNSUPPORTED (more than 2^42 values), CUDA. */
+ * Errors: INVALID_ARG (max_norm negative or NaN among them), UNSUPPORTED (more than 2^41 values), CUDA. */
 typedef struct {
     const void *data;          /* DEVICE, aligned to its element size */
     void *out;                 /* DEVICE, of the same size and type   */

@@ -1936,6 +1936,7 @@ bool gradients_apart(const tc_gradient *g, int n, const float *norm)
     }
     return true;
 }
+constexpr long long kMostGradients = 1ll << 41;        // values of a list: its rows of 8 KB are numbered in 32 bits
 tc_status gradients(tc_ctx *ctx, const tc_gradient *list, int32_t n, bool clip, float max_norm, float *norm, void *cuda_stream)
 try {
     if (!ctx || n < 0 || (n > 0 && !list) || !norm || !aligned_to(4, norm) || (clip && !(max_norm >= 0.f))) return TC_ERR_INVALID_ARG;
@@ -1945,7 +1946,7 @@ try {
         const tc_gradient &g = list[i];
         if ((g.dtype != TC_F32 && g.dtype != TC_BF16) || g.count < 0) return TC_ERR_INVALID_ARG;
         if (g.count > 0 && (!g.data || (clip && !g.out) || !aligned_to(element_size(g.dtype), g.data, g.out))) return TC_ERR_INVALID_ARG;
-        if (g.count > 1ll << 42 || (values += g.count) > 1ll << 42) return TC_ERR_UNSUPPORTED;
+        if (g.count > kMostGradients || (values += g.count) > kMostGradients) return TC_ERR_UNSUPPORTED;
     }
     if (!clip) {                                              // (the norm writes none)
         reads.assign(list, list + n);
