@@ -589,8 +589,8 @@ tc_status tc_group_norm_backward(tc_ctx *ctx, const tc_tensor *x, const tc_group
 
 /* The norm of many gradients together, and their clipping by it:
  *     norm = sqrt(sum over all values of all tensors of x^2),   out = x min(1, max_norm / norm)
- * for a list of tensors of any number and sizes, fp32 and bf16 mixed.  Squares are summed in fp64 (a few at a time in fp32 where that loses nothing), in an order that
- * the sizes and alignments decide; max_norm / norm and the products are fp32, rounded once to the tensor's type.  Where norm <= max_norm or is not finite
+ * for a list of tensors of any number and sizes, fp32 and bf16 mixed.  Squares are summed in fp64 (16 or 32 at a time in fp32, in sums of four or eight, where that neither overflows nor
+ * drops small ones: ten roundings of 2^-24 of their sum), in an order that the sizes, alignments and the device decide; max_norm / norm and the products are fp32, rounded once to the tensor's type.  Where norm <= max_norm or is not finite
  * the values keep their bits.  `out` may be the tensor itself (then nothing is written unless it is scaled), otherwise outputs overlap neither one another nor
  * inputs; tc_gradient_norm does not look at it.  `list` is HOST memory, read before the call returns; `norm` DEVICE float [1] receives the norm
  * before clipping.  May be captured into a graph.

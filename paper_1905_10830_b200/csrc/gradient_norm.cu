@@ -8,8 +8,8 @@
 // of together 47 MB: 27.5 us, of which 14.5 are what a copy needs for the bytes and the rest two launches and the blocks' sums that lie between; 290 of 1.9 GB: 930 us
 // (5.9 TB/s with the second read).
 //
-// A thread's squares of those rows, 16 or 32 of them, are summed in fp32 where that neither overflows nor loses what is small, else in fp64;
-// everything else is summed in fp64, in an order that the list's sizes alone decide.
+// A thread's squares of those rows, 16 or 32 of them, are summed in fp32 (four sums of four or eight, each addition rounded to 2^-24) where that neither overflows nor drops what is
+// small, else in fp64; everything else is summed in fp64, in an order that the list's sizes, its alignments and the number of SMs decide.
 #include "block_codes.cuh"
 #include "tc_internal.h"
 
