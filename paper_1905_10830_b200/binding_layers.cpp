@@ -487,6 +487,7 @@ PyObject *group_norm(PyObject *, PyObject *const *args, Py_ssize_t n)
         if (groups < 1 || t.c % groups) throw Bad{"groups: expected a divisor of the number of channels"};
         const tc_group_params p{(int32_t)groups, activation_of(a[5]), vector(a[2], t.c, c.device, "weight"), vector(a[3], t.c, c.device, "bias"), (float)eps};
         const bool both = PyUnicode_Check(a[6]) && PyUnicode_CompareWithASCIIString(a[6], "both") == 0;
+        if (PyUnicode_Check(a[6]) && !both) throw Bad{"codes: False, True or \"both\""};
         const int codes = both || PyObject_IsTrue(a[6]);
         if (PyErr_Occurred()) throw Raised{};
         PyObject *out_y = a[7], *out_codes = a[7];
