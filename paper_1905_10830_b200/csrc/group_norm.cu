@@ -5,7 +5,7 @@
 // Bound by the bytes moved, x once and y once.  A map or two, and maps that a block holds, are read once: each of a cluster's blocks (up to sixteen)
 // takes its pixels to shared memory by bulk copies, finds its moments, they are put together through the cluster's shared memory, and the values leave from where
 // they lie.  Others take two kernels: moments of runs of pixels, and the values, the pixels through a ring in shared memory where their rows begin at 16 bytes.
-// 256x56x56 x 128 bf16: 104 us, 5.9 TB/s with the second reading of x; one map of 256x14x14: 6.7 us.
+// 256x56x56 x 128 bf16: 107 us, 5.8 TB/s with the second reading of x; one map of 256x14x14: 7.1 us.
 //
 // Moments are put together as (n, mean, M2): no sum of squares is taken about a mean far from its own.
 #include "group_norm.cuh"
@@ -272,7 +272,7 @@ __device__ __forceinline__ void write_values(const T *src, P &pieces, long long 
 }
 
 // The same as codes, and as values too where they are wanted: a team of lanes a pixel, its largest magnitude first.  A pixel's values stay in registers
-// until the codes where a lane has no more than kKeep vectors of them (256x14x14 x 1024 bf16, silu: 112 us, 141 where they are computed again), else they are computed again.  `table`: [3][c] floats of shared memory.
+// until the codes where a lane has no more than kKeep vectors of them (256x14x14 x 1024 bf16, silu: 114 us, 140 where they are computed again), else they are computed again.  `table`: [3][c] floats of shared memory.
 template <int V> constexpr int kKeep = V == 8 ? 2 : V == 4 ? 4 : 8;
 template <typename T, int V, int kAct, bool kKeeps, typename P, typename F>
 __device__ __forceinline__ void codes_of_run(const T *src, P &pieces, long long first, const GroupArgs &a, const Lay &lay, F stats, float *table)
@@ -453,6 +453,7 @@ __global__ void __launch_bounds__(512, 2) group_norm_map_kernel(const __grid_con
 // ---- maps in runs of pixels ----------------------------------------------------------------------
 // A group's mean and 1 / deviation from its runs' moments, by a team of `size` lanes, as channel_moments.  A lane has kHeld runs, or more of them (kMore).
 constexpr int kHeld = 4;
+static_assert(kInlineRuns <= 32 * kHeld, "a team of 32 lanes holds all runs that are joined inline");
 template <bool kMore>
 __device__ __forceinline__ float2 join_runs(const GroupArgs &a, long long map, int g, int rank, int size)
 {
@@ -614,7 +615,7 @@ void cut_runs(GroupPlan &p, long long n, int hw, int columns, long long row, int
     long long share;
     if (ring_blocks) {
         // So many that the blocks' work is least: a run costs as much as kRunCost more of each tensor, and the last ones leave half of the blocks idle.  (Fitted: 128x56x56 x 128 bf16,
-        // gradient, in runs of 128, 242, 349, 448 and 628 pixels: 176, 134, 117, 121 and 118 us; 256x56x56 x 128 forward, 126, 349 and 628: 120, 104 and 108.)
+        // gradient, in runs of 128, 242, 349, 448 and 628 pixels: 174, 131, 115, 117 and 116 us; 256x56x56 x 128 forward, 126, 349 and 628: 107, 105 and 109.)
         const double blocks = (double)ring_blocks * sm_count;
         const long long shortest = std::max(least, kRunLeast / (row * tensors));
         double best_cost = 0.0;
@@ -649,8 +650,8 @@ GroupPlan tc_plan_group_norm(const GroupNormArgs &m, int sm_count)
     a.groups = m.groups;
     auto bytes = [&](int shares) { return shared_bytes(a, (m.hw + shares - 1) / shares, element, p.vector, p.threads); };
     if (p.vector * element == 16) {
-        // On chip where a block has a map of some size, or for a map or two.  (Others read x a second time from L2, which costs less than waiting for clusters: 256x14x14 bf16 x 1, 4, 30: 6.8,
-        // 7.2 and 13.2 us on chip, 6.7, 6.4 and 10.4 by runs; 832x19x19 x 2: 10.0 and 11.7; without clusters, 256x14x14 x 290: 21 and 26, 64x7x7 x 290: 9.5 and 8.6.)
+        // On chip where a block has a map of some size, or for a map or two.  (Others read x a second time from L2, which costs less than waiting for clusters: 256x14x14 bf16 x 1, 8, 30: 7.3,
+        // 9.1 and 13.1 us on chip, 7.9, 7.5 and 9.3 by runs; 832x19x19 x 2: 10.6 both; without clusters, 256x14x14 x 290: 22 and 26, 64x7x7 x 290: 11.2 and 9.5.)
         const int shares = shares_on_chip(m.n, m.hw, 2, sm_count, bytes);
         if (shares && (m.n <= 2 || (shares == 1 && (long long)m.hw * m.c * element >= kWorthKeeping))) {
             p.shares = shares;

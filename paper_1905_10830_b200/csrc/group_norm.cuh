@@ -315,8 +315,8 @@ struct Pieces {
     __device__ __forceinline__ void done(int) const {}
 };
 // Of a run that is longer than its block's shared memory: pieces of kRounds rounds of the rows through a ring of kSlots, that a warp of its own fills by bulk copies.  Loads of the threads
-// keep too little on its way (gradient of silu, 128x56x56 x 128 bf16: 143 us, ring 117; 256x56x56 x 128 forward 114 and 104).  Few long pieces: more and shorter ones, of the
-// same bytes, cost more waits than their earlier refills are worth (125 and 106).
+// keep too little on its way (gradient of silu, 128x56x56 x 128 bf16: 144 us, ring 116; 256x56x56 x 128 forward 116 and 105).  Few long pieces: more and shorter ones, of the
+// same bytes, cost more waits than their earlier refills are worth (123 and 107).
 template <int kSlots_, int kRounds, int kTensors>
 struct Ring {
     static constexpr int kSlots = kSlots_, kRows = kTensors * kSlots * kRounds;
