@@ -465,9 +465,7 @@ row_matmul_pair_kernel(const __grid_constant__ RowArgs a, const __grid_constant_
                         if (c + h + 32 == kCols) hand_back();
                         finish_rows<kCols, 16>(a, r, v + h / 2, scales, c + h);
                     }
-                    // boxes in turn: one may still be on its way out.  (A box outside the output is not filled either: every turn has its group of copies, so that the one that may
-                    // be pending is the other box's.)
-                    if (first_row >= a.rows_a || col0 + c >= a.rows_b) continue;
+                    // boxes in turn: one may still be on its way out
                     const uint32_t box = boxes + turn * kBoxBytes;
                     turn = (turn + 1) % kBoxes;
                     if (a.store_tma && lane == 0) {
@@ -478,8 +476,13 @@ row_matmul_pair_kernel(const __grid_constant__ RowArgs a, const __grid_constant_
                     fill_box<T>(box, v, lane);
                     if (a.store_tma) fence_proxy_async_smem();
                     __syncwarp();
-                    if (!a.store_tma) store_box<T>(a, box, first_row, col0 + c, lane);
-                    else if (lane == 0) tma_store_2d(&map_out, col0 + c, first_row, box);
+                    // (every turn has its group of copies, one outside the output an empty one, so that the group that may be pending is the other box's.  Boxes outside that took no turn
+                    // instead made the turns' addresses unknown to the compiler: 256 to 256 of 1024 maps of 14x14 69 us for 65)
+                    if (first_row < a.rows_a && col0 + c < a.rows_b) {
+                        if (!a.store_tma) store_box<T>(a, box, first_row, col0 + c, lane);
+                        else if (lane == 0) tma_store_2d(&map_out, col0 + c, first_row, box);
+                    } else if (a.store_tma && lane == 0)
+                        tma_store_none();
                 }
             } else {
 #pragma unroll

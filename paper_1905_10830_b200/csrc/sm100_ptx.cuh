@@ -317,6 +317,7 @@ __device__ __forceinline__ void tma_store_2d(const void *tensor_map, int x, int 
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];\n\tcp.async.bulk.commit_group;"
                  ::"l"(tensor_map), "r"(x), "r"(y), "r"(smem_src) : "memory");
 }
+__device__ __forceinline__ void tma_store_none() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }     // a group without a copy
 __device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void tma_store_wait_read_but_one() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
 __device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }

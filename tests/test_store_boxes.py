@@ -8,19 +8,20 @@ import pytest
 from paper_1905_10830_b200 import build
 
 OUTSIDE = r"if \(first_row >= a\.rows_a \|\| col0 \+ c >= a\.rows_b\) continue;"
-STEPS = {"skip": OUTSIDE, "turn": r"turn = \(turn \+ 1\) % kBoxes;", "wait": r"tma_store_wait_read_but_one\(\)", "fill": r"fill_box<T>\(box,", "store": r"tma_store_2d\("}
+STEPS = {"skip": OUTSIDE, "turn": r"turn = \(turn \+ 1\) % kBoxes;", "wait": r"tma_store_wait_read_but_one\(\)", "fill": r"fill_box<T>\(box,", "store": r"tma_store_2d\(",
+         "none": r"else if \(a\.store_tma && lane == 0\)\s*tma_store_none\(\);"}
 INSIDE = "first_row < a.rows_a && col0 + c < a.rows_b"
 
 
 def _steps():
-    """The steps of a box by rows in their order; a store is "guarded" where it asks for boxes inside the output."""
+    """The steps of a box by rows in their order; a store is "guarded" where it asks for boxes inside the output, and "none" is a group without a copy for the others."""
     code = re.sub(r"//[^\n]*", "", open(os.path.join(build.CSRC, "row_matmul.cu")).read())
     body = next(b for b in re.findall(r"^\{$(.*?)^\}", code, re.M | re.S) if "tma_store_wait_read_but_one" in b)
     body = body[body.index("if (a.by_rows)"):]
     body = body[:body.index("store_lanes<")]
     at = sorted((m.start(), name) for name, pattern in STEPS.items() for m in re.finditer(pattern, body))
     names = [name for _, name in at]
-    assert [n for n in names if n != "skip"] == ["turn", "wait", "fill", "store"], names
+    assert [n for n in names if n not in ("skip", "none")] == ["turn", "wait", "fill", "store"], names
     return names, INSIDE in body
 
 
@@ -40,6 +41,8 @@ def _overwritten(names, guarded, inside):
                 return True
             elif name == "store" and (here or not guarded):
                 pending.append(box)
+            elif name == "none" and not here:
+                pending.append(None)
     return False
 
 
@@ -56,3 +59,5 @@ def test_no_box_is_filled_under_a_copy(columns_of_box):
 def test_the_count_sees_a_turn_without_a_copy():
     assert _overwritten(["turn", "wait", "fill", "store"], True, [True, False, True])
     assert not _overwritten(["turn", "wait", "fill", "store"], False, [True, False, True])
+    assert not _overwritten(["turn", "wait", "fill", "store", "none"], True, [True, False, True])
+    assert not _overwritten(["skip", "turn", "wait", "fill", "store"], True, [True, False, True])
