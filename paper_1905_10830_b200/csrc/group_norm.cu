@@ -5,7 +5,7 @@
 // Bound by the bytes moved, x once and y once.  A map or two, and maps that a block holds, are read once: each of a cluster's blocks (up to sixteen)
 // takes its pixels to shared memory by bulk copies, finds its moments, they are put together through the cluster's shared memory, and the values leave from where
 // they lie.  Others take two kernels: moments of runs of pixels, and the values, the pixels through a ring in shared memory where their rows begin at 16 bytes.
-// 256x56x56 x 128 bf16: 107 us, 5.8 TB/s with the second reading of x; one map of 256x14x14: 7.1 us.
+// 256x56x56 x 128 bf16: 107 us, 5.8 TB/s with the second reading of x; one map of 256x14x14: 6.7 us.
 //
 // Moments are put together as (n, mean, M2): no sum of squares is taken about a mean far from its own.
 #include "group_norm.cuh"
@@ -127,15 +127,24 @@ __device__ __forceinline__ void channel_moments(const Lay &lay, int block, const
 // the first piece and whenever there are twice as many (by t, what the sums are corrected by: sum d - n t, sum d^2 - t (2 sum d - n t)).  (p - mean)^2 of one of n pixels is at most their sum
 // of squares, so what the first correction takes away is no more than n times what stays, n being up to kStepRounds; later ones take away at most as much as stays: no sum of squares is
 // taken about a value far from its values' mean, wherever the pixels lie that are far from the rest.
+// kNear (few_pixels): p is the first pixel's value in all rows, whose sums are simply added; what is taken away in the end is no more than the block's pixels times what stays.
 // to(group, (mean, M2)) by one thread each.  red: red_values() float2; channels: c float2.
-template <typename T, int V, typename P, typename F>
+template <typename T, int V, bool kNear, typename P, typename F>
 __device__ __forceinline__ void block_moments(const T *src, P &given, const GroupArgs &a, const Lay &lay, float2 *red, float2 *channels, F to)
 {
     decltype(auto) pieces = in_steps(given, lay);
     const int per_group = a.c / a.groups, pixels = pieces.pixels;
     const float per_channel = 1.0f / (float)per_group, n = (float)pixels;
-    const bool in_warps = groups_in_warps(lay, per_group), moves = pixels > kStepRounds * lay.rows;
-    const RowCounts count(pixels, lay);
+    const bool in_warps = groups_in_warps(lay, per_group), moves = !kNear && pixels > kStepRounds * lay.rows;
+    // a channel's mean and squares, and in warps its group's.  (Products that are not left to be fused: the statistics' bits are the same in every variant of the kernels.)
+    auto channel = [&](int ch, float mean, float m2) {
+        if (in_warps) {
+            const float m = __fmul_rn(sum_over(mean, per_group), per_channel);
+            m2 = sum_over(fmaf(__fmul_rn(n, mean - m), mean - m, m2), per_group);
+            if (ch >= 0 && (ch & (per_group - 1)) == 0) to(ch / per_group, make_float2(m, m2));
+        } else if (ch >= 0)
+            channels[ch] = make_float2(mean, m2);
+    };
     for (int b = 0; b < lay.blocks; ++b) {
         Pairs<V> from = {}, sum = {}, squares = {};           // (-p)
         const bool here = lay.at(b) && lay.row < pixels;
@@ -146,9 +155,17 @@ __device__ __forceinline__ void block_moments(const T *src, P &given, const Grou
             if (here) {
                 const T *const p = src + pieces.at(piece) * a.c + c;
                 if (piece == 0) {                             // (each row has a pixel in the first piece)
-                    load_pairs<V>(p + lay.row * a.c, from);
+                    load_pairs<V>(kNear ? p : p + lay.row * a.c, from);
 #pragma unroll
-                    for (int k = 0; k < kPairs<V>; ++k) from[k] ^= kMinus;
+                    for (int k = 0; k < kPairs<V>; ++k) {
+                        float x, y;
+                        halves(from[k], x, y);
+                        if (kNear && lay.row == 0) {          // (a ring's first pixel may be gone when the mean is computed)
+                            channels[c + 2 * k].x = x;
+                            if (V > 1) channels[c + 2 * k + 1].x = y;
+                        }
+                        from[k] ^= kMinus;
+                    }
                 }
                 Raw<T, V> raw[kAhead<V>];
                 in_batches<kAhead<V>>(
@@ -179,27 +196,33 @@ __device__ __forceinline__ void block_moments(const T *src, P &given, const Grou
             }
             pieces.done(piece);
         }
-        // the thread's mean, p + s / n, and M2
         float mean[2 * kPairs<V>] = {}, m2[2 * kPairs<V>] = {};
-        if (here) {
-            const uint64_t per = both(reciprocal_fast(count(lay.row)));
+        if constexpr (kNear) {
+            // the sums
+            const float per_pixel = pixels ? 1.0f / (float)pixels : 0.f;
 #pragma unroll
             for (int k = 0; k < kPairs<V>; ++k) {
-                const uint64_t step = mul2(sum[k], per);
-                halves(add2(step, from[k] ^ kMinus), mean[2 * k], mean[2 * k + 1]);
-                halves(fma2(sum[k] ^ kMinus, step, squares[k]), m2[2 * k], m2[2 * k + 1]);
+                halves(sum[k], mean[2 * k], mean[2 * k + 1]);
+                halves(squares[k], m2[2 * k], m2[2 * k + 1]);
             }
+            channel_sums<V>(lay, b, mean, m2, red, [&](int ch, float s, float q) {
+                const float d = __fmul_rn(s, per_pixel);
+                channel(ch, ch >= 0 && pixels > 0 ? __fadd_rn(channels[ch].x, d) : 0.f, max_nan(fmaf(-s, d, q), 0.f));
+            });
+        } else {
+            // the thread's mean, p + s / n, and M2
+            const RowCounts count(pixels, lay);
+            if (here) {
+                const uint64_t per = both(reciprocal_fast(count(lay.row)));
+#pragma unroll
+                for (int k = 0; k < kPairs<V>; ++k) {
+                    const uint64_t step = mul2(sum[k], per);
+                    halves(add2(step, from[k] ^ kMinus), mean[2 * k], mean[2 * k + 1]);
+                    halves(fma2(sum[k] ^ kMinus, step, squares[k]), m2[2 * k], m2[2 * k + 1]);
+                }
+            }
+            channel_moments<V>(lay, b, count, mean, m2, red, channel);
         }
-        // a channel's mean and squares, and in warps its group's
-        channel_moments<V>(lay, b, count, mean, m2, red, [&](int ch, float mean, float m2) {
-            // (products that are not left to be fused: the statistics' bits are the same in every variant of the kernels)
-            if (in_warps) {
-                const float m = __fmul_rn(sum_over(mean, per_group), per_channel);
-                m2 = sum_over(fmaf(__fmul_rn(n, mean - m), mean - m, m2), per_group);
-                if (ch >= 0 && (ch & (per_group - 1)) == 0) to(ch / per_group, make_float2(m, m2));
-            } else if (ch >= 0)
-                channels[ch] = make_float2(mean, m2);
-        });
     }
     if (in_warps) return;
     lay.sync();
@@ -384,7 +407,7 @@ size_t shared_bytes(const GroupArgs &a, int pixels, int element, int v, int thre
     return ((size_t)pixels * a.c * element + 15) / 16 * 16 + 8 * (size_t)red_values(a.c / v, threads, v) + 16 * (size_t)a.groups + 12 * (size_t)a.c;
 }
 
-template <typename T, int V, int kAct, bool kCodes>
+template <typename T, int V, int kAct, bool kCodes, bool kNear>
 __global__ void __launch_bounds__(512, 2) group_norm_map_kernel(const __grid_constant__ GroupArgs a)
 {
     using namespace sm100;
@@ -416,7 +439,7 @@ __global__ void __launch_bounds__(512, 2) group_norm_map_kernel(const __grid_con
             for (uint32_t at = from; at < to; at += 16384) bulk_load(smem_u32(smem) + at, src + at, min(16384u, to - at), smem_u32(&s_full[i]));
         }
     }
-    block_moments<T, V>(data, pieces, a, lay, red, table, [&](int g, float2 m) { moments[g] = m; });
+    block_moments<T, V, kNear>(data, pieces, a, lay, red, table, [&](int g, float2 m) { moments[g] = m; });
     if (a.shares > 1) cluster_sync();
     else __syncthreads();
     const float count = (float)a.hw * (float)per_group;
@@ -506,7 +529,7 @@ __global__ void __launch_bounds__(256) group_join_kernel(const __grid_constant__
 }
 
 // part[map][run][group]: moments of a run of pixels.  [ring][red: red_values() float2][channels: c float2]
-template <typename T, int V, bool kRing>
+template <typename T, int V, bool kRing, bool kNear>
 __global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kRing ? kNormBlocks : 4) group_moments_kernel(const __grid_constant__ GroupArgs a, int ring_size)
 {
     extern __shared__ __align__(128) unsigned char smem[];
@@ -515,7 +538,7 @@ __global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kRing 
     const Run run(a, blockIdx.x);
     float2 *const part = a.part + (long long)run.index * a.groups;
     with_run<T, NormRing, kRing>(a, run, lay, smem, ring_size, [&](const T *src, const T *, auto &pieces) {
-        block_moments<T, V>(src, pieces, a, lay, red, channels, [&](int g, float2 m) { part[g] = m; });
+        block_moments<T, V, kNear>(src, pieces, a, lay, red, channels, [&](int g, float2 m) { part[g] = m; });
     });
 }
 
@@ -548,23 +571,32 @@ __global__ void __launch_bounds__(kRing ? kRunThreads + 32 : kRunThreads, kRing 
     });
 }
 
-template <typename T, int V, int kAct, bool kCodes>
+// Whether a block's `pixels` are so few that their squares can be summed about the first one's value.  Sums of n squares, of which a thread has n / rows and a channel's last sum half of the rows' one
+// after the other, are off by half as many roundings each, and by n times that where the first pixel is as far from the rest as it can be: 512 roundings of 2^-24 of the variance at most, and
+// in all ordinary cases a few.  (The general way has longer code, which small calls wait for: one map of 256x14x14 6.7 us and 7.2, 290 of 64x7x7 8.3 and 9.2.)
+bool few_pixels(int pixels, int columns, int threads)
+{
+    const int blocks = (columns + threads - 1) / threads, rows = threads / ((columns + blocks - 1) / blocks);
+    return (long long)pixels * ((pixels + rows - 1) / rows + std::min(pixels, rows) / 2) <= 1024;
+}
+
+template <typename T, int V, int kAct, bool kCodes, bool kNear>
 tc_status launch_map(int device, const GroupArgs &a, int threads, size_t smem, cudaStream_t s)
 {
-    constexpr auto kernel = group_norm_map_kernel<T, V, kAct, kCodes>;
+    constexpr auto kernel = group_norm_map_kernel<T, V, kAct, kCodes, kNear>;
     if (!allow_shared<kernel>(device, kMostShared) || !allow_large_clusters<kernel>(device)) return TC_ERR_CUDA;
     return launch_first_cluster(a.shares, kernel, dim3((unsigned int)(a.n * a.shares)), dim3(threads), smem, s, a) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
 template <typename T, int V, int kAct, bool kCodes, bool kRing>
 tc_status launch_runs(int device, const GroupArgs &a, cudaStream_t s)
 {
-    constexpr auto moments = group_moments_kernel<T, V, kRing>;
+    constexpr auto general = group_moments_kernel<T, V, kRing, false>, near = group_moments_kernel<T, V, kRing, true>;
     constexpr auto values = group_values_kernel<T, V, kAct, kCodes, kRing>;
     const size_t ring = kRing ? ring_bytes<NormRing>(a.c / V) : 0;
     const size_t first = ring + 8 * (size_t)red_values(a.c / V, kRunThreads, V) + 8 * (size_t)a.c, last = ring + 8 * (size_t)a.groups + (kCodes ? 12 * (size_t)a.c : 0);
-    if (!allow_shared<moments>(device, kMostShared) || !allow_shared<values>(device, kMostShared)) return TC_ERR_CUDA;
+    if (!allow_shared<general>(device, kMostShared) || !allow_shared<near>(device, kMostShared) || !allow_shared<values>(device, kMostShared)) return TC_ERR_CUDA;
     const dim3 grid((unsigned int)(a.n * a.shares)), block(kRing ? kRunThreads + 32 : kRunThreads);
-    if (launch_first(true, moments, grid, block, first, s, a, (int)ring) != cudaSuccess) return TC_ERR_CUDA;
+    if (launch_first(true, few_pixels(a.share, a.c / V, kRunThreads) ? near : general, grid, block, first, s, a, (int)ring) != cudaSuccess) return TC_ERR_CUDA;
     if (a.sums && launch_chained(true, group_join_kernel, dim3((unsigned int)((a.n * a.groups + 7) / 8)), dim3(256), 0, s, a) != cudaSuccess) return TC_ERR_CUDA;
     return launch_chained(true, values, grid, block, last, s, a, (int)ring) == cudaSuccess ? TC_OK : TC_ERR_CUDA;
 }
@@ -576,7 +608,9 @@ tc_status launch(int device, const GroupArgs &a, const GroupPlan &p, int act, cu
 #define TC_NORM(kAct, kCodes) \
     do { \
         if constexpr (V * sizeof(T) == 16) { \
-            if (p.shared) return launch_map<T, V, kAct, kCodes>(device, a, p.threads, p.shared, s); \
+            if (p.shared) \
+                return few_pixels(a.share, a.c / V, p.threads) ? launch_map<T, V, kAct, kCodes, true>(device, a, p.threads, p.shared, s) \
+                                                               : launch_map<T, V, kAct, kCodes, false>(device, a, p.threads, p.shared, s); \
             if (ring_takes(a.c, V, sizeof(T))) return launch_runs<T, V, kAct, kCodes, true>(device, a, s); \
         } \
         return launch_runs<T, V, kAct, kCodes, false>(device, a, s); \
@@ -650,8 +684,8 @@ GroupPlan tc_plan_group_norm(const GroupNormArgs &m, int sm_count)
     a.groups = m.groups;
     auto bytes = [&](int shares) { return shared_bytes(a, (m.hw + shares - 1) / shares, element, p.vector, p.threads); };
     if (p.vector * element == 16) {
-        // On chip where a block has a map of some size, or for a map or two.  (Others read x a second time from L2, which costs less than waiting for clusters: 256x14x14 bf16 x 1, 8, 30: 7.3,
-        // 9.1 and 13.1 us on chip, 7.9, 7.5 and 9.3 by runs; 832x19x19 x 2: 10.6 both; without clusters, 256x14x14 x 290: 22 and 26, 64x7x7 x 290: 11.2 and 9.5.)
+        // On chip where a block has a map of some size, or for a map or two.  (Others read x a second time from L2, which costs less than waiting for clusters: 256x14x14 bf16 x 1, 2, 8, 30: 6.8,
+        // 6.9, 8.7 and 12.8 us on chip, 7.2, 7.1, 7.1 and 10.0 by runs; 832x19x19 x 2: 10.2 and 9.5; without clusters, 256x14x14 x 290: 22 and 26, 64x7x7 x 290: 9.4 and 8.4.)
         const int shares = shares_on_chip(m.n, m.hw, 2, sm_count, bytes);
         if (shares && (m.n <= 2 || (shares == 1 && (long long)m.hw * m.c * element >= kWorthKeeping))) {
             p.shares = shares;

@@ -431,8 +431,8 @@ struct GroupPlan {
 constexpr long long kRunBytes = 192 * 1024, kRunLeast = 8 * 1024, kRunMost = 512 * 1024, kRunCost = 32 * 1024;
 constexpr int kMostRounds = 128;                // of a block's rows over a run's pixels
 constexpr long long kWorthKeeping = 64 * 1024;  // bytes of a map
-// Runs of a map whose sums every run's block joins; more are joined by a kernel (4 maps of 256x128x128 bf16, 111 runs: 30 us with it, 40 without; 12 of 256x64x64 f32, 37 runs: 32 and 35; 42 of
-// 114x28x28, few runs: 13.8 and 12.9).
+// Runs of a map whose sums every run's block joins; more are joined by a kernel (4 maps of 256x128x128 bf16, 111 runs: 30 us with it, 40 without; 12 of 256x64x64 f32, 37 runs: 33 and 36; 42 of
+// 114x28x28, few runs: 13.9 and 12.9).
 constexpr int kInlineRuns = 32;
 int tc_group_threads(int columns);
 GroupPlan tc_plan_group_norm(const GroupNormArgs &a, int sm_count);

@@ -20,7 +20,9 @@ def ctx():
 
 # On chip, one block and a cluster; runs through a ring, few and many of them; without one: rows not at 16 bytes, two channels a lane and one, more vectors than threads
 SHAPES = [((1, 256, 14, 14), 32), ((2, 64, 40, 40), 64), ((3, 8, 100, 100), 1), ((300, 16, 56, 56), 4), ((40, 256, 28, 28), 256), ((1, 24, 700, 700), 3), ((40, 8, 128, 128), 8), ((3, 30, 60, 61), 3), ((200, 33, 56, 57), 33),
-          ((60, 3, 200, 200), 1), ((2, 2056, 20, 21), 257), ((3, 4, 1, 3), 2)]
+          ((60, 3, 200, 200), 1), ((2, 2056, 20, 21), 257), ((3, 4, 1, 3), 2),
+          # blocks of a few dozen pixels
+          ((290, 64, 7, 7), 64), ((30, 256, 14, 14), 256), ((100, 512, 5, 6), 512), ((1, 2048, 5, 5), 32), ((2, 33, 9, 9), 33)]
 
 
 def _far(x, where, far):
