@@ -5,7 +5,7 @@
 // Bound by the bytes moved, x once and y once.  A map or two, and maps that a block holds, are read once: each of a cluster's blocks (up to sixteen)
 // takes its pixels to shared memory by bulk copies, finds its moments, they are put together through the cluster's shared memory, and the values leave from where
 // they lie.  Others take two kernels: moments of runs of pixels, and the values, the pixels through a ring in shared memory where their rows begin at 16 bytes.
-// 256x56x56 x 128 bf16: 107 us, 5.8 TB/s with the second reading of x; one map of 256x14x14: 6.7 us.
+// 256x56x56 x 128 bf16: 105 us, 5.9 TB/s with the second reading of x; one map of 256x14x14: 6.7 us.
 //
 // Moments are put together as (n, mean, M2): no sum of squares is taken about a mean far from its own.
 #include "group_norm.cuh"

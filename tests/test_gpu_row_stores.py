@@ -20,7 +20,7 @@ def ctx():
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("rest", [8, 32, 40, 64, 96, 128, 136, 160, 192, 224])
+@pytest.mark.parametrize("rest", [4, 8, 32, 36, 40, 64, 96, 128, 132, 136, 160, 192, 224])
 def test_products_of_short_sums(ctx, rest, dtype):
     for n, k, o in ((25088, 320, 768 + rest), (8200, 512, 1024 + rest), (20010, 64, 256 + rest)):
         a, b = _operand(n, k, 1), _operand(o, k, 2)
